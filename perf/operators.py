@@ -209,7 +209,8 @@ def _norm_bwd_plain(s):
 
 
 def _ce_rows(z, s):
-    """-> per-token log-prob and lse (NaN where the mask is 0), the four loss means, dL/dz or None."""
+    """-> per-token log-prob and lse (NaN where the mask is 0), the four loss means (total, negative
+    log-prob, smoothing term, lse^2; the third is 0 without smoothing), dL/dz or None."""
     case = s["case"]
     eps, zc, V = case["smoothing"], case["z_coef"], case["V"]
     live = s["mask"] != 0
@@ -220,7 +221,7 @@ def _ce_rows(z, s):
     S = e.sum(dim=1, keepdim=True)
     lse = m + torch.log(S)
     logp = (z.gather(1, y) - m) - torch.log(S)
-    smooth = lse - z.mean(dim=1, keepdim=True)
+    smooth = lse - z.mean(dim=1, keepdim=True) if eps else torch.zeros_like(lse)
     nan = torch.full_like(lse, float("nan"))
     terms = torch.cat([(1.0 - eps) * -logp + eps * smooth + zc * lse * lse, -logp, smooth, lse * lse], dim=1)
     loss = torch.where(live[:, None], terms, torch.zeros_like(terms)).double().sum(dim=0) / n
@@ -392,8 +393,8 @@ def exact(case, seed):
         at = torch.arange(r.numel(), device=DEV)
         l = torch.logsumexp(z, dim=1)
         logp[r], lse[r] = lp[at, y], l
-        smooth = -lp.mean(dim=1)
         nll = -lp[at, y]
+        smooth = -lp.mean(dim=1) if eps else 0.0 * nll
         sums += torch.stack([((1 - eps) * nll + eps * smooth + zc * l * l).sum(), nll.sum(), smooth.sum(), (l * l).sum()])
         if want:
             target = torch.full_like(z, eps / V)
