@@ -73,6 +73,7 @@ typedef enum { RLF_BF16 = 0, RLF_F32 = 1 } rlf_dtype;
 #define RLF_FN_FUSED_LMHEAD 4
 #define RLF_FN_LOGP_ENTROPY 5
 #define RLF_FN_FUSED_LOGP_ENTROPY 6
+#define RLF_FN_NORM_BWD 7
 
 typedef struct CUstream_st *rlf_stream_t;
 
@@ -390,6 +391,56 @@ rlf_status rlf_fused_lmhead_logp_entropy(const void *hidden, const void *W, int6
                                          const int32_t *ids, float *logp_out, float *entropy_out,
                                          void *workspace, size_t workspace_bytes, int32_t *dev_status,
                                          rlf_stream_t stream);
+
+/*
+ * The norm between the model's last block and the LM head (paper Sec. 2.2: pi_theta is the language
+ * model; the paper prints no layer of it, these are the two usual norms).  Per row:
+ *     h = x + residual (residual may be NULL: h = x)
+ *     RLF_NORM_LAYER: mu = mean(h), r = 1 / sqrt(mean((h - mu)^2) + eps)
+ *     RLF_NORM_RMS:   mu = 0,       r = 1 / sqrt(mean(h^2) + eps)
+ *     y = (h - mu) r weight + bias
+ * Statistics are fp32; y is formed from the unrounded h and rounded once.
+ *
+ *   x, residual  [T, D] dt, row r starts at element r * x_stride (x_stride >= D; both have this stride)
+ *   weight [D], bias [D] or NULL: w_dt, a type of their own
+ *   eps          > 0 (else RLF_ERR_UNSUPPORTED)
+ *   sum_out      [T, D] dt dense, or NULL: h rounded to dt (the residual stream; what rlf_norm_bwd takes as x)
+ *   y_out        [T, D] dt dense
+ *   mean_out     [T] fp32 or NULL (zeros for the RMS form);  rstd_out [T] fp32 or NULL: r
+ * Outputs may not overlap inputs or each other, except that sum_out may be x or residual itself, and
+ * y_out may be x or residual itself, when that input is dense (x_stride = D).
+ * Non-finite inputs give what the formulas give, in their own row only.  T = 0 is valid.
+ */
+#define RLF_NORM_RMS 0
+#define RLF_NORM_LAYER 1
+rlf_status rlf_norm_fwd(const void *x, const void *residual, rlf_dtype dt, int64_t T, int32_t D,
+                        int64_t x_stride, const void *weight, const void *bias, rlf_dtype w_dt,
+                        int kind, float eps, void *sum_out, void *y_out, float *mean_out,
+                        float *rstd_out, rlf_stream_t stream);
+
+/*
+ * Backward of rlf_norm_fwd.  With xh = (x - mean) rstd and g = grad_y * weight, per row
+ *     grad_x      = rstd (g - mean(g) [layer form only] - xh mean(g xh)) + grad_skip
+ * and over all rows
+ *     grad_weight = sum_t grad_y xh,   grad_bias = sum_t grad_y
+ * Sums are fp32 in a fixed order (results are run-to-run identical).
+ *
+ *   grad_y     [T, D] dt with row stride grad_y_stride (e.g. the grad_hidden of a fused LM-head call)
+ *   x          [T, D] dt with row stride x_stride: what was normalised (x, or sum_out with a residual)
+ *   mean       [T] fp32 from the forward call (not read for the RMS form, may be NULL there);  rstd [T] fp32
+ *   grad_skip  [T, D] dt dense, or NULL: gradient that reaches the residual stream by another path
+ *   grad_x     [T, D] dt dense, or NULL; it is the gradient of x and of residual alike.  May be grad_y,
+ *              x (when dense) or grad_skip itself
+ *   grad_weight, grad_bias  [D] fp32 or NULL each; added to the buffers if accumulate != 0
+ *   workspace  rlf_workspace_bytes(RLF_FN_NORM_BWD, T, 0, D, dt) bytes, 256-byte aligned; may be NULL
+ *              when neither weight gradient is wanted.  Contents need not be initialised.
+ * T = 0 is valid (weight gradients are then zero, or unchanged with accumulate).
+ */
+rlf_status rlf_norm_bwd(const void *grad_y, int64_t grad_y_stride, const void *x, int64_t x_stride,
+                        rlf_dtype dt, int64_t T, int32_t D, const void *weight, rlf_dtype w_dt,
+                        int kind, const float *mean, const float *rstd, const void *grad_skip,
+                        void *grad_x, float *grad_weight, float *grad_bias, int accumulate,
+                        void *workspace, size_t workspace_bytes, rlf_stream_t stream);
 
 /* Bytes of workspace the given entry point needs for these sizes (0 for unknown selectors). */
 size_t rlf_workspace_bytes(int which_fn, int64_t T, int32_t V, int32_t D, rlf_dtype dt);

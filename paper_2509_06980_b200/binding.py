@@ -14,12 +14,12 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "librlf.so")
 
 RLF_BF16, RLF_F32 = 0, 1
-FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY = 3, 4, 5, 6
+FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY, FN_NORM_BWD = 3, 4, 5, 6, 7
 DEV_BAD_TARGET, DEV_BAD_SEQ, DEV_NONFINITE, DEV_TIMEOUT = 1, 2, 4, 8
 
 EXPORTS = [
     "rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward", "rlf_grpo_logp_loss_fwd_bwd",
-    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
+    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
     "rlf_tune_logits_kernel", "rlf_tune_logits_grid", "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing", "rlf_launch_count", "rlf_status_string", "rlf_version",
 ]
 
@@ -68,11 +68,14 @@ _lib.rlf_logp_entropy_fwd.argtypes = [_vp, _int, _i64, _i32, _i64, _vp, _vp, _vp
 _lib.rlf_fused_lmhead_grpo_obj.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _f32, _f32,
                                            _f32, _int, _int, _vp, _vp, _vp, _vp, _vp, _int, _vp, _sz, _vp, _vp]
 _lib.rlf_fused_lmhead_logp_entropy.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
+_lib.rlf_norm_fwd.argtypes = [_vp, _vp, _int, _i64, _i32, _i64, _vp, _vp, _int, _int, _f32, _vp, _vp, _vp, _vp, _vp]
+_lib.rlf_norm_bwd.argtypes = [_vp, _i64, _vp, _i64, _int, _i64, _i32, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp,
+                              _int, _vp, _sz, _vp]
 # every entry point that returns an rlf_status
 for _n in ("rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward",
            "rlf_grpo_logp_loss_fwd_bwd", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_grpo_logp_loss_fwd_bwd_skip_masked",
            "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj",
-           "rlf_fused_lmhead_logp_entropy", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
+           "rlf_fused_lmhead_logp_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
            "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing"):
     getattr(_lib, _n).restype = _int
 
@@ -106,12 +109,12 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
-def _dt(t):
+def _dt(t, what="logits"):
     if t.dtype == torch.bfloat16:
         return RLF_BF16
     if t.dtype == torch.float32:
         return RLF_F32
-    raise TypeError("logits must be bfloat16 or float32")
+    raise TypeError("%s must be bfloat16 or float32" % what)
 
 
 def version():
@@ -440,6 +443,101 @@ def rlf_fused_lmhead_logp_entropy(hidden, W, ids, want_entropy=True, logp_out=No
         _ptr(logp_out, torch.float32), _ptr(entropy_out, torch.float32), workspace.data_ptr(), workspace.numel(),
         _ptr(dev_status, torch.int32), _stream()), "rlf_fused_lmhead_logp_entropy")
     return logp_out, entropy_out
+
+
+NORM_RMS, NORM_LAYER = 0, 1
+
+
+def _rows(t, what):
+    """Base address and row stride of a [T, D] tensor whose rows may be strided (last dimension dense)."""
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be 2-dimensional with a contiguous last dimension" % what)
+    T, D = t.shape
+    return (t.data_ptr() if T > 0 else None), (t.stride(0) if T > 1 else D)
+
+
+def _like(t, shape, dtype, what):
+    if t is not None and (t.shape != shape or t.dtype != dtype):
+        raise ValueError("%s must be a %s tensor of shape %s" % (what, dtype, tuple(shape)))
+    return t
+
+
+def _one_device(*tensors):
+    """The kernels run on the current device and stream; a tensor of another device is refused."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != here:
+            raise ValueError("a tensor is on cuda:%s, the current device is cuda:%d" % (t.device.index, here))
+
+
+def rlf_norm_fwd(x, weight, bias=None, residual=None, kind=NORM_RMS, eps=1e-6, y_out=None, sum_out=None,
+                 mean_out=None, rstd_out=None):
+    """Layer norm (NORM_LAYER) or its RMS form (NORM_RMS) of the rows of x (+ residual).
+    x, residual: [T, D] (rows may be strided, the same stride); weight, bias: [D], bf16 or fp32.
+    -> (y [T, D], x + residual [T, D] | None without residual, mean fp32[T] | None for the RMS form, rstd fp32[T])."""
+    xp, xs = _rows(x, "x")
+    T, D = x.shape
+    dev, dt = x.device, x.dtype
+    _one_device(x, weight, bias, residual, y_out, sum_out, mean_out, rstd_out)
+    rp = None
+    if residual is not None:
+        _like(residual, x.shape, dt, "residual")
+        rp, rs = _rows(residual, "residual")
+        if T > 1 and rs != xs:
+            raise ValueError("residual must have the row stride of x")
+    _like(weight, (D,), weight.dtype, "weight")
+    _like(bias, (D,), weight.dtype, "bias")
+    if y_out is None:
+        y_out = torch.empty((T, D), dtype=dt, device=dev)
+    if sum_out is None and residual is not None:
+        sum_out = torch.empty((T, D), dtype=dt, device=dev)
+    if mean_out is None and kind == NORM_LAYER:
+        mean_out = torch.empty(T, dtype=torch.float32, device=dev)
+    if rstd_out is None:
+        rstd_out = torch.empty(T, dtype=torch.float32, device=dev)
+    _like(y_out, x.shape, dt, "y_out")
+    _like(sum_out, x.shape, dt, "sum_out")
+    _like(mean_out, (T,), torch.float32, "mean_out")
+    _like(rstd_out, (T,), torch.float32, "rstd_out")
+    _check(_lib.rlf_norm_fwd(xp, rp, _dt(x, "x"), T, D, xs, _ptr(weight), _ptr(bias), _dt(weight, "weight"), int(kind), float(eps),
+                             _ptr(sum_out), _ptr(y_out), _ptr(mean_out), _ptr(rstd_out), _stream()), "rlf_norm_fwd")
+    return y_out, sum_out, mean_out, rstd_out
+
+
+def rlf_norm_bwd(grad_y, x, weight, mean, rstd, kind=NORM_RMS, grad_skip=None, want_grad_x=True, want_grad_weight=True,
+                 want_grad_bias=False, grad_x=None, grad_weight=None, grad_bias=None, accumulate=False, workspace=None):
+    """Backward of rlf_norm_fwd; x is what was normalised (the sum, with a residual); grad_skip is added to grad_x.
+    -> (grad_x [T, D] | None, grad_weight fp32[D] | None, grad_bias fp32[D] | None)."""
+    xp, xs = _rows(x, "x")
+    T, D = x.shape
+    dev, dt = x.device, x.dtype
+    _one_device(x, grad_y, weight, mean, rstd, grad_skip, grad_x, grad_weight, grad_bias, workspace)
+    _like(grad_y, x.shape, dt, "grad_y")
+    gp, gs = _rows(grad_y, "grad_y")
+    _like(weight, (D,), weight.dtype, "weight")
+    if accumulate and ((grad_weight is None and want_grad_weight) or (grad_bias is None and want_grad_bias)):
+        raise ValueError("accumulate needs the buffers that are added to")
+    if grad_x is None and want_grad_x:
+        grad_x = torch.empty((T, D), dtype=dt, device=dev)
+    if grad_weight is None and want_grad_weight:
+        grad_weight = torch.empty(D, dtype=torch.float32, device=dev)
+    if grad_bias is None and want_grad_bias:
+        grad_bias = torch.empty(D, dtype=torch.float32, device=dev)
+    _like(grad_x, x.shape, dt, "grad_x")
+    _like(grad_skip, x.shape, dt, "grad_skip")
+    _like(grad_weight, (D,), torch.float32, "grad_weight")
+    _like(grad_bias, (D,), torch.float32, "grad_bias")
+    _like(mean, (T,), torch.float32, "mean")
+    _like(rstd, (T,), torch.float32, "rstd")
+    if workspace is None and (grad_weight is not None or grad_bias is not None):
+        workspace = new_workspace(FN_NORM_BWD, T, 0, D, RLF_F32, dev)
+    _check(_lib.rlf_norm_bwd(gp, gs, xp, xs, _dt(x, "x"), T, D, _ptr(weight), _dt(weight, "weight"), int(kind), _ptr(mean), _ptr(rstd),
+                             _ptr(grad_skip), _ptr(grad_x), _ptr(grad_weight), _ptr(grad_bias), 1 if accumulate else 0,
+                             None if workspace is None else workspace.data_ptr(),
+                             0 if workspace is None else workspace.numel(), _stream()), "rlf_norm_bwd")
+    return grad_x, grad_weight, grad_bias
 
 
 def step_arena_bytes(T, V, B, dt=RLF_BF16):

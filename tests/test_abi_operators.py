@@ -1,0 +1,52 @@
+"""Host-side refusals of the cross-entropy and norm entry points: every case fails validation before a device
+is touched (no compute without a GPU)."""
+import ctypes
+
+import pytest
+
+vp, i32, i64, f32, sz, ci = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t, ctypes.c_int)
+FAKE = 4096          # never dereferenced
+NULL, SHAPE, ALIGN, DTYPE, WORKSPACE, UNSUPPORTED = -1, -2, -3, -4, -5, -8
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2509_06980_b200 import build
+    return ctypes.CDLL(build.build())
+
+
+def test_norm_forward_refuses(lib):
+    f = lib.rlf_norm_fwd
+    f.argtypes = [vp, vp, ci, i64, i32, i64, vp, vp, ci, ci, f32, vp, vp, vp, vp, vp]
+
+    def call(x=FAKE, res=None, dt=0, T=4, D=64, stride=64, w=FAKE, b=None, w_dt=0, kind=0, eps=1e-6, s=None, y=FAKE,
+             mean=None, rstd=None):
+        return f(x, res, dt, T, D, stride, w, b, w_dt, kind, eps, s, y, mean, rstd, None)
+
+    assert call(dt=2) == DTYPE and call(w_dt=-1) == DTYPE
+    assert call(T=-1) == SHAPE and call(D=0) == SHAPE and call(stride=63) == SHAPE
+    assert call(kind=2) == UNSUPPORTED
+    for eps in (0.0, -1.0, float("nan"), float("inf")):
+        assert call(eps=eps) == UNSUPPORTED
+    assert call(x=None) == NULL and call(w=None) == NULL and call(y=None) == NULL
+    assert call(x=4097) == ALIGN and call(dt=1, x=4098) == ALIGN and call(res=4097) == ALIGN and call(w_dt=1, w=4098) == ALIGN
+    assert call(mean=4098) == ALIGN and call(rstd=4098) == ALIGN and call(b=4097) == ALIGN and call(s=4097) == ALIGN
+    assert call(T=0, x=None, w=None, y=None) == 0
+
+
+def test_norm_backward_refuses(lib):
+    f = lib.rlf_norm_bwd
+    f.argtypes = [vp, i64, vp, i64, ci, i64, i32, vp, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp, sz, vp]
+
+    def call(dy=FAKE, dys=64, x=FAKE, xs=64, dt=0, T=4, D=64, w=FAKE, w_dt=0, kind=0, mean=None, rstd=FAKE, skip=None,
+             gx=FAKE, gw=FAKE, gb=None, ws=FAKE, wsb=1 << 30):
+        return f(dy, dys, x, xs, dt, T, D, w, w_dt, kind, mean, rstd, skip, gx, gw, gb, 0, ws, wsb, None)
+
+    assert call(dt=3) == DTYPE and call(w_dt=9) == DTYPE and call(kind=-1) == UNSUPPORTED
+    assert call(T=-1) == SHAPE and call(D=0) == SHAPE and call(dys=1) == SHAPE and call(xs=1) == SHAPE
+    assert call(dy=None) == NULL and call(x=None) == NULL and call(w=None) == NULL and call(rstd=None) == NULL
+    assert call(kind=1, mean=None) == NULL
+    assert call(dy=4097) == ALIGN and call(skip=4097) == ALIGN and call(gx=4097) == ALIGN and call(gw=4098) == ALIGN
+    assert call(rstd=4098) == ALIGN
+    assert call(ws=None) == WORKSPACE and call(ws=4100) == WORKSPACE and call(wsb=64) == WORKSPACE
+    assert call(gw=None, gb=FAKE, ws=None) == WORKSPACE
