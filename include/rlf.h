@@ -74,6 +74,7 @@ typedef enum { RLF_BF16 = 0, RLF_F32 = 1 } rlf_dtype;
 #define RLF_FN_LOGP_ENTROPY 5
 #define RLF_FN_FUSED_LOGP_ENTROPY 6
 #define RLF_FN_NORM_BWD 7
+#define RLF_FN_CROSS_ENTROPY 8
 
 typedef struct CUstream_st *rlf_stream_t;
 
@@ -391,6 +392,40 @@ rlf_status rlf_fused_lmhead_logp_entropy(const void *hidden, const void *W, int6
                                          const int32_t *ids, float *logp_out, float *entropy_out,
                                          void *workspace, size_t workspace_bytes, int32_t *dev_status,
                                          rlf_stream_t stream);
+
+/*
+ * Softmax cross entropy over materialised logits, forward and backward: the supervised stage that
+ * precedes the RL update (fine-tuning on tool-use trajectories) and its validation loss.  (Paper Sec.
+ * 2.2: the policy pi_theta(a | s_t); Sec. 2.3.2: a loss mask excludes tool results.  The formulas are
+ * the textbook ones.)  Per row t with mask[t] != 0 and y = ids[t]:
+ *     lse = log sum_v exp z[t,v];   logp = z[t,y] - lse;   smooth = lse - mean_v z[t,v]
+ *     l   = (1 - eps) (-logp) + eps smooth + zeta lse^2       eps = label_smoothing, zeta = z_coef
+ *     N   = *denom if denom != NULL else the number of rows with mask != 0;   Nd = max(N, 1)
+ *     loss_out = { sum l, sum -logp, sum smooth, sum lse^2 } / Nd     (the third is 0 when eps = 0)
+ *     grad_logits[t,v] = (1/Nd) ((1 + 2 zeta lse) softmax(z[t,:])[v] - eps/V - (1 - eps) 1[v = y])
+ * Rows with mask 0 are not read (their target id is not looked at either): log-prob and lse NaN, gradient
+ * zeros.  So are rows whose target lies outside [0, V) (RLF_DEV_BAD_TARGET) or whose lse, log-prob or
+ * (with smoothing) mean logit is not finite (RLF_DEV_NONFINITE); those still count in N.
+ * Logits of -inf are zero probability; with smoothing they make the mean logit, and so the row, non-finite.
+ * Sums are fp32 within a row and fp64 in a fixed order over the rows (results are run-to-run identical).
+ *
+ *   logits       [T, V] dt, row r starts at element r * row_stride (row_stride >= V); any V, stride and
+ *                element-aligned base
+ *   ids          [T] int32;  mask [T] uint8 or NULL (every row counts)
+ *   label_smoothing in [0, 1], z_coef >= 0 and finite (else RLF_ERR_UNSUPPORTED)
+ *   denom        [1] int64 on the device, or NULL; the global count when a batch is split over calls
+ *   logp_out     [T] fp32;  lse_out [T] fp32 or NULL;  loss_out [4] fp64
+ *   grad_logits  [T, V] dt with the same row_stride, or NULL (forward only); may be logits itself
+ *   workspace    rlf_workspace_bytes(RLF_FN_CROSS_ENTROPY, T, V, 0, dt) bytes, 256-byte aligned; contents
+ *                need not be initialised
+ * T = 0 is valid (loss_out = 0).  T beyond 2^31 - 1 returns RLF_ERR_UNSUPPORTED.
+ */
+rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T, int32_t V,
+                                     int64_t row_stride, const int32_t *ids, const uint8_t *mask,
+                                     float label_smoothing, float z_coef, const int64_t *denom,
+                                     float *logp_out, float *lse_out, double *loss_out,
+                                     void *grad_logits, void *workspace, size_t workspace_bytes,
+                                     int32_t *dev_status, rlf_stream_t stream);
 
 /*
  * The norm between the model's last block and the LM head (paper Sec. 2.2: pi_theta is the language

@@ -14,12 +14,12 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "librlf.so")
 
 RLF_BF16, RLF_F32 = 0, 1
-FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY, FN_NORM_BWD = 3, 4, 5, 6, 7
+FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY, FN_NORM_BWD, FN_CROSS_ENTROPY = 3, 4, 5, 6, 7, 8
 DEV_BAD_TARGET, DEV_BAD_SEQ, DEV_NONFINITE, DEV_TIMEOUT = 1, 2, 4, 8
 
 EXPORTS = [
     "rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward", "rlf_grpo_logp_loss_fwd_bwd",
-    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
+    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
     "rlf_tune_logits_kernel", "rlf_tune_logits_grid", "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing", "rlf_launch_count", "rlf_status_string", "rlf_version",
 ]
 
@@ -68,6 +68,8 @@ _lib.rlf_logp_entropy_fwd.argtypes = [_vp, _int, _i64, _i32, _i64, _vp, _vp, _vp
 _lib.rlf_fused_lmhead_grpo_obj.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _f32, _f32,
                                            _f32, _int, _int, _vp, _vp, _vp, _vp, _vp, _int, _vp, _sz, _vp, _vp]
 _lib.rlf_fused_lmhead_logp_entropy.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
+_lib.rlf_cross_entropy_fwd_bwd.argtypes = [_vp, _int, _i64, _i32, _i64, _vp, _vp, _f32, _f32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                           _sz, _vp, _vp]
 _lib.rlf_norm_fwd.argtypes = [_vp, _vp, _int, _i64, _i32, _i64, _vp, _vp, _int, _int, _f32, _vp, _vp, _vp, _vp, _vp]
 _lib.rlf_norm_bwd.argtypes = [_vp, _i64, _vp, _i64, _int, _i64, _i32, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp,
                               _int, _vp, _sz, _vp]
@@ -75,7 +77,7 @@ _lib.rlf_norm_bwd.argtypes = [_vp, _i64, _vp, _i64, _int, _i64, _i32, _vp, _int,
 for _n in ("rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward",
            "rlf_grpo_logp_loss_fwd_bwd", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_grpo_logp_loss_fwd_bwd_skip_masked",
            "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj",
-           "rlf_fused_lmhead_logp_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
+           "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
            "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing"):
     getattr(_lib, _n).restype = _int
 
@@ -470,6 +472,43 @@ def _one_device(*tensors):
     for t in tensors:
         if t is not None and t.is_cuda and t.device.index != here:
             raise ValueError("a tensor is on cuda:%s, the current device is cuda:%d" % (t.device.index, here))
+
+
+def rlf_cross_entropy_fwd_bwd(logits, ids, mask=None, label_smoothing=0.0, z_coef=0.0, denom=None, grad_logits=None,
+                              want_grad=True, in_place=False, logp_out=None, lse_out=None, want_lse=True, loss_out=None,
+                              workspace=None, dev_status=None):
+    """Softmax cross entropy of the rows of logits [T, V] (rows may be strided) at targets ids, masked mean.
+    -> (logp fp32[T], lse fp32[T] | None, loss fp64[4], grad_logits | None), all on the device."""
+    zp, stride = _rows(logits, "logits")
+    T, V = logits.shape
+    dev = logits.device
+    _one_device(logits, ids, mask, denom, grad_logits, logp_out, lse_out, loss_out, workspace, dev_status)
+    if grad_logits is None and want_grad:
+        grad_logits = logits if in_place else torch.empty_strided((T, V), (stride, 1), dtype=logits.dtype, device=dev)
+    gp = None
+    if grad_logits is not None:
+        _like(grad_logits, logits.shape, logits.dtype, "grad_logits")
+        gp, gs = _rows(grad_logits, "grad_logits")
+        if T > 1 and gs != stride:
+            raise ValueError("grad_logits must have the row stride of logits")
+    if logp_out is None:
+        logp_out = torch.empty(T, dtype=torch.float32, device=dev)
+    if lse_out is None and want_lse:
+        lse_out = torch.empty(T, dtype=torch.float32, device=dev)
+    if loss_out is None:
+        loss_out = torch.empty(4, dtype=torch.float64, device=dev)
+    _like(ids, (T,), torch.int32, "ids")
+    _like(mask, (T,), torch.uint8, "mask")
+    _like(logp_out, (T,), torch.float32, "logp_out")
+    _like(lse_out, (T,), torch.float32, "lse_out")
+    _like(loss_out, (4,), torch.float64, "loss_out")
+    if workspace is None:
+        workspace = new_workspace(FN_CROSS_ENTROPY, T, V, 0, RLF_BF16, dev)
+    _check(_lib.rlf_cross_entropy_fwd_bwd(
+        zp, _dt(logits), T, V, stride, _ptr(ids), _ptr(mask), float(label_smoothing), float(z_coef),
+        _ptr(denom, torch.int64), _ptr(logp_out), _ptr(lse_out), _ptr(loss_out), gp, workspace.data_ptr(),
+        workspace.numel(), _ptr(dev_status, torch.int32), _stream()), "rlf_cross_entropy_fwd_bwd")
+    return logp_out, lse_out, loss_out, grad_logits
 
 
 def rlf_norm_fwd(x, weight, bias=None, residual=None, kind=NORM_RMS, eps=1e-6, y_out=None, sum_out=None,

@@ -6,7 +6,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librlf.so")
-SOURCES = ["mask.cu", "advantage.cu", "logits_loss.cu", "lmhead.cu", "norm.cu", "api.cu"]
+SOURCES = ["mask.cu", "advantage.cu", "logits_loss.cu", "lmhead.cu", "cross_entropy.cu", "norm.cu", "api.cu"]
 HEADERS = [os.path.join(CSRC, "common.cuh"), os.path.join(HERE, "..", "include", "rlf.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]

@@ -31,6 +31,13 @@ rlf_status launch_seq_weights(const void* rec, const int32_t* seq_id, int64_t T,
                               const long long* denom_or_null, int* cnt, long long* s_slot, float* wtok,
                               cudaStream_t s);
 
+// cross-entropy stages (cross_entropy.cu), also used by the fused LM-head form: count of rows with loss
+// weight, the loss scalars from per-token terms {-logp, smooth, lse, counts} (float4), argument check
+rlf_status ce_launch_count(const uint8_t* mask, int64_t T, long long* count, cudaStream_t s);
+rlf_status ce_launch_loss(const void* terms, int64_t T, const long long* denom, float eps, float zeta, double* loss_out,
+                          cudaStream_t s);
+rlf_status ce_check_objective(float label_smoothing, float z_coef);
+
 inline rlf_status cuda_ok(cudaError_t e) { return e == cudaSuccess ? RLF_OK : RLF_ERR_CUDA; }
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }

@@ -50,3 +50,24 @@ def test_norm_backward_refuses(lib):
     assert call(rstd=4098) == ALIGN
     assert call(ws=None) == WORKSPACE and call(ws=4100) == WORKSPACE and call(wsb=64) == WORKSPACE
     assert call(gw=None, gb=FAKE, ws=None) == WORKSPACE
+
+
+def test_cross_entropy_refuses(lib):
+    f = lib.rlf_cross_entropy_fwd_bwd
+    f.argtypes = [vp, ci, i64, i32, i64, vp, vp, f32, f32, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+
+    def call(z=FAKE, dt=0, T=4, V=64, stride=64, ids=FAKE, mask=FAKE, eps=0.0, zc=0.0, denom=None, logp=FAKE, lse=None,
+             loss=FAKE, grad=None, ws=FAKE, wsb=1 << 20):
+        return f(z, dt, T, V, stride, ids, mask, eps, zc, denom, logp, lse, loss, grad, ws, wsb, None, None)
+
+    assert call(dt=2) == DTYPE
+    assert call(T=-1) == SHAPE and call(V=0) == SHAPE and call(stride=63) == SHAPE
+    for eps in (-0.1, 1.1, float("nan")):
+        assert call(eps=eps) == UNSUPPORTED
+    for zc in (-1e-9, float("inf"), float("nan")):
+        assert call(zc=zc) == UNSUPPORTED
+    assert call(T=1 << 31, wsb=1 << 62) == UNSUPPORTED
+    assert call(z=None) == NULL and call(ids=None) == NULL and call(logp=None) == NULL and call(loss=None) == NULL
+    assert call(z=4097) == ALIGN and call(dt=1, z=4098) == ALIGN and call(grad=4097) == ALIGN and call(loss=4100) == ALIGN
+    assert call(denom=4100) == ALIGN and call(lse=4098) == ALIGN
+    assert call(ws=None) == WORKSPACE and call(ws=4100) == WORKSPACE and call(wsb=256) == WORKSPACE
