@@ -75,6 +75,7 @@ typedef enum { RLF_BF16 = 0, RLF_F32 = 1 } rlf_dtype;
 #define RLF_FN_FUSED_LOGP_ENTROPY 6
 #define RLF_FN_NORM_BWD 7
 #define RLF_FN_CROSS_ENTROPY 8
+#define RLF_FN_FUSED_CROSS_ENTROPY 9
 
 typedef struct CUstream_st *rlf_stream_t;
 
@@ -426,6 +427,34 @@ rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T
                                      float *logp_out, float *lse_out, double *loss_out,
                                      void *grad_logits, void *workspace, size_t workspace_bytes,
                                      int32_t *dev_status, rlf_stream_t stream);
+
+/*
+ * rlf_cross_entropy_fwd_bwd with the logits formed on the fly, z = hidden W^T, so that they never reach
+ * HBM (the supervised counterpart of rlf_fused_lmhead_grpo; paper Sec. 2.2).  Loss, statistics and the
+ * treatment of rows without loss weight, of bad targets and of non-finite rows are those of
+ * rlf_cross_entropy_fwd_bwd; rows without loss weight are not multiplied at all.  Gradients:
+ *     grad_hidden[t,:] = sum_v grad_z[t,v] W[v,:]       (bf16; zeros for rows without loss weight)
+ *     grad_W[v,:]      = sum_t grad_z[t,v] hidden[t,:]  (grad_W_dt: bf16, rounded once from the fp32 sum, or fp32)
+ * grad_z enters the two products as bf16; its uniform smoothing part stays outside them, in fp32.
+ *
+ *   hidden [T, D] bf16, W [V, D] bf16, both dense and 16-byte aligned; D a multiple of 64 and V a
+ *               multiple of 8 (else RLF_ERR_SHAPE)
+ *   ids, mask, label_smoothing, z_coef, denom, logp_out, lse_out, loss_out: as rlf_cross_entropy_fwd_bwd
+ *   grad_hidden [T, D] bf16 or NULL;  grad_W [V, D] or NULL (both NULL: forward only)
+ *   accumulate_grad_W  adds to an fp32 grad_W; with a bf16 grad_W it returns RLF_ERR_UNSUPPORTED
+ *   workspace   rlf_workspace_bytes(RLF_FN_FUSED_CROSS_ENTROPY, T, V, D, grad_W_dt) bytes, 256-byte aligned
+ *               (chiefly a bf16 scratch of min(T, 18944) rows by V; with a bf16 grad_W and T > 18944 also
+ *               an fp32 [V, D] sum); contents need not be initialised
+ * T = 0 is valid (loss_out = 0; grad_W zeros, or unchanged when accumulated).
+ */
+rlf_status rlf_fused_lmhead_cross_entropy(const void *hidden, const void *W, int64_t T, int32_t D,
+                                          int32_t V, const int32_t *ids, const uint8_t *mask,
+                                          float label_smoothing, float z_coef, const int64_t *denom,
+                                          float *logp_out, float *lse_out, double *loss_out,
+                                          void *grad_hidden, void *grad_W, rlf_dtype grad_W_dt,
+                                          int accumulate_grad_W, void *workspace,
+                                          size_t workspace_bytes, int32_t *dev_status,
+                                          rlf_stream_t stream);
 
 /*
  * The norm between the model's last block and the LM head (paper Sec. 2.2: pi_theta is the language

@@ -47,9 +47,11 @@ def cross_entropy(z, ids, mask=None, smoothing=0.0, z_coef=0.0, denom=None):
 def fused_cross_entropy(H, W, ids, mask=None, smoothing=0.0, z_coef=0.0, denom=None):
     """The same with z = H W^T.  -> the dict of cross_entropy plus grad_hidden [T, D], grad_W [V, D]"""
     H, W = np.asarray(H, np.float64), np.asarray(W, np.float64)
-    r = cross_entropy(H @ W.T, ids, mask, smoothing, z_coef, denom)
+    with np.errstate(invalid="ignore"):
+        r = cross_entropy(H @ W.T, ids, mask, smoothing, z_coef, denom)
     r["grad_hidden"] = r["grad"] @ W
-    r["grad_W"] = r["grad"].T @ H
+    on = r["live"]                      # a row that does not take part may hold anything
+    r["grad_W"] = r["grad"][on].T @ H[on]
     return r
 
 

@@ -14,12 +14,12 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "librlf.so")
 
 RLF_BF16, RLF_F32 = 0, 1
-FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY, FN_NORM_BWD, FN_CROSS_ENTROPY = 3, 4, 5, 6, 7, 8
+FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY, FN_NORM_BWD, FN_CROSS_ENTROPY, FN_FUSED_CROSS_ENTROPY = 3, 4, 5, 6, 7, 8, 9
 DEV_BAD_TARGET, DEV_BAD_SEQ, DEV_NONFINITE, DEV_TIMEOUT = 1, 2, 4, 8
 
 EXPORTS = [
     "rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward", "rlf_grpo_logp_loss_fwd_bwd",
-    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
+    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
     "rlf_tune_logits_kernel", "rlf_tune_logits_grid", "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing", "rlf_launch_count", "rlf_status_string", "rlf_version",
 ]
 
@@ -70,6 +70,8 @@ _lib.rlf_fused_lmhead_grpo_obj.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _vp,
 _lib.rlf_fused_lmhead_logp_entropy.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
 _lib.rlf_cross_entropy_fwd_bwd.argtypes = [_vp, _int, _i64, _i32, _i64, _vp, _vp, _f32, _f32, _vp, _vp, _vp, _vp, _vp, _vp,
                                            _sz, _vp, _vp]
+_lib.rlf_fused_lmhead_cross_entropy.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _f32, _f32, _vp, _vp, _vp, _vp, _vp,
+                                                _vp, _int, _int, _vp, _sz, _vp, _vp]
 _lib.rlf_norm_fwd.argtypes = [_vp, _vp, _int, _i64, _i32, _i64, _vp, _vp, _int, _int, _f32, _vp, _vp, _vp, _vp, _vp]
 _lib.rlf_norm_bwd.argtypes = [_vp, _i64, _vp, _i64, _int, _i64, _i32, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp,
                               _int, _vp, _sz, _vp]
@@ -77,7 +79,7 @@ _lib.rlf_norm_bwd.argtypes = [_vp, _i64, _vp, _i64, _int, _i64, _i32, _vp, _int,
 for _n in ("rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward",
            "rlf_grpo_logp_loss_fwd_bwd", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_grpo_logp_loss_fwd_bwd_skip_masked",
            "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj",
-           "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
+           "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
            "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing"):
     getattr(_lib, _n).restype = _int
 
@@ -509,6 +511,50 @@ def rlf_cross_entropy_fwd_bwd(logits, ids, mask=None, label_smoothing=0.0, z_coe
         _ptr(denom, torch.int64), _ptr(logp_out), _ptr(lse_out), _ptr(loss_out), gp, workspace.data_ptr(),
         workspace.numel(), _ptr(dev_status, torch.int32), _stream()), "rlf_cross_entropy_fwd_bwd")
     return logp_out, lse_out, loss_out, grad_logits
+
+
+def rlf_fused_lmhead_cross_entropy(hidden, W, ids, mask=None, label_smoothing=0.0, z_coef=0.0, denom=None,
+                                   want_grad_hidden=True, want_grad_W=True, grad_hidden=None, grad_W=None,
+                                   grad_W_dtype=torch.float32, accumulate_grad_W=False, logp_out=None, lse_out=None,
+                                   want_lse=True, loss_out=None, workspace=None, dev_status=None):
+    """rlf_cross_entropy_fwd_bwd of the logits hidden W^T, which are never stored.
+    -> (logp fp32[T], lse fp32[T] | None, loss fp64[4], grad_hidden bf16[T,D] | None, grad_W [V,D] | None);
+    grad_W is fp32 or (grad_W_dtype=torch.bfloat16) bf16."""
+    T, D = hidden.shape
+    V = W.shape[0]
+    dev = hidden.device
+    _one_device(hidden, W, ids, mask, denom, grad_hidden, grad_W, logp_out, lse_out, loss_out, workspace, dev_status)
+    if accumulate_grad_W and grad_W is None:
+        raise ValueError("accumulate_grad_W needs the buffer that is added to")
+    if grad_hidden is None and want_grad_hidden:
+        grad_hidden = torch.empty((T, D), dtype=torch.bfloat16, device=dev)
+    if grad_W is None and want_grad_W:
+        grad_W = torch.empty((V, D), dtype=grad_W_dtype, device=dev)
+    if logp_out is None:
+        logp_out = torch.empty(T, dtype=torch.float32, device=dev)
+    if lse_out is None and want_lse:
+        lse_out = torch.empty(T, dtype=torch.float32, device=dev)
+    if loss_out is None:
+        loss_out = torch.empty(4, dtype=torch.float64, device=dev)
+    _like(W, (V, D), torch.bfloat16, "W")
+    _like(ids, (T,), torch.int32, "ids")
+    _like(mask, (T,), torch.uint8, "mask")
+    _like(grad_hidden, (T, D), torch.bfloat16, "grad_hidden")
+    _like(logp_out, (T,), torch.float32, "logp_out")
+    _like(lse_out, (T,), torch.float32, "lse_out")
+    _like(loss_out, (4,), torch.float64, "loss_out")
+    w_dt = RLF_F32
+    if grad_W is not None:
+        _like(grad_W, (V, D), grad_W.dtype, "grad_W")
+        w_dt = _dt(grad_W, "grad_W")
+    if workspace is None:
+        workspace = new_workspace(FN_FUSED_CROSS_ENTROPY, T, V, D, w_dt, dev)
+    _check(_lib.rlf_fused_lmhead_cross_entropy(
+        _ptr(hidden, torch.bfloat16), _ptr(W), T, D, V, _ptr(ids), _ptr(mask), float(label_smoothing), float(z_coef),
+        _ptr(denom, torch.int64), _ptr(logp_out), _ptr(lse_out), _ptr(loss_out), _ptr(grad_hidden), _ptr(grad_W), w_dt,
+        1 if accumulate_grad_W else 0, workspace.data_ptr(), workspace.numel(), _ptr(dev_status, torch.int32),
+        _stream()), "rlf_fused_lmhead_cross_entropy")
+    return logp_out, lse_out, loss_out, grad_hidden, grad_W
 
 
 def rlf_norm_fwd(x, weight, bias=None, residual=None, kind=NORM_RMS, eps=1e-6, y_out=None, sum_out=None,

@@ -112,6 +112,11 @@ struct GemmParams {
     // each fetches its slabs from HBM on its own.  Waits are bounded and only delay loads: a worker
     // that gives up runs on unpaced.
     int* pace;
+    // Cross-entropy form (the CE instantiations only).  Label smoothing adds a rank-one term to either gradient:
+    const float* col_vec;     // kGradHidden (optional): out += row_add[r] * col_vec[col];  kGradW (optional): out += col_vec[col]
+    const float* row_add;     // kGradHidden with col_vec: factor of compact row r
+    __nv_bfloat16* out_w16;   // kGradW: the result goes here as bf16 instead of to out_f32 (last chunk of a call)
+    const float* add_f32;     // kGradW with out_w16 (optional): earlier chunks' fp32 sum, [M][out_stride], added before rounding
 };
 
 // ---- PTX wrappers ---------------------------------------------------------------------------
@@ -261,7 +266,7 @@ struct SmemCtl {
 static_assert(sizeof(SmemCtl) <= 256, "the barriers share a 256-byte slot behind the stage ring");
 
 // ---- the kernel -----------------------------------------------------------------------------
-template <bool PAIR, bool ACC2>
+template <bool PAIR, bool ACC2, bool CE = false>
 __global__ void __launch_bounds__(kThreads, 1)
 umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                  const GemmParams p) {
@@ -607,6 +612,26 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 // 32-column chunks of the accumulator(s), software-pipelined: the tensor-memory load of
                 // chunk ac + 1 is in flight while chunk ac is consumed (with two accumulators the drain is
                 // not hidden behind the next unit's multiplies, so its latency chain matters)
+                // (CE) four columns of one grad_W row: the smoothing term is added; with a bf16 result the
+                // earlier chunks' sum too, and the row's piece is stored -> true.  false: still to be stored.
+                auto finish_w = [&](int r, int c, float4& val) -> bool {
+                    if (p.col_vec) {
+                        const float4 g = *reinterpret_cast<const float4*>(p.col_vec + c);
+                        val.x += g.x; val.y += g.y; val.z += g.z; val.w += g.w;
+                    }
+                    if (!p.out_w16) return false;
+                    const long long o = (long long)r * p.out_stride + c;
+                    if (p.add_f32) {
+                        const float4 a = *reinterpret_cast<const float4*>(p.add_f32 + o);
+                        val.x += a.x; val.y += a.y; val.z += a.z; val.w += a.w;
+                    }
+                    uint2 q;
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.x) : "f"(val.y), "f"(val.x));
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.y) : "f"(val.w), "f"(val.z));
+                    *reinterpret_cast<uint2*>(p.out_w16 + o) = q;
+                    return true;
+                };
+                (void)finish_w;
                 auto consume = [&](int ac, uint32_t (&v)[32]) {
                     // accumulator a of this unit: the token (vocabulary) tile 2 a further on, TMEM columns a * 256 ..
                     const int a = ac / (BN / 32), c = ac - a * (BN / 32);
@@ -664,12 +689,19 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             const long long orow = p.row_index ? (long long)p.row_index[p.live_off + row_a] : (long long)row_a;
                             __nv_bfloat16* dst = p.out_bf16 + orow * p.out_stride + cb;
                             const float sc = p.row_scale ? p.row_scale[row_a] : 1.0f;
+                            if (CE) {
+                                const float ra = p.row_add[row_a];
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (i < nvalid) v[i] = __float_as_uint(fmaf(__uint_as_float(v[i]), sc, ra * p.col_vec[cb + i]));
+                            }
+                            const float so = CE ? 1.0f : sc;
                             if (nvalid == 32) {
                                 uint32_t o[16];
 #pragma unroll
                                 for (int i = 0; i < 16; ++i)
                                     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i])
-                                        : "f"(__uint_as_float(v[2 * i + 1]) * sc), "f"(__uint_as_float(v[2 * i]) * sc));
+                                        : "f"(__uint_as_float(v[2 * i + 1]) * so), "f"(__uint_as_float(v[2 * i]) * so));
                                 uint4* d4 = reinterpret_cast<uint4*>(dst);
                                 d4[0] = make_uint4(o[0], o[1], o[2], o[3]);
                                 d4[1] = make_uint4(o[4], o[5], o[6], o[7]);
@@ -678,7 +710,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             } else {
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
-                                    if (i < nvalid) dst[i] = __float2bfloat16_rn(__uint_as_float(v[i]) * sc);
+                                    if (i < nvalid) dst[i] = __float2bfloat16_rn(__uint_as_float(v[i]) * so);
                             }
                         }
                     } else if (ACC2 && nvalid == 32) {   // kGradW, two-accumulator form: the drain is not hidden
@@ -698,8 +730,9 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const int r = rq + 4 * j;
-                            const float4 val = *reinterpret_cast<const float4*>(stg + r * kDrainPitch + piece * 4);
+                            float4 val = *reinterpret_cast<const float4*>(stg + r * kDrainPitch + piece * 4);
                             if (row_w0 + r < M) {
+                                if (CE && finish_w(row_w0 + r, cb + piece * 4, val)) continue;
                                 float4* d4 = reinterpret_cast<float4*>(p.out_f32 + (long long)(row_w0 + r) * p.out_stride + cb) + piece;
                                 // accumulation is a fire-and-forget vector reduction at the memory side (no
                                 // read round trip in the drain); each element gets exactly one addend per
@@ -713,7 +746,22 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         }
                         __syncwarp();                                    // the tile is free for the next chunk
                     } else {   // kGradW
-                        if (row_ok_a) {
+                        if (CE && row_ok_a && (p.col_vec || p.out_w16)) {
+                            // nvalid is a multiple of 4 (the hidden size is a multiple of 64)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                if (4 * i >= nvalid) continue;
+                                float4 val = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                                                         __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                                if (finish_w(row_a, cb + 4 * i, val)) continue;
+                                float4* d4 = reinterpret_cast<float4*>(p.out_f32 + (long long)row_a * p.out_stride + cb + 4 * i);
+                                if (p.accumulate)
+                                    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
+                                                 :: "l"(d4), "f"(val.x), "f"(val.y), "f"(val.z), "f"(val.w) : "memory");
+                                else
+                                    *d4 = val;
+                            }
+                        } else if (row_ok_a) {
                             float* dst = p.out_f32 + (long long)row_a * p.out_stride + cb;
                             if (nvalid == 32) {
                                 float4* d4 = reinterpret_cast<float4*>(dst);
@@ -1052,6 +1100,10 @@ scale_rows_kernel(const __nv_bfloat16* __restrict__ Hl, int D, int rows_max, con
         return;
     }
     const float f = scale_g[off + r];
+    if (f == 0.0f) {                       // a row that was taken out: its hidden state may hold anything
+        for (int i = threadIdx.x; i < nv; i += blockDim.x) dst[i] = make_uint4(0u, 0u, 0u, 0u);
+        return;
+    }
     const uint4* src = reinterpret_cast<const uint4*>(Hl + (long long)r * D);
     for (int i = threadIdx.x; i < nv; i += blockDim.x) {
         const uint4 z = src[i];
@@ -1070,11 +1122,15 @@ scale_rows_kernel(const __nv_bfloat16* __restrict__ Hl, int D, int rows_max, con
 // to the next multiple of 256 become zeros.  A work item is one (token tile, 256-column tile): four adjacent
 // blocks of the scratch, 64 KB of contiguous memory; the CTAs stride over the items (the launch is
 // usually one that a device flag turns into a no-op, which a small grid makes cheap).
+// CE (cross-entropy form): the row's target entry comes ready-made in tgt_g, y_g is negative for a row
+// without a gradient, and zy / idx are not used.
+template <bool CE>
 __global__ void __launch_bounds__(256)
 dz_from_e_kernel(__nv_bfloat16* __restrict__ ebuf, int V, int n_tiles, const float* __restrict__ tmax, int rows_max,
                  const int* __restrict__ count, int off, const float* __restrict__ lse_g,
                  const float* __restrict__ coef_g, const int32_t* __restrict__ y_g, const int32_t* __restrict__ idx,
-                 const float* __restrict__ zy, const int* __restrict__ run_flag, int run_want) {
+                 const float* __restrict__ zy, const float* __restrict__ tgt_g, const int* __restrict__ run_flag,
+                 int run_want) {
     __shared__ float f_s[kDzBlockRows];          // signed scale of each row for this column tile
     if (run_flag && *run_flag != run_want) return;
     __shared__ int live_s[kDzBlockRows];
@@ -1093,7 +1149,7 @@ dz_from_e_kernel(__nv_bfloat16* __restrict__ ebuf, int V, int n_tiles, const flo
             f = copysignf(ex2_approx(fmaf(tmax[(long long)r * n_tiles + jt], kLog2e, c2)), coef);
         }
         f_s[threadIdx.x] = f;
-        live_s[threadIdx.x] = coef != 0.0f;
+        live_s[threadIdx.x] = CE ? (r < n && y_g[off + r] >= 0) : (coef != 0.0f);
     }
     __syncthreads();
     uint4* base = reinterpret_cast<uint4*>(ebuf + dz_offset((long long)tt * kDzBlockRows, jt * BN, nc));
@@ -1119,6 +1175,10 @@ dz_from_e_kernel(__nv_bfloat16* __restrict__ ebuf, int V, int n_tiles, const flo
         const int r = tt * kDzBlockRows + threadIdx.x;
         const int y = y_g[off + r];
         if (y >= jt * BN && y < jt * BN + BN && y < V) {
+            if (CE) {
+                ebuf[dz_offset(r, y, nc)] = __float2bfloat16_rn(tgt_g[off + r]);
+                continue;
+            }
             const float coef = coef_g[off + r];
             const float py = ex2_approx((zy[idx[off + r]] - lse_g[off + r]) * kLog2e);
             ebuf[dz_offset(r, y, nc)] = __float2bfloat16_rn(fmaf(coef, py, -coef));
@@ -1174,7 +1234,7 @@ static std::atomic<int> g_chunk_tiles{0};   // token tiles per backward chunk; 0
 static std::atomic<int> g_pace{1};          // pacing of the workers' loads (see GemmParams::pace): 1 on, 0 off
 static std::atomic<int> g_row_ref{1};       // backward scratch: 1 exponentials against a per-row reference, 0 per-tile maxima
 
-template <bool PAIR, bool ACC2>
+template <bool PAIR, bool ACC2, bool CE = false>
 static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, const GemmParams& p, cudaStream_t s) {
     static std::mutex mu;
     static bool opted[64] = {};
@@ -1183,7 +1243,7 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
     {
         std::lock_guard<std::mutex> lock(mu);
         if (dev >= 0 && dev < 64 && !opted[dev]) {
-            if (cudaFuncSetAttribute((const void*)umma_gemm_kernel<PAIR, ACC2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+            if (cudaFuncSetAttribute((const void*)umma_gemm_kernel<PAIR, ACC2, CE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      Cfg<PAIR, ACC2>::kSmemBytes) != cudaSuccess) {
                 cudaGetLastError();
                 return RLF_ERR_CUDA;
@@ -1246,7 +1306,7 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
     at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, umma_gemm_kernel<PAIR, ACC2>, ma, mb, q) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, umma_gemm_kernel<PAIR, ACC2, CE>, ma, mb, q) != cudaSuccess) {
         cudaGetLastError();
         return RLF_ERR_CUDA;
     }
@@ -1257,6 +1317,10 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
 static std::atomic<int> g_acc2{1};          // gradient contractions in pair form: 1 two accumulators per CTA, 0 one
 static rlf_status launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const GemmParams& p, bool pair,
                               cudaStream_t s) {
+    if (p.col_vec || p.out_w16) {             // a gradient contraction of the cross-entropy form
+        if (!pair) return launch_gemm_t<false, false, true>(ma, mb, p, s);
+        return g_acc2.load() != 0 ? launch_gemm_t<true, true, true>(ma, mb, p, s) : launch_gemm_t<true, false, true>(ma, mb, p, s);
+    }
     if (!pair) return launch_gemm_t<false, false>(ma, mb, p, s);
     if (p.mode != kLse && g_acc2.load() != 0) return launch_gemm_t<true, true>(ma, mb, p, s);
     return launch_gemm_t<true, false>(ma, mb, p, s);
@@ -1490,8 +1554,8 @@ static rlf_status fused_lmhead_impl(const void* hidden, const void* W, int64_t T
         const int64_t tcp = (tc + 255) & ~(int64_t)255;
         auto dz_pass = [&](const int* run_flag) {
             const long long dz_items = (tcp / kDzBlockRows) * (long long)z.n_tiles;
-            dz_from_e_kernel<<<(unsigned)(dz_items < 148 * 8 ? dz_items : 148 * 8), 256, 0, s>>>(
-                dz, V, z.n_tiles, z.tmax, (int)tc, counts, (int)t0, lse_g, coef_g, y_g, idx_live, zy, run_flag, 1);
+            dz_from_e_kernel<false><<<(unsigned)(dz_items < 148 * 8 ? dz_items : 148 * 8), 256, 0, s>>>(
+                dz, V, z.n_tiles, z.tmax, (int)tc, counts, (int)t0, lse_g, coef_g, y_g, idx_live, zy, nullptr, run_flag, 1);
             count_launch();
         };
         if (row_ref) {
@@ -1677,6 +1741,556 @@ extern "C" rlf_status rlf_fused_lmhead_logp_entropy(const void* hidden, const vo
                                                                              entropy_out, dev_status);
     count_launch();
     return cuda_ok(cudaGetLastError());
+}
+
+// ---------------------------------------------------------------------------------------------
+// Cross entropy through the fused head (the objective of rlf_cross_entropy_fwd_bwd).  Same sweeps and
+// gradient contractions as above over the rows that carry loss, with, per row,
+//   A_t = 1 + 2 zeta lse_t,   dZ_t = c A_t p_t - c eps / V - c (1 - eps) e_y,   c = 1 / N:
+// the scratch holds e = exp(z - rho_t) with the target column overwritten, factor f_t = c A_t exp(rho_t - lse_t),
+// and the uniform part -c eps / V never enters it: it is rank one, so with u = sum_v W_v
+//   grad_hidden_t += a_t u,   grad_W_v += sum_t a_t h_t,   a_t = -c eps / V,
+// two fp32 vectors of length D added in the contractions' epilogues; the mean logit is h_t . u / V.
+namespace rlf {
+namespace lm {
+
+// One CTA turns mask and ids into the work list: idx_live / y_live (rows that carry loss, in token order),
+// idx_dead (the others), counts[0 / 1], and the number of rows with mask != 0.  Four tokens per thread
+// and step.
+__global__ void __launch_bounds__(1024)
+ce_plan_kernel(const int32_t* __restrict__ ids, const uint8_t* __restrict__ mask, int T, int V,
+               int32_t* __restrict__ idx_live, int32_t* __restrict__ y_live, int32_t* __restrict__ idx_dead,
+               int* __restrict__ counts, long long* __restrict__ n_mask, int32_t* __restrict__ dev_status) {
+    __shared__ int warp_tot[32];
+    __shared__ int masked_s[32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int base = 0, masked_in = 0;
+    bool bad = false;
+    for (int t0 = 0; t0 < T; t0 += 4096) {
+        int y[4], live[4], mine = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int t = t0 + 4 * tid + k;
+            const bool in = t < T && (mask == nullptr || mask[t] != 0);
+            y[k] = in ? ids[t] : 0;
+            live[k] = in && y[k] >= 0 && y[k] < V;
+            masked_in += in;
+            bad |= in && !live[k];
+            mine += live[k];
+        }
+        int incl = mine;                                   // inclusive scan over the warp
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 31) warp_tot[warp] = incl;
+        __syncthreads();
+        int before = base + incl - mine, total = 0;
+        for (int w = 0; w < 32; ++w) {
+            if (w < warp) before += warp_tot[w];
+            total += warp_tot[w];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int t = t0 + 4 * tid + k;
+            if (live[k]) {
+                idx_live[before] = t;
+                y_live[before] = y[k];
+                ++before;
+            } else if (t < T) {
+                idx_dead[t - before] = t;
+            }
+        }
+        base += total;
+    }
+    if (bad && dev_status) atomicOr(dev_status, RLF_DEV_BAD_TARGET);
+    masked_in = __reduce_add_sync(0xffffffffu, masked_in);
+    if (lane == 0) masked_s[warp] = masked_in;
+    __syncthreads();
+    if (tid == 0) {
+        long long n = 0;
+        for (int w = 0; w < 32; ++w) n += masked_s[w];
+        *n_mask = n;
+        counts[0] = base;
+        counts[1] = T - base;
+    }
+}
+
+// compact row r <- hidden row idx[r] for r < *count, its target logit, its mean logit (with u) and the
+// reference of its stored exponentials; rows up to the next multiple of 256 are zero-filled
+__global__ void __launch_bounds__(128)
+ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloat16* __restrict__ W, int D,
+                      const int32_t* __restrict__ idx, const int32_t* __restrict__ y_live, const int* __restrict__ count,
+                      const float* __restrict__ u, float inv_v, __nv_bfloat16* __restrict__ out, float* __restrict__ zy_g,
+                      float* __restrict__ mean_g, float* __restrict__ ref_g) {
+    __shared__ float red[2][4];
+    const int n = *count;
+    const int r = blockIdx.x;
+    if (r >= ((n + 255) & ~255)) return;
+    uint4* dst = reinterpret_cast<uint4*>(out + (long long)r * D);
+    const int nv = D / 8;
+    if (r >= n) {
+        for (int i = threadIdx.x; i < nv; i += 128) dst[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (threadIdx.x == 0) ref_g[r] = 0.0f;
+        return;
+    }
+    const uint4* src = reinterpret_cast<const uint4*>(hidden + (long long)idx[r] * D);
+    const uint4* w = reinterpret_cast<const uint4*>(W + (long long)y_live[r] * D);
+    float a = 0.0f, b = 0.0f;
+    for (int i = threadIdx.x; i < nv; i += 128) {
+        const uint4 h = src[i], ww = w[i];
+        dst[i] = h;
+        const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, wv[4] = {ww.x, ww.y, ww.z, ww.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float h0 = __uint_as_float(hw[k] << 16), h1 = __uint_as_float(hw[k] & 0xffff0000u);
+            a = fmaf(h0, __uint_as_float(wv[k] << 16), a);
+            a = fmaf(h1, __uint_as_float(wv[k] & 0xffff0000u), a);
+            if (u) {
+                b = fmaf(h0, u[8 * i + 2 * k], b);
+                b = fmaf(h1, u[8 * i + 2 * k + 1], b);
+            }
+        }
+    }
+    a = warp_sum(a);
+    b = warp_sum(b);
+    if ((threadIdx.x & 31) == 0) {
+        red[0][threadIdx.x >> 5] = a;
+        red[1][threadIdx.x >> 5] = b;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const float zy = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
+        zy_g[r] = zy;
+        mean_g[r] = ((red[1][0] + red[1][1]) + (red[1][2] + red[1][3])) * inv_v;
+        ref_g[r] = zy + kRefShift;
+    }
+}
+
+// rows without loss: NaN statistics, no loss term, a zero row of grad_hidden
+__global__ void __launch_bounds__(128)
+ce_dead_rows_kernel(const int32_t* __restrict__ idx, const int* __restrict__ count, int D, float* __restrict__ logp_out,
+                    float* __restrict__ lse_out, float4* __restrict__ terms, __nv_bfloat16* __restrict__ grad_hidden) {
+    const int r = blockIdx.x;
+    if (r >= *count) return;
+    const int t = idx[r];
+    if (threadIdx.x == 0) {
+        const float nan = __int_as_float(0x7fc00000);
+        logp_out[t] = nan;
+        if (lse_out) lse_out[t] = nan;
+        terms[t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    if (grad_hidden)
+        for (int i = threadIdx.x; i < D / 8; i += 128)
+            reinterpret_cast<uint4*>(grad_hidden + (long long)t * D)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+struct CeCombine {
+    const float2* part;
+    int nsplit, rows_max;
+    const int32_t* idx;
+    const int32_t* y_live;
+    const int* count;
+    int off;
+    const float* zy_g;
+    const float* mean_g;
+    const long long* denom;
+    float eps, zeta, inv_v;
+    float* logp_out;
+    float* lse_out;
+    float4* terms;
+    int32_t* dev_status;
+    // backward only
+    float* lse_g;
+    float* coef_g;              // c A_t
+    float* tgt_g;               // dZ at the target column
+    int32_t* ok_y;              // target id, -1 for a row without a gradient
+    float* add_g;               // a_t
+    float* scale_g;
+    const float* ref_g;         // per-row references, or NULL: the scratch will hold dZ itself
+    __nv_bfloat16* dz;
+    int dz_nc;
+    int* fallback;
+    const int* run_flag;
+};
+// As combine_rows_kernel: statistics, outputs and gradient factors of one chunk's rows.  The target
+// entry is formed as (expm1(logp) + 2 zeta lse p_y + eps) / A_t, which keeps its digits as p_y -> 1;
+// with |A_t| below a half (a log-sum-exp near -1 / (2 zeta)) that quotient is not formed, the chunk is
+// redone with dZ itself in the scratch.
+__global__ void __launch_bounds__(256)
+ce_combine_rows_kernel(const CeCombine p) {
+    if (p.run_flag && *p.run_flag != 1) return;
+    const int r = blockIdx.x * blockDim.x + threadIdx.x;
+    const int n = max(0, min(*p.count - p.off, p.rows_max));
+    if (r >= n) return;
+    const int g = p.off + r, t = p.idx[g];
+    const float2* parts = p.part + (long long)r * p.nsplit;
+    float M = -INFINITY;
+    for (int j = 0; j < p.nsplit; ++j) M = fmaxf(M, parts[j].x);
+    float S = 0.0f;
+    for (int j = 0; j < p.nsplit; ++j) {
+        const float2 ms = parts[j];
+        if (ms.x != -INFINITY) S += ms.y * expf(ms.x - M);
+    }
+    const float ln_s = logf(S), zy = p.zy_g[g];
+    const float lse = M + ln_s, logp = (zy - M) - ln_s;
+    const float smooth = p.eps > 0.0f ? (M - p.mean_g[g]) + ln_s : 0.0f;
+    const bool ok = (M > -INFINITY) && (M < INFINITY) && (S > 0.0f) && (S < INFINITY) && (fabsf(lse) < INFINITY) &&
+                    (fabsf(logp) < INFINITY) && (fabsf(smooth) < INFINITY);
+    const float A = 1.0f + 2.0f * p.zeta * lse;
+    if (p.ref_g) {
+        const float rho = p.ref_g[g];
+        if (!(ok && (lse - rho <= kRefWindow) && fabsf(A) >= 0.5f)) {
+            atomicOr(p.fallback, 1);
+            return;
+        }
+    }
+    const float nan = __int_as_float(0x7fc00000);
+    p.logp_out[t] = ok ? logp : nan;
+    if (p.lse_out) p.lse_out[t] = ok ? lse : nan;
+    p.terms[t] = ok ? make_float4(-logp, smooth, lse, 1.0f) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (!ok && p.dev_status) atomicOr(p.dev_status, RLF_DEV_NONFINITE);
+    if (!p.scale_g) return;
+    const long long N = *p.denom;
+    const float c = 1.0f / (float)(N > 1 ? N : 1);
+    const float tgt = expm1f(logp) + fmaf(2.0f * p.zeta * lse, expf(logp), p.eps);
+    p.add_g[g] = ok ? -c * p.eps * p.inv_v : 0.0f;
+    if (p.ref_g) {
+        const float rho = p.ref_g[g];
+        p.scale_g[g] = c * A * expf(rho - lse);
+        p.dz[dz_offset(r, p.y_live[g], p.dz_nc)] = __float2bfloat16_rn(tgt / A * expf(lse - rho));
+        return;
+    }
+    p.scale_g[g] = ok ? 1.0f : 0.0f;
+    p.lse_g[g] = ok ? lse : 0.0f;
+    p.coef_g[g] = ok ? c * A : 0.0f;
+    p.tgt_g[g] = c * tgt;
+    p.ok_y[g] = ok ? p.y_live[g] : -1;
+}
+
+// out[d] = sum_r weight[r] M[r, d] (weight NULL: 1) over the rows r < rows (or *count - off, if given and less):
+// CTA (x, y) covers 256 columns of slice y and leaves partial row y; rows of weight 0 are not looked at.
+__global__ void __launch_bounds__(256)
+colsum_kernel(const __nv_bfloat16* __restrict__ M, long long rows, int D, const float* __restrict__ weight,
+              const int* __restrict__ count, int off, float* __restrict__ part) {
+    __shared__ float red[8][256];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (count) rows = min(rows, (long long)max(0, *count - off));
+    const int col = blockIdx.x * 256 + lane * 8;
+    float acc[8] = {};
+    if (col < D) {
+        const long long step = (long long)gridDim.y * 8;
+        auto add = [&](const uint4& v, float w) {
+            const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                acc[2 * k] = fmaf(w, __uint_as_float(q[k] << 16), acc[2 * k]);
+                acc[2 * k + 1] = fmaf(w, __uint_as_float(q[k] & 0xffff0000u), acc[2 * k + 1]);
+            }
+        };
+        long long r = (long long)blockIdx.y * 8 + warp;
+        for (; r + 3 * step < rows; r += 4 * step) {       // four loads in flight
+            uint4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint4*>(M + (r + k * step) * D + col);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float w = weight ? weight[r + k * step] : 1.0f;
+                if (w != 0.0f) add(v[k], w);
+            }
+        }
+        for (; r < rows; r += step) {
+            const float w = weight ? weight[r] : 1.0f;
+            if (w != 0.0f) add(*reinterpret_cast<const uint4*>(M + r * D + col), w);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) red[warp][lane * 8 + k] = acc[k];
+    __syncthreads();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c < D) {
+        float s = 0.0f;
+        for (int w = 0; w < 8; ++w) s += red[w][threadIdx.x];
+        part[(long long)blockIdx.y * D + c] = s;
+    }
+}
+__global__ void __launch_bounds__(256)
+colsum_reduce_kernel(const float* __restrict__ part, int parts, int D, float* __restrict__ out) {
+    __shared__ float acc[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (col < D)
+        for (int k = warp; k < parts; k += 8) s += part[(long long)k * D + col];
+    acc[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && col < D) {
+        for (int w = 1; w < 8; ++w) s += acc[w][lane];
+        out[col] = s;
+    }
+}
+constexpr int kColsumParts = 128;
+static rlf_status launch_colsum(const __nv_bfloat16* M, int64_t rows, int32_t D, const float* weight, const int* count,
+                                int off, float* part, float* out, cudaStream_t s) {
+    const int64_t want = (rows + 63) / 64;
+    const int parts = (int)(want < kColsumParts ? (want > 0 ? want : 1) : kColsumParts);
+    colsum_kernel<<<dim3((unsigned)((D + 255) / 256), (unsigned)parts), 256, 0, s>>>(M, rows, D, weight, count, off, part);
+    colsum_reduce_kernel<<<(unsigned)((D + 31) / 32), 256, 0, s>>>(part, parts, D, out);
+    count_launch(2);
+    return cuda_ok(cudaGetLastError());
+}
+
+struct CeWs {
+    size_t head, terms, zy, mean, part, idx_live, idx_dead, y_live, ok_y, lse_g, coef_g, tgt_g, add_g, ref_g, scale_g, ucol,
+        gcol, col_part, hidden_g, hidden_s, tmax, gw_acc, dz, total;
+};
+static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
+    CeWs w;
+    size_t o = 0;
+    const size_t Tn = (size_t)(T > 0 ? T : 0), Tp = (Tn + 255) & ~(size_t)255, Dn = (size_t)D;
+    const size_t chunk = Tp < (size_t)kChunkTokens ? Tp : (size_t)kChunkTokens;
+    const size_t tiles = (size_t)((V + BN - 1) / BN);
+    auto take = [&](size_t bytes) { const size_t at = o; o += up1k(bytes); return at; };
+    w.head = take(1024);             // [0] mask count, [64] live / other rows, [128] chunk flag, [256] pacing counter
+    w.terms = take(16 * Tn);
+    w.zy = take(4 * Tp);
+    w.mean = take(4 * Tp);
+    w.part = take(8 * Tn * kMaxSplit);
+    w.idx_live = take(4 * Tp);
+    w.idx_dead = take(4 * Tp);
+    w.y_live = take(4 * Tp);
+    w.ok_y = take(4 * Tp);
+    w.lse_g = take(4 * Tp);
+    w.coef_g = take(4 * Tp);
+    w.tgt_g = take(4 * Tp);
+    w.add_g = take(4 * Tp);
+    w.ref_g = take(4 * Tp);
+    w.scale_g = take(4 * Tp);
+    w.ucol = take(4 * Dn);
+    w.gcol = take(4 * Dn);
+    w.col_part = take(4 * Dn * kColsumParts);
+    w.hidden_g = take(2 * Tp * Dn);
+    w.hidden_s = take(2 * chunk * Dn);
+    w.tmax = take(4 * chunk * tiles);
+    // fp32 sum of grad_W over the chunks of a call whose result is bf16
+    w.gw_acc = take(w16 && Tn > (size_t)kChunkTokens ? 4 * (size_t)V * Dn : 0);
+    w.dz = take(2 * chunk * tiles * BN);
+    w.total = o + 1024;
+    return w;
+}
+
+}  // namespace lm
+
+size_t lmhead_ce_workspace_bytes(int64_t T, int32_t V, int32_t D, int grad_w_bf16) {
+    if (V < 1 || D < 1) return 0;
+    return lm::ce_workspace(T, V, D, grad_w_bf16 != 0).total;
+}
+
+}  // namespace rlf
+
+extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const void* W, int64_t T, int32_t D, int32_t V,
+                                                     const int32_t* ids, const uint8_t* mask, float label_smoothing,
+                                                     float z_coef, const int64_t* denom, float* logp_out, float* lse_out,
+                                                     double* loss_out, void* grad_hidden, void* grad_W, rlf_dtype grad_W_dt,
+                                                     int accumulate_grad_W, void* workspace, size_t workspace_bytes,
+                                                     int32_t* dev_status, rlf_stream_t stream) {
+    using namespace rlf;
+    using namespace rlf::lm;
+    if (grad_W_dt != RLF_BF16 && grad_W_dt != RLF_F32) return RLF_ERR_DTYPE;
+    if (T < 0 || V < 1 || D < 1) return RLF_ERR_SHAPE;
+    if (D % 64 != 0 || V % 8 != 0) return RLF_ERR_SHAPE;
+    rlf_status st = ce_check_objective(label_smoothing, z_coef);
+    if (st != RLF_OK) return st;
+    const bool w16 = grad_W && grad_W_dt == RLF_BF16;
+    if (T >= (1ll << 30) || (w16 && accumulate_grad_W)) return RLF_ERR_UNSUPPORTED;
+    if (!loss_out) return RLF_ERR_NULL;
+    if (T > 0 && (!hidden || !W || !ids || !logp_out)) return RLF_ERR_NULL;
+    if (!aligned(hidden, 16) || !aligned(W, 16) || !aligned(grad_hidden, 16) || !aligned(grad_W, 16) || !aligned(ids, 4) ||
+        !aligned(logp_out, 4) || !aligned(lse_out, 4) || !aligned(loss_out, 8) || !aligned(denom, 8))
+        return RLF_ERR_ALIGN;
+    const CeWs w = ce_workspace(T, V, D, w16);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < w.total) return RLF_ERR_WORKSPACE;
+    st = check_arch();
+    if (st != RLF_OK) return st;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 1023) & ~(uintptr_t)1023);
+    auto at = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+    long long* n_mask = reinterpret_cast<long long*>(ws + w.head);
+    int* counts = reinterpret_cast<int*>(ws + w.head + 64);
+    int* chunk_flag = reinterpret_cast<int*>(ws + w.head + 128);
+    const long long* dn = denom ? reinterpret_cast<const long long*>(denom) : n_mask;
+    float4* terms = reinterpret_cast<float4*>(ws + w.terms);
+    const __nv_bfloat16* H = static_cast<const __nv_bfloat16*>(hidden);
+    const __nv_bfloat16* Wm = static_cast<const __nv_bfloat16*>(W);
+    if (T == 0) {
+        // no rows: a zero loss, and a gradient of zero unless it is accumulated
+        if (!denom) {
+            st = ce_launch_count(nullptr, 0, n_mask, s);
+            if (st != RLF_OK) return st;
+        }
+        if (grad_W && !accumulate_grad_W &&
+            cudaMemsetAsync(grad_W, 0, (size_t)V * D * (w16 ? 2 : 4), s) != cudaSuccess)
+            return RLF_ERR_CUDA;
+        return ce_launch_loss(terms, 0, dn, label_smoothing, z_coef, loss_out, s);
+    }
+
+    int32_t* idx_live = reinterpret_cast<int32_t*>(ws + w.idx_live);
+    int32_t* idx_dead = reinterpret_cast<int32_t*>(ws + w.idx_dead);
+    int32_t* y_live = reinterpret_cast<int32_t*>(ws + w.y_live);
+    __nv_bfloat16* Hl = reinterpret_cast<__nv_bfloat16*>(ws + w.hidden_g);
+    __nv_bfloat16* Hs = reinterpret_cast<__nv_bfloat16*>(ws + w.hidden_s);
+    __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + w.dz);
+    const int64_t Tp = (T + 255) & ~(int64_t)255;
+    const bool bwd = grad_hidden || grad_W, smoothing = label_smoothing > 0.0f;
+    const bool row_ref = bwd && g_row_ref.load() != 0;
+    float* ucol = smoothing ? at(w.ucol) : nullptr;
+    ce_plan_kernel<<<1, 1024, 0, s>>>(ids, mask, (int)T, V, idx_live, y_live, idx_dead, counts, n_mask, dev_status);
+    count_launch();
+    if (smoothing) {
+        st = launch_colsum(Wm, V, D, nullptr, nullptr, 0, at(w.col_part), ucol, s);
+        if (st != RLF_OK) return st;
+    }
+    const float inv_v = 1.0f / (float)V;
+    ce_gather_rows_kernel<<<(unsigned)Tp, 128, 0, s>>>(H, Wm, D, idx_live, y_live, counts, ucol, inv_v, Hl, at(w.zy),
+                                                       at(w.mean), at(w.ref_g));
+    ce_dead_rows_kernel<<<(unsigned)T, 128, 0, s>>>(idx_dead, counts + 1, D, logp_out, lse_out, terms,
+                                                    static_cast<__nv_bfloat16*>(grad_hidden));
+    count_launch(2);
+    if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
+
+    const bool pair = g_pair.load() != 0;
+    CUtensorMap mapW;
+    if (!make_map(&mapW, Wm, (uint64_t)V, (uint64_t)D, (uint64_t)D, BK, pair ? BN / 2 : BN)) return RLF_ERR_CUDA;
+    // (a bf16 grad_W of a call that fits one built-in chunk is not cut further: its workspace holds no fp32 sum)
+    const int tuned_tiles = g_chunk_tiles.load();
+    const bool tuned = tuned_tiles > 0 && tuned_tiles * BM < kChunkTokens && !(w16 && T <= kChunkTokens);
+    const int64_t chunk_tokens = tuned ? tuned_tiles * BM : kChunkTokens;
+    for (int64_t t0 = 0; t0 < T; t0 += chunk_tokens) {
+        const int64_t tc = (T - t0) < chunk_tokens ? (T - t0) : chunk_tokens;
+        const int64_t tcp = (tc + 255) & ~(int64_t)255;
+        CUtensorMap mapHc;
+        if (!make_map(&mapHc, Hl + t0 * D, (uint64_t)tc, (uint64_t)D, (uint64_t)D, BK, BM)) return RLF_ERR_CUDA;
+        GemmParams z = {};
+        z.mode = kLse;
+        z.N = V;
+        z.n_tiles = (V + BN - 1) / BN;
+        z.k_slabs = D / BK;
+        z.M = (int)tc;
+        z.m_tiles = (int)((tc + BM - 1) / BM);
+        z.nsplit = pick_split(z.n_tiles);
+        z.n_tiles_per_split = (z.n_tiles + z.nsplit - 1) / z.nsplit;
+        z.part = reinterpret_cast<float2*>(ws + w.part);
+        z.dev_status = dev_status;
+        z.pace = reinterpret_cast<int*>(ws + w.head + 256);
+        z.live_count = counts;
+        z.live_off = (int)t0;
+        if (bwd) {
+            z.dz = dz;
+            z.dz_nc = 4 * z.n_tiles;
+            z.tmax = at(w.tmax);
+        }
+        CeCombine c = {};
+        c.part = z.part; c.nsplit = z.nsplit; c.rows_max = (int)tc; c.idx = idx_live; c.y_live = y_live; c.count = counts;
+        c.off = (int)t0; c.zy_g = at(w.zy); c.mean_g = at(w.mean); c.denom = dn; c.eps = label_smoothing; c.zeta = z_coef;
+        c.inv_v = inv_v; c.logp_out = logp_out; c.lse_out = lse_out; c.terms = terms; c.dev_status = dev_status;
+        if (bwd) {
+            c.lse_g = at(w.lse_g); c.coef_g = at(w.coef_g); c.tgt_g = at(w.tgt_g);
+            c.ok_y = reinterpret_cast<int32_t*>(ws + w.ok_y); c.add_g = at(w.add_g); c.scale_g = at(w.scale_g);
+            c.dz = dz; c.dz_nc = z.dz_nc;
+        }
+        const unsigned row_blocks = (unsigned)((tc + 255) / 256);
+        if (row_ref) {
+            if (cudaMemsetAsync(chunk_flag, 0, sizeof(int), s) != cudaSuccess) return RLF_ERR_CUDA;
+            z.ref = at(w.ref_g) + t0;
+            st = launch_gemm(mapHc, mapW, z, pair, s);
+            if (st != RLF_OK) return st;
+            CeCombine cr = c;
+            cr.ref_g = at(w.ref_g);
+            cr.fallback = chunk_flag;
+            ce_combine_rows_kernel<<<row_blocks, 256, 0, s>>>(cr);
+            count_launch();
+            // queued always, run only if some row of the chunk raised the flag
+            z.ref = nullptr;
+            z.run_flag = chunk_flag;
+            z.run_want = 1;
+            c.run_flag = chunk_flag;
+        }
+        st = launch_gemm(mapHc, mapW, z, pair, s);
+        if (st != RLF_OK) return st;
+        ce_combine_rows_kernel<<<row_blocks, 256, 0, s>>>(c);
+        count_launch();
+        if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
+        if (!bwd) continue;
+        const long long dz_items = (tcp / kDzBlockRows) * (long long)z.n_tiles;
+        dz_from_e_kernel<true><<<(unsigned)(dz_items < 148 * 8 ? dz_items : 148 * 8), 256, 0, s>>>(
+            dz, V, z.n_tiles, z.tmax, (int)tc, counts, (int)t0, c.lse_g, c.coef_g, c.ok_y, nullptr, nullptr, c.tgt_g,
+            z.run_flag, 1);
+        count_launch();
+        const uint64_t dz_rows = (uint64_t)(tcp / kDzBlockRows) * (uint64_t)(4 * z.n_tiles) * kDzBlockRows;
+        if (grad_hidden) {
+            CUtensorMap mapDzK, mapWn;
+            if (!make_map(&mapDzK, dz, dz_rows, kDzBlockCols, kDzBlockCols, BK, BM)) return RLF_ERR_CUDA;
+            if (!make_map(&mapWn, Wm, (uint64_t)V, (uint64_t)D, (uint64_t)D, 64, BK)) return RLF_ERR_CUDA;
+            GemmParams h = {};
+            h.mode = kGradHidden;
+            h.M = (int)tc;
+            h.N = D;
+            h.m_tiles = (int)((tc + BM - 1) / BM);
+            h.n_tiles = (D + BN - 1) / BN;
+            h.k_slabs = 4 * z.n_tiles;
+            h.dz_nc = z.dz_nc;
+            h.out_bf16 = static_cast<__nv_bfloat16*>(grad_hidden);
+            h.out_stride = D;
+            h.dev_status = dev_status;
+            h.live_count = counts;
+            h.live_off = (int)t0;
+            h.row_index = idx_live;
+            h.row_scale = row_ref ? c.scale_g + t0 : nullptr;
+            h.col_vec = ucol;
+            h.row_add = c.add_g + t0;
+            h.pace = z.pace;
+            st = launch_gemm(mapDzK, mapWn, h, pair, s);
+            if (st != RLF_OK) return st;
+        }
+        if (grad_W) {
+            scale_rows_kernel<<<(unsigned)tcp, 128, 0, s>>>(Hl + t0 * D, D, (int)tc, counts, (int)t0, c.scale_g, Hs);
+            count_launch();
+            if (smoothing) {
+                st = launch_colsum(Hl + t0 * D, tc, D, c.add_g + t0, counts, (int)t0, at(w.col_part), at(w.gcol), s);
+                if (st != RLF_OK) return st;
+            }
+            CUtensorMap mapDzM, mapHn;
+            if (!make_map(&mapDzM, dz, dz_rows, kDzBlockCols, kDzBlockCols, 64, BK)) return RLF_ERR_CUDA;
+            if (!make_map(&mapHn, Hs, (uint64_t)tc, (uint64_t)D, (uint64_t)D, 64, BK)) return RLF_ERR_CUDA;
+            const bool last = t0 + chunk_tokens >= T;
+            GemmParams q = {};
+            q.mode = kGradW;
+            q.M = V;
+            q.N = D;
+            q.m_tiles = (V + BM - 1) / BM;
+            q.n_tiles = (D + BN - 1) / BN;
+            q.k_slabs = (int)((tc + BK - 1) / BK);
+            q.dz_nc = z.dz_nc;
+            q.out_f32 = w16 ? at(w.gw_acc) : static_cast<float*>(grad_W);
+            q.out_stride = D;
+            q.accumulate = (accumulate_grad_W || t0 > 0) ? 1 : 0;
+            if (w16 && last) {                 // bf16 result: rounded once, from the sum over the chunks
+                q.out_w16 = static_cast<__nv_bfloat16*>(grad_W);
+                q.add_f32 = t0 > 0 ? at(w.gw_acc) : nullptr;
+                q.accumulate = 0;
+            }
+            q.dev_status = dev_status;
+            q.live_count = counts;
+            q.live_off = (int)t0;
+            q.col_vec = smoothing ? at(w.gcol) : nullptr;
+            q.pace = z.pace;
+            st = launch_gemm(mapDzM, mapHn, q, pair, s);
+            if (st != RLF_OK) return st;
+        }
+    }
+    return ce_launch_loss(terms, T, dn, label_smoothing, z_coef, loss_out, s);
 }
 
 extern "C" rlf_status rlf_tune_lmhead(int pair_ctas) {

@@ -71,3 +71,34 @@ def test_cross_entropy_refuses(lib):
     assert call(z=4097) == ALIGN and call(dt=1, z=4098) == ALIGN and call(grad=4097) == ALIGN and call(loss=4100) == ALIGN
     assert call(denom=4100) == ALIGN and call(lse=4098) == ALIGN
     assert call(ws=None) == WORKSPACE and call(ws=4100) == WORKSPACE and call(wsb=256) == WORKSPACE
+
+
+def test_fused_cross_entropy_refuses(lib):
+    f = lib.rlf_fused_lmhead_cross_entropy
+    f.argtypes = [vp, vp, i64, i32, i32, vp, vp, f32, f32, vp, vp, vp, vp, vp, vp, ci, ci, vp, sz, vp, vp]
+
+    def call(H=FAKE, W=FAKE, T=4, D=64, V=64, ids=FAKE, eps=0.0, zc=0.0, denom=None, logp=FAKE, lse=None, loss=FAKE, gh=None,
+             gw=None, gdt=1, acc=0, ws=FAKE, wsb=1 << 40):
+        return f(H, W, T, D, V, ids, None, eps, zc, denom, logp, lse, loss, gh, gw, gdt, acc, ws, wsb, None, None)
+
+    assert call(gdt=2) == DTYPE
+    assert call(T=-1) == SHAPE and call(D=100) == SHAPE and call(V=63) == SHAPE and call(V=0) == SHAPE and call(D=0) == SHAPE
+    assert call(eps=2.0) == UNSUPPORTED and call(zc=-1.0) == UNSUPPORTED and call(T=1 << 30) == UNSUPPORTED
+    assert call(gw=FAKE, gdt=0, acc=1) == UNSUPPORTED
+    assert call(H=None) == NULL and call(W=None) == NULL and call(ids=None) == NULL and call(logp=None) == NULL
+    assert call(loss=None) == NULL
+    assert call(H=4104) == ALIGN and call(W=4104) == ALIGN and call(gh=4104) == ALIGN and call(gw=4104) == ALIGN
+    assert call(loss=4100) == ALIGN and call(denom=4100) == ALIGN
+    assert call(ws=None) == WORKSPACE and call(ws=4100) == WORKSPACE and call(wsb=1000) == WORKSPACE
+
+
+def test_workspace_sizes_grow_with_the_problem(lib):
+    f = lib.rlf_workspace_bytes
+    f.restype = sz
+    f.argtypes = [ci, i64, i32, i32, ci]
+    assert f(7, 0, 0, 64, 0) > 0 and f(7, 4096, 0, 64, 0) >= f(7, 64, 0, 64, 0) and f(7, 5, 0, 0, 0) == 0
+    assert f(8, 0, 100, 0, 0) >= 256 and f(8, 1000, 100, 0, 0) >= 256 + 16000
+    assert f(9, 100, 0, 64, 0) == 0
+    # the scratch of a chunk, and an fp32 sum beside a bf16 gradient of more than one chunk
+    assert f(9, 8192, 151936, 4096, 1) >= 2 * 8192 * 151936 and f(9, 18944, 512, 64, 0) == f(9, 18944, 512, 64, 1)
+    assert f(9, 18945, 512, 64, 0) - f(9, 18945, 512, 64, 1) >= 4 * 512 * 64
