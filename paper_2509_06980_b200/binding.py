@@ -462,6 +462,15 @@ def _rows(t, what):
     return (t.data_ptr() if T > 0 else None), (t.stride(0) if T > 1 else D)
 
 
+def _empty_rows_like(t, stride):
+    """An empty [T, V] tensor whose rows sit in their 16-byte vectors as t's rows do (what the fast kernels need)."""
+    T, V = t.shape
+    off = t.data_ptr() % 16 // t.element_size() if T > 0 else 0
+    if off == 0:
+        return torch.empty_strided((T, V), (stride, 1), dtype=t.dtype, device=t.device)
+    return torch.empty((T - 1) * stride + V + off, dtype=t.dtype, device=t.device).as_strided((T, V), (stride, 1), off)
+
+
 def _like(t, shape, dtype, what):
     if t is not None and (t.shape != shape or t.dtype != dtype):
         raise ValueError("%s must be a %s tensor of shape %s" % (what, dtype, tuple(shape)))
@@ -486,7 +495,7 @@ def rlf_cross_entropy_fwd_bwd(logits, ids, mask=None, label_smoothing=0.0, z_coe
     dev = logits.device
     _one_device(logits, ids, mask, denom, grad_logits, logp_out, lse_out, loss_out, workspace, dev_status)
     if grad_logits is None and want_grad:
-        grad_logits = logits if in_place else torch.empty_strided((T, V), (stride, 1), dtype=logits.dtype, device=dev)
+        grad_logits = logits if in_place else _empty_rows_like(logits, stride)
     gp = None
     if grad_logits is not None:
         _like(grad_logits, logits.shape, logits.dtype, "grad_logits")

@@ -129,8 +129,11 @@ def test_gradient_buffer_of_another_alignment_and_guard(dt):
         g = gbuf[off:off + T * (V + 2)].view(T, V + 2)[:, :V]
         out = run(z, ids, mask, 0.1, grad_logits=g)
         check(out, z, ids, mask, 0.1)
+        # an entry is c p - u, u = c eps / V: at most one rounding (2^-8) of c p and one of the entry in either call, so
+        # the two are at most 2^-8 (|c p| + 2 |entry|) apart, |c p| <= |entry| + u, besides fp32 errors
         err = (g.double() - ref[3].double()).abs()
-        assert (err <= 2.0 ** -6 * ref[3].double().abs() + 1e-9).all()
+        u = 0.1 / V / max(int((mask != 0).sum()), 1)
+        assert (err <= 1.05 * 2.0 ** -8 * (3 * ref[3].double().abs() + u)).all()
         g.fill_(3.0)
         assert (gbuf == 3.0).all()
 
@@ -259,7 +262,9 @@ def test_repeated_captured_and_concurrent_calls(dt, V):
     z.copy_(z0.flip(0)), ids.copy_(ids0.flip(0)), mask.copy_(mask0.flip(0))
     g.replay()
     torch.cuda.synchronize()
-    assert torch.equal(out[3].flip(0), ref[3])
+    # (not the first result's rows in reverse: where a row's vectors begin decides which thread adds what)
+    assert all(torch.equal(a.nan_to_num(7.0), b_.nan_to_num(7.0)) for a, b_ in zip(out, call()))
+    check(out, z, ids, mask, 0.1, 1e-4)
     z.copy_(z0), ids.copy_(ids0), mask.copy_(mask0)
     g.replay()
     torch.cuda.synchronize()
