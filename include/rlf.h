@@ -419,7 +419,7 @@ rlf_status rlf_fused_lmhead_logp_entropy(const void *hidden, const void *W, int6
  *   grad_logits  [T, V] dt with the same row_stride, or NULL (forward only); may be logits itself
  *   workspace    rlf_workspace_bytes(RLF_FN_CROSS_ENTROPY, T, V, 0, dt) bytes, 256-byte aligned; contents
  *                need not be initialised
- * T = 0 is valid (loss_out = 0).  T beyond 2^31 - 1 returns RLF_ERR_UNSUPPORTED.
+ * T = 0 is valid (loss_out = 0).  T of 2^30 and more returns RLF_ERR_UNSUPPORTED.
  */
 rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T, int32_t V,
                                      int64_t row_stride, const int32_t *ids, const uint8_t *mask,

@@ -7,9 +7,9 @@
 // The target column is formed as (1/N) [ 2 zeta lse p_y - S'/S + eps - eps/V ], S' the sum over the
 // other columns, so that it keeps its digits when p_y rounds to one.
 //
-// Kernels, in launch order: ce_count_kernel (only without a given count), the row kernel (writes logp,
-// lse, the row's loss terms and grad_logits), ce_loss_kernel (fp64 sums in a fixed order).
-// Rows without loss weight are not read at all; their gradient is written as zeros.
+// Kernels, in launch order: ce_plan_kernel (work list: the rows that carry loss, then the others; their
+// count), the row kernel (writes logp, lse, the row's loss terms and grad_logits), ce_loss_kernel (fp64 sums in
+// a fixed order).  Rows without loss weight are not read at all; their gradient is written as zeros.
 #include <map>
 #include <mutex>
 #include <tuple>
@@ -20,9 +20,11 @@
 namespace rlf {
 namespace ce {
 
-// workspace: [0] int64 count of rows with loss weight; [256 ..) one float4 of loss terms per token:
-// {lse - z_y, lse - mean z (0 without smoothing), lse, 1 if the row counts}
+// workspace: [0] int64 number of rows with mask != 0; [64] int number of live rows; [256 ..) one float4 of loss terms
+// per token, {lse - z_y, lse - mean z (0 without smoothing), lse, 1 if the row counts}; then the work list, one
+// int2 per token: {row, target id} of the live rows in order, then {row, -1} of the others
 constexpr size_t kWsTermsOff = 256;
+constexpr size_t ws_list_off(int64_t T) { return kWsTermsOff + 16 * (size_t)(T > 0 ? T : 0); }
 
 struct RowParams {
     const void* logits;
@@ -30,8 +32,8 @@ struct RowParams {
     long long stride;           // elements
     long long T;
     int V;
-    const int32_t* ids;
-    const uint8_t* mask;        // nullable: every row counts
+    const int2* list;           // {row, target id} of the live rows, then {row, -1} of the others
+    const int* n_live;
     const long long* denom;     // device count of rows with loss weight
     float* logp_out;
     float* lse_out;             // nullable
@@ -46,15 +48,6 @@ template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v
 template <typename T> __device__ __forceinline__ T from_f(float v);
 template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-
-constexpr int kTargetNone = -1, kTargetBad = -2;
-// target id of a row, kTargetNone for a row without loss weight (its id is not looked at), kTargetBad
-// for one whose id lies outside the vocabulary
-__device__ __forceinline__ int row_target(const int32_t* ids, const uint8_t* mask, long long t, int V) {
-    if (mask && mask[t] == 0) return kTargetNone;
-    const int y = ids[t];
-    return (y >= 0 && y < V) ? y : kTargetBad;
-}
 
 // what a row leaves behind once its statistics are known; returns whether it takes part
 struct RowStats {
@@ -100,10 +93,12 @@ ce_row_general_kernel(const RowParams p) {
         }
         __syncthreads();
     };
-    for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
+    for (long long k = blockIdx.x; k < p.T; k += gridDim.x) {
+        const int2 job = p.list[k];
+        const long long t = job.x;
+        const int y = job.y;
         const T* z = static_cast<const T*>(p.logits) + t * p.stride;
         T* g = p.grad ? static_cast<T*>(p.grad) + t * p.stride : nullptr;
-        const int y = row_target(p.ids, p.mask, t, p.V);
         RowStats r = {};
         float M = 0.0f, S = 1.0f, others = 0.0f;
         if (y >= 0) {
@@ -133,8 +128,7 @@ ce_row_general_kernel(const RowParams p) {
         }
         if (tid == 0) {
             write_row(p, t, r);
-            if (y == kTargetBad) status |= RLF_DEV_BAD_TARGET;
-            else if (y >= 0 && !r.ok) status |= RLF_DEV_NONFINITE;
+            if (y >= 0 && !r.ok) status |= RLF_DEV_NONFINITE;
         }
         if (g == nullptr) continue;
         if (!r.ok) {
@@ -181,6 +175,9 @@ struct ClusterParams {
     RowParams r;
     int per_cta_vec;            // vectors of a row per CTA of the cluster
     float inv_v;                // 1 / V
+    // launch constants, kept out of the registers
+    int csize, num_clusters;
+    uint32_t row_bytes;         // bytes that every CTA receives per exchanged row
 };
 
 template <typename T> struct Elem;
@@ -198,8 +195,39 @@ template <> struct Elem<float> {
         asm volatile("st.shared.b32 [%0], %1;" :: "r"(smem_u32(at)), "r"(0xFF800000u) : "memory");
     }
 };
+// elements [from, to) of a 16-byte vector in shared memory stay, the others become -inf
+template <typename T>
+__device__ __forceinline__ void keep_elements(uint4* at, int from, int to) {
+    uint4 v = *at;
+    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (sizeof(T) == 2) {
+            const uint32_t lo = (2 * j >= from && 2 * j < to) ? w[j] & 0xffffu : 0xFF80u;
+            const uint32_t hi = (2 * j + 1 >= from && 2 * j + 1 < to) ? w[j] & 0xffff0000u : 0xFF800000u;
+            w[j] = lo | hi;
+        } else if (j < from || j >= to) {
+            w[j] = 0xFF800000u;
+        }
+    }
+    *at = v;
+}
 __device__ __forceinline__ void cp_async16_part(void* smem_dst, const void* gmem_src, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(smem_u32(smem_dst)), "l"(gmem_src), "r"(bytes) : "memory");
+}
+
+// Programmatic dependent launch: the next kernel of a call may be set up while this one runs; it waits here before it
+// reads anything that an earlier kernel wrote.
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// Bounded wait for a row's exchange (about a second).  What it remembers of a wait that ran out sits in shared
+// memory: a register carried through the row loop costs spills.
+__device__ __forceinline__ void wait_row(uint32_t bar, uint32_t parity, int* timed_out) {
+    for (int i = 0; i < kWaitPolls; ++i) {
+        if (mbar_try_wait(bar, parity)) return;
+        if ((i & 1023) == 1023 && *reinterpret_cast<volatile int*>(timed_out)) return;
+    }
+    *reinterpret_cast<volatile int*>(timed_out) = 1;
 }
 
 template <typename T, int THREADS, int NV, bool EDGE, int CMAX>
@@ -217,10 +245,12 @@ ce_row_cluster_kernel(const ClusterParams cp) {
     __shared__ __align__(16) uint4 edge_slot[EDGE ? 2 : 1];   // gradients of a row's first and last vector
     __shared__ __align__(8) unsigned long long row_bar[2];
 
-    const int csize = (int)cluster_nctarank(), crank = (int)cluster_ctarank();
-    const int cluster_id = blockIdx.x / csize, num_clusters = gridDim.x / csize;
+    __shared__ float inv_n_s;
+    __shared__ int timed_out;                                 // a wait ran out: no wait is taken again, the loops end, reported
+    __shared__ __align__(8) int2 job_slot[8];                 // ring of work-list entries, fetched three rows ahead
+
+    const int crank = (int)cluster_ctarank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int npairs = csize * NWARPS;
     const int vbeg = crank * cp.per_cta_vec + tid;            // this thread's vectors: vbeg + i THREADS
     const int vcap = (crank + 1) * cp.per_cta_vec;
     const bool smooth = p.eps > 0.0f;
@@ -236,72 +266,108 @@ ce_row_cluster_kernel(const ClusterParams cp) {
         const int vend = min(nvec, vcap);
         return vend > vbeg ? min(NV, (vend - vbeg + THREADS - 1) / THREADS) : 0;
     };
-    // 1 / N, re-read where it is used: a register held across the passes costs more than an L1 hit
-    auto weight = [&]() -> float {
-        const long long N = *p.denom;
-        return 1.0f / (float)(N > 1 ? N : 1);
-    };
     const int nvalid_all = EDGE ? 0 : count_valid(p.V / VE);
 
-    auto prefetch = [&](int row, bool have) {
-        if (have) {
-            const int head = row_head(row);
-            const T* src = static_cast<const T*>(p.logits) + (long long)row * p.stride - head;
-            const int nvec = row_vecs(head), nvalid = EDGE ? count_valid(nvec) : nvalid_all;
-            const int last_bytes = EDGE ? (head + p.V - (nvec - 1) * VE) * (int)sizeof(T) : 16;
+    auto prefetch = [&](int row) {
+        const int head = row_head(row);
+        const T* row0 = static_cast<const T*>(p.logits) + (long long)row * p.stride - head;
+        const uint4* src = reinterpret_cast<const uint4*>(row0) + vbeg;
+        uint4* dst = stage + tid;
+        const int nvec = row_vecs(head), nvalid = EDGE ? count_valid(nvec) : nvalid_all;
+        const int last_bytes = EDGE ? (head + p.V - (nvec - 1) * VE) * (int)sizeof(T) : 16;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (i >= nvalid) continue;
+        for (int i = 0; i < NV; ++i) {
+            if (i < nvalid) {
                 const int v = vbeg + i * THREADS;
-                uint4* dst = stage + i * THREADS + tid;
                 if (EDGE && v == 0 && head != 0 && row == 0) {
-                    T* d = reinterpret_cast<T*>(dst);
-                    for (int e = head; e < VE && e < head + p.V; ++e) d[e] = src[e];
+                    T* d = reinterpret_cast<T*>(dst + i * THREADS);
+                    for (int e = head; e < VE && e < head + p.V; ++e) d[e] = row0[e];
                 } else if (EDGE && v == nvec - 1) {
-                    cp_async16_part(dst, src + (long long)v * VE, last_bytes);
+                    cp_async16_part(dst + i * THREADS, src + i * THREADS, last_bytes);
                 } else {
-                    cp_async16_cg(dst, src + (long long)v * VE);
+                    cp_async16_cg(dst + i * THREADS, src + i * THREADS);
                 }
             }
         }
-        cp_async_commit();
     };
 
     if (tid == 0) {
         mbar_init(smem_u32(&row_bar[0]), 1);
         mbar_init(smem_u32(&row_bar[1]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        timed_out = 0;
     }
-    int y = cluster_id < nrows ? row_target(p.ids, p.mask, cluster_id, p.V) : kTargetNone;
-    int y_next = cluster_id + num_clusters < nrows ? row_target(p.ids, p.mask, cluster_id + num_clusters, p.V) : kTargetNone;
-    prefetch(cluster_id, y >= 0);
+    pdl_wait();
+    pdl_trigger();
+    if (tid == 0) {
+        const long long N = *p.denom;
+        inv_n_s = 1.0f / (float)(N > 1 ? N : 1);
+    }
+    const int cluster_id = blockIdx.x / cp.csize;
+    const int n_live = *p.n_live;
+    // thread 0 fetches the entry of this cluster's j-th row, in the cp.async group of an earlier row's data
+    auto fetch_job = [&](int j) {
+        const long long at = (long long)cluster_id + (long long)j * cp.num_clusters;
+        if (tid == 0 && at < n_live)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(smem_u32(&job_slot[j & 7])), "l"(p.list + at) : "memory");
+    };
+    auto job_row = [&](int j) -> int { return reinterpret_cast<const volatile int*>(job_slot)[2 * (j & 7)]; };
+    auto job_target = [&](int j) -> int { return reinterpret_cast<const volatile int*>(job_slot)[2 * (j & 7) + 1]; };
+    for (int j = 0; j < 3; ++j) fetch_job(j);
+    cp_async_wait_all();
+    __syncthreads();
+    if (cluster_id < n_live) prefetch(job_row(0));
+    cp_async_commit();
     // every CTA of the cluster is running before any peer may address its shared memory
     cluster_sync_all();
 
-    const uint32_t row_bytes = (uint32_t)npairs * (smooth ? 12u : 8u) + 4u;
-    int status = 0;
-    int it = 0;                          // rows exchanged so far: rows without loss weight need no exchange
-    bool gave_up = false;
-    for (int k = cluster_id; k < nrows; k += num_clusters) {
-        const int next = k + num_clusters;
-        const int head = row_head(k);
+    // a row's own elements of its first and last vector, by the thread that has put them into edge_slot
+    auto store_edges = [&](T* g_row, int head, int nvec, int nvalid) {
+        const int lrel = nvec - 1 - vbeg;
+        const bool first = vbeg == 0 && nvalid > 0;
+        const bool last = nvec > 1 && lrel >= 0 && (lrel & (THREADS - 1)) == 0 && lrel / THREADS < nvalid;
+        if (first || last) {
+#pragma unroll 1
+            for (int side = first ? 0 : 1; side <= (last ? 1 : 0); ++side) {
+                const uint4 o = edge_slot[side];
+                const T* oe = reinterpret_cast<const T*>(&o);
+                const int base = (side == 0 ? 0 : nvec - 1) * VE - head;    // column of the vector's element 0
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+                    if (base + e >= 0 && base + e < p.V) g_row[base + e] = oe[e];
+            }
+        }
+    };
+    auto zero_row = [&](int row, int head, int nvec, int nvalid) {
+        T* g_row = static_cast<T*>(p.grad) + (long long)row * p.stride;
+        uint4* dst = reinterpret_cast<uint4*>(g_row - head) + vbeg;
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < nvalid; ++i) {
+            const int v = vbeg + i * THREADS;
+            if (EDGE && v == 0) edge_slot[0] = zero;
+            else if (EDGE && v == nvec - 1) edge_slot[1] = zero;
+            else st_stream(dst + i * THREADS, zero);
+        }
+        if (EDGE) store_edges(g_row, head, nvec, nvalid);
+    };
+    int it = 0;
+    int k = cluster_id;
+    for (; k < n_live; k += cp.num_clusters, ++it) {
+        const int head = row_head(job_row(it));
         const int nvec = row_vecs(head), nvalid = EDGE ? count_valid(nvec) : nvalid_all;
-        RowStats st = {};
-        float M = 0.0f, S = 1.0f, others = 0.0f, m_ws = 0.0f;
+        float m_ws;
         uint4 d[NV];
-        if (y >= 0) {
+        {
             const int parity = it & 1;
             const uint32_t bar = smem_u32(&row_bar[parity]);
             cp_async_wait_all();
-            if (tid == 0) mbar_arrive_expect_tx(bar, row_bytes);
+            if (tid == 0) mbar_arrive_expect_tx(bar, cp.row_bytes);
             if (EDGE) {
                 // what lies in the first and the last vector beside the row is not part of it
                 const int tail = head + p.V - (nvec - 1) * VE;          // elements of the last vector up to the row's end
-                if (vbeg == 0 && nvalid > 0)
-                    for (int e = 0; e < head; ++e) Elem<T>::store_neg_inf(reinterpret_cast<T*>(&stage[tid]) + e);
+                if (vbeg == 0 && nvalid > 0) keep_elements<T>(&stage[tid], head, VE);
                 const int lrel = nvec - 1 - vbeg;
-                if (lrel >= 0 && (lrel & (THREADS - 1)) == 0 && lrel / THREADS < nvalid)
-                    for (int e = tail; e < VE; ++e) Elem<T>::store_neg_inf(reinterpret_cast<T*>(&stage[lrel + tid]) + e);
+                if (lrel >= 0 && (lrel & (THREADS - 1)) == 0 && lrel / THREADS < nvalid) keep_elements<T>(&stage[lrel + tid], 0, tail);
             }
             // the mean logit, from the staging slots (the row's own elements only)
             if (smooth) {
@@ -329,17 +395,17 @@ ce_row_cluster_kernel(const ClusterParams cp) {
                     }
                 }
                 q = warp_sum(q);
-                if (lane < csize)
+                if (lane < cp.csize)
                     st_async_f1(smem_u32(&mean_slot[parity][crank * NWARPS + warp]), bar, (uint32_t)lane, q);
             }
             // the owner of the target column sends its logit to every CTA and takes it out of the sums: the
             // target's gradient needs the sum over the OTHER columns
-            const int ye = y + head, yrel = ye / VE - vbeg;
+            const int ye = job_target(it) + head, yrel = ye / VE - vbeg;
             const bool own_y = yrel >= 0 && (yrel & (THREADS - 1)) == 0 && yrel / THREADS < nvalid;
             if (own_y) {
                 T* sv = reinterpret_cast<T*>(&stage[yrel + tid]) + ye % VE;
                 const float zt = to_f<T>(*sv);
-                for (int r = 0; r < csize; ++r) st_async_f1(smem_u32(&zy_slot[parity]), bar, (uint32_t)r, zt);
+                for (int r = 0; r < cp.csize; ++r) st_async_f1(smem_u32(&zy_slot[parity]), bar, (uint32_t)r, zt);
                 Elem<T>::store_neg_inf(sv);
             }
             const uint32_t ninf = Elem<T>::neg_inf();
@@ -362,7 +428,10 @@ ce_row_cluster_kernel(const ClusterParams cp) {
                     m_w = fmaxf(m_w, fmaxf(fmaxf(__uint_as_float(d[i].x), __uint_as_float(d[i].y)),
                                            fmaxf(__uint_as_float(d[i].z), __uint_as_float(d[i].w))));
             }
-            prefetch(next, y_next >= 0);             // the slots are in registers: queue the next row
+            // the slots are in registers: queue the next row
+            if ((long long)k + cp.num_clusters < n_live) prefetch(job_row(it + 1));
+            fetch_job(it + 3);
+            cp_async_commit();
             m_w = ord2f(__reduce_max_sync(0xffffffffu, f2ord(m_w)));
             m_ws = (m_w == -INFINITY) ? 0.0f : m_w;
             float s0 = 0.0f, s1 = 0.0f;
@@ -400,14 +469,11 @@ ce_row_cluster_kernel(const ClusterParams cp) {
                 }
             }
             const float s_w = warp_sum(s0 + s1);
-            if (lane < csize) st_async_f2(smem_u32(&pair_slot[parity][crank * NWARPS + warp]), bar, (uint32_t)lane, m_w, s_w);
-            if (!gave_up && !mbar_wait_bounded(bar, (uint32_t)(it >> 1) & 1u)) {
-                gave_up = true;
-                status |= RLF_DEV_TIMEOUT;
-            }
-            ++it;
+            if (lane < cp.csize) st_async_f2(smem_u32(&pair_slot[parity][crank * NWARPS + warp]), bar, (uint32_t)lane, m_w, s_w);
+            wait_row(bar, (uint32_t)(it >> 1) & 1u, &timed_out);
             // merge all warps' pairs of the row, lanes in parallel, identically in every warp
-            M = -INFINITY;
+            const int npairs = cp.csize * NWARPS;
+            float M = -INFINITY;
             float2 e[(MAXE + 31) / 32];
             float Q = 0.0f;
 #pragma unroll
@@ -420,79 +486,67 @@ ce_row_cluster_kernel(const ClusterParams cp) {
             M = ord2f(__reduce_max_sync(0xffffffffu, f2ord(M)));
             const float zy = zy_slot[parity];
             M = fmaxf(M, zy);
-            others = 0.0f;
+            float others = 0.0f;
 #pragma unroll
             for (int j = 0; j < (MAXE + 31) / 32; ++j)
                 if (e[j].x != -INFINITY) others += e[j].y * ex2_approx((e[j].x - M) * kLog2e);
             others = warp_sum(others);
             if (smooth) Q = warp_sum(Q);
-            S = others + ex2_approx((zy - M) * kLog2e);
-            st = row_stats(M, S, zy, Q, p.eps);
-        } else {
-            prefetch(next, y_next >= 0);
-        }
-        if (crank == 0 && tid == 0) {
-            write_row(p, k, st);
-            if (y == kTargetBad) status |= RLF_DEV_BAD_TARGET;
-            else if (y >= 0 && !st.ok) status |= RLF_DEV_NONFINITE;
-        }
-        if (p.grad != nullptr) {
-            T* g_row = static_cast<T*>(p.grad) + (long long)k * p.stride;
-            uint4* dst = reinterpret_cast<uint4*>(g_row - head) + vbeg;
-            float a = 0.0f, u = 0.0f;
-            if (st.ok) {
-                // entries are a e - u: the registers hold 2^((z - m_w) log2e)
-                const float inv_n = weight();
-                a = inv_n * (1.0f + 2.0f * p.zeta * st.lse) / S * ex2_approx((m_ws - M) * kLog2e);
-                u = inv_n * p.eps * cp.inv_v;
+            const float S = others + ex2_approx((zy - M) * kLog2e);
+            const RowStats st = row_stats(M, S, zy, Q, p.eps);
+            if (crank == 0 && tid == 0) {
+                write_row(p, job_row(it), st);
+                if (!st.ok && p.dev_status) atomicOr(p.dev_status, RLF_DEV_NONFINITE);
             }
+            if (p.grad != nullptr) {
+                if (!st.ok) {
+                    zero_row(job_row(it), head, nvec, nvalid);
+                } else {
+                    // entries are a e - u: the registers hold 2^((z - m_w) log2e)
+                    // (fast divisions, two ulp: an exact one holds a slow path that the row in the registers is spilled for)
+                    const float a = __fdividef(inv_n_s * (1.0f + 2.0f * p.zeta * st.lse), S) * ex2_approx((m_ws - M) * kLog2e);
+                    const float u = inv_n_s * p.eps * cp.inv_v;
+                    T* g_row = static_cast<T*>(p.grad) + (long long)job_row(it) * p.stride;
+                    uint4* dst = reinterpret_cast<uint4*>(g_row - head) + vbeg;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (i >= nvalid) continue;
-                uint4 o = make_uint4(0u, 0u, 0u, 0u);
-                if (st.ok) {
-                    uint32_t* w = reinterpret_cast<uint32_t*>(&o);
-                    const uint32_t* x = reinterpret_cast<const uint32_t*>(&d[i]);
+                    for (int i = 0; i < NV; ++i) {
+                        if (i >= nvalid) continue;
+                        uint4 o;
+                        uint32_t* w = reinterpret_cast<uint32_t*>(&o);
+                        const uint32_t* x = reinterpret_cast<const uint32_t*>(&d[i]);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        w[j] = BF ? pack_bf16x2(fmaf(bf_lo(x[j]), a, -u), fmaf(bf_hi(x[j]), a, -u))
-                                  : __float_as_uint(fmaf(__uint_as_float(x[j]), a, -u));
-                }
-                const int v = vbeg + i * THREADS;
-                if (EDGE && v == 0) edge_slot[0] = o;
-                else if (EDGE && v == nvec - 1) edge_slot[1] = o;
-                else st_stream(dst + i * THREADS, o);
-            }
-            if (EDGE) {
-                // the row's own elements of its first and last vector, by the thread that has just put them down
-                const int lrel = nvec - 1 - vbeg;
-                const bool first = vbeg == 0 && nvalid > 0;
-                const bool last = nvec > 1 && lrel >= 0 && (lrel & (THREADS - 1)) == 0 && lrel / THREADS < nvalid;
-                for (int side = 0; side < 2; ++side) {
-                    if (!(side == 0 ? first : last)) continue;
-                    const T* o = reinterpret_cast<const T*>(&edge_slot[side]);
-                    const int base = (side == 0 ? 0 : nvec - 1) * VE - head;        // column of the vector's element 0
-                    for (int e = 0; e < VE; ++e)
-                        if (base + e >= 0 && base + e < p.V) g_row[base + e] = o[e];
-                }
-            }
-            if (st.ok) {
-                // the target id again, by its owner (not held in a register across the passes)
-                const int yt = p.ids[k], ye = yt + head, yrel = ye / VE - vbeg;
-                if (yrel >= 0 && (yrel & (THREADS - 1)) == 0 && yrel / THREADS < nvalid) {
-                    const float py = 1.0f - others / S;
-                    g_row[yt] = from_f<T>(weight() * (2.0f * p.zeta * st.lse * py - others / S + p.eps) - u);
+                        for (int j = 0; j < 4; ++j)
+                            w[j] = BF ? pack_bf16x2(fmaf(bf_lo(x[j]), a, -u), fmaf(bf_hi(x[j]), a, -u))
+                                      : __float_as_uint(fmaf(__uint_as_float(x[j]), a, -u));
+                        const int v = vbeg + i * THREADS;
+                        if (EDGE && v == 0) edge_slot[0] = o;
+                        else if (EDGE && v == nvec - 1) edge_slot[1] = o;
+                        else st_stream(dst + i * THREADS, o);
+                    }
+                    if (EDGE) store_edges(g_row, head, nvec, nvalid);
+                    // (the target id is re-read from its slot, not held in a register across the passes)
+                    const int yt = job_target(it), yr = (yt + head) / VE - vbeg;
+                    if (yr >= 0 && (yr & (THREADS - 1)) == 0 && yr / THREADS < nvalid) {
+                        const float rest = __fdividef(others, S);                       // 1 - p_y
+                        g_row[yt] = from_f<T>(inv_n_s * (2.0f * p.zeta * st.lse * (1.0f - rest) - rest + p.eps) - u);
+                    }
                 }
             }
         }
-        y = y_next;
-        // needed when that row's loads are queued, in the next iteration
-        y_next = (long long)next + num_clusters < nrows ? row_target(p.ids, p.mask, next + num_clusters, p.V) : kTargetNone;
     }
-    if (status && p.dev_status) atomicOr(p.dev_status, status);
+    // rows without loss weight (or without such a target) are not read, their gradient is zeros
+    for (; k < nrows; k += cp.num_clusters) {
+        const int row = p.list[k].x;
+        if (crank == 0 && tid == 0) write_row(p, row, RowStats{});
+        if (p.grad == nullptr) continue;
+        const int head = row_head(row), nvec = row_vecs(head);
+        zero_row(row, head, nvec, EDGE ? count_valid(nvec) : nvalid_all);
+    }
     // a warp that gave up: peers' stores of the last rows may still be on their way into this CTA
-    if (gave_up)
+    if (*reinterpret_cast<volatile int*>(&timed_out)) {
+        if (lane == 0 && p.dev_status) atomicOr(p.dev_status, RLF_DEV_TIMEOUT);
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
     cluster_sync_all();                  // no CTA leaves while a peer could still address its shared memory
 }
 
@@ -500,59 +554,60 @@ ce_row_cluster_kernel(const ClusterParams cp) {
 typedef void (*RowKernel)(const ClusterParams);
 struct RowShape { int cluster, threads, nv; };
 
-template <typename T, int THREADS, bool EDGE, int CMAX>
-static RowKernel kernel_for_nv(int nv) {
+// one CTA per row for rows of up to 1024 vectors: 64 or 128 threads, an even number of vectors each
+template <typename T, int THREADS, bool EDGE>
+static RowKernel narrow_kernel(int nv) {
     switch (nv) {
-        case 1: return ce_row_cluster_kernel<T, THREADS, 1, EDGE, CMAX>;
-        case 2: return ce_row_cluster_kernel<T, THREADS, 2, EDGE, CMAX>;
-        case 3: return ce_row_cluster_kernel<T, THREADS, 3, EDGE, CMAX>;
-        case 4: return ce_row_cluster_kernel<T, THREADS, 4, EDGE, CMAX>;
-        case 5: return ce_row_cluster_kernel<T, THREADS, 5, EDGE, CMAX>;
+        case 2: return ce_row_cluster_kernel<T, THREADS, 2, EDGE, 1>;
+        case 4: return ce_row_cluster_kernel<T, THREADS, 4, EDGE, 1>;
+        case 6: return ce_row_cluster_kernel<T, THREADS, 6, EDGE, 1>;
+        case 8: return ce_row_cluster_kernel<T, THREADS, 8, EDGE, 1>;
+    }
+    return nullptr;
+}
+// clusters of 1 to 8 CTAs, or (CMAX = 16) of 10 and 16: 6 to 10 vectors per thread
+template <typename T, int THREADS, bool EDGE, int CMAX>
+static RowKernel wide_kernel(int nv) {
+    switch (nv) {
         case 6: return ce_row_cluster_kernel<T, THREADS, 6, EDGE, CMAX>;
         case 7: return ce_row_cluster_kernel<T, THREADS, 7, EDGE, CMAX>;
         case 8: return ce_row_cluster_kernel<T, THREADS, 8, EDGE, CMAX>;
         case 9: return ce_row_cluster_kernel<T, THREADS, 9, EDGE, CMAX>;
-        case 10: return ce_row_cluster_kernel<T, THREADS, 10, EDGE, CMAX>;
-    }
-    return nullptr;
-}
-// the wider shapes hold rows of 20481 vectors and more: 6 to 10 vectors per thread
-template <typename T, int THREADS, bool EDGE>
-static RowKernel wide_kernel_for_nv(int nv) {
-    switch (nv) {
-        case 6: return ce_row_cluster_kernel<T, THREADS, 6, EDGE, 16>;
-        case 7: return ce_row_cluster_kernel<T, THREADS, 7, EDGE, 16>;
-        case 8: return ce_row_cluster_kernel<T, THREADS, 8, EDGE, 16>;
-        case 9: return ce_row_cluster_kernel<T, THREADS, 9, EDGE, 16>;
-        case 10: return ce_row_cluster_kernel<T, THREADS, 10, EDGE, 16>;
+        case 10: return EDGE ? nullptr : ce_row_cluster_kernel<T, THREADS, 10, false, CMAX>;
     }
     return nullptr;
 }
 template <typename T, bool EDGE>
 static RowKernel row_kernel(const RowShape& sh) {
-    if (sh.cluster <= 8) return kernel_for_nv<T, 256, EDGE, 8>(sh.nv);
-    return sh.threads == 256 ? wide_kernel_for_nv<T, 256, EDGE>(sh.nv) : wide_kernel_for_nv<T, 512, EDGE>(sh.nv);
+    if (sh.threads == 64) return narrow_kernel<T, 64, EDGE>(sh.nv);
+    if (sh.threads == 128) return narrow_kernel<T, 128, EDGE>(sh.nv);
+    if (sh.threads == 512) return wide_kernel<T, 512, EDGE, 16>(sh.nv);
+    return sh.cluster <= 8 ? wide_kernel<T, 256, EDGE, 8>(sh.nv) : wide_kernel<T, 256, EDGE, 16>(sh.nv);
 }
 
 // 16-byte vectors of a row per CTA: an even split rounded up to whole 128-byte lines
 static int per_cta_vectors(int nvec, int cluster) { return (((nvec + cluster - 1) / cluster) + 7) & ~7; }
 
-// The smallest cluster of 256-thread CTAs that holds a row of nvec vectors with at most 10 per thread (1, 2, 4
-// or 8 CTAs; then 10 and 16, beyond the portable size), then 16 CTAs of 512 threads.  false: no shape holds it.
-static bool pick_shape(int nvec, RowShape* out) {
-    static const int clusters[] = {1, 2, 4, 8, 10, 16};
-    for (int th = 256; th <= 512; th *= 2)
-        for (int c : clusters) {
-            if (th == 512 && c != 16) continue;
-            int nv = (per_cta_vectors(nvec, c) + th - 1) / th;
-            if (nv > 10) continue;
-            if (c > 8 && nv < 6) nv = 6;
-            *out = {c, th, nv};
-            return true;
-        }
+// Rows of up to 512 vectors go to one CTA of 64 threads, up to 1024 to one of 128 (what a short row costs is its chain of
+// latencies, so as many rows as possible are under way: 65536 x 2048 bf16 took 229 us as 256 threads a row, 139 as 64);
+// longer ones to the smallest cluster of 256-thread CTAs that holds them (1, 2, 4 or 8 CTAs; then 10 and 16, beyond
+// the portable size), the longest to 16 CTAs of 512 threads.  At most 10 vectors per thread (9 with EDGE, 8 in the
+// small CTAs): the most that the registers hold without spilling more than a few words.  false: no shape holds it.
+static bool pick_shape(int nvec, bool edge, RowShape* out) {
+    static const RowShape shapes[] = {{1, 64, 8}, {1, 128, 8}, {1, 256, 10}, {2, 256, 10}, {4, 256, 10},
+                                      {8, 256, 10}, {10, 256, 10}, {16, 256, 10}, {16, 512, 10}};
+    for (const RowShape& sh : shapes) {
+        int nv = (per_cta_vectors(nvec, sh.cluster) + sh.threads - 1) / sh.threads;
+        if (nv > (edge && sh.nv > 9 ? 9 : sh.nv)) continue;
+        if (sh.threads < 256) nv = (nv + 1) & ~1;
+        else if (nv < 6) nv = 6;
+        *out = {sh.cluster, sh.threads, nv};
+        return true;
+    }
     return false;
 }
 
+// at: two attributes, the second (programmatic dependent launch) added by the launch itself
 static void cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int grid, const RowShape& sh, cudaStream_t s) {
     *cfg = cudaLaunchConfig_t{};
     cfg->gridDim = dim3(grid);
@@ -580,7 +635,7 @@ static int resident_clusters(RowKernel k, const RowShape& sh) {
     if (hit != cache.end()) return hit->second;
     int n = 0;
     cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     cluster_config(&cfg, at, sh.cluster * 148 * 8, sh, nullptr);
     if (cudaFuncSetAttribute((const void*)k, cudaFuncAttributeMaxDynamicSharedMemorySize, stage_bytes(sh.threads, sh.nv)) != cudaSuccess ||
         (sh.cluster > 8 && cudaFuncSetAttribute((const void*)k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
@@ -592,9 +647,10 @@ static int resident_clusters(RowKernel k, const RowShape& sh) {
     return n;
 }
 
-// A cluster handles about two dozen rows before it retires (whole generations of what is resident at once): with
-// one generation of persistent clusters all of them load, then all of them store, in step for the whole launch.
-constexpr int kRowsPerCluster = 24;
+// A cluster handles about ten rows before it retires (whole generations of what is resident at once): with one
+// generation of persistent clusters all of them load, then all of them store, in step for the whole launch
+// (8192 x 151936 bf16, rows per cluster 8 / 10 / 14 / 20 / 32 / 100: 784 / 785 / 790 / 799 / 817 / 1082 us).
+constexpr int kRowsPerCluster = 10;
 static int clusters_for(int resident, long long rows) {
     const long long per_generation = (long long)resident * kRowsPerCluster;
     long long nc = (rows + per_generation - 1) / per_generation * resident;
@@ -602,77 +658,202 @@ static int clusters_for(int resident, long long rows) {
     return (int)(nc < (1 << 26) ? nc : (1 << 26));
 }
 
-// number of rows with loss weight (one CTA; integer sum)
-__global__ void __launch_bounds__(1024)
-ce_count_kernel(const uint8_t* __restrict__ mask, long long T, long long* __restrict__ count) {
-    __shared__ int red[32];
-    int c = 0;
-    if (mask == nullptr) {
-        if (threadIdx.x == 0) *count = T;
-        return;
-    }
-    const long long head = min(T, (long long)((16 - (reinterpret_cast<uintptr_t>(mask) & 15)) & 15));
-    for (long long t = threadIdx.x; t < head; t += 1024) c += mask[t] != 0;
-    const uint4* m4 = reinterpret_cast<const uint4*>(mask + head);
-    const long long n4 = (T - head) / 16;
-    for (long long i = threadIdx.x; i < n4; i += 1024) {
-        const uint4 v = m4[i];
-        // 0xff in every non-zero byte
-        c += (__popc(__vcmpne4(v.x, 0u)) + __popc(__vcmpne4(v.y, 0u)) + __popc(__vcmpne4(v.z, 0u)) +
-              __popc(__vcmpne4(v.w, 0u))) >> 3;
-    }
-    for (long long t = head + 16 * n4 + threadIdx.x; t < T; t += 1024) c += mask[t] != 0;
-    c = __reduce_add_sync(0xffffffffu, c);
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = c;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        long long s = 0;
-        for (int w = 0; w < 32; ++w) s += red[w];
-        *count = s;
-    }
+// ---- the small kernels around the row kernel ---------------------------------------------------
+// Both run as one cluster of up to 8 CTAs (one SM each): a single CTA needs 30 us for 65536 tokens, a grid would need a
+// second launch to join its parts.
+constexpr int kPlanThreads = 1024, kPlanPer = 8, kMaxPlanCtas = 8;
+constexpr int kPlanTokens = kPlanThreads * kPlanPer;         // tokens per CTA and step
+
+// the 32-bit word at the same shared-memory place in CTA `rank` of the cluster
+__device__ __forceinline__ int ld_cluster_int(const int* local, int rank) {
+    uint32_t remote;
+    int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(local)), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
+    return v;
+}
+__device__ __forceinline__ double ld_cluster_double(const double* local, int rank) {
+    uint32_t remote;
+    double v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(local)), "r"(rank));
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(remote) : "memory");
+    return v;
 }
 
-// loss terms -> loss_out[4] in fp64.  Every thread adds its tokens in index order, then a fixed tree: the
-// same order on every launch.
+// mask and ids -> the work list: {row, target id} of the rows with loss weight and a target inside the vocabulary, in
+// order, then {row, -1} of the others (from the end backwards); *n_live of the first kind, and the number of rows with
+// mask != 0.  CTA r takes the r-th stretch of kPlanTokens tokens of every step, a thread every 1024th token of it.
+__global__ void __launch_bounds__(kPlanThreads)
+ce_plan_kernel(const int32_t* __restrict__ ids, const uint8_t* __restrict__ mask, int T, int V, int2* __restrict__ list,
+               int* __restrict__ n_live, long long* __restrict__ n_mask, int32_t* __restrict__ dev_status) {
+    __shared__ int piece[kPlanPer * 32];     // live rows of each (k, warp) of this CTA, then their exclusive sums
+    __shared__ int cta_live[2];              // live rows of this CTA in a step, two steps in turn
+    __shared__ int cta_masked;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int csize = (int)cluster_nctarank(), crank = (int)cluster_ctarank();
+    pdl_trigger();
+    int base = 0, masked_in = 0, step = 0;
+    bool bad = false;
+    for (long long s0 = 0; s0 < T; s0 += (long long)csize * kPlanTokens, step ^= 1) {
+        const long long t0 = s0 + (long long)crank * kPlanTokens;
+        int y[kPlanPer];
+        unsigned b[kPlanPer];
+        int in[kPlanPer];
+#pragma unroll
+        for (int k = 0; k < kPlanPer; ++k) {
+            const long long t = t0 + 1024 * k + tid;
+            in[k] = t < T ? (mask ? mask[t] : 1) : 0;
+            y[k] = t < T ? ids[t] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kPlanPer; ++k) {
+            const bool live = in[k] && y[k] >= 0 && y[k] < V;
+            masked_in += in[k] != 0;
+            bad |= in[k] && !live;
+            b[k] = __ballot_sync(0xffffffffu, live);
+            if (lane == 0) piece[k * 32 + warp] = __popc(b[k]);
+        }
+        __syncthreads();
+        if (warp == 0) {
+            // exclusive sums of the 256 pieces in row order, eight per lane
+            int c[kPlanPer], mine = 0;
+#pragma unroll
+            for (int k = 0; k < kPlanPer; ++k) {
+                c[k] = piece[lane * kPlanPer + k];
+                mine += c[k];
+            }
+            int incl = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += up;
+            }
+            int at = incl - mine;
+#pragma unroll
+            for (int k = 0; k < kPlanPer; ++k) {
+                piece[lane * kPlanPer + k] = at;
+                at += c[k];
+            }
+            if (lane == 31) cta_live[step] = incl;
+        }
+        if (csize > 1) cluster_sync_all();
+        else __syncthreads();
+        int before = base, total = 0;
+        for (int r = 0; r < csize; ++r) {
+            const int n = csize > 1 ? ld_cluster_int(&cta_live[step], r) : cta_live[step];
+            if (r < crank) before += n;
+            total += n;
+        }
+#pragma unroll
+        for (int k = 0; k < kPlanPer; ++k) {
+            const long long t = t0 + 1024 * k + tid;
+            const int at = before + piece[k * 32 + warp] + __popc(b[k] & ((1u << lane) - 1u));
+            if ((b[k] >> lane) & 1u) list[at] = make_int2((int)t, y[k]);
+            else if (t < T) list[T - 1 - ((int)t - at)] = make_int2((int)t, -1);
+        }
+        base += total;
+        __syncthreads();                     // the pieces are free for the next step
+    }
+    if (bad && dev_status) atomicOr(dev_status, RLF_DEV_BAD_TARGET);
+    masked_in = __reduce_add_sync(0xffffffffu, masked_in);
+    if (lane == 0) piece[warp] = masked_in;
+    __syncthreads();
+    if (tid == 0) {
+        int n = 0;
+        for (int w = 0; w < 32; ++w) n += piece[w];
+        cta_masked = n;
+    }
+    if (csize > 1) cluster_sync_all();
+    if (crank == 0 && tid == 0) {
+        long long n = 0;
+        for (int r = 0; r < csize; ++r) n += csize > 1 ? ld_cluster_int(&cta_masked, r) : cta_masked;
+        *n_mask = n;
+        *n_live = base;
+    }
+    if (csize > 1) cluster_sync_all();       // no CTA leaves while another may read its shared memory
+}
+
+// loss terms -> loss_out[4] in fp64.  Every thread adds its tokens in index order, then a fixed tree over the CTA and the
+// CTAs in order: the same order on every launch.
 constexpr int kLossThreads = 1024;
 __global__ void __launch_bounds__(kLossThreads)
 ce_loss_kernel(const float4* __restrict__ terms, long long T, const long long* __restrict__ denom, float eps, float zeta,
                double* __restrict__ loss_out) {
     __shared__ double red[3][kLossThreads / 32];
+    __shared__ double cta_sum[3];
+    const int csize = (int)cluster_nctarank(), crank = (int)cluster_ctarank();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_wait();
     double a = 0.0, b = 0.0, c = 0.0;
-    for (long long t = threadIdx.x; t < T; t += kLossThreads) {
+#pragma unroll 4
+    for (long long t = (long long)crank * kLossThreads + threadIdx.x; t < T; t += (long long)csize * kLossThreads) {
         const float4 r = terms[t];
-        if (r.w == 0.0f) continue;
-        a += (double)r.x;
-        b += (double)r.y;
-        c += (double)r.z * (double)r.z;
+        if (r.w != 0.0f) {
+            a += (double)r.x;
+            b += (double)r.y;
+            c += (double)r.z * (double)r.z;
+        }
     }
+    auto tree = [](double v) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        a += __shfl_xor_sync(0xffffffffu, a, o);
-        b += __shfl_xor_sync(0xffffffffu, b, o);
-        c += __shfl_xor_sync(0xffffffffu, c, o);
-    }
-    if ((threadIdx.x & 31) == 0) {
-        red[0][threadIdx.x >> 5] = a;
-        red[1][threadIdx.x >> 5] = b;
-        red[2][threadIdx.x >> 5] = c;
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    };
+    a = tree(a);
+    b = tree(b);
+    c = tree(c);
+    if (lane == 0) {
+        red[0][warp] = a;
+        red[1][warp] = b;
+        red[2][warp] = c;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        a = b = c = 0.0;
-        for (int w = 0; w < kLossThreads / 32; ++w) {
-            a += red[0][w];
-            b += red[1][w];
-            c += red[2][w];
-        }
+    if (warp < 3) {
+        const double v = tree(red[warp][lane]);
+        if (lane == 0) cta_sum[warp] = v;
+    }
+    if (csize > 1) cluster_sync_all();
+    else __syncthreads();
+    if (crank == 0 && threadIdx.x == 0) {
+        double q[3] = {0.0, 0.0, 0.0};
+        for (int k = 0; k < 3; ++k)
+            for (int r = 0; r < csize; ++r) q[k] += csize > 1 ? ld_cluster_double(&cta_sum[k], r) : cta_sum[k];
         const long long N = *denom;
         const double nd = (double)(N > 1 ? N : 1);
-        loss_out[0] = ((1.0 - (double)eps) * a + (double)eps * b + (double)zeta * c) / nd;
-        loss_out[1] = a / nd;
-        loss_out[2] = b / nd;
-        loss_out[3] = c / nd;
+        loss_out[0] = ((1.0 - (double)eps) * q[0] + (double)eps * q[1] + (double)zeta * q[2]) / nd;
+        loss_out[1] = q[0] / nd;
+        loss_out[2] = q[1] / nd;
+        loss_out[3] = q[2] / nd;
     }
+    if (csize > 1) cluster_sync_all();
+}
+
+// one cluster of `ctas` CTAs; pdl: the launch may overlap the end of the kernel before it (the kernel waits by itself)
+template <typename... Args>
+static rlf_status launch_cluster(void (*k)(Args...), int ctas, int threads, bool pdl, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[2];
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = s;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ctas;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = pdl ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, k, args...) != cudaSuccess) {
+        cudaGetLastError();
+        return RLF_ERR_CUDA;
+    }
+    count_launch();
+    return RLF_OK;
+}
+static int small_ctas(int64_t T, int64_t per_cta) {
+    const int64_t n = (T + per_cta - 1) / per_cta;
+    return (int)(n < 1 ? 1 : n < kMaxPlanCtas ? n : kMaxPlanCtas);
 }
 
 // The cluster kernel wherever a shape holds the row and the gradient rows sit like the logits rows within their
@@ -686,7 +867,7 @@ static rlf_status launch_rows(const RowParams& p, rlf_dtype dt, cudaStream_t s) 
     // a row on no boundary may take one vector more than its length fills
     const long long nvec = edge ? ((long long)p.V + 2 * ve - 2) / ve : p.V / ve;
     RowShape sh;
-    if (same && nvec < (1 << 24) && pick_shape((int)nvec, &sh)) {
+    if (same && nvec < (1 << 24) && pick_shape((int)nvec, edge, &sh)) {
         const RowKernel k = dt == RLF_BF16 ? (edge ? row_kernel<__nv_bfloat16, true>(sh) : row_kernel<__nv_bfloat16, false>(sh))
                                            : (edge ? row_kernel<float, true>(sh) : row_kernel<float, false>(sh));
         const int resident = k ? resident_clusters(k, sh) : 0;
@@ -696,8 +877,14 @@ static rlf_status launch_rows(const RowParams& p, rlf_dtype dt, cudaStream_t s) 
             cp.per_cta_vec = per_cta_vectors((int)nvec, sh.cluster);
             cp.inv_v = 1.0f / (float)p.V;
             cudaLaunchConfig_t cfg;
-            cudaLaunchAttribute at[1];
-            cluster_config(&cfg, at, clusters_for(resident, p.T) * sh.cluster, sh, s);
+            cudaLaunchAttribute at[2];
+            cp.csize = sh.cluster;
+            cp.num_clusters = clusters_for(resident, p.T);
+            cp.row_bytes = (uint32_t)(sh.cluster * (sh.threads / 32)) * (p.eps > 0.0f ? 12u : 8u) + 4u;
+            cluster_config(&cfg, at, cp.num_clusters * sh.cluster, sh, s);
+            at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            at[1].val.programmaticStreamSerializationAllowed = 1;
+            cfg.numAttrs = 2;
             if (cudaLaunchKernelEx(&cfg, k, cp) != cudaSuccess) {
                 cudaGetLastError();
                 return RLF_ERR_CUDA;
@@ -715,23 +902,22 @@ static rlf_status launch_rows(const RowParams& p, rlf_dtype dt, cudaStream_t s) 
 
 }  // namespace ce
 
-rlf_status ce_launch_count(const uint8_t* mask, int64_t T, long long* count, cudaStream_t s) {
-    ce::ce_count_kernel<<<1, 1024, 0, s>>>(mask, T, count);
-    count_launch();
-    return cuda_ok(cudaGetLastError());
+rlf_status ce_launch_plan(const int32_t* ids, const uint8_t* mask, int64_t T, int32_t V, void* list, int* n_live,
+                          long long* n_mask, int32_t* dev_status, cudaStream_t s) {
+    return ce::launch_cluster(ce::ce_plan_kernel, ce::small_ctas(T, ce::kPlanTokens), ce::kPlanThreads, false, s, ids, mask,
+                              (int)T, (int)V, static_cast<int2*>(list), n_live, n_mask, dev_status);
 }
 rlf_status ce_launch_loss(const void* terms, int64_t T, const long long* denom, float eps, float zeta, double* loss_out,
                           cudaStream_t s) {
-    ce::ce_loss_kernel<<<1, ce::kLossThreads, 0, s>>>(static_cast<const float4*>(terms), T, denom, eps, zeta, loss_out);
-    count_launch();
-    return cuda_ok(cudaGetLastError());
+    return ce::launch_cluster(ce::ce_loss_kernel, ce::small_ctas(T, 4 * ce::kLossThreads), ce::kLossThreads, true, s,
+                              static_cast<const float4*>(terms), (long long)T, denom, eps, zeta, loss_out);
 }
 rlf_status ce_check_objective(float label_smoothing, float z_coef) {
     if (!(label_smoothing >= 0.0f && label_smoothing <= 1.0f)) return RLF_ERR_UNSUPPORTED;
     if (!(z_coef >= 0.0f && z_coef < INFINITY)) return RLF_ERR_UNSUPPORTED;
     return RLF_OK;
 }
-size_t cross_entropy_workspace_bytes(int64_t T) { return ce::kWsTermsOff + 16 * (size_t)(T > 0 ? T : 0); }
+size_t cross_entropy_workspace_bytes(int64_t T) { return ce::ws_list_off(T) + 8 * (size_t)(T > 0 ? T : 0); }
 
 }  // namespace rlf
 
@@ -746,7 +932,7 @@ extern "C" rlf_status rlf_cross_entropy_fwd_bwd(const void* logits, rlf_dtype dt
     if (T < 0 || V < 1 || row_stride < V) return RLF_ERR_SHAPE;
     rlf_status st = ce_check_objective(label_smoothing, z_coef);
     if (st != RLF_OK) return st;
-    if (T >= (1ll << 31)) return RLF_ERR_UNSUPPORTED;
+    if (T >= (1ll << 30)) return RLF_ERR_UNSUPPORTED;
     if (!loss_out) return RLF_ERR_NULL;
     if (T > 0 && (!logits || !ids || !logp_out)) return RLF_ERR_NULL;
     const size_t esz = dt == RLF_BF16 ? 2 : 4;
@@ -758,14 +944,14 @@ extern "C" rlf_status rlf_cross_entropy_fwd_bwd(const void* logits, rlf_dtype dt
     if (st != RLF_OK) return st;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
-    const long long* dn = reinterpret_cast<const long long*>(denom);
-    if (!dn) {
-        st = ce_launch_count(mask, T, reinterpret_cast<long long*>(ws), s);
-        if (st != RLF_OK) return st;
-        dn = reinterpret_cast<const long long*>(ws);
-    }
+    int2* list = reinterpret_cast<int2*>(ws + ws_list_off(T));
+    long long* n_mask = reinterpret_cast<long long*>(ws);
+    int* n_live = reinterpret_cast<int*>(ws + 64);
+    st = ce_launch_plan(ids, mask, T, V, list, n_live, n_mask, dev_status, s);
+    if (st != RLF_OK) return st;
+    const long long* dn = denom ? reinterpret_cast<const long long*>(denom) : n_mask;
     RowParams p;
-    p.logits = logits; p.grad = grad_logits; p.stride = row_stride; p.T = T; p.V = V; p.ids = ids; p.mask = mask;
+    p.logits = logits; p.grad = grad_logits; p.stride = row_stride; p.T = T; p.V = V; p.list = list; p.n_live = n_live;
     p.denom = dn; p.logp_out = logp_out; p.lse_out = lse_out; p.terms = reinterpret_cast<float4*>(ws + kWsTermsOff);
     p.dev_status = dev_status; p.eps = label_smoothing; p.zeta = z_coef;
     if (T > 0) {

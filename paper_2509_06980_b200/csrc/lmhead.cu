@@ -1754,76 +1754,11 @@ extern "C" rlf_status rlf_fused_lmhead_logp_entropy(const void* hidden, const vo
 namespace rlf {
 namespace lm {
 
-// One CTA turns mask and ids into the work list: idx_live / y_live (rows that carry loss, in token order),
-// idx_dead (the others), counts[0 / 1], and the number of rows with mask != 0.  Four tokens per thread
-// and step.
-__global__ void __launch_bounds__(1024)
-ce_plan_kernel(const int32_t* __restrict__ ids, const uint8_t* __restrict__ mask, int T, int V,
-               int32_t* __restrict__ idx_live, int32_t* __restrict__ y_live, int32_t* __restrict__ idx_dead,
-               int* __restrict__ counts, long long* __restrict__ n_mask, int32_t* __restrict__ dev_status) {
-    __shared__ int warp_tot[32];
-    __shared__ int masked_s[32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int base = 0, masked_in = 0;
-    bool bad = false;
-    for (int t0 = 0; t0 < T; t0 += 4096) {
-        int y[4], live[4], mine = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int t = t0 + 4 * tid + k;
-            const bool in = t < T && (mask == nullptr || mask[t] != 0);
-            y[k] = in ? ids[t] : 0;
-            live[k] = in && y[k] >= 0 && y[k] < V;
-            masked_in += in;
-            bad |= in && !live[k];
-            mine += live[k];
-        }
-        int incl = mine;                                   // inclusive scan over the warp
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += up;
-        }
-        if (lane == 31) warp_tot[warp] = incl;
-        __syncthreads();
-        int before = base + incl - mine, total = 0;
-        for (int w = 0; w < 32; ++w) {
-            if (w < warp) before += warp_tot[w];
-            total += warp_tot[w];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int t = t0 + 4 * tid + k;
-            if (live[k]) {
-                idx_live[before] = t;
-                y_live[before] = y[k];
-                ++before;
-            } else if (t < T) {
-                idx_dead[t - before] = t;
-            }
-        }
-        base += total;
-    }
-    if (bad && dev_status) atomicOr(dev_status, RLF_DEV_BAD_TARGET);
-    masked_in = __reduce_add_sync(0xffffffffu, masked_in);
-    if (lane == 0) masked_s[warp] = masked_in;
-    __syncthreads();
-    if (tid == 0) {
-        long long n = 0;
-        for (int w = 0; w < 32; ++w) n += masked_s[w];
-        *n_mask = n;
-        counts[0] = base;
-        counts[1] = T - base;
-    }
-}
-
-// compact row r <- hidden row idx[r] for r < *count, its target logit, its mean logit (with u) and the
+// compact row r <- hidden row of work-list entry r for r < *count, its target logit, its mean logit (with u) and the
 // reference of its stored exponentials; rows up to the next multiple of 256 are zero-filled
 __global__ void __launch_bounds__(128)
 ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloat16* __restrict__ W, int D,
-                      const int32_t* __restrict__ idx, const int32_t* __restrict__ y_live, const int* __restrict__ count,
-                      const float* __restrict__ u, float inv_v, __nv_bfloat16* __restrict__ out, float* __restrict__ zy_g,
+                      const int2* __restrict__ list, const int* __restrict__ count, const float* __restrict__ u, float inv_v, __nv_bfloat16* __restrict__ out, int32_t* __restrict__ idx, float* __restrict__ zy_g,
                       float* __restrict__ mean_g, float* __restrict__ ref_g) {
     __shared__ float red[2][4];
     const int n = *count;
@@ -1836,8 +1771,9 @@ ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloa
         if (threadIdx.x == 0) ref_g[r] = 0.0f;
         return;
     }
-    const uint4* src = reinterpret_cast<const uint4*>(hidden + (long long)idx[r] * D);
-    const uint4* w = reinterpret_cast<const uint4*>(W + (long long)y_live[r] * D);
+    const int2 job = list[r];
+    const uint4* src = reinterpret_cast<const uint4*>(hidden + (long long)job.x * D);
+    const uint4* w = reinterpret_cast<const uint4*>(W + (long long)job.y * D);
     float a = 0.0f, b = 0.0f;
     for (int i = threadIdx.x; i < nv; i += 128) {
         const uint4 h = src[i], ww = w[i];
@@ -1863,6 +1799,7 @@ ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloa
     __syncthreads();
     if (threadIdx.x == 0) {
         const float zy = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
+        idx[r] = job.x;                    // (the gradient contraction's epilogue looks its output rows up here)
         zy_g[r] = zy;
         mean_g[r] = ((red[1][0] + red[1][1]) + (red[1][2] + red[1][3])) * inv_v;
         ref_g[r] = zy + kRefShift;
@@ -1871,11 +1808,10 @@ ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloa
 
 // rows without loss: NaN statistics, no loss term, a zero row of grad_hidden
 __global__ void __launch_bounds__(128)
-ce_dead_rows_kernel(const int32_t* __restrict__ idx, const int* __restrict__ count, int D, float* __restrict__ logp_out,
-                    float* __restrict__ lse_out, float4* __restrict__ terms, __nv_bfloat16* __restrict__ grad_hidden) {
-    const int r = blockIdx.x;
-    if (r >= *count) return;
-    const int t = idx[r];
+ce_dead_rows_kernel(const int2* __restrict__ list, const int* __restrict__ count, int T, int D,
+                    float* __restrict__ logp_out, float* __restrict__ lse_out, float4* __restrict__ terms, __nv_bfloat16* __restrict__ grad_hidden) {
+    if ((int)blockIdx.x >= T - *count) return;
+    const int t = list[T - 1 - (int)blockIdx.x].x;
     if (threadIdx.x == 0) {
         const float nan = __int_as_float(0x7fc00000);
         logp_out[t] = nan;
@@ -1890,8 +1826,7 @@ ce_dead_rows_kernel(const int32_t* __restrict__ idx, const int* __restrict__ cou
 struct CeCombine {
     const float2* part;
     int nsplit, rows_max;
-    const int32_t* idx;
-    const int32_t* y_live;
+    const int2* list;
     const int* count;
     int off;
     const float* zy_g;
@@ -1925,7 +1860,9 @@ ce_combine_rows_kernel(const CeCombine p) {
     const int r = blockIdx.x * blockDim.x + threadIdx.x;
     const int n = max(0, min(*p.count - p.off, p.rows_max));
     if (r >= n) return;
-    const int g = p.off + r, t = p.idx[g];
+    const int g = p.off + r;
+    const int2 job = p.list[g];
+    const int t = job.x;
     const float2* parts = p.part + (long long)r * p.nsplit;
     float M = -INFINITY;
     for (int j = 0; j < p.nsplit; ++j) M = fmaxf(M, parts[j].x);
@@ -1960,14 +1897,14 @@ ce_combine_rows_kernel(const CeCombine p) {
     if (p.ref_g) {
         const float rho = p.ref_g[g];
         p.scale_g[g] = c * A * expf(rho - lse);
-        p.dz[dz_offset(r, p.y_live[g], p.dz_nc)] = __float2bfloat16_rn(tgt / A * expf(lse - rho));
+        p.dz[dz_offset(r, job.y, p.dz_nc)] = __float2bfloat16_rn(tgt / A * expf(lse - rho));
         return;
     }
     p.scale_g[g] = ok ? 1.0f : 0.0f;
     p.lse_g[g] = ok ? lse : 0.0f;
     p.coef_g[g] = ok ? c * A : 0.0f;
     p.tgt_g[g] = c * tgt;
-    p.ok_y[g] = ok ? p.y_live[g] : -1;
+    p.ok_y[g] = ok ? job.y : -1;
 }
 
 // out[d] = sum_r weight[r] M[r, d] (weight NULL: 1) over the rows r < rows (or *count - off, if given and less):
@@ -2043,7 +1980,7 @@ static rlf_status launch_colsum(const __nv_bfloat16* M, int64_t rows, int32_t D,
 }
 
 struct CeWs {
-    size_t head, terms, zy, mean, part, idx_live, idx_dead, y_live, ok_y, lse_g, coef_g, tgt_g, add_g, ref_g, scale_g, ucol,
+    size_t head, terms, list, zy, mean, part, idx_live, ok_y, lse_g, coef_g, tgt_g, add_g, ref_g, scale_g, ucol,
         gcol, col_part, hidden_g, hidden_s, tmax, gw_acc, dz, total;
 };
 static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
@@ -2053,14 +1990,13 @@ static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
     const size_t chunk = Tp < (size_t)kChunkTokens ? Tp : (size_t)kChunkTokens;
     const size_t tiles = (size_t)((V + BN - 1) / BN);
     auto take = [&](size_t bytes) { const size_t at = o; o += up1k(bytes); return at; };
-    w.head = take(1024);             // [0] mask count, [64] live / other rows, [128] chunk flag, [256] pacing counter
+    w.head = take(1024);             // [0] mask count, [64] live rows, [128] chunk flag, [256] pacing counter
     w.terms = take(16 * Tn);
+    w.list = take(8 * Tn);
     w.zy = take(4 * Tp);
     w.mean = take(4 * Tp);
     w.part = take(8 * Tn * kMaxSplit);
     w.idx_live = take(4 * Tp);
-    w.idx_dead = take(4 * Tp);
-    w.y_live = take(4 * Tp);
     w.ok_y = take(4 * Tp);
     w.lse_g = take(4 * Tp);
     w.coef_g = take(4 * Tp);
@@ -2127,7 +2063,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     if (T == 0) {
         // no rows: a zero loss, and a gradient of zero unless it is accumulated
         if (!denom) {
-            st = ce_launch_count(nullptr, 0, n_mask, s);
+            st = ce_launch_plan(nullptr, nullptr, 0, V, nullptr, counts, n_mask, dev_status, s);
             if (st != RLF_OK) return st;
         }
         if (grad_W && !accumulate_grad_W &&
@@ -2137,8 +2073,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     }
 
     int32_t* idx_live = reinterpret_cast<int32_t*>(ws + w.idx_live);
-    int32_t* idx_dead = reinterpret_cast<int32_t*>(ws + w.idx_dead);
-    int32_t* y_live = reinterpret_cast<int32_t*>(ws + w.y_live);
+    int2* list = reinterpret_cast<int2*>(ws + w.list);
     __nv_bfloat16* Hl = reinterpret_cast<__nv_bfloat16*>(ws + w.hidden_g);
     __nv_bfloat16* Hs = reinterpret_cast<__nv_bfloat16*>(ws + w.hidden_s);
     __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + w.dz);
@@ -2146,16 +2081,16 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     const bool bwd = grad_hidden || grad_W, smoothing = label_smoothing > 0.0f;
     const bool row_ref = bwd && g_row_ref.load() != 0;
     float* ucol = smoothing ? at(w.ucol) : nullptr;
-    ce_plan_kernel<<<1, 1024, 0, s>>>(ids, mask, (int)T, V, idx_live, y_live, idx_dead, counts, n_mask, dev_status);
-    count_launch();
+    st = ce_launch_plan(ids, mask, T, V, list, counts, n_mask, dev_status, s);
+    if (st != RLF_OK) return st;
     if (smoothing) {
         st = launch_colsum(Wm, V, D, nullptr, nullptr, 0, at(w.col_part), ucol, s);
         if (st != RLF_OK) return st;
     }
     const float inv_v = 1.0f / (float)V;
-    ce_gather_rows_kernel<<<(unsigned)Tp, 128, 0, s>>>(H, Wm, D, idx_live, y_live, counts, ucol, inv_v, Hl, at(w.zy),
+    ce_gather_rows_kernel<<<(unsigned)Tp, 128, 0, s>>>(H, Wm, D, list, counts, ucol, inv_v, Hl, idx_live, at(w.zy),
                                                        at(w.mean), at(w.ref_g));
-    ce_dead_rows_kernel<<<(unsigned)T, 128, 0, s>>>(idx_dead, counts + 1, D, logp_out, lse_out, terms,
+    ce_dead_rows_kernel<<<(unsigned)T, 128, 0, s>>>(list, counts, (int)T, D, logp_out, lse_out, terms,
                                                     static_cast<__nv_bfloat16*>(grad_hidden));
     count_launch(2);
     if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
@@ -2192,7 +2127,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             z.tmax = at(w.tmax);
         }
         CeCombine c = {};
-        c.part = z.part; c.nsplit = z.nsplit; c.rows_max = (int)tc; c.idx = idx_live; c.y_live = y_live; c.count = counts;
+        c.part = z.part; c.nsplit = z.nsplit; c.rows_max = (int)tc; c.list = list; c.count = counts;
         c.off = (int)t0; c.zy_g = at(w.zy); c.mean_g = at(w.mean); c.denom = dn; c.eps = label_smoothing; c.zeta = z_coef;
         c.inv_v = inv_v; c.logp_out = logp_out; c.lse_out = lse_out; c.terms = terms; c.dev_status = dev_status;
         if (bwd) {
