@@ -9,6 +9,10 @@
 // Both directions are bound by HBM: a row is read once and written once (about 10 arithmetic
 // instructions per element).  All sums and statistics are fp32; the sum h is rounded to the
 // activations' type only where it is stored, and y is formed from the unrounded h.
+#include <map>
+#include <mutex>
+#include <tuple>
+
 #include "common.cuh"
 
 namespace rlf {
@@ -168,30 +172,745 @@ norm_dw_general_kernel(const BwdParams p, long long rows_per_slice) {
     }
 }
 
-// partial rows -> gradient, added in a fixed order (results are run-to-run identical).  A CTA covers 32
-// columns; warp w adds the partials w, w + 8, ... and the eight sums are added in order.
-__global__ void __launch_bounds__(256)
+// partial rows -> gradient, added in a fixed order (results are run-to-run identical).  A CTA covers 32 columns; warp w
+// adds the partials w, w + 32, ... and the 32 sums are added in order.  It may be set up while the kernel before it
+// still runs (programmatic dependent launch) and waits for that kernel's results here.
+__global__ void __launch_bounds__(1024)
 norm_dw_reduce_kernel(const float* __restrict__ part, const float* __restrict__ part_b, int parts, int D, int accumulate,
                       float* __restrict__ dw, float* __restrict__ db) {
-    __shared__ float acc[8][32];
+    __shared__ float acc[32][33];
     const float* src = blockIdx.y == 0 ? part : part_b;
     float* dst = blockIdx.y == 0 ? dw : db;
     if (dst == nullptr) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int col = blockIdx.x * 32 + lane;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     float s = 0.0f;
-    if (col < D)
-        for (int k = warp; k < parts; k += 8) s += src[(long long)k * D + col];
+    if (col < D) {
+#pragma unroll 4
+        for (int k = warp; k < parts; k += 32) s += src[(long long)k * D + col];
+    }
     acc[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && col < D) {
-        for (int w = 1; w < 8; ++w) s += acc[w][lane];
+        for (int w = 1; w < 32; ++w) s += acc[w][lane];
         dst[col] = accumulate ? dst[col] + s : s;
     }
 }
 
-// Most partial rows of a weight gradient; sizes the workspace.
-constexpr int kMaxParts = 1024;
+// ---- fast forms -----------------------------------------------------------------------------
+// A CTA works on R rows at a time, with the next R rows on their way into the other half of a shared-memory buffer
+// (cp.async), so that HBM is kept busy through the sums' exchanges; the rows stay in shared memory between the pass that
+// sums and the pass that writes.  One exchange (one barrier) serves the R rows' sums.
+//   wide    every row starts on 16 bytes and the width fills its 16-byte vectors: a thread owns NV vectors of each row, copies
+//           them itself and reads back only those; its columns' weights and weight gradients live in registers;
+//   staged  any width, stride and base: a row is copied as the aligned 16-byte chunks that cover it, by whichever thread, and a
+//           thread owns every blockDim-th column; weights and weight gradients live in shared memory.
+constexpr int kMaxThreads = 512;
+constexpr int kSmemLimit = 200 * 1024;           // most dynamic shared memory that a fast form asks for
+
+__device__ __forceinline__ void cp_async16(uint32_t smem_dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(smem_dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async16_part(uint32_t smem_dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(smem_dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_wait1() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_wait0() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// Pairs of fp32 values in one register pair: one instruction for two additions, products or multiply-adds (at one each the
+// fast forms are bound by instruction issue before HBM).
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 f2_make(float lo, float hi) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void f2_split(f2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f2 f2_add(f2 a, f2 b) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 f2_mul(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 f2_fma(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float f2_sum(f2 v) {
+    float a, b;
+    f2_split(v, a, b);
+    return a + b;
+}
+
+// 16-byte vectors of either type as pairs
+template <typename T> struct Vec;
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int N = 8, P = 4;
+    static __device__ __forceinline__ void unpack(const uint4& r, f2 (&f)[4]) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] = f2_make(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
+    }
+    static __device__ __forceinline__ uint4 pack(const f2 (&f)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float lo, hi;
+            f2_split(f[k], lo, hi);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(hi), "f"(lo));
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <> struct Vec<float> {
+    static constexpr int N = 4, P = 2;
+    static __device__ __forceinline__ void unpack(const uint4& r, f2 (&f)[2]) {
+        f[0] = f2_make(__uint_as_float(r.x), __uint_as_float(r.y));
+        f[1] = f2_make(__uint_as_float(r.z), __uint_as_float(r.w));
+    }
+    static __device__ __forceinline__ uint4 pack(const f2 (&f)[2]) {
+        float a, b, c, d;
+        f2_split(f[0], a, b);
+        f2_split(f[1], c, d);
+        return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+    }
+};
+
+// K sums over the CTA at once, each the same in every thread afterwards.  Inside a warp the K values are halved with every
+// exchange (a lane passes on the half that its partner keeps), K - 1 + 5 - log2 K shuffles instead of 5 K; across warps they
+// go through `red` (two halves of [16][K] floats used in turn: one barrier per call).
+template <int K>
+__device__ __forceinline__ void cta_sums(float (&v)[K], float* red, int& turn) {
+    static_assert(K == 1 || K == 2 || K == 4 || K == 8, "power of two");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    int o = 16;
+    float w[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) w[k] = v[k];
+#pragma unroll
+    for (int n = K; n > 1; n >>= 1, o >>= 1) {
+        const bool up = (lane & o) != 0;
+#pragma unroll
+        for (int k = 0; k < n / 2; ++k) {
+            const float keep = up ? w[k + n / 2] : w[k], give = up ? w[k] : w[k + n / 2];
+            w[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    float t = w[0];
+#pragma unroll
+    for (; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    // a lane now holds the sum whose number its top log2 K bits spell
+    constexpr int kShift = K == 1 ? 5 : K == 2 ? 4 : K == 4 ? 3 : 2;
+    if (warps == 1) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = __shfl_sync(0xffffffffu, t, k << kShift);
+        return;
+    }
+    float* r = red + turn * (kMaxThreads / 32) * K;
+    turn ^= 1;
+    if ((lane & ((1 << kShift) - 1)) == 0) r[warp * K + (lane >> kShift)] = t;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = 0.0f;
+    for (int q = 0; q < warps; ++q) {
+        if constexpr (K >= 4) {
+#pragma unroll
+            for (int k = 0; k < K; k += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(r + q * K + k);
+                v[k] += x.x; v[k + 1] += x.y; v[k + 2] += x.z; v[k + 3] += x.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] += r[q * K + k];
+        }
+    }
+}
+
+// weights of a thread's columns, widened (0 beyond the width or without a vector)
+template <int P, int NV>
+__device__ __forceinline__ void load_w(const void* w, int w_bf16, int D, f2 (&f)[NV][P]) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            const int c = ((i * (int)blockDim.x + (int)threadIdx.x) * P + e) * 2;
+            const bool in = w != nullptr && c < D;               // the width fills its vectors: c + 1 is in it too
+            f[i][e] = in ? f2_make(ld_w(w, w_bf16, c), ld_w(w, w_bf16, c + 1)) : 0ull;
+        }
+}
+
+// Forward.  The rows' elements (x + residual) are held unpacked in registers through the passes.
+template <typename T, int NV, int R, bool LAYER>
+__global__ void __launch_bounds__(kMaxThreads)
+norm_fwd_wide_kernel(const FwdParams p) {
+    using V = Vec<T>;
+    constexpr int P = V::P, N = V::N;
+    extern __shared__ __align__(16) uint4 stage[];      // [2][R][arrays][NV][blockDim], a slot is its thread's own
+    __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * R];
+    int turn = 0;
+    const int nvec = p.D / N, th = blockDim.x, tid = threadIdx.x;
+    const int arrays = p.res ? 2 : 1;
+    const float inv_d = 1.0f / (float)p.D;
+    auto slot = [&](int buf, int k, int a, int i) -> uint4* { return stage + (((buf * R + k) * arrays + a) * NV + i) * th + tid; };
+    auto fetch = [&](long long t0, int buf) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const long long t = t0 + k;
+            if (t < p.T) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = tid + i * th;
+                    if (c < nvec) {
+                        cp_async16(smem_at(slot(buf, k, 0, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + t * p.x_stride) + c);
+                        if (p.res) cp_async16(smem_at(slot(buf, k, 1, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.res) + t * p.x_stride) + c);
+                    }
+                }
+            }
+        }
+        cp_async_commit();
+    };
+    const long long step = (long long)gridDim.x * R;
+    long long t0 = (long long)blockIdx.x * R;
+    fetch(t0, 0);
+    f2 w[NV][P], b[LAYER ? NV : 1][P];                  // (the RMS form's bias, rare, is fetched where it is used)
+    load_w<P, NV>(p.w, p.w_bf16, p.D, w);
+    if constexpr (LAYER) load_w<P, NV>(p.b, p.w_bf16, p.D, b);
+    for (int buf = 0; t0 < p.T; t0 += step, buf ^= 1) {
+        fetch(t0 + step, buf ^ 1);
+        cp_async_wait1();
+        f2 h[R][NV][P];
+        float s[R], mu[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            f2 q = 0ull;
+            mu[k] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (tid + i * th < nvec) {
+                    V::unpack(*slot(buf, k, 0, i), h[k][i]);
+                    if (p.res) {
+                        f2 z[P];
+                        V::unpack(*slot(buf, k, 1, i), z);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) h[k][i][e] = f2_add(h[k][i][e], z[e]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < P; ++e) q = LAYER ? f2_add(q, h[k][i][e]) : f2_fma(h[k][i][e], h[k][i][e], q);
+                }
+            s[k] = f2_sum(q);
+        }
+        cta_sums<R>(s, red, turn);
+        if (LAYER) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                mu[k] = s[k] * inv_d;
+                const f2 m2 = f2_make(-mu[k], -mu[k]);
+                f2 q = 0ull;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (tid + i * th < nvec) {
+#pragma unroll
+                        for (int e = 0; e < P; ++e) {
+                            const f2 d = f2_add(h[k][i][e], m2);
+                            q = f2_fma(d, d, q);
+                        }
+                    }
+                s[k] = f2_sum(q);
+            }
+            cta_sums<R>(s, red, turn);
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const long long t = t0 + k;
+            if (t >= p.T) continue;
+            const float r = rsqrtf(s[k] * inv_d + p.eps);
+            const f2 r2 = f2_make(r, r), m2 = f2_make(-mu[k], -mu[k]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = tid + i * th;
+                if (c >= nvec) continue;
+                f2 o[P];
+                if (p.sum) reinterpret_cast<uint4*>(static_cast<T*>(p.sum) + t * p.D)[c] = V::pack(h[k][i]);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    o[e] = f2_mul(f2_mul(LAYER ? f2_add(h[k][i][e], m2) : h[k][i][e], r2), w[i][e]);
+                    if (LAYER) o[e] = f2_add(o[e], b[LAYER ? i : 0][e]);
+                    else if (p.b) o[e] = f2_add(o[e], f2_make(ld_w(p.b, p.w_bf16, c * N + 2 * e), ld_w(p.b, p.w_bf16, c * N + 2 * e + 1)));
+                }
+                reinterpret_cast<uint4*>(static_cast<T*>(p.y) + t * p.D)[c] = V::pack(o);
+            }
+            if (tid == 0) {
+                if (p.mean) p.mean[t] = mu[k];
+                if (p.rstd) p.rstd[t] = r;
+            }
+        }
+    }
+    cp_async_wait0();
+}
+
+// Backward: a CTA owns the row.  One sum per row, mean(g xh), and with FULL (layer form, or a bias gradient asked for) also
+// mean(g) and the bias gradient; a CTA's weight gradients are added up row after row and leave as one partial row per CTA.
+template <typename T, int NV, int R, bool FULL>
+__global__ void __launch_bounds__(kMaxThreads)
+norm_bwd_wide_kernel(const BwdParams p) {
+    using V = Vec<T>;
+    constexpr int P = V::P, N = V::N, K = FULL ? 2 * R : R;
+    extern __shared__ __align__(16) uint4 stage[];      // [2][R][dy, x (, skip)][NV][blockDim]
+    __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * K];
+    int turn = 0;
+    const int nvec = p.D / N, th = blockDim.x, tid = threadIdx.x;
+    const int arrays = p.skip ? 3 : 2;
+    const float inv_d = 1.0f / (float)p.D;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    auto slot = [&](int buf, int k, int a, int i) -> uint4* { return stage + (((buf * R + k) * arrays + a) * NV + i) * th + tid; };
+    float mu_next[R], r_next[R];
+    auto fetch = [&](long long t0, int buf) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const long long t = t0 + k;
+            mu_next[k] = r_next[k] = 0.0f;
+            if (t < p.T) {
+                if (FULL && p.layer) mu_next[k] = p.mean[t];
+                r_next[k] = p.rstd[t];
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = tid + i * th;
+                    if (c < nvec) {
+                        cp_async16(smem_at(slot(buf, k, 0, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.dy) + t * p.dy_stride) + c);
+                        cp_async16(smem_at(slot(buf, k, 1, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + t * p.x_stride) + c);
+                        if (p.skip) cp_async16(smem_at(slot(buf, k, 2, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.skip) + t * p.D) + c);
+                    }
+                }
+            }
+        }
+        cp_async_commit();
+    };
+    const long long step = (long long)gridDim.x * R;
+    long long t0 = (long long)blockIdx.x * R;
+    fetch(t0, 0);
+    f2 w[NV][P], dw[NV][P], db[FULL ? NV : 1][P];
+    load_w<P, NV>(p.w, p.w_bf16, p.D, w);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            dw[i][e] = 0ull;
+            if (FULL) db[FULL ? i : 0][e] = 0ull;
+        }
+    for (int buf = 0; t0 < p.T; t0 += step, buf ^= 1) {
+        float mu[R], r[R], s[K];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            mu[k] = mu_next[k];
+            r[k] = r_next[k];
+        }
+        fetch(t0 + step, buf ^ 1);
+        cp_async_wait1();
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            f2 a = 0ull, b = 0ull;
+            if (t0 + k < p.T) {
+                const f2 m2 = f2_make(-mu[k], -mu[k]), r2 = f2_make(r[k], r[k]);
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (tid + i * th < nvec) {
+                        f2 x[P], dy[P];
+                        V::unpack(*slot(buf, k, 0, i), dy);
+                        V::unpack(*slot(buf, k, 1, i), x);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) {
+                            const f2 xh = f2_mul(FULL ? f2_add(x[e], m2) : x[e], r2), q = f2_mul(dy[e], xh);
+                            a = f2_fma(q, w[i][e], a);
+                            dw[i][e] = f2_add(dw[i][e], q);
+                            if (FULL) {
+                                b = f2_fma(dy[e], w[i][e], b);
+                                db[FULL ? i : 0][e] = f2_add(db[FULL ? i : 0][e], dy[e]);
+                            }
+                        }
+                    }
+            }
+            s[k] = f2_sum(a);
+            if (FULL) s[FULL ? R + k : 0] = f2_sum(b);
+        }
+        if (p.dx == nullptr) continue;
+        cta_sums<K>(s, red, turn);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const long long t = t0 + k;
+            if (t >= p.T) continue;
+            // r (g - b - (x - mu) r a) = r g + x (- r^2 a) + (mu r^2 a - r b)
+            const float a = s[k] * inv_d * r[k] * r[k];
+            const float b = (FULL && p.layer) ? r[k] * (s[FULL ? R + k : 0] * inv_d) : 0.0f;
+            const f2 r2 = f2_make(r[k], r[k]), a2 = f2_make(-a, -a), b2 = f2_make(-b, -b), m2 = f2_make(-mu[k], -mu[k]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = tid + i * th;
+                if (c >= nvec) continue;
+                f2 x[P], dy[P], o[P];
+                V::unpack(*slot(buf, k, 0, i), dy);
+                V::unpack(*slot(buf, k, 1, i), x);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    o[e] = f2_mul(f2_mul(dy[e], w[i][e]), r2);
+                    if (FULL) o[e] = f2_add(o[e], b2);
+                    o[e] = f2_fma(FULL ? f2_add(x[e], m2) : x[e], a2, o[e]);
+                }
+                if (p.skip) {
+                    f2 q[P];
+                    V::unpack(*slot(buf, k, 2, i), q);
+#pragma unroll
+                    for (int e = 0; e < P; ++e) o[e] = f2_add(o[e], q[e]);
+                }
+                reinterpret_cast<uint4*>(static_cast<T*>(p.dx) + t * p.D)[c] = V::pack(o);
+            }
+        }
+    }
+    cp_async_wait0();
+    auto leave = [&](float* part, const f2 (&g)[P], int i) {
+        const int c = (tid + i * th) * N;
+        if (part == nullptr || c >= p.D) return;
+        ulonglong2* d = reinterpret_cast<ulonglong2*>(part + (long long)blockIdx.x * p.D + c);
+#pragma unroll
+        for (int e = 0; e < P; e += 2) d[e / 2] = make_ulonglong2(g[e], g[e + 1]);
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        leave(p.part, dw[i], i);
+        if (FULL) leave(p.part_b, db[FULL ? i : 0], i);
+    }
+}
+
+// A row of any alignment into shared memory, by the whole CTA: the aligned 16-byte chunks that cover it.  Returns where its
+// element 0 then lies.  Only the row's own bytes and, before them, bytes of the chunk it starts in are read; a tensor's first
+// row, before which there may be nothing, has the elements of that chunk copied one by one.
+__device__ __forceinline__ int chunk_head(const void* src) { return (int)(reinterpret_cast<uintptr_t>(src) & 15); }
+template <typename T>
+__device__ __forceinline__ void copy_row(char* dst, const T* src, int D, bool first) {
+    const int head = chunk_head(src), bytes = head + D * (int)sizeof(T);
+    const char* from = reinterpret_cast<const char*>(src) - head;
+    for (int o = 16 * threadIdx.x; o < bytes; o += 16 * blockDim.x) {
+        if (first && o < head) {
+            for (int e = head; e < 16 && e < bytes; e += (int)sizeof(T)) *reinterpret_cast<T*>(dst + e) = *reinterpret_cast<const T*>(from + e);
+        } else {
+            cp_async16_part(smem_at(dst + o), from + o, min(16, bytes - o));
+        }
+    }
+}
+__host__ __device__ constexpr int staged_pitch(int D, int esz) { return (D * esz + 15 + 16) / 16 * 16; }
+
+template <typename T, int R, bool LAYER>
+__global__ void __launch_bounds__(kMaxThreads)
+norm_fwd_staged_kernel(const FwdParams p) {
+    extern __shared__ __align__(16) char smem[];        // [2][R][arrays] rows, then the weights (and biases) in fp32
+    __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * R];
+    int turn = 0;
+    const int th = blockDim.x, tid = threadIdx.x, D = p.D;
+    const int arrays = p.res ? 2 : 1, pitch = staged_pitch(D, (int)sizeof(T));
+    const float inv_d = 1.0f / (float)D;
+    float* w_s = reinterpret_cast<float*>(smem + 2 * R * arrays * pitch);
+    float* b_s = w_s + D;
+    auto at = [&](int buf, int k, int a) -> char* { return smem + ((buf * R + k) * arrays + a) * pitch; };
+    auto fetch = [&](long long t0, int buf) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const long long t = t0 + k;
+            if (t < p.T) {
+                copy_row(at(buf, k, 0), static_cast<const T*>(p.x) + t * p.x_stride, D, t == 0);
+                if (p.res) copy_row(at(buf, k, 1), static_cast<const T*>(p.res) + t * p.x_stride, D, t == 0);
+            }
+        }
+        cp_async_commit();
+    };
+    const long long step = (long long)gridDim.x * R;
+    long long t0 = (long long)blockIdx.x * R;
+    fetch(t0, 0);
+    for (int c = tid; c < D; c += th) {
+        w_s[c] = ld_w(p.w, p.w_bf16, c);
+        if (p.b) b_s[c] = ld_w(p.b, p.w_bf16, c);
+    }
+    for (int buf = 0; t0 < p.T; t0 += step, buf ^= 1) {
+        __syncthreads();                                // the other half has been read by everyone
+        fetch(t0 + step, buf ^ 1);
+        cp_async_wait1();
+        __syncthreads();                                // everyone's chunks of this half are here
+        const T* x[R];
+        const T* res[R];
+        float s[R], mu[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const long long t = min(t0 + k, p.T - 1);
+            x[k] = reinterpret_cast<const T*>(at(buf, k, 0) + chunk_head(static_cast<const T*>(p.x) + t * p.x_stride));
+            res[k] = p.res ? reinterpret_cast<const T*>(at(buf, k, 1) + chunk_head(static_cast<const T*>(p.res) + t * p.x_stride)) : x[k];
+            s[k] = mu[k] = 0.0f;
+        }
+        auto h = [&](int k, int c) -> float { return to_f<T>(x[k][c]) + (p.res ? to_f<T>(res[k][c]) : 0.0f); };
+#pragma unroll 2
+        for (int c = tid; c < D; c += th)
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                const float v = h(k, c);
+                s[k] = LAYER ? s[k] + v : fmaf(v, v, s[k]);
+            }
+        cta_sums<R>(s, red, turn);
+        if (LAYER) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                mu[k] = s[k] * inv_d;
+                s[k] = 0.0f;
+            }
+#pragma unroll 2
+            for (int c = tid; c < D; c += th)
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    const float v = h(k, c) - mu[k];
+                    s[k] = fmaf(v, v, s[k]);
+                }
+            cta_sums<R>(s, red, turn);
+        }
+        float r[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            r[k] = rsqrtf(s[k] * inv_d + p.eps);
+            if (tid == 0 && t0 + k < p.T) {
+                if (p.mean) p.mean[t0 + k] = mu[k];
+                if (p.rstd) p.rstd[t0 + k] = r[k];
+            }
+        }
+#pragma unroll 2
+        for (int c = tid; c < D; c += th) {
+            const float wc = w_s[c], bc = p.b ? b_s[c] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (t0 + k >= p.T) continue;
+                const float v = h(k, c);
+                if (p.sum) static_cast<T*>(p.sum)[(t0 + k) * D + c] = from_f<T>(v);
+                static_cast<T*>(p.y)[(t0 + k) * D + c] = from_f<T>((v - mu[k]) * r[k] * wc + bc);
+            }
+        }
+    }
+    cp_async_wait0();
+}
+
+template <typename T, int R, bool FULL>
+__global__ void __launch_bounds__(kMaxThreads)
+norm_bwd_staged_kernel(const BwdParams p) {
+    extern __shared__ __align__(16) char smem[];        // [2][R][dy, x (, skip)] rows, then w, dw (and db) in fp32
+    __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * 2 * R];
+    int turn = 0;
+    const int th = blockDim.x, tid = threadIdx.x, D = p.D;
+    const int arrays = p.skip ? 3 : 2, pitch = staged_pitch(D, (int)sizeof(T));
+    const float inv_d = 1.0f / (float)D;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    float* w_s = reinterpret_cast<float*>(smem + 2 * R * arrays * pitch);
+    float* dw_s = w_s + D;
+    float* db_s = dw_s + D;
+    auto at = [&](int buf, int k, int a) -> char* { return smem + ((buf * R + k) * arrays + a) * pitch; };
+    auto fetch = [&](long long t0, int buf) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const long long t = t0 + k;
+            if (t < p.T) {
+                copy_row(at(buf, k, 0), static_cast<const T*>(p.dy) + t * p.dy_stride, D, t == 0);
+                copy_row(at(buf, k, 1), static_cast<const T*>(p.x) + t * p.x_stride, D, t == 0);
+                if (p.skip) copy_row(at(buf, k, 2), static_cast<const T*>(p.skip) + t * D, D, t == 0);
+            }
+        }
+        cp_async_commit();
+    };
+    const long long step = (long long)gridDim.x * R;
+    long long t0 = (long long)blockIdx.x * R;
+    fetch(t0, 0);
+    for (int c = tid; c < D; c += th) {
+        w_s[c] = ld_w(p.w, p.w_bf16, c);
+        dw_s[c] = 0.0f;
+        if (FULL && p.part_b) db_s[c] = 0.0f;
+    }
+    for (int buf = 0; t0 < p.T; t0 += step, buf ^= 1) {
+        __syncthreads();
+        fetch(t0 + step, buf ^ 1);
+        const T* dy[R];
+        const T* x[R];
+        const T* skip[R];
+        float mu[R], r[R], s[2 * R];
+        bool row[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            row[k] = t0 + k < p.T;
+            const long long t = min(t0 + k, p.T - 1);
+            dy[k] = reinterpret_cast<const T*>(at(buf, k, 0) + chunk_head(static_cast<const T*>(p.dy) + t * p.dy_stride));
+            x[k] = reinterpret_cast<const T*>(at(buf, k, 1) + chunk_head(static_cast<const T*>(p.x) + t * p.x_stride));
+            skip[k] = p.skip ? reinterpret_cast<const T*>(at(buf, k, 2) + chunk_head(static_cast<const T*>(p.skip) + t * D)) : x[k];
+            mu[k] = p.layer ? p.mean[t] : 0.0f;
+            r[k] = p.rstd[t];
+            s[2 * k] = s[2 * k + 1] = 0.0f;
+        }
+        cp_async_wait1();
+        __syncthreads();
+#pragma unroll 2
+        for (int c = tid; c < D; c += th) {
+            const float wc = w_s[c];
+            float qs = 0.0f, ds = 0.0f;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (!row[k]) continue;
+                const float d = to_f<T>(dy[k][c]), q = d * ((to_f<T>(x[k][c]) - mu[k]) * r[k]);
+                s[2 * k] = fmaf(q, wc, s[2 * k]);
+                if (FULL) s[2 * k + 1] = fmaf(d, wc, s[2 * k + 1]);
+                qs += q;
+                ds += d;
+            }
+            dw_s[c] += qs;
+            if (FULL && p.part_b) db_s[c] += ds;
+        }
+        if (p.dx == nullptr) continue;
+        cta_sums<2 * R>(s, red, turn);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            s[2 * k] *= inv_d;
+            s[2 * k + 1] = p.layer ? s[2 * k + 1] * inv_d : 0.0f;
+        }
+#pragma unroll 2
+        for (int c = tid; c < D; c += th) {
+            const float wc = w_s[c];
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (!row[k]) continue;
+                float o = r[k] * (fmaf(to_f<T>(dy[k][c]), wc, -s[2 * k + 1]) - (to_f<T>(x[k][c]) - mu[k]) * r[k] * s[2 * k]);
+                if (p.skip) o += to_f<T>(skip[k][c]);
+                static_cast<T*>(p.dx)[(t0 + k) * D + c] = from_f<T>(o);
+            }
+        }
+    }
+    cp_async_wait0();
+    for (int c = tid; c < D; c += th) {                 // (a thread's own columns)
+        if (p.part) p.part[(long long)blockIdx.x * D + c] = dw_s[c];
+        if (FULL && p.part_b) p.part_b[(long long)blockIdx.x * D + c] = db_s[c];
+    }
+}
+
+// ---- host side --------------------------------------------------------------------------------
+// Most partial rows of a weight gradient (sizes the workspace): enough for one per resident CTA.
+static long long max_parts(long long T, int D) {
+    long long n = (1ll << 21) / D;
+    if (n < 1024) n = 1024;
+    if (n > 4096) n = 4096;
+    if (n > T) n = T;
+    return n < 1 ? 1 : n;
+}
+
+// floats from one gradient's partial rows to the other's (keeps 16-byte alignment)
+static size_t part_stride(int parts, int D) { return ((size_t)parts * (size_t)D + 63) & ~(size_t)63; }
+
+// how rows are cut: wide (nv vectors per thread) or staged, `threads` threads, `rows` rows at a time, bytes of shared memory
+struct Cut { bool wide; int nv, threads, rows, smem; };
+
+// false: no fast form holds the rows (the general kernels do: rows beyond 512 threads x 4 vectors, or that do not fit shared
+// memory when staged).  `arrays` rows are read per row; the staged form keeps `vectors` fp32 vectors of the width.
+//   Forward: CTAs of up to 256 threads, two rows at a time.  32768 x 2560 bf16, no residual: 58.7 us with 256 threads and two
+//   rows, 63.7 with one row, 66 with 512 threads; with the residual 106 - 108 us whichever.
+//   Backward: bf16 rows without the second sum (RMS form, no bias) four vectors per thread, one row at a time: 32768 x 2560
+//   bf16 110 us against 117 - 122 with one or two vectors; else up to 512 threads of two vectors, two rows at a time:
+//   8191 x 4096 bf16 layer form 49 us against 54 with four vectors, 32768 x 2560 fp32 162 against 190.
+static bool pick_cut(bool bf16, bool wide, bool fwd, bool full, long long T, int D, int arrays, int vectors, Cut* c) {
+    const int esz = bf16 ? 2 : 4, nvec = D * esz / 16;
+    c->wide = wide;
+    c->nv = 1;
+    if (wide) {
+        const int most = fwd ? 256 : (bf16 && !full && nvec <= 512) ? 128 : bf16 ? 256 : 512;
+        while ((nvec + c->nv - 1) / c->nv > most && c->nv < 4) c->nv *= 2;
+        c->threads = ((nvec + c->nv - 1) / c->nv + 31) / 32 * 32;
+        if (c->threads > kMaxThreads) return false;
+        c->rows = c->nv == 4 ? 1 : (!fwd && nvec <= 64) ? 4 : 2;
+    } else {
+        c->threads = D <= 512 ? 128 : 256;
+        c->rows = 2;
+    }
+    // too few rows to put several on a CTA
+    while (c->rows > 1 && T < 148ll * 4 * c->rows) c->rows /= 2;
+    for (;; c->rows /= 2) {
+        const int batch = 2 * c->rows * arrays;
+        c->smem = wide ? batch * c->nv * c->threads * 16 : batch * staged_pitch(D, esz) + 4 * vectors * D;
+        if (c->smem <= (c->rows > 1 ? kSmemLimit / 2 : kSmemLimit)) return true;
+        if (c->rows == 1) return false;
+    }
+}
+
+typedef void (*FwdKernel)(const FwdParams);
+typedef void (*BwdKernel)(const BwdParams);
+template <typename T, int R, bool F>
+static FwdKernel fwd_kernel_form(const Cut& c) {
+    if (!c.wide) return norm_fwd_staged_kernel<T, R, F>;
+    if (c.nv == 1) return norm_fwd_wide_kernel<T, 1, R, F>;
+    if (c.nv == 2) return norm_fwd_wide_kernel<T, 2, R, F>;
+    return R == 1 ? norm_fwd_wide_kernel<T, 4, 1, F> : nullptr;
+}
+template <typename T, int R, bool F>
+static BwdKernel bwd_kernel_form(const Cut& c) {
+    if (c.nv == 1 && c.wide) return norm_bwd_wide_kernel<T, 1, R, F>;
+    if (R == 4) return nullptr;                  // (narrow rows only)
+    if (!c.wide) return norm_bwd_staged_kernel<T, (R < 4 ? R : 1), F>;
+    if (c.nv == 2) return norm_bwd_wide_kernel<T, 2, (R < 4 ? R : 1), F>;
+    return R == 1 ? norm_bwd_wide_kernel<T, 4, 1, F> : nullptr;
+}
+template <bool F>
+static FwdKernel fwd_kernel(bool bf16, const Cut& c) {
+    if (c.rows == 1) return bf16 ? fwd_kernel_form<__nv_bfloat16, 1, F>(c) : fwd_kernel_form<float, 1, F>(c);
+    return bf16 ? fwd_kernel_form<__nv_bfloat16, 2, F>(c) : fwd_kernel_form<float, 2, F>(c);
+}
+template <bool F>
+static BwdKernel bwd_kernel(bool bf16, const Cut& c) {
+    if (c.rows == 1) return bf16 ? bwd_kernel_form<__nv_bfloat16, 1, F>(c) : bwd_kernel_form<float, 1, F>(c);
+    if (c.rows == 2) return bf16 ? bwd_kernel_form<__nv_bfloat16, 2, F>(c) : bwd_kernel_form<float, 2, F>(c);
+    return bf16 ? bwd_kernel_form<__nv_bfloat16, 4, F>(c) : bwd_kernel_form<float, 4, F>(c);
+}
+
+// CTAs of this kernel that are resident at once (0: none fits); cached per device, kernel, width and shared memory, and opts
+// the kernel in to its shared memory on the way
+static int resident_ctas(const void* k, const Cut& c) {
+    static std::mutex mu;
+    static std::map<std::tuple<int, const void*, int, int>, int> cache;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    std::lock_guard<std::mutex> lock(mu);
+    const auto key = std::make_tuple(dev, k, c.threads, c.smem);
+    const auto hit = cache.find(key);
+    if (hit != cache.end()) return hit->second;
+    int per_sm = 0, sms = 0;
+    if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, c.threads, c.smem) != cudaSuccess) {
+        cudaGetLastError();
+        per_sm = 0;
+    }
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    return cache[key] = per_sm * (sms > 0 ? sms : 148);
+}
+
+static rlf_status launch_reduce(const float* part, const float* part_b, int parts, int D, int accumulate, float* dw, float* db,
+                                cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    cfg.gridDim = dim3((unsigned)((D + 31) / 32), db ? 2 : 1);
+    cfg.blockDim = dim3(1024);
+    cfg.stream = s;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, norm_dw_reduce_kernel, part, part_b, parts, D, accumulate, dw, db) != cudaSuccess) {
+        cudaGetLastError();
+        return RLF_ERR_CUDA;
+    }
+    count_launch();
+    return RLF_OK;
+}
 
 static int row_grid(long long T) { return (int)(T < 148 * 8 ? T : 148 * 8); }
 
@@ -206,8 +925,7 @@ static rlf_status check_norm(int64_t T, int32_t D, rlf_dtype dt, rlf_dtype w_dt,
 
 size_t norm_bwd_workspace_bytes(int64_t T, int32_t D) {
     if (D < 1) return 0;
-    const size_t parts = (size_t)(T < 1 ? 1 : T < nm::kMaxParts ? T : nm::kMaxParts);
-    return 2 * parts * (size_t)D * sizeof(float) + 256;
+    return 2 * nm::part_stride((int)nm::max_parts(T, D), D) * sizeof(float);
 }
 
 }  // namespace rlf
@@ -235,6 +953,24 @@ extern "C" rlf_status rlf_norm_fwd(const void* x, const void* residual, rlf_dtyp
     p.x = x; p.res = residual; p.x_stride = x_stride; p.w = weight; p.b = bias; p.w_bf16 = w_dt == RLF_BF16;
     p.layer = kind == RLF_NORM_LAYER; p.sum = sum_out; p.y = y_out; p.mean = mean_out; p.rstd = rstd_out;
     p.T = T; p.D = D; p.eps = eps;
+    const bool bf16 = dt == RLF_BF16;
+    const int v = bf16 ? 8 : 4;
+    const bool wide = D % v == 0 && x_stride % v == 0 && aligned(x, 16) && aligned(residual, 16) && aligned(sum_out, 16) &&
+                      aligned(y_out, 16);
+    Cut c;
+    if (pick_cut(bf16, wide, true, p.layer, T, D, residual ? 2 : 1, bias ? 2 : 1, &c)) {
+        const FwdKernel k = p.layer ? fwd_kernel<true>(bf16, c) : fwd_kernel<false>(bf16, c);
+        const int resident = k ? resident_ctas((const void*)k, c) : 0;
+        if (resident > 0) {
+            // CTAs that retire after a quarter of a resident generation's rows: in step for the whole launch, all of them
+            // load, then all store (32768 x 2560 bf16 with residual: 130 us as one generation, 109 as four)
+            long long grid = (T + c.rows - 1) / c.rows;
+            if (grid > 4ll * resident) grid = 4ll * resident;
+            k<<<(unsigned)grid, c.threads, c.smem, s>>>(p);
+            count_launch();
+            return cuda_ok(cudaGetLastError());
+        }
+    }
     if (dt == RLF_BF16) norm_fwd_general_kernel<__nv_bfloat16><<<row_grid(T), kGenThreads, 0, s>>>(p);
     else norm_fwd_general_kernel<float><<<row_grid(T), kGenThreads, 0, s>>>(p);
     count_launch();
@@ -266,32 +1002,55 @@ extern "C" rlf_status rlf_norm_bwd(const void* grad_y, int64_t grad_y_stride, co
     p.dy = grad_y; p.dy_stride = grad_y_stride; p.x = x; p.x_stride = x_stride; p.w = weight; p.w_bf16 = w_dt == RLF_BF16;
     p.layer = layer; p.mean = mean; p.rstd = rstd; p.skip = grad_skip; p.dx = grad_x; p.T = T; p.D = D;
     p.part = p.part_b = nullptr;
+    // with no rows the weight gradient is zero (or what was accumulated before)
     int parts = 0;
+    float* part = static_cast<float*>(workspace);
     if (T > 0) {
-        if (want_w) {
-            const long long rows = T < kMaxParts ? 1 : (T + 127) / 128;      // per slice: at most 128 slices of a long batch
-            parts = (int)((T + rows - 1) / rows);
-            p.part = grad_weight ? static_cast<float*>(workspace) : nullptr;
-            p.part_b = grad_bias ? static_cast<float*>(workspace) + (size_t)parts * D : nullptr;
-            const dim3 grid((unsigned)((D + 31) / 32), (unsigned)parts);
-            if (dt == RLF_BF16) norm_dw_general_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(p, rows);
-            else norm_dw_general_kernel<float><<<grid, 256, 0, s>>>(p, rows);
-            count_launch();
-            if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
+        const bool bf16 = dt == RLF_BF16;
+        const int v = bf16 ? 8 : 4;
+        const bool wide = D % v == 0 && x_stride % v == 0 && grad_y_stride % v == 0 && aligned(grad_y, 16) && aligned(x, 16) &&
+                          aligned(grad_skip, 16) && aligned(grad_x, 16);
+        const bool full = layer || grad_bias;
+        Cut c;
+        BwdKernel k = nullptr;
+        long long resident = 0;
+        if (pick_cut(bf16, wide, false, full, T, D, grad_skip ? 3 : 2, grad_bias ? 3 : 2, &c)) {
+            k = full ? bwd_kernel<true>(bf16, c) : bwd_kernel<false>(bf16, c);
+            resident = k ? resident_ctas((const void*)k, c) : 0;
         }
-        // last: grad_x may be the buffer of x or grad_y
-        if (grad_x) {
-            if (dt == RLF_BF16) norm_bwd_general_kernel<__nv_bfloat16><<<row_grid(T), kGenThreads, 0, s>>>(p);
-            else norm_bwd_general_kernel<float><<<row_grid(T), kGenThreads, 0, s>>>(p);
-            count_launch();
-            if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
+        if (resident > 0) {
+            long long grid = (T + c.rows - 1) / c.rows;
+            const long long most = max_parts(T, D);
+            if (grid > resident) grid = resident;        // (more CTAs would mean more partial rows: 110 -> 117 us at twice as many)
+            if (grid > most) grid = most;
+            parts = (int)grid;
+            p.part = grad_weight ? part : nullptr;
+            p.part_b = grad_bias ? part + part_stride(parts, D) : nullptr;
+            if (grad_x || want_w) {
+                k<<<(unsigned)grid, c.threads, c.smem, s>>>(p);
+                count_launch();
+            }
+        } else {
+            if (want_w) {
+                const long long rows = T < 1024 ? 1 : (T + 127) / 128;       // per slice: at most 128 slices of a long batch
+                parts = (int)((T + rows - 1) / rows);
+                p.part = grad_weight ? part : nullptr;
+                p.part_b = grad_bias ? part + part_stride(parts, D) : nullptr;
+                const dim3 grid((unsigned)((D + 31) / 32), (unsigned)parts);
+                if (bf16) norm_dw_general_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(p, rows);
+                else norm_dw_general_kernel<float><<<grid, 256, 0, s>>>(p, rows);
+                count_launch();
+                if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
+            }
+            // last: grad_x may be the buffer of x or grad_y
+            if (grad_x) {
+                if (bf16) norm_bwd_general_kernel<__nv_bfloat16><<<row_grid(T), kGenThreads, 0, s>>>(p);
+                else norm_bwd_general_kernel<float><<<row_grid(T), kGenThreads, 0, s>>>(p);
+                count_launch();
+            }
         }
+        if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
     }
     if (!want_w) return RLF_OK;
-    // with no rows the gradient is zero (or what was accumulated before)
-    const float* part = static_cast<const float*>(workspace);
-    norm_dw_reduce_kernel<<<dim3((unsigned)((D + 31) / 32), 2), 256, 0, s>>>(
-        part, part + (size_t)parts * D, parts, D, accumulate, grad_weight, grad_bias);
-    count_launch();
-    return cuda_ok(cudaGetLastError());
+    return launch_reduce(part, part + part_stride(parts, D), parts, D, accumulate, grad_weight, grad_bias, s);
 }
