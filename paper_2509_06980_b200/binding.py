@@ -450,12 +450,36 @@ def rlf_fused_lmhead_logp_entropy(hidden, W, ids, want_entropy=True, logp_out=No
 
 
 NORM_RMS, NORM_LAYER = 0, 1
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _rows(t, what):
+def _here(t):
+    """Index of the current device; the kernels run there, so a tensor of another device is refused."""
+    here = torch.cuda.current_device()
+    if t.get_device() != here:
+        raise ValueError("expected tensors on the current device, cuda:%d" % here)
+    return here
+
+
+def _at(t, here, what, dtype=None, shape=None):
+    """Address of a dense tensor on the current device (None passes)."""
+    if t is None:
+        return None
+    if t.get_device() != here:
+        raise ValueError("%s must be on the current device, cuda:%d" % (what, here))
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % what)
+    return t.data_ptr()
+
+
+def _rows(t, here, what):
     """Base address and row stride of a [T, D] tensor whose rows may be strided (last dimension dense)."""
-    if not t.is_cuda:
-        raise ValueError("expected a CUDA tensor")
+    if t.get_device() != here:
+        raise ValueError("%s must be on the current device, cuda:%d" % (what, here))
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("%s must be 2-dimensional with a contiguous last dimension" % what)
     T, D = t.shape
@@ -471,18 +495,13 @@ def _empty_rows_like(t, stride):
     return torch.empty((T - 1) * stride + V + off, dtype=t.dtype, device=t.device).as_strided((T, V), (stride, 1), off)
 
 
-def _like(t, shape, dtype, what):
-    if t is not None and (t.shape != shape or t.dtype != dtype):
-        raise ValueError("%s must be a %s tensor of shape %s" % (what, dtype, tuple(shape)))
-    return t
-
-
-def _one_device(*tensors):
-    """The kernels run on the current device and stream; a tensor of another device is refused."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != here:
-            raise ValueError("a tensor is on cuda:%s, the current device is cuda:%d" % (t.device.index, here))
+def _workspace(workspace, here, which_fn, T, V, D, dt, dev):
+    if workspace is None:
+        n = _lib.rlf_workspace_bytes(which_fn, T, V, D, dt)
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=dev)
+    elif workspace.get_device() != here or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current device")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def rlf_cross_entropy_fwd_bwd(logits, ids, mask=None, label_smoothing=0.0, z_coef=0.0, denom=None, grad_logits=None,
@@ -490,35 +509,32 @@ def rlf_cross_entropy_fwd_bwd(logits, ids, mask=None, label_smoothing=0.0, z_coe
                               workspace=None, dev_status=None):
     """Softmax cross entropy of the rows of logits [T, V] (rows may be strided) at targets ids, masked mean.
     -> (logp fp32[T], lse fp32[T] | None, loss fp64[4], grad_logits | None), all on the device."""
-    zp, stride = _rows(logits, "logits")
+    here = _here(logits)
+    zp, stride = _rows(logits, here, "logits")
     T, V = logits.shape
-    dev = logits.device
-    _one_device(logits, ids, mask, denom, grad_logits, logp_out, lse_out, loss_out, workspace, dev_status)
+    dev, f32 = logits.device, torch.float32
     if grad_logits is None and want_grad:
         grad_logits = logits if in_place else _empty_rows_like(logits, stride)
     gp = None
     if grad_logits is not None:
-        _like(grad_logits, logits.shape, logits.dtype, "grad_logits")
-        gp, gs = _rows(grad_logits, "grad_logits")
+        if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
+            raise ValueError("grad_logits must have the shape and type of logits")
+        gp, gs = _rows(grad_logits, here, "grad_logits")
         if T > 1 and gs != stride:
             raise ValueError("grad_logits must have the row stride of logits")
     if logp_out is None:
-        logp_out = torch.empty(T, dtype=torch.float32, device=dev)
+        logp_out = torch.empty(T, dtype=f32, device=dev)
     if lse_out is None and want_lse:
-        lse_out = torch.empty(T, dtype=torch.float32, device=dev)
+        lse_out = torch.empty(T, dtype=f32, device=dev)
     if loss_out is None:
         loss_out = torch.empty(4, dtype=torch.float64, device=dev)
-    _like(ids, (T,), torch.int32, "ids")
-    _like(mask, (T,), torch.uint8, "mask")
-    _like(logp_out, (T,), torch.float32, "logp_out")
-    _like(lse_out, (T,), torch.float32, "lse_out")
-    _like(loss_out, (4,), torch.float64, "loss_out")
-    if workspace is None:
-        workspace = new_workspace(FN_CROSS_ENTROPY, T, V, 0, RLF_BF16, dev)
+    workspace, wp, wn = _workspace(workspace, here, FN_CROSS_ENTROPY, T, V, 0, RLF_BF16, dev)
     _check(_lib.rlf_cross_entropy_fwd_bwd(
-        zp, _dt(logits), T, V, stride, _ptr(ids), _ptr(mask), float(label_smoothing), float(z_coef),
-        _ptr(denom, torch.int64), _ptr(logp_out), _ptr(lse_out), _ptr(loss_out), gp, workspace.data_ptr(),
-        workspace.numel(), _ptr(dev_status, torch.int32), _stream()), "rlf_cross_entropy_fwd_bwd")
+        zp, _dt(logits), T, V, stride, _at(ids, here, "ids", torch.int32, (T,)),
+        _at(mask, here, "mask", torch.uint8, (T,)), label_smoothing, z_coef, _at(denom, here, "denom", torch.int64),
+        _at(logp_out, here, "logp_out", f32, (T,)), _at(lse_out, here, "lse_out", f32, (T,)),
+        _at(loss_out, here, "loss_out", torch.float64, (4,)), gp, wp, wn,
+        _at(dev_status, here, "dev_status", torch.int32), _raw_stream(here)), "rlf_cross_entropy_fwd_bwd")
     return logp_out, lse_out, loss_out, grad_logits
 
 
@@ -529,40 +545,32 @@ def rlf_fused_lmhead_cross_entropy(hidden, W, ids, mask=None, label_smoothing=0.
     """rlf_cross_entropy_fwd_bwd of the logits hidden W^T, which are never stored.
     -> (logp fp32[T], lse fp32[T] | None, loss fp64[4], grad_hidden bf16[T,D] | None, grad_W [V,D] | None);
     grad_W is fp32 or (grad_W_dtype=torch.bfloat16) bf16."""
+    here = _here(hidden)
     T, D = hidden.shape
     V = W.shape[0]
-    dev = hidden.device
-    _one_device(hidden, W, ids, mask, denom, grad_hidden, grad_W, logp_out, lse_out, loss_out, workspace, dev_status)
+    dev, f32, bf16 = hidden.device, torch.float32, torch.bfloat16
     if accumulate_grad_W and grad_W is None:
         raise ValueError("accumulate_grad_W needs the buffer that is added to")
     if grad_hidden is None and want_grad_hidden:
-        grad_hidden = torch.empty((T, D), dtype=torch.bfloat16, device=dev)
+        grad_hidden = torch.empty((T, D), dtype=bf16, device=dev)
     if grad_W is None and want_grad_W:
         grad_W = torch.empty((V, D), dtype=grad_W_dtype, device=dev)
     if logp_out is None:
-        logp_out = torch.empty(T, dtype=torch.float32, device=dev)
+        logp_out = torch.empty(T, dtype=f32, device=dev)
     if lse_out is None and want_lse:
-        lse_out = torch.empty(T, dtype=torch.float32, device=dev)
+        lse_out = torch.empty(T, dtype=f32, device=dev)
     if loss_out is None:
         loss_out = torch.empty(4, dtype=torch.float64, device=dev)
-    _like(W, (V, D), torch.bfloat16, "W")
-    _like(ids, (T,), torch.int32, "ids")
-    _like(mask, (T,), torch.uint8, "mask")
-    _like(grad_hidden, (T, D), torch.bfloat16, "grad_hidden")
-    _like(logp_out, (T,), torch.float32, "logp_out")
-    _like(lse_out, (T,), torch.float32, "lse_out")
-    _like(loss_out, (4,), torch.float64, "loss_out")
-    w_dt = RLF_F32
-    if grad_W is not None:
-        _like(grad_W, (V, D), grad_W.dtype, "grad_W")
-        w_dt = _dt(grad_W, "grad_W")
-    if workspace is None:
-        workspace = new_workspace(FN_FUSED_CROSS_ENTROPY, T, V, D, w_dt, dev)
+    w_dt = RLF_F32 if grad_W is None else _dt(grad_W, "grad_W")
+    workspace, wp, wn = _workspace(workspace, here, FN_FUSED_CROSS_ENTROPY, T, V, D, w_dt, dev)
     _check(_lib.rlf_fused_lmhead_cross_entropy(
-        _ptr(hidden, torch.bfloat16), _ptr(W), T, D, V, _ptr(ids), _ptr(mask), float(label_smoothing), float(z_coef),
-        _ptr(denom, torch.int64), _ptr(logp_out), _ptr(lse_out), _ptr(loss_out), _ptr(grad_hidden), _ptr(grad_W), w_dt,
-        1 if accumulate_grad_W else 0, workspace.data_ptr(), workspace.numel(), _ptr(dev_status, torch.int32),
-        _stream()), "rlf_fused_lmhead_cross_entropy")
+        _at(hidden, here, "hidden", bf16), _at(W, here, "W", bf16, (V, D)), T, D, V,
+        _at(ids, here, "ids", torch.int32, (T,)), _at(mask, here, "mask", torch.uint8, (T,)), label_smoothing, z_coef,
+        _at(denom, here, "denom", torch.int64), _at(logp_out, here, "logp_out", f32, (T,)),
+        _at(lse_out, here, "lse_out", f32, (T,)), _at(loss_out, here, "loss_out", torch.float64, (4,)),
+        _at(grad_hidden, here, "grad_hidden", bf16, (T, D)), _at(grad_W, here, "grad_W", None, (V, D)), w_dt,
+        1 if accumulate_grad_W else 0, wp, wn, _at(dev_status, here, "dev_status", torch.int32), _raw_stream(here)),
+        "rlf_fused_lmhead_cross_entropy")
     return logp_out, lse_out, loss_out, grad_hidden, grad_W
 
 
@@ -571,32 +579,31 @@ def rlf_norm_fwd(x, weight, bias=None, residual=None, kind=NORM_RMS, eps=1e-6, y
     """Layer norm (NORM_LAYER) or its RMS form (NORM_RMS) of the rows of x (+ residual).
     x, residual: [T, D] (rows may be strided, the same stride); weight, bias: [D], bf16 or fp32.
     -> (y [T, D], x + residual [T, D] | None without residual, mean fp32[T] | None for the RMS form, rstd fp32[T])."""
-    xp, xs = _rows(x, "x")
-    T, D = x.shape
-    dev, dt = x.device, x.dtype
-    _one_device(x, weight, bias, residual, y_out, sum_out, mean_out, rstd_out)
+    here = _here(x)
+    xp, xs = _rows(x, here, "x")
+    shape = T, D = x.shape
+    dev, dt, f32 = x.device, x.dtype, torch.float32
     rp = None
     if residual is not None:
-        _like(residual, x.shape, dt, "residual")
-        rp, rs = _rows(residual, "residual")
+        if residual.shape != x.shape or residual.dtype != dt:
+            raise ValueError("residual must have the shape and type of x")
+        rp, rs = _rows(residual, here, "residual")
         if T > 1 and rs != xs:
             raise ValueError("residual must have the row stride of x")
-    _like(weight, (D,), weight.dtype, "weight")
-    _like(bias, (D,), weight.dtype, "bias")
+        if sum_out is None:
+            sum_out = torch.empty(shape, dtype=dt, device=dev)
     if y_out is None:
-        y_out = torch.empty((T, D), dtype=dt, device=dev)
-    if sum_out is None and residual is not None:
-        sum_out = torch.empty((T, D), dtype=dt, device=dev)
+        y_out = torch.empty(shape, dtype=dt, device=dev)
     if mean_out is None and kind == NORM_LAYER:
-        mean_out = torch.empty(T, dtype=torch.float32, device=dev)
+        mean_out = torch.empty(T, dtype=f32, device=dev)
     if rstd_out is None:
-        rstd_out = torch.empty(T, dtype=torch.float32, device=dev)
-    _like(y_out, x.shape, dt, "y_out")
-    _like(sum_out, x.shape, dt, "sum_out")
-    _like(mean_out, (T,), torch.float32, "mean_out")
-    _like(rstd_out, (T,), torch.float32, "rstd_out")
-    _check(_lib.rlf_norm_fwd(xp, rp, _dt(x, "x"), T, D, xs, _ptr(weight), _ptr(bias), _dt(weight, "weight"), int(kind), float(eps),
-                             _ptr(sum_out), _ptr(y_out), _ptr(mean_out), _ptr(rstd_out), _stream()), "rlf_norm_fwd")
+        rstd_out = torch.empty(T, dtype=f32, device=dev)
+    _check(_lib.rlf_norm_fwd(
+        xp, rp, _dt(x, "x"), T, D, xs, _at(weight, here, "weight", None, (D,)),
+        _at(bias, here, "bias", weight.dtype, (D,)), _dt(weight, "weight"), kind, eps,
+        _at(sum_out, here, "sum_out", dt, shape), _at(y_out, here, "y_out", dt, shape),
+        _at(mean_out, here, "mean_out", f32, (T,)), _at(rstd_out, here, "rstd_out", f32, (T,)), _raw_stream(here)),
+        "rlf_norm_fwd")
     return y_out, sum_out, mean_out, rstd_out
 
 
@@ -604,33 +611,30 @@ def rlf_norm_bwd(grad_y, x, weight, mean, rstd, kind=NORM_RMS, grad_skip=None, w
                  want_grad_bias=False, grad_x=None, grad_weight=None, grad_bias=None, accumulate=False, workspace=None):
     """Backward of rlf_norm_fwd; x is what was normalised (the sum, with a residual); grad_skip is added to grad_x.
     -> (grad_x [T, D] | None, grad_weight fp32[D] | None, grad_bias fp32[D] | None)."""
-    xp, xs = _rows(x, "x")
-    T, D = x.shape
-    dev, dt = x.device, x.dtype
-    _one_device(x, grad_y, weight, mean, rstd, grad_skip, grad_x, grad_weight, grad_bias, workspace)
-    _like(grad_y, x.shape, dt, "grad_y")
-    gp, gs = _rows(grad_y, "grad_y")
-    _like(weight, (D,), weight.dtype, "weight")
+    here = _here(x)
+    xp, xs = _rows(x, here, "x")
+    shape = T, D = x.shape
+    dev, dt, f32 = x.device, x.dtype, torch.float32
+    if grad_y.shape != x.shape or grad_y.dtype != dt:
+        raise ValueError("grad_y must have the shape and type of x")
+    gp, gs = _rows(grad_y, here, "grad_y")
     if accumulate and ((grad_weight is None and want_grad_weight) or (grad_bias is None and want_grad_bias)):
         raise ValueError("accumulate needs the buffers that are added to")
     if grad_x is None and want_grad_x:
-        grad_x = torch.empty((T, D), dtype=dt, device=dev)
+        grad_x = torch.empty(shape, dtype=dt, device=dev)
     if grad_weight is None and want_grad_weight:
-        grad_weight = torch.empty(D, dtype=torch.float32, device=dev)
+        grad_weight = torch.empty(D, dtype=f32, device=dev)
     if grad_bias is None and want_grad_bias:
-        grad_bias = torch.empty(D, dtype=torch.float32, device=dev)
-    _like(grad_x, x.shape, dt, "grad_x")
-    _like(grad_skip, x.shape, dt, "grad_skip")
-    _like(grad_weight, (D,), torch.float32, "grad_weight")
-    _like(grad_bias, (D,), torch.float32, "grad_bias")
-    _like(mean, (T,), torch.float32, "mean")
-    _like(rstd, (T,), torch.float32, "rstd")
-    if workspace is None and (grad_weight is not None or grad_bias is not None):
-        workspace = new_workspace(FN_NORM_BWD, T, 0, D, RLF_F32, dev)
-    _check(_lib.rlf_norm_bwd(gp, gs, xp, xs, _dt(x, "x"), T, D, _ptr(weight), _dt(weight, "weight"), int(kind), _ptr(mean), _ptr(rstd),
-                             _ptr(grad_skip), _ptr(grad_x), _ptr(grad_weight), _ptr(grad_bias), 1 if accumulate else 0,
-                             None if workspace is None else workspace.data_ptr(),
-                             0 if workspace is None else workspace.numel(), _stream()), "rlf_norm_bwd")
+        grad_bias = torch.empty(D, dtype=f32, device=dev)
+    wp, wn = None, 0
+    if workspace is not None or grad_weight is not None or grad_bias is not None:
+        workspace, wp, wn = _workspace(workspace, here, FN_NORM_BWD, T, 0, D, RLF_F32, dev)
+    _check(_lib.rlf_norm_bwd(
+        gp, gs, xp, xs, _dt(x, "x"), T, D, _at(weight, here, "weight", None, (D,)), _dt(weight, "weight"), kind,
+        _at(mean, here, "mean", f32, (T,)), _at(rstd, here, "rstd", f32, (T,)),
+        _at(grad_skip, here, "grad_skip", dt, shape), _at(grad_x, here, "grad_x", dt, shape),
+        _at(grad_weight, here, "grad_weight", f32, (D,)), _at(grad_bias, here, "grad_bias", f32, (D,)),
+        1 if accumulate else 0, wp, wn, _raw_stream(here)), "rlf_norm_bwd")
     return grad_x, grad_weight, grad_bias
 
 
