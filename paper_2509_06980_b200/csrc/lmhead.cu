@@ -49,7 +49,9 @@ constexpr int kDrainPitch = 36;              // floats per row of a drain stagin
 // matrix.  The two accumulators take all 512 TMEM columns, so the drain of a unit does not overlap the
 // next unit's multiplies; with K running over the whole vocabulary or a whole chunk of tokens the
 // drain is a per cent or two of a unit.
-template <bool PAIR, bool ACC2 = false> struct Cfg {
+// The cross-entropy form's gradient contractions (CE) keep two bf16 output tiles of 32 rows x 64 columns per drain warp
+// instead of the fp32 staging tile: grad_W leaves them by TMA stores.
+template <bool PAIR, bool ACC2 = false, bool CE = false> struct Cfg {
     static_assert(PAIR || !ACC2, "two accumulators per CTA exist in pair form only");
     static constexpr int kAcc = ACC2 ? 2 : 1;
     static constexpr int kStages = ACC2 ? 4 : (PAIR ? 6 : 4);
@@ -57,7 +59,7 @@ template <bool PAIR, bool ACC2 = false> struct Cfg {
     static constexpr int kBBytes = kBRows * BK * 2;
     static constexpr int kStageBytes = kAcc * kABytes + kBBytes;
     // + alignment slack, the barriers, and (two-accumulator form) a 32 x 32 fp32 staging tile per drain warp
-    static constexpr int kDrainBytes = ACC2 ? 4 * 32 * kDrainPitch * 4 : 0;
+    static constexpr int kDrainBytes = CE ? 4 * 2 * 4096 : ACC2 ? 4 * 32 * kDrainPitch * 4 : 0;
     static constexpr int kSmemBytes = kStages * kStageBytes + 1024 + 256 + kDrainBytes;
 };
 constexpr int kMaxStages = 6;
@@ -112,11 +114,19 @@ struct GemmParams {
     // each fetches its slabs from HBM on its own.  Waits are bounded and only delay loads: a worker
     // that gives up runs on unpaced.
     int* pace;
-    // Cross-entropy form (the CE instantiations only).  Label smoothing adds a rank-one term to either gradient:
+    // Sweep over device-counted rows (optional): with few row units the number of vocabulary splits is chosen on the device
+    // (auto_split; nsplit is then the most there may be, and the partials' stride)
+    int auto_split;
+    // Cross-entropy form (CE, the gradient contractions).  Label smoothing adds a rank-one term to either gradient:
     const float* col_vec;     // kGradHidden (optional): out += row_add[r] * col_vec[col];  kGradW (optional): out += col_vec[col]
     const float* row_add;     // kGradHidden with col_vec: factor of compact row r
-    __nv_bfloat16* out_w16;   // kGradW: the result goes here as bf16 instead of to out_f32 (last chunk of a call)
-    const float* add_f32;     // kGradW with out_w16 (optional): earlier chunks' fp32 sum, [M][out_stride], added before rounding
+    int store_w16;            // kGradW: the result goes to map_c's matrix as bf16 instead of to out_f32 (last chunk of a call)
+    const float* add_f32;     // kGradW with store_w16 (optional): earlier chunks' fp32 sum, [M][out_stride], added before rounding
+    // kGradHidden: with few row units the vocabulary (the long axis) is cut into up to k_split_max pieces (hidden_splits), whose
+    // raw sums go to k_part, [piece][k_part_rows][out_stride] fp32, for ce_join_hidden_kernel
+    int k_split_max;
+    float* k_part;
+    long long k_part_rows;
 };
 
 // ---- PTX wrappers ---------------------------------------------------------------------------
@@ -265,12 +275,35 @@ struct SmemCtl {
 
 static_assert(sizeof(SmemCtl) <= 256, "the barriers share a 256-byte slot behind the stage ring");
 
+// Vocabulary splits of a sweep with few row units: the persistent workers take the m_units x s units round-robin, so the
+// launch lasts about ceil(m_units s / workers) rounds of ceil(n_tiles / s) tiles (and a little per unit); the smallest such s.
+// (593 column tiles, 74 pairs: one row unit 74 splits instead of 60, 8 or 9 tiles each; six row units of 125 tiles 12 splits,
+// one round of 11 tiles, instead of 16, two rounds of 8.)  Every lane of a full warp calls it.
+constexpr int kAutoSplitUnits = 16;          // with more row units the fixed split and its L2 blocking are kept
+__device__ __forceinline__ int auto_split(int m_units, int n_tiles, int workers, int most) {
+    const int lane = threadIdx.x & 31;
+    unsigned best = 0xffffffffu;
+    for (int s = lane + 1; s <= most && s <= n_tiles; s += 32) {
+        const unsigned rounds = (unsigned)((m_units * s + workers - 1) / workers), tiles = (unsigned)((n_tiles + s - 1) / s);
+        const unsigned cost = (rounds * (8 * tiles + 1)) << 8 | (unsigned)s;
+        best = best < cost ? best : cost;
+    }
+    return (int)(__reduce_min_sync(0xffffffffu, best) & 255u);
+}
+// Pieces that the vocabulary is cut into in grad_hidden: as many as keep the workers busy, each of 16 slabs at least.
+__host__ __device__ __forceinline__ int hidden_splits(int m_units, int n_tiles, int k_slabs, int workers, int most) {
+    int k = m_units > 0 ? workers / (m_units * n_tiles) : 1;
+    if (k > k_slabs / 16) k = k_slabs / 16;
+    if (k > most) k = most;
+    return k < 1 ? 1 : k;
+}
+
 // ---- the kernel -----------------------------------------------------------------------------
 template <bool PAIR, bool ACC2, bool CE = false>
 __global__ void __launch_bounds__(kThreads, 1)
 umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                 const GemmParams p) {
-    using C = Cfg<PAIR, ACC2>;
+                 const __grid_constant__ CUtensorMap map_c, const GemmParams p) {
+    using C = Cfg<PAIR, ACC2, CE>;
     constexpr int NACC = C::kAcc;
     extern __shared__ unsigned char smem_raw[];
     // a launch that is conditional on a device-side flag (uniform over the grid): leave before
@@ -279,8 +312,8 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // operand stages must sit on 1024-byte boundaries (swizzle atom)
     const uint32_t raw = smem_addr(smem_raw);
     const uint32_t tiles = (raw + 1023u) & ~1023u;
-    SmemCtl* ctl = reinterpret_cast<SmemCtl*>(smem_raw + (tiles - raw) + C::kStages * C::kStageBytes);
-    float* drain_stage = reinterpret_cast<float*>(smem_raw + (tiles - raw) + C::kStages * C::kStageBytes + 256);
+    float* drain_stage = reinterpret_cast<float*>(smem_raw + (tiles - raw) + C::kStages * C::kStageBytes);   // 1 KB aligned
+    SmemCtl* ctl = reinterpret_cast<SmemCtl*>(smem_raw + (tiles - raw) + C::kStages * C::kStageBytes + C::kDrainBytes);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool a_mn = p.mode == kGradW;
@@ -301,9 +334,12 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // CTA's tile for accumulator a of unit m is kTilesPerUnit * m + 2 * a + rank
     constexpr int kTilesPerUnit = (PAIR ? 2 : 1) * NACC;
     const int m_units = (m_tiles + kTilesPerUnit - 1) / kTilesPerUnit;
-    const int units = (no_k && p.accumulate) ? 0 : sweep ? m_units * p.nsplit : m_units * p.n_tiles;
     const int worker = PAIR ? blockIdx.x >> 1 : blockIdx.x;
     const int workers = PAIR ? gridDim.x >> 1 : gridDim.x;
+    int nsplit = p.nsplit;
+    if (sweep && p.auto_split && m_units <= kAutoSplitUnits) nsplit = auto_split(m_units, p.n_tiles, workers, p.nsplit);
+    const int k_split = (CE && p.mode == kGradHidden) ? hidden_splits(m_units, p.n_tiles, k_slabs, workers, p.k_split_max) : 1;
+    const int units = (no_k && p.accumulate) ? 0 : sweep ? m_units * nsplit : m_units * p.n_tiles * k_split;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kStages; ++s) {
@@ -335,13 +371,13 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const uint32_t tmem_base = ctl->tmem_base;
 
     // unit -> (m unit, first n tile, one-past-last n tile)
-    const int split_base = sweep ? p.n_tiles / p.nsplit : 0, split_rem = sweep ? p.n_tiles % p.nsplit : 0;
+    const int split_base = sweep ? p.n_tiles / nsplit : 0, split_rem = sweep ? p.n_tiles % nsplit : 0;
     auto unit_range = [&](int u, int& m, int& n0, int& n1) {
         if (sweep) {
             // blocks of m_block row units; inside a block, units run over its row units first, then
             // over the splits: the CTAs running at one time share both the rows of the head they
             // sweep and a set of token tiles small enough to stay in L2
-            const int per_block = p.m_block * p.nsplit;
+            const int per_block = p.m_block * nsplit;
             const int blk = u / per_block, within = u - blk * per_block;
             const int rows_here = min(p.m_block, m_units - blk * p.m_block);
             const int sp = within / rows_here;
@@ -354,7 +390,18 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             // rows or columns) in L2 instead of each streaming the whole scratch from HBM
             n0 = u % p.n_tiles;
             m = u / p.n_tiles;
+            if (CE) m %= m_units;            // (pieces of the long axis slowest)
             n1 = n0 + 1;
+        }
+    };
+    // unit -> its k-slabs
+    auto unit_k = [&](int u, int& k0, int& k1) {
+        k0 = 0;
+        k1 = k_slabs;
+        if (CE && k_split > 1) {
+            const int piece = u / (m_units * p.n_tiles);
+            k0 = (int)((long long)k_slabs * piece / k_split);
+            k1 = (int)((long long)k_slabs * (piece + 1) / k_split);
         }
     };
 
@@ -372,10 +419,12 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 int m, n0, n1;
                 unit_range(u, m, n0, n1);
                 const int with_me = min(workers, units - iter * workers);     // workers that have a unit number `iter`
+                int k0, k1;
+                unit_k(u, k0, k1);
                 long long pos = 0;
                 for (int n = n0; n < n1 && ok; ++n) {
                     const int b_row0 = n * BN + rank * C::kBRows;      // this CTA's rows of the B tile
-                    for (int kb = 0; kb < k_slabs; ++kb, ++pos) {
+                    for (int kb = k0; kb < k1; ++kb, ++pos) {
                         // the meeting point before a unit: announce the arrival and read the counter; the value
                         // is looked at two k-slabs later, so its round trip to L2 overlaps the issue of those
                         // slabs' loads instead of draining the ring
@@ -440,13 +489,14 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             uint32_t tphase[2] = {0, 0};
             bool ok = true;
             for (int u = worker; u < units && ok && !no_k; u += workers) {
-                int m, n0, n1;
+                int m, n0, n1, k0, k1;
                 unit_range(u, m, n0, n1);
+                unit_k(u, k0, k1);
                 for (int n = n0; n < n1 && ok; ++n) {
                     if (!mbar_wait(smem_addr(&ctl->tmem_empty[buf]), tphase[buf] ^ 1u, &ctl->abort_flag)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t d_tmem = tmem_base + (uint32_t)buf * BN;
-                    for (int kb = 0; kb < k_slabs; ++kb) {
+                    for (int kb = k0; kb < k1; ++kb) {
                         if (!mbar_wait(smem_addr(&ctl->full[stage]), phase, &ctl->abort_flag)) { ok = false; break; }
                         tc_fence_after();
                         const uint32_t sa = tiles + stage * C::kStageBytes;
@@ -460,11 +510,11 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                                 for (int a = 0; a < NACC; ++a)
                                     tc_mma2(tmem_base + (uint32_t)(a * BN),
                                             adesc + (uint64_t)(a * (kABytes >> 4)) + (uint64_t)(k * a_kstep),
-                                            bdesc + (uint64_t)(k * b_kstep), idesc, (kb | k) ? 1u : 0u);
+                                            bdesc + (uint64_t)(k * b_kstep), idesc, ((kb - k0) | k) ? 1u : 0u);
                             } else if (PAIR) tc_mma2(d_tmem, adesc + (uint64_t)(k * a_kstep), bdesc + (uint64_t)(k * b_kstep), idesc,
-                                                     (kb | k) ? 1u : 0u);
+                                                     ((kb - k0) | k) ? 1u : 0u);
                             else tc_mma(d_tmem, adesc + (uint64_t)(k * a_kstep), bdesc + (uint64_t)(k * b_kstep), idesc,
-                                        (kb | k) ? 1u : 0u);
+                                        ((kb - k0) | k) ? 1u : 0u);
                         }
                         // frees the stage (in both CTAs) when these MMAs retire
                         if (PAIR) tc_commit2(smem_addr(&ctl->empty[stage]));
@@ -485,6 +535,8 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const int quarter = warp & 3;                    // TMEM lane quarter this warp may read
         const int row_in_tile = quarter * 32 + lane;
         int buf = 0;
+        int out_tile = 0;                                // CE: which of this warp's two output tiles is filled next
+        (void)out_tile;
         uint32_t tphase[2] = {0, 0};
         bool ok = true;
         for (int u = worker; u < units && ok; u += workers) {
@@ -494,6 +546,8 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const bool row_ok = row < M;
             float run_m = -INFINITY, run_s = 0.0f;       // kLse
             float run_u = 0.0f;                          // kLse with entropy: sum of 2^x x against run_m
+            const int piece = (CE && k_split > 1) ? u / (m_units * p.n_tiles) : 0;
+            (void)piece;
             for (int n = n0; n < n1 && ok; ++n) {
                 if (!no_k) {
                     // one lane polls for the warp (128 polling threads would only burn issue slots and
@@ -612,26 +666,79 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 // 32-column chunks of the accumulator(s), software-pipelined: the tensor-memory load of
                 // chunk ac + 1 is in flight while chunk ac is consumed (with two accumulators the drain is
                 // not hidden behind the next unit's multiplies, so its latency chain matters)
-                // (CE) four columns of one grad_W row: the smoothing term is added; with a bf16 result the
-                // earlier chunks' sum too, and the row's piece is stored -> true.  false: still to be stored.
-                auto finish_w = [&](int r, int c, float4& val) -> bool {
+                // (CE, grad_W) one thread's 32 columns of its row: the smoothing term is added; then, for a bf16 result, the
+                // earlier chunks' sum, and the piece goes into this warp's 32 x 64 output tile (128-byte rows, swizzled
+                // like every TMA box here), which lane 0 stores once its second half is in.  nvalid is 32 (the hidden size
+                // is a multiple of 64).
+                auto drain_w = [&](int row_r, int cb, uint32_t (&v)[32]) {
                     if (p.col_vec) {
-                        const float4 g = *reinterpret_cast<const float4*>(p.col_vec + c);
-                        val.x += g.x; val.y += g.y; val.z += g.z; val.w += g.w;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 g = reinterpret_cast<const float4*>(p.col_vec + cb)[i];
+                            v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + g.x);
+                            v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + g.y);
+                            v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + g.z);
+                            v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + g.w);
+                        }
                     }
-                    if (!p.out_w16) return false;
-                    const long long o = (long long)r * p.out_stride + c;
-                    if (p.add_f32) {
-                        const float4 a = *reinterpret_cast<const float4*>(p.add_f32 + o);
-                        val.x += a.x; val.y += a.y; val.z += a.z; val.w += a.w;
+                    if (!p.store_w16) {
+                        if (row_r < M) {
+                            float4* d4 = reinterpret_cast<float4*>(p.out_f32 + (long long)row_r * p.out_stride + cb);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                if (p.accumulate)
+                                    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
+                                                 :: "l"(d4 + i), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]),
+                                                    "r"(v[4 * i + 3]) : "memory");
+                                else
+                                    d4[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                                                        __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                            }
+                        }
+                        return;
                     }
-                    uint2 q;
-                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.x) : "f"(val.y), "f"(val.x));
-                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.y) : "f"(val.w), "f"(val.z));
-                    *reinterpret_cast<uint2*>(p.out_w16 + o) = q;
-                    return true;
+                    if (p.add_f32 && row_r < M) {
+                        const float4* a4 = reinterpret_cast<const float4*>(p.add_f32 + (long long)row_r * p.out_stride + cb);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 g = a4[i];
+                            v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + g.x);
+                            v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + g.y);
+                            v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + g.z);
+                            v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + g.w);
+                        }
+                    }
+                    const int half = (cb >> 5) & 1;
+                    const uint32_t tile = smem_addr(drain_stage) + (uint32_t)((warp - 2) * 8192 + out_tile * 4096);
+                    if (half == 0) {                     // the store that read this tile last has read it
+                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                        __syncwarp();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t q[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q[j])
+                                : "f"(__uint_as_float(v[8 * i + 2 * j + 1])), "f"(__uint_as_float(v[8 * i + 2 * j])));
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                     :: "r"(tile + (uint32_t)(lane * 128 + (((4 * half + i) ^ (lane & 7)) << 4))),
+                                        "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
+                    }
+                    if (half == 1) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            // (rows past the vocabulary's end are clipped by the tensor map)
+                            if (row_r - lane < M)
+                                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                                             :: "l"(&map_c), "r"(tile), "r"(cb - 32), "r"(row_r) : "memory");
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                        out_tile ^= 1;
+                    }
                 };
-                (void)finish_w;
+                (void)drain_w;
                 auto consume = [&](int ac, uint32_t (&v)[32]) {
                     // accumulator a of this unit: the token (vocabulary) tile 2 a further on, TMEM columns a * 256 ..
                     const int a = ac / (BN / 32), c = ac - a * (BN / 32);
@@ -644,6 +751,10 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         for (int i = 0; i < 32; ++i) v[i] = 0u;
                     }
                     const int nvalid = min(32, p.N - cb);
+                    if (CE && p.mode == kGradW) {
+                        drain_w(row_a, cb, v);
+                        return;
+                    }
                     if (p.mode == kLse) {
                         float cm = -INFINITY;
 #pragma unroll
@@ -689,13 +800,24 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             const long long orow = p.row_index ? (long long)p.row_index[p.live_off + row_a] : (long long)row_a;
                             __nv_bfloat16* dst = p.out_bf16 + orow * p.out_stride + cb;
                             const float sc = p.row_scale ? p.row_scale[row_a] : 1.0f;
-                            if (CE) {
+                            float so = sc;
+                            if (CE && k_split > 1) {
+                                // a piece's raw sums (nvalid is a multiple of 4)
+                                float4* d4 = reinterpret_cast<float4*>(p.k_part + ((long long)piece * p.k_part_rows + row_a) * p.out_stride + cb);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i)
+                                    if (4 * i < nvalid)
+                                        d4[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                                                            __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                                return;
+                            }
+                            if (CE && p.col_vec) {
                                 const float ra = p.row_add[row_a];
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
                                     if (i < nvalid) v[i] = __float_as_uint(fmaf(__uint_as_float(v[i]), sc, ra * p.col_vec[cb + i]));
+                                so = 1.0f;
                             }
-                            const float so = CE ? 1.0f : sc;
                             if (nvalid == 32) {
                                 uint32_t o[16];
 #pragma unroll
@@ -725,15 +847,14 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             w4[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
                                                 __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
                         __syncwarp();
-                        const int piece = lane & 7, rq = lane >> 3;
+                        const int piece8 = lane & 7, rq = lane >> 3;
                         const int row_w0 = row_a - lane;                 // first row of this warp's 32
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const int r = rq + 4 * j;
-                            float4 val = *reinterpret_cast<const float4*>(stg + r * kDrainPitch + piece * 4);
+                            const float4 val = *reinterpret_cast<const float4*>(stg + r * kDrainPitch + piece8 * 4);
                             if (row_w0 + r < M) {
-                                if (CE && finish_w(row_w0 + r, cb + piece * 4, val)) continue;
-                                float4* d4 = reinterpret_cast<float4*>(p.out_f32 + (long long)(row_w0 + r) * p.out_stride + cb) + piece;
+                                float4* d4 = reinterpret_cast<float4*>(p.out_f32 + (long long)(row_w0 + r) * p.out_stride + cb) + piece8;
                                 // accumulation is a fire-and-forget vector reduction at the memory side (no
                                 // read round trip in the drain); each element gets exactly one addend per
                                 // launch, so the result does not depend on timing
@@ -746,22 +867,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         }
                         __syncwarp();                                    // the tile is free for the next chunk
                     } else {   // kGradW
-                        if (CE && row_ok_a && (p.col_vec || p.out_w16)) {
-                            // nvalid is a multiple of 4 (the hidden size is a multiple of 64)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                if (4 * i >= nvalid) continue;
-                                float4 val = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
-                                                         __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
-                                if (finish_w(row_a, cb + 4 * i, val)) continue;
-                                float4* d4 = reinterpret_cast<float4*>(p.out_f32 + (long long)row_a * p.out_stride + cb + 4 * i);
-                                if (p.accumulate)
-                                    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
-                                                 :: "l"(d4), "f"(val.x), "f"(val.y), "f"(val.z), "f"(val.w) : "memory");
-                                else
-                                    *d4 = val;
-                            }
-                        } else if (row_ok_a) {
+                        if (row_ok_a) {
                             float* dst = p.out_f32 + (long long)row_a * p.out_stride + cb;
                             if (nvalid == 32) {
                                 float4* d4 = reinterpret_cast<float4*>(dst);
@@ -819,6 +925,8 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (p.part_u) p.part_u[(long long)row * p.nsplit + sp] = run_u;
             }
         }
+        // (CE) the last output tiles have been written before their shared memory goes
+        if (CE && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 
     // ---------------- teardown ----------------
@@ -1235,7 +1343,8 @@ static std::atomic<int> g_pace{1};          // pacing of the workers' loads (see
 static std::atomic<int> g_row_ref{1};       // backward scratch: 1 exponentials against a per-row reference, 0 per-tile maxima
 
 template <bool PAIR, bool ACC2, bool CE = false>
-static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, const GemmParams& p, cudaStream_t s) {
+static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const GemmParams& p,
+                                cudaStream_t s, int* workers_out) {
     static std::mutex mu;
     static bool opted[64] = {};
     int dev = 0;
@@ -1244,7 +1353,7 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
         std::lock_guard<std::mutex> lock(mu);
         if (dev >= 0 && dev < 64 && !opted[dev]) {
             if (cudaFuncSetAttribute((const void*)umma_gemm_kernel<PAIR, ACC2, CE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     Cfg<PAIR, ACC2>::kSmemBytes) != cudaSuccess) {
+                                     Cfg<PAIR, ACC2, CE>::kSmemBytes) != cudaSuccess) {
                 cudaGetLastError();
                 return RLF_ERR_CUDA;
             }
@@ -1254,7 +1363,7 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
     const bool sweep = p.mode == kLse;
     constexpr int kTilesPerUnit = (PAIR ? 2 : 1) * (ACC2 ? 2 : 1);
     const int m_units = (p.m_tiles + kTilesPerUnit - 1) / kTilesPerUnit;
-    const int units = sweep ? m_units * p.nsplit : m_units * p.n_tiles;
+    const int units = sweep ? m_units * p.nsplit : m_units * p.n_tiles * (p.k_split_max > 1 ? p.k_split_max : 1);
     if (units <= 0) return RLF_OK;
     int workers = PAIR ? sm_count_lm() / 2 : sm_count_lm();
     // Sweep schedule: the CTAs (or pairs) running at one time cover m_block row units x (workers / m_block)
@@ -1286,6 +1395,7 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
     }
     if (g_m_block.load() > 0) q.m_block = g_m_block.load();
     if (workers > units) workers = units;
+    if (workers_out) *workers_out = workers;
     // Pacing, measured at full size with one-pass ncu counts: grad_hidden 32 -> 10 GB of HBM reads and
     // 9.6 -> 8.5 ms per launch, grad_W 35 -> 11 GB and 10.3 -> 9.1 ms (D = 2560); the sweep at D = 4096
     // 71 -> 61 ms.  Meeting points inside a unit were tried too and cost more than they return.
@@ -1297,7 +1407,7 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(PAIR ? 2 * workers : workers);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Cfg<PAIR, ACC2>::kSmemBytes;
+    cfg.dynamicSmemBytes = Cfg<PAIR, ACC2, CE>::kSmemBytes;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -1306,7 +1416,7 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
     at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, umma_gemm_kernel<PAIR, ACC2, CE>, ma, mb, q) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, umma_gemm_kernel<PAIR, ACC2, CE>, ma, mb, mc, q) != cudaSuccess) {
         cudaGetLastError();
         return RLF_ERR_CUDA;
     }
@@ -1316,14 +1426,17 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
 
 static std::atomic<int> g_acc2{1};          // gradient contractions in pair form: 1 two accumulators per CTA, 0 one
 static rlf_status launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const GemmParams& p, bool pair,
-                              cudaStream_t s) {
-    if (p.col_vec || p.out_w16) {             // a gradient contraction of the cross-entropy form
-        if (!pair) return launch_gemm_t<false, false, true>(ma, mb, p, s);
-        return g_acc2.load() != 0 ? launch_gemm_t<true, true, true>(ma, mb, p, s) : launch_gemm_t<true, false, true>(ma, mb, p, s);
-    }
-    if (!pair) return launch_gemm_t<false, false>(ma, mb, p, s);
-    if (p.mode != kLse && g_acc2.load() != 0) return launch_gemm_t<true, true>(ma, mb, p, s);
-    return launch_gemm_t<true, false>(ma, mb, p, s);
+                              cudaStream_t s, int* workers_out = nullptr) {
+    if (!pair) return launch_gemm_t<false, false>(ma, mb, ma, p, s, workers_out);
+    if (p.mode != kLse && g_acc2.load() != 0) return launch_gemm_t<true, true>(ma, mb, ma, p, s, workers_out);
+    return launch_gemm_t<true, false>(ma, mb, ma, p, s, workers_out);
+}
+// gradient contractions of the cross-entropy form; mc: the bf16 grad_W that they store to, if any
+static rlf_status launch_gemm_ce(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const GemmParams& p,
+                                 bool pair, bool acc2, cudaStream_t s, int* workers_out = nullptr) {
+    if (!pair) return launch_gemm_t<false, false, true>(ma, mb, mc, p, s, workers_out);
+    if (acc2) return launch_gemm_t<true, true, true>(ma, mb, mc, p, s, workers_out);
+    return launch_gemm_t<true, false, true>(ma, mb, mc, p, s, workers_out);
 }
 
 // Rows of dZ held in scratch at a time: up to 148 token tiles = 37 units of the two-accumulator
@@ -1825,7 +1938,8 @@ ce_dead_rows_kernel(const int2* __restrict__ list, const int* __restrict__ count
 
 struct CeCombine {
     const float2* part;
-    int nsplit, rows_max;
+    int nsplit, rows_max;       // the partials' stride; the number of splits itself is found as the sweep found it:
+    int n_tiles, workers, rows_per_unit;
     const int2* list;
     const int* count;
     int off;
@@ -1859,15 +1973,17 @@ ce_combine_rows_kernel(const CeCombine p) {
     if (p.run_flag && *p.run_flag != 1) return;
     const int r = blockIdx.x * blockDim.x + threadIdx.x;
     const int n = max(0, min(*p.count - p.off, p.rows_max));
+    const int m_units = (n + p.rows_per_unit - 1) / p.rows_per_unit;
+    const int nsplit = m_units <= kAutoSplitUnits ? auto_split(m_units, p.n_tiles, p.workers, p.nsplit) : p.nsplit;
     if (r >= n) return;
     const int g = p.off + r;
     const int2 job = p.list[g];
     const int t = job.x;
     const float2* parts = p.part + (long long)r * p.nsplit;
     float M = -INFINITY;
-    for (int j = 0; j < p.nsplit; ++j) M = fmaxf(M, parts[j].x);
+    for (int j = 0; j < nsplit; ++j) M = fmaxf(M, parts[j].x);
     float S = 0.0f;
-    for (int j = 0; j < p.nsplit; ++j) {
+    for (int j = 0; j < nsplit; ++j) {
         const float2 ms = parts[j];
         if (ms.x != -INFINITY) S += ms.y * expf(ms.x - M);
     }
@@ -1905,6 +2021,37 @@ ce_combine_rows_kernel(const CeCombine p) {
     p.coef_g[g] = ok ? c * A : 0.0f;
     p.tgt_g[g] = c * tgt;
     p.ok_y[g] = ok ? job.y : -1;
+}
+
+// joins the pieces of grad_hidden's long axis: row r (of *count - off) of the output, factors applied as in the contraction's
+// epilogue.  Nothing to do where hidden_splits made one piece.
+__global__ void __launch_bounds__(256)
+ce_join_hidden_kernel(const float* __restrict__ part, long long part_rows, int D, const int* __restrict__ count, int off,
+                      int rows_max, const int32_t* __restrict__ row_index, const float* __restrict__ row_scale,
+                      const float* __restrict__ col_vec, const float* __restrict__ row_add, int rows_per_unit, int k_slabs,
+                      int workers, int k_split_max, __nv_bfloat16* __restrict__ out) {
+    const int n = max(0, min(*count - off, rows_max));
+    const int r = blockIdx.x;
+    const int pieces = hidden_splits((n + rows_per_unit - 1) / rows_per_unit, (D + BN - 1) / BN, k_slabs, workers, k_split_max);
+    if (r >= n || pieces == 1) return;
+    const float sc = row_scale ? row_scale[r] : 1.0f, ra = col_vec ? row_add[r] : 0.0f;
+    __nv_bfloat16* o = out + (long long)row_index[off + r] * D;
+    for (int c = 4 * threadIdx.x; c < D; c += 4 * blockDim.x) {
+        float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = 0; k < pieces; ++k) {
+            const float4 q = *reinterpret_cast<const float4*>(part + ((long long)k * part_rows + r) * D + c);
+            a.x += q.x; a.y += q.y; a.z += q.z; a.w += q.w;
+        }
+        a.x *= sc; a.y *= sc; a.z *= sc; a.w *= sc;
+        if (col_vec) {
+            const float4 u = *reinterpret_cast<const float4*>(col_vec + c);
+            a.x = fmaf(ra, u.x, a.x); a.y = fmaf(ra, u.y, a.y); a.z = fmaf(ra, u.z, a.z); a.w = fmaf(ra, u.w, a.w);
+        }
+        uint2 q;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.x) : "f"(a.y), "f"(a.x));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.y) : "f"(a.w), "f"(a.z));
+        *reinterpret_cast<uint2*>(o + c) = q;
+    }
 }
 
 // out[d] = sum_r weight[r] M[r, d] (weight NULL: 1) over the rows r < rows (or *count - off, if given and less):
@@ -1979,9 +2126,17 @@ static rlf_status launch_colsum(const __nv_bfloat16* M, int64_t rows, int32_t D,
     return cuda_ok(cudaGetLastError());
 }
 
+constexpr int kCeSplit = 80;                // most vocabulary splits of a sweep (sizes the partials): one row unit on 74 pairs
+// most pieces of grad_hidden's long axis: what 256 MB of fp32 rows hold
+static int hidden_pieces(int64_t T, int32_t D) {
+    int64_t rows = ((T > 0 ? T : 1) + 255) & ~(int64_t)255;
+    if (rows > kChunkTokens) rows = kChunkTokens;
+    const int64_t k = (64ll << 20) / (rows * D);
+    return (int)(k < 1 ? 1 : k > 64 ? 64 : k);
+}
 struct CeWs {
     size_t head, terms, list, zy, mean, part, idx_live, ok_y, lse_g, coef_g, tgt_g, add_g, ref_g, scale_g, ucol,
-        gcol, col_part, hidden_g, hidden_s, tmax, gw_acc, dz, total;
+        gcol, col_part, hidden_g, hidden_s, tmax, gw_acc, k_part, dz, total;
 };
 static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
     CeWs w;
@@ -1995,7 +2150,7 @@ static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
     w.list = take(8 * Tn);
     w.zy = take(4 * Tp);
     w.mean = take(4 * Tp);
-    w.part = take(8 * Tn * kMaxSplit);
+    w.part = take(8 * Tn * kCeSplit);
     w.idx_live = take(4 * Tp);
     w.ok_y = take(4 * Tp);
     w.lse_g = take(4 * Tp);
@@ -2012,6 +2167,7 @@ static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
     w.tmax = take(4 * chunk * tiles);
     // fp32 sum of grad_W over the chunks of a call whose result is bf16
     w.gw_acc = take(w16 && Tn > (size_t)kChunkTokens ? 4 * (size_t)V * Dn : 0);
+    w.k_part = take(4 * (size_t)hidden_pieces(T, D) * chunk * Dn);
     w.dz = take(2 * chunk * tiles * BN);
     w.total = o + 1024;
     return w;
@@ -2114,7 +2270,10 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
         z.k_slabs = D / BK;
         z.M = (int)tc;
         z.m_tiles = (int)((tc + BM - 1) / BM);
-        z.nsplit = pick_split(z.n_tiles);
+        // with few row units the sweep chooses its splits itself (auto_split); the host's choice is for more
+        const int64_t tile_units = (tc + 2 * BM - 1) / (2 * BM);
+        z.auto_split = 1;
+        z.nsplit = tile_units <= kAutoSplitUnits ? (kCeSplit < z.n_tiles ? kCeSplit : z.n_tiles) : pick_split(z.n_tiles);
         z.n_tiles_per_split = (z.n_tiles + z.nsplit - 1) / z.nsplit;
         z.part = reinterpret_cast<float2*>(ws + w.part);
         z.dev_status = dev_status;
@@ -2129,7 +2288,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
         CeCombine c = {};
         c.part = z.part; c.nsplit = z.nsplit; c.rows_max = (int)tc; c.list = list; c.count = counts;
         c.off = (int)t0; c.zy_g = at(w.zy); c.mean_g = at(w.mean); c.denom = dn; c.eps = label_smoothing; c.zeta = z_coef;
-        c.inv_v = inv_v; c.logp_out = logp_out; c.lse_out = lse_out; c.terms = terms; c.dev_status = dev_status;
+        c.inv_v = inv_v; c.n_tiles = z.n_tiles; c.rows_per_unit = (pair ? 2 : 1) * BM; c.logp_out = logp_out; c.lse_out = lse_out; c.terms = terms; c.dev_status = dev_status;
         if (bwd) {
             c.lse_g = at(w.lse_g); c.coef_g = at(w.coef_g); c.tgt_g = at(w.tgt_g);
             c.ok_y = reinterpret_cast<int32_t*>(ws + w.ok_y); c.add_g = at(w.add_g); c.scale_g = at(w.scale_g);
@@ -2139,7 +2298,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
         if (row_ref) {
             if (cudaMemsetAsync(chunk_flag, 0, sizeof(int), s) != cudaSuccess) return RLF_ERR_CUDA;
             z.ref = at(w.ref_g) + t0;
-            st = launch_gemm(mapHc, mapW, z, pair, s);
+            st = launch_gemm(mapHc, mapW, z, pair, s, &c.workers);
             if (st != RLF_OK) return st;
             CeCombine cr = c;
             cr.ref_g = at(w.ref_g);
@@ -2152,7 +2311,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             z.run_want = 1;
             c.run_flag = chunk_flag;
         }
-        st = launch_gemm(mapHc, mapW, z, pair, s);
+        st = launch_gemm(mapHc, mapW, z, pair, s, &c.workers);
         if (st != RLF_OK) return st;
         ce_combine_rows_kernel<<<row_blocks, 256, 0, s>>>(c);
         count_launch();
@@ -2185,9 +2344,21 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             h.row_scale = row_ref ? c.scale_g + t0 : nullptr;
             h.col_vec = ucol;
             h.row_add = c.add_g + t0;
+            h.k_split_max = hidden_pieces(T, D);
+            h.k_part = at(w.k_part);
+            h.k_part_rows = tcp;
             h.pace = z.pace;
-            st = launch_gemm(mapDzK, mapWn, h, pair, s);
+            // up to 256 rows fill one pair's accumulator: the second one would multiply nothing
+            const bool acc2 = g_acc2.load() != 0 && tc > 2 * BM;
+            int workers = 0;
+            st = launch_gemm_ce(mapDzK, mapWn, mapDzK, h, pair, acc2, s, &workers);
             if (st != RLF_OK) return st;
+            if (h.k_split_max > 1) {
+                ce_join_hidden_kernel<<<(unsigned)tc, 256, 0, s>>>(
+                    h.k_part, tcp, D, counts, (int)t0, (int)tc, idx_live, h.row_scale, ucol, h.row_add,
+                    (pair ? 2 : 1) * (pair && acc2 ? 2 : 1) * BM, h.k_slabs, workers, h.k_split_max, h.out_bf16);
+                count_launch();
+            }
         }
         if (grad_W) {
             scale_rows_kernel<<<(unsigned)tcp, 128, 0, s>>>(Hl + t0 * D, D, (int)tc, counts, (int)t0, c.scale_g, Hs);
@@ -2211,8 +2382,10 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             q.out_f32 = w16 ? at(w.gw_acc) : static_cast<float*>(grad_W);
             q.out_stride = D;
             q.accumulate = (accumulate_grad_W || t0 > 0) ? 1 : 0;
+            CUtensorMap mapGw = mapDzM;
             if (w16 && last) {                 // bf16 result: rounded once, from the sum over the chunks
-                q.out_w16 = static_cast<__nv_bfloat16*>(grad_W);
+                if (!make_map(&mapGw, grad_W, (uint64_t)V, (uint64_t)D, (uint64_t)D, 64, 32)) return RLF_ERR_CUDA;
+                q.store_w16 = 1;
                 q.add_f32 = t0 > 0 ? at(w.gw_acc) : nullptr;
                 q.accumulate = 0;
             }
@@ -2221,7 +2394,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             q.live_off = (int)t0;
             q.col_vec = smoothing ? at(w.gcol) : nullptr;
             q.pace = z.pace;
-            st = launch_gemm(mapDzM, mapHn, q, pair, s);
+            st = launch_gemm_ce(mapDzM, mapHn, mapGw, q, pair, g_acc2.load() != 0, s);
             if (st != RLF_OK) return st;
         }
     }

@@ -276,7 +276,7 @@ def test_refusals():
     assert e.value.code == -8
     with pytest.raises(ValueError):
         run(H, W, ids, mask, accumulate_grad_W=True)
-    with pytest.raises(ValueError):
+    with pytest.raises(TypeError):
         run(H, W.float(), ids, mask)
     with pytest.raises(b.RlfError):
         run(H, W[:63].contiguous(), ids, mask)
