@@ -114,9 +114,10 @@ struct GemmParams {
     // each fetches its slabs from HBM on its own.  Waits are bounded and only delay loads: a worker
     // that gives up runs on unpaced.
     int* pace;
-    // Sweep over device-counted rows (optional): with few row units the number of vocabulary splits is chosen on the device
-    // (auto_split; nsplit is then the most there may be, and the partials' stride)
-    int auto_split;
+    // Sweep over device-counted rows (optional): with at most auto_units row units the number of vocabulary splits is chosen
+    // on the device (auto_split); with more it is fixed_split, and only block_workers workers take part (the host's L2
+    // blocking).  nsplit is then the most splits there may be, and the partials' stride.
+    int auto_units, fixed_split, block_workers;
     // Cross-entropy form (CE, the gradient contractions).  Label smoothing adds a rank-one term to either gradient:
     const float* col_vec;     // kGradHidden (optional): out += row_add[r] * col_vec[col];  kGradW (optional): out += col_vec[col]
     const float* row_add;     // kGradHidden with col_vec: factor of compact row r
@@ -275,27 +276,32 @@ struct SmemCtl {
 
 static_assert(sizeof(SmemCtl) <= 256, "the barriers share a 256-byte slot behind the stage ring");
 
-// Vocabulary splits of a sweep with few row units: the persistent workers take the m_units x s units round-robin, so the
-// launch lasts about ceil(m_units s / workers) rounds of ceil(n_tiles / s) tiles (and a little per unit); the smallest such s.
-// (593 column tiles, 74 pairs: one row unit 74 splits instead of 60, 8 or 9 tiles each; six row units of 125 tiles 12 splits,
-// one round of 11 tiles, instead of 16, two rounds of 8.)  Every lane of a full warp calls it.
-constexpr int kAutoSplitUnits = 16;          // with more row units the fixed split and its L2 blocking are kept
+// Vocabulary splits of a sweep whose token tiles all stay in L2: the persistent workers take the m_units x s units
+// round-robin, so the launch lasts about ceil(m_units s / workers) rounds of ceil(n_tiles / s) tiles (and a little per unit); the
+// best such s.  (593 column tiles, 74 pairs: one row unit 74 splits of 8 or 9 tiles instead of 60 of 9 or 10; six row units of
+// 125 tiles 12 splits, one round of 11, instead of 16, two rounds of 8.)  Every lane of a full warp calls it.
 __device__ __forceinline__ int auto_split(int m_units, int n_tiles, int workers, int most) {
     const int lane = threadIdx.x & 31;
     unsigned best = 0xffffffffu;
     for (int s = lane + 1; s <= most && s <= n_tiles; s += 32) {
         const unsigned rounds = (unsigned)((m_units * s + workers - 1) / workers), tiles = (unsigned)((n_tiles + s - 1) / s);
-        const unsigned cost = (rounds * (8 * tiles + 1)) << 8 | (unsigned)s;
+        const unsigned cost = (rounds * (8 * tiles + 1)) << 7 | (unsigned)s;
         best = best < cost ? best : cost;
     }
-    return (int)(__reduce_min_sync(0xffffffffu, best) & 255u);
+    return (int)(__reduce_min_sync(0xffffffffu, best) & 127u);
 }
-// Pieces that the vocabulary is cut into in grad_hidden: as many as keep the workers busy, each of 16 slabs at least.
-__host__ __device__ __forceinline__ int hidden_splits(int m_units, int n_tiles, int k_slabs, int workers, int most) {
-    int k = m_units > 0 ? workers / (m_units * n_tiles) : 1;
-    if (k > k_slabs / 16) k = k_slabs / 16;
-    if (k > most) k = most;
-    return k < 1 ? 1 : k;
+// Pieces that the vocabulary is cut into in grad_hidden, `units` output tiles of k_slabs each on the workers: rounds of a
+// piece's slabs (six more for its drain), and a quarter of a slab's time per unit and piece to write and join its raw sums.
+// (10 row units x 16 column tiles on 74 pairs: three rounds uncut, 2.33 in three pieces.)  Every lane of a full warp calls it.
+__device__ __forceinline__ int hidden_splits(int units, int k_slabs, int workers, int most) {
+    const int lane = threadIdx.x & 31;
+    unsigned best = 0xffffffffu;
+    for (int k = lane + 1; k <= most && (k == 1 || k_slabs >= 16 * k); k += 32) {
+        const unsigned rounds = (unsigned)((units * k + workers - 1) / workers), slabs = (unsigned)((k_slabs + k - 1) / k);
+        const unsigned cost = (rounds * (slabs + 6) + (k > 1 ? (unsigned)(units * k + 3) / 4 : 0)) << 7 | (unsigned)k;
+        best = best < cost ? best : cost;
+    }
+    return (int)(__reduce_min_sync(0xffffffffu, best) & 127u);
 }
 
 // ---- the kernel -----------------------------------------------------------------------------
@@ -335,11 +341,20 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     constexpr int kTilesPerUnit = (PAIR ? 2 : 1) * NACC;
     const int m_units = (m_tiles + kTilesPerUnit - 1) / kTilesPerUnit;
     const int worker = PAIR ? blockIdx.x >> 1 : blockIdx.x;
-    const int workers = PAIR ? gridDim.x >> 1 : gridDim.x;
-    int nsplit = p.nsplit;
-    if (sweep && p.auto_split && m_units <= kAutoSplitUnits) nsplit = auto_split(m_units, p.n_tiles, workers, p.nsplit);
-    const int k_split = (CE && p.mode == kGradHidden) ? hidden_splits(m_units, p.n_tiles, k_slabs, workers, p.k_split_max) : 1;
-    const int units = (no_k && p.accumulate) ? 0 : sweep ? m_units * nsplit : m_units * p.n_tiles * k_split;
+    int workers = PAIR ? gridDim.x >> 1 : gridDim.x;
+    int nsplit = p.nsplit, m_block = p.m_block;
+    if (sweep && p.auto_units > 0) {
+        if (m_units <= p.auto_units) {
+            nsplit = auto_split(m_units, p.n_tiles, workers, p.nsplit);
+            m_block = p.auto_units;
+        } else {
+            nsplit = p.fixed_split;
+            workers = min(workers, p.block_workers);
+        }
+    }
+    const int k_split = (CE && p.mode == kGradHidden) ? hidden_splits(m_units * p.n_tiles, k_slabs, workers, p.k_split_max) : 1;
+    const int all_units = (no_k && p.accumulate) ? 0 : sweep ? m_units * nsplit : m_units * p.n_tiles * k_split;
+    const int units = worker < workers ? all_units : 0;      // (a worker beyond those that take part has nothing to do)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kStages; ++s) {
@@ -377,11 +392,11 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             // blocks of m_block row units; inside a block, units run over its row units first, then
             // over the splits: the CTAs running at one time share both the rows of the head they
             // sweep and a set of token tiles small enough to stay in L2
-            const int per_block = p.m_block * nsplit;
+            const int per_block = m_block * nsplit;
             const int blk = u / per_block, within = u - blk * per_block;
-            const int rows_here = min(p.m_block, m_units - blk * p.m_block);
+            const int rows_here = min(m_block, m_units - blk * m_block);
             const int sp = within / rows_here;
-            m = blk * p.m_block + (within - sp * rows_here);
+            m = blk * m_block + (within - sp * rows_here);
             // column tiles dealt evenly: the first split_rem splits hold one tile more than the others
             n0 = sp * split_base + min(sp, split_rem);
             n1 = n0 + split_base + (sp < split_rem ? 1 : 0);
@@ -418,7 +433,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             for (int u = worker; u < units && ok && !no_k; u += workers, ++iter) {
                 int m, n0, n1;
                 unit_range(u, m, n0, n1);
-                const int with_me = min(workers, units - iter * workers);     // workers that have a unit number `iter`
+                const int with_me = min(workers, all_units - iter * workers);     // workers that have a unit number `iter`
                 int k0, k1;
                 unit_k(u, k0, k1);
                 long long pos = 0;
@@ -1342,9 +1357,12 @@ static std::atomic<int> g_chunk_tiles{0};   // token tiles per backward chunk; 0
 static std::atomic<int> g_pace{1};          // pacing of the workers' loads (see GemmParams::pace): 1 on, 0 off
 static std::atomic<int> g_row_ref{1};       // backward scratch: 1 exponentials against a per-row reference, 0 per-tile maxima
 
+// what a launch settled that the kernels after it have to know
+struct Sched { int workers, auto_units; };
+
 template <bool PAIR, bool ACC2, bool CE = false>
 static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const GemmParams& p,
-                                cudaStream_t s, int* workers_out) {
+                                cudaStream_t s, Sched* sched) {
     static std::mutex mu;
     static bool opted[64] = {};
     int dev = 0;
@@ -1391,11 +1409,20 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
             if (w > best_w) { best_w = w; best_mb = mb; }
         }
         q.m_block = best_mb;
-        workers = best_w;
+        // a sweep that may size itself on the device launches every worker; the blocked form leaves some of them out there
+        q.block_workers = best_w;
+        if (p.auto_units > 0) q.auto_units = hi < 64 ? hi : 64;
+        else workers = best_w;
+    } else {
+        q.block_workers = workers;
+        if (p.auto_units > 0) q.auto_units = 1;
     }
     if (g_m_block.load() > 0) q.m_block = g_m_block.load();
     if (workers > units) workers = units;
-    if (workers_out) *workers_out = workers;
+    if (sched) {
+        sched->workers = workers;
+        sched->auto_units = q.auto_units;
+    }
     // Pacing, measured at full size with one-pass ncu counts: grad_hidden 32 -> 10 GB of HBM reads and
     // 9.6 -> 8.5 ms per launch, grad_W 35 -> 11 GB and 10.3 -> 9.1 ms (D = 2560); the sweep at D = 4096
     // 71 -> 61 ms.  Meeting points inside a unit were tried too and cost more than they return.
@@ -1426,17 +1453,17 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
 
 static std::atomic<int> g_acc2{1};          // gradient contractions in pair form: 1 two accumulators per CTA, 0 one
 static rlf_status launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const GemmParams& p, bool pair,
-                              cudaStream_t s, int* workers_out = nullptr) {
-    if (!pair) return launch_gemm_t<false, false>(ma, mb, ma, p, s, workers_out);
-    if (p.mode != kLse && g_acc2.load() != 0) return launch_gemm_t<true, true>(ma, mb, ma, p, s, workers_out);
-    return launch_gemm_t<true, false>(ma, mb, ma, p, s, workers_out);
+                              cudaStream_t s, Sched* sched = nullptr) {
+    if (!pair) return launch_gemm_t<false, false>(ma, mb, ma, p, s, sched);
+    if (p.mode != kLse && g_acc2.load() != 0) return launch_gemm_t<true, true>(ma, mb, ma, p, s, sched);
+    return launch_gemm_t<true, false>(ma, mb, ma, p, s, sched);
 }
 // gradient contractions of the cross-entropy form; mc: the bf16 grad_W that they store to, if any
 static rlf_status launch_gemm_ce(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const GemmParams& p,
-                                 bool pair, bool acc2, cudaStream_t s, int* workers_out = nullptr) {
-    if (!pair) return launch_gemm_t<false, false, true>(ma, mb, mc, p, s, workers_out);
-    if (acc2) return launch_gemm_t<true, true, true>(ma, mb, mc, p, s, workers_out);
-    return launch_gemm_t<true, false, true>(ma, mb, mc, p, s, workers_out);
+                                 bool pair, bool acc2, cudaStream_t s, Sched* sched = nullptr) {
+    if (!pair) return launch_gemm_t<false, false, true>(ma, mb, mc, p, s, sched);
+    if (acc2) return launch_gemm_t<true, true, true>(ma, mb, mc, p, s, sched);
+    return launch_gemm_t<true, false, true>(ma, mb, mc, p, s, sched);
 }
 
 // Rows of dZ held in scratch at a time: up to 148 token tiles = 37 units of the two-accumulator
@@ -1939,7 +1966,8 @@ ce_dead_rows_kernel(const int2* __restrict__ list, const int* __restrict__ count
 struct CeCombine {
     const float2* part;
     int nsplit, rows_max;       // the partials' stride; the number of splits itself is found as the sweep found it:
-    int n_tiles, workers, rows_per_unit;
+    int n_tiles, fixed_split, rows_per_unit;
+    Sched sched;
     const int2* list;
     const int* count;
     int off;
@@ -1974,7 +2002,7 @@ ce_combine_rows_kernel(const CeCombine p) {
     const int r = blockIdx.x * blockDim.x + threadIdx.x;
     const int n = max(0, min(*p.count - p.off, p.rows_max));
     const int m_units = (n + p.rows_per_unit - 1) / p.rows_per_unit;
-    const int nsplit = m_units <= kAutoSplitUnits ? auto_split(m_units, p.n_tiles, p.workers, p.nsplit) : p.nsplit;
+    const int nsplit = m_units <= p.sched.auto_units ? auto_split(m_units, p.n_tiles, p.sched.workers, p.nsplit) : p.fixed_split;
     if (r >= n) return;
     const int g = p.off + r;
     const int2 job = p.list[g];
@@ -2032,7 +2060,8 @@ ce_join_hidden_kernel(const float* __restrict__ part, long long part_rows, int D
                       int workers, int k_split_max, __nv_bfloat16* __restrict__ out) {
     const int n = max(0, min(*count - off, rows_max));
     const int r = blockIdx.x;
-    const int pieces = hidden_splits((n + rows_per_unit - 1) / rows_per_unit, (D + BN - 1) / BN, k_slabs, workers, k_split_max);
+    const int units = (n + rows_per_unit - 1) / rows_per_unit * ((D + BN - 1) / BN);
+    const int pieces = hidden_splits(units, k_slabs, workers, k_split_max);
     if (r >= n || pieces == 1) return;
     const float sc = row_scale ? row_scale[r] : 1.0f, ra = col_vec ? row_add[r] : 0.0f;
     __nv_bfloat16* o = out + (long long)row_index[off + r] * D;
@@ -2127,11 +2156,11 @@ static rlf_status launch_colsum(const __nv_bfloat16* M, int64_t rows, int32_t D,
 }
 
 constexpr int kCeSplit = 80;                // most vocabulary splits of a sweep (sizes the partials): one row unit on 74 pairs
-// most pieces of grad_hidden's long axis: what 256 MB of fp32 rows hold
+// most pieces of grad_hidden's long axis: what a gigabyte of fp32 rows holds
 static int hidden_pieces(int64_t T, int32_t D) {
     int64_t rows = ((T > 0 ? T : 1) + 255) & ~(int64_t)255;
     if (rows > kChunkTokens) rows = kChunkTokens;
-    const int64_t k = (64ll << 20) / (rows * D);
+    const int64_t k = (256ll << 20) / (rows * D);
     return (int)(k < 1 ? 1 : k > 64 ? 64 : k);
 }
 struct CeWs {
@@ -2270,10 +2299,10 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
         z.k_slabs = D / BK;
         z.M = (int)tc;
         z.m_tiles = (int)((tc + BM - 1) / BM);
-        // with few row units the sweep chooses its splits itself (auto_split); the host's choice is for more
-        const int64_t tile_units = (tc + 2 * BM - 1) / (2 * BM);
-        z.auto_split = 1;
-        z.nsplit = tile_units <= kAutoSplitUnits ? (kCeSplit < z.n_tiles ? kCeSplit : z.n_tiles) : pick_split(z.n_tiles);
+        // the sweep chooses its splits itself where the live rows' tiles stay in L2 (auto_split)
+        z.auto_units = 1;                      // (set to their number by the launch)
+        z.nsplit = kCeSplit < z.n_tiles ? kCeSplit : z.n_tiles;
+        z.fixed_split = pick_split(z.n_tiles);
         z.n_tiles_per_split = (z.n_tiles + z.nsplit - 1) / z.nsplit;
         z.part = reinterpret_cast<float2*>(ws + w.part);
         z.dev_status = dev_status;
@@ -2288,7 +2317,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
         CeCombine c = {};
         c.part = z.part; c.nsplit = z.nsplit; c.rows_max = (int)tc; c.list = list; c.count = counts;
         c.off = (int)t0; c.zy_g = at(w.zy); c.mean_g = at(w.mean); c.denom = dn; c.eps = label_smoothing; c.zeta = z_coef;
-        c.inv_v = inv_v; c.n_tiles = z.n_tiles; c.rows_per_unit = (pair ? 2 : 1) * BM; c.logp_out = logp_out; c.lse_out = lse_out; c.terms = terms; c.dev_status = dev_status;
+        c.inv_v = inv_v; c.n_tiles = z.n_tiles; c.fixed_split = z.fixed_split; c.rows_per_unit = (pair ? 2 : 1) * BM; c.logp_out = logp_out; c.lse_out = lse_out; c.terms = terms; c.dev_status = dev_status;
         if (bwd) {
             c.lse_g = at(w.lse_g); c.coef_g = at(w.coef_g); c.tgt_g = at(w.tgt_g);
             c.ok_y = reinterpret_cast<int32_t*>(ws + w.ok_y); c.add_g = at(w.add_g); c.scale_g = at(w.scale_g);
@@ -2298,7 +2327,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
         if (row_ref) {
             if (cudaMemsetAsync(chunk_flag, 0, sizeof(int), s) != cudaSuccess) return RLF_ERR_CUDA;
             z.ref = at(w.ref_g) + t0;
-            st = launch_gemm(mapHc, mapW, z, pair, s, &c.workers);
+            st = launch_gemm(mapHc, mapW, z, pair, s, &c.sched);
             if (st != RLF_OK) return st;
             CeCombine cr = c;
             cr.ref_g = at(w.ref_g);
@@ -2311,7 +2340,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             z.run_want = 1;
             c.run_flag = chunk_flag;
         }
-        st = launch_gemm(mapHc, mapW, z, pair, s, &c.workers);
+        st = launch_gemm(mapHc, mapW, z, pair, s, &c.sched);
         if (st != RLF_OK) return st;
         ce_combine_rows_kernel<<<row_blocks, 256, 0, s>>>(c);
         count_launch();
@@ -2350,13 +2379,13 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             h.pace = z.pace;
             // up to 256 rows fill one pair's accumulator: the second one would multiply nothing
             const bool acc2 = g_acc2.load() != 0 && tc > 2 * BM;
-            int workers = 0;
-            st = launch_gemm_ce(mapDzK, mapWn, mapDzK, h, pair, acc2, s, &workers);
+            Sched sched;
+            st = launch_gemm_ce(mapDzK, mapWn, mapDzK, h, pair, acc2, s, &sched);
             if (st != RLF_OK) return st;
             if (h.k_split_max > 1) {
                 ce_join_hidden_kernel<<<(unsigned)tc, 256, 0, s>>>(
                     h.k_part, tcp, D, counts, (int)t0, (int)tc, idx_live, h.row_scale, ucol, h.row_add,
-                    (pair ? 2 : 1) * (pair && acc2 ? 2 : 1) * BM, h.k_slabs, workers, h.k_split_max, h.out_bf16);
+                    (pair ? 2 : 1) * (pair && acc2 ? 2 : 1) * BM, h.k_slabs, sched.workers, h.k_split_max, h.out_bf16);
                 count_launch();
             }
         }
