@@ -1946,6 +1946,8 @@ ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloa
     }
 }
 
+constexpr int kCeSplit = 80;                // most vocabulary splits of a sweep (sizes the partials): one row unit on 74 pairs
+
 // rows without loss: NaN statistics, no loss term, a zero row of grad_hidden
 __global__ void __launch_bounds__(128)
 ce_dead_rows_kernel(const int2* __restrict__ list, const int* __restrict__ count, int T, int D,
@@ -1996,25 +1998,35 @@ struct CeCombine {
 // entry is formed as (expm1(logp) + 2 zeta lse p_y + eps) / A_t, which keeps its digits as p_y -> 1;
 // with |A_t| below a half (a log-sum-exp near -1 / (2 zeta)) that quotient is not formed, the chunk is
 // redone with dZ itself in the scratch.
+// One warp per row, its lanes along the splits.
 __global__ void __launch_bounds__(256)
 ce_combine_rows_kernel(const CeCombine p) {
     if (p.run_flag && *p.run_flag != 1) return;
-    const int r = blockIdx.x * blockDim.x + threadIdx.x;
+    const int r = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int n = max(0, min(*p.count - p.off, p.rows_max));
+    if (r >= n) return;
     const int m_units = (n + p.rows_per_unit - 1) / p.rows_per_unit;
     const int nsplit = m_units <= p.sched.auto_units ? auto_split(m_units, p.n_tiles, p.sched.workers, p.nsplit) : p.fixed_split;
-    if (r >= n) return;
     const int g = p.off + r;
     const int2 job = p.list[g];
     const int t = job.x;
     const float2* parts = p.part + (long long)r * p.nsplit;
+    constexpr int kPer = (kCeSplit + 31) / 32;
+    float2 q[kPer];
     float M = -INFINITY;
-    for (int j = 0; j < nsplit; ++j) M = fmaxf(M, parts[j].x);
-    float S = 0.0f;
-    for (int j = 0; j < nsplit; ++j) {
-        const float2 ms = parts[j];
-        if (ms.x != -INFINITY) S += ms.y * expf(ms.x - M);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int k = lane + 32 * j;
+        q[j] = k < nsplit ? parts[k] : make_float2(-INFINITY, 0.0f);
+        M = fmaxf(M, q[j].x);
     }
+    M = warp_max(M);
+    float S = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (q[j].x != -INFINITY) S += q[j].y * expf(q[j].x - M);
+    S = warp_sum(S);
+    if (lane != 0) return;
     const float ln_s = logf(S), zy = p.zy_g[g];
     const float lse = M + ln_s, logp = (zy - M) - ln_s;
     const float smooth = p.eps > 0.0f ? (M - p.mean_g[g]) + ln_s : 0.0f;
@@ -2067,6 +2079,7 @@ ce_join_hidden_kernel(const float* __restrict__ part, long long part_rows, int D
     __nv_bfloat16* o = out + (long long)row_index[off + r] * D;
     for (int c = 4 * threadIdx.x; c < D; c += 4 * blockDim.x) {
         float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
         for (int k = 0; k < pieces; ++k) {
             const float4 q = *reinterpret_cast<const float4*>(part + ((long long)k * part_rows + r) * D + c);
             a.x += q.x; a.y += q.y; a.z += q.z; a.w += q.w;
@@ -2155,7 +2168,6 @@ static rlf_status launch_colsum(const __nv_bfloat16* M, int64_t rows, int32_t D,
     return cuda_ok(cudaGetLastError());
 }
 
-constexpr int kCeSplit = 80;                // most vocabulary splits of a sweep (sizes the partials): one row unit on 74 pairs
 // most pieces of grad_hidden's long axis: what a gigabyte of fp32 rows holds
 static int hidden_pieces(int64_t T, int32_t D) {
     int64_t rows = ((T > 0 ? T : 1) + 255) & ~(int64_t)255;
@@ -2323,7 +2335,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             c.ok_y = reinterpret_cast<int32_t*>(ws + w.ok_y); c.add_g = at(w.add_g); c.scale_g = at(w.scale_g);
             c.dz = dz; c.dz_nc = z.dz_nc;
         }
-        const unsigned row_blocks = (unsigned)((tc + 255) / 256);
+        const unsigned row_blocks = (unsigned)((tc + 7) / 8);        // a warp per row
         if (row_ref) {
             if (cudaMemsetAsync(chunk_flag, 0, sizeof(int), s) != cudaSuccess) return RLF_ERR_CUDA;
             z.ref = at(w.ref_g) + t0;
@@ -2422,8 +2434,10 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             q.live_count = counts;
             q.live_off = (int)t0;
             q.col_vec = smoothing ? at(w.gcol) : nullptr;
-            q.pace = z.pace;
-            st = launch_gemm_ce(mapDzM, mapHn, mapGw, q, pair, g_acc2.load() != 0, s);
+            q.pace = tc > 512 ? z.pace : nullptr;        // (few tokens: a unit is shorter than a meeting)
+            // (129 to 512 tokens: a unit is mostly drain, which the form with one accumulator per unit overlaps with the next
+            // unit: 512 x 2560 x 151936 1.05 ms in all against 1.12; up to 128 the drain is all there is, 637 - 674 us either way)
+            st = launch_gemm_ce(mapDzM, mapHn, mapGw, q, pair, g_acc2.load() != 0 && !(tc > 2 * BK && tc <= 8 * BK), s);
             if (st != RLF_OK) return st;
         }
     }
