@@ -14,8 +14,11 @@ all-reduce sums over NCCL:
   3. for the fused LM-head path, grad_W [V, D] fp32 (the ordinary data-parallel weight-gradient
      all-reduce; grad_hidden and grad_logits stay with the rank that owns the rows).
 
-This module holds the host-side plan (which groups go to which rank) and the three-phase step.  The
-kernels are the C-ABI library's, passed in as `ops` (the binding module by default), so the same
+The supervised stage before the RL update (sharded_sft_step) is cut the same way, between responses
+(plan_shards with groups of one): the count, the four loss scalars, and the weight gradients of the
+head and of the norm in front of it are what the ranks exchange.
+
+This module holds the host-side plan (which groups go to which rank) and the steps.  The kernels are the C-ABI library's, passed in as `ops` (the binding module by default), so the same
 step can be driven by any implementation of those calls.
 """
 import numpy as np
@@ -150,4 +153,58 @@ def sharded_grpo_step(ids, cu_seqlens, rewards, group_size, old_logp, ref_logp, 
         _all_reduce_sum(out["grad_W"], group)
     out["loss"] = _all_reduce_sum(out["loss"].clone(), group)
     out.update(mask=mask, seq_id=seq_id, n_local=n_local, n_global=n_global)
+    return out
+
+
+def sharded_sft_step(ids, cu_seqlens, open_id, close_id, logits=None, hidden=None, W=None, residual=None,
+                     norm_weight=None, norm_bias=None, norm_kind=0, norm_eps=1e-6, label_smoothing=0.0, z_coef=0.0,
+                     grad_W=None, accumulate_grad_W=False, group=None, ops=None, reduce_grads=True, n_global=None):
+    """This rank's part of one supervised step over packed multi-turn responses: cross entropy of the model's own
+    tokens (tool observations carry no loss), averaged over the whole batch's loss-carrying tokens.
+
+    Give `logits` [T_local, V] (returns grad_logits), or `hidden` [T_local, D] and the head `W` [V, D] (returns
+    grad_hidden and grad_W; the logits are never stored).  With `norm_weight`, `hidden` (+ `residual`) is the last
+    block's output: it goes through the final norm (norm_kind: NORM_RMS or NORM_LAYER of the binding) first, and
+    grad_hidden is the gradient before that norm; grad_norm_weight (and grad_norm_bias) come back too.
+    `group`, `n_global`: as sharded_grpo_step; reduce_grads=False leaves the weight gradients unreduced (all but
+    the last of several accumulated micro-batches; the norm's gradients of those are this call's own).
+    -> dict(mask, n_local, n_global, logp, lse, loss (global, fp64[4]), grad_logits | grad_hidden, grad_W,
+       grad_norm_weight, grad_norm_bias)
+    """
+    ops = _ops(ops)
+    if (logits is None) == (hidden is None):
+        raise ValueError("give either logits or hidden + W")
+    if norm_weight is None and (norm_bias is not None or residual is not None):
+        raise ValueError("norm_bias and residual belong to the norm: give norm_weight")
+    if logits is not None and norm_weight is not None:
+        raise ValueError("the norm applies to hidden states, not to logits")
+    mask, _, n_local = count_phase(ids, cu_seqlens, open_id, close_id, ops)
+    if n_global is None:
+        n_global = _all_reduce_sum(n_local.clone(), group)
+    out = dict(mask=mask, n_local=n_local, n_global=n_global)
+    if logits is not None:
+        logp, lse, loss, grad = ops.rlf_cross_entropy_fwd_bwd(logits, ids, mask, label_smoothing=label_smoothing,
+                                                              z_coef=z_coef, denom=n_global)
+        out.update(grad_logits=grad)
+    else:
+        x, mean, rstd = hidden, None, None
+        if norm_weight is not None:
+            normed, total, mean, rstd = ops.rlf_norm_fwd(hidden, norm_weight, bias=norm_bias, residual=residual,
+                                                         kind=norm_kind, eps=norm_eps)
+            x, hidden = (hidden if total is None else total), normed
+        logp, lse, loss, gh, gw = ops.rlf_fused_lmhead_cross_entropy(hidden, W, ids, mask, label_smoothing=label_smoothing,
+                                                                     z_coef=z_coef, denom=n_global, grad_W=grad_W,
+                                                                     accumulate_grad_W=accumulate_grad_W)
+        if norm_weight is not None:
+            gh, gnw, gnb = ops.rlf_norm_bwd(gh, x, norm_weight, mean, rstd, kind=norm_kind,
+                                            want_grad_bias=norm_bias is not None)
+            out.update(grad_norm_weight=gnw)
+            if gnb is not None:
+                out.update(grad_norm_bias=gnb)
+        if reduce_grads:
+            for g in (gw, out.get("grad_norm_weight"), out.get("grad_norm_bias")):
+                if g is not None:
+                    _all_reduce_sum(g, group)
+        out.update(grad_hidden=gh, grad_W=gw)
+    out.update(logp=logp, lse=lse, loss=_all_reduce_sum(loss.clone(), group))
     return out
