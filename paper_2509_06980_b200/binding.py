@@ -450,14 +450,22 @@ def rlf_fused_lmhead_logp_entropy(hidden, W, ids, want_entropy=True, logp_out=No
 
 
 NORM_RMS, NORM_LAYER = 0, 1
+
+# The calls below are short next to a decoding step or a small batch, so their host side is kept lean: outputs are made by
+# the cheapest factory call and not checked again, workspace sizes are computed once per shape.
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_get_device = torch._C._cuda_getDevice
+_f32, _f64, _bf16, _i32t, _i64t, _u8 = (torch.float32, torch.float64, torch.bfloat16, torch.int32, torch.int64, torch.uint8)
+_DTYPES = {torch.bfloat16: RLF_BF16, torch.float32: RLF_F32}
 
 
-def _here(t):
-    """Index of the current device; the kernels run there, so a tensor of another device is refused."""
-    here = torch.cuda.current_device()
-    if t.get_device() != here:
-        raise ValueError("expected tensors on the current device, cuda:%d" % here)
+def _device_of(t):
+    """Index of the current device.  The kernels run there, so a tensor of another device is refused."""
+    here = t.get_device()
+    if here < 0:
+        raise ValueError("expected a CUDA tensor")
+    if here != _get_device():
+        raise ValueError("a tensor is on cuda:%d, the current device is cuda:%d" % (here, _get_device()))
     return here
 
 
@@ -480,28 +488,43 @@ def _rows(t, here, what):
     """Base address and row stride of a [T, D] tensor whose rows may be strided (last dimension dense)."""
     if t.get_device() != here:
         raise ValueError("%s must be on the current device, cuda:%d" % (what, here))
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be 2-dimensional with a contiguous last dimension" % what)
+    if t.dim() != 2:
+        raise ValueError("%s must be 2-dimensional" % what)
     T, D = t.shape
-    return (t.data_ptr() if T > 0 else None), (t.stride(0) if T > 1 else D)
+    rs, cs = t.stride()
+    if cs != 1 and D > 1:
+        raise ValueError("%s must have a contiguous last dimension" % what)
+    return (t.data_ptr() if T > 0 else None), (rs if T > 1 else D)
+
+
+def _dense_like(t):
+    """An empty dense tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 def _empty_rows_like(t, stride):
     """An empty [T, V] tensor whose rows sit in their 16-byte vectors as t's rows do (what the fast kernels need)."""
+    off = t.data_ptr() % 16 // t.element_size()
+    if off == 0 and t.is_contiguous():
+        return torch.empty_like(t)
     T, V = t.shape
-    off = t.data_ptr() % 16 // t.element_size() if T > 0 else 0
-    if off == 0:
-        return torch.empty_strided((T, V), (stride, 1), dtype=t.dtype, device=t.device)
-    return torch.empty((T - 1) * stride + V + off, dtype=t.dtype, device=t.device).as_strided((T, V), (stride, 1), off)
+    return t.new_empty((max(T, 1) - 1) * stride + V + off).as_strided((T, V), (stride, 1), off)
 
 
-def _workspace(workspace, here, which_fn, T, V, D, dt, dev):
+_bytes_of = {}
+
+
+def _workspace(workspace, here, like, *key):
+    """(tensor, address, bytes): the caller's workspace, or a new one of rlf_workspace_bytes(*key)."""
     if workspace is None:
-        n = _lib.rlf_workspace_bytes(which_fn, T, V, D, dt)
-        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=dev)
-    elif workspace.get_device() != here or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous tensor on the current device")
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        n = _bytes_of.get(key)
+        if n is None:
+            if len(_bytes_of) > 4096:
+                _bytes_of.clear()
+            n = _bytes_of[key] = max(int(_lib.rlf_workspace_bytes(*key)), 256)
+        workspace = like.new_empty(n, dtype=_u8)
+        return workspace, workspace.data_ptr(), n
+    return workspace, _at(workspace, here, "workspace"), workspace.numel() * workspace.element_size()
 
 
 def rlf_cross_entropy_fwd_bwd(logits, ids, mask=None, label_smoothing=0.0, z_coef=0.0, denom=None, grad_logits=None,
@@ -509,32 +532,33 @@ def rlf_cross_entropy_fwd_bwd(logits, ids, mask=None, label_smoothing=0.0, z_coe
                               workspace=None, dev_status=None):
     """Softmax cross entropy of the rows of logits [T, V] (rows may be strided) at targets ids, masked mean.
     -> (logp fp32[T], lse fp32[T] | None, loss fp64[4], grad_logits | None), all on the device."""
-    here = _here(logits)
+    here = _device_of(logits)
     zp, stride = _rows(logits, here, "logits")
     T, V = logits.shape
-    dev, f32 = logits.device, torch.float32
-    if grad_logits is None and want_grad:
-        grad_logits = logits if in_place else _empty_rows_like(logits, stride)
+    n = (T,)
     gp = None
-    if grad_logits is not None:
+    if grad_logits is None:
+        if want_grad:
+            grad_logits = logits if in_place else _empty_rows_like(logits, stride)
+            gp = grad_logits.data_ptr() if T > 0 else None
+    else:
         if grad_logits.shape != logits.shape or grad_logits.dtype != logits.dtype:
             raise ValueError("grad_logits must have the shape and type of logits")
         gp, gs = _rows(grad_logits, here, "grad_logits")
         if T > 1 and gs != stride:
             raise ValueError("grad_logits must have the row stride of logits")
     if logp_out is None:
-        logp_out = torch.empty(T, dtype=f32, device=dev)
+        logp_out = logits.new_empty(T, dtype=_f32)
     if lse_out is None and want_lse:
-        lse_out = torch.empty(T, dtype=f32, device=dev)
+        lse_out = logits.new_empty(T, dtype=_f32)
     if loss_out is None:
-        loss_out = torch.empty(4, dtype=torch.float64, device=dev)
-    workspace, wp, wn = _workspace(workspace, here, FN_CROSS_ENTROPY, T, V, 0, RLF_BF16, dev)
+        loss_out = logits.new_empty(4, dtype=_f64)
+    workspace, wp, wn = _workspace(workspace, here, logits, FN_CROSS_ENTROPY, T, V, 0, RLF_BF16)
     _check(_lib.rlf_cross_entropy_fwd_bwd(
-        zp, _dt(logits), T, V, stride, _at(ids, here, "ids", torch.int32, (T,)),
-        _at(mask, here, "mask", torch.uint8, (T,)), label_smoothing, z_coef, _at(denom, here, "denom", torch.int64),
-        _at(logp_out, here, "logp_out", f32, (T,)), _at(lse_out, here, "lse_out", f32, (T,)),
-        _at(loss_out, here, "loss_out", torch.float64, (4,)), gp, wp, wn,
-        _at(dev_status, here, "dev_status", torch.int32), _raw_stream(here)), "rlf_cross_entropy_fwd_bwd")
+        zp, _dt(logits), T, V, stride, _at(ids, here, "ids", _i32t, n), _at(mask, here, "mask", _u8, n), label_smoothing,
+        z_coef, _at(denom, here, "denom", _i64t), _at(logp_out, here, "logp_out", _f32, n),
+        _at(lse_out, here, "lse_out", _f32, n), _at(loss_out, here, "loss_out", _f64, (4,)), gp, wp, wn,
+        _at(dev_status, here, "dev_status", _i32t), _raw_stream(here)), "rlf_cross_entropy_fwd_bwd")
     return logp_out, lse_out, loss_out, grad_logits
 
 
@@ -545,32 +569,31 @@ def rlf_fused_lmhead_cross_entropy(hidden, W, ids, mask=None, label_smoothing=0.
     """rlf_cross_entropy_fwd_bwd of the logits hidden W^T, which are never stored.
     -> (logp fp32[T], lse fp32[T] | None, loss fp64[4], grad_hidden bf16[T,D] | None, grad_W [V,D] | None);
     grad_W is fp32 or (grad_W_dtype=torch.bfloat16) bf16."""
-    here = _here(hidden)
+    here = _device_of(hidden)
     T, D = hidden.shape
     V = W.shape[0]
-    dev, f32, bf16 = hidden.device, torch.float32, torch.bfloat16
+    n = (T,)
     if accumulate_grad_W and grad_W is None:
         raise ValueError("accumulate_grad_W needs the buffer that is added to")
     if grad_hidden is None and want_grad_hidden:
-        grad_hidden = torch.empty((T, D), dtype=bf16, device=dev)
+        grad_hidden = hidden.new_empty((T, D), dtype=_bf16)
     if grad_W is None and want_grad_W:
-        grad_W = torch.empty((V, D), dtype=grad_W_dtype, device=dev)
+        grad_W = hidden.new_empty((V, D), dtype=grad_W_dtype)
     if logp_out is None:
-        logp_out = torch.empty(T, dtype=f32, device=dev)
+        logp_out = hidden.new_empty(T, dtype=_f32)
     if lse_out is None and want_lse:
-        lse_out = torch.empty(T, dtype=f32, device=dev)
+        lse_out = hidden.new_empty(T, dtype=_f32)
     if loss_out is None:
-        loss_out = torch.empty(4, dtype=torch.float64, device=dev)
+        loss_out = hidden.new_empty(4, dtype=_f64)
     w_dt = RLF_F32 if grad_W is None else _dt(grad_W, "grad_W")
-    workspace, wp, wn = _workspace(workspace, here, FN_FUSED_CROSS_ENTROPY, T, V, D, w_dt, dev)
+    workspace, wp, wn = _workspace(workspace, here, hidden, FN_FUSED_CROSS_ENTROPY, T, V, D, w_dt)
     _check(_lib.rlf_fused_lmhead_cross_entropy(
-        _at(hidden, here, "hidden", bf16), _at(W, here, "W", bf16, (V, D)), T, D, V,
-        _at(ids, here, "ids", torch.int32, (T,)), _at(mask, here, "mask", torch.uint8, (T,)), label_smoothing, z_coef,
-        _at(denom, here, "denom", torch.int64), _at(logp_out, here, "logp_out", f32, (T,)),
-        _at(lse_out, here, "lse_out", f32, (T,)), _at(loss_out, here, "loss_out", torch.float64, (4,)),
-        _at(grad_hidden, here, "grad_hidden", bf16, (T, D)), _at(grad_W, here, "grad_W", None, (V, D)), w_dt,
-        1 if accumulate_grad_W else 0, wp, wn, _at(dev_status, here, "dev_status", torch.int32), _raw_stream(here)),
-        "rlf_fused_lmhead_cross_entropy")
+        _at(hidden, here, "hidden", _bf16), _at(W, here, "W", _bf16, (V, D)), T, D, V, _at(ids, here, "ids", _i32t, n),
+        _at(mask, here, "mask", _u8, n), label_smoothing, z_coef, _at(denom, here, "denom", _i64t),
+        _at(logp_out, here, "logp_out", _f32, n), _at(lse_out, here, "lse_out", _f32, n),
+        _at(loss_out, here, "loss_out", _f64, (4,)), _at(grad_hidden, here, "grad_hidden", _bf16, (T, D)),
+        _at(grad_W, here, "grad_W", None, (V, D)), w_dt, 1 if accumulate_grad_W else 0, wp, wn,
+        _at(dev_status, here, "dev_status", _i32t), _raw_stream(here)), "rlf_fused_lmhead_cross_entropy")
     return logp_out, lse_out, loss_out, grad_hidden, grad_W
 
 
@@ -579,31 +602,41 @@ def rlf_norm_fwd(x, weight, bias=None, residual=None, kind=NORM_RMS, eps=1e-6, y
     """Layer norm (NORM_LAYER) or its RMS form (NORM_RMS) of the rows of x (+ residual).
     x, residual: [T, D] (rows may be strided, the same stride); weight, bias: [D], bf16 or fp32.
     -> (y [T, D], x + residual [T, D] | None without residual, mean fp32[T] | None for the RMS form, rstd fp32[T])."""
-    here = _here(x)
+    here = _device_of(x)
     xp, xs = _rows(x, here, "x")
     shape = T, D = x.shape
-    dev, dt, f32 = x.device, x.dtype, torch.float32
+    dt, w_dt = x.dtype, weight.dtype
+    if dt not in _DTYPES or w_dt not in _DTYPES:
+        raise TypeError("x and weight must be bfloat16 or float32")
     rp = None
     if residual is not None:
-        if residual.shape != x.shape or residual.dtype != dt:
+        if residual.shape != shape or residual.dtype != dt:
             raise ValueError("residual must have the shape and type of x")
         rp, rs = _rows(residual, here, "residual")
         if T > 1 and rs != xs:
             raise ValueError("residual must have the row stride of x")
         if sum_out is None:
-            sum_out = torch.empty(shape, dtype=dt, device=dev)
+            sum_out = _dense_like(x)
+            sp = sum_out.data_ptr()
+        else:
+            sp = _at(sum_out, here, "sum_out", dt, shape)
+    else:
+        sp = _at(sum_out, here, "sum_out", dt, shape)
     if y_out is None:
-        y_out = torch.empty(shape, dtype=dt, device=dev)
+        y_out = _dense_like(x)
+        yp = y_out.data_ptr()
+    else:
+        yp = _at(y_out, here, "y_out", dt, shape)
     if mean_out is None and kind == NORM_LAYER:
-        mean_out = torch.empty(T, dtype=f32, device=dev)
+        mean_out = x.new_empty(T, dtype=_f32)
     if rstd_out is None:
-        rstd_out = torch.empty(T, dtype=f32, device=dev)
+        rstd_out = x.new_empty(T, dtype=_f32)
+        qp = rstd_out.data_ptr()
+    else:
+        qp = _at(rstd_out, here, "rstd_out", _f32, (T,))
     _check(_lib.rlf_norm_fwd(
-        xp, rp, _dt(x, "x"), T, D, xs, _at(weight, here, "weight", None, (D,)),
-        _at(bias, here, "bias", weight.dtype, (D,)), _dt(weight, "weight"), kind, eps,
-        _at(sum_out, here, "sum_out", dt, shape), _at(y_out, here, "y_out", dt, shape),
-        _at(mean_out, here, "mean_out", f32, (T,)), _at(rstd_out, here, "rstd_out", f32, (T,)), _raw_stream(here)),
-        "rlf_norm_fwd")
+        xp, rp, _DTYPES[dt], T, D, xs, _at(weight, here, "weight", w_dt, (D,)), _at(bias, here, "bias", w_dt, (D,)),
+        _DTYPES[w_dt], kind, eps, sp, yp, _at(mean_out, here, "mean_out", _f32, (T,)), qp, _raw_stream(here)), "rlf_norm_fwd")
     return y_out, sum_out, mean_out, rstd_out
 
 
@@ -611,30 +644,36 @@ def rlf_norm_bwd(grad_y, x, weight, mean, rstd, kind=NORM_RMS, grad_skip=None, w
                  want_grad_bias=False, grad_x=None, grad_weight=None, grad_bias=None, accumulate=False, workspace=None):
     """Backward of rlf_norm_fwd; x is what was normalised (the sum, with a residual); grad_skip is added to grad_x.
     -> (grad_x [T, D] | None, grad_weight fp32[D] | None, grad_bias fp32[D] | None)."""
-    here = _here(x)
+    here = _device_of(x)
     xp, xs = _rows(x, here, "x")
     shape = T, D = x.shape
-    dev, dt, f32 = x.device, x.dtype, torch.float32
-    if grad_y.shape != x.shape or grad_y.dtype != dt:
+    dt, w_dt = x.dtype, weight.dtype
+    if dt not in _DTYPES or w_dt not in _DTYPES:
+        raise TypeError("x and weight must be bfloat16 or float32")
+    if grad_y.shape != shape or grad_y.dtype != dt:
         raise ValueError("grad_y must have the shape and type of x")
     gp, gs = _rows(grad_y, here, "grad_y")
     if accumulate and ((grad_weight is None and want_grad_weight) or (grad_bias is None and want_grad_bias)):
         raise ValueError("accumulate needs the buffers that are added to")
-    if grad_x is None and want_grad_x:
-        grad_x = torch.empty(shape, dtype=dt, device=dev)
+    if grad_x is None:
+        xo = None
+        if want_grad_x:
+            grad_x = _dense_like(x)
+            xo = grad_x.data_ptr()
+    else:
+        xo = _at(grad_x, here, "grad_x", dt, shape)
     if grad_weight is None and want_grad_weight:
-        grad_weight = torch.empty(D, dtype=f32, device=dev)
+        grad_weight = x.new_empty(D, dtype=_f32)
     if grad_bias is None and want_grad_bias:
-        grad_bias = torch.empty(D, dtype=f32, device=dev)
+        grad_bias = x.new_empty(D, dtype=_f32)
     wp, wn = None, 0
     if workspace is not None or grad_weight is not None or grad_bias is not None:
-        workspace, wp, wn = _workspace(workspace, here, FN_NORM_BWD, T, 0, D, RLF_F32, dev)
+        workspace, wp, wn = _workspace(workspace, here, x, FN_NORM_BWD, T, 0, D, RLF_F32)
     _check(_lib.rlf_norm_bwd(
-        gp, gs, xp, xs, _dt(x, "x"), T, D, _at(weight, here, "weight", None, (D,)), _dt(weight, "weight"), kind,
-        _at(mean, here, "mean", f32, (T,)), _at(rstd, here, "rstd", f32, (T,)),
-        _at(grad_skip, here, "grad_skip", dt, shape), _at(grad_x, here, "grad_x", dt, shape),
-        _at(grad_weight, here, "grad_weight", f32, (D,)), _at(grad_bias, here, "grad_bias", f32, (D,)),
-        1 if accumulate else 0, wp, wn, _raw_stream(here)), "rlf_norm_bwd")
+        gp, gs, xp, xs, _DTYPES[dt], T, D, _at(weight, here, "weight", w_dt, (D,)), _DTYPES[w_dt], kind,
+        _at(mean, here, "mean", _f32, (T,)), _at(rstd, here, "rstd", _f32, (T,)),
+        _at(grad_skip, here, "grad_skip", dt, shape), xo, _at(grad_weight, here, "grad_weight", _f32, (D,)),
+        _at(grad_bias, here, "grad_bias", _f32, (D,)), 1 if accumulate else 0, wp, wn, _raw_stream(here)), "rlf_norm_bwd")
     return grad_x, grad_weight, grad_bias
 
 
