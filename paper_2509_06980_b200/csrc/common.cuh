@@ -33,9 +33,9 @@ rlf_status launch_seq_weights(const void* rec, const int32_t* seq_id, int64_t T,
 
 // cross-entropy stages (cross_entropy.cu), also used by the fused LM-head form: the work list (int2 {row, target id} of
 // the live rows in order, then {row, -1} of the others, last row first), the loss scalars from per-token terms
-// {-logp, smooth, lse, counts} (float4), argument check
+// {-logp, smooth, lse, counts} (float4), argument check.  The plan also zeroes zero_words (at most 1024) words at `zero`.
 rlf_status ce_launch_plan(const int32_t* ids, const uint8_t* mask, int64_t T, int32_t V, void* list, int* n_live,
-                          long long* n_mask, int32_t* dev_status, cudaStream_t s);
+                          long long* n_mask, int* zero, int zero_words, int32_t* dev_status, cudaStream_t s);
 rlf_status ce_launch_loss(const void* terms, int64_t T, const long long* denom, float eps, float zeta, double* loss_out,
                           cudaStream_t s);
 rlf_status ce_check_objective(float label_smoothing, float z_coef);

@@ -685,13 +685,15 @@ __device__ __forceinline__ double ld_cluster_double(const double* local, int ran
 // mask != 0.  CTA r takes the r-th stretch of kPlanTokens tokens of every step, a thread every 1024th token of it.
 __global__ void __launch_bounds__(kPlanThreads)
 ce_plan_kernel(const int32_t* __restrict__ ids, const uint8_t* __restrict__ mask, int T, int V, int2* __restrict__ list,
-               int* __restrict__ n_live, long long* __restrict__ n_mask, int32_t* __restrict__ dev_status) {
+               int* __restrict__ n_live, long long* __restrict__ n_mask, int* __restrict__ zero, int zero_words,
+               int32_t* __restrict__ dev_status) {
     __shared__ int piece[kPlanPer * 32];     // live rows of each (k, warp) of this CTA, then their exclusive sums
     __shared__ int cta_live[2];              // live rows of this CTA in a step, two steps in turn
     __shared__ int cta_masked;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int csize = (int)cluster_nctarank(), crank = (int)cluster_ctarank();
     pdl_trigger();
+    if (crank == 0 && tid < zero_words) zero[tid] = 0;       // flags and counters of the caller's later launches
     int base = 0, masked_in = 0, step = 0;
     bool bad = false;
     for (long long s0 = 0; s0 < T; s0 += (long long)csize * kPlanTokens, step ^= 1) {
@@ -903,9 +905,9 @@ static rlf_status launch_rows(const RowParams& p, rlf_dtype dt, cudaStream_t s) 
 }  // namespace ce
 
 rlf_status ce_launch_plan(const int32_t* ids, const uint8_t* mask, int64_t T, int32_t V, void* list, int* n_live,
-                          long long* n_mask, int32_t* dev_status, cudaStream_t s) {
+                          long long* n_mask, int* zero, int zero_words, int32_t* dev_status, cudaStream_t s) {
     return ce::launch_cluster(ce::ce_plan_kernel, ce::small_ctas(T, ce::kPlanTokens), ce::kPlanThreads, false, s, ids, mask,
-                              (int)T, (int)V, static_cast<int2*>(list), n_live, n_mask, dev_status);
+                              (int)T, (int)V, static_cast<int2*>(list), n_live, n_mask, zero, zero_words, dev_status);
 }
 rlf_status ce_launch_loss(const void* terms, int64_t T, const long long* denom, float eps, float zeta, double* loss_out,
                           cudaStream_t s) {
@@ -947,7 +949,7 @@ extern "C" rlf_status rlf_cross_entropy_fwd_bwd(const void* logits, rlf_dtype dt
     int2* list = reinterpret_cast<int2*>(ws + ws_list_off(T));
     long long* n_mask = reinterpret_cast<long long*>(ws);
     int* n_live = reinterpret_cast<int*>(ws + 64);
-    st = ce_launch_plan(ids, mask, T, V, list, n_live, n_mask, dev_status, s);
+    st = ce_launch_plan(ids, mask, T, V, list, n_live, n_mask, nullptr, 0, dev_status, s);
     if (st != RLF_OK) return st;
     const long long* dn = denom ? reinterpret_cast<const long long*>(denom) : n_mask;
     RowParams p;

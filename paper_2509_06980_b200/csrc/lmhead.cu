@@ -114,6 +114,7 @@ struct GemmParams {
     // each fetches its slabs from HBM on its own.  Waits are bounded and only delay loads: a worker
     // that gives up runs on unpaced.
     int* pace;
+    int pace_is_zero;         // the counter has been zeroed already (else the launch does it)
     // Sweep over device-counted rows (optional): with at most auto_units row units the number of vocabulary splits is chosen
     // on the device (auto_split); with more it is fixed_split, and only block_workers workers take part (the host's L2
     // blocking).  nsplit is then the most splits there may be, and the partials' stride.
@@ -1223,10 +1224,6 @@ scale_rows_kernel(const __nv_bfloat16* __restrict__ Hl, int D, int rows_max, con
         return;
     }
     const float f = scale_g[off + r];
-    if (f == 0.0f) {                       // a row that was taken out: its hidden state may hold anything
-        for (int i = threadIdx.x; i < nv; i += blockDim.x) dst[i] = make_uint4(0u, 0u, 0u, 0u);
-        return;
-    }
     const uint4* src = reinterpret_cast<const uint4*>(Hl + (long long)r * D);
     for (int i = threadIdx.x; i < nv; i += blockDim.x) {
         const uint4 z = src[i];
@@ -1427,7 +1424,7 @@ static rlf_status launch_gemm_t(const CUtensorMap& ma, const CUtensorMap& mb, co
     // 9.6 -> 8.5 ms per launch, grad_W 35 -> 11 GB and 10.3 -> 9.1 ms (D = 2560); the sweep at D = 4096
     // 71 -> 61 ms.  Meeting points inside a unit were tried too and cost more than they return.
     if (q.pace && g_pace.load() != 0) {
-        if (cudaMemsetAsync(q.pace, 0, sizeof(int), s) != cudaSuccess) return RLF_ERR_CUDA;
+        if (!q.pace_is_zero && cudaMemsetAsync(q.pace, 0, sizeof(int), s) != cudaSuccess) return RLF_ERR_CUDA;
     } else {
         q.pace = nullptr;
     }
@@ -1894,23 +1891,38 @@ extern "C" rlf_status rlf_fused_lmhead_logp_entropy(const void* hidden, const vo
 namespace rlf {
 namespace lm {
 
-// compact row r <- hidden row of work-list entry r for r < *count, its target logit, its mean logit (with u) and the
-// reference of its stored exponentials; rows up to the next multiple of 256 are zero-filled
+// Entry r of the work list.  A live row (r < n): its hidden row goes to compact row r, with its target logit, its mean logit
+// (with u), the reference of its stored exponentials and its place in the output; the compact rows up to the next multiple of
+// 256 are zero-filled.  A row without loss (n <= r < T): NaN statistics, no loss term, a zero row of grad_hidden.
 __global__ void __launch_bounds__(128)
-ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloat16* __restrict__ W, int D,
-                      const int2* __restrict__ list, const int* __restrict__ count, const float* __restrict__ u, float inv_v, __nv_bfloat16* __restrict__ out, int32_t* __restrict__ idx, float* __restrict__ zy_g,
-                      float* __restrict__ mean_g, float* __restrict__ ref_g) {
+ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloat16* __restrict__ W, int T, int D,
+                      const int2* __restrict__ list, const int* __restrict__ count, const float* __restrict__ u,
+                      float inv_v, __nv_bfloat16* __restrict__ out, int32_t* __restrict__ idx, float* __restrict__ zy_g,
+                      float* __restrict__ mean_g, float* __restrict__ ref_g, float* __restrict__ logp_out,
+                      float* __restrict__ lse_out, float4* __restrict__ terms, __nv_bfloat16* __restrict__ grad_hidden) {
     __shared__ float red[2][4];
     const int n = *count;
     const int r = blockIdx.x;
-    if (r >= ((n + 255) & ~255)) return;
-    uint4* dst = reinterpret_cast<uint4*>(out + (long long)r * D);
     const int nv = D / 8;
     if (r >= n) {
-        for (int i = threadIdx.x; i < nv; i += 128) dst[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (threadIdx.x == 0) ref_g[r] = 0.0f;
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        if (r < ((n + 255) & ~255)) {
+            for (int i = threadIdx.x; i < nv; i += 128) reinterpret_cast<uint4*>(out + (long long)r * D)[i] = zero;
+            if (threadIdx.x == 0) ref_g[r] = 0.0f;
+        }
+        if (r >= T) return;
+        const int t = list[r].x;
+        if (threadIdx.x == 0) {
+            const float nan = __int_as_float(0x7fc00000);
+            logp_out[t] = nan;
+            if (lse_out) lse_out[t] = nan;
+            terms[t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+        if (grad_hidden)
+            for (int i = threadIdx.x; i < nv; i += 128) reinterpret_cast<uint4*>(grad_hidden + (long long)t * D)[i] = zero;
         return;
     }
+    uint4* dst = reinterpret_cast<uint4*>(out + (long long)r * D);
     const int2 job = list[r];
     const uint4* src = reinterpret_cast<const uint4*>(hidden + (long long)job.x * D);
     const uint4* w = reinterpret_cast<const uint4*>(W + (long long)job.y * D);
@@ -1948,23 +1960,6 @@ ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloa
 
 constexpr int kCeSplit = 80;                // most vocabulary splits of a sweep (sizes the partials): one row unit on 74 pairs
 
-// rows without loss: NaN statistics, no loss term, a zero row of grad_hidden
-__global__ void __launch_bounds__(128)
-ce_dead_rows_kernel(const int2* __restrict__ list, const int* __restrict__ count, int T, int D,
-                    float* __restrict__ logp_out, float* __restrict__ lse_out, float4* __restrict__ terms, __nv_bfloat16* __restrict__ grad_hidden) {
-    if ((int)blockIdx.x >= T - *count) return;
-    const int t = list[T - 1 - (int)blockIdx.x].x;
-    if (threadIdx.x == 0) {
-        const float nan = __int_as_float(0x7fc00000);
-        logp_out[t] = nan;
-        if (lse_out) lse_out[t] = nan;
-        terms[t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    }
-    if (grad_hidden)
-        for (int i = threadIdx.x; i < D / 8; i += 128)
-            reinterpret_cast<uint4*>(grad_hidden + (long long)t * D)[i] = make_uint4(0u, 0u, 0u, 0u);
-}
-
 struct CeCombine {
     const float2* part;
     int nsplit, rows_max;       // the partials' stride; the number of splits itself is found as the sweep found it:
@@ -1993,7 +1988,30 @@ struct CeCombine {
     int dz_nc;
     int* fallback;
     const int* run_flag;
+    // grad_W wanted: the chunk's rows Hl times their factors go to Hs (zeros for a row that was taken out, whose hidden
+    // state may hold anything, and up to the next multiple of 256 rows)
+    const __nv_bfloat16* Hl;
+    __nv_bfloat16* Hs;
+    int D;
 };
+__device__ __forceinline__ void scale_row(const CeCombine& p, int r, float f, int lane) {
+    if (!p.Hs) return;
+    const uint4* src = reinterpret_cast<const uint4*>(p.Hl + (long long)r * p.D);
+    uint4* dst = reinterpret_cast<uint4*>(p.Hs + (long long)r * p.D);
+    for (int i = lane; i < p.D / 8; i += 32) {
+        uint4 o = make_uint4(0u, 0u, 0u, 0u);
+        if (f != 0.0f) {
+            const uint4 z = src[i];
+            const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+            uint32_t* q = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q[k])
+                    : "f"(__uint_as_float(w[k] & 0xffff0000u) * f), "f"(__uint_as_float(w[k] << 16) * f));
+        }
+        dst[i] = o;
+    }
+}
 // As combine_rows_kernel: statistics, outputs and gradient factors of one chunk's rows.  The target
 // entry is formed as (expm1(logp) + 2 zeta lse p_y + eps) / A_t, which keeps its digits as p_y -> 1;
 // with |A_t| below a half (a log-sum-exp near -1 / (2 zeta)) that quotient is not formed, the chunk is
@@ -2004,7 +2022,10 @@ ce_combine_rows_kernel(const CeCombine p) {
     if (p.run_flag && *p.run_flag != 1) return;
     const int r = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int n = max(0, min(*p.count - p.off, p.rows_max));
-    if (r >= n) return;
+    if (r >= n) {
+        if (r < ((n + 255) & ~255)) scale_row(p, r, 0.0f, lane);
+        return;
+    }
     const int m_units = (n + p.rows_per_unit - 1) / p.rows_per_unit;
     const int nsplit = m_units <= p.sched.auto_units ? auto_split(m_units, p.n_tiles, p.sched.workers, p.nsplit) : p.fixed_split;
     const int g = p.off + r;
@@ -2026,37 +2047,36 @@ ce_combine_rows_kernel(const CeCombine p) {
     for (int j = 0; j < kPer; ++j)
         if (q[j].x != -INFINITY) S += q[j].y * expf(q[j].x - M);
     S = warp_sum(S);
-    if (lane != 0) return;
     const float ln_s = logf(S), zy = p.zy_g[g];
     const float lse = M + ln_s, logp = (zy - M) - ln_s;
     const float smooth = p.eps > 0.0f ? (M - p.mean_g[g]) + ln_s : 0.0f;
     const bool ok = (M > -INFINITY) && (M < INFINITY) && (S > 0.0f) && (S < INFINITY) && (fabsf(lse) < INFINITY) &&
                     (fabsf(logp) < INFINITY) && (fabsf(smooth) < INFINITY);
     const float A = 1.0f + 2.0f * p.zeta * lse;
-    if (p.ref_g) {
-        const float rho = p.ref_g[g];
-        if (!(ok && (lse - rho <= kRefWindow) && fabsf(A) >= 0.5f)) {
-            atomicOr(p.fallback, 1);
-            return;
-        }
+    const long long N = *p.denom;
+    const float c = 1.0f / (float)(N > 1 ? N : 1);
+    const float rho = p.ref_g ? p.ref_g[g] : 0.0f;
+    if (p.ref_g && !(ok && (lse - rho <= kRefWindow) && fabsf(A) >= 0.5f)) {
+        if (lane == 0) atomicOr(p.fallback, 1);
+        return;
     }
+    // the row's factor (uniform over the warp)
+    const float f = p.ref_g ? c * A * expf(rho - lse) : ok ? 1.0f : 0.0f;
+    scale_row(p, r, f, lane);
+    if (lane != 0) return;
     const float nan = __int_as_float(0x7fc00000);
     p.logp_out[t] = ok ? logp : nan;
     if (p.lse_out) p.lse_out[t] = ok ? lse : nan;
     p.terms[t] = ok ? make_float4(-logp, smooth, lse, 1.0f) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (!ok && p.dev_status) atomicOr(p.dev_status, RLF_DEV_NONFINITE);
     if (!p.scale_g) return;
-    const long long N = *p.denom;
-    const float c = 1.0f / (float)(N > 1 ? N : 1);
     const float tgt = expm1f(logp) + fmaf(2.0f * p.zeta * lse, expf(logp), p.eps);
     p.add_g[g] = ok ? -c * p.eps * p.inv_v : 0.0f;
+    p.scale_g[g] = f;
     if (p.ref_g) {
-        const float rho = p.ref_g[g];
-        p.scale_g[g] = c * A * expf(rho - lse);
         p.dz[dz_offset(r, job.y, p.dz_nc)] = __float2bfloat16_rn(tgt / A * expf(lse - rho));
         return;
     }
-    p.scale_g[g] = ok ? 1.0f : 0.0f;
     p.lse_g[g] = ok ? lse : 0.0f;
     p.coef_g[g] = ok ? c * A : 0.0f;
     p.tgt_g[g] = c * tgt;
@@ -2186,7 +2206,7 @@ static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
     const size_t chunk = Tp < (size_t)kChunkTokens ? Tp : (size_t)kChunkTokens;
     const size_t tiles = (size_t)((V + BN - 1) / BN);
     auto take = [&](size_t bytes) { const size_t at = o; o += up1k(bytes); return at; };
-    w.head = take(1024);             // [0] mask count, [64] live rows, [128] chunk flag, [256] pacing counter
+    w.head = take(1024);             // [0] mask count, [64] live rows, [128] chunk flag and pacing counters
     w.terms = take(16 * Tn);
     w.list = take(8 * Tn);
     w.zy = take(4 * Tp);
@@ -2253,6 +2273,8 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     long long* n_mask = reinterpret_cast<long long*>(ws + w.head);
     int* counts = reinterpret_cast<int*>(ws + w.head + 64);
     int* chunk_flag = reinterpret_cast<int*>(ws + w.head + 128);
+    constexpr int kFlagWords = 8;                // [0] the chunk's flag, [4 ..] four meeting counters
+    int* pace = chunk_flag + 4;
     const long long* dn = denom ? reinterpret_cast<const long long*>(denom) : n_mask;
     float4* terms = reinterpret_cast<float4*>(ws + w.terms);
     const __nv_bfloat16* H = static_cast<const __nv_bfloat16*>(hidden);
@@ -2260,7 +2282,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     if (T == 0) {
         // no rows: a zero loss, and a gradient of zero unless it is accumulated
         if (!denom) {
-            st = ce_launch_plan(nullptr, nullptr, 0, V, nullptr, counts, n_mask, dev_status, s);
+            st = ce_launch_plan(nullptr, nullptr, 0, V, nullptr, counts, n_mask, nullptr, 0, dev_status, s);
             if (st != RLF_OK) return st;
         }
         if (grad_W && !accumulate_grad_W &&
@@ -2278,18 +2300,17 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     const bool bwd = grad_hidden || grad_W, smoothing = label_smoothing > 0.0f;
     const bool row_ref = bwd && g_row_ref.load() != 0;
     float* ucol = smoothing ? at(w.ucol) : nullptr;
-    st = ce_launch_plan(ids, mask, T, V, list, counts, n_mask, dev_status, s);
+    st = ce_launch_plan(ids, mask, T, V, list, counts, n_mask, chunk_flag, kFlagWords, dev_status, s);
     if (st != RLF_OK) return st;
     if (smoothing) {
         st = launch_colsum(Wm, V, D, nullptr, nullptr, 0, at(w.col_part), ucol, s);
         if (st != RLF_OK) return st;
     }
     const float inv_v = 1.0f / (float)V;
-    ce_gather_rows_kernel<<<(unsigned)Tp, 128, 0, s>>>(H, Wm, D, list, counts, ucol, inv_v, Hl, idx_live, at(w.zy),
-                                                       at(w.mean), at(w.ref_g));
-    ce_dead_rows_kernel<<<(unsigned)T, 128, 0, s>>>(list, counts, (int)T, D, logp_out, lse_out, terms,
-                                                    static_cast<__nv_bfloat16*>(grad_hidden));
-    count_launch(2);
+    ce_gather_rows_kernel<<<(unsigned)Tp, 128, 0, s>>>(H, Wm, (int)T, D, list, counts, ucol, inv_v, Hl, idx_live, at(w.zy),
+                                                       at(w.mean), at(w.ref_g), logp_out, lse_out, terms,
+                                                       static_cast<__nv_bfloat16*>(grad_hidden));
+    count_launch();
     if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
 
     const bool pair = g_pair.load() != 0;
@@ -2318,7 +2339,10 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
         z.n_tiles_per_split = (z.n_tiles + z.nsplit - 1) / z.nsplit;
         z.part = reinterpret_cast<float2*>(ws + w.part);
         z.dev_status = dev_status;
-        z.pace = reinterpret_cast<int*>(ws + w.head + 256);
+        // the chunk's flag and its launches' meeting counters, zeroed by the plan kernel or, from the second chunk on, here
+        if (t0 > 0 && cudaMemsetAsync(chunk_flag, 0, kFlagWords * sizeof(int), s) != cudaSuccess) return RLF_ERR_CUDA;
+        z.pace = pace;
+        z.pace_is_zero = 1;
         z.live_count = counts;
         z.live_off = (int)t0;
         if (bwd) {
@@ -2335,9 +2359,13 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             c.ok_y = reinterpret_cast<int32_t*>(ws + w.ok_y); c.add_g = at(w.add_g); c.scale_g = at(w.scale_g);
             c.dz = dz; c.dz_nc = z.dz_nc;
         }
-        const unsigned row_blocks = (unsigned)((tc + 7) / 8);        // a warp per row
+        if (grad_W) {
+            c.Hl = Hl + t0 * D;
+            c.Hs = Hs;
+            c.D = D;
+        }
+        const unsigned row_blocks = (unsigned)(tcp / 8);             // a warp per row, whole multiples of 256 rows
         if (row_ref) {
-            if (cudaMemsetAsync(chunk_flag, 0, sizeof(int), s) != cudaSuccess) return RLF_ERR_CUDA;
             z.ref = at(w.ref_g) + t0;
             st = launch_gemm(mapHc, mapW, z, pair, s, &c.sched);
             if (st != RLF_OK) return st;
@@ -2351,6 +2379,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             z.run_flag = chunk_flag;
             z.run_want = 1;
             c.run_flag = chunk_flag;
+            z.pace = pace + 1;
         }
         st = launch_gemm(mapHc, mapW, z, pair, s, &c.sched);
         if (st != RLF_OK) return st;
@@ -2388,7 +2417,8 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             h.k_split_max = hidden_pieces(T, D);
             h.k_part = at(w.k_part);
             h.k_part_rows = tcp;
-            h.pace = z.pace;
+            h.pace = pace + 2;
+            h.pace_is_zero = 1;
             // up to 256 rows fill one pair's accumulator: the second one would multiply nothing
             const bool acc2 = g_acc2.load() != 0 && tc > 2 * BM;
             Sched sched;
@@ -2402,8 +2432,6 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             }
         }
         if (grad_W) {
-            scale_rows_kernel<<<(unsigned)tcp, 128, 0, s>>>(Hl + t0 * D, D, (int)tc, counts, (int)t0, c.scale_g, Hs);
-            count_launch();
             if (smoothing) {
                 st = launch_colsum(Hl + t0 * D, tc, D, c.add_g + t0, counts, (int)t0, at(w.col_part), at(w.gcol), s);
                 if (st != RLF_OK) return st;
@@ -2434,7 +2462,8 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             q.live_count = counts;
             q.live_off = (int)t0;
             q.col_vec = smoothing ? at(w.gcol) : nullptr;
-            q.pace = tc > 512 ? z.pace : nullptr;        // (few tokens: a unit is shorter than a meeting)
+            q.pace_is_zero = 1;
+            q.pace = tc > 512 ? pace + 3 : nullptr;      // (few tokens: a unit is shorter than a meeting)
             // (129 to 512 tokens: a unit is mostly drain, which the form with one accumulator per unit overlaps with the next
             // unit: 512 x 2560 x 151936 1.05 ms in all against 1.12; up to 128 the drain is all there is, 637 - 674 us either way)
             st = launch_gemm_ce(mapDzM, mapHn, mapGw, q, pair, g_acc2.load() != 0 && !(tc > 2 * BK && tc <= 8 * BK), s);
