@@ -419,7 +419,7 @@ rlf_status rlf_fused_lmhead_logp_entropy(const void *hidden, const void *W, int6
  *   grad_logits  [T, V] dt with the same row_stride, or NULL (forward only); may be logits itself
  *   workspace    rlf_workspace_bytes(RLF_FN_CROSS_ENTROPY, T, V, 0, dt) bytes, 256-byte aligned; contents
  *                need not be initialised
- * T = 0 is valid (loss_out = 0).  T of 2^30 and more returns RLF_ERR_UNSUPPORTED.
+ * T = 0 is valid (loss_out = 0).  T or V of 2^30 and more returns RLF_ERR_UNSUPPORTED.
  */
 rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T, int32_t V,
                                      int64_t row_stride, const int32_t *ids, const uint8_t *mask,
@@ -445,7 +445,8 @@ rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T
  *   workspace   rlf_workspace_bytes(RLF_FN_FUSED_CROSS_ENTROPY, T, V, D, grad_W_dt) bytes, 256-byte aligned
  *               (chiefly a bf16 scratch of min(T, 18944) rows by V; with a bf16 grad_W and T > 18944 also
  *               an fp32 [V, D] sum); contents need not be initialised
- * T = 0 is valid (loss_out = 0; grad_W zeros, or unchanged when accumulated).
+ * T = 0 is valid (loss_out = 0; grad_W zeros, or unchanged when accumulated).  T, V or D of 2^30 and more
+ * returns RLF_ERR_UNSUPPORTED.
  */
 rlf_status rlf_fused_lmhead_cross_entropy(const void *hidden, const void *W, int64_t T, int32_t D,
                                           int32_t V, const int32_t *ids, const uint8_t *mask,
@@ -473,7 +474,8 @@ rlf_status rlf_fused_lmhead_cross_entropy(const void *hidden, const void *W, int
  *   mean_out     [T] fp32 or NULL (zeros for the RMS form);  rstd_out [T] fp32 or NULL: r
  * Outputs may not overlap inputs or each other, except that sum_out may be x or residual itself, and
  * y_out may be x or residual itself, when that input is dense (x_stride = D).
- * Non-finite inputs give what the formulas give, in their own row only.  T = 0 is valid.
+ * Non-finite inputs give what the formulas give, in their own row only.  T = 0 is valid.  D of 2^30 and
+ * more returns RLF_ERR_UNSUPPORTED (here and in rlf_norm_bwd).
  */
 #define RLF_NORM_RMS 0
 #define RLF_NORM_LAYER 1

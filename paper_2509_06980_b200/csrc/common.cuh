@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "../../include/rlf.h"
 
 namespace rlf {
@@ -43,6 +45,29 @@ rlf_status ce_check_objective(float label_smoothing, float z_coef);
 inline rlf_status cuda_ok(cudaError_t e) { return e == cudaSuccess ? RLF_OK : RLF_ERR_CUDA; }
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+// What fits on a device at once, remembered per (device, kernel, launch shape); a shape beyond the table's size replaces the
+// oldest.  Nothing here allocates, so nothing can throw through a C entry.
+struct ResidentTable {
+    struct Entry { int dev; const void* kernel; int a, b, n; };
+    std::mutex mu;
+    Entry entry[256];
+    int count = 0;
+    template <typename Ask> int get(const void* kernel, int a, int b, Ask ask) {
+        int dev = 0;
+        cudaGetDevice(&dev);
+        std::lock_guard<std::mutex> lock(mu);
+        const int have = count < 256 ? count : 256;
+        for (int i = 0; i < have; ++i) {
+            const Entry& e = entry[i];
+            if (e.dev == dev && e.kernel == kernel && e.a == a && e.b == b) return e.n;
+        }
+        const int n = ask(dev);
+        entry[count & 255] = {dev, kernel, a, b, n};
+        count = count == 511 ? 256 : count + 1;
+        return n;
+    }
+};
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;

@@ -10,10 +10,6 @@
 // Kernels, in launch order: ce_plan_kernel (work list: the rows that carry loss, then the others; their
 // count), the row kernel (writes logp, lse, the row's loss terms and grad_logits), ce_loss_kernel (fp64 sums in
 // a fixed order).  Rows without loss weight are not read at all; their gradient is written as zeros.
-#include <map>
-#include <mutex>
-#include <tuple>
-
 #include "common.cuh"
 #include "row.cuh"
 
@@ -625,26 +621,20 @@ static void cluster_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* at, int
 // clusters of this shape that are resident at once (0: the device takes none); cached per device, kernel and
 // cluster size, and opts the kernel in to its staging buffer on the way
 static int resident_clusters(RowKernel k, const RowShape& sh) {
-    static std::mutex mu;
-    static std::map<std::tuple<int, RowKernel, int>, int> cache;
-    int dev = 0;
-    cudaGetDevice(&dev);
-    std::lock_guard<std::mutex> lock(mu);
-    const auto key = std::make_tuple(dev, k, sh.cluster);
-    const auto hit = cache.find(key);
-    if (hit != cache.end()) return hit->second;
-    int n = 0;
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute at[2];
-    cluster_config(&cfg, at, sh.cluster * 148 * 8, sh, nullptr);
-    if (cudaFuncSetAttribute((const void*)k, cudaFuncAttributeMaxDynamicSharedMemorySize, stage_bytes(sh.threads, sh.nv)) != cudaSuccess ||
-        (sh.cluster > 8 && cudaFuncSetAttribute((const void*)k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
-        cudaOccupancyMaxActiveClusters(&n, (void*)k, &cfg) != cudaSuccess) {
-        cudaGetLastError();
-        n = 0;
-    }
-    cache[key] = n;
-    return n;
+    static ResidentTable table;
+    return table.get((const void*)k, sh.cluster, sh.threads, [&](int) {
+        int n = 0;
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute at[2];
+        cluster_config(&cfg, at, sh.cluster * 148 * 8, sh, nullptr);
+        if (cudaFuncSetAttribute((const void*)k, cudaFuncAttributeMaxDynamicSharedMemorySize, stage_bytes(sh.threads, sh.nv)) != cudaSuccess ||
+            (sh.cluster > 8 && cudaFuncSetAttribute((const void*)k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
+            cudaOccupancyMaxActiveClusters(&n, (void*)k, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            n = 0;
+        }
+        return n;
+    });
 }
 
 // A cluster handles about ten rows before it retires (whole generations of what is resident at once): with one
@@ -860,7 +850,7 @@ static int small_ctas(int64_t T, int64_t per_cta) {
 
 // The cluster kernel wherever a shape holds the row and the gradient rows sit like the logits rows within their
 // 16-byte vectors; otherwise (rows beyond 81,920 vectors, a gradient buffer of another alignment) the general one,
-// which reads a row three times (V = 151936 bf16, 8192 rows: 3.69 ms against 1.07).
+// which reads a row three times (V = 151936 bf16, 8192 rows: 3.69 ms against 0.79).
 static rlf_status launch_rows(const RowParams& p, rlf_dtype dt, cudaStream_t s) {
     const size_t esz = dt == RLF_BF16 ? 2 : 4;
     const int ve = (int)(16 / esz);
@@ -934,7 +924,7 @@ extern "C" rlf_status rlf_cross_entropy_fwd_bwd(const void* logits, rlf_dtype dt
     if (T < 0 || V < 1 || row_stride < V) return RLF_ERR_SHAPE;
     rlf_status st = ce_check_objective(label_smoothing, z_coef);
     if (st != RLF_OK) return st;
-    if (T >= (1ll << 30)) return RLF_ERR_UNSUPPORTED;
+    if (T >= (1ll << 30) || V >= (1 << 30)) return RLF_ERR_UNSUPPORTED;      // the kernels count both in 32 bits
     if (!loss_out) return RLF_ERR_NULL;
     if (T > 0 && (!logits || !ids || !logp_out)) return RLF_ERR_NULL;
     const size_t esz = dt == RLF_BF16 ? 2 : 4;

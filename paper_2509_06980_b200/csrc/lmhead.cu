@@ -2257,7 +2257,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     rlf_status st = ce_check_objective(label_smoothing, z_coef);
     if (st != RLF_OK) return st;
     const bool w16 = grad_W && grad_W_dt == RLF_BF16;
-    if (T >= (1ll << 30) || (w16 && accumulate_grad_W)) return RLF_ERR_UNSUPPORTED;
+    if (T >= (1ll << 30) || V >= (1 << 30) || D >= (1 << 30) || (w16 && accumulate_grad_W)) return RLF_ERR_UNSUPPORTED;
     if (!loss_out) return RLF_ERR_NULL;
     if (T > 0 && (!hidden || !W || !ids || !logp_out)) return RLF_ERR_NULL;
     if (!aligned(hidden, 16) || !aligned(W, 16) || !aligned(grad_hidden, 16) || !aligned(grad_W, 16) || !aligned(ids, 4) ||

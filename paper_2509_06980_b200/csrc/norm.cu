@@ -9,10 +9,6 @@
 // Both directions are bound by HBM: a row is read once and written once (about 10 arithmetic
 // instructions per element).  All sums and statistics are fp32; the sum h is rounded to the
 // activations' type only where it is stored, and y is formed from the unrounded h.
-#include <map>
-#include <mutex>
-#include <tuple>
-
 #include "common.cuh"
 
 namespace rlf {
@@ -820,7 +816,9 @@ struct Cut { bool wide; int nv, threads, rows, smem; };
 //   bf16 110 us against 117 - 122 with one or two vectors; else up to 512 threads of two vectors, two rows at a time:
 //   8191 x 4096 bf16 layer form 49 us against 54 with four vectors, 32768 x 2560 fp32 162 against 190.
 static bool pick_cut(bool bf16, bool wide, bool fwd, bool full, long long T, int D, int arrays, int vectors, Cut* c) {
-    const int esz = bf16 ? 2 : 4, nvec = D * esz / 16;
+    const int esz = bf16 ? 2 : 4;
+    if (D > kSmemLimit / esz) return false;            // (before any product of D)
+    const int nvec = D * esz / 16;
     c->wide = wide;
     c->nv = 1;
     if (wide) {
@@ -875,22 +873,17 @@ static BwdKernel bwd_kernel(bool bf16, const Cut& c) {
 // CTAs of this kernel that are resident at once (0: none fits); cached per device, kernel, width and shared memory, and opts
 // the kernel in to its shared memory on the way
 static int resident_ctas(const void* k, const Cut& c) {
-    static std::mutex mu;
-    static std::map<std::tuple<int, const void*, int, int>, int> cache;
-    int dev = 0;
-    cudaGetDevice(&dev);
-    std::lock_guard<std::mutex> lock(mu);
-    const auto key = std::make_tuple(dev, k, c.threads, c.smem);
-    const auto hit = cache.find(key);
-    if (hit != cache.end()) return hit->second;
-    int per_sm = 0, sms = 0;
-    if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, c.threads, c.smem) != cudaSuccess) {
-        cudaGetLastError();
-        per_sm = 0;
-    }
-    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    return cache[key] = per_sm * (sms > 0 ? sms : 148);
+    static ResidentTable table;
+    return table.get(k, c.threads, c.smem, [&](int dev) {
+        int per_sm = 0, sms = 0;
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, c.threads, c.smem) != cudaSuccess) {
+            cudaGetLastError();
+            per_sm = 0;
+        }
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        return per_sm * (sms > 0 ? sms : 148);
+    });
 }
 
 static rlf_status launch_reduce(const float* part, const float* part_b, int parts, int D, int accumulate, float* dw, float* db,
@@ -917,6 +910,7 @@ static int row_grid(long long T) { return (int)(T < 148 * 8 ? T : 148 * 8); }
 static rlf_status check_norm(int64_t T, int32_t D, rlf_dtype dt, rlf_dtype w_dt, int kind) {
     if ((dt != RLF_BF16 && dt != RLF_F32) || (w_dt != RLF_BF16 && w_dt != RLF_F32)) return RLF_ERR_DTYPE;
     if (T < 0 || D < 1) return RLF_ERR_SHAPE;
+    if (D >= (1 << 30)) return RLF_ERR_UNSUPPORTED;    // the kernels count columns in 32 bits
     if (kind != RLF_NORM_LAYER && kind != RLF_NORM_RMS) return RLF_ERR_UNSUPPORTED;
     return RLF_OK;
 }

@@ -18,7 +18,8 @@ The supervised stage before the RL update (sharded_sft_step) is cut the same way
 (plan_shards with groups of one): the count, the four loss scalars, and the weight gradients of the
 head and of the norm in front of it are what the ranks exchange.
 
-This module holds the host-side plan (which groups go to which rank) and the steps.  The kernels are the C-ABI library's, passed in as `ops` (the binding module by default), so the same
+This module holds the host-side plan (which groups go to which rank) and the steps.  The
+kernels are the C-ABI library's, passed in as `ops` (the binding module by default), so the same
 step can be driven by any implementation of those calls.
 """
 import numpy as np

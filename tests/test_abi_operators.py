@@ -102,3 +102,23 @@ def test_workspace_sizes_grow_with_the_problem(lib):
     # the scratch of a chunk, and an fp32 sum beside a bf16 gradient of more than one chunk
     assert f(9, 8192, 151936, 4096, 1) >= 2 * 8192 * 151936 and f(9, 18944, 512, 64, 0) == f(9, 18944, 512, 64, 1)
     assert f(9, 18945, 512, 64, 0) - f(9, 18945, 512, 64, 1) >= 4 * 512 * 64
+
+
+def test_sizes_beyond_the_counters_are_refused(lib):
+    """Columns, tokens and vocabulary entries are counted in 32 bits with room for one more step of a loop."""
+    big = 1 << 30
+    f = lib.rlf_norm_fwd
+    f.argtypes = [vp, vp, ci, i64, i32, i64, vp, vp, ci, ci, f32, vp, vp, vp, vp, vp]
+    for D in (big, 2 ** 31 - 1):
+        assert f(FAKE, None, 0, 1, D, D, FAKE, None, 0, 0, 1e-6, None, FAKE, None, None, None) == UNSUPPORTED
+    f = lib.rlf_norm_bwd
+    f.argtypes = [vp, i64, vp, i64, ci, i64, i32, vp, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp, sz, vp]
+    assert f(FAKE, big, FAKE, big, 0, 1, big, FAKE, 0, 0, None, FAKE, None, FAKE, FAKE, None, 0, FAKE, 1 << 62, None) == UNSUPPORTED
+    f = lib.rlf_cross_entropy_fwd_bwd
+    f.argtypes = [vp, ci, i64, i32, i64, vp, vp, f32, f32, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    assert f(FAKE, 0, 1, big, big, FAKE, None, 0.0, 0.0, None, FAKE, None, FAKE, None, FAKE, 1 << 20, None, None) == UNSUPPORTED
+    f = lib.rlf_fused_lmhead_cross_entropy
+    f.argtypes = [vp, vp, i64, i32, i32, vp, vp, f32, f32, vp, vp, vp, vp, vp, vp, ci, ci, vp, sz, vp, vp]
+    for D, V in ((64, big), (big, 64)):
+        assert f(FAKE, FAKE, 1, D, V, FAKE, None, 0.0, 0.0, None, FAKE, None, FAKE, None, None, 1, 0, FAKE, 1 << 62, None,
+                 None) == UNSUPPORTED
