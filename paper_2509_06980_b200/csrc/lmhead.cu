@@ -827,7 +827,11 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                                                             __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
                                 return;
                             }
-                            if (CE && p.col_vec) {
+                            if (CE && sc == 0.0f) {
+                                // a row that was taken out: zeros, whatever its zero entries met in W
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) v[i] = 0u;
+                            } else if (CE && p.col_vec) {
                                 const float ra = p.row_add[row_a];
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
@@ -2095,17 +2099,17 @@ ce_join_hidden_kernel(const float* __restrict__ part, long long part_rows, int D
     const int units = (n + rows_per_unit - 1) / rows_per_unit * ((D + BN - 1) / BN);
     const int pieces = hidden_splits(units, k_slabs, workers, k_split_max);
     if (r >= n || pieces == 1) return;
-    const float sc = row_scale ? row_scale[r] : 1.0f, ra = col_vec ? row_add[r] : 0.0f;
+    const float sc = row_scale[r], ra = col_vec ? row_add[r] : 0.0f;
     __nv_bfloat16* o = out + (long long)row_index[off + r] * D;
     for (int c = 4 * threadIdx.x; c < D; c += 4 * blockDim.x) {
         float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
-        for (int k = 0; k < pieces; ++k) {
+        for (int k = 0; sc != 0.0f && k < pieces; ++k) {       // (sc = 0: zeros, as in the epilogue)
             const float4 q = *reinterpret_cast<const float4*>(part + ((long long)k * part_rows + r) * D + c);
             a.x += q.x; a.y += q.y; a.z += q.z; a.w += q.w;
         }
         a.x *= sc; a.y *= sc; a.z *= sc; a.w *= sc;
-        if (col_vec) {
+        if (col_vec && sc != 0.0f) {
             const float4 u = *reinterpret_cast<const float4*>(col_vec + c);
             a.x = fmaf(ra, u.x, a.x); a.y = fmaf(ra, u.y, a.y); a.z = fmaf(ra, u.z, a.z); a.w = fmaf(ra, u.w, a.w);
         }
@@ -2411,7 +2415,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             h.live_count = counts;
             h.live_off = (int)t0;
             h.row_index = idx_live;
-            h.row_scale = row_ref ? c.scale_g + t0 : nullptr;
+            h.row_scale = c.scale_g + t0;      // 1 without the reference, 0 for a row that was taken out
             h.col_vec = ucol;
             h.row_add = c.add_g + t0;
             h.k_split_max = hidden_pieces(T, D);

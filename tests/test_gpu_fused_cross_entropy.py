@@ -201,6 +201,20 @@ def test_a_non_finite_row_is_taken_out_alone(form):
         assert not r["live"][[3, 77]].any() and torch.isfinite(out[4]).all() and torch.isfinite(out[3]).all()
 
 
+@pytest.mark.parametrize("T", [5, 300])
+def test_a_head_with_a_non_finite_row_gives_zero_gradients(form, T):
+    """Every row's logits hold a NaN (or, with smoothing, an infinite mean): all rows are taken out, gradients zeros."""
+    b = gc.binding()
+    H, W, ids, mask = _inputs(T, 64, 1032, 12)
+    H = H.abs() + 1.0
+    for bad, eps in ((float("nan"), 0.0), (float("nan"), 0.1), (float("-inf"), 0.1), (float("inf"), 0.0)):
+        W[5, 7] = bad
+        for dt in (BF, F32):
+            lp, lse, _, gh, gw = run(H, W, ids, mask, eps, status=b.DEV_NONFINITE, grad_W_dtype=dt)
+            assert torch.isnan(lp).all() and torch.isnan(lse).all()
+            assert not gh.any() and not gw.any()
+
+
 def test_targets_far_below_the_maximum_take_the_universal_scratch():
     """A target 130 below its row's maximum lies outside the window of the per-row reference: its chunk is redone,
     with the universal form's bits."""
