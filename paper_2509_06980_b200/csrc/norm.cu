@@ -40,6 +40,7 @@ struct FwdParams {
     float* rstd;                // nullable
     long long T;
     int D;
+    int period;                 // edge form: rows t and t + period sit alike in their 16-byte vectors
     float eps;
 };
 
@@ -59,6 +60,7 @@ struct BwdParams {
     float* part_b;
     long long T;
     int D;
+    int period;                 // as in FwdParams
 };
 
 constexpr int kGenThreads = 256;
@@ -200,6 +202,11 @@ norm_dw_reduce_kernel(const float* __restrict__ part, const float* __restrict__ 
 // sums and the pass that writes.  One exchange (one barrier) serves the R rows' sums.
 //   wide    every row starts on 16 bytes and the width fills its 16-byte vectors: a thread owns NV vectors of each row, copies
 //           them itself and reads back only those; its columns' weights and weight gradients live in registers;
+//   edge    (wide kernels with EDGE) rows on no boundary, all tensors' rows alike: with a stride that is no multiple of a vector
+//           the row's place in its vectors repeats after 2, 4 or 8 rows, so a CTA takes every 2nd, 4th or 8th row and its
+//           threads keep fixed columns all the same; only a row's first and last vector are masked and stored by element.  Forward
+//           (backward) of 20000 x 2603 bf16, layer form with residual: 114 us (125), the staged form 151 (198); 4999 x 1021
+//           fp32: 21 (23), staged 23 (29);
 //   staged  any width, stride and base: a row is copied as the aligned 16-byte chunks that cover it, by whichever thread, and a
 //           thread owns every blockDim-th column; weights and weight gradients live in shared memory.
 constexpr int kMaxThreads = 512;
@@ -330,21 +337,93 @@ __device__ __forceinline__ void cta_sums(float (&v)[K], float* red, int& turn) {
     }
 }
 
-// weights of a thread's columns, widened (0 beyond the width or without a vector)
+// Where a CTA's rows lie.  EDGE: rows q, q + period, ... with q = blockIdx.x mod period; `lead` elements of a row's first vector
+// belong to what lies before the row.
+template <typename T, bool EDGE>
+struct Rows {
+    long long q = 0, n;         // first row, number of rows
+    int lead = 0, nvec, period = 1;
+    long long first, step;      // this CTA's first batch and the way to the next, in rows of its class
+    __device__ __forceinline__ Rows(const void* x, long long stride, long long T_, int D, int period_, int R) {
+        constexpr int N = Vec<T>::N;
+        if constexpr (EDGE) {
+            period = period_;
+            q = blockIdx.x & (period - 1);
+            n = (T_ - q + period - 1) / period;
+            lead = (int)(reinterpret_cast<uintptr_t>(static_cast<const T*>(x) + q * stride) & 15) / (int)sizeof(T);
+            nvec = (lead + D + N - 1) / N;
+            first = (long long)(blockIdx.x / period) * R;
+            step = (long long)(gridDim.x / period) * R;
+        } else {
+            n = T_;
+            nvec = D / N;
+            first = (long long)blockIdx.x * R;
+            step = (long long)gridDim.x * R;
+        }
+    }
+    __device__ __forceinline__ long long row(long long j) const { return EDGE ? q + j * period : j; }
+    // vector c of the row that starts at src, on its way to dst; a tensor's very first vector is not read before its start
+    __device__ __forceinline__ void copy(uint4* dst, const T* src, int c, int D, bool top) const {
+        constexpr int N = Vec<T>::N;
+        const uint4* from = reinterpret_cast<const uint4*>(src - lead) + c;
+        if constexpr (!EDGE) {
+            cp_async16(smem_at(dst), from);
+        } else if (top && c == 0 && lead > 0) {
+            for (int e = lead; e < N && e < lead + D; ++e) reinterpret_cast<T*>(dst)[e] = src[e - lead];
+        } else {
+            cp_async16_part(smem_at(dst), from, min(16, (lead + D - c * N) * (int)sizeof(T)));
+        }
+    }
+    // which elements of vector c are the row's
+    __device__ __forceinline__ unsigned bits(int c, int D) const {
+        constexpr int N = Vec<T>::N;
+        const int lo = max(0, lead - c * N), hi = min(N, lead + D - c * N);
+        return hi > lo ? ((1u << hi) - 1u) & ~((1u << lo) - 1u) : 0u;
+    }
+    __device__ __forceinline__ void store(T* row_start, int c, const uint4& v, unsigned keep) const {
+        constexpr int N = Vec<T>::N;
+        T* d = row_start - lead;
+        if (!EDGE || keep == (1u << N) - 1u) {
+            reinterpret_cast<uint4*>(d)[c] = v;
+        } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if ((keep >> e) & 1u) {
+                    if constexpr (N == 4) reinterpret_cast<uint32_t*>(d)[c * N + e] = w[e];
+                    else reinterpret_cast<uint16_t*>(d)[c * N + e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+                }
+        }
+    }
+};
+// what a first or last vector holds of other rows becomes zero
+template <int P>
+__device__ __forceinline__ void mask_pairs(f2 (&v)[P], unsigned keep) {
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+        float lo, hi;
+        f2_split(v[e], lo, hi);
+        v[e] = f2_make((keep >> (2 * e)) & 1u ? lo : 0.0f, (keep >> (2 * e + 1)) & 1u ? hi : 0.0f);
+    }
+}
+__device__ __forceinline__ float ld_w_in(const void* w, int w_bf16, int D, int c) {
+    return c >= 0 && c < D ? ld_w(w, w_bf16, c) : 0.0f;
+}
+
+// weights of a thread's columns, widened (0 outside the width or without a vector)
 template <int P, int NV>
-__device__ __forceinline__ void load_w(const void* w, int w_bf16, int D, f2 (&f)[NV][P]) {
+__device__ __forceinline__ void load_w(const void* w, int w_bf16, int D, int lead, f2 (&f)[NV][P]) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < P; ++e) {
-            const int c = ((i * (int)blockDim.x + (int)threadIdx.x) * P + e) * 2;
-            const bool in = w != nullptr && c < D;               // the width fills its vectors: c + 1 is in it too
-            f[i][e] = in ? f2_make(ld_w(w, w_bf16, c), ld_w(w, w_bf16, c + 1)) : 0ull;
+            const int c = ((i * (int)blockDim.x + (int)threadIdx.x) * P + e) * 2 - lead;
+            f[i][e] = w != nullptr ? f2_make(ld_w_in(w, w_bf16, D, c), ld_w_in(w, w_bf16, D, c + 1)) : 0ull;
         }
 }
 
 // Forward.  The rows' elements (x + residual) are held unpacked in registers through the passes.
-template <typename T, int NV, int R, bool LAYER>
+template <typename T, int NV, int R, bool LAYER, bool EDGE>
 __global__ void __launch_bounds__(kMaxThreads)
 norm_fwd_wide_kernel(const FwdParams p) {
     using V = Vec<T>;
@@ -352,35 +431,40 @@ norm_fwd_wide_kernel(const FwdParams p) {
     extern __shared__ __align__(16) uint4 stage[];      // [2][R][arrays][NV][blockDim], a slot is its thread's own
     __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * R];
     int turn = 0;
-    const int nvec = p.D / N, th = blockDim.x, tid = threadIdx.x;
+    const int th = blockDim.x, tid = threadIdx.x;
     const int arrays = p.res ? 2 : 1;
+    const Rows<T, EDGE> rows(p.x, p.x_stride, p.T, p.D, p.period, R);
+    const int nvec = rows.nvec;
     const float inv_d = 1.0f / (float)p.D;
     auto slot = [&](int buf, int k, int a, int i) -> uint4* { return stage + (((buf * R + k) * arrays + a) * NV + i) * th + tid; };
-    auto fetch = [&](long long t0, int buf) {
+    unsigned keep[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) keep[i] = EDGE ? rows.bits(tid + i * th, p.D) : (1u << N) - 1u;
+    auto masked = [&](int i) { return EDGE && keep[i] != (1u << N) - 1u; };
+    auto fetch = [&](long long j0, int buf) {
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const long long t = t0 + k;
-            if (t < p.T) {
+            const long long t = rows.row(j0 + k);
+            if (j0 + k < rows.n) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int c = tid + i * th;
                     if (c < nvec) {
-                        cp_async16(smem_at(slot(buf, k, 0, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + t * p.x_stride) + c);
-                        if (p.res) cp_async16(smem_at(slot(buf, k, 1, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.res) + t * p.x_stride) + c);
+                        rows.copy(slot(buf, k, 0, i), static_cast<const T*>(p.x) + t * p.x_stride, c, p.D, t == 0);
+                        if (p.res) rows.copy(slot(buf, k, 1, i), static_cast<const T*>(p.res) + t * p.x_stride, c, p.D, t == 0);
                     }
                 }
             }
         }
         cp_async_commit();
     };
-    const long long step = (long long)gridDim.x * R;
-    long long t0 = (long long)blockIdx.x * R;
-    fetch(t0, 0);
+    long long j0 = rows.first;
+    fetch(j0, 0);
     f2 w[NV][P], b[LAYER ? NV : 1][P];                  // (the RMS form's bias, rare, is fetched where it is used)
-    load_w<P, NV>(p.w, p.w_bf16, p.D, w);
-    if constexpr (LAYER) load_w<P, NV>(p.b, p.w_bf16, p.D, b);
-    for (int buf = 0; t0 < p.T; t0 += step, buf ^= 1) {
-        fetch(t0 + step, buf ^ 1);
+    load_w<P, NV>(p.w, p.w_bf16, p.D, rows.lead, w);
+    if constexpr (LAYER) load_w<P, NV>(p.b, p.w_bf16, p.D, rows.lead, b);
+    for (int buf = 0; j0 < rows.n; j0 += rows.step, buf ^= 1) {
+        fetch(j0 + rows.step, buf ^ 1);
         cp_async_wait1();
         f2 h[R][NV][P];
         float s[R], mu[R];
@@ -398,6 +482,7 @@ norm_fwd_wide_kernel(const FwdParams p) {
 #pragma unroll
                         for (int e = 0; e < P; ++e) h[k][i][e] = f2_add(h[k][i][e], z[e]);
                     }
+                    if (masked(i)) mask_pairs<P>(h[k][i], keep[i]);
 #pragma unroll
                     for (int e = 0; e < P; ++e) q = LAYER ? f2_add(q, h[k][i][e]) : f2_fma(h[k][i][e], h[k][i][e], q);
                 }
@@ -413,11 +498,12 @@ norm_fwd_wide_kernel(const FwdParams p) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
                     if (tid + i * th < nvec) {
+                        f2 d[P];
 #pragma unroll
-                        for (int e = 0; e < P; ++e) {
-                            const f2 d = f2_add(h[k][i][e], m2);
-                            q = f2_fma(d, d, q);
-                        }
+                        for (int e = 0; e < P; ++e) d[e] = f2_add(h[k][i][e], m2);
+                        if (masked(i)) mask_pairs<P>(d, keep[i]);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) q = f2_fma(d[e], d[e], q);
                     }
                 s[k] = f2_sum(q);
             }
@@ -425,8 +511,8 @@ norm_fwd_wide_kernel(const FwdParams p) {
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const long long t = t0 + k;
-            if (t >= p.T) continue;
+            if (j0 + k >= rows.n) continue;
+            const long long t = rows.row(j0 + k);
             const float r = rsqrtf(s[k] * inv_d + p.eps);
             const f2 r2 = f2_make(r, r), m2 = f2_make(-mu[k], -mu[k]);
 #pragma unroll
@@ -434,14 +520,14 @@ norm_fwd_wide_kernel(const FwdParams p) {
                 const int c = tid + i * th;
                 if (c >= nvec) continue;
                 f2 o[P];
-                if (p.sum) reinterpret_cast<uint4*>(static_cast<T*>(p.sum) + t * p.D)[c] = V::pack(h[k][i]);
+                if (p.sum) rows.store(static_cast<T*>(p.sum) + t * p.D, c, V::pack(h[k][i]), keep[i]);
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
                     o[e] = f2_mul(f2_mul(LAYER ? f2_add(h[k][i][e], m2) : h[k][i][e], r2), w[i][e]);
                     if (LAYER) o[e] = f2_add(o[e], b[LAYER ? i : 0][e]);
-                    else if (p.b) o[e] = f2_add(o[e], f2_make(ld_w(p.b, p.w_bf16, c * N + 2 * e), ld_w(p.b, p.w_bf16, c * N + 2 * e + 1)));
+                    else if (p.b) o[e] = f2_add(o[e], f2_make(ld_w_in(p.b, p.w_bf16, p.D, c * N + 2 * e - rows.lead), ld_w_in(p.b, p.w_bf16, p.D, c * N + 2 * e + 1 - rows.lead)));
                 }
-                reinterpret_cast<uint4*>(static_cast<T*>(p.y) + t * p.D)[c] = V::pack(o);
+                rows.store(static_cast<T*>(p.y) + t * p.D, c, V::pack(o), keep[i]);
             }
             if (tid == 0) {
                 if (p.mean) p.mean[t] = mu[k];
@@ -454,7 +540,7 @@ norm_fwd_wide_kernel(const FwdParams p) {
 
 // Backward: a CTA owns the row.  One sum per row, mean(g xh), and with FULL (layer form, or a bias gradient asked for) also
 // mean(g) and the bias gradient; a CTA's weight gradients are added up row after row and leave as one partial row per CTA.
-template <typename T, int NV, int R, bool FULL>
+template <typename T, int NV, int R, bool FULL, bool EDGE>
 __global__ void __launch_bounds__(kMaxThreads)
 norm_bwd_wide_kernel(const BwdParams p) {
     using V = Vec<T>;
@@ -462,38 +548,43 @@ norm_bwd_wide_kernel(const BwdParams p) {
     extern __shared__ __align__(16) uint4 stage[];      // [2][R][dy, x (, skip)][NV][blockDim]
     __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * K];
     int turn = 0;
-    const int nvec = p.D / N, th = blockDim.x, tid = threadIdx.x;
+    const int th = blockDim.x, tid = threadIdx.x;
     const int arrays = p.skip ? 3 : 2;
+    const Rows<T, EDGE> rows(p.x, p.x_stride, p.T, p.D, p.period, R);
+    const int nvec = rows.nvec;
     const float inv_d = 1.0f / (float)p.D;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     auto slot = [&](int buf, int k, int a, int i) -> uint4* { return stage + (((buf * R + k) * arrays + a) * NV + i) * th + tid; };
     float mu_next[R], r_next[R];
-    auto fetch = [&](long long t0, int buf) {
+    unsigned keep[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) keep[i] = EDGE ? rows.bits(tid + i * th, p.D) : (1u << N) - 1u;
+    auto masked = [&](int i) { return EDGE && keep[i] != (1u << N) - 1u; };
+    auto fetch = [&](long long j0, int buf) {
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const long long t = t0 + k;
+            const long long t = rows.row(j0 + k);
             mu_next[k] = r_next[k] = 0.0f;
-            if (t < p.T) {
+            if (j0 + k < rows.n) {
                 if (FULL && p.layer) mu_next[k] = p.mean[t];
                 r_next[k] = p.rstd[t];
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int c = tid + i * th;
                     if (c < nvec) {
-                        cp_async16(smem_at(slot(buf, k, 0, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.dy) + t * p.dy_stride) + c);
-                        cp_async16(smem_at(slot(buf, k, 1, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + t * p.x_stride) + c);
-                        if (p.skip) cp_async16(smem_at(slot(buf, k, 2, i)), reinterpret_cast<const uint4*>(static_cast<const T*>(p.skip) + t * p.D) + c);
+                        rows.copy(slot(buf, k, 0, i), static_cast<const T*>(p.dy) + t * p.dy_stride, c, p.D, t == 0);
+                        rows.copy(slot(buf, k, 1, i), static_cast<const T*>(p.x) + t * p.x_stride, c, p.D, t == 0);
+                        if (p.skip) rows.copy(slot(buf, k, 2, i), static_cast<const T*>(p.skip) + t * p.D, c, p.D, t == 0);
                     }
                 }
             }
         }
         cp_async_commit();
     };
-    const long long step = (long long)gridDim.x * R;
-    long long t0 = (long long)blockIdx.x * R;
-    fetch(t0, 0);
+    long long j0 = rows.first;
+    fetch(j0, 0);
     f2 w[NV][P], dw[NV][P], db[FULL ? NV : 1][P];
-    load_w<P, NV>(p.w, p.w_bf16, p.D, w);
+    load_w<P, NV>(p.w, p.w_bf16, p.D, rows.lead, w);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -501,19 +592,19 @@ norm_bwd_wide_kernel(const BwdParams p) {
             dw[i][e] = 0ull;
             if (FULL) db[FULL ? i : 0][e] = 0ull;
         }
-    for (int buf = 0; t0 < p.T; t0 += step, buf ^= 1) {
+    for (int buf = 0; j0 < rows.n; j0 += rows.step, buf ^= 1) {
         float mu[R], r[R], s[K];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             mu[k] = mu_next[k];
             r[k] = r_next[k];
         }
-        fetch(t0 + step, buf ^ 1);
+        fetch(j0 + rows.step, buf ^ 1);
         cp_async_wait1();
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             f2 a = 0ull, b = 0ull;
-            if (t0 + k < p.T) {
+            if (j0 + k < rows.n) {
                 const f2 m2 = f2_make(-mu[k], -mu[k]), r2 = f2_make(r[k], r[k]);
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
@@ -521,6 +612,10 @@ norm_bwd_wide_kernel(const BwdParams p) {
                         f2 x[P], dy[P];
                         V::unpack(*slot(buf, k, 0, i), dy);
                         V::unpack(*slot(buf, k, 1, i), x);
+                        if (masked(i)) {
+                            mask_pairs<P>(dy, keep[i]);
+                            mask_pairs<P>(x, keep[i]);
+                        }
 #pragma unroll
                         for (int e = 0; e < P; ++e) {
                             const f2 xh = f2_mul(FULL ? f2_add(x[e], m2) : x[e], r2), q = f2_mul(dy[e], xh);
@@ -540,8 +635,8 @@ norm_bwd_wide_kernel(const BwdParams p) {
         cta_sums<K>(s, red, turn);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const long long t = t0 + k;
-            if (t >= p.T) continue;
+            if (j0 + k >= rows.n) continue;
+            const long long t = rows.row(j0 + k);
             // r (g - b - (x - mu) r a) = r g + x (- r^2 a) + (mu r^2 a - r b)
             const float a = s[k] * inv_d * r[k] * r[k];
             const float b = (FULL && p.layer) ? r[k] * (s[FULL ? R + k : 0] * inv_d) : 0.0f;
@@ -565,14 +660,25 @@ norm_bwd_wide_kernel(const BwdParams p) {
 #pragma unroll
                     for (int e = 0; e < P; ++e) o[e] = f2_add(o[e], q[e]);
                 }
-                reinterpret_cast<uint4*>(static_cast<T*>(p.dx) + t * p.D)[c] = V::pack(o);
+                rows.store(static_cast<T*>(p.dx) + t * p.D, c, V::pack(o), keep[i]);
             }
         }
     }
     cp_async_wait0();
     auto leave = [&](float* part, const f2 (&g)[P], int i) {
         const int c = (tid + i * th) * N;
-        if (part == nullptr || c >= p.D) return;
+        if (part == nullptr || tid + i * th >= nvec) return;
+        if constexpr (EDGE) {
+            float* d = part + (long long)blockIdx.x * p.D - rows.lead + c;
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                float lo, hi;
+                f2_split(g[e], lo, hi);
+                if ((keep[i] >> (2 * e)) & 1u) d[2 * e] = lo;
+                if ((keep[i] >> (2 * e + 1)) & 1u) d[2 * e + 1] = hi;
+            }
+            return;
+        }
         ulonglong2* d = reinterpret_cast<ulonglong2*>(part + (long long)blockIdx.x * p.D + c);
 #pragma unroll
         for (int e = 0; e < P; e += 2) d[e / 2] = make_ulonglong2(g[e], g[e + 1]);
@@ -806,7 +912,8 @@ static long long max_parts(long long T, int D) {
 static size_t part_stride(int parts, int D) { return ((size_t)parts * (size_t)D + 63) & ~(size_t)63; }
 
 // how rows are cut: wide (nv vectors per thread) or staged, `threads` threads, `rows` rows at a time, bytes of shared memory
-struct Cut { bool wide; int nv, threads, rows, smem; };
+enum Form { kStaged, kWide, kEdge };
+struct Cut { Form form; int nv, threads, rows, smem; };
 
 // false: no fast form holds the rows (the general kernels do: rows beyond 512 threads x 4 vectors, or that do not fit shared
 // memory when staged).  `arrays` rows are read per row; the staged form keeps `vectors` fp32 vectors of the width.
@@ -815,11 +922,12 @@ struct Cut { bool wide; int nv, threads, rows, smem; };
 //   Backward: bf16 rows without the second sum (RMS form, no bias) four vectors per thread, one row at a time: 32768 x 2560
 //   bf16 110 us against 117 - 122 with one or two vectors; else up to 512 threads of two vectors, two rows at a time:
 //   8191 x 4096 bf16 layer form 49 us against 54 with four vectors, 32768 x 2560 fp32 162 against 190.
-static bool pick_cut(bool bf16, bool wide, bool fwd, bool full, long long T, int D, int arrays, int vectors, Cut* c) {
+static bool pick_cut(bool bf16, Form form, bool fwd, bool full, long long T, int D, int arrays, int vectors, Cut* c) {
     const int esz = bf16 ? 2 : 4;
     if (D > kSmemLimit / esz) return false;            // (before any product of D)
-    const int nvec = D * esz / 16;
-    c->wide = wide;
+    const int v = 16 / esz, nvec = form == kEdge ? (D + 2 * v - 2) / v : D / v;
+    const bool wide = form != kStaged;
+    c->form = form;
     c->nv = 1;
     if (wide) {
         const int most = fwd ? 256 : (bf16 && !full && nvec <= 512) ? 128 : bf16 ? 256 : 512;
@@ -843,20 +951,28 @@ static bool pick_cut(bool bf16, bool wide, bool fwd, bool full, long long T, int
 
 typedef void (*FwdKernel)(const FwdParams);
 typedef void (*BwdKernel)(const BwdParams);
+template <typename T, int R, bool F, bool E>
+static FwdKernel fwd_wide_form(const Cut& c) {
+    if (c.nv == 1) return norm_fwd_wide_kernel<T, 1, R, F, E>;
+    if (c.nv == 2) return norm_fwd_wide_kernel<T, 2, R, F, E>;
+    return R == 1 ? norm_fwd_wide_kernel<T, 4, 1, F, E> : nullptr;
+}
 template <typename T, int R, bool F>
 static FwdKernel fwd_kernel_form(const Cut& c) {
-    if (!c.wide) return norm_fwd_staged_kernel<T, R, F>;
-    if (c.nv == 1) return norm_fwd_wide_kernel<T, 1, R, F>;
-    if (c.nv == 2) return norm_fwd_wide_kernel<T, 2, R, F>;
-    return R == 1 ? norm_fwd_wide_kernel<T, 4, 1, F> : nullptr;
+    if (c.form == kStaged) return norm_fwd_staged_kernel<T, R, F>;
+    return c.form == kEdge ? fwd_wide_form<T, R, F, true>(c) : fwd_wide_form<T, R, F, false>(c);
+}
+template <typename T, int R, bool F, bool E>
+static BwdKernel bwd_wide_form(const Cut& c) {
+    if (c.nv == 1) return norm_bwd_wide_kernel<T, 1, R, F, E>;
+    if (R == 4) return nullptr;                  // (narrow rows only)
+    if (c.nv == 2) return norm_bwd_wide_kernel<T, 2, (R < 4 ? R : 1), F, E>;
+    return R == 1 ? norm_bwd_wide_kernel<T, 4, 1, F, E> : nullptr;
 }
 template <typename T, int R, bool F>
 static BwdKernel bwd_kernel_form(const Cut& c) {
-    if (c.nv == 1 && c.wide) return norm_bwd_wide_kernel<T, 1, R, F>;
-    if (R == 4) return nullptr;                  // (narrow rows only)
-    if (!c.wide) return norm_bwd_staged_kernel<T, (R < 4 ? R : 1), F>;
-    if (c.nv == 2) return norm_bwd_wide_kernel<T, 2, (R < 4 ? R : 1), F>;
-    return R == 1 ? norm_bwd_wide_kernel<T, 4, 1, F> : nullptr;
+    if (c.form == kStaged) return R == 4 ? nullptr : norm_bwd_staged_kernel<T, (R < 4 ? R : 1), F>;
+    return c.form == kEdge ? bwd_wide_form<T, R, F, true>(c) : bwd_wide_form<T, R, F, false>(c);
 }
 template <bool F>
 static FwdKernel fwd_kernel(bool bf16, const Cut& c) {
@@ -905,6 +1021,27 @@ static rlf_status launch_reduce(const float* part, const float* part_b, int part
     return RLF_OK;
 }
 
+// Which of the forms fits rows at these addresses (NULL: not there) with these strides; `period` for the edge form: rows of all
+// tensors must sit alike in their vectors, and a CTA takes every period-th row.
+static Form row_form(bool bf16, long long T, int D, const void* const* at, int n, long long stride_a, long long stride_b, int* period) {
+    const int v = bf16 ? 8 : 4;
+    const uintptr_t base = reinterpret_cast<uintptr_t>(at[0]);
+    *period = 1;
+    for (int i = 1; i < n; ++i)
+        if (at[i] && (reinterpret_cast<uintptr_t>(at[i]) - base) % 16 != 0) return kStaged;
+    if (T > 1 && (stride_a % v != D % v || stride_b % v != D % v)) return kStaged;
+    if (base % 16 == 0 && D % v == 0) return kWide;
+    while (T > 1 && *period * (long long)D % v != 0) *period *= 2;
+    return T < *period ? kStaged : kEdge;
+}
+
+// CTAs that give each one batch: whole multiples of the period in the edge form
+static long long batches(long long T, const Cut& c, int period) {
+    if (c.form != kEdge) return (T + c.rows - 1) / c.rows;
+    const long long rows = (T + period - 1) / period;
+    return (rows + c.rows - 1) / c.rows * period;
+}
+
 static int row_grid(long long T) { return (int)(T < 148 * 8 ? T : 148 * 8); }
 
 static rlf_status check_norm(int64_t T, int32_t D, rlf_dtype dt, rlf_dtype w_dt, int kind) {
@@ -948,18 +1085,18 @@ extern "C" rlf_status rlf_norm_fwd(const void* x, const void* residual, rlf_dtyp
     p.layer = kind == RLF_NORM_LAYER; p.sum = sum_out; p.y = y_out; p.mean = mean_out; p.rstd = rstd_out;
     p.T = T; p.D = D; p.eps = eps;
     const bool bf16 = dt == RLF_BF16;
-    const int v = bf16 ? 8 : 4;
-    const bool wide = D % v == 0 && x_stride % v == 0 && aligned(x, 16) && aligned(residual, 16) && aligned(sum_out, 16) &&
-                      aligned(y_out, 16);
+    const void* const at[] = {x, residual, sum_out, y_out};
+    const Form form = row_form(bf16, T, D, at, 4, x_stride, x_stride, &p.period);
     Cut c;
-    if (pick_cut(bf16, wide, true, p.layer, T, D, residual ? 2 : 1, bias ? 2 : 1, &c)) {
+    auto cut = [&](Form f) { return pick_cut(bf16, f, true, p.layer, T, D, residual ? 2 : 1, bias ? 2 : 1, &c); };
+    if (cut(form) || (form == kEdge && cut(kStaged))) {
         const FwdKernel k = p.layer ? fwd_kernel<true>(bf16, c) : fwd_kernel<false>(bf16, c);
         const int resident = k ? resident_ctas((const void*)k, c) : 0;
         if (resident > 0) {
             // CTAs that retire after a quarter of a resident generation's rows: in step for the whole launch, all of them
             // load, then all store (32768 x 2560 bf16 with residual: 130 us as one generation, 109 as four)
-            long long grid = (T + c.rows - 1) / c.rows;
-            if (grid > 4ll * resident) grid = 4ll * resident;
+            long long grid = batches(T, c, p.period);
+            if (grid > 4ll * resident) grid = 4ll * resident / p.period * p.period;
             k<<<(unsigned)grid, c.threads, c.smem, s>>>(p);
             count_launch();
             return cuda_ok(cudaGetLastError());
@@ -1001,22 +1138,21 @@ extern "C" rlf_status rlf_norm_bwd(const void* grad_y, int64_t grad_y_stride, co
     float* part = static_cast<float*>(workspace);
     if (T > 0) {
         const bool bf16 = dt == RLF_BF16;
-        const int v = bf16 ? 8 : 4;
-        const bool wide = D % v == 0 && x_stride % v == 0 && grad_y_stride % v == 0 && aligned(grad_y, 16) && aligned(x, 16) &&
-                          aligned(grad_skip, 16) && aligned(grad_x, 16);
+        const void* const at[] = {x, grad_y, grad_skip, grad_x};
+        const Form form = row_form(bf16, T, D, at, 4, x_stride, grad_y_stride, &p.period);
         const bool full = layer || grad_bias;
         Cut c;
         BwdKernel k = nullptr;
         long long resident = 0;
-        if (pick_cut(bf16, wide, false, full, T, D, grad_skip ? 3 : 2, grad_bias ? 3 : 2, &c)) {
+        auto cut = [&](Form f) { return pick_cut(bf16, f, false, full, T, D, grad_skip ? 3 : 2, grad_bias ? 3 : 2, &c); };
+        if (cut(form) || (form == kEdge && cut(kStaged))) {
             k = full ? bwd_kernel<true>(bf16, c) : bwd_kernel<false>(bf16, c);
             resident = k ? resident_ctas((const void*)k, c) : 0;
         }
         if (resident > 0) {
-            long long grid = (T + c.rows - 1) / c.rows;
-            const long long most = max_parts(T, D);
-            if (grid > resident) grid = resident;        // (more CTAs would mean more partial rows: 110 -> 117 us at twice as many)
-            if (grid > most) grid = most;
+            long long grid = batches(T, c, p.period), most = max_parts(T, D);
+            if (most > resident) most = resident;        // (more CTAs would mean more partial rows: 110 -> 117 us at twice as many)
+            if (grid > most) grid = c.form == kEdge ? most / p.period * p.period : most;
             parts = (int)grid;
             p.part = grad_weight ? part : nullptr;
             p.part_b = grad_bias ? part + part_stride(parts, D) : nullptr;

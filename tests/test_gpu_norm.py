@@ -175,6 +175,35 @@ def test_a_non_finite_row_stays_in_its_row(D):
         assert torch.equal(gx[keep], gc_[keep])
 
 
+@pytest.mark.parametrize("T,D", [(1, 5), (3, 640), (9, 5), (8, 13), (40, 1021), (301, 2603), (23, 2048), (1200, 77)])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("off", [0, 1, 3])
+def test_rows_off_their_vectors(T, D, dt, off):
+    """All tensors start `off` elements into a 16-byte vector and the strides differ by whole vectors; what lies between
+    the rows is NaN and stays as it is."""
+    b = gc.binding()
+    nan = float("nan")
+
+    def place(src, gap):
+        buf = torch.full((off + T * (D + gap) + 16,), nan, dtype=dt, device=DEV)
+        v = buf.as_strided((T, D), (D + gap, 1), off)
+        v.copy_(src)
+        return buf, v
+
+    for layer in (False, True):
+        kind = b.NORM_LAYER if layer else b.NORM_RMS
+        x0, res0, w, bias = _draw(T, D, dt, BF, 5 * T + D + off, residual=True, bias=True)
+        dy0, skip0, _, _ = _draw(T, D, dt, BF, 7 * T + D, residual=True, scale=1e-2, offset=0.0)
+        (_, x), (_, res), (by, y), (bs, s) = place(x0, 8), place(res0, 8), place(x0, 0), place(x0, 0)
+        out = b.rlf_norm_fwd(x, w, bias=bias, residual=res, kind=kind, y_out=y, sum_out=s)
+        check_fwd(out, x0, res0, w, bias, layer, 1e-6)
+        (_, dy), (_, sk), (bg, gx) = place(dy0, 16), place(skip0, 0), place(x0, 0)
+        got = b.rlf_norm_bwd(dy, s, w, out[2], out[3], kind=kind, grad_skip=sk, grad_x=gx, want_grad_bias=True)
+        check_bwd(got, dy0, s, w, out[2], out[3], layer, skip0)
+        for buf in (by, bs, bg):
+            assert torch.isnan(buf[:off]).all() and torch.isnan(buf[off + T * D:]).all()
+
+
 def test_constant_zero_and_offset_rows():
     """A constant row (variance zero) gives the bias and no NaN; a large common offset costs the layer form only
     the digits that the fp32 input does not hold."""
