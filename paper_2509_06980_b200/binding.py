@@ -553,7 +553,7 @@ def rlf_cross_entropy_fwd_bwd(logits, ids, mask=None, label_smoothing=0.0, z_coe
         lse_out = logits.new_empty(T, dtype=_f32)
     if loss_out is None:
         loss_out = logits.new_empty(4, dtype=_f64)
-    workspace, wp, wn = _workspace(workspace, here, logits, FN_CROSS_ENTROPY, T, V, 0, RLF_BF16)
+    workspace, wp, wn = _workspace(workspace, here, logits, FN_CROSS_ENTROPY, T, V, 0, _dt(logits))
     _check(_lib.rlf_cross_entropy_fwd_bwd(
         zp, _dt(logits), T, V, stride, _at(ids, here, "ids", _i32t, n), _at(mask, here, "mask", _u8, n), label_smoothing,
         z_coef, _at(denom, here, "denom", _i64t), _at(logp_out, here, "logp_out", _f32, n),

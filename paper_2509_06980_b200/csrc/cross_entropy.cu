@@ -10,6 +10,9 @@
 // Kernels, in launch order: ce_plan_kernel (work list: the rows that carry loss, then the others; their
 // count), the row kernel (writes logp, lse, the row's loss terms and grad_logits), ce_loss_kernel (fp64 sums in
 // a fixed order).  Rows without loss weight are not read at all; their gradient is written as zeros.
+// Without a gradient many long rows take ce_stream_kernel and ce_stream_join_kernel in place of the row kernel.
+#include <type_traits>
+
 #include "common.cuh"
 #include "row.cuh"
 
@@ -18,7 +21,7 @@ namespace ce {
 
 // workspace: [0] int64 number of rows with mask != 0; [64] int number of live rows; [256 ..) one float4 of loss terms
 // per token, {lse - z_y, lse - mean z (0 without smoothing), lse, 1 if the row counts}; then the work list, one
-// int2 per token: {row, target id} of the live rows in order, then {row, -1} of the others
+// int2 per token: {row, target id} of the live rows in order, then {row, -1} of the others; then the streaming form's parts
 constexpr size_t kWsTermsOff = 256;
 constexpr size_t ws_list_off(int64_t T) { return kWsTermsOff + 16 * (size_t)(T > 0 ? T : 0); }
 
@@ -546,6 +549,186 @@ ce_row_cluster_kernel(const ClusterParams cp) {
     cluster_sync_all();                  // no CTA leaves while a peer could still address its shared memory
 }
 
+// ---------------------------------------------------------------------------------------------
+// Forward only, long rows: without a gradient nobody has to hold a row.  A work unit is one chunk of a live row (up to
+// 256 x NV vectors); every warp leaves its (max, sum, share of the mean) of a unit and a second kernel joins a row's.  No
+// exchange and no barrier: a thread reads only the staging slots that it filled itself, so that the warps of a CTA drift
+// and loads and exponentials overlap.  Bound by HBM.  EDGE as in the cluster kernel.
+constexpr int kStreamThreads = 256, kStreamWarps = kStreamThreads / 32, kStreamNV = 8, kStreamCtasPerSm = 4;
+constexpr int kStreamUnits = 8;              // units per CTA: it then retires, as the cluster kernel's CTAs do
+
+struct StreamParams {
+    RowParams r;
+    int chunks, per_chunk_vec;               // of a row; vectors of a chunk (the last may hold fewer)
+    float inv_v;
+    float4* part;                            // [live row][chunks][kStreamWarps]: max, sum 2^((z - max) log2 e), sum z / V, -
+};
+// chunks of a row that covers nvec vectors
+static int stream_chunks(int64_t nvec) { return (int)((nvec + kStreamThreads * kStreamNV - 1) / (kStreamThreads * kStreamNV)); }
+
+template <typename T, bool EDGE>
+__global__ void __launch_bounds__(kStreamThreads, kStreamCtasPerSm)
+ce_stream_kernel(const StreamParams sp) {
+    const RowParams& p = sp.r;
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int VE = Elem<T>::kPer, THREADS = kStreamThreads, NV = kStreamNV;
+    extern __shared__ __align__(16) uint4 stage[];            // [NV][THREADS], slot (i, tid) private to thread tid
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool smooth = p.eps > 0.0f;
+    // the elements of a vector, two at a time
+    auto for_pairs = [](const uint4& v, auto f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        if constexpr (BF) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f(f2_make(bf_lo(w[j]), bf_hi(w[j])));
+        } else {
+            f(f2_make(__uint_as_float(w[0]), __uint_as_float(w[1])));
+            f(f2_make(__uint_as_float(w[2]), __uint_as_float(w[3])));
+        }
+    };
+    struct Unit { int head, nvec, vbeg, nvalid; };
+    auto unit = [&](long long u, int row) -> Unit {
+        Unit q;
+        q.head = EDGE ? (int)((reinterpret_cast<uintptr_t>(p.logits) / sizeof(T) + (unsigned long long)((long long)row * p.stride)) % VE) : 0;
+        q.nvec = EDGE ? (q.head + p.V + VE - 1) / VE : p.V / VE;
+        const int chunk = (int)(u % sp.chunks);
+        q.vbeg = chunk * sp.per_chunk_vec + tid;
+        const int vend = min(q.nvec, (chunk + 1) * sp.per_chunk_vec);
+        q.nvalid = vend > q.vbeg ? (vend - q.vbeg + THREADS - 1) / THREADS : 0;
+        return q;
+    };
+    pdl_wait();
+    pdl_trigger();
+    const long long units = (long long)*p.n_live * sp.chunks, step = gridDim.x;
+    auto row_of = [&](long long u) -> int { return u < units ? p.list[u / sp.chunks].x : 0; };
+    auto prefetch = [&](long long u, int row) {
+        if (u < units) {
+            const Unit q = unit(u, row);
+            const T* row0 = static_cast<const T*>(p.logits) + (long long)row * p.stride - q.head;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < q.nvalid) {
+                    const int v = q.vbeg + i * THREADS;
+                    const uint4* src = reinterpret_cast<const uint4*>(row0) + v;
+                    uint4* dst = stage + i * THREADS + tid;
+                    if (EDGE && v == 0 && q.head != 0 && row == 0) {
+                        T* e = reinterpret_cast<T*>(dst);
+                        for (int j = q.head; j < VE && j < q.head + p.V; ++j) e[j] = row0[j];
+                    } else if (EDGE && v == q.nvec - 1) {
+                        cp_async16_part(dst, src, (q.head + p.V - v * VE) * (int)sizeof(T));
+                    } else {
+                        cp_async16_cg(dst, src);
+                    }
+                }
+        }
+        cp_async_commit();
+    };
+    long long u = blockIdx.x;
+    int row = row_of(u), row_next = row_of(u + step);          // (entries of the list are fetched a unit ahead of their data)
+    prefetch(u, row);
+    for (; u < units; u += step) {
+        const Unit q = unit(u, row);
+        cp_async_wait_all();
+        float mean = 0.0f;
+        if (EDGE) {
+            // what lies in the first and the last vector beside the row is not part of it
+            if (q.vbeg == 0 && q.nvalid > 0) keep_elements<T>(&stage[tid], q.head, VE);
+            const int lrel = q.nvec - 1 - q.vbeg;
+            if (lrel >= 0 && lrel % THREADS == 0 && lrel / THREADS < q.nvalid)
+                keep_elements<T>(&stage[lrel + tid], 0, q.head + p.V - (q.nvec - 1) * VE);
+        }
+        const uint32_t ninf = Elem<T>::neg_inf();
+        uint4 d[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (i < q.nvalid) d[i] = stage[i * THREADS + tid];
+            else d[i] = make_uint4(ninf, ninf, ninf, ninf);
+        }
+        if (smooth) {
+            const f2 inv2 = f2_make(sp.inv_v, sp.inv_v);
+            f2 mean2 = 0ull;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = q.vbeg + i * THREADS;
+                if (i >= q.nvalid) continue;
+                if (EDGE && (v == 0 || v == q.nvec - 1)) {
+                    const T* e = reinterpret_cast<const T*>(&stage[i * THREADS + tid]);
+                    for (int j = 0; j < VE; ++j)
+                        if (v * VE + j >= q.head && v * VE + j < q.head + p.V) mean = fmaf(to_f<T>(e[j]), sp.inv_v, mean);
+                    continue;
+                }
+                for_pairs(d[i], [&](f2 z) { mean2 = f2_fma(z, inv2, mean2); });
+            }
+            mean = warp_sum(mean + f2_sum(mean2));
+        }
+        prefetch(u + step, row_next);                          // the slots are in registers
+        row = row_next;
+        row_next = row_of(u + 2 * step);
+        float m;
+        if (BF) {
+            uint32_t mx = ninf;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) mx = max_bf16x2(mx, max_bf16x2(max_bf16x2(d[i].x, d[i].y), max_bf16x2(d[i].z, d[i].w)));
+            m = fmaxf(bf_lo(mx), bf_hi(mx));
+        } else {
+            m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(d[i].x), __uint_as_float(d[i].y)),
+                                   fmaxf(__uint_as_float(d[i].z), __uint_as_float(d[i].w))));
+        }
+        m = ord2f(__reduce_max_sync(0xffffffffu, f2ord(m)));
+        const float ms = (m == -INFINITY) ? 0.0f : m;
+        const bool fold = BF && fabsf(ms) <= kRobustAbove;     // as in the cluster kernel
+        const f2 off2 = f2_make(-ms * kLog2e, -ms * kLog2e), ms2 = f2_make(-ms, -ms), c2 = f2_make(kLog2e, kLog2e);
+        f2 sum2 = 0ull;
+        auto add = [&](auto folded) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                for_pairs(d[i], [&](f2 z) {
+                    float a, b;
+                    f2_split(decltype(folded)::value ? f2_fma(z, c2, off2) : f2_mul(f2_add(z, ms2), c2), a, b);
+                    sum2 = f2_add(sum2, f2_make(ex2_approx(a), ex2_approx(b)));
+                });
+        };
+        if (fold) add(std::true_type{});
+        else add(std::false_type{});
+        const float s = warp_sum(f2_sum(sum2));
+        if (lane == 0) sp.part[u * kStreamWarps + warp] = make_float4(m, s, mean, 0.0f);
+    }
+    cp_async_wait_all();
+}
+
+// one warp per entry of the work list: a live row's parts are joined, any other row gets its NaNs
+template <typename T>
+__global__ void __launch_bounds__(256)
+ce_stream_join_kernel(const StreamParams sp) {
+    const RowParams& p = sp.r;
+    const int lane = threadIdx.x & 31, per_row = sp.chunks * kStreamWarps;
+    const long long k = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    pdl_wait();
+    pdl_trigger();
+    if (k >= p.T) return;
+    const int2 job = p.list[k];
+    RowStats r = {};
+    if (k < *p.n_live) {
+        const float4* part = sp.part + k * per_row;
+        const float zy = to_f<T>(static_cast<const T*>(p.logits)[(long long)job.x * p.stride + job.y]);
+        float M = -INFINITY, S = 0.0f, Q = 0.0f;
+        for (int c = lane; c < per_row; c += 32) M = fmaxf(M, part[c].x);
+        M = ord2f(__reduce_max_sync(0xffffffffu, f2ord(M)));
+        for (int c = lane; c < per_row; c += 32) {
+            const float4 e = part[c];
+            // (a part of -inf logits has the sum 0, or NaN where it held a NaN)
+            S += e.x == -INFINITY ? e.y : e.y * ex2_approx((e.x - M) * kLog2e);
+            Q += e.z;
+        }
+        r = row_stats(M, warp_sum(S), zy, warp_sum(Q), p.eps);
+        if (lane == 0 && !r.ok && p.dev_status) atomicOr(p.dev_status, RLF_DEV_NONFINITE);
+    }
+    if (lane == 0) write_row(p, job.x, r);
+}
+
 // ---- launch shape ---------------------------------------------------------------------------
 typedef void (*RowKernel)(const ClusterParams);
 struct RowShape { int cluster, threads, nv; };
@@ -843,22 +1026,71 @@ static rlf_status launch_cluster(void (*k)(Args...), int ctas, int threads, bool
     count_launch();
     return RLF_OK;
 }
+// a launch whose kernel waits by itself for the kernel before it
+template <typename P>
+static rlf_status launch_after(void (*k)(const P), long long grid, int threads, int smem, cudaStream_t s, const P& p) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, k, p) != cudaSuccess) {
+        cudaGetLastError();
+        return RLF_ERR_CUDA;
+    }
+    count_launch();
+    return RLF_OK;
+}
 static int small_ctas(int64_t T, int64_t per_cta) {
     const int64_t n = (T + per_cta - 1) / per_cta;
     return (int)(n < 1 ? 1 : n < kMaxPlanCtas ? n : kMaxPlanCtas);
 }
 
+// vectors of 16 bytes that a row may take: one more than its length fills when it lies on no boundary
+static int64_t row_vectors(int32_t V, int ve, bool edge) { return edge ? ((int64_t)V + 2 * ve - 2) / ve : V / ve; }
+// Forward only, the streaming form against the cluster kernel (which a row of up to 2560 vectors needs one CTA of): 8192 rows
+// of 151936 bf16 426 us (5.8 TB/s) against 527, 4096 of fp32 365 (6.8 TB/s) against 495, 8192 of 24000 bf16 104 either way;
+// 512 rows of 151936 bf16 48 us against 50, 8 rows 28 against 26 (one launch more).
+static bool streams(int64_t T, int64_t nvec) { return nvec > 2560 && T >= 512; }
+static size_t ws_part_off(int64_t T) { return (ws_list_off(T) + 8 * (size_t)(T > 0 ? T : 0) + 15) & ~(size_t)15; }
+static size_t part_bytes(int64_t T, int32_t V, rlf_dtype dt) {
+    const int64_t nvec = row_vectors(V, dt == RLF_BF16 ? 8 : 4, true);
+    return streams(T, nvec) ? 16 * (size_t)T * stream_chunks(nvec) * kStreamWarps : 0;
+}
+
 // The cluster kernel wherever a shape holds the row and the gradient rows sit like the logits rows within their
 // 16-byte vectors; otherwise (rows beyond 81,920 vectors, a gradient buffer of another alignment) the general one,
 // which reads a row three times (V = 151936 bf16, 8192 rows: 3.69 ms against 0.79).
-static rlf_status launch_rows(const RowParams& p, rlf_dtype dt, cudaStream_t s) {
+// Forward only, rows beyond one CTA: the streaming form (parts: the workspace's room for its partials).
+static rlf_status launch_rows(const RowParams& p, rlf_dtype dt, float4* parts, cudaStream_t s) {
     const size_t esz = dt == RLF_BF16 ? 2 : 4;
     const int ve = (int)(16 / esz);
     const bool edge = p.V % ve != 0 || p.stride % ve != 0 || !aligned(p.logits, 16);
     const bool same = !p.grad || (reinterpret_cast<uintptr_t>(p.grad) - reinterpret_cast<uintptr_t>(p.logits)) % 16 == 0;
-    // a row on no boundary may take one vector more than its length fills
-    const long long nvec = edge ? ((long long)p.V + 2 * ve - 2) / ve : p.V / ve;
+    const int64_t nvec = row_vectors(p.V, ve, edge);
     RowShape sh;
+    if (!p.grad && streams(p.T, nvec)) {
+        StreamParams sp;
+        sp.r = p;
+        sp.chunks = stream_chunks(nvec);
+        sp.per_chunk_vec = (int)((nvec + sp.chunks - 1) / sp.chunks);
+        sp.inv_v = 1.0f / (float)p.V;
+        sp.part = parts;
+        const long long units = (long long)p.T * sp.chunks, resident = 148ll * kStreamCtasPerSm;
+        long long grid = (units + kStreamUnits - 1) / kStreamUnits;
+        if (grid < resident) grid = resident < units ? resident : units;
+        if (grid > (1 << 30)) grid = 1 << 30;
+        void (*k)(const StreamParams) = dt == RLF_BF16 ? (edge ? ce_stream_kernel<__nv_bfloat16, true> : ce_stream_kernel<__nv_bfloat16, false>)
+                                                       : (edge ? ce_stream_kernel<float, true> : ce_stream_kernel<float, false>);
+        const rlf_status st = launch_after(k, grid, kStreamThreads, kStreamNV * kStreamThreads * 16, s, sp);
+        if (st != RLF_OK) return st;
+        return launch_after(dt == RLF_BF16 ? ce_stream_join_kernel<__nv_bfloat16> : ce_stream_join_kernel<float>, (p.T + 7) / 8, 256, 0, s, sp);
+    }
     if (same && nvec < (1 << 24) && pick_shape((int)nvec, edge, &sh)) {
         const RowKernel k = dt == RLF_BF16 ? (edge ? row_kernel<__nv_bfloat16, true>(sh) : row_kernel<__nv_bfloat16, false>(sh))
                                            : (edge ? row_kernel<float, true>(sh) : row_kernel<float, false>(sh));
@@ -909,7 +1141,9 @@ rlf_status ce_check_objective(float label_smoothing, float z_coef) {
     if (!(z_coef >= 0.0f && z_coef < INFINITY)) return RLF_ERR_UNSUPPORTED;
     return RLF_OK;
 }
-size_t cross_entropy_workspace_bytes(int64_t T) { return ce::ws_list_off(T) + 8 * (size_t)(T > 0 ? T : 0); }
+size_t cross_entropy_workspace_bytes(int64_t T, int32_t V, rlf_dtype dt) {
+    return V < 1 ? 0 : ce::ws_part_off(T) + ce::part_bytes(T, V, dt);
+}
 
 }  // namespace rlf
 
@@ -931,7 +1165,7 @@ extern "C" rlf_status rlf_cross_entropy_fwd_bwd(const void* logits, rlf_dtype dt
     if (!aligned(logits, esz) || !aligned(grad_logits, esz) || !aligned(ids, 4) || !aligned(logp_out, 4) ||
         !aligned(lse_out, 4) || !aligned(loss_out, 8) || !aligned(denom, 8))
         return RLF_ERR_ALIGN;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < cross_entropy_workspace_bytes(T)) return RLF_ERR_WORKSPACE;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < cross_entropy_workspace_bytes(T, V, dt)) return RLF_ERR_WORKSPACE;
     st = check_arch();
     if (st != RLF_OK) return st;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
@@ -947,7 +1181,7 @@ extern "C" rlf_status rlf_cross_entropy_fwd_bwd(const void* logits, rlf_dtype dt
     p.denom = dn; p.logp_out = logp_out; p.lse_out = lse_out; p.terms = reinterpret_cast<float4*>(ws + kWsTermsOff);
     p.dev_status = dev_status; p.eps = label_smoothing; p.zeta = z_coef;
     if (T > 0) {
-        st = launch_rows(p, dt, s);
+        st = launch_rows(p, dt, reinterpret_cast<float4*>(ws + ws_part_off(T)), s);
         if (st != RLF_OK) return st;
     }
     return ce_launch_loss(p.terms, T, dn, label_smoothing, z_coef, loss_out, s);

@@ -172,6 +172,79 @@ def test_infinities_lowest_values_and_nan(dt, V):
     check(run(z, ids, mask), z, ids, mask)
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+def _check_live(out, z, ids, mask, eps=0.0, zc=0.0):
+    """check() of a forward-only call, of the rows with a mask and a few others."""
+    sel = mask != 0
+    sel[::97] = True
+    sub = tuple(None if t is None else t[sel] for t in out[:2])
+    return check(sub + (out[2], None), z[sel], ids[sel], mask[sel], eps, zc)
+
+
+@pytest.mark.parametrize("T,V", [(511, 20488), (512, 10241), (700, 10248), (600, 20480), (512, 20481), (513, 20487), (530, 32003),
+                                 (512, 50304), (520, 151936), (3, 700001)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_forward_only_of_long_rows(T, V, dt):
+    """Without a gradient a long row is cut into chunks that nobody joins before the second kernel."""
+    b = gc.binding()
+    for k, (pad, offset) in enumerate([(0, 0), (8, 0), (3, 1)]):
+        z, ids, mask, buf = _rows(T, V, dt, 3 * T + V + k, pad, offset)
+        mask[torch.arange(T, device=DEV) % 29 != 2] = 0
+        mask[2 % T] = mask[T - 1] = 1
+        keep = buf.clone()
+        for eps, zc in ((0.0, 0.0), (0.1, 1e-3)):
+            out = run(z, ids, mask, eps, zc, want_grad=False)
+            _check_live(out, z, ids, mask, eps, zc)
+        every = run(z, ids, None, 0.1, 1e-3, want_grad=False)
+        assert torch.equal(every[0][mask != 0], out[0][mask != 0]) and torch.isfinite(every[0]).all()
+        assert torch.isnan(run(z, ids, torch.zeros_like(mask), want_grad=False)[0]).all()
+        assert torch.equal(buf, keep)
+    if T < 100:
+        return
+    # rows that hold infinities, the lowest value, a NaN
+    low = torch.finfo(dt).min
+    mask[:8] = 1
+    z[0, : V - 3] = float("-inf")
+    ids[0] = V - 1
+    z[1, 1:] = low
+    ids[1] = 0
+    z[2] = -1e30
+    _check_live(run(z, ids, mask, want_grad=False), z, ids, mask)
+    z[3, V // 3] = float("nan")
+    z[4] = float("-inf")
+    z[4, 7] = float("nan")
+    z[5, V - 1] = float("inf")
+    for eps in (0.0, 0.1):
+        _check_live(run(z, ids, mask, eps, status=b.DEV_NONFINITE, want_grad=False), z, ids, mask, eps)
+    ids[6] = V
+    _check_live(run(z, ids, mask, status=b.DEV_NONFINITE | b.DEV_BAD_TARGET, want_grad=False), z, ids, mask)
+    mask[3:7] = 0
+    _check_live(run(z, ids, mask, want_grad=False), z, ids, mask)
+
+
+def test_forward_only_captured_and_replayed():
+    z, ids, mask, _ = _rows(600, 32003, BF, 17)
+    eager = run(z, ids, mask, 0.1, want_grad=False)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b = gc.binding()
+    with torch.cuda.stream(s):
+        b.rlf_cross_entropy_fwd_bwd(z, ids, mask, label_smoothing=0.1, want_grad=False)
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = b.rlf_cross_entropy_fwd_bwd(z, ids, mask, label_smoothing=0.1, want_grad=False)
+    mask0 = mask.clone()
+    mask.copy_(1 - mask0)
+    g.replay()
+    flipped = [t.clone() for t in out[:3]]
+    want = run(z, ids, mask, 0.1, want_grad=False)
+    assert all(torch.equal(p.nan_to_num(9.0), q.nan_to_num(9.0)) for p, q in zip(flipped, want))
+    mask.copy_(mask0)
+    g.replay()
+    assert all(torch.equal(p.nan_to_num(9.0), q.nan_to_num(9.0)) for p, q in zip(out[:3], eager))
+
+
 def test_targets_out_of_range_and_ignored_ids():
     b = gc.binding()
     z, ids, mask, _ = _rows(20, 1000, BF, 5)
