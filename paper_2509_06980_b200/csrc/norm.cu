@@ -889,10 +889,14 @@ struct Cut { Form form; int nv, threads, rows, smem; };
 // memory when staged).  `arrays` rows are read per row; the staged form keeps `vectors` fp32 vectors of the width.
 //   Forward: CTAs of up to 256 threads, two rows at a time.  32768 x 2560 bf16, no residual: 58.7 us with 256 threads and two
 //   rows, 63.7 with one row, 66 with 512 threads; with the residual 106 - 108 us whichever.
+//   Rows of up to 256 vectors without a residual, or off their vectors: 128 threads (32768 rows, 256 threads -> 128: 2048 bf16
+//   68 -> 62 us layer, 52 -> 48 RMS; 1024 fp32 layer 57 -> 50; 1531 bf16 with residual 132 -> 96); with one they cost 1 - 4 %.
 //   Backward: bf16 rows without the second sum (RMS form, no bias) four vectors per thread, one row at a time: 32768 x 2560
 //   bf16 110 us against 117 - 122 with one or two vectors; else up to 512 threads of two vectors, two rows at a time:
-//   8191 x 4096 bf16 layer form 49 us against 54 with four vectors, 32768 x 2560 fp32 162 against 190.
-static bool pick_cut(bool bf16, Form form, bool fwd, bool full, long long T, int D, int arrays, int vectors, Cut* c) {
+//   8191 x 4096 bf16 layer form 49 us against 54 with four vectors, 32768 x 2560 fp32 162 against 190.  The layer form takes
+//   two vectors per thread at shorter rows too (32768 rows, one vector -> two: 2048 bf16 99 -> 81 us, 1024 bf16
+//   54 -> 47, 1024 fp32 81 -> 71); rows of up to 64 vectors keep one, four rows at a time.
+static bool pick_cut(bool bf16, Form form, bool fwd, bool layer, bool full, long long T, int D, int arrays, int vectors, Cut* c) {
     const int esz = bf16 ? 2 : 4;
     if (D > kSmemLimit / esz) return false;            // (before any product of D)
     const int v = 16 / esz, nvec = form == kEdge ? (D + 2 * v - 2) / v : D / v;
@@ -900,7 +904,8 @@ static bool pick_cut(bool bf16, Form form, bool fwd, bool full, long long T, int
     c->form = form;
     c->nv = 1;
     if (wide) {
-        const int most = fwd ? 256 : (bf16 && !full && nvec <= 512) ? 128 : bf16 ? 256 : 512;
+        int most = fwd ? (nvec <= 256 && (arrays == 1 || form == kEdge) ? 128 : 256) : (bf16 && !full && nvec <= 512) ? 128 : bf16 ? 256 : 512;
+        if (!fwd && layer && nvec > 64 && nvec <= 2 * most) most = nvec <= 128 ? 64 : (nvec + 63) / 64 * 32;
         while ((nvec + c->nv - 1) / c->nv > most && c->nv < 4) c->nv *= 2;
         c->threads = ((nvec + c->nv - 1) / c->nv + 31) / 32 * 32;
         if (c->threads > kMaxThreads) return false;
@@ -1058,7 +1063,7 @@ extern "C" rlf_status rlf_norm_fwd(const void* x, const void* residual, rlf_dtyp
     const void* const at[] = {x, residual, sum_out, y_out};
     const Form form = row_form(bf16, T, D, at, 4, x_stride, x_stride, &p.period);
     Cut c;
-    auto cut = [&](Form f) { return pick_cut(bf16, f, true, p.layer, T, D, residual ? 2 : 1, bias ? 2 : 1, &c); };
+    auto cut = [&](Form f) { return pick_cut(bf16, f, true, p.layer, p.layer, T, D, residual ? 2 : 1, bias ? 2 : 1, &c); };
     if (cut(form) || (form == kEdge && cut(kStaged))) {
         const FwdKernel k = p.layer ? fwd_kernel<true>(bf16, c) : fwd_kernel<false>(bf16, c);
         const int resident = k ? resident_ctas((const void*)k, c) : 0;
@@ -1114,7 +1119,7 @@ extern "C" rlf_status rlf_norm_bwd(const void* grad_y, int64_t grad_y_stride, co
         Cut c;
         BwdKernel k = nullptr;
         long long resident = 0;
-        auto cut = [&](Form f) { return pick_cut(bf16, f, false, full, T, D, grad_skip ? 3 : 2, grad_bias ? 3 : 2, &c); };
+        auto cut = [&](Form f) { return pick_cut(bf16, f, false, layer, full, T, D, grad_skip ? 3 : 2, grad_bias ? 3 : 2, &c); };
         if (cut(form) || (form == kEdge && cut(kStaged))) {
             k = full ? bwd_kernel<true>(bf16, c) : bwd_kernel<false>(bf16, c);
             resident = k ? resident_ctas((const void*)k, c) : 0;
