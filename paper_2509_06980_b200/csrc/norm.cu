@@ -891,6 +891,8 @@ struct Cut { Form form; int nv, threads, rows, smem; };
 //   rows, 63.7 with one row, 66 with 512 threads; with the residual 106 - 108 us whichever.
 //   Rows of up to 256 vectors without a residual, or off their vectors: 128 threads (32768 rows, 256 threads -> 128: 2048 bf16
 //   68 -> 62 us layer, 52 -> 48 RMS; 1024 fp32 layer 57 -> 50; 1531 bf16 with residual 132 -> 96); with one they cost 1 - 4 %.
+//   bf16 rows of more than 512 vectors, layer form, either direction: up to 512 threads, one row at a time (16384 x 8192: 140 ->
+//   130 us forward, 175 -> 167 backward; 16384 x 5120 with residual 125 -> 116, 139 -> 115).
 //   Backward: bf16 rows without the second sum (RMS form, no bias) four vectors per thread, one row at a time: 32768 x 2560
 //   bf16 110 us against 117 - 122 with one or two vectors; else up to 512 threads of two vectors, two rows at a time:
 //   8191 x 4096 bf16 layer form 49 us against 54 with four vectors, 32768 x 2560 fp32 162 against 190.  The layer form takes
@@ -906,10 +908,12 @@ static bool pick_cut(bool bf16, Form form, bool fwd, bool layer, bool full, long
     if (wide) {
         int most = fwd ? (nvec <= 256 && (arrays == 1 || form == kEdge) ? 128 : 256) : (bf16 && !full && nvec <= 512) ? 128 : bf16 ? 256 : 512;
         if (!fwd && layer && nvec > 64 && nvec <= 2 * most) most = nvec <= 128 ? 64 : (nvec + 63) / 64 * 32;
+        const bool long_layer = bf16 && layer && nvec > 512;
+        if (long_layer) most = 512;
         while ((nvec + c->nv - 1) / c->nv > most && c->nv < 4) c->nv *= 2;
         c->threads = ((nvec + c->nv - 1) / c->nv + 31) / 32 * 32;
         if (c->threads > kMaxThreads) return false;
-        c->rows = c->nv == 4 ? 1 : (!fwd && nvec <= 64) ? 4 : 2;
+        c->rows = c->nv == 4 || long_layer ? 1 : (!fwd && nvec <= 64) ? 4 : 2;
     } else {
         c->threads = D <= 512 ? 128 : 256;
         c->rows = 2;
