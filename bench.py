@@ -44,9 +44,9 @@ WORKLOAD = "cfg1_qwen3_4b_microbatch: 16 responses x 2048 tokens, V=151936 bf16 
 #   streaming forward kernel: the T = 4096 capture, per token (traffic is proportional to rows);
 #   fused LM-head: every kernel of one forward / one forward + backward call at cfg 3 full size
 #   (one-pass capture of the whole call), per call.
-NCU_TRAFFIC = {"logits_loss_cu_sha1": "ee482c3f18de39e50fed56d917e964b8673b1d59", "dram_bytes_per_token": 606028.0}
-NCU_TRAFFIC_FUSED = {"lmhead_cu_sha1": "23538aaabeed8d9a0c763b7f7e3bb6ee625b306d",
-                     "fwd_bytes_per_call": 3957591808.0, "fwd_bwd_bytes_per_call": 34875904256.0}
+NCU_TRAFFIC = {"logits_loss_cu_sha1": "fcb111935e9c644afd2910dc4607cb7d124136e3", "dram_bytes_per_token": 606039.0}
+NCU_TRAFFIC_FUSED = {"lmhead_cu_sha1": "9d7f117d29a6b76721e95748be8d98d7d4d21ae5",
+                     "fwd_bytes_per_call": 3841895680.0, "fwd_bwd_bytes_per_call": 32138049024.0}
 
 
 def _peaks():
