@@ -409,6 +409,7 @@ rlf_status rlf_fused_lmhead_logp_entropy(const void *hidden, const void *W, int6
  * (with smoothing) mean logit is not finite (RLF_DEV_NONFINITE); those still count in N.
  * Logits of -inf are zero probability; with smoothing they make the mean logit, and so the row, non-finite.
  * Sums are fp32 within a row and fp64 in a fixed order over the rows (results are run-to-run identical).
+ * A call without a gradient may add a row up in another order than one with it (differences of fp32 rounding).
  *
  *   logits       [T, V] dt, row r starts at element r * row_stride (row_stride >= V); any V, stride and
  *                element-aligned base

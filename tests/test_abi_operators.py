@@ -98,6 +98,8 @@ def test_workspace_sizes_grow_with_the_problem(lib):
     f.argtypes = [ci, i64, i32, i32, ci]
     assert f(7, 0, 0, 64, 0) > 0 and f(7, 4096, 0, 64, 0) >= f(7, 64, 0, 64, 0) and f(7, 5, 0, 0, 0) == 0
     assert f(8, 0, 100, 0, 0) >= 256 and f(8, 1000, 100, 0, 0) >= 256 + 16000
+    # the partial sums of long rows that a forward-only call streams; more of them for fp32 rows
+    assert f(8, 1000, 151936, 0, 1) > f(8, 1000, 151936, 0, 0) > f(8, 1000, 100, 0, 0) and f(8, 1000, 0, 0, 0) == 0
     assert f(9, 100, 0, 64, 0) == 0
     # the scratch of a chunk, and an fp32 sum beside a bf16 gradient of more than one chunk
     assert f(9, 8192, 151936, 4096, 1) >= 2 * 8192 * 151936 and f(9, 18944, 512, 64, 0) == f(9, 18944, 512, 64, 1)
