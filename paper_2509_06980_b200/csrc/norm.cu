@@ -393,8 +393,11 @@ __device__ __forceinline__ void load_w(const void* w, int w_bf16, int D, int lea
 }
 
 // Forward.  The rows' elements (x + residual) are held unpacked in registers through the passes.
+// fp32 rows, two vectors and two rows per thread: asking for three CTAs of 256 threads per SM keeps the compiler at 68 registers
+// (32768 x 1024 layer form 49.7 -> 45.7 us, 4999 x 1021 19.1 -> 17.6); the bf16 form would spill (124 -> 136 us at 32768 x 4096).
+// 0 asks for nothing; even 1 changes the bf16 code for the worse (32768 x 2560 RMS 58 -> 66 us).
 template <typename T, int NV, int R, bool LAYER, bool EDGE>
-__global__ void __launch_bounds__(kMaxThreads)
+__global__ void __launch_bounds__(sizeof(T) == 4 && R == 2 ? 256 : kMaxThreads, sizeof(T) == 4 && R == 2 && NV == 2 ? 3 : 0)
 norm_fwd_wide_kernel(const FwdParams p) {
     using V = Vec<T>;
     constexpr int P = V::P, N = V::N;
