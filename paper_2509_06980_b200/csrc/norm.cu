@@ -206,10 +206,11 @@ norm_dw_reduce_kernel(const float* __restrict__ part, const float* __restrict__ 
 //           the row's place in its vectors repeats after 2, 4 or 8 rows, so a CTA takes every 2nd, 4th or 8th row and its
 //           threads keep fixed columns all the same; only a row's first and last vector are masked and stored by element.  Forward
 //           (backward) of 20000 x 2603 bf16, layer form with residual: 114 us (125), the staged form 151 (198); 4999 x 1021
-//           fp32: 21 (23), staged 23 (29);
+//           fp32: 17 (23), staged 23 (29);
 //   staged  any width, stride and base: a row is copied as the aligned 16-byte chunks that cover it, by whichever thread, and a
 //           thread owns every blockDim-th column; weights and weight gradients live in shared memory.
 constexpr int kMaxThreads = 512;
+constexpr int kShortRow = 96;                    // vectors of a row that the backward takes four rows at a time, a thread each
 constexpr int kSmemLimit = 200 * 1024;           // most dynamic shared memory that a fast form asks for
 
 __device__ __forceinline__ void cp_async16(uint32_t smem_dst, const void* src) {
@@ -513,8 +514,10 @@ norm_fwd_wide_kernel(const FwdParams p) {
 
 // Backward: a CTA owns the row.  One sum per row, mean(g xh), and with FULL (layer form, or a bias gradient asked for) also
 // mean(g) and the bias gradient; a CTA's weight gradients are added up row after row and leave as one partial row per CTA.
+// Short rows (four at a time) are compiled for CTAs of up to kShortRow threads, six or more per SM: left at 512 threads the
+// compiler chose 50 - 64 registers and overlapped the four rows less (65536 x 512 bf16 RMS 50 -> 42 us, layer form 54 -> 51).
 template <typename T, int NV, int R, bool FULL, bool EDGE>
-__global__ void __launch_bounds__(kMaxThreads)
+__global__ void __launch_bounds__(R == 4 ? kShortRow : kMaxThreads, R == 4 ? 6 : 0)
 norm_bwd_wide_kernel(const BwdParams p) {
     using V = Vec<T>;
     constexpr int P = V::P, N = V::N, K = FULL ? 2 * R : R;
@@ -900,7 +903,8 @@ struct Cut { Form form; int nv, threads, rows, smem; };
 //   bf16 110 us against 117 - 122 with one or two vectors; else up to 512 threads of two vectors, two rows at a time:
 //   8191 x 4096 bf16 layer form 49 us against 54 with four vectors, 32768 x 2560 fp32 162 against 190.  The layer form takes
 //   two vectors per thread at shorter rows too (32768 rows, one vector -> two: 2048 bf16 99 -> 81 us, 1024 bf16
-//   54 -> 47, 1024 fp32 81 -> 71); rows of up to 64 vectors keep one, four rows at a time.
+//   54 -> 47, 1024 fp32 81 -> 71); rows of up to 96 vectors keep one, four rows at a time (65536 rows,
+//   two rows -> four: 768 bf16 layer form 79 -> 72 us, 384 fp32 72 -> 57; 128 vectors gained nothing more and lost 12 % at 1013 bf16).
 static bool pick_cut(bool bf16, Form form, bool fwd, bool layer, bool full, long long T, int D, int arrays, int vectors, Cut* c) {
     const int esz = bf16 ? 2 : 4;
     if (D > kSmemLimit / esz) return false;            // (before any product of D)
@@ -910,13 +914,13 @@ static bool pick_cut(bool bf16, Form form, bool fwd, bool layer, bool full, long
     c->nv = 1;
     if (wide) {
         int most = fwd ? (nvec <= 256 && (arrays == 1 || form == kEdge) ? 128 : 256) : (bf16 && !full && nvec <= 512) ? 128 : bf16 ? 256 : 512;
-        if (!fwd && layer && nvec > 64 && nvec <= 2 * most) most = nvec <= 128 ? 64 : (nvec + 63) / 64 * 32;
+        if (!fwd && layer && nvec > kShortRow && nvec <= 2 * most) most = nvec <= 128 ? 64 : (nvec + 63) / 64 * 32;
         const bool long_layer = bf16 && layer && nvec > 512;
         if (long_layer) most = 512;
         while ((nvec + c->nv - 1) / c->nv > most && c->nv < 4) c->nv *= 2;
         c->threads = ((nvec + c->nv - 1) / c->nv + 31) / 32 * 32;
         if (c->threads > kMaxThreads) return false;
-        c->rows = c->nv == 4 || long_layer ? 1 : (!fwd && nvec <= 64) ? 4 : 2;
+        c->rows = c->nv == 4 || long_layer ? 1 : (!fwd && nvec <= kShortRow) ? 4 : 2;
     } else {
         c->threads = D <= 512 ? 128 : 256;
         c->rows = 2;
