@@ -533,7 +533,10 @@ ce_row_cluster_kernel(const ClusterParams cp) {
             }
         }
     }
-    // rows without loss weight (or without such a target) are not read, their gradient is zeros
+    // rows without loss weight (or without such a target) are not read, their gradient is zeros.  Among live rows the exchange
+    // keeps a row's edge_slot apart from the next row's; here, where the last vector may be another thread's, the barrier does:
+    // every thread has stored its edges of the last live row before a slot becomes zero.
+    if (EDGE) __syncthreads();
     for (; k < nrows; k += cp.num_clusters) {
         const int row = p.list[k].x;
         if (crank == 0 && tid == 0) write_row(p, row, RowStats{});

@@ -1,0 +1,104 @@
+"""GPU parity of rlf_cross_entropy_fwd_bwd where a cluster of CTAs takes many rows one after the other.
+
+The bounds are those that tests/test_gpu_cross_entropy.py derives, evaluated for all rows at once in 64 bits on the GPU.
+"""
+import pytest
+import torch
+
+import gpu_common as gc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U = 2.0 ** -24
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def rows(T, V, dt, seed, pad=0, offset=0, live=0.5, std=3.0, lift=12.0):
+    """[T, V] logits in a buffer `pad` elements wider that starts `offset` elements in, targets, loss mask, the buffer."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    buf = torch.full((T * (V + pad) + offset + 8,), 5.0, dtype=dt, device=DEV)
+    z = buf[offset:offset + T * (V + pad)].view(T, V + pad)[:, :V]
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    for a in range(0, T, 4096):
+        b = min(T, a + 4096)
+        x = torch.randn(b - a, V, generator=g, device=DEV) * std
+        up = lift * torch.rand(b - a, 1, generator=g, device=DEV) * (torch.arange(b - a, device=DEV)[:, None] % 2)
+        x.scatter_add_(1, ids[a:b].long()[:, None], up)
+        z[a:b] = x.to(dt)
+    mask = (torch.rand(T, generator=g, device=DEV) < live).to(torch.uint8)
+    mask[T // 2] = 1
+    return z, ids, mask, buf
+
+
+def run(z, ids, mask, eps=0.0, zc=0.0, status=0, **kw):
+    b = gc.binding()
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out = b.rlf_cross_entropy_fwd_bwd(z, ids, mask, label_smoothing=eps, z_coef=zc, dev_status=st, **kw)
+    assert st.item() == status, st.item()
+    return out
+
+
+def check(out, z, ids, mask, eps=0.0, zc=0.0):
+    """Every row's log-prob, log-sum-exp and gradient; every row of finite logits is live where mask is set."""
+    logp, lse, loss, grad = out
+    T, V = z.shape
+    live = mask != 0
+    n = max(int(live.sum()), 1)
+    assert torch.equal(torch.isnan(logp), ~live) and (lse is None or torch.equal(torch.isnan(lse), ~live))
+    if grad is not None:
+        assert not grad[~live].any()
+    C = max(64, V // 256 + 13)
+    bf = z.dtype == BF
+    half = 2.0 ** -8 if bf else U
+    at = torch.nonzero(live).flatten()
+    step = max(1, (1 << 26) // V)
+    nll = 0.0
+    tol = 0.0
+    for a in range(0, at.numel(), step):
+        r = at[a:a + step]
+        x = z[r].double()
+        y = ids[r].long()[:, None]
+        M = x.max(dim=1, keepdim=True).values
+        l = torch.logsumexp(x, dim=1, keepdim=True)
+        lp = torch.log_softmax(x, dim=1)
+        p = lp.exp()
+        below = torch.where(p > 0, M - x, torch.zeros_like(x))
+        D = U * (M.abs() + 2 * (p * below).sum(dim=1, keepdim=True) + C + 3 * l.abs() + 8) + 2.0 ** -22
+        want_lp = lp.gather(1, y)
+        err = (logp[r].double()[:, None] - want_lp).abs()
+        lim = D + 3 * U * want_lp.abs()
+        assert (err <= lim).all(), ((err / lim).max().item(), r[(err / lim).argmax()].item())
+        nll += -want_lp.sum().item()
+        tol += (D + 4 * U * want_lp.abs()).sum().item()
+        if lse is not None:
+            assert ((lse[r].double()[:, None] - l).abs() <= D).all()
+        if grad is None:
+            continue
+        A = (1 + 2 * zc * l).abs() / n
+        want = (1 + 2 * zc * l) * p - eps / V
+        others = torch.where(torch.arange(V, device=DEV) == y, torch.zeros_like(p), p).sum(dim=1, keepdim=True)
+        py = p.gather(1, y)
+        want.scatter_(1, y, 2 * zc * l * py - others + eps - eps / V)
+        want /= n
+        rel = D + U * (M.abs() + 2 * below + 12) + 2.0 ** -21 + 2 * zc * D
+        bound = A * p * (rel + (1.01 * 2.0 ** -8 if bf else 0.0)) + 1.01 * half * want.abs() + 8 * U * eps / V / n
+        wy = want.gather(1, y).abs()
+        bound.scatter_(1, y, (others + 2 * zc * l.abs() * py) * (rel.gather(1, y) + D) / n + 1.01 * half * wy
+                       + 8 * U * (eps + 2 * zc * l.abs()) / n)
+        g = grad[r].double()
+        err = (g - want).abs()
+        ok = (err <= bound) | ((want.abs() < 2.0 ** -125) & (g.abs() < 2.0 ** -125))
+        assert ok.all(), (r[torch.nonzero(~ok)[0, 0]].item(), torch.nonzero(~ok)[:4].tolist(), (err / bound)[~ok][:4])
+    assert abs(loss[1].item() - nll / n) <= tol / n + 1e-12 * abs(nll / n)
+
+
+# The last vector of a row lies with thread 31 or 32 (63 or 64 with the longer rows), by where the row starts
+@pytest.mark.parametrize("dt,V", [(BF, 252), (BF, 508), (F32, 126), (F32, 254)])
+def test_edges_of_the_last_live_row_before_a_row_without_loss(dt, V):
+    """Rows whose first and last vectors are stored by element: a cluster's last live row is followed by rows that are
+    zeroed, whose last vector another warp may hold."""
+    z, ids, mask, _ = rows(60000, V, dt, V, pad=1, offset=1)
+    for live in (mask, torch.ones_like(mask)):
+        for _ in range(3):
+            check(run(z, ids, live), z, ids, live)
