@@ -156,8 +156,9 @@ ce_row_general_kernel(const RowParams p) {
 // EDGE serves rows that start on no 16-byte boundary or whose length fills no vector: a row is then the aligned
 // vectors that cover it, with the elements that are not its own set to -inf in the staging slot, and those two
 // vectors' gradients stored element by element.  All loads stay inside the logits' own memory: the last vector
-// is copied up to the row's end, and the first vector of the first row element by element (before it there may
-// be nothing); another row's first vector starts in the row before it.
+// is copied up to the row's end, and a first vector that starts before the logits do element by element (row 0's,
+// and those of the few rows after it that lie in the same vector when rows are shorter than one); any other row's
+// first vector starts in a row before it.
 constexpr int kSmemBudget = 220 * 1024;
 constexpr int stage_bytes(int threads, int nv) { return nv * threads * 16; }
 constexpr int ctas_per_sm(int threads, int nv) {
@@ -278,7 +279,7 @@ ce_row_cluster_kernel(const ClusterParams cp) {
         for (int i = 0; i < NV; ++i) {
             if (i < nvalid) {
                 const int v = vbeg + i * THREADS;
-                if (EDGE && v == 0 && head != 0 && row == 0) {
+                if (EDGE && v == 0 && (long long)row * p.stride < head) {
                     T* d = reinterpret_cast<T*>(dst + i * THREADS);
                     for (int e = head; e < VE && e < head + p.V; ++e) d[e] = row0[e];
                 } else if (EDGE && v == nvec - 1) {
@@ -614,7 +615,7 @@ ce_stream_kernel(const StreamParams sp) {
                     const int v = q.vbeg + i * THREADS;
                     const uint4* src = reinterpret_cast<const uint4*>(row0) + v;
                     uint4* dst = stage + i * THREADS + tid;
-                    if (EDGE && v == 0 && q.head != 0 && row == 0) {
+                    if (EDGE && v == 0 && q.head != 0 && row == 0) {        // (rows are longer than a vector here)
                         T* e = reinterpret_cast<T*>(dst);
                         for (int j = q.head; j < VE && j < q.head + p.V; ++j) e[j] = row0[j];
                     } else if (EDGE && v == q.nvec - 1) {

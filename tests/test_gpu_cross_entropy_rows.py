@@ -102,3 +102,22 @@ def test_edges_of_the_last_live_row_before_a_row_without_loss(dt, V):
     for live in (mask, torch.ones_like(mask)):
         for _ in range(3):
             check(run(z, ids, live), z, ids, live)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_rows_shorter_than_a_vector_on_any_base(dt):
+    """Several rows share the 16-byte vector that the logits start in; what lies before the base (and behind the rows) is
+    neither part of a row nor written."""
+    for V in (1, 2, 3, 7):
+        for pad in (0, 1):
+            for offset in range(0, 8):
+                z, ids, mask, buf = rows(41, V, dt, V + offset, pad, offset)
+                buf[:offset] = float("nan")
+                keep = buf.clone()
+                out = run(z, ids, mask, 0.1)
+                check(out, z, ids, mask, 0.1)
+                assert torch.equal(buf[offset:], keep[offset:])
+                same = run(z, ids, mask, 0.1, in_place=True)
+                assert torch.equal(same[3], out[3])
+                z.fill_(5.0)
+                assert torch.isnan(buf[:offset]).all() and (buf[offset:] == 5.0).all()
