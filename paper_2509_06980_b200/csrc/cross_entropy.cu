@@ -489,7 +489,9 @@ ce_row_cluster_kernel(const ClusterParams cp) {
             float others = 0.0f;
 #pragma unroll
             for (int j = 0; j < (MAXE + 31) / 32; ++j)
-                if (e[j].x != -INFINITY) others += e[j].y * ex2_approx((e[j].x - M) * kLog2e);
+                // (a warp whose logits are all -inf has the sum 0; one whose logits are -inf and NaN has the same maximum and the
+                // sum NaN, which takes the row out)
+                others += e[j].x == -INFINITY ? e[j].y : e[j].y * ex2_approx((e[j].x - M) * kLog2e);
             others = warp_sum(others);
             if (smooth) Q = warp_sum(Q);
             const float S = others + ex2_approx((zy - M) * kLog2e);

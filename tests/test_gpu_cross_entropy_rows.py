@@ -121,3 +121,42 @@ def test_rows_shorter_than_a_vector_on_any_base(dt):
                 assert torch.equal(same[3], out[3])
                 z.fill_(5.0)
                 assert torch.isnan(buf[:offset]).all() and (buf[offset:] == 5.0).all()
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("T", [8, 600])
+def test_nan_that_a_warp_sees_with_no_finite_logit(dt, T):
+    """A NaN whose neighbours in the same warp are -inf, the target, or nothing at all still takes its row out: NaN
+    statistics, a zero gradient, the status; with a gradient or without one, on the cluster and the chunked kernels."""
+    b = gc.binding()
+    nan, inf = float("nan"), float("inf")
+    vec = 8 if dt == BF else 4
+    for V in (32 * vec, 32 * vec + 1, 33 * vec, 1000, 2048 * vec + 8, 2600 * vec + 1):
+        z, ids, mask, _ = rows(T, V, dt, V, live=1.1)
+        ids[:6] = V // 2
+        z[0, V - 1] = nan                       # the last column, perhaps its warp's only one
+        z[1] = nan
+        z[1, V // 2] = 1.0                      # nothing but the target is a number
+        z[2] = -inf
+        z[2, V // 2], z[2, V - 1] = 0.5, nan    # a masked vocabulary with one NaN
+        z[3] = -inf
+        z[3, V // 2], z[3, 0] = 0.5, 0.25       # a masked vocabulary, sound
+        z[4] = nan
+        z[5, :V // 2] = nan
+        dead = torch.tensor([0, 1, 2, 4, 5], device=DEV)
+        sound = torch.ones_like(mask)
+        sound[dead] = 0
+        for eps in (0.0, 0.1):
+            gone = sound.clone()
+            if eps:
+                gone[3] = 0                     # (the mean logit of -inf)
+            for grad in (True, False):
+                lp, lse, loss, g = run(z, ids, mask, eps, status=b.DEV_NONFINITE, want_grad=grad)
+                assert torch.equal(torch.isnan(lp), gone == 0) and torch.equal(torch.isnan(lse), gone == 0), (V, eps, grad)
+                assert torch.isfinite(loss).all()
+                if grad:
+                    assert torch.isfinite(g).all() and not g[gone == 0].any()
+            # the others are what they are without the bad rows (their count apart)
+            n = torch.full((1,), T, dtype=torch.int64, device=DEV)
+            a, c = run(z, ids, mask, eps, status=b.DEV_NONFINITE, denom=n), run(z, ids, gone, eps, denom=n)
+            assert torch.equal(a[0].nan_to_num(7.0), c[0].nan_to_num(7.0)) and torch.equal(a[2], c[2]) and torch.equal(a[3], c[3])
