@@ -680,7 +680,8 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             d4[3] = make_uint4(o[12], o[13], o[14], o[15]);
                         }
                     }
-                    if (tm != -INFINITY) run_s += (ts0 + ts1) * ex2_approx((tm - run_m) * kLog2e);
+                    // (a tile of -inf has the sum 0; one of -inf and NaN has the same maximum and the sum NaN, which must stay)
+                    run_s += tm == -INFINITY ? ts0 + ts1 : (ts0 + ts1) * ex2_approx((tm - run_m) * kLog2e);
                     if (row_ok) p.tmax[(long long)row * p.n_tiles + n] = tms;
                 } else {
                 // 32-column chunks of the accumulator(s), software-pipelined: the tensor-memory load of
@@ -2061,7 +2062,7 @@ ce_combine_rows_kernel(const CeCombine p) {
     float S = 0.0f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (q[j].x != -INFINITY) S += q[j].y * expf(q[j].x - M);
+        S += q[j].x == -INFINITY ? q[j].y : q[j].y * expf(q[j].x - M);      // (0 for a split of -inf, NaN where it held a NaN)
     S = warp_sum(S);
     const float ln_s = logf(S), zy = p.zy_g[g];
     const float lse = M + ln_s, logp = (zy - M) - ln_s;

@@ -1,0 +1,29 @@
+"""rlf_fused_lmhead_cross_entropy on heads with NaN and infinite rows."""
+import pytest
+import torch
+
+import gpu_common as gc
+from test_gpu_fused_cross_entropy import _inputs, check, form, run          # noqa: F401  (form: a fixture)
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("T", [5, 300])
+@pytest.mark.parametrize("V,first,last", [(1032, 1024, 1032), (1032, 256, 512), (1032, 0, 256), (2056, 2048, 2056), (264, 256, 264),
+                                          (20008, 19968, 20008)])
+def test_nan_rows_that_fill_a_column_tile(form, T, V, first, last):
+    """Uninitialised padding rows of the head: a column tile (or a whole split of the vocabulary) holds nothing but NaN.
+    Every row of logits has a NaN, so every row is taken out, whichever gradients are asked for."""
+    b = gc.binding()
+    H, W, ids, mask = _inputs(T, 64, V, 21)
+    W[first:last] = float("nan")
+    ids.clamp_(max=first - 1) if first else ids.clamp_(min=last)
+    for eps in (0.0, 0.1):
+        for want_h, want_w, dt in ((True, True, BF), (True, True, F32), (True, False, F32), (False, False, F32)):
+            lp, lse, loss, gh, gw = run(H, W, ids, mask, eps, status=b.DEV_NONFINITE, want_grad_hidden=want_h,
+                                        want_grad_W=want_w, grad_W_dtype=dt)
+            assert torch.isnan(lp).all() and torch.isnan(lse).all() and not loss.any()
+            assert gh is None or not gh.any()
+            assert gw is None or not gw.any()
