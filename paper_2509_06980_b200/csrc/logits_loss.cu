@@ -182,8 +182,8 @@ __device__ __forceinline__ float2 exp_sum_ent_pass(const uint4 (&d)[NV], float m
         const uint32_t w[4] = {d[i].x, d[i].y, d[i].z, d[i].w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const float x0 = fmaxf(expo<ROBUST>(bf_lo(w[k]), m, off), -1e30f);
-            const float x1 = fmaxf(expo<ROBUST>(bf_hi(w[k]), m, off), -1e30f);
+            const float x0 = max_or_nan(expo<ROBUST>(bf_lo(w[k]), m, off), -1e30f);
+            const float x1 = max_or_nan(expo<ROBUST>(bf_hi(w[k]), m, off), -1e30f);
             const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
             s0 += e0;
             s1 += e1;
@@ -378,8 +378,10 @@ grpo_row_cluster_kernel(const FastParams p) {
         const float s_w = warp_sum(s_t);
         // every warp hands its (max, sum) to every CTA of the cluster, then waits until its own CTA
         // has received the whole row's worth (the only synchronisation in the loop)
+        // (the maximum passes over NaNs and the sum keeps them: a warp that saw one reports an infinite maximum, which takes the
+        // row out whatever else it holds)
         if (lane < csize) {
-            st_async_f2(smem_u32(&pair_slot[parity][crank * NWARPS + warp]), bar, (uint32_t)lane, m_w, s_w);
+            st_async_f2(smem_u32(&pair_slot[parity][crank * NWARPS + warp]), bar, (uint32_t)lane, s_w == s_w ? m_w : INFINITY, s_w);
             if (ENT) st_async_f1(smem_u32(&ent_slot[parity][crank * NWARPS + warp]), bar, (uint32_t)lane, u_w);
         }
         if (!gave_up && !mbar_wait_bounded(bar, (uint32_t)(it >> 1) & 1u)) {
@@ -560,7 +562,7 @@ grpo_row_general_kernel(const GenParams p) {
         // the sums leave the target column out; it comes back in once per row below.  S' = sum over the
         // other columns gives the target's gradient as -c S' / S without the cancellation of c (p_y - 1)
         for (int v = tid; v < p.V; v += kGenThreads) {
-            const float x = fmaxf((to_f32<T>(z[v]) - Ms) * kLog2e, -1e30f);
+            const float x = max_or_nan((to_f32<T>(z[v]) - Ms) * kLog2e, -1e30f);
             const float e = (v == y) ? 0.0f : ex2_approx(x);
             s += e;
             u = fmaf(e, x, u);                 // for the entropy: sum 2^x * x
@@ -578,7 +580,7 @@ grpo_row_general_kernel(const GenParams p) {
         }
         __syncthreads();
         const float S_others = bcast;
-        const float x_y = fmaxf((zy - Ms) * kLog2e, -1e30f);
+        const float x_y = max_or_nan((zy - Ms) * kLog2e, -1e30f);
         const float e_y = ex2_approx(x_y);
         const float S = S_others + e_y;
         const float U = fmaf(e_y, x_y, bcast_u);
@@ -1197,7 +1199,7 @@ __device__ __forceinline__ float2 stream_exp_pass(const uint4 (&d)[NV], float of
         const uint32_t w[4] = {d[i].x, d[i].y, d[i].z, d[i].w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t wc = WANT_U ? max_bf16x2(w[k], kFloorPair) : w[k];
+            const uint32_t wc = WANT_U ? max_bf16x2_or_nan(w[k], kFloorPair) : w[k];
             const uint64_t x2 = fma_f32x2(f32x2(bf_lo(wc), bf_hi(wc)), c2, off2);
             float x0, x1;
             f32x2_split(x2, x0, x1);
@@ -1303,7 +1305,10 @@ logp_entropy_merge_kernel(const float4* __restrict__ partial, int per_row, const
     float S = 0.0f, U = 0.0f;
     for (int c = lane; c < per_row; c += 32) {
         const float4 e = row[c];
-        if (e.x == -INFINITY) continue;
+        if (e.x == -INFINITY) {
+            S += e.y;                            // 0, or NaN where there was one
+            continue;
+        }
         const float dx = (e.x - M) * kLog2e;
         const float f = ex2_approx(dx);
         S += e.y * f;
