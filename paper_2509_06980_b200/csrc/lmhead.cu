@@ -1017,7 +1017,7 @@ __device__ __forceinline__ TokenStats token_stats(const float2* __restrict__ par
     float S = 0.0f;
     for (int j = 0; j < nsplit; ++j) {
         const float2 ms = parts[j];
-        if (ms.x != -INFINITY) S += ms.y * expf(ms.x - M);
+        S += ms.x == -INFINITY ? ms.y : ms.y * expf(ms.x - M);      // (0 for a split of -inf, NaN where it held a NaN)
     }
     TokenStats o;
     o.lse = M + logf(S);
@@ -1087,7 +1087,10 @@ combine_logp_entropy_kernel(const float2* __restrict__ part, const float* __rest
     float S = 0.0f, U = 0.0f;
     for (int j = 0; j < nsplit; ++j) {
         const float2 ms = part[t * nsplit + j];
-        if (ms.x == -INFINITY) continue;
+        if (ms.x == -INFINITY) {
+            S += ms.y;                           // 0, or NaN where there was one
+            continue;
+        }
         const float dx = (ms.x - M) * kLog2e;
         const float f = exp2f(dx);
         S += ms.y * f;

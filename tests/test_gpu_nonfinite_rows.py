@@ -59,3 +59,28 @@ def test_rows_of_logits(T, V, dt):
             logp, ent = b.rlf_logp_entropy_fwd(z, ids, want_entropy=want, dev_status=st)
             assert st.item() == b.DEV_NONFINITE and torch.equal(torch.isnan(logp), gone), (want, logp[:6])
             assert ent is None or torch.isnan(ent[gone]).all()
+
+
+@pytest.mark.parametrize("T", [5, 300])
+@pytest.mark.parametrize("V,first,last", [(1032, 1024, 1032), (1032, 256, 512), (1032, 0, 256), (264, 256, 264), (20008, 19968, 20008)])
+def test_nan_rows_of_a_head(T, V, first, last):
+    b = gc.binding()
+    g, ids, seq, adv, old, mask = _tokens(T, V, 7)
+    H = torch.randn(T, 64, generator=g, device=DEV).to(BF)
+    W = (0.25 * torch.randn(V, 64, generator=g, device=DEV)).to(BF)
+    W[first:last] = float("nan")
+    ids.clamp_(max=first - 1) if first else ids.clamp_(min=last)
+    for agg in (0, 1):
+        for row_reference in (1, 0):
+            st = torch.zeros(1, dtype=torch.int32, device=DEV)
+            b.tune_lmhead_backward(row_reference, 1)
+            try:
+                logp, loss = b.rlf_fused_lmhead_grpo_obj(H, W, ids, seq, adv, old, old, mask, 0.2, 0.2, 0.01, aggregation=agg,
+                                                         dev_status=st)[:2]
+            finally:
+                b.tune_lmhead_backward(1, 1)
+            assert st.item() == b.DEV_NONFINITE and torch.isnan(logp).all() and torch.isfinite(loss).all(), (agg, row_reference)
+    for want in (True, False):
+        st = torch.zeros(1, dtype=torch.int32, device=DEV)
+        logp, ent = b.rlf_fused_lmhead_logp_entropy(H, W, ids, want_entropy=want, dev_status=st)
+        assert st.item() == b.DEV_NONFINITE and torch.isnan(logp).all() and (ent is None or torch.isnan(ent).all()), want
