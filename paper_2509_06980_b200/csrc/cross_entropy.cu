@@ -170,6 +170,12 @@ constexpr int ctas_per_sm(int threads, int nv) {
 // exponents of bf16 rows are formed by one multiply-add from a rounded -max log2 e; rows whose maximum is huge in
 // magnitude subtract first
 constexpr float kRobustAbove = 2048.0f;
+// The rounding of m log2 e is the same for every exponent of a warp and known exactly, r = (m log2 e rounded) - m log2 e: what the
+// multiply-adds give stands for 2^-r times the exponentials, and sums and gradients are put right by 1 + r', r' = r ln 2
+// (|r| <= 2^-13 up to kRobustAbove, so that r'^2 / 2 is below 2^-27).  Without it a log-prob is off by up to 8e-5 at |m| = 2000.
+__device__ __forceinline__ float offset_error(float m) {
+    return fmaf(-m, kLog2e, __fmul_rn(m, kLog2e)) * kLn2;
+}
 
 struct ClusterParams {
     RowParams r;
@@ -436,7 +442,7 @@ ce_row_cluster_kernel(const ClusterParams cp) {
             m_ws = (m_w == -INFINITY) ? 0.0f : m_w;
             float s0 = 0.0f, s1 = 0.0f;
             if (BF && fabsf(m_ws) <= kRobustAbove) {
-                const float off = -m_ws * kLog2e;
+                const float off = -__fmul_rn(m_ws, kLog2e);
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     uint32_t* w = reinterpret_cast<uint32_t*>(&d[i]);
@@ -448,6 +454,8 @@ ce_row_cluster_kernel(const ClusterParams cp) {
                         w[j] = pack_bf16x2(e0, e1);
                     }
                 }
+                s0 = fmaf(s0, offset_error(m_ws), s0);
+                s1 = fmaf(s1, offset_error(m_ws), s1);
             } else {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
@@ -506,7 +514,8 @@ ce_row_cluster_kernel(const ClusterParams cp) {
                 } else {
                     // entries are a e - u: the registers hold 2^((z - m_w) log2e)
                     // (fast divisions, two ulp: an exact one holds a slow path that the row in the registers is spilled for)
-                    const float a = __fdividef(inv_n_s * (1.0f + 2.0f * p.zeta * st.lse), S) * ex2_approx((m_ws - M) * kLog2e);
+                    float a = __fdividef(inv_n_s * (1.0f + 2.0f * p.zeta * st.lse), S) * ex2_approx((m_ws - M) * kLog2e);
+                    if (BF && fabsf(m_ws) <= kRobustAbove) a = fmaf(a, offset_error(m_ws), a);
                     const float u = inv_n_s * p.eps * cp.inv_v;
                     T* g_row = static_cast<T*>(p.grad) + (long long)job_row(it) * p.stride;
                     uint4* dst = reinterpret_cast<uint4*>(g_row - head) + vbeg;
@@ -686,7 +695,8 @@ ce_stream_kernel(const StreamParams sp) {
         m = ord2f(__reduce_max_sync(0xffffffffu, f2ord(m)));
         const float ms = (m == -INFINITY) ? 0.0f : m;
         const bool fold = BF && fabsf(ms) <= kRobustAbove;     // as in the cluster kernel
-        const f2 off2 = f2_make(-ms * kLog2e, -ms * kLog2e), ms2 = f2_make(-ms, -ms), c2 = f2_make(kLog2e, kLog2e);
+        const float off = -__fmul_rn(ms, kLog2e);
+        const f2 off2 = f2_make(off, off), ms2 = f2_make(-ms, -ms), c2 = f2_make(kLog2e, kLog2e);
         f2 sum2 = 0ull;
         auto add = [&](auto folded) {
 #pragma unroll
@@ -699,7 +709,8 @@ ce_stream_kernel(const StreamParams sp) {
         };
         if (fold) add(std::true_type{});
         else add(std::false_type{});
-        const float s = warp_sum(f2_sum(sum2));
+        float s = warp_sum(f2_sum(sum2));
+        if (fold) s = fmaf(s, offset_error(ms), s);
         if (lane == 0) sp.part[u * kStreamWarps + warp] = make_float4(m, s, mean, 0.0f);
     }
     cp_async_wait_all();

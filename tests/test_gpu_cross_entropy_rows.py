@@ -160,3 +160,40 @@ def test_nan_that_a_warp_sees_with_no_finite_logit(dt, T):
             n = torch.full((1,), T, dtype=torch.int64, device=DEV)
             a, c = run(z, ids, mask, eps, status=b.DEV_NONFINITE, denom=n), run(z, ids, gone, eps, denom=n)
             assert torch.equal(a[0].nan_to_num(7.0), c[0].nan_to_num(7.0)) and torch.equal(a[2], c[2]) and torch.equal(a[3], c[3])
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("T,V,grad", [(768, 1024, True), (768, 20488, True), (768, 20488, False), (768, 5003, True)])
+def test_log_prob_of_rows_far_from_zero(dt, T, V, grad):
+    """Rows around +-40 ... 4000.  The differences z - max are exact there, so the log-prob keeps the digits that it has
+    around zero: an exponential 2^-22 and u (2 (M - z)) relative, the sum C additions, the logarithm and the last difference
+    u each (u = 2^-24, C as in check()); a maximum M itself leaves no error.  The log-sum-exp has u |M| from its rounding."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    z = (2.0 * torch.randn(T, V, generator=g, device=DEV)).to(BF).float()
+    z -= z.max(dim=1, keepdim=True).values
+    far = torch.exp(torch.rand(T, 1, generator=g, device=DEV) * 4.6 + 3.7) * (1 - 2 * (torch.arange(T, device=DEV)[:, None] % 2))
+    z = (z + far.to(BF).float()).to(dt)
+    ids = z.argmax(dim=1).int()
+    other = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    ids = torch.where(torch.arange(T, device=DEV) % 3 == 0, other, ids)
+    logp, lse, loss, gr = run(z, ids, None, want_grad=grad)
+    x = z.double()
+    M = x.max(dim=1, keepdim=True).values
+    want = torch.log_softmax(x, dim=1)
+    p = want.exp()
+    below = torch.where(p > 0, M - x, torch.zeros_like(x))
+    C = max(64, V // 256 + 13)
+    lp = want.gather(1, ids.long()[:, None])[:, 0]
+    D = U * (2 * (p * below).sum(dim=1) + C + 8) + 2.0 ** -22 + 3 * U * lp.abs()
+    err = (logp.double() - lp).abs()
+    assert (err <= D).all(), ((err / D).max().item(), err.max().item())
+    assert ((lse.double() - torch.logsumexp(x, dim=1)).abs() <= D + U * M[:, 0].abs() * 2).all()
+    if grad and dt == BF:
+        # two roundings to bf16 (the kept exponential and the entry), and the errors above
+        want_g = p / T
+        want_g.scatter_add_(1, ids.long()[:, None], torch.full((T, 1), -1.0 / T, dtype=torch.float64, device=DEV))
+        rel = D[:, None] + U * (2 * below + 12) + 2.0 ** -21 + 2.02 * 2.0 ** -8
+        off = torch.ones_like(p, dtype=torch.bool).scatter_(1, ids.long()[:, None], False)
+        e = (gr.double() - want_g).abs()
+        assert (e <= rel * p / T + 2.0 ** -125)[off].all()
