@@ -790,7 +790,8 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             run_s *= f;
                             run_m = cm;
                         }
-                        const float off = -run_m * kLog2e;
+                        // (nothing but -inf so far, log-prob only: they add zero; against a maximum of -inf they would add NaN)
+                        const float off = (run_m == -INFINITY && !p.part_u) ? 0.0f : -run_m * kLog2e;
                         float s0 = 0.0f, s1 = 0.0f;
                         if (p.part_u) {
                             float u0 = 0.0f, u1 = 0.0f;

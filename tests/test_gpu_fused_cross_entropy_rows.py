@@ -27,3 +27,20 @@ def test_nan_rows_that_fill_a_column_tile(form, T, V, first, last):
             assert torch.isnan(lp).all() and torch.isnan(lse).all() and not loss.any()
             assert gh is None or not gh.any()
             assert gw is None or not gw.any()
+
+
+@pytest.mark.parametrize("T", [5, 300])
+@pytest.mark.parametrize("V,first,last", [(1032, 0, 64), (1032, 0, 256), (1032, 256, 512), (1032, 1024, 1032), (20008, 19968, 20008)])
+def test_masked_columns_without_gradients(T, V, first, last):
+    """Columns of -inf (a head whose padding rows hold -inf in a feature that is one) have probability zero, wherever they
+    lie; the statistics are those of the other columns."""
+    H, W, ids, mask = _inputs(T, 64, V, 22)
+    H[:, 3] = 1.0
+    ids.clamp_(max=first - 1) if first else ids.clamp_(min=last)
+    W[first:last, 3] = float("-inf")
+    keep = torch.ones(V, dtype=torch.bool, device=DEV)
+    keep[first:last] = False
+    at = torch.cumsum(keep, 0).int() - 1
+    for zc in (0.0, 1e-3):
+        out = run(H, W, ids, mask, 0.0, zc, want_grad_hidden=False, want_grad_W=False)
+        check(out, H, W[keep], at[ids.long()], mask, 0.0, zc)
