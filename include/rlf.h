@@ -444,8 +444,9 @@ rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T
  *   grad_hidden [T, D] bf16 or NULL;  grad_W [V, D] or NULL (both NULL: forward only)
  *   accumulate_grad_W  adds to an fp32 grad_W; with a bf16 grad_W it returns RLF_ERR_UNSUPPORTED
  *   workspace   rlf_workspace_bytes(RLF_FN_FUSED_CROSS_ENTROPY, T, V, D, grad_W_dt) bytes, 256-byte aligned
- *               (chiefly a bf16 scratch of min(T, 18944) rows by V; with a bf16 grad_W and T > 18944 also
- *               an fp32 [V, D] sum); contents need not be initialised
+ *               (chiefly a bf16 scratch of min(T, 18944) rows by V; fp32 partial sums of grad_hidden where its
+ *               sum over a long vocabulary is cut into pieces, at most 1 GiB; with a bf16 grad_W and T > 18944
+ *               also an fp32 [V, D] sum); contents need not be initialised
  * T = 0 is valid (loss_out = 0; grad_W zeros, or unchanged when accumulated).  T, V or D of 2^30 and more
  * returns RLF_ERR_UNSUPPORTED.
  */

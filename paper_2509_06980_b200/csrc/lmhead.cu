@@ -129,10 +129,10 @@ struct GemmParams {
     int store_w16;            // kGradW: the result goes to map_c's matrix as bf16 instead of to out_f32 (last chunk of a call)
     const float* add_f32;     // kGradW with store_w16 (optional): earlier chunks' fp32 sum, [M][out_stride], added before rounding
     // kGradHidden: with few row units the vocabulary (the long axis) is cut into up to k_split_max pieces (hidden_splits), whose
-    // raw sums go to k_part, [piece][k_part_rows][out_stride] fp32, for ce_join_hidden_kernel
+    // raw sums go to k_part, [piece][live rows of the chunk][out_stride] fp32, for ce_join_hidden_kernel
     int k_split_max;
     float* k_part;
-    long long k_part_rows;
+    long long k_part_floats;  // what k_part holds: there are never more pieces than fit
 };
 
 // ---- PTX wrappers ---------------------------------------------------------------------------
@@ -297,15 +297,19 @@ __device__ __forceinline__ int auto_split(int m_units, int n_tiles, int workers,
 }
 // Pieces that the vocabulary is cut into in grad_hidden, `units` output tiles of k_slabs each on the workers: rounds of a
 // piece's slabs (six more for its drain), and a quarter of a slab's time per unit and piece to write and join its raw sums.
-// (10 row units x 16 column tiles on 74 pairs: three rounds uncut, 2.33 in three pieces.)  Every lane of a full warp calls it.
-__device__ __forceinline__ int hidden_splits(int units, int k_slabs, int workers, int most) {
+// (10 row units x 16 column tiles on 74 pairs: three rounds uncut, 2.33 in three pieces.)
+constexpr int kSlabsPerPiece = 16;          // a piece holds at least so many k-slabs
+__host__ __device__ constexpr unsigned hidden_cost(int units, int k_slabs, int workers, int k) {
+    const unsigned rounds = (unsigned)((units * k + workers - 1) / workers), slabs = (unsigned)((k_slabs + k - 1) / k);
+    return (rounds * (slabs + 6) + (k > 1 ? (unsigned)(units * k + 3) / 4 : 0)) << 7 | (unsigned)k;
+}
+// room: floats that the pieces may take, `rows` rows of D each.  Every lane of a full warp calls it.
+__device__ __forceinline__ int hidden_splits(int units, int k_slabs, int workers, int most, long long room, int rows, int D) {
     const int lane = threadIdx.x & 31;
+    const long long fit = room / ((long long)max(rows, 1) * D);
+    if (fit < most) most = fit < 1 ? 1 : (int)fit;
     unsigned best = 0xffffffffu;
-    for (int k = lane + 1; k <= most && (k == 1 || k_slabs >= 16 * k); k += 32) {
-        const unsigned rounds = (unsigned)((units * k + workers - 1) / workers), slabs = (unsigned)((k_slabs + k - 1) / k);
-        const unsigned cost = (rounds * (slabs + 6) + (k > 1 ? (unsigned)(units * k + 3) / 4 : 0)) << 7 | (unsigned)k;
-        best = best < cost ? best : cost;
-    }
+    for (int k = lane + 1; k <= most && (k == 1 || k_slabs >= kSlabsPerPiece * k); k += 32) best = min(best, hidden_cost(units, k_slabs, workers, k));
     return (int)(__reduce_min_sync(0xffffffffu, best) & 127u);
 }
 
@@ -357,7 +361,8 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             workers = min(workers, p.block_workers);
         }
     }
-    const int k_split = (CE && p.mode == kGradHidden) ? hidden_splits(m_units * p.n_tiles, k_slabs, workers, p.k_split_max) : 1;
+    const int k_split = (CE && p.mode == kGradHidden)
+                            ? hidden_splits(m_units * p.n_tiles, k_slabs, workers, p.k_split_max, p.k_part_floats, M, (int)p.out_stride) : 1;
     const int all_units = (no_k && p.accumulate) ? 0 : sweep ? m_units * nsplit : m_units * p.n_tiles * k_split;
     const int units = worker < workers ? all_units : 0;      // (a worker beyond those that take part has nothing to do)
 
@@ -825,7 +830,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             float so = sc;
                             if (CE && k_split > 1) {
                                 // a piece's raw sums (nvalid is a multiple of 4)
-                                float4* d4 = reinterpret_cast<float4*>(p.k_part + ((long long)piece * p.k_part_rows + row_a) * p.out_stride + cb);
+                                float4* d4 = reinterpret_cast<float4*>(p.k_part + ((long long)piece * M + row_a) * p.out_stride + cb);
 #pragma unroll
                                 for (int i = 0; i < 8; ++i)
                                     if (4 * i < nvalid)
@@ -2107,14 +2112,14 @@ ce_combine_rows_kernel(const CeCombine p) {
 // joins the pieces of grad_hidden's long axis: row r (of *count - off) of the output, factors applied as in the contraction's
 // epilogue.  Nothing to do where hidden_splits made one piece.
 __global__ void __launch_bounds__(256)
-ce_join_hidden_kernel(const float* __restrict__ part, long long part_rows, int D, const int* __restrict__ count, int off,
+ce_join_hidden_kernel(const float* __restrict__ part, long long part_floats, int D, const int* __restrict__ count, int off,
                       int rows_max, const int32_t* __restrict__ row_index, const float* __restrict__ row_scale,
                       const float* __restrict__ col_vec, const float* __restrict__ row_add, int rows_per_unit, int k_slabs,
                       int workers, int k_split_max, __nv_bfloat16* __restrict__ out) {
     const int n = max(0, min(*count - off, rows_max));
     const int r = blockIdx.x;
     const int units = (n + rows_per_unit - 1) / rows_per_unit * ((D + BN - 1) / BN);
-    const int pieces = hidden_splits(units, k_slabs, workers, k_split_max);
+    const int pieces = hidden_splits(units, k_slabs, workers, k_split_max, part_floats, n, D);
     if (r >= n || pieces == 1) return;
     const float sc = row_scale[r], ra = col_vec ? row_add[r] : 0.0f;
     __nv_bfloat16* o = out + (long long)row_index[off + r] * D;
@@ -2122,7 +2127,7 @@ ce_join_hidden_kernel(const float* __restrict__ part, long long part_rows, int D
         float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
         for (int k = 0; sc != 0.0f && k < pieces; ++k) {       // (sc = 0: zeros, as in the epilogue)
-            const float4 q = *reinterpret_cast<const float4*>(part + ((long long)k * part_rows + r) * D + c);
+            const float4 q = *reinterpret_cast<const float4*>(part + ((long long)k * n + r) * D + c);
             a.x += q.x; a.y += q.y; a.z += q.z; a.w += q.w;
         }
         a.x *= sc; a.y *= sc; a.z *= sc; a.w *= sc;
@@ -2209,12 +2214,40 @@ static rlf_status launch_colsum(const __nv_bfloat16* M, int64_t rows, int32_t D,
     return cuda_ok(cudaGetLastError());
 }
 
-// most pieces of grad_hidden's long axis: what a gigabyte of fp32 rows holds
-static int hidden_pieces(int64_t T, int32_t D) {
+// Most pieces of grad_hidden's long axis: what it has slabs for, and a gigabyte of fp32 rows holds.
+static int hidden_pieces(int64_t T, int32_t V, int32_t D) {
     int64_t rows = ((T > 0 ? T : 1) + 255) & ~(int64_t)255;
     if (rows > kChunkTokens) rows = kChunkTokens;
-    const int64_t k = (256ll << 20) / (rows * D);
+    int64_t k = (256ll << 20) / (rows * D);
+    const int64_t slabs = 4ll * ((V + BN - 1) / BN);
+    if (k > slabs / kSlabsPerPiece) k = slabs / kSlabsPerPiece;
     return (int)(k < 1 ? 1 : k > 64 ? 64 : k);
+}
+// Floats that their raw sums take at most: over every number of live rows, the pieces that hidden_splits would make of them in
+// any form of the contraction (units of 512 or 256 rows on pairs of SMs, of 128 on single ones).
+static size_t hidden_part_floats(int64_t T, int32_t V, int32_t D) {
+    const int most = hidden_pieces(T, V, D);
+    if (most < 2) return 0;
+    const int64_t rows = T < kChunkTokens ? T : kChunkTokens;
+    const int slabs = 4 * ((V + BN - 1) / BN), n_tiles = (D + BN - 1) / BN, sms = sm_count_lm();
+    size_t need = 0;
+    for (int unit_rows = 128; unit_rows <= 512; unit_rows *= 2) {
+        const int64_t m_units = (rows + unit_rows - 1) / unit_rows;
+        const int64_t all = m_units * n_tiles * most;
+        int workers = unit_rows == 128 ? sms : sms / 2;
+        if (workers > all) workers = (int)all;
+        for (int64_t m = 1; m <= m_units; ++m) {
+            unsigned best = 0xffffffffu;
+            for (int k = 1; k <= most; ++k) {
+                const unsigned cost = hidden_cost((int)(m * n_tiles), slabs, workers, k);
+                best = best < cost ? best : cost;
+            }
+            const int64_t live = m * unit_rows < rows ? m * unit_rows : rows;
+            const size_t floats = (best & 127u) > 1 ? (size_t)(best & 127u) * (size_t)live * (size_t)D : 0;
+            need = need > floats ? need : floats;
+        }
+    }
+    return need;
 }
 struct CeWs {
     size_t head, terms, list, zy, mean, part, idx_live, ok_y, lse_g, coef_g, tgt_g, add_g, ref_g, scale_g, ucol,
@@ -2249,7 +2282,7 @@ static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
     w.tmax = take(4 * chunk * tiles);
     // fp32 sum of grad_W over the chunks of a call whose result is bf16
     w.gw_acc = take(w16 && Tn > (size_t)kChunkTokens ? 4 * (size_t)V * Dn : 0);
-    w.k_part = take(4 * (size_t)hidden_pieces(T, D) * chunk * Dn);
+    w.k_part = take(4 * hidden_part_floats(T, V, D));
     w.dz = take(2 * chunk * tiles * BN);
     w.total = o + 1024;
     return w;
@@ -2435,9 +2468,9 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             h.row_scale = c.scale_g + t0;      // 1 without the reference, 0 for a row that was taken out
             h.col_vec = ucol;
             h.row_add = c.add_g + t0;
-            h.k_split_max = hidden_pieces(T, D);
+            h.k_part_floats = (long long)((w.dz - w.k_part) / sizeof(float));
+            h.k_split_max = h.k_part_floats > 0 ? hidden_pieces(T, V, D) : 1;
             h.k_part = at(w.k_part);
-            h.k_part_rows = tcp;
             h.pace = pace + 2;
             h.pace_is_zero = 1;
             // up to 256 rows fill one pair's accumulator: the second one would multiply nothing
@@ -2447,7 +2480,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
             if (st != RLF_OK) return st;
             if (h.k_split_max > 1) {
                 ce_join_hidden_kernel<<<(unsigned)tc, 256, 0, s>>>(
-                    h.k_part, tcp, D, counts, (int)t0, (int)tc, idx_live, h.row_scale, ucol, h.row_add,
+                    h.k_part, h.k_part_floats, D, counts, (int)t0, (int)tc, idx_live, h.row_scale, ucol, h.row_add,
                     (pair ? 2 : 1) * (pair && acc2 ? 2 : 1) * BM, h.k_slabs, sched.workers, h.k_split_max, h.out_bf16);
                 count_launch();
             }

@@ -44,3 +44,15 @@ def test_masked_columns_without_gradients(T, V, first, last):
     for zc in (0.0, 1e-3):
         out = run(H, W, ids, mask, 0.0, zc, want_grad_hidden=False, want_grad_W=False)
         check(out, H, W[keep], at[ids.long()], mask, 0.0, zc)
+
+
+@pytest.mark.parametrize("T,D,V", [(1, 64, 20008), (64, 512, 20008), (257, 320, 4360), (700, 256, 8200), (1500, 64, 1032)])
+def test_exactly_the_workspace_asked_for(form, T, D, V):
+    """Nothing is written beside the bytes asked for, and the pieces of grad_hidden fit them for any number of live rows."""
+    b = gc.binding()
+    H, W, ids, mask = _inputs(T, D, V, 23)
+    n = b.workspace_bytes(b.FN_FUSED_CROSS_ENTROPY, T, V, D, b.RLF_F32)
+    buf = torch.full((n + 4096,), 171, dtype=torch.uint8, device=DEV)
+    for live in (mask, torch.ones_like(mask), (torch.arange(T, device=DEV) < max(1, T // 9)).to(torch.uint8)):
+        check(run(H, W, ids, live, 0.1, 1e-4, workspace=buf[:n]), H, W, ids, live, 0.1, 1e-4)
+        assert (buf[n:] == 171).all()
