@@ -76,6 +76,7 @@ typedef enum { RLF_BF16 = 0, RLF_F32 = 1 } rlf_dtype;
 #define RLF_FN_NORM_BWD 7
 #define RLF_FN_CROSS_ENTROPY 8
 #define RLF_FN_FUSED_CROSS_ENTROPY 9
+#define RLF_FN_FUSED_CROSS_ENTROPY_FWD 10   /* the same call without gradients */
 
 typedef struct CUstream_st *rlf_stream_t;
 
@@ -446,7 +447,8 @@ rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T
  *   workspace   rlf_workspace_bytes(RLF_FN_FUSED_CROSS_ENTROPY, T, V, D, grad_W_dt) bytes, 256-byte aligned
  *               (chiefly a bf16 scratch of min(T, 18944) rows by V; fp32 partial sums of grad_hidden where its
  *               sum over a long vocabulary is cut into pieces, at most 1 GiB; with a bf16 grad_W and T > 18944
- *               also an fp32 [V, D] sum); contents need not be initialised
+ *               also an fp32 [V, D] sum); contents need not be initialised.  Forward only, with
+ *               RLF_FN_FUSED_CROSS_ENTROPY_FWD: none of these, the hidden rows once and some 700 bytes a token
  * T = 0 is valid (loss_out = 0; grad_W zeros, or unchanged when accumulated).  T, V or D of 2^30 and more
  * returns RLF_ERR_UNSUPPORTED.
  */

@@ -15,6 +15,7 @@ _LIB_PATH = os.path.join(_HERE, "librlf.so")
 
 RLF_BF16, RLF_F32 = 0, 1
 FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY, FN_NORM_BWD, FN_CROSS_ENTROPY, FN_FUSED_CROSS_ENTROPY = 3, 4, 5, 6, 7, 8, 9
+FN_FUSED_CROSS_ENTROPY_FWD = 10
 DEV_BAD_TARGET, DEV_BAD_SEQ, DEV_NONFINITE, DEV_TIMEOUT = 1, 2, 4, 8
 
 EXPORTS = [
@@ -586,7 +587,8 @@ def rlf_fused_lmhead_cross_entropy(hidden, W, ids, mask=None, label_smoothing=0.
     if loss_out is None:
         loss_out = hidden.new_empty(4, dtype=_f64)
     w_dt = RLF_F32 if grad_W is None else _dt(grad_W, "grad_W")
-    workspace, wp, wn = _workspace(workspace, here, hidden, FN_FUSED_CROSS_ENTROPY, T, V, D, w_dt)
+    fn = FN_FUSED_CROSS_ENTROPY_FWD if grad_hidden is None and grad_W is None else FN_FUSED_CROSS_ENTROPY
+    workspace, wp, wn = _workspace(workspace, here, hidden, fn, T, V, D, w_dt)
     _check(_lib.rlf_fused_lmhead_cross_entropy(
         _at(hidden, here, "hidden", _bf16), _at(W, here, "W", _bf16, (V, D)), T, D, V, _at(ids, here, "ids", _i32t, n),
         _at(mask, here, "mask", _u8, n), label_smoothing, z_coef, _at(denom, here, "denom", _i64t),

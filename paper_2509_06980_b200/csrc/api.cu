@@ -31,7 +31,7 @@ size_t entropy_workspace_bytes(int64_t T, int32_t V);             // logits_loss
 size_t lmhead_logp_workspace_bytes(int64_t T);                    // lmhead.cu
 size_t norm_bwd_workspace_bytes(int64_t T, int32_t D);            // norm.cu
 size_t cross_entropy_workspace_bytes(int64_t T, int32_t V, rlf_dtype dt);                  // cross_entropy.cu
-size_t lmhead_ce_workspace_bytes(int64_t T, int32_t V, int32_t D, int grad_w_bf16);  // lmhead.cu
+size_t lmhead_ce_workspace_bytes(int64_t T, int32_t V, int32_t D, bool grad_w_bf16, bool grads);  // lmhead.cu
 
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -88,7 +88,8 @@ extern "C" size_t rlf_workspace_bytes(int which_fn, int64_t T, int32_t V, int32_
     if (which_fn == RLF_FN_LOGP_ENTROPY) return rlf::entropy_workspace_bytes(T, V);
     if (which_fn == RLF_FN_FUSED_LOGP_ENTROPY) return rlf::lmhead_logp_workspace_bytes(T);
     if (which_fn == RLF_FN_CROSS_ENTROPY) return rlf::cross_entropy_workspace_bytes(T, V, (rlf_dtype)dt);
-    if (which_fn == RLF_FN_FUSED_CROSS_ENTROPY) return rlf::lmhead_ce_workspace_bytes(T, V, D, dt == RLF_BF16);
+    if (which_fn == RLF_FN_FUSED_CROSS_ENTROPY) return rlf::lmhead_ce_workspace_bytes(T, V, D, dt == RLF_BF16, true);
+    if (which_fn == RLF_FN_FUSED_CROSS_ENTROPY_FWD) return rlf::lmhead_ce_workspace_bytes(T, V, D, false, false);
     if (which_fn == RLF_FN_NORM_BWD) return rlf::norm_bwd_workspace_bytes(T, D);
     return 0;
 }

@@ -2253,8 +2253,9 @@ struct CeWs {
     size_t head, terms, list, zy, mean, part, idx_live, ok_y, lse_g, coef_g, tgt_g, add_g, ref_g, scale_g, ucol,
         gcol, col_part, hidden_g, hidden_s, tmax, gw_acc, k_part, dz, total;
 };
-static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
-    CeWs w;
+// grads: false for a forward-only call, which keeps no scratch
+static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16, bool grads) {
+    CeWs w = {};
     size_t o = 0;
     const size_t Tn = (size_t)(T > 0 ? T : 0), Tp = (Tn + 255) & ~(size_t)255, Dn = (size_t)D;
     const size_t chunk = Tp < (size_t)kChunkTokens ? Tp : (size_t)kChunkTokens;
@@ -2267,32 +2268,34 @@ static CeWs ce_workspace(int64_t T, int32_t V, int32_t D, bool w16) {
     w.mean = take(4 * Tp);
     w.part = take(8 * Tn * kCeSplit);
     w.idx_live = take(4 * Tp);
-    w.ok_y = take(4 * Tp);
-    w.lse_g = take(4 * Tp);
-    w.coef_g = take(4 * Tp);
-    w.tgt_g = take(4 * Tp);
-    w.add_g = take(4 * Tp);
     w.ref_g = take(4 * Tp);
-    w.scale_g = take(4 * Tp);
     w.ucol = take(4 * Dn);
-    w.gcol = take(4 * Dn);
     w.col_part = take(4 * Dn * kColsumParts);
     w.hidden_g = take(2 * Tp * Dn);
-    w.hidden_s = take(2 * chunk * Dn);
-    w.tmax = take(4 * chunk * tiles);
-    // fp32 sum of grad_W over the chunks of a call whose result is bf16
-    w.gw_acc = take(w16 && Tn > (size_t)kChunkTokens ? 4 * (size_t)V * Dn : 0);
-    w.k_part = take(4 * hidden_part_floats(T, V, D));
-    w.dz = take(2 * chunk * tiles * BN);
+    if (grads) {
+        w.ok_y = take(4 * Tp);
+        w.lse_g = take(4 * Tp);
+        w.coef_g = take(4 * Tp);
+        w.tgt_g = take(4 * Tp);
+        w.add_g = take(4 * Tp);
+        w.scale_g = take(4 * Tp);
+        w.gcol = take(4 * Dn);
+        w.hidden_s = take(2 * chunk * Dn);
+        w.tmax = take(4 * chunk * tiles);
+        // fp32 sum of grad_W over the chunks of a call whose result is bf16
+        w.gw_acc = take(w16 && Tn > (size_t)kChunkTokens ? 4 * (size_t)V * Dn : 0);
+        w.k_part = take(4 * hidden_part_floats(T, V, D));
+        w.dz = take(2 * chunk * tiles * BN);
+    }
     w.total = o + 1024;
     return w;
 }
 
 }  // namespace lm
 
-size_t lmhead_ce_workspace_bytes(int64_t T, int32_t V, int32_t D, int grad_w_bf16) {
+size_t lmhead_ce_workspace_bytes(int64_t T, int32_t V, int32_t D, bool grad_w_bf16, bool grads) {
     if (V < 1 || D < 1) return 0;
-    return lm::ce_workspace(T, V, D, grad_w_bf16 != 0).total;
+    return lm::ce_workspace(T, V, D, grad_w_bf16, grads).total;
 }
 
 }  // namespace rlf
@@ -2317,7 +2320,8 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     if (!aligned(hidden, 16) || !aligned(W, 16) || !aligned(grad_hidden, 16) || !aligned(grad_W, 16) || !aligned(ids, 4) ||
         !aligned(logp_out, 4) || !aligned(lse_out, 4) || !aligned(loss_out, 8) || !aligned(denom, 8))
         return RLF_ERR_ALIGN;
-    const CeWs w = ce_workspace(T, V, D, w16);
+    const bool bwd = grad_hidden || grad_W;
+    const CeWs w = ce_workspace(T, V, D, w16, bwd);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < w.total) return RLF_ERR_WORKSPACE;
     st = check_arch();
     if (st != RLF_OK) return st;
@@ -2351,7 +2355,7 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
     __nv_bfloat16* Hs = reinterpret_cast<__nv_bfloat16*>(ws + w.hidden_s);
     __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + w.dz);
     const int64_t Tp = (T + 255) & ~(int64_t)255;
-    const bool bwd = grad_hidden || grad_W, smoothing = label_smoothing > 0.0f;
+    const bool smoothing = label_smoothing > 0.0f;
     const bool row_ref = bwd && g_row_ref.load() != 0;
     float* ucol = smoothing ? at(w.ucol) : nullptr;
     st = ce_launch_plan(ids, mask, T, V, list, counts, n_mask, chunk_flag, kFlagWords, dev_status, s);

@@ -56,3 +56,18 @@ def test_exactly_the_workspace_asked_for(form, T, D, V):
     for live in (mask, torch.ones_like(mask), (torch.arange(T, device=DEV) < max(1, T // 9)).to(torch.uint8)):
         check(run(H, W, ids, live, 0.1, 1e-4, workspace=buf[:n]), H, W, ids, live, 0.1, 1e-4)
         assert (buf[n:] == 171).all()
+
+
+@pytest.mark.parametrize("T,D,V", [(1, 64, 8), (64, 512, 20008), (700, 256, 8200), (19100, 64, 264)])
+def test_exactly_the_workspace_of_a_call_without_gradients(form, T, D, V):
+    b = gc.binding()
+    H, W, ids, mask = _inputs(T, D, V, 24)
+    n = b.workspace_bytes(b.FN_FUSED_CROSS_ENTROPY_FWD, T, V, D, b.RLF_F32)
+    buf = torch.full((n + 4096,), 171, dtype=torch.uint8, device=DEV)
+    for live in (mask, torch.ones_like(mask)):
+        for eps in (0.0, 0.1):
+            out = run(H, W, ids, live, eps, 1e-4, want_grad_hidden=False, want_grad_W=False, workspace=buf[:n])
+            check(out, H, W, ids, live, eps, 1e-4)
+            assert (buf[n:] == 171).all()
+    with pytest.raises(b.RlfError):                   # too small for a gradient
+        run(H, W, ids, mask, want_grad_W=False, workspace=buf[:n])

@@ -33,3 +33,11 @@ def test_partial_sums_stay_below_the_scratch(b, T, D, V):
     n = b.workspace_bytes(b.FN_FUSED_CROSS_ENTROPY, T, V, D, b.RLF_F32)
     beside = n - _scratch(T, V) - _rows(T, D) - T * (8 * 80 + 128) - 4 * D * 140 - 4 * T * (V // 256 + 2)
     assert beside <= _scratch(T, V)
+
+
+@pytest.mark.parametrize("T,D,V", [(8192, 4096, 151936), (64, 2560, 151936), (40000, 64, 264), (0, 64, 8)])
+def test_a_call_without_gradients_keeps_no_scratch(b, T, D, V):
+    n = b.workspace_bytes(b.FN_FUSED_CROSS_ENTROPY_FWD, T, V, D, b.RLF_F32)
+    assert 0 < n <= _rows(T, D) // 2 + T * (8 * 80 + 128) + 4 * D * 140 + (1 << 16)
+    assert n == b.workspace_bytes(b.FN_FUSED_CROSS_ENTROPY_FWD, T, V, D, b.RLF_BF16)
+    assert n < b.workspace_bytes(b.FN_FUSED_CROSS_ENTROPY, T, V, D, b.RLF_F32)
