@@ -159,7 +159,8 @@ def sharded_grpo_step(ids, cu_seqlens, rewards, group_size, old_logp, ref_logp, 
 
 def sharded_sft_step(ids, cu_seqlens, open_id, close_id, logits=None, hidden=None, W=None, residual=None,
                      norm_weight=None, norm_bias=None, norm_kind=0, norm_eps=1e-6, label_smoothing=0.0, z_coef=0.0,
-                     grad_W=None, accumulate_grad_W=False, group=None, ops=None, reduce_grads=True, n_global=None):
+                     grad_W=None, accumulate_grad_W=False, group=None, ops=None, reduce_grads=True, n_global=None,
+                     grad_norm_weight=None, grad_norm_bias=None):
     """This rank's part of one supervised step over packed multi-turn responses: cross entropy of the model's own
     tokens (tool observations carry no loss), averaged over the whole batch's loss-carrying tokens.
 
@@ -168,7 +169,9 @@ def sharded_sft_step(ids, cu_seqlens, open_id, close_id, logits=None, hidden=Non
     block's output: it goes through the final norm (norm_kind: NORM_RMS or NORM_LAYER of the binding) first, and
     grad_hidden is the gradient before that norm; grad_norm_weight (and grad_norm_bias) come back too.
     `group`, `n_global`: as sharded_grpo_step; reduce_grads=False leaves the weight gradients unreduced (all but
-    the last of several accumulated micro-batches; the norm's gradients of those are this call's own).
+    the last of several accumulated micro-batches).  Buffers given as grad_W, grad_norm_weight and grad_norm_bias take
+    those gradients; accumulate_grad_W adds to all that are given, so that the last micro-batch reduces every weight
+    gradient's sum once.  A norm gradient without a buffer is this call's own.
     -> dict(mask, n_local, n_global, logp, lse, loss (global, fp64[4]), grad_logits | grad_hidden, grad_W,
        grad_norm_weight, grad_norm_bias)
     """
@@ -177,6 +180,10 @@ def sharded_sft_step(ids, cu_seqlens, open_id, close_id, logits=None, hidden=Non
         raise ValueError("give either logits or hidden + W")
     if norm_weight is None and (norm_bias is not None or residual is not None):
         raise ValueError("norm_bias and residual belong to the norm: give norm_weight")
+    if (grad_norm_weight is not None and norm_weight is None) or (grad_norm_bias is not None and norm_bias is None):
+        raise ValueError("grad_norm_weight and grad_norm_bias are the gradients of norm_weight and norm_bias")
+    if accumulate_grad_W and norm_bias is not None and (grad_norm_weight is None) != (grad_norm_bias is None):
+        raise ValueError("to accumulate the norm's gradients give both buffers")
     if logits is not None and norm_weight is not None:
         raise ValueError("the norm applies to hidden states, not to logits")
     mask, _, n_local = count_phase(ids, cu_seqlens, open_id, close_id, ops)
@@ -197,8 +204,11 @@ def sharded_sft_step(ids, cu_seqlens, open_id, close_id, logits=None, hidden=Non
                                                                      z_coef=z_coef, denom=n_global, grad_W=grad_W,
                                                                      accumulate_grad_W=accumulate_grad_W)
         if norm_weight is not None:
+            into = {}
+            if grad_norm_weight is not None or grad_norm_bias is not None:
+                into = dict(grad_weight=grad_norm_weight, grad_bias=grad_norm_bias, accumulate=accumulate_grad_W)
             gh, gnw, gnb = ops.rlf_norm_bwd(gh, x, norm_weight, mean, rstd, kind=norm_kind,
-                                            want_grad_bias=norm_bias is not None)
+                                            want_grad_bias=norm_bias is not None, **into)
             out.update(grad_norm_weight=gnw)
             if gnb is not None:
                 out.update(grad_norm_bias=gnb)
