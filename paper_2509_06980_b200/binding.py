@@ -454,8 +454,9 @@ NORM_RMS, NORM_LAYER = 0, 1
 
 # The calls below are short next to a decoding step or a small batch, so their host side is kept lean: outputs are made by
 # the cheapest factory call and not checked again, workspace sizes are computed once per shape.
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_get_device = torch._C._cuda_getDevice
+# (torch's own short cuts where this build of it has them; without CUDA it has neither, and the module is still to be imported)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _f32, _f64, _bf16, _i32t, _i64t, _u8 = (torch.float32, torch.float64, torch.bfloat16, torch.int32, torch.int64, torch.uint8)
 _DTYPES = {torch.bfloat16: RLF_BF16, torch.float32: RLF_F32}
 
