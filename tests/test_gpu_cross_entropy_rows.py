@@ -197,3 +197,23 @@ def test_log_prob_of_rows_far_from_zero(dt, T, V, grad):
         off = torch.ones_like(p, dtype=torch.bool).scatter_(1, ids.long()[:, None], False)
         e = (gr.double() - want_g).abs()
         assert (e <= rel * p / T + 2.0 ** -125)[off].all()
+
+
+# by launch shape: CTAs of 64 and 128 threads, clusters of 1, 2, 4, 8, 10 and 16 CTAs; several rows per cluster each
+@pytest.mark.parametrize("T,V", [(15000, 504), (7000, 6007), (6500, 8000), (3200, 16001), (1700, 30016), (1600, 32003), (800, 70001),
+                                 (450, 151936), (420, 151937), (260, 196001), (160, 300008), (90, 500001)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_many_rows_per_cluster(dt, T, V):
+    if dt == F32:
+        V = (V + 1) // 2
+    for pad, offset in ((0, 0), (3, 1)):
+        z, ids, mask, buf = rows(T, V, dt, T + V + pad, pad, offset, live=0.7)
+        for eps, zc in ((0.0, 0.0), (0.1, 1e-3)):
+            out = run(z, ids, mask, eps, zc)
+            check(out, z, ids, mask, eps, zc)
+            again = run(z, ids, mask, eps, zc)
+            assert torch.equal(again[3], out[3]) and torch.equal(again[2], out[2])
+        same = run(z, ids, mask, 0.1, 1e-3, in_place=True)
+        assert torch.equal(same[3], out[3])
+        z.fill_(5.0)
+        assert (buf == 5.0).all()
