@@ -1910,10 +1910,13 @@ extern "C" rlf_status rlf_fused_lmhead_logp_entropy(const void* hidden, const vo
 // What bounds it, at the measured 1662 (burst) and 1399 TFLOP/s (under the power cap) and 6.56 TB/s:
 //   8192 x 4096 x 151936, 4768 live rows: the tensor pipe; 3 x 2 T V D = 17.8 TFLOP in 12.4 ms at full clocks (1.44 PFLOP/s),
 //     13.4 - 14.0 ms back to back (1.27 - 1.33);
-//   2047 x 2048 x 32000, 1433 live rows: 619 us = 180 + 188 + 183 us of contractions at 1.0 PFLOP/s: six row tiles of 256 (93 %
+//   2047 x 2048 x 32000, 1433 live rows: 614 - 680 us, 619 of them = 180 + 188 + 183 us of contractions at 1.0 PFLOP/s: six row tiles of 256 (93 %
 //     filled) by 125 column tiles are 10.1 rounds of 74 pairs, so an eleventh round runs nearly empty, and each of the launches
 //     fills and drains once; 65 us of small kernels, 32 of them the sum of W's rows for the smoothing;
-//   64 x 2560 x 151936: HBM; W is read twice and a bf16 grad_W written once, 2.3 GB in 617 us (writes alone reach 3.9 TB/s here).
+//   64 x 2560 x 151936: 617 - 655 us.  Sweep 162 us (reads W at 4.8 TB/s, and writes 64 MB of exponentials for a tile of 256 rows),
+//     grad_hidden 157 us (W again, and those), a bf16 grad_W 263 us: 714 MB at 2.7 TB/s, K is one slab, so that a unit is its drain and
+//     a drain warp has two 4 KB tiles under way; 50 us of small kernels.  An fp32 grad_W leaves row by row from the registers,
+//     1.5 GB in 830 us (1.8 TB/s): 1.2 ms in all.
 namespace rlf {
 namespace lm {
 
@@ -2015,7 +2018,9 @@ struct CeCombine {
     int* fallback;
     const int* run_flag;
     // grad_W wanted: the chunk's rows Hl times their factors go to Hs (zeros for a row that was taken out, whose hidden
-    // state may hold anything, and up to the next multiple of 256 rows)
+    // state may hold anything, and up to the next multiple of 256 rows).  bf16, as the tensor cores take it: one rounding of grad_W's
+    // terms besides the stored exponential's.  The factor is known only after the sweep, so that it could not go into the
+    // exponentials without another pass over the scratch, which would round them once more all the same.
     const __nv_bfloat16* Hl;
     __nv_bfloat16* Hs;
     int D;
