@@ -441,7 +441,8 @@ rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T
  *     grad_W[v,:]      = sum_t grad_z[t,v] hidden[t,:]  (grad_W_dt: bf16, rounded once from the fp32 sum, or fp32)
  * grad_z enters the two products as bf16, and hidden enters grad_W's times a factor per row, bf16 as well (so a term of
  * grad_W carries two roundings, of grad_hidden one, before the sums in fp32); its uniform smoothing part stays outside
- * them, in fp32.  The logits are tensor-core sums, which round toward zero: lse is low by about 4e-9 D.
+ * them, in fp32.  The logits are tensor-core sums, which round toward zero: lse is low by about 4e-9 D where the large
+ * logits are around ten.
  *
  *   hidden [T, D] bf16, W [V, D] bf16, both dense and 16-byte aligned; D a multiple of 64 and V a
  *               multiple of 8 (else RLF_ERR_SHAPE)
