@@ -333,14 +333,14 @@ struct Rows {
         }
     }
     __device__ __forceinline__ long long row(long long j) const { return EDGE ? q + j * period : j; }
-    // vector c of the row that starts at src, `from_base` elements into its tensor, on its way to dst; a vector that starts
-    // before the tensor does (row 0's; with rows shorter than a vector, the next few rows' too) is copied by element
-    __device__ __forceinline__ void copy(uint4* dst, const T* src, int c, int D, long long from_base) const {
+    // vector c of the row that starts at src, on its way to dst; a tensor's very first vector is not read before its start (only
+    // row 0, `top`, can start in it: rows are as long as a vector or longer)
+    __device__ __forceinline__ void copy(uint4* dst, const T* src, int c, int D, bool top) const {
         constexpr int N = Vec<T>::N;
         const uint4* from = reinterpret_cast<const uint4*>(src - lead) + c;
         if constexpr (!EDGE) {
             cp_async16(smem_at(dst), from);
-        } else if (c == 0 && from_base < lead) {
+        } else if (top && c == 0 && lead > 0) {
             for (int e = lead; e < N && e < lead + D; ++e) reinterpret_cast<T*>(dst)[e] = src[e - lead];
         } else {
             cp_async16_part(smem_at(dst), from, min(16, (lead + D - c * N) * (int)sizeof(T)));
@@ -425,8 +425,8 @@ norm_fwd_wide_kernel(const FwdParams p) {
                 for (int i = 0; i < NV; ++i) {
                     const int c = tid + i * th;
                     if (c < nvec) {
-                        rows.copy(slot(buf, k, 0, i), static_cast<const T*>(p.x) + t * p.x_stride, c, p.D, t * p.x_stride);
-                        if (p.res) rows.copy(slot(buf, k, 1, i), static_cast<const T*>(p.res) + t * p.x_stride, c, p.D, t * p.x_stride);
+                        rows.copy(slot(buf, k, 0, i), static_cast<const T*>(p.x) + t * p.x_stride, c, p.D, t == 0);
+                        if (p.res) rows.copy(slot(buf, k, 1, i), static_cast<const T*>(p.res) + t * p.x_stride, c, p.D, t == 0);
                     }
                 }
             }
@@ -549,9 +549,9 @@ norm_bwd_wide_kernel(const BwdParams p) {
                 for (int i = 0; i < NV; ++i) {
                     const int c = tid + i * th;
                     if (c < nvec) {
-                        rows.copy(slot(buf, k, 0, i), static_cast<const T*>(p.dy) + t * p.dy_stride, c, p.D, t * p.dy_stride);
-                        rows.copy(slot(buf, k, 1, i), static_cast<const T*>(p.x) + t * p.x_stride, c, p.D, t * p.x_stride);
-                        if (p.skip) rows.copy(slot(buf, k, 2, i), static_cast<const T*>(p.skip) + t * p.D, c, p.D, t * p.D);
+                        rows.copy(slot(buf, k, 0, i), static_cast<const T*>(p.dy) + t * p.dy_stride, c, p.D, t == 0);
+                        rows.copy(slot(buf, k, 1, i), static_cast<const T*>(p.x) + t * p.x_stride, c, p.D, t == 0);
+                        if (p.skip) rows.copy(slot(buf, k, 2, i), static_cast<const T*>(p.skip) + t * p.D, c, p.D, t == 0);
                     }
                 }
             }
@@ -668,16 +668,16 @@ norm_bwd_wide_kernel(const BwdParams p) {
 }
 
 // A row of any alignment into shared memory, by the whole CTA: the aligned 16-byte chunks that cover it.  Returns where its
-// element 0 then lies.  Only the row's own bytes and, before them, bytes of the chunk it starts in are read; where that chunk
-// starts before the tensor does (`from_base` elements lie between the tensor's start and the row's), its elements are copied
-// one by one.
+// element 0 then lies.  Only the row's own bytes and, before them, bytes of the chunk it starts in are read; a tensor's first
+// row, before which there may be nothing, has the elements of that chunk copied one by one (rows are as long as a chunk or
+// longer, so that no other row starts in the tensor's first).
 __device__ __forceinline__ int chunk_head(const void* src) { return (int)(reinterpret_cast<uintptr_t>(src) & 15); }
 template <typename T>
-__device__ __forceinline__ void copy_row(char* dst, const T* src, int D, long long from_base) {
+__device__ __forceinline__ void copy_row(char* dst, const T* src, int D, bool first) {
     const int head = chunk_head(src), bytes = head + D * (int)sizeof(T);
     const char* from = reinterpret_cast<const char*>(src) - head;
     for (int o = 16 * threadIdx.x; o < bytes; o += 16 * blockDim.x) {
-        if (o < head && from_base * (long long)sizeof(T) < head) {
+        if (first && o < head) {
             for (int e = head; e < 16 && e < bytes; e += (int)sizeof(T)) *reinterpret_cast<T*>(dst + e) = *reinterpret_cast<const T*>(from + e);
         } else {
             cp_async16_part(smem_at(dst + o), from + o, min(16, bytes - o));
@@ -703,8 +703,8 @@ norm_fwd_staged_kernel(const FwdParams p) {
         for (int k = 0; k < R; ++k) {
             const long long t = t0 + k;
             if (t < p.T) {
-                copy_row(at(buf, k, 0), static_cast<const T*>(p.x) + t * p.x_stride, D, t * p.x_stride);
-                if (p.res) copy_row(at(buf, k, 1), static_cast<const T*>(p.res) + t * p.x_stride, D, t * p.x_stride);
+                copy_row(at(buf, k, 0), static_cast<const T*>(p.x) + t * p.x_stride, D, t == 0);
+                if (p.res) copy_row(at(buf, k, 1), static_cast<const T*>(p.res) + t * p.x_stride, D, t == 0);
             }
         }
         cp_async_commit();
@@ -798,9 +798,9 @@ norm_bwd_staged_kernel(const BwdParams p) {
         for (int k = 0; k < R; ++k) {
             const long long t = t0 + k;
             if (t < p.T) {
-                copy_row(at(buf, k, 0), static_cast<const T*>(p.dy) + t * p.dy_stride, D, t * p.dy_stride);
-                copy_row(at(buf, k, 1), static_cast<const T*>(p.x) + t * p.x_stride, D, t * p.x_stride);
-                if (p.skip) copy_row(at(buf, k, 2), static_cast<const T*>(p.skip) + t * D, D, t * (long long)D);
+                copy_row(at(buf, k, 0), static_cast<const T*>(p.dy) + t * p.dy_stride, D, t == 0);
+                copy_row(at(buf, k, 1), static_cast<const T*>(p.x) + t * p.x_stride, D, t == 0);
+                if (p.skip) copy_row(at(buf, k, 2), static_cast<const T*>(p.skip) + t * D, D, t == 0);
             }
         }
         cp_async_commit();
@@ -894,7 +894,8 @@ enum Form { kStaged, kWide, kEdge };
 struct Cut { Form form; int nv, threads, rows, smem; };
 
 // false: no fast form holds the rows (the general kernels do: rows beyond 512 threads x 4 vectors, or that do not fit shared
-// memory when staged).  `arrays` rows are read per row; the staged form keeps `vectors` fp32 vectors of the width.
+// memory when staged; and rows shorter than a vector, several of which may start in the vector that their tensor starts in: a
+// test for them in the copies costs the others 3 - 8 %, 20000 x 2603 bf16 with a stride of 2606 142 -> 152 us).  `arrays` rows are read per row; the staged form keeps `vectors` fp32 vectors of the width.
 //   Forward: CTAs of up to 256 threads, two rows at a time.  32768 x 2560 bf16, no residual: 58.7 us with 256 threads and two
 //   rows, 63.7 with one row, 66 with 512 threads; with the residual 106 - 108 us whichever.
 //   Rows of up to 256 vectors without a residual, or off their vectors: 128 threads (32768 rows, 256 threads -> 128: 2048 bf16
@@ -911,6 +912,7 @@ static bool pick_cut(bool bf16, Form form, bool fwd, bool layer, bool full, long
     const int esz = bf16 ? 2 : 4;
     if (D > kSmemLimit / esz) return false;            // (before any product of D)
     const int v = 16 / esz, nvec = form == kEdge ? (D + 2 * v - 2) / v : D / v;
+    if (D < v) return false;
     const bool wide = form != kStaged;
     c->form = form;
     c->nv = 1;
