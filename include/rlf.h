@@ -442,7 +442,8 @@ rlf_status rlf_cross_entropy_fwd_bwd(const void *logits, rlf_dtype dt, int64_t T
  * grad_z enters the two products as bf16, and hidden enters grad_W's times a factor per row, bf16 as well (so a term of
  * grad_W carries two roundings, of grad_hidden one, before the sums in fp32); its uniform smoothing part stays outside
  * them, in fp32.  The logits are tensor-core sums, which round toward zero: lse is low by about 4e-9 D where the large
- * logits are around ten.
+ * logits are around ten.  The target's logit is the same sum's, so that log p is off by no more than 1 - p times a
+ * logit's error and is never above zero.
  *
  *   hidden [T, D] bf16, W [V, D] bf16, both dense and 16-byte aligned; D a multiple of 64 and V a
  *               multiple of 8 (else RLF_ERR_SHAPE)

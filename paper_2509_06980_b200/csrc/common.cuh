@@ -72,6 +72,13 @@ struct ResidentTable {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// Exponents formed as one multiply-add from a rounded offset, x log2 e - (m log2 e rounded), all lack the same r = (m log2 e rounded) -
+// m log2 e, which is known exactly: the exponentials, and their sums, are put right by the factor 2^r = 1 + r ln 2 (|r| <= 2^-13 up
+// to |m| = 2048, so that the next term is below 2^-27).  Returns r ln 2.
+__device__ __forceinline__ float offset_error(float m) {
+    return fmaf(-m, kLog2e, __fmul_rn(m, kLog2e)) * kLn2;
+}
+
 __device__ __forceinline__ float ex2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -170,12 +170,8 @@ constexpr int ctas_per_sm(int threads, int nv) {
 // exponents of bf16 rows are formed by one multiply-add from a rounded -max log2 e; rows whose maximum is huge in
 // magnitude subtract first
 constexpr float kRobustAbove = 2048.0f;
-// The rounding of m log2 e is the same for every exponent of a warp and known exactly, r = (m log2 e rounded) - m log2 e: what the
-// multiply-adds give stands for 2^-r times the exponentials, and sums and gradients are put right by 1 + r', r' = r ln 2
-// (|r| <= 2^-13 up to kRobustAbove, so that r'^2 / 2 is below 2^-27).  Without it a log-prob is off by up to 8e-5 at |m| = 2000.
-__device__ __forceinline__ float offset_error(float m) {
-    return fmaf(-m, kLog2e, __fmul_rn(m, kLog2e)) * kLn2;
-}
+// (the rounding is the same for every exponent of a warp and known: sums and gradients are put right by offset_error; without it
+// a log-prob is off by up to 8e-5 at |max| = 2000)
 
 struct ClusterParams {
     RowParams r;

@@ -109,6 +109,10 @@ struct GemmParams {
     int live_off;
     const int32_t* row_index; // kGradHidden: output row of compact row r is row_index[live_off + r]
     const float* ref;         // kLse with dz (optional): per-row reference of the stored exponentials (see below)
+    // kLse (optional): {., target column} of compact row r.  Its logit goes to target_logit[r] and stays out of the row's sums (and,
+    // as a zero, of the scratch)
+    const int2* target;
+    float* target_logit;
     const float* row_scale;   // kGradHidden (optional): fp32 factor of compact row r applied to its output row
     const int* run_flag;      // optional: the launch does nothing unless *run_flag == run_want
     int run_want;
@@ -573,6 +577,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             float run_u = 0.0f;                          // kLse with entropy: sum of 2^x x against run_m
             const int piece = (CE && k_split > 1) ? u / (m_units * p.n_tiles) : 0;
             (void)piece;
+            const int target = (!CE && sweep && p.target && row_ok) ? p.target[row].y : -1;
             for (int n = n0; n < n1 && ok; ++n) {
                 if (!no_k) {
                     // one lane polls for the warp (128 polling threads would only burn issue slots and
@@ -585,6 +590,20 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 }
                 const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)buf * BN;
                 const int col0 = n * BN;
+                // takes the target's logit out of the 32 columns from cb on (a vote per tile, and per 32 columns of a tile that holds
+                // a target of the warp's rows, keeps the selection out of the others)
+                const bool target_here = !CE && sweep && __any_sync(0xffffffffu, (unsigned)(target - col0) < (unsigned)BN);
+                auto take_target = [&](int cb, uint32_t (&v)[32]) {
+                    const int at = target - cb;
+                    if (!target_here || !__any_sync(0xffffffffu, (unsigned)at < 32u)) return;
+                    uint32_t z = 0u;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        z = i == at ? v[i] : z;
+                        v[i] = i == at ? 0xff800000u : v[i];
+                    }
+                    if ((unsigned)at < 32u) p.target_logit[row] = __uint_as_float(z);
+                };
                 if (p.mode == kLse && p.dz && p.ref) {
                     // Forward sweep that keeps the tile for the backward, exponentials taken against a
                     // reference rho known BEFORE the sweep (one per row): e = exp(z - rho) is summed for
@@ -604,6 +623,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         if (nvalid > 0) {                  // warp-uniform: the tensor-memory load is a warp-wide instruction
                             uint32_t v[32];
                             tc_ld32(t_row + (uint32_t)(c * 32), v);
+                            take_target(cb, v);
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
                                 float e0 = ex2_approx(fmaf(__uint_as_float(v[2 * i]), kLog2e, off));
@@ -641,6 +661,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         if (cb >= p.N) break;
                         uint32_t v[32];
                         tc_ld32(t_row + (uint32_t)(c * 32), v);
+                        take_target(cb, v);
                         const int nvalid = min(32, p.N - cb);
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
@@ -663,6 +684,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         if (nvalid > 0) {
                             uint32_t v[32];
                             tc_ld32(t_row + (uint32_t)(c * 32), v);
+                            take_target(cb, v);
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
                                 float e0 = ex2_approx(fmaf(__uint_as_float(v[2 * i]), kLog2e, off));
@@ -782,6 +804,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         return;
                     }
                     if (p.mode == kLse) {
+                        take_target(cb, v);
                         float cm = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
@@ -1981,7 +2004,7 @@ ce_gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, const __nv_bfloa
     if (threadIdx.x == 0) {
         const float zy = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
         idx[r] = job.x;                    // (the gradient contraction's epilogue looks its output rows up here)
-        zy_g[r] = zy;
+        zy_g[r] = zy;                      // (the sweep puts its own there)
         mean_g[r] = ((red[1][0] + red[1][1]) + (red[1][2] + red[1][3])) * inv_v;
         ref_g[r] = zy + kRefShift;
     }
@@ -1997,7 +2020,7 @@ struct CeCombine {
     const int2* list;
     const int* count;
     int off;
-    const float* zy_g;
+    const float* zy_g;          // target logit as the sweep has it
     const float* mean_g;
     const long long* denom;
     float eps, zeta, inv_v;
@@ -2043,7 +2066,9 @@ __device__ __forceinline__ void scale_row(const CeCombine& p, int r, float f, in
         dst[i] = o;
     }
 }
-// As combine_rows_kernel: statistics, outputs and gradient factors of one chunk's rows.  The target
+// As combine_rows_kernel: statistics, outputs and gradient factors of one chunk's rows.  Target logit and sums come from the
+// same tensor-core products, whose errors (they round toward zero: a logit of 20 loses up to 1e-4 at D = 4096) then leave log p
+// and 1 - p alone as p goes to one; with the target's logit from another sum, log p of such tokens came out above zero.  The target
 // entry is formed as (expm1(logp) + 2 zeta lse p_y + eps) / A_t, which keeps its digits as p_y -> 1;
 // with |A_t| below a half (a log-sum-exp near -1 / (2 zeta)) that quotient is not formed, the chunk is
 // redone with dZ itself in the scratch.
@@ -2072,15 +2097,19 @@ ce_combine_rows_kernel(const CeCombine p) {
         q[j] = k < nsplit ? parts[k] : make_float2(-INFINITY, 0.0f);
         M = fmaxf(M, q[j].x);
     }
-    M = warp_max(M);
-    float S = 0.0f;
+    const float zy = p.zy_g[g];
+    M = fmaxf(warp_max(M), zy);
+    float others = 0.0f;                       // the sum over the other columns
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        S += q[j].x == -INFINITY ? q[j].y : q[j].y * expf(q[j].x - M);      // (0 for a split of -inf, NaN where it held a NaN)
-    S = warp_sum(S);
-    const float ln_s = logf(S), zy = p.zy_g[g];
-    const float lse = M + ln_s, logp = (zy - M) - ln_s;
-    const float smooth = p.eps > 0.0f ? (M - p.mean_g[g]) + ln_s : 0.0f;
+        others += q[j].x == -INFINITY ? q[j].y : q[j].y * expf(q[j].x - M);      // (0 for a split of -inf, NaN where it held a NaN)
+    others = warp_sum(others);
+    if (p.ref_g) others = fmaf(others, offset_error(M), others);     // (M is the reference, below which the target lies)
+    const float e_y = expf(zy - M), S = others + e_y, odds = others / e_y;
+    // log p = -log(1 + odds) keeps its digits as p goes to one, where z_y - lse has none left
+    const bool near = odds < 1e30f;
+    const float logp = near ? -log1pf(odds) : (zy - M) - logf(S), lse = near ? zy - logp : M + logf(S);
+    const float smooth = p.eps > 0.0f ? lse - p.mean_g[g] : 0.0f;
     const bool ok = (M > -INFINITY) && (M < INFINITY) && (S > 0.0f) && (S < INFINITY) && (fabsf(lse) < INFINITY) &&
                     (fabsf(logp) < INFINITY) && (fabsf(smooth) < INFINITY);
     const float A = 1.0f + 2.0f * p.zeta * lse;
@@ -2408,6 +2437,8 @@ extern "C" rlf_status rlf_fused_lmhead_cross_entropy(const void* hidden, const v
         z.pace_is_zero = 1;
         z.live_count = counts;
         z.live_off = (int)t0;
+        z.target = list + t0;
+        z.target_logit = at(w.zy) + t0;
         if (bwd) {
             z.dz = dz;
             z.dz_nc = 4 * z.n_tiles;

@@ -71,3 +71,55 @@ def test_exactly_the_workspace_of_a_call_without_gradients(form, T, D, V):
             assert (buf[n:] == 171).all()
     with pytest.raises(b.RlfError):                   # too small for a gradient
         run(H, W, ids, mask, want_grad_W=False, workspace=buf[:n])
+
+
+@pytest.mark.parametrize("T,D,V", [(512, 2560, 4104), (300, 64, 1032), (700, 1024, 20008), (64, 4096, 8008)])
+def test_tokens_that_the_model_is_sure_of(form, T, D, V):
+    """Targets of probability 0.5 to 1 - 1e-13.  dz bounds a logit's error as in check() (tensor-core sums); the log-prob's
+    derivative by a logit is [v = y] - p_v, so that errors of the logits move it by at most 2 (1 - p_y) dz; so do relative
+    errors of the sum over the other columns against the target's exponential, u = 2^-24: an exponent's rounding u |z - rho| with
+    rho = z_y + 32, the target's 32 u, 340 additions, 2^-21 for the exponentials and the logarithm.  It is never above zero.
+    A gradient entry p_v (or p_y - 1) carries these twice (its own logit and the row's sum) besides its rounding to bf16 (two
+    where the scratch holds dZ itself: the exponential's and the entry's)."""
+    b = gc.binding()
+    U, HB = 2.0 ** -24, 2.0 ** -8
+    g = torch.Generator(device=DEV)
+    g.manual_seed(D + T)
+    W = (torch.randn(V, D, generator=g, device=DEV) * 2.0 / D ** 0.5).to(BF)
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    w = W[ids.long()].float()
+    lift = torch.linspace(8, 42, T, device=DEV)[:, None]
+    H = (torch.randn(T, D, generator=g, device=DEV) + lift * w / (w * w).sum(1, keepdim=True)).to(BF)
+    z = H.double() @ W.double().t()
+    y = ids.long()[:, None]
+    acc = lambda K: (K / 8 + 16) * 2.0 ** -23
+    dz = acc(D) * (H.double().abs() @ W.double().abs().t()).amax(dim=1)
+    # 1 - p_y without cancellation
+    zy = z.gather(1, y)
+    others = torch.exp(z - zy).scatter_(1, y, 0.0).sum(dim=1)
+    lp, q = -torch.log1p(others), others / (1 + others)
+    p = torch.exp(z - zy) / (1 + others)[:, None]
+    rel0 = U * (z.abs().amax(dim=1) + zy[:, 0].abs() + 64 + 340) + 2.0 ** -21
+    stored = (2.02 if form == "universal" else 1.01) * HB
+    for grad in (True, False):
+        logp, lse, loss, gh, gw = run(H, W, ids, None, want_grad_hidden=grad, want_grad_W=grad)
+        assert (logp <= 0).all()
+        # d log p = q (relative change of the odds)
+        rel = torch.expm1(2 * dz) + rel0
+        err = (logp.double() - lp).abs()
+        assert (err <= q * rel * 1.01 + 3 * U * lp.abs()).all(), (err / (q * rel + 3 * U * lp.abs())).max().item()
+        assert ((lse.double() - torch.logsumexp(z, 1)).abs() <= dz + rel0 + 4 * U * z.abs().amax(dim=1)).all()
+        if not grad:
+            continue
+        want = p.clone()
+        want.scatter_(1, y, -q[:, None])
+        e = p * (2 * rel + stored)[:, None]
+        e.scatter_(1, y, (q * (rel + 1.01 * HB))[:, None])
+        e = (e + 2.0 ** -126 * 8e13) / T              # (entries that the scratch's range drops)
+        want /= T
+        mag = want.abs() + e
+        got = gh.double()
+        ref = want @ W.double()
+        bound = e @ W.double().abs() + acc(V) * (mag @ W.double().abs()) + 1.01 * HB * ref.abs()
+        over = (got - ref).abs() / bound
+        assert (over <= 1).all(), (over.max().item(), torch.nonzero(over > 1)[0].tolist())
