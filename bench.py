@@ -44,9 +44,9 @@ WORKLOAD = "cfg1_qwen3_4b_microbatch: 16 responses x 2048 tokens, V=151936 bf16 
 #   streaming forward kernel: the T = 4096 capture, per token (traffic is proportional to rows);
 #   fused LM-head: every kernel of one forward / one forward + backward call at cfg 3 full size
 #   (one-pass capture of the whole call), per call.
-NCU_TRAFFIC = {"logits_loss_cu_sha1": "fcb111935e9c644afd2910dc4607cb7d124136e3", "dram_bytes_per_token": 606039.0}
-NCU_TRAFFIC_FUSED = {"lmhead_cu_sha1": "9d7f117d29a6b76721e95748be8d98d7d4d21ae5",
-                     "fwd_bytes_per_call": 3841895680.0, "fwd_bwd_bytes_per_call": 32138049024.0}
+NCU_TRAFFIC = {"logits_loss_cu_sha1": "f677834462926bd52c8faddef2c1d875a01aaf90", "dram_bytes_per_token": 606037.0}
+NCU_TRAFFIC_FUSED = {"lmhead_cu_sha1": "fc51f75e5ed9ddb05e9bd12bbeae290302321cf3",
+                     "fwd_bytes_per_call": 3843304192.0, "fwd_bwd_bytes_per_call": 32057314688.0}
 
 
 def _peaks():
@@ -196,7 +196,7 @@ def time_fused_lmhead(rlf, dev, steps, tokens_per_response=0, cfg=3, responses=0
 
 
 # the same for the forward-only log-prob + entropy pass (profiles/logp_entropy_stream_kernel_T4096_ncu_full.md)
-NCU_TRAFFIC_ENTROPY = {"section_sha1": "cbd417db69ba91bea4be00d3c9c3cda5dee7abb9", "dram_bytes_per_token": 305813.0}
+NCU_TRAFFIC_ENTROPY = {"section_sha1": "3a408802c510134819ae4b6adbb1c3f7f1e69f09", "dram_bytes_per_token": 305079.0}
 
 
 def _entropy_section_sha1():
