@@ -77,6 +77,7 @@ typedef enum { RLF_BF16 = 0, RLF_F32 = 1 } rlf_dtype;
 #define RLF_FN_CROSS_ENTROPY 8
 #define RLF_FN_FUSED_CROSS_ENTROPY 9
 #define RLF_FN_FUSED_CROSS_ENTROPY_FWD 10   /* the same call without gradients */
+#define RLF_FN_LINEAR_BWD 11                /* T tokens, V rows of W (2 N when gated), D inputs */
 
 typedef struct CUstream_st *rlf_stream_t;
 
@@ -518,6 +519,66 @@ rlf_status rlf_norm_bwd(const void *grad_y, int64_t grad_y_stride, const void *x
                         void *grad_x, float *grad_weight, float *grad_bias, int accumulate,
                         void *workspace, size_t workspace_bytes, rlf_stream_t stream);
 
+/*
+ * Linear layer with bias, activation and residual: the layers of a block in front of the head, and the value or
+ * reward head of a critic.  (Paper Sec. 2.2: pi_theta is the language model; Sec. 2.3.1: a PPO-style update, whose
+ * values a critic gives; the paper prints no layer, the formulas are the usual ones.)  Per row:
+ *     z = x W^T + bias
+ *     plain  y = act(z) + residual                      W [N, D]
+ *     gated  y = act(z_gate) z_up + residual            W [2 N, D]: the N gate rows first, then the N up rows
+ *     act    RLF_ACT_NONE z;  RELU max(z, 0);  SILU z / (1 + e^-z);  GELU z Phi(z);
+ *            GELU_TANH z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2
+ * Products are bf16 x bf16 with fp32 sums on the tensor cores (which round toward zero); N <= 4 without gate is
+ * summed in plain fp32.  Bias, activation and residual are fp32, y is rounded once.
+ *
+ *   x        [T, D] bf16, row r starts at element r * x_stride (x_stride >= D)
+ *   W        bf16 dense;  D a multiple of 8 (else RLF_ERR_SHAPE);  x and W 16-byte aligned and x_stride a multiple
+ *            of 8 (else RLF_ERR_ALIGN);  any N
+ *   bias     [N] (gated [2 N]) of bias_dt, or NULL
+ *   residual [T, N] y_dt with row stride residual_stride, or NULL;  may be y_out itself when dense
+ *   y_out    [T, N] y_dt dense
+ *   pre_out  [T, N] (gated [T, 2 N]) bf16 dense, or NULL: z, what rlf_linear_bwd takes as pre
+ * Outputs may not overlap inputs or each other otherwise.  Non-finite inputs give what the formulas give, in their
+ * own row only.  T = 0 is valid.  T or D of 2^30 or N of 2^29 and more returns RLF_ERR_UNSUPPORTED.
+ * Waits inside the kernels are bounded: RLF_DEV_TIMEOUT in *dev_status means that the outputs are not valid.
+ */
+#define RLF_ACT_NONE 0
+#define RLF_ACT_RELU 1
+#define RLF_ACT_SILU 2
+#define RLF_ACT_GELU 3
+#define RLF_ACT_GELU_TANH 4
+rlf_status rlf_linear_fwd(const void *x, int64_t T, int32_t D, int64_t x_stride, const void *W, int32_t N,
+                          const void *bias, rlf_dtype bias_dt, int act, int gated, const void *residual,
+                          int64_t residual_stride, void *y_out, rlf_dtype y_dt, void *pre_out,
+                          int32_t *dev_status, rlf_stream_t stream);
+
+/*
+ * Backward of rlf_linear_fwd (the residual's gradient is grad_y itself).  With z = pre:
+ *     plain  gz = grad_y act'(z)
+ *     gated  gz = [ grad_y z_up act'(z_gate),  grad_y act(z_gate) ]
+ *     grad_x = gz W;   grad_W = gz^T x;   grad_bias = sum_t gz
+ * gz enters the two products as bf16 (one rounding; none where it is a bf16 grad_y without activation, or N <= 4
+ * without gate, which is summed in fp32);  grad_bias is summed from the unrounded gz in fp32 in a fixed order.
+ * Results are run-to-run identical.
+ *
+ *   grad_y    [T, N] grad_y_dt with row stride grad_y_stride
+ *   pre       [T, N] (gated [T, 2 N]) bf16 dense from the forward call; not read without activation and gate
+ *   x, W      as in the forward call
+ *   grad_x    [T, D] bf16 dense, 16-byte aligned, or NULL
+ *   grad_W    [N, D] (gated [2 N, D]) grad_W_dt dense, or NULL
+ *   grad_bias [N] (gated [2 N]) fp32, or NULL
+ *   accumulate  != 0: added to grad_W and grad_bias (grad_W in fp32 only, else RLF_ERR_UNSUPPORTED)
+ *   workspace rlf_workspace_bytes(RLF_FN_LINEAR_BWD, T, rows of W, D, RLF_BF16) bytes, 256-byte aligned; contents need
+ *             not be initialised
+ * Outputs may not overlap inputs or each other.  T = 0 is valid (weight gradients are then zero, or unchanged
+ * with accumulate).
+ */
+rlf_status rlf_linear_bwd(const void *grad_y, rlf_dtype grad_y_dt, int64_t grad_y_stride, const void *pre,
+                          const void *x, int64_t T, int32_t D, int64_t x_stride, const void *W, int32_t N, int act,
+                          int gated, void *grad_x, void *grad_W, rlf_dtype grad_W_dt, float *grad_bias,
+                          int accumulate, void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                          rlf_stream_t stream);
+
 /* Bytes of workspace the given entry point needs for these sizes (0 for unknown selectors). */
 size_t rlf_workspace_bytes(int which_fn, int64_t T, int32_t V, int32_t D, rlf_dtype dt);
 
@@ -596,6 +657,12 @@ rlf_status rlf_tune_lmhead_backward(int row_reference, int two_accumulators);
  * itself.  Only loads are delayed, every wait is bounded, and a worker whose wait runs out goes on
  * unpaced.  0: no meeting points.  Results do not depend on it. */
 rlf_status rlf_tune_lmhead_pacing(int on);
+
+/* Form of the linear layer's products for later calls in this process.  form: 1 = pairs of CTAs on 256-row tiles, 2 = the
+ * streamed form for few rows, 0 = chosen per call (built-in).  tile: accumulator columns of a pair's tile (128, 256), or
+ * rows of the streamed form's tile (16 to 256); split: CTAs that share a streamed tile's sum (1, 2, 4, 8); 0 = chosen per
+ * call.  Results agree up to fp32 summation order. */
+rlf_status rlf_tune_linear(int form, int tile, int split);
 
 /* Number of kernels this library has launched in this process (for accounting). */
 int64_t rlf_launch_count(void);

@@ -15,13 +15,13 @@ _LIB_PATH = os.path.join(_HERE, "librlf.so")
 
 RLF_BF16, RLF_F32 = 0, 1
 FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY, FN_NORM_BWD, FN_CROSS_ENTROPY, FN_FUSED_CROSS_ENTROPY = 3, 4, 5, 6, 7, 8, 9
-FN_FUSED_CROSS_ENTROPY_FWD = 10
+FN_FUSED_CROSS_ENTROPY_FWD, FN_LINEAR_BWD = 10, 11
 DEV_BAD_TARGET, DEV_BAD_SEQ, DEV_NONFINITE, DEV_TIMEOUT = 1, 2, 4, 8
 
 EXPORTS = [
     "rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward", "rlf_grpo_logp_loss_fwd_bwd",
-    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
-    "rlf_tune_logits_kernel", "rlf_tune_logits_grid", "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing", "rlf_launch_count", "rlf_status_string", "rlf_version",
+    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_linear_fwd", "rlf_linear_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
+    "rlf_tune_logits_kernel", "rlf_tune_logits_grid", "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing", "rlf_tune_linear", "rlf_launch_count", "rlf_status_string", "rlf_version",
 ]
 
 if not os.path.exists(_LIB_PATH):
@@ -76,12 +76,16 @@ _lib.rlf_fused_lmhead_cross_entropy.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp,
 _lib.rlf_norm_fwd.argtypes = [_vp, _vp, _int, _i64, _i32, _i64, _vp, _vp, _int, _int, _f32, _vp, _vp, _vp, _vp, _vp]
 _lib.rlf_norm_bwd.argtypes = [_vp, _i64, _vp, _i64, _int, _i64, _i32, _vp, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp,
                               _int, _vp, _sz, _vp]
+_lib.rlf_linear_fwd.argtypes = [_vp, _i64, _i32, _i64, _vp, _i32, _vp, _int, _int, _int, _vp, _i64, _vp, _int, _vp, _vp, _vp]
+_lib.rlf_linear_bwd.argtypes = [_vp, _int, _i64, _vp, _vp, _i64, _i32, _i64, _vp, _i32, _int, _int, _vp, _vp, _int, _vp, _int,
+                                _vp, _sz, _vp, _vp]
+_lib.rlf_tune_linear.argtypes = [_int, _int, _int]
 # every entry point that returns an rlf_status
 for _n in ("rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward",
            "rlf_grpo_logp_loss_fwd_bwd", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_grpo_logp_loss_fwd_bwd_skip_masked",
            "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj",
-           "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
-           "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing"):
+           "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_linear_fwd", "rlf_linear_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
+           "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing", "rlf_tune_linear"):
     getattr(_lib, _n).restype = _int
 
 
@@ -166,6 +170,10 @@ def tune_lmhead_pacing(on=1):
 def tune_lmhead_schedule(m_block=0, max_workers=0, chunk_tiles=0):
     _check(_lib.rlf_tune_lmhead_schedule(int(m_block), int(max_workers), int(chunk_tiles)),
            "rlf_tune_lmhead_schedule")
+
+
+def tune_linear(form=0, tile=0, split=0):
+    _check(_lib.rlf_tune_linear(int(form), int(tile), int(split)), "rlf_tune_linear")
 
 
 def rlf_build_loss_mask(ids, cu_seqlens, open_id, close_id, valid=None, mask_out=None, seq_id_out=None,
@@ -679,6 +687,81 @@ def rlf_norm_bwd(grad_y, x, weight, mean, rstd, kind=NORM_RMS, grad_skip=None, w
         _at(grad_skip, here, "grad_skip", dt, shape), xo, _at(grad_weight, here, "grad_weight", _f32, (D,)),
         _at(grad_bias, here, "grad_bias", _f32, (D,)), 1 if accumulate else 0, wp, wn, _raw_stream(here)), "rlf_norm_bwd")
     return grad_x, grad_weight, grad_bias
+
+
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
+
+
+def rlf_linear_fwd(x, W, bias=None, act=ACT_NONE, gated=False, residual=None, out_dtype=None, want_pre=False, y_out=None,
+                   pre_out=None, dev_status=None):
+    """Linear layer with its epilogue: act(x W^T + bias) + residual, or gated, with W's rows the N gate rows and then the
+    N up rows: act(z_gate) z_up + residual.  x [T, D] bf16 (rows may be strided), W [N | 2 N, D] bf16, bias bf16 or fp32.
+    The output's type is out_dtype, or the residual's, or bf16.
+    -> (y [T, N], z bf16 [T, N | 2 N] | None: what rlf_linear_bwd takes as pre, with want_pre)."""
+    here = _device_of(x)
+    xp, xs = _rows(x, here, "x")
+    T, D = x.shape
+    if x.dtype != _bf16:
+        raise TypeError("x must be bfloat16")
+    if W.dim() != 2 or W.shape[1] != D or (gated and W.shape[0] % 2):
+        raise ValueError("W must be [N, %d], gated [2 N, %d]" % (D, D))
+    rows = W.shape[0]
+    N = rows // 2 if gated else rows
+    shape = (T, N)
+    if y_out is None:
+        y_out = x.new_empty(shape, dtype=out_dtype or (_bf16 if residual is None else residual.dtype))
+    elif out_dtype is not None and y_out.dtype != out_dtype:
+        raise TypeError("y_out must be %s" % out_dtype)
+    dt = _dt(y_out, "the output")
+    rp, rs = None, 0
+    if residual is not None:
+        if residual.shape != shape or residual.dtype != y_out.dtype:
+            raise ValueError("residual must have the shape and type of the output")
+        rp, rs = _rows(residual, here, "residual")
+    if pre_out is None and want_pre:
+        pre_out = x.new_empty((T, rows))
+    _check(_lib.rlf_linear_fwd(
+        xp, T, D, xs, _at(W, here, "W", _bf16), N, _at(bias, here, "bias", None, (rows,)), 0 if bias is None else _dt(bias, "bias"),
+        act, 1 if gated else 0, rp, rs, _at(y_out, here, "y_out", None, shape), dt, _at(pre_out, here, "pre_out", _bf16, (T, rows)),
+        _at(dev_status, here, "dev_status", _i32t), _raw_stream(here)), "rlf_linear_fwd")
+    return y_out, pre_out
+
+
+def rlf_linear_bwd(grad_y, x, W, pre=None, act=ACT_NONE, gated=False, want_grad_x=True, want_grad_W=True, want_grad_bias=False,
+                   grad_x=None, grad_W=None, grad_W_dtype=torch.float32, grad_bias=None, accumulate=False, workspace=None,
+                   dev_status=None):
+    """Backward of rlf_linear_fwd; pre is the z it left (needed with an activation or a gate); the residual's gradient is
+    grad_y.  accumulate adds to the buffers given as grad_W (fp32) and grad_bias.
+    -> (grad_x bf16 [T, D] | None, grad_W [N | 2 N, D] | None, grad_bias fp32 [N | 2 N] | None)."""
+    here = _device_of(x)
+    xp, xs = _rows(x, here, "x")
+    T, D = x.shape
+    if x.dtype != _bf16:
+        raise TypeError("x must be bfloat16")
+    if W.dim() != 2 or W.shape[1] != D or (gated and W.shape[0] % 2):
+        raise ValueError("W must be [N, %d], gated [2 N, %d]" % (D, D))
+    rows = W.shape[0]
+    N = rows // 2 if gated else rows
+    if grad_y.shape != (T, N):
+        raise ValueError("grad_y must have shape %s, got %s" % ((T, N), tuple(grad_y.shape)))
+    gp, gs = _rows(grad_y, here, "grad_y")
+    if pre is None and (gated or act != ACT_NONE):
+        raise ValueError("an activation or a gate needs pre, the z of the forward call")
+    if accumulate and ((grad_W is None and want_grad_W) or (grad_bias is None and want_grad_bias)):
+        raise ValueError("accumulate needs the buffers that are added to")
+    if grad_x is None and want_grad_x:
+        grad_x = x.new_empty((T, D))
+    if grad_W is None and want_grad_W:
+        grad_W = x.new_empty((rows, D), dtype=grad_W_dtype)
+    if grad_bias is None and want_grad_bias:
+        grad_bias = x.new_empty(rows, dtype=_f32)
+    workspace, wp, wn = _workspace(workspace, here, x, FN_LINEAR_BWD, T, rows, D, RLF_BF16)
+    _check(_lib.rlf_linear_bwd(
+        gp, _dt(grad_y, "grad_y"), gs, _at(pre, here, "pre", _bf16, (T, rows)), xp, T, D, xs, _at(W, here, "W", _bf16), N, act,
+        1 if gated else 0, _at(grad_x, here, "grad_x", _bf16, (T, D)), _at(grad_W, here, "grad_W", None, (rows, D)),
+        RLF_F32 if grad_W is None else _dt(grad_W, "grad_W"), _at(grad_bias, here, "grad_bias", _f32, (rows,)),
+        1 if accumulate else 0, wp, wn, _at(dev_status, here, "dev_status", _i32t), _raw_stream(here)), "rlf_linear_bwd")
+    return grad_x, grad_W, grad_bias
 
 
 def step_arena_bytes(T, V, B, dt=RLF_BF16):

@@ -1,0 +1,1219 @@
+// Linear layer, forward and backward:
+//
+//   z = x W^T + b;   y = act(z) (+ residual),   or gated, with W's rows in two halves:  y = act(z_gate) z_up (+ residual)
+//   gz = dy act'(z)  (gated: dy z_up act'(z_gate) and dy act(z_gate));   dx = gz W;   dW = gz^T x;   db = sum_t gz
+//
+// All three products are out[m][n] = sum_k A[m][k] B[n][k] on bf16 operands with fp32 accumulation in tensor memory:
+//   y:  A = x,    B = W     (both K-major)
+//   dx: A = gz,   B = W^T   (W is stored with n running along its rows: an N-major operand)
+//   dW: A = gz^T, B = x^T   (both M-/N-major: the tokens, which are summed over, are the rows)
+// and one epilogue serves them: out = act(acc + bias) + residual (accumulation into dW is a residual that is the output itself).
+// Two kernels share it:
+//   pair    large products: a persistent pair of CTAs multiplies 256 x 256 tiles (tcgen05 cta_group::2), bound by the tensor cores;
+//   narrow  few rows (decoding, short batches) or few tiles: the operand with the output's columns is streamed in 128-row tiles
+//           as the M side of the multiplies, the few rows are their N side, and K is cut over a cluster whose CTAs add up their
+//           accumulators through distributed shared memory.  Bound by reading the streamed operand.
+// An output of at most four columns (the values of a critic, a few reward scores) takes no tensor cores: it is bound by
+// reading x, and its sums are plain fp32 ones.
+#include <atomic>
+
+#include "row.cuh"
+#include "umma.cuh"
+
+namespace rlf {
+namespace ln {
+
+using tc::instr_desc;
+using tc::kSlabBytes;
+using tc::make_map;
+using tc::map_to_cta;
+using tc::mbar_arrive_cluster;
+using tc::mbar_expect_tx;
+using tc::mbar_wait;
+using tc::pair_rank;
+using tc::smem_addr;
+using tc::smem_desc;
+using tc::tc_commit;
+using tc::tc_commit2;
+using tc::tc_fence_after;
+using tc::tc_fence_before;
+using tc::tc_ld32;
+using tc::tc_mma;
+using tc::tc_mma2;
+using tc::tma_load_2d;
+using tc::tma_load_2d_pair;
+
+constexpr int kFewOutputs = 4;
+
+// What becomes of an accumulator: out[row][col] = act(acc + bias[col]) (times the up half, when gated) + res[row][col].
+struct Epilogue {
+    int act, gated;
+    int N;                          // output columns
+    const void* bias;               // [N], gated [2 N]; nullable
+    int bias_bf16;
+    const void* res;                // rows of the output's type; nullable
+    long long res_stride;
+    void* out;
+    long long out_stride;
+    int out_f32;
+    __nv_bfloat16* pre;             // acc + bias as bf16, [rows][N], gated [rows][2 N]; nullable
+    long long pre_stride;
+    int vec, vec_pre;               // rows of out and res (of pre) lie on 16-byte boundaries
+};
+
+// ---- activations ------------------------------------------------------------------------------
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 1 / (1 + e^-x); an e^-x beyond fp32 gives 0
+__device__ __forceinline__ float sigmoid(float x) { return rcp_approx(1.0f + ex2_approx(-kLog2e * x)); }
+constexpr float kGeluRoot = 0.7978845608028654f, kGeluCube = 0.044715f, kInvSqrt2Pi = 0.3989422804014327f;
+
+// (the tanh form: 0.5 (1 + tanh u) = sigmoid(2 u))
+template <int ACT> __device__ __forceinline__ float act_value(float z) {
+    if (ACT == RLF_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (ACT == RLF_ACT_SILU) return z * sigmoid(z);
+    if (ACT == RLF_ACT_GELU) return z * normcdff(z);
+    if (ACT == RLF_ACT_GELU_TANH) return z * sigmoid(2.0f * kGeluRoot * z * fmaf(kGeluCube * z, z, 1.0f));
+    return z;
+}
+template <int ACT> __device__ __forceinline__ float act_slope(float z) {
+    if (ACT == RLF_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (ACT == RLF_ACT_SILU) {
+        const float s = sigmoid(z);
+        return s * fmaf(z, 1.0f - s, 1.0f);
+    }
+    if (ACT == RLF_ACT_GELU) return normcdff(z) + z * kInvSqrt2Pi * ex2_approx(-0.5f * kLog2e * z * z);
+    if (ACT == RLF_ACT_GELU_TANH) {
+        const float s = sigmoid(2.0f * kGeluRoot * z * fmaf(kGeluCube * z, z, 1.0f));
+        return s + z * s * (1.0f - s) * 2.0f * kGeluRoot * fmaf(3.0f * kGeluCube * z, z, 1.0f);
+    }
+    return 1.0f;
+}
+template <int ACT, int N> __device__ __forceinline__ void act_all(float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = act_value<ACT>(v[i]);
+}
+template <int N> __device__ __forceinline__ void activate(int act, float (&v)[N]) {
+    switch (act) {
+        case RLF_ACT_RELU: act_all<RLF_ACT_RELU, N>(v); break;
+        case RLF_ACT_SILU: act_all<RLF_ACT_SILU, N>(v); break;
+        case RLF_ACT_GELU: act_all<RLF_ACT_GELU, N>(v); break;
+        case RLF_ACT_GELU_TANH: act_all<RLF_ACT_GELU_TANH, N>(v); break;
+        default: break;
+    }
+}
+__device__ __forceinline__ float slope_of(int act, float z) {
+    switch (act) {
+        case RLF_ACT_RELU: return act_slope<RLF_ACT_RELU>(z);
+        case RLF_ACT_SILU: return act_slope<RLF_ACT_SILU>(z);
+        case RLF_ACT_GELU: return act_slope<RLF_ACT_GELU>(z);
+        case RLF_ACT_GELU_TANH: return act_slope<RLF_ACT_GELU_TANH>(z);
+        default: return 1.0f;
+    }
+}
+__device__ __forceinline__ float value_of(int act, float z) {
+    float v[1] = {z};
+    activate<1>(act, v);
+    return v[0];
+}
+
+__device__ __forceinline__ float load_any(const void* p, int f32, long long i) {
+    return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+__device__ __forceinline__ void store_any(void* p, int f32, long long i, float v) {
+    if (f32) static_cast<float*>(p)[i] = v;
+    else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// ---- large products: pairs of CTAs, 256-row tiles ---------------------------------------------
+constexpr int kBK = 64;
+constexpr int kTileRows = 128;                        // rows of a tile that a CTA holds
+constexpr int kStages = 6;
+constexpr int kABytes = kTileRows * kBK * 2, kBBytes = 128 * kBK * 2, kStageBytes = kABytes + kBBytes;
+constexpr int kDrainWarps = 8;
+constexpr int kPairThreads = 64 + 32 * kDrainWarps;
+constexpr int kDrainPitch = 33;                       // floats per row of a drain staging tile
+constexpr int kDrainBytes = kDrainWarps * 32 * kDrainPitch * 4;
+constexpr int kPairSmem = kStages * kStageBytes + kDrainBytes + 1024 + 256;
+static_assert(kPairSmem <= 227 * 1024, "the most shared memory a CTA can have");
+
+struct PairParams {
+    int M;                          // output rows
+    int m_units, n_tiles, k_slabs;  // 256-row units, column tiles, 64-deep slabs
+    int bn;                         // accumulator columns of a tile (gated: half of them gate, half up)
+    int a_mn, b_mn;                 // operand stored with the summed axis along its rows
+    int group;                      // row units that are taken together (see the raster)
+    int up_row;                     // gated: B's row with which the up half begins
+    Epilogue e;
+    int32_t* dev_status;
+};
+
+struct PairCtl {
+    unsigned long long full[kStages], empty[kStages], tmem_full[2], tmem_empty[2];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+static_assert(sizeof(PairCtl) <= 256, "the barriers have 256 bytes behind the stage ring");
+
+// 32 columns of one row per thread -> memory.  Rows on 16-byte boundaries are stored by their threads; others (and a ragged
+// last piece) go through a staging tile, so that a warp stores 32 columns of a row at a time.  With ADD, res is added.
+template <bool F32>
+__device__ __forceinline__ void store_piece(void* out, long long stride, const void* res, long long res_stride, int row, bool row_ok,
+                                            int M, int col, int nvalid, bool vec, float (&v)[32], float* stage, int lane) {
+    if (vec && nvalid == 32) {
+        if (!row_ok) return;
+        if (F32) {
+            float4* d = reinterpret_cast<float4*>(static_cast<float*>(out) + row * stride + col);
+            if (res) {
+                const float4* r = reinterpret_cast<const float4*>(static_cast<const float*>(res) + row * res_stride + col);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float4 q = r[i];
+                    d[i] = make_float4(v[4 * i] + q.x, v[4 * i + 1] + q.y, v[4 * i + 2] + q.z, v[4 * i + 3] + q.w);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
+        } else {
+            uint4* d = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + row * stride + col);
+            if (res) {
+                const uint4* r = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(res) + row * res_stride + col);
+                uint4 q[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] = r[i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        v[8 * i + 2 * k] += bf_lo(w[k]);
+                        v[8 * i + 2 * k + 1] += bf_hi(w[k]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                d[i] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
+                                  pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) stage[lane * kDrainPitch + i] = v[i];
+    __syncwarp();
+    const int row0 = row - lane, rows = min(32, M - row0);
+    if (lane < nvalid) {
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+            float o = stage[r * kDrainPitch + lane];
+            if (res) o += load_any(res, F32, (long long)(row0 + r) * res_stride + col + lane);
+            store_any(out, F32, (long long)(row0 + r) * stride + col + lane, o);
+        }
+    }
+    __syncwarp();
+}
+
+__global__ void __launch_bounds__(kPairThreads, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const PairParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_addr(smem_raw);
+    const uint32_t ring = (raw + 1023u) & ~1023u;          // operand stages sit on 1024-byte boundaries (swizzle atom)
+    float* drain = reinterpret_cast<float*>(smem_raw + (ring - raw) + kStages * kStageBytes);
+    PairCtl* ctl = reinterpret_cast<PairCtl*>(smem_raw + (ring - raw) + kStages * kStageBytes + kDrainBytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)pair_rank();
+    const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1;
+    const long long units = (long long)p.m_units * p.n_tiles;
+    const int b_rows = p.bn / 2;                           // rows of B that a CTA stages
+    const uint32_t stage_tx = (uint32_t)(kABytes + b_rows * kBK * 2);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(smem_addr(&ctl->full[s]), 1);
+            mbar_init(smem_addr(&ctl->empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_addr(&ctl->tmem_full[b]), 1);
+            mbar_init(smem_addr(&ctl->tmem_empty[b]), 2 * kDrainWarps);
+        }
+        ctl->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(smem_addr(&ctl->tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                    // both CTAs' barriers exist before either signals the other
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+
+    // Raster: groups of row units; inside a group row units fastest, so that the workers running at one time cover a block of
+    // about as many rows as columns and share both operands through L2.
+    auto unit_at = [&](long long u, int& m, int& n) {
+        const long long per_group = (long long)p.group * p.n_tiles;
+        const int g = (int)(u / per_group);
+        const int within = (int)(u - g * per_group), rows_here = min(p.group, p.m_units - g * p.group);
+        n = within / rows_here;
+        m = g * p.group + (within - n * rows_here);
+    };
+
+    if (warp == 0) {
+        // ---------------- loads (each CTA its own rows of A and half of B) ----------------
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (long long u = worker; u < units && ok; u += workers) {
+                int m, n;
+                unit_at(u, m, n);
+                const int a_row = (2 * m + rank) * kTileRows;
+                const int b_row = p.e.gated ? (rank ? p.up_row : 0) + n * b_rows : n * p.bn + rank * b_rows;
+                for (int kb = 0; kb < p.k_slabs; ++kb) {
+                    if (!mbar_wait(smem_addr(&ctl->empty[stage]), phase ^ 1u, &ctl->abort_flag)) { ok = false; break; }
+                    const uint32_t own = smem_addr(&ctl->full[stage]), bar = map_to_cta(own, 0);   // the leader's barrier
+                    const uint32_t sa = ring + stage * kStageBytes, sb = sa + kABytes;
+                    if (rank == 0) mbar_expect_tx(own, 2 * stage_tx);
+                    if (!p.a_mn) {
+                        tma_load_2d_pair(sa, &map_a, bar, kb * kBK, a_row);
+                    } else {
+                        for (int j = 0; j < kTileRows / 64; ++j) tma_load_2d_pair(sa + j * kSlabBytes, &map_a, bar, a_row + j * 64, kb * kBK);
+                    }
+                    if (!p.b_mn) {
+                        tma_load_2d_pair(sb, &map_b, bar, kb * kBK, b_row);
+                    } else {
+                        for (int j = 0; j < b_rows / 64; ++j) tma_load_2d_pair(sb + j * kSlabBytes, &map_b, bar, b_row + j * 64, kb * kBK);
+                    }
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- multiplies (one thread of the leader CTA) ----------------
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = instr_desc(p.a_mn, p.b_mn, 2 * kTileRows, p.bn);
+            const uint32_t a_step = p.a_mn ? (16 * 128) >> 4 : 32 >> 4, b_step = p.b_mn ? (16 * 128) >> 4 : 32 >> 4;
+            int stage = 0, buf = 0;
+            uint32_t phase = 0, tphase[2] = {0, 0};
+            bool ok = true;
+            for (long long u = worker; u < units && ok; u += workers) {
+                if (!mbar_wait(smem_addr(&ctl->tmem_empty[buf]), tphase[buf] ^ 1u, &ctl->abort_flag)) break;
+                tc_fence_after();
+                const uint32_t d = tmem_base + (uint32_t)buf * 256u;
+                for (int kb = 0; kb < p.k_slabs; ++kb) {
+                    if (!mbar_wait(smem_addr(&ctl->full[stage]), phase, &ctl->abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sa = ring + stage * kStageBytes;
+                    const uint64_t ad = smem_desc(sa, p.a_mn), bd = smem_desc(sa + kABytes, p.b_mn);
+#pragma unroll
+                    for (int k = 0; k < kBK / 16; ++k)
+                        tc_mma2(d, ad + (uint64_t)(k * a_step), bd + (uint64_t)(k * b_step), idesc, (kb | k) ? 1u : 0u);
+                    tc_commit2(smem_addr(&ctl->empty[stage]));       // frees the stage in both CTAs when these retire
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                }
+                if (!ok) break;
+                tc_commit2(smem_addr(&ctl->tmem_full[buf]));
+                tphase[buf] ^= 1u;
+                buf ^= 1;
+            }
+        }
+    } else {
+        // ---------------- epilogue: one row per thread, two warps share a row's 32-column pieces ----------------
+        const Epilogue& e = p.e;
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        float* stage = drain + (warp - 2) * 32 * kDrainPitch;
+        const int width = e.gated ? p.bn / 2 : p.bn;
+        int buf = 0;
+        uint32_t tphase[2] = {0, 0};
+        for (long long u = worker; u < units; u += workers) {
+            int m, n;
+            unit_at(u, m, n);
+            const int row = (2 * m + rank) * kTileRows + quarter * 32 + lane;
+            const bool row_ok = row < p.M;
+            int got = 0;
+            if (lane == 0) got = mbar_wait(smem_addr(&ctl->tmem_full[buf]), tphase[buf], &ctl->abort_flag) ? 1 : 0;
+            if (!__shfl_sync(0xffffffffu, got, 0)) break;
+            tc_fence_after();
+            const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)buf * 256u;
+#pragma unroll 1
+            for (int c = half; c < width / 32; c += 2) {
+                const int col = n * width + c * 32;
+                if (col >= e.N) break;                     // (warp-uniform)
+                const int nvalid = min(32, e.N - col);
+                uint32_t raw_v[32];
+                float v[32];
+                auto take = [&](uint32_t at, int shift) {  // accumulator columns + bias
+                    tc_ld32(t_row + at, raw_v);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw_v[i]);
+                    if (e.bias) {
+                        stage[lane] = lane < nvalid ? load_any(e.bias, !e.bias_bf16, shift + col + lane) : 0.0f;
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] += stage[i];
+                        __syncwarp();
+                    }
+                    if (e.pre) {
+                        float w[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) w[i] = v[i];
+                        store_piece<false>(e.pre + shift, e.pre_stride, nullptr, 0, row, row_ok, p.M, col, nvalid, e.vec_pre, w, stage, lane);
+                    }
+                };
+                take((uint32_t)(c * 32), 0);
+                activate<32>(e.act, v);
+                if (e.gated) {
+                    float g[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) g[i] = v[i];
+                    take((uint32_t)(width + c * 32), e.N);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] *= g[i];
+                }
+                if (e.out_f32) store_piece<true>(e.out, e.out_stride, e.res, e.res_stride, row, row_ok, p.M, col, nvalid, e.vec, v, stage, lane);
+                else store_piece<false>(e.out, e.out_stride, e.res, e.res_stride, row, row_ok, p.M, col, nvalid, e.vec, v, stage, lane);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_addr(&ctl->tmem_empty[buf]), 0));
+            tphase[buf] ^= 1u;
+            buf ^= 1;
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (ctl->abort_flag) {
+        // copies or multiplies may still be in flight: give them time before the memory is released
+        if (threadIdx.x == 0 && p.dev_status) atomicOr(p.dev_status, RLF_DEV_TIMEOUT);
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
+    cluster_sync_all();                                    // the peer may still be signalling this CTA's barriers until here
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(512u) : "memory");
+    }
+}
+
+// ---- few rows, or few tiles: the streamed form -------------------------------------------------
+// out[j][i] = sum_k S[i][k] F[j][k]: S is streamed in tiles of 128 i (gated: 64 gate rows and the 64 up rows that belong to them),
+// F's rows j, up to 256 in a tile, are the N side.  A cluster of `split` CTAs takes one tile, each a part of K.
+// Tensor memory: a CTA takes nn / 512 of it (at least 32 columns) and more than that share of the shared memory, in every
+// shape below, so that CTAs which are on an SM together never wait for one another's columns.
+constexpr int kNarrowThreads = 192;
+constexpr int kNarrowPitch = 132;                     // floats between two j of the staged accumulator
+constexpr int kMaxNarrowStages = 12;
+
+struct NarrowParams {
+    int J;                          // output rows
+    int k_slabs, nn, stages;
+    int s_mn, f_mn;                 // operand stored with the summed axis along its rows
+    int up_row;
+    Epilogue e;
+    int32_t* dev_status;
+};
+struct NarrowCtl {
+    unsigned long long full[kMaxNarrowStages], empty[kMaxNarrowStages], tmem_full;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+static_assert(sizeof(NarrowCtl) <= 256, "the barriers have 256 bytes behind the stage ring");
+
+__host__ __device__ constexpr int narrow_stage_bytes(int nn) { return kABytes + nn * kBK * 2; }
+__host__ __device__ constexpr int narrow_ring_bytes(int nn, int stages) {
+    const int r = stages * narrow_stage_bytes(nn), staged = nn * kNarrowPitch * 4;
+    return r > staged ? r : (staged + 255) / 256 * 256;
+}
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t local_addr, uint32_t rank) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(map_to_cta(local_addr, rank)) : "memory");
+    return v;
+}
+// four columns of a row: bias, then `pre`
+__device__ __forceinline__ void narrow_bias_pre(const Epilogue& e, int row, int col, int nvalid, int shift, float (&z)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (e.bias && k < nvalid) z[k] += load_any(e.bias, !e.bias_bf16, shift + col + k);
+    if (e.pre) {
+        __nv_bfloat16* d = e.pre + row * e.pre_stride + shift + col;
+        if (e.vec_pre && nvalid == 4) {
+            *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < nvalid) d[k] = __float2bfloat16_rn(z[k]);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kNarrowThreads)
+linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_f, const NarrowParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_addr(smem_raw);
+    const uint32_t ring = (raw + 1023u) & ~1023u;
+    float* staged = reinterpret_cast<float*>(smem_raw + (ring - raw));
+    const int stage_bytes = narrow_stage_bytes(p.nn);
+    NarrowCtl* ctl = reinterpret_cast<NarrowCtl*>(smem_raw + (ring - raw) + narrow_ring_bytes(p.nn, p.stages));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
+    const int it = blockIdx.x / split, jt = blockIdx.y;
+    const int k0 = (int)((long long)p.k_slabs * rank / split), k1 = (int)((long long)p.k_slabs * (rank + 1) / split);
+    const uint32_t columns = p.nn < 32 ? 32u : (uint32_t)p.nn;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(smem_addr(&ctl->full[s]), 1);
+            mbar_init(smem_addr(&ctl->empty[s]), 1);
+        }
+        mbar_init(smem_addr(&ctl->tmem_full), 1);
+        ctl->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(smem_addr(&ctl->tmem_base)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            const int i0 = p.e.gated ? it * 64 : it * 128, i1 = p.e.gated ? p.up_row + i0 : i0 + 64;
+            for (int kb = k0; kb < k1; ++kb) {
+                if (!mbar_wait(smem_addr(&ctl->empty[stage]), phase ^ 1u, &ctl->abort_flag)) break;
+                const uint32_t bar = smem_addr(&ctl->full[stage]);
+                const uint32_t ss = ring + stage * stage_bytes, sf = ss + kABytes;
+                mbar_expect_tx(bar, (uint32_t)stage_bytes);
+                if (p.s_mn) {
+                    tma_load_2d(ss, &map_s, bar, i0, kb * kBK);
+                    tma_load_2d(ss + kSlabBytes, &map_s, bar, i1, kb * kBK);
+                } else {
+                    tma_load_2d(ss, &map_s, bar, kb * kBK, i0);
+                    tma_load_2d(ss + kSlabBytes, &map_s, bar, kb * kBK, i1);
+                }
+                if (p.f_mn) {
+                    for (int j = 0; j < p.nn / 64; ++j) tma_load_2d(sf + j * kSlabBytes, &map_f, bar, jt * p.nn + j * 64, kb * kBK);
+                } else {
+                    tma_load_2d(sf, &map_f, bar, kb * kBK, jt * p.nn);
+                }
+                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = instr_desc(p.s_mn, p.f_mn, 128, p.nn);
+            const uint32_t s_step = p.s_mn ? (16 * 128) >> 4 : 32 >> 4, f_step = p.f_mn ? (16 * 128) >> 4 : 32 >> 4;
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int kb = k0; kb < k1; ++kb) {
+                if (!mbar_wait(smem_addr(&ctl->full[stage]), phase, &ctl->abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t ss = ring + stage * stage_bytes;
+                const uint64_t sd = smem_desc(ss, p.s_mn), fd = smem_desc(ss + kABytes, p.f_mn);
+#pragma unroll
+                for (int k = 0; k < kBK / 16; ++k)
+                    tc_mma(tmem_base, sd + (uint64_t)(k * s_step), fd + (uint64_t)(k * f_step), idesc, (kb > k0 || k) ? 1u : 0u);
+                tc_commit(smem_addr(&ctl->empty[stage]));
+                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+            }
+            if (ok) tc_commit(smem_addr(&ctl->tmem_full));
+        }
+    } else {
+        // the accumulator goes to shared memory as [j][i] (the ring's memory: every copy has been multiplied by then)
+        int got = 0;
+        if (lane == 0) got = mbar_wait(smem_addr(&ctl->tmem_full), 0, &ctl->abort_flag) ? 1 : 0;
+        if (__shfl_sync(0xffffffffu, got, 0)) {
+            tc_fence_after();
+            const int i = (warp & 3) * 32 + lane;
+#pragma unroll 1
+            for (int c = 0; c < p.nn; c += 32) {
+                uint32_t v[32];
+                tc_ld32(tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c, v);
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (c + j < p.nn) staged[(c + j) * kNarrowPitch + i] = __uint_as_float(v[j]);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (ctl->abort_flag) {
+        if (threadIdx.x == 0 && p.dev_status) atomicOr(p.dev_status, RLF_DEV_TIMEOUT);
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
+    cluster_sync_all();                                    // every CTA's part is staged
+    // the tile's rows j are dealt over the cluster; parts are added in rank order
+    const Epilogue& e = p.e;
+    const int rows = min(p.nn, p.J - jt * p.nn);
+    const int j0 = rows * rank / split, j1 = rows * (rank + 1) / split;
+    const int groups = e.gated ? 16 : 32;                  // of four columns
+    const uint32_t base = smem_addr(staged);
+    for (int x = threadIdx.x; x < (j1 - j0) * groups; x += kNarrowThreads) {
+        const int j = j0 + x / groups, g = x % groups;
+        const int row = jt * p.nn + j, col = it * 4 * groups + 4 * g;
+        const int nvalid = min(4, e.N - col);
+        if (nvalid <= 0) continue;
+        float z[4] = {0.0f, 0.0f, 0.0f, 0.0f}, up[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const uint32_t at = base + (uint32_t)(j * kNarrowPitch + 4 * g) * 4u;
+#pragma unroll 4
+        for (int q = 0; q < split; ++q) {
+            const float4 a = ld_cluster_f4(at, (uint32_t)q);
+            z[0] += a.x; z[1] += a.y; z[2] += a.z; z[3] += a.w;
+            if (e.gated) {
+                const float4 b = ld_cluster_f4(at + 256u, (uint32_t)q);
+                up[0] += b.x; up[1] += b.y; up[2] += b.z; up[3] += b.w;
+            }
+        }
+        narrow_bias_pre(e, row, col, nvalid, 0, z);
+        activate<4>(e.act, z);
+        if (e.gated) {
+            narrow_bias_pre(e, row, col, nvalid, e.N, up);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] *= up[k];
+        }
+        const long long o = row * e.out_stride + col, ro = row * e.res_stride + col;
+        if (e.vec && nvalid == 4) {
+            if (e.out_f32) {
+                if (e.res) {
+                    const float4 r = *reinterpret_cast<const float4*>(static_cast<const float*>(e.res) + ro);
+                    z[0] += r.x; z[1] += r.y; z[2] += r.z; z[3] += r.w;
+                }
+                *reinterpret_cast<float4*>(static_cast<float*>(e.out) + o) = make_float4(z[0], z[1], z[2], z[3]);
+            } else {
+                if (e.res) {
+                    const uint2 r = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(e.res) + ro);
+                    z[0] += bf_lo(r.x); z[1] += bf_hi(r.x); z[2] += bf_lo(r.y); z[3] += bf_hi(r.y);
+                }
+                *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(e.out) + o) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < nvalid) {
+                    if (e.res) z[k] += load_any(e.res, e.out_f32, ro + k);
+                    store_any(e.out, e.out_f32, o + k, z[k]);
+                }
+        }
+    }
+    cluster_sync_all();                                    // the others have read this CTA's part
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(columns) : "memory");
+    }
+}
+
+// ---- at most four outputs ------------------------------------------------------------------------
+// Forward: a warp takes R tokens; its lanes run along the row, 16 bytes of x and of each weight row at a time.
+template <int N, int R>
+__global__ void __launch_bounds__(256)
+linear_few_fwd_kernel(const __nv_bfloat16* __restrict__ x, long long x_stride, const __nv_bfloat16* __restrict__ W, long long T, int D, const Epilogue e) {
+    const int lane = threadIdx.x & 31;
+    const long long t0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * R;
+    if (t0 >= T) return;
+    const int nvec = D / 8;
+    const uint4* xr[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) xr[r] = reinterpret_cast<const uint4*>(x + min(t0 + r, T - 1) * x_stride);
+    f2 acc[R][N];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int n = 0; n < N; ++n) acc[r][n] = 0ull;
+#pragma unroll(R == 1 ? 4 : 2)
+    for (int c = lane; c < nvec; c += 32) {
+        uint4 xv[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) xv[r] = xr[r][c];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint4 wv = reinterpret_cast<const uint4*>(W + (long long)n * D)[c];
+            const uint32_t w[4] = {wv.x, wv.y, wv.z, wv.w};
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const uint32_t q[4] = {xv[r].x, xv[r].y, xv[r].z, xv[r].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[r][n] = f2_fma(f2_make(bf_lo(q[k]), bf_hi(q[k])), f2_make(bf_lo(w[k]), bf_hi(w[k])), acc[r][n]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const float s = warp_sum(f2_sum(acc[r][n]));
+            const long long t = t0 + r;
+            if (lane != (r * N + n) % 32 || t >= T) continue;
+            const float z = s + (e.bias ? load_any(e.bias, !e.bias_bf16, n) : 0.0f);
+            if (e.pre) e.pre[t * e.pre_stride + n] = __float2bfloat16_rn(z);
+            float y = value_of(e.act, z);
+            if (e.res) y += load_any(e.res, e.out_f32, t * e.res_stride + n);
+            store_any(e.out, e.out_f32, t * e.out_stride + n, y);
+        }
+}
+
+struct FewBwd {
+    const void* dy;
+    long long dy_stride;
+    int dy_f32, act;
+    const __nv_bfloat16* pre;       // [T, N], nullable
+    const __nv_bfloat16* x;
+    long long x_stride;
+    const __nv_bfloat16* W;         // [N, D]
+    __nv_bfloat16* dx;              // [T, D], nullable
+    float* part_w;                  // [slices][N][D], nullable
+    float* part_b;                  // [slices][N], nullable
+    long long T, rows;              // tokens, tokens of a slice
+    int D;
+};
+// Backward: a CTA takes a slice of tokens and up to 2048 columns, eight to a thread (threadIdx.x); threadIdx.y deals the tokens.
+// x is read and dx written once; the sums over tokens leave as one partial row per slice.
+constexpr int kFewChunk = 64;                         // tokens whose gz is worked out at a time
+template <int N>
+__global__ void __launch_bounds__(256)
+linear_few_bwd_kernel(const FewBwd p) {
+    __shared__ float gz[kFewChunk][N];
+    __shared__ float sum[256][9];
+    const int tx = threadIdx.x, ty = threadIdx.y, nx = blockDim.x, ny = blockDim.y, tid = ty * nx + tx;
+    const int col = (blockIdx.x * nx + tx) * 8;
+    const bool live = col < p.D;
+    const long long t0 = (long long)blockIdx.y * p.rows, t1 = min(p.T, t0 + p.rows);
+    f2 w[N][4], acc[N][4];
+    float bias[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (live) v = *reinterpret_cast<const uint4*>(p.W + (long long)n * p.D + col);
+        const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+        bias[n] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            w[n][k] = f2_make(bf_lo(q[k]), bf_hi(q[k]));
+            acc[n][k] = 0ull;
+        }
+    }
+    for (long long tc0 = t0; tc0 < t1; tc0 += kFewChunk) {
+        const int tokens = (int)min((long long)kFewChunk, t1 - tc0);
+        __syncthreads();
+        for (int i = tid; i < tokens * N; i += 256) {
+            const int r = i / N, n = i - r * N;
+            float g = load_any(p.dy, p.dy_f32, (tc0 + r) * p.dy_stride + n);
+            if (p.pre) g *= slope_of(p.act, __bfloat162float(p.pre[(tc0 + r) * N + n]));
+            gz[r][n] = g;
+        }
+        __syncthreads();
+        if (p.part_b && blockIdx.x == 0 && tid == 0)
+            for (int r = 0; r < tokens; ++r)
+#pragma unroll
+                for (int n = 0; n < N; ++n) bias[n] += gz[r][n];
+        if (!live) continue;
+#pragma unroll 4
+        for (int r = ty; r < tokens; r += ny) {
+            const long long t = tc0 + r;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (p.part_w) v = *reinterpret_cast<const uint4*>(p.x + t * p.x_stride + col);
+            const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+            f2 d[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const f2 g = f2_make(gz[r][n], gz[r][n]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    acc[n][k] = f2_fma(g, f2_make(bf_lo(q[k]), bf_hi(q[k])), acc[n][k]);
+                    d[k] = f2_fma(g, w[n][k], d[k]);
+                }
+            }
+            if (p.dx) {
+                uint32_t o[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float a, b;
+                    f2_split(d[k], a, b);
+                    o[k] = pack_bf16x2(a, b);
+                }
+                *reinterpret_cast<uint4*>(p.dx + t * p.D + col) = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+        }
+    }
+    if (p.part_b && blockIdx.x == 0 && tid == 0)
+#pragma unroll
+        for (int n = 0; n < N; ++n) p.part_b[(long long)blockIdx.y * N + n] = bias[n];
+    if (!p.part_w) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f2_split(acc[n][k], f[2 * k], f[2 * k + 1]);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[tid][k] = f[k];
+        __syncthreads();
+        if (ty == 0 && live) {
+            for (int y = 1; y < ny; ++y)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) f[k] += sum[y * nx + tx][k];
+            float4* d = reinterpret_cast<float4*>(p.part_w + ((long long)blockIdx.y * N + n) * p.D + col);
+            d[0] = make_float4(f[0], f[1], f[2], f[3]);
+            d[1] = make_float4(f[4], f[5], f[6], f[7]);
+        }
+    }
+}
+
+// partial rows -> sum, in a fixed order.  A CTA covers 32 columns; warp w adds the rows w, w + 32, ..., and the 32 sums in order.
+__global__ void __launch_bounds__(1024)
+linear_join_kernel(const float* __restrict__ part, int parts, long long width, int accumulate, void* out, int out_f32) {
+    __shared__ float acc[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long col = (long long)blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (col < width) {
+#pragma unroll 4
+        for (int k = warp; k < parts; k += 32) s += part[(long long)k * width + col];
+    }
+    acc[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && col < width) {
+        for (int w = 1; w < 32; ++w) s += acc[w][lane];
+        if (accumulate) s += load_any(out, out_f32, col);
+        store_any(out, out_f32, col, s);
+    }
+}
+
+// ---- gradient before the activation --------------------------------------------------------------
+struct PreGrad {
+    const void* dy;
+    long long dy_stride;
+    int dy_f32, act, gated;
+    const __nv_bfloat16* pre;       // [T, N], gated [T, 2 N]; nullable
+    __nv_bfloat16* gz;              // rows of gz_stride; nullable (only the bias gradient is wanted)
+    long long gz_stride;
+    float* part_b;                  // [slices][N], gated [slices][2 N]; nullable
+    long long T, rows;              // tokens, tokens of a slice
+    int N;
+};
+// gz in bf16 (the products' operand: its one rounding) and, in fp32 and unrounded, its sums over a slice of tokens.  A thread keeps V
+// columns; threadIdx.y deals the tokens.  V = 8: rows on 16-byte boundaries; 1: any.
+template <int V, int ACT, bool GATED>
+__global__ void __launch_bounds__(256)
+linear_pregrad_kernel(const PreGrad p) {
+    __shared__ float sum[8][32 * V + 1];
+    const int tx = threadIdx.x, ty = threadIdx.y;          // 32 x 8
+    const int col = (blockIdx.x * 32 + tx) * V;
+    const long long t0 = (long long)blockIdx.y * p.rows, t1 = min(p.T, t0 + p.rows);
+    constexpr int H = GATED ? 2 : 1;
+    float acc[H][V];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int k = 0; k < V; ++k) acc[h][k] = 0.0f;
+    const bool with_pre = ACT != RLF_ACT_NONE || GATED;
+    if (col < p.N) {
+#pragma unroll 2
+        for (long long t = t0 + ty; t < t1; t += 8) {
+            float g[V], z[H][V], o[H][V];
+            if constexpr (V == 8) {
+                if (p.dy_f32) {
+                    const float4* d = reinterpret_cast<const float4*>(static_cast<const float*>(p.dy) + t * p.dy_stride + col);
+                    const float4 a = d[0], b = d[1];
+                    g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w; g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
+                } else {
+                    const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.dy) + t * p.dy_stride + col);
+                    const uint32_t q[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) { g[2 * k] = bf_lo(q[k]); g[2 * k + 1] = bf_hi(q[k]); }
+                }
+                if (with_pre) {
+#pragma unroll
+                    for (int h = 0; h < H; ++h) {
+                        const uint4 a = *reinterpret_cast<const uint4*>(p.pre + (t * H + h) * p.N + col);
+                        const uint32_t q[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) { z[h][2 * k] = bf_lo(q[k]); z[h][2 * k + 1] = bf_hi(q[k]); }
+                    }
+                }
+            } else {
+                g[0] = load_any(p.dy, p.dy_f32, t * p.dy_stride + col);
+                if (with_pre)
+#pragma unroll
+                    for (int h = 0; h < H; ++h) z[h][0] = __bfloat162float(p.pre[(t * H + h) * p.N + col]);
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                if (GATED) {
+                    o[0][k] = g[k] * z[H - 1][k] * act_slope<ACT>(z[0][k]);
+                    o[H - 1][k] = g[k] * act_value<ACT>(z[0][k]);
+                } else {
+                    o[0][k] = ACT == RLF_ACT_NONE ? g[k] : g[k] * act_slope<ACT>(z[0][k]);
+                }
+#pragma unroll
+                for (int h = 0; h < H; ++h) acc[h][k] += o[h][k];
+            }
+            if (p.gz) {
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    __nv_bfloat16* d = p.gz + t * p.gz_stride + (long long)h * p.N + col;
+                    if constexpr (V == 8)
+                        *reinterpret_cast<uint4*>(d) = make_uint4(pack_bf16x2(o[h][0], o[h][1]), pack_bf16x2(o[h][2], o[h][3]),
+                                                                  pack_bf16x2(o[h][4], o[h][5]), pack_bf16x2(o[h][6], o[h][7]));
+                    else
+                        d[0] = __float2bfloat16_rn(o[h][0]);
+                }
+            }
+        }
+    }
+    if (!p.part_b) return;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < V; ++k) sum[ty][tx * V + k] = acc[h][k];
+        __syncthreads();
+        const int first = blockIdx.x * 32 * V;
+        for (int c = ty * 32 + tx; c < 32 * V && first + c < p.N; c += 256) {
+            float s = 0.0f;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) s += sum[y][c];
+            p.part_b[((long long)blockIdx.y * H + h) * p.N + first + c] = s;
+        }
+    }
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+static int sm_count() {
+    static ResidentTable table;
+    return table.get(nullptr, 0, 0, [](int dev) {
+        int v = 0;
+        cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev);
+        return v > 0 ? v : 148;
+    });
+}
+
+// form of the products for later calls (rlf_tune_linear); 0: chosen per call
+static std::atomic<int> g_form{0}, g_tile{0}, g_split{0};
+
+// an operand with `rows` output rows (columns): [rows][K] row-major, or with mn [K][rows] row-major
+struct Operand {
+    const void* at;
+    long long stride;
+    int mn;
+};
+
+struct Plan {
+    bool narrow;
+    int tile;                       // pair: accumulator columns; narrow: rows of a tile
+    int split;                      // narrow: CTAs that share a tile's K
+};
+static int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+static int narrow_split(long long tiles, int k_slabs, int sms) {
+    int split = 1;
+    while (split < 8 && tiles * split < 2ll * sms && k_slabs >= 8 * split) split *= 2;
+    return split;
+}
+static Plan choose(long long M, int N, int k_slabs, bool gated, bool f_mn, bool s_mn) {
+    const int sms = sm_count();
+    const int cols = gated ? 64 : 128;
+    Plan q = {false, 256, 1};
+    const int form = g_form.load(), tile = g_tile.load(), split = g_split.load();
+    const bool few = form == 2 || (form == 0 && M <= 256);
+    const int tile_cols = gated ? 128 : 256;
+    const long long units = (long long)div_up(M, 256) * div_up(N, tile_cols);
+    if (few) {
+        q.narrow = true;
+        q.tile = f_mn ? 64 : 16;
+        while (q.tile < M && q.tile < 256) q.tile *= 2;
+        if (tile > 0 && (tile == 16 || tile == 32 || tile == 64 || tile == 128 || tile == 256) && (!f_mn || tile >= 64)) q.tile = tile;
+        q.split = split > 0 ? split : narrow_split((long long)div_up(N, cols) * div_up(M, q.tile), k_slabs, sms);
+        if (q.split > k_slabs) q.split = k_slabs >= 4 ? 4 : k_slabs >= 2 ? 2 : 1;      // (every CTA has a part of K)
+    } else {
+        if (units < sms / 2) q.tile = 128;
+        if (tile == 128 || tile == 256) q.tile = tile;
+    }
+    (void)s_mn;
+    return q;
+}
+
+static bool opt_in(const void* kernel, int bytes) {
+    static ResidentTable table;
+    return table.get(kernel, 0, 0, [&](int) {
+        const bool ok = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+        if (!ok) cudaGetLastError();
+        return ok ? 1 : 0;
+    }) == 1;
+}
+
+static rlf_status launch_cluster(void* kernel, dim3 grid, int threads, int smem, int cluster, const CUtensorMap& a, const CUtensorMap& b,
+                                 const void* params, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    void* args[] = {const_cast<CUtensorMap*>(&a), const_cast<CUtensorMap*>(&b), const_cast<void*>(params)};
+    if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) {
+        cudaGetLastError();
+        return RLF_ERR_CUDA;
+    }
+    count_launch();
+    return RLF_OK;
+}
+
+// out[m][n] = epilogue(sum_k A[m][k] B[n][k]), M rows, e.N columns (gated: B has 2 e.N rows), K terms
+static rlf_status product(const Operand& A, const Operand& B, long long M, long long K, const Epilogue& e, int32_t* dev_status, cudaStream_t s) {
+    const int rows_b = e.gated ? 2 * e.N : e.N;
+    const int k_slabs = div_up(K, kBK);
+    const Plan plan = choose(M, e.N, k_slabs, e.gated, A.mn, B.mn);
+    CUtensorMap ma, mb;
+    auto encode = [&](CUtensorMap* map, const Operand& o, long long rows, int box_rows) {
+        return o.mn ? make_map(map, o.at, (uint64_t)K, (uint64_t)rows, (uint64_t)o.stride, 64, 64)
+                    : make_map(map, o.at, (uint64_t)rows, (uint64_t)K, (uint64_t)o.stride, 64, (uint32_t)box_rows);
+    };
+    if (plan.narrow) {
+        NarrowParams p = {};
+        p.J = (int)M; p.k_slabs = k_slabs; p.nn = plan.tile; p.s_mn = B.mn; p.f_mn = A.mn; p.up_row = e.N; p.e = e; p.dev_status = dev_status;
+        const int per_cta = plan.tile <= 128 ? 112 * 1024 : 220 * 1024;       // two CTAs per SM while the tile is small
+        p.stages = (per_cta - 1024 - 256) / narrow_stage_bytes(plan.tile);
+        if (p.stages > kMaxNarrowStages) p.stages = kMaxNarrowStages;
+        const int smem = narrow_ring_bytes(plan.tile, p.stages) + 1024 + 256;
+        if (!encode(&mb, B, rows_b, 64) || !encode(&ma, A, M, plan.tile)) return RLF_ERR_CUDA;
+        if (!opt_in((const void*)linear_narrow_kernel, 227 * 1024)) return RLF_ERR_CUDA;
+        const int i_tiles = div_up(e.N, e.gated ? 64 : 128), j_tiles = div_up(M, plan.tile);
+        return launch_cluster((void*)linear_narrow_kernel, dim3((unsigned)(i_tiles * plan.split), (unsigned)j_tiles), kNarrowThreads, smem,
+                              plan.split, mb, ma, &p, s);
+    }
+    PairParams p = {};
+    p.M = (int)M; p.m_units = div_up(M, 2 * kTileRows); p.k_slabs = k_slabs; p.bn = plan.tile;
+    p.n_tiles = div_up(e.N, e.gated ? plan.tile / 2 : plan.tile);
+    p.a_mn = A.mn; p.b_mn = B.mn; p.up_row = e.N; p.e = e; p.dev_status = dev_status;
+    p.group = 8;
+    if (!encode(&ma, A, M, kTileRows) || !encode(&mb, B, rows_b, plan.tile / 2)) return RLF_ERR_CUDA;
+    if (!opt_in((const void*)linear_pair_kernel, kPairSmem)) return RLF_ERR_CUDA;
+    const long long units = (long long)p.m_units * p.n_tiles;
+    const int pairs = sm_count() / 2;
+    const int workers = units < pairs ? (int)units : pairs;
+    return launch_cluster((void*)linear_pair_kernel, dim3((unsigned)(2 * workers)), kPairThreads, kPairSmem, 2, ma, mb, &p, s);
+}
+
+static bool rows_aligned(const void* at, long long stride, int esz) { return aligned(at, 16) && stride * esz % 16 == 0; }
+
+// slices of tokens of the elementwise passes (each leaves one partial row of a weight or bias gradient)
+static int token_slices(int64_t T) {
+    const int64_t n = (T + 31) / 32;
+    return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
+}
+static long long up8(long long n) { return (n + 7) & ~7ll; }
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+struct BwdWs { size_t gz, part_b, part_w, total; };
+static BwdWs bwd_workspace(int64_t T, int32_t rows, int32_t D) {
+    BwdWs w;
+    size_t o = 0;
+    const size_t slices = (size_t)token_slices(T);
+    w.gz = o;     o += rows <= kFewOutputs ? 0 : up256((size_t)T * (size_t)up8(rows) * 2);
+    w.part_b = o; o += up256(slices * (size_t)rows * 4);
+    w.part_w = o; o += rows <= kFewOutputs ? up256(slices * (size_t)rows * (size_t)D * 4) : 0;
+    w.total = o;
+    return w;
+}
+
+static rlf_status check_linear(int64_t T, int32_t D, int32_t N, int act, int gated) {
+    if (T < 0 || D < 1 || N < 1) return RLF_ERR_SHAPE;
+    if (D % 8 != 0) return RLF_ERR_SHAPE;
+    if (T >= (1 << 30) || D >= (1 << 30) || N >= (1 << 29)) return RLF_ERR_UNSUPPORTED;   // rows and columns are counted in 32 bits
+    if (act < RLF_ACT_NONE || act > RLF_ACT_GELU_TANH || (gated != 0 && gated != 1)) return RLF_ERR_UNSUPPORTED;
+    return RLF_OK;
+}
+
+template <int R>
+static void launch_few_fwd(int N, unsigned grid, const __nv_bfloat16* x, long long xs, const __nv_bfloat16* W, int64_t T, int D, const Epilogue& e, cudaStream_t s) {
+    switch (N) {
+        case 1: linear_few_fwd_kernel<1, R><<<grid, 256, 0, s>>>(x, xs, W, T, D, e); break;
+        case 2: linear_few_fwd_kernel<2, R><<<grid, 256, 0, s>>>(x, xs, W, T, D, e); break;
+        case 3: linear_few_fwd_kernel<3, R><<<grid, 256, 0, s>>>(x, xs, W, T, D, e); break;
+        default: linear_few_fwd_kernel<4, R><<<grid, 256, 0, s>>>(x, xs, W, T, D, e); break;
+    }
+}
+
+template <int V, bool GATED>
+static void launch_pregrad(const PreGrad& p, dim3 grid, cudaStream_t s) {
+    const dim3 block(32, 8);
+    switch (p.act) {
+        case RLF_ACT_RELU: linear_pregrad_kernel<V, RLF_ACT_RELU, GATED><<<grid, block, 0, s>>>(p); break;
+        case RLF_ACT_SILU: linear_pregrad_kernel<V, RLF_ACT_SILU, GATED><<<grid, block, 0, s>>>(p); break;
+        case RLF_ACT_GELU: linear_pregrad_kernel<V, RLF_ACT_GELU, GATED><<<grid, block, 0, s>>>(p); break;
+        case RLF_ACT_GELU_TANH: linear_pregrad_kernel<V, RLF_ACT_GELU_TANH, GATED><<<grid, block, 0, s>>>(p); break;
+        default: linear_pregrad_kernel<V, RLF_ACT_NONE, GATED><<<grid, block, 0, s>>>(p); break;
+    }
+}
+
+static rlf_status launch_join(const float* part, int parts, long long width, int accumulate, void* out, int out_f32, cudaStream_t s) {
+    linear_join_kernel<<<(unsigned)((width + 31) / 32), 1024, 0, s>>>(part, parts, width, accumulate, out, out_f32);
+    count_launch();
+    return cuda_ok(cudaGetLastError());
+}
+
+}  // namespace ln
+
+size_t linear_bwd_workspace_bytes(int64_t T, int32_t rows, int32_t D) {
+    if (T < 0 || rows < 1 || D < 1) return 0;
+    return ln::bwd_workspace(T, rows, D).total;
+}
+
+}  // namespace rlf
+
+extern "C" rlf_status rlf_linear_fwd(const void* x, int64_t T, int32_t D, int64_t x_stride, const void* W, int32_t N, const void* bias,
+                                     rlf_dtype bias_dt, int act, int gated, const void* residual, int64_t residual_stride, void* y_out,
+                                     rlf_dtype y_dt, void* pre_out, int32_t* dev_status, rlf_stream_t stream) {
+    using namespace rlf;
+    using namespace rlf::ln;
+    if ((y_dt != RLF_BF16 && y_dt != RLF_F32) || (bias && bias_dt != RLF_BF16 && bias_dt != RLF_F32)) return RLF_ERR_DTYPE;
+    rlf_status st = check_linear(T, D, N, act, gated);
+    if (st != RLF_OK) return st;
+    if (x_stride < D || (residual && residual_stride < N)) return RLF_ERR_SHAPE;
+    if (T == 0) return RLF_OK;
+    if (!x || !W || !y_out) return RLF_ERR_NULL;
+    const size_t osz = y_dt == RLF_F32 ? 4 : 2;
+    if (!aligned(x, 16) || !aligned(W, 16) || x_stride % 8 != 0 || !aligned(bias, bias_dt == RLF_F32 ? 4 : 2) || !aligned(residual, osz) ||
+        !aligned(y_out, osz) || !aligned(pre_out, 2) || !aligned(dev_status, 4))
+        return RLF_ERR_ALIGN;
+    st = check_arch();
+    if (st != RLF_OK) return st;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    Epilogue e = {};
+    e.act = act; e.gated = gated; e.N = N; e.bias = bias; e.bias_bf16 = bias_dt == RLF_BF16;
+    e.res = residual; e.res_stride = residual_stride; e.out = y_out; e.out_stride = N; e.out_f32 = y_dt == RLF_F32;
+    e.pre = static_cast<__nv_bfloat16*>(pre_out); e.pre_stride = gated ? 2ll * N : N;
+    e.vec = rows_aligned(y_out, N, (int)osz) && (!residual || rows_aligned(residual, residual_stride, (int)osz));
+    e.vec_pre = rows_aligned(pre_out, N, 2);
+    if (!gated && N <= kFewOutputs) {
+        const __nv_bfloat16* xb = static_cast<const __nv_bfloat16*>(x);
+        const __nv_bfloat16* wb = static_cast<const __nv_bfloat16*>(W);
+        if (T >= 8ll * 4 * sm_count()) launch_few_fwd<4>(N, (unsigned)((T + 31) / 32), xb, x_stride, wb, T, D, e, s);
+        else launch_few_fwd<1>(N, (unsigned)((T + 7) / 8), xb, x_stride, wb, T, D, e, s);
+        count_launch();
+        return cuda_ok(cudaGetLastError());
+    }
+    return product({x, x_stride, 0}, {W, D, 0}, T, D, e, dev_status, s);
+}
+
+extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, int64_t grad_y_stride, const void* pre, const void* x, int64_t T,
+                                     int32_t D, int64_t x_stride, const void* W, int32_t N, int act, int gated, void* grad_x, void* grad_W,
+                                     rlf_dtype grad_W_dt, float* grad_bias, int accumulate, void* workspace, size_t workspace_bytes,
+                                     int32_t* dev_status, rlf_stream_t stream) {
+    using namespace rlf;
+    using namespace rlf::ln;
+    if ((grad_y_dt != RLF_BF16 && grad_y_dt != RLF_F32) || (grad_W && grad_W_dt != RLF_BF16 && grad_W_dt != RLF_F32)) return RLF_ERR_DTYPE;
+    rlf_status st = check_linear(T, D, N, act, gated);
+    if (st != RLF_OK) return st;
+    if (x_stride < D || grad_y_stride < N) return RLF_ERR_SHAPE;
+    if (accumulate && grad_W && grad_W_dt != RLF_F32) return RLF_ERR_UNSUPPORTED;
+    const bool need_pre = act != RLF_ACT_NONE || gated;
+    const int rows = gated ? 2 * N : N;
+    if (T > 0 && (!grad_y || (need_pre && !pre) || (grad_W && !x) || (grad_x && !W))) return RLF_ERR_NULL;
+    const size_t ysz = grad_y_dt == RLF_F32 ? 4 : 2, wsz = grad_W_dt == RLF_F32 ? 4 : 2;
+    if (!aligned(grad_y, ysz) || !aligned(pre, 2) || !aligned(x, 16) || x_stride % 8 != 0 || !aligned(W, 16) || !aligned(grad_x, 16) ||
+        !aligned(grad_W, grad_W ? wsz : 1) || !aligned(grad_bias, 4) || !aligned(dev_status, 4))
+        return RLF_ERR_ALIGN;
+    if (T > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < linear_bwd_workspace_bytes(T, rows, D))) return RLF_ERR_WORKSPACE;
+    st = check_arch();
+    if (st != RLF_OK) return st;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        // no tokens: the weights' gradients are zero (or what was accumulated before)
+        if (!accumulate && grad_W && cudaMemsetAsync(grad_W, 0, (size_t)rows * (size_t)D * wsz, s) != cudaSuccess) return RLF_ERR_CUDA;
+        if (!accumulate && grad_bias && cudaMemsetAsync(grad_bias, 0, (size_t)rows * 4, s) != cudaSuccess) return RLF_ERR_CUDA;
+        return RLF_OK;
+    }
+    if (!grad_x && !grad_W && !grad_bias) return RLF_OK;
+    const BwdWs ws = bwd_workspace(T, rows, D);
+    char* base = static_cast<char*>(workspace);
+    float* part_b = grad_bias ? reinterpret_cast<float*>(base + ws.part_b) : nullptr;
+    const int slices = token_slices(T);
+    const long long per_slice = (T + slices - 1) / slices;
+    const int used = (int)((T + per_slice - 1) / per_slice);
+
+    if (!gated && N <= kFewOutputs) {
+        FewBwd p = {};
+        p.dy = grad_y; p.dy_stride = grad_y_stride; p.dy_f32 = grad_y_dt == RLF_F32; p.act = act;
+        p.pre = need_pre ? static_cast<const __nv_bfloat16*>(pre) : nullptr;
+        p.x = static_cast<const __nv_bfloat16*>(x); p.x_stride = x_stride; p.W = static_cast<const __nv_bfloat16*>(W);
+        p.dx = static_cast<__nv_bfloat16*>(grad_x); p.part_w = grad_W ? reinterpret_cast<float*>(base + ws.part_w) : nullptr; p.part_b = part_b;
+        p.T = T; p.rows = per_slice; p.D = D;
+        int nx = 1;
+        while (nx < 256 && nx * 8 < D) nx *= 2;
+        const dim3 block(nx, 256 / nx), grid((unsigned)((D + nx * 8 - 1) / (nx * 8)), (unsigned)used);
+        switch (N) {
+            case 1: linear_few_bwd_kernel<1><<<grid, block, 0, s>>>(p); break;
+            case 2: linear_few_bwd_kernel<2><<<grid, block, 0, s>>>(p); break;
+            case 3: linear_few_bwd_kernel<3><<<grid, block, 0, s>>>(p); break;
+            default: linear_few_bwd_kernel<4><<<grid, block, 0, s>>>(p); break;
+        }
+        count_launch();
+        if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
+        if (grad_W) st = launch_join(p.part_w, used, (long long)N * D, accumulate, grad_W, grad_W_dt == RLF_F32, s);
+        if (st == RLF_OK && grad_bias) st = launch_join(part_b, used, N, accumulate, grad_bias, 1, s);
+        return st;
+    }
+
+    // gz: grad_y itself where nothing is to be done to it and TMA can read it
+    const bool in_place = !need_pre && grad_y_dt == RLF_BF16 && rows_aligned(grad_y, grad_y_stride, 2);
+    Operand gz = {grad_y, grad_y_stride, 0};
+    if (!in_place) gz = {base + ws.gz, up8(rows), 0};
+    if ((!in_place && (grad_x || grad_W)) || grad_bias) {
+        PreGrad p = {};
+        p.dy = grad_y; p.dy_stride = grad_y_stride; p.dy_f32 = grad_y_dt == RLF_F32; p.act = act; p.gated = gated;
+        p.pre = need_pre ? static_cast<const __nv_bfloat16*>(pre) : nullptr;
+        p.gz = !in_place && (grad_x || grad_W) ? reinterpret_cast<__nv_bfloat16*>(base + ws.gz) : nullptr;
+        p.gz_stride = up8(rows); p.part_b = part_b; p.T = T; p.rows = per_slice; p.N = N;
+        const bool wide = N % 8 == 0 && rows_aligned(grad_y, grad_y_stride, (int)ysz) && (!p.pre || aligned(p.pre, 16));
+        const dim3 grid((unsigned)((N + (wide ? 255 : 31)) / (wide ? 256 : 32)), (unsigned)used);
+        if (wide) gated ? launch_pregrad<8, true>(p, grid, s) : launch_pregrad<8, false>(p, grid, s);
+        else gated ? launch_pregrad<1, true>(p, grid, s) : launch_pregrad<1, false>(p, grid, s);
+        count_launch();
+        if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
+        if (grad_bias) st = launch_join(part_b, used, rows, accumulate, grad_bias, 1, s);
+        if (st != RLF_OK) return st;
+    }
+    if (grad_x) {
+        Epilogue e = {};
+        e.N = D; e.out = grad_x; e.out_stride = D; e.vec = 1;
+        st = product(gz, {W, D, 1}, T, rows, e, dev_status, s);
+        if (st != RLF_OK) return st;
+    }
+    if (grad_W) {
+        Epilogue e = {};
+        e.N = D; e.out = grad_W; e.out_stride = D; e.out_f32 = grad_W_dt == RLF_F32;
+        e.vec = rows_aligned(grad_W, D, (int)wsz);
+        if (accumulate) { e.res = grad_W; e.res_stride = D; }
+        st = product({gz.at, gz.stride, 1}, {x, x_stride, 1}, rows, T, e, dev_status, s);
+    }
+    return st;
+}
+
+extern "C" rlf_status rlf_tune_linear(int form, int tile, int split) {
+    if (form < 0 || form > 2 || (tile != 0 && tile != 16 && tile != 32 && tile != 64 && tile != 128 && tile != 256)) return RLF_ERR_SHAPE;
+    if (split != 0 && split != 1 && split != 2 && split != 4 && split != 8) return RLF_ERR_SHAPE;
+    rlf::ln::g_form = form;
+    rlf::ln::g_tile = tile;
+    rlf::ln::g_split = split;
+    return RLF_OK;
+}
