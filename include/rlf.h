@@ -78,6 +78,7 @@ typedef enum { RLF_BF16 = 0, RLF_F32 = 1 } rlf_dtype;
 #define RLF_FN_FUSED_CROSS_ENTROPY 9
 #define RLF_FN_FUSED_CROSS_ENTROPY_FWD 10   /* the same call without gradients */
 #define RLF_FN_LINEAR_BWD 11                /* T tokens, V rows of W (2 N when gated), D inputs */
+#define RLF_FN_BLOCK_NORM_BWD 12
 
 typedef struct CUstream_st *rlf_stream_t;
 
@@ -578,6 +579,66 @@ rlf_status rlf_linear_bwd(const void *grad_y, rlf_dtype grad_y_dt, int64_t grad_
                           int gated, void *grad_x, void *grad_W, rlf_dtype grad_W_dt, float *grad_bias,
                           int accumulate, void *workspace, size_t workspace_bytes, int32_t *dev_status,
                           rlf_stream_t stream);
+
+/*
+ * The norms after one block and before the next, with the block's gate and the residual's scale, in one pass.  (Paper Sec.
+ * 2.2: pi_theta is the language model; the paper prints no layer of it, these are the usual forms.)  Per row:
+ *     n = norm_post(x)                       x: the block's output;  RLF_NORM_NONE: n = x
+ *     h = alpha residual + beta gate n       the residual stream;  gate per column, per row, or absent (1)
+ *     y = norm_pre(h)                        the next block's (or the head's) input;  RLF_NORM_NONE: no y
+ * with the norms of rlf_norm_fwd.  Statistics are fp32; y is formed from the unrounded h; each output is rounded once.
+ *
+ *   x        [T, D] dt, row r starts at element r * x_stride (x_stride >= D);  residual [T, D] dt dense
+ *   post_weight, pre_weight [D] w_dt (needed where their norm is there);  post_bias, pre_bias [D] w_dt or NULL
+ *   gate     RLF_GATE_COLUMN [D] w_dt;  RLF_GATE_ROW [T] fp32;  RLF_GATE_NONE: not read
+ *   alpha, beta  finite, eps > 0 (else RLF_ERR_UNSUPPORTED);  one of the two norms has to be there (else RLF_ERR_UNSUPPORTED)
+ *   h_out    [T, D] dt dense;  y_out [T, D] dt dense (not written without the pre norm)
+ *   stats_out [4, T] fp32 or NULL: mean and 1 / spread of the post norm, then of the pre norm (0 and 1 where a norm is
+ *            absent; mean 0 for the RMS form)
+ * Any width, stride and alignment.  Outputs may not overlap inputs or each other, except that h_out may be residual itself.
+ * Non-finite inputs give what the formulas give, in their own row only.  T = 0 is valid.  D of 2^30 and more returns
+ * RLF_ERR_UNSUPPORTED (here and in rlf_block_norm_bwd).
+ */
+#define RLF_NORM_NONE 2                      /* these two entry points only */
+#define RLF_GATE_NONE 0
+#define RLF_GATE_COLUMN 1
+#define RLF_GATE_ROW 2
+rlf_status rlf_block_norm_fwd(const void *x, int64_t x_stride, const void *residual, rlf_dtype dt, int64_t T, int32_t D,
+                              const void *post_weight, const void *post_bias, int post_kind, const void *pre_weight,
+                              const void *pre_bias, int pre_kind, rlf_dtype w_dt, const void *gate, int gate_form,
+                              float alpha, float beta, float eps, void *h_out, void *y_out, float *stats_out,
+                              rlf_stream_t stream);
+
+/*
+ * Backward of rlf_block_norm_fwd.  With u = (h - pre mean) pre rstd, v = (x - post mean) post rstd, s = beta gate:
+ *     q = grad_y pre_weight;   gh = grad_h + pre rstd (q - mean(q) [layer form only] - u mean(q u))
+ *     g = s gh post_weight;    grad_x = post rstd (g - mean(g) [layer form only] - v mean(g v))     (no post norm: s gh)
+ *     grad_residual = alpha gh
+ *     grad_pre_weight = sum_t grad_y u;   grad_pre_bias = sum_t grad_y
+ *     grad_post_weight = sum_t s gh v;    grad_post_bias = sum_t s gh
+ *     grad_gate = beta sum gh n  over the tokens (column gate) or over the row (row gate)
+ * Sums are fp32 in a fixed order (results are run-to-run identical); gh is not rounded in between.
+ *
+ *   grad_y   [T, D] dt dense: gradient of y (not read without the pre norm);  grad_h [T, D] dt dense: gradient that reaches h
+ *            by another path, or NULL (needed without the pre norm)
+ *   x        as in the forward call;  h [T, D] dt dense: its h_out (not read without the pre norm);  stats [4, T] its stats_out
+ *   post_bias  as in the forward call: enters grad_gate only
+ *   grad_x, grad_residual [T, D] dt dense or NULL each
+ *   grad_gate  [D] (column gate) or [T] (row gate) fp32, or NULL;  grad_*_weight, grad_*_bias [D] fp32 or NULL each.  A
+ *            gradient of what is not there returns RLF_ERR_UNSUPPORTED
+ *   accumulate != 0: added to the gradients over tokens, [D] each (a row gate's gradient is overwritten)
+ *   workspace rlf_workspace_bytes(RLF_FN_BLOCK_NORM_BWD, T, 0, D, dt) bytes, 256-byte aligned; may be NULL when no gradient
+ *            over tokens is wanted.  Contents need not be initialised
+ * Outputs may not overlap inputs or each other.  T = 0 is valid (gradients over tokens are then zero, or unchanged with
+ * accumulate).
+ */
+rlf_status rlf_block_norm_bwd(const void *grad_y, const void *grad_h, const void *x, int64_t x_stride, const void *h,
+                              rlf_dtype dt, int64_t T, int32_t D, const void *post_weight, const void *post_bias,
+                              int post_kind, const void *pre_weight, int pre_kind, rlf_dtype w_dt, const void *gate,
+                              int gate_form, float alpha, float beta, const float *stats, void *grad_x,
+                              void *grad_residual, float *grad_gate, float *grad_post_weight, float *grad_post_bias,
+                              float *grad_pre_weight, float *grad_pre_bias, int accumulate, void *workspace,
+                              size_t workspace_bytes, rlf_stream_t stream);
 
 /* Bytes of workspace the given entry point needs for these sizes (0 for unknown selectors). */
 size_t rlf_workspace_bytes(int which_fn, int64_t T, int32_t V, int32_t D, rlf_dtype dt);

@@ -15,12 +15,12 @@ _LIB_PATH = os.path.join(_HERE, "librlf.so")
 
 RLF_BF16, RLF_F32 = 0, 1
 FN_LOGP_LOSS, FN_FUSED_LMHEAD, FN_LOGP_ENTROPY, FN_FUSED_LOGP_ENTROPY, FN_NORM_BWD, FN_CROSS_ENTROPY, FN_FUSED_CROSS_ENTROPY = 3, 4, 5, 6, 7, 8, 9
-FN_FUSED_CROSS_ENTROPY_FWD, FN_LINEAR_BWD = 10, 11
+FN_FUSED_CROSS_ENTROPY_FWD, FN_LINEAR_BWD, FN_BLOCK_NORM_BWD = 10, 11, 12
 DEV_BAD_TARGET, DEV_BAD_SEQ, DEV_NONFINITE, DEV_TIMEOUT = 1, 2, 4, 8
 
 EXPORTS = [
     "rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward", "rlf_grpo_logp_loss_fwd_bwd",
-    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_linear_fwd", "rlf_linear_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
+    "rlf_grpo_logp_loss_fwd_bwd_static", "rlf_grpo_logp_loss_fwd_bwd_skip_masked", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj", "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_linear_fwd", "rlf_linear_bwd", "rlf_block_norm_fwd", "rlf_block_norm_bwd", "rlf_workspace_bytes", "rlf_grpo_step_host", "rlf_step_arena_bytes",
     "rlf_tune_logits_kernel", "rlf_tune_logits_grid", "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing", "rlf_tune_linear", "rlf_launch_count", "rlf_status_string", "rlf_version",
 ]
 
@@ -79,12 +79,16 @@ _lib.rlf_norm_bwd.argtypes = [_vp, _i64, _vp, _i64, _int, _i64, _i32, _vp, _int,
 _lib.rlf_linear_fwd.argtypes = [_vp, _i64, _i32, _i64, _vp, _i32, _vp, _int, _int, _int, _vp, _i64, _vp, _int, _vp, _vp, _vp]
 _lib.rlf_linear_bwd.argtypes = [_vp, _int, _i64, _vp, _vp, _i64, _i32, _i64, _vp, _i32, _int, _int, _vp, _vp, _int, _vp, _int,
                                 _vp, _sz, _vp, _vp]
+_lib.rlf_block_norm_fwd.argtypes = [_vp, _i64, _vp, _int, _i64, _i32, _vp, _vp, _int, _vp, _vp, _int, _int, _vp, _int, _f32, _f32, _f32,
+                                    _vp, _vp, _vp, _vp]
+_lib.rlf_block_norm_bwd.argtypes = [_vp, _vp, _vp, _i64, _vp, _int, _i64, _i32, _vp, _vp, _int, _vp, _int, _int, _vp, _int, _f32, _f32, _vp,
+                                    _vp, _vp, _vp, _vp, _vp, _vp, _vp, _int, _vp, _sz, _vp]
 _lib.rlf_tune_linear.argtypes = [_int, _int, _int]
 # every entry point that returns an rlf_status
 for _n in ("rlf_build_loss_mask", "rlf_count_live_responses", "rlf_group_advantage", "rlf_rule_reward", "rlf_kl_in_reward",
            "rlf_grpo_logp_loss_fwd_bwd", "rlf_grpo_logp_loss_fwd_bwd_obj", "rlf_grpo_logp_loss_fwd_bwd_skip_masked",
            "rlf_logp_entropy_fwd", "rlf_fused_lmhead_grpo", "rlf_fused_lmhead_grpo_obj",
-           "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_linear_fwd", "rlf_linear_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
+           "rlf_fused_lmhead_logp_entropy", "rlf_cross_entropy_fwd_bwd", "rlf_fused_lmhead_cross_entropy", "rlf_norm_fwd", "rlf_norm_bwd", "rlf_linear_fwd", "rlf_linear_bwd", "rlf_block_norm_fwd", "rlf_block_norm_bwd", "rlf_grpo_step_host", "rlf_tune_logits_kernel", "rlf_tune_logits_grid",
            "rlf_tune_lmhead", "rlf_tune_lmhead_schedule", "rlf_tune_lmhead_backward", "rlf_tune_lmhead_pacing", "rlf_tune_linear"):
     getattr(_lib, _n).restype = _int
 
@@ -458,7 +462,7 @@ def rlf_fused_lmhead_logp_entropy(hidden, W, ids, want_entropy=True, logp_out=No
     return logp_out, entropy_out
 
 
-NORM_RMS, NORM_LAYER = 0, 1
+NORM_RMS, NORM_LAYER, NORM_NONE = 0, 1, 2      # (NORM_NONE: the block norm's only)
 
 # The calls below are short next to a decoding step or a small batch, so their host side is kept lean: outputs are made by
 # the cheapest factory call and not checked again, workspace sizes are computed once per shape.
@@ -762,6 +766,111 @@ def rlf_linear_bwd(grad_y, x, W, pre=None, act=ACT_NONE, gated=False, want_grad_
         RLF_F32 if grad_W is None else _dt(grad_W, "grad_W"), _at(grad_bias, here, "grad_bias", _f32, (rows,)),
         1 if accumulate else 0, wp, wn, _at(dev_status, here, "dev_status", _i32t), _raw_stream(here)), "rlf_linear_bwd")
     return grad_x, grad_W, grad_bias
+
+
+GATE_NONE, GATE_COLUMN, GATE_ROW = 0, 1, 2
+
+
+def _norm_vectors(x, here, post_kind, pre_kind, gate_form, gate, **vectors):
+    """Checks of the block norm's [D] vectors (one type among them) and its gate.
+    -> (their type's code, their addresses by name, the gate's address)"""
+    T, D = x.shape
+    if x.dtype not in _DTYPES:
+        raise TypeError("x must be bfloat16 or float32")
+    if (gate is None) != (gate_form == GATE_NONE):
+        raise ValueError("gate and gate_form go together")
+    there = [t for t in vectors.values() if t is not None]
+    if gate_form == GATE_COLUMN:
+        there.append(gate)
+    w_dt = there[0].dtype if there else _f32
+    if w_dt not in _DTYPES:
+        raise TypeError("weights, biases and a column gate must be bfloat16 or float32")
+    for name, kind in (("post", post_kind), ("pre", pre_kind)):
+        if kind != NORM_NONE and vectors[name + "_weight"] is None:
+            raise ValueError("the %s norm needs %s_weight" % (name, name))
+        if kind == NORM_NONE and (vectors[name + "_weight"] is not None or vectors.get(name + "_bias") is not None):
+            raise ValueError("%s_weight and %s_bias belong to the %s norm" % (name, name, name))
+    at = {k: _at(t, here, k, w_dt, (D,)) for k, t in vectors.items()}
+    gp = _at(gate, here, "gate", w_dt if gate_form == GATE_COLUMN else _f32, (D,) if gate_form == GATE_COLUMN else (T,))
+    return _DTYPES[w_dt], at, gp
+
+
+def rlf_block_norm_fwd(x, residual, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, post_kind=NORM_RMS,
+                       pre_kind=NORM_RMS, gate=None, gate_form=GATE_NONE, alpha=1.0, beta=1.0, eps=1e-6, h_out=None, y_out=None,
+                       stats_out=None):
+    """The norm after a block, its gate, the residual and the norm before the next block:
+    h = alpha residual + beta gate norm_post(x), y = norm_pre(h).  x [T, D] (rows may be strided), residual [T, D]; weights,
+    biases and a column gate [D] of one type, bf16 or fp32; a row gate [T] fp32; NORM_NONE leaves a norm out.
+    -> (h [T, D], y [T, D] | None without the pre norm, stats fp32 [4, T]: post mean and rstd, pre mean and rstd)."""
+    here = _device_of(x)
+    xp, xs = _rows(x, here, "x")
+    shape = T, D = x.shape
+    w_dt, at, gp = _norm_vectors(x, here, post_kind, pre_kind, gate_form, gate, post_weight=post_weight, post_bias=post_bias,
+                                 pre_weight=pre_weight, pre_bias=pre_bias)
+    dt = x.dtype
+    rp = _at(residual, here, "residual", dt, shape)
+    if residual is None:
+        raise ValueError("residual is needed")
+    if h_out is None:
+        h_out = _dense_like(x)
+    if y_out is None and pre_kind != NORM_NONE:
+        y_out = _dense_like(x)
+    if stats_out is None:
+        stats_out = x.new_empty((4, T), dtype=_f32)
+    _check(_lib.rlf_block_norm_fwd(
+        xp, xs, rp, _DTYPES[dt], T, D, at["post_weight"], at["post_bias"], post_kind, at["pre_weight"], at["pre_bias"], pre_kind, w_dt,
+        gp, gate_form, alpha, beta, eps, _at(h_out, here, "h_out", dt, shape), _at(y_out, here, "y_out", dt, shape),
+        _at(stats_out, here, "stats_out", _f32, (4, T)), _raw_stream(here)), "rlf_block_norm_fwd")
+    return h_out, y_out, stats_out
+
+
+def rlf_block_norm_bwd(grad_y, grad_h, x, h, stats, post_weight=None, post_bias=None, pre_weight=None, post_kind=NORM_RMS,
+                       pre_kind=NORM_RMS, gate=None, gate_form=GATE_NONE, alpha=1.0, beta=1.0, want_grad_x=True,
+                       want_grad_residual=True, want_grad_weight=True, want_grad_bias=False, want_grad_gate=True, grad_x=None,
+                       grad_residual=None, grad_gate=None, grad_post_weight=None, grad_post_bias=None, grad_pre_weight=None,
+                       grad_pre_bias=None, accumulate=False, workspace=None):
+    """Backward of rlf_block_norm_fwd; h and stats are what it left (h is not read without the pre norm, grad_y neither);
+    grad_h is the gradient that reaches h by another path, or None.  accumulate adds to the [D] gradients' buffers.
+    -> dict(grad_x, grad_residual [T, D], grad_gate, grad_post_weight, grad_post_bias, grad_pre_weight, grad_pre_bias fp32), None
+    where not wanted or not there."""
+    here = _device_of(x)
+    xp, xs = _rows(x, here, "x")
+    shape = T, D = x.shape
+    w_dt, at, gp = _norm_vectors(x, here, post_kind, pre_kind, gate_form, gate, post_weight=post_weight, post_bias=post_bias,
+                                 pre_weight=pre_weight)
+    dt = x.dtype
+    pre, post = pre_kind != NORM_NONE, post_kind != NORM_NONE
+    if pre and (grad_y is None or h is None):
+        raise ValueError("the pre norm needs grad_y and h")
+    if not pre and grad_h is None:
+        raise ValueError("without the pre norm grad_h is needed")
+    wanted = dict(grad_post_weight=post and want_grad_weight, grad_post_bias=post and want_grad_bias, grad_pre_weight=pre and want_grad_weight,
+                  grad_pre_bias=pre and want_grad_bias, grad_gate=gate_form != GATE_NONE and want_grad_gate)
+    out = dict(grad_x=grad_x, grad_residual=grad_residual, grad_gate=grad_gate, grad_post_weight=grad_post_weight,
+               grad_post_bias=grad_post_bias, grad_pre_weight=grad_pre_weight, grad_pre_bias=grad_pre_bias)
+    over_tokens = False
+    for k, want in wanted.items():
+        per_row = k == "grad_gate" and gate_form == GATE_ROW
+        if out[k] is None and want:
+            if accumulate and not per_row:
+                raise ValueError("accumulate needs the buffers that are added to")
+            out[k] = x.new_empty(T if per_row else D, dtype=_f32)
+        over_tokens = over_tokens or (out[k] is not None and not per_row)
+    if out["grad_x"] is None and want_grad_x:
+        out["grad_x"] = _dense_like(x)
+    if out["grad_residual"] is None and want_grad_residual:
+        out["grad_residual"] = _dense_like(x)
+    wp, wn = None, 0
+    if workspace is not None or over_tokens:
+        workspace, wp, wn = _workspace(workspace, here, x, FN_BLOCK_NORM_BWD, T, 0, D, RLF_F32)
+    vec = lambda k: _at(out[k], here, k, _f32, (T,) if k == "grad_gate" and gate_form == GATE_ROW else (D,))
+    _check(_lib.rlf_block_norm_bwd(
+        _at(grad_y, here, "grad_y", dt, shape) if pre else None, _at(grad_h, here, "grad_h", dt, shape), xp, xs,
+        _at(h, here, "h", dt, shape) if pre else None, _DTYPES[dt], T, D, at["post_weight"], at["post_bias"], post_kind, at["pre_weight"],
+        pre_kind, w_dt, gp, gate_form, alpha, beta, _at(stats, here, "stats", _f32, (4, T)), _at(out["grad_x"], here, "grad_x", dt, shape),
+        _at(out["grad_residual"], here, "grad_residual", dt, shape), vec("grad_gate"), vec("grad_post_weight"), vec("grad_post_bias"),
+        vec("grad_pre_weight"), vec("grad_pre_bias"), 1 if accumulate else 0, wp, wn, _raw_stream(here)), "rlf_block_norm_bwd")
+    return out
 
 
 def step_arena_bytes(T, V, B, dt=RLF_BF16):

@@ -33,6 +33,7 @@ size_t norm_bwd_workspace_bytes(int64_t T, int32_t D);            // norm.cu
 size_t cross_entropy_workspace_bytes(int64_t T, int32_t V, rlf_dtype dt);                  // cross_entropy.cu
 size_t lmhead_ce_workspace_bytes(int64_t T, int32_t V, int32_t D, bool grad_w_bf16, bool grads);  // lmhead.cu
 size_t linear_bwd_workspace_bytes(int64_t T, int32_t rows, int32_t D);                             // linear.cu
+size_t block_norm_bwd_workspace_bytes(int64_t T, int32_t D);                                       // block_norm.cu
 
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -91,6 +92,7 @@ extern "C" size_t rlf_workspace_bytes(int which_fn, int64_t T, int32_t V, int32_
     if (which_fn == RLF_FN_CROSS_ENTROPY) return rlf::cross_entropy_workspace_bytes(T, V, (rlf_dtype)dt);
     if (which_fn == RLF_FN_FUSED_CROSS_ENTROPY) return rlf::lmhead_ce_workspace_bytes(T, V, D, dt == RLF_BF16, true);
     if (which_fn == RLF_FN_FUSED_CROSS_ENTROPY_FWD) return rlf::lmhead_ce_workspace_bytes(T, V, D, false, false);
+    if (which_fn == RLF_FN_BLOCK_NORM_BWD) return rlf::block_norm_bwd_workspace_bytes(T, D);
     if (which_fn == RLF_FN_LINEAR_BWD) return rlf::linear_bwd_workspace_bytes(T, V, D);
     if (which_fn == RLF_FN_NORM_BWD) return rlf::norm_bwd_workspace_bytes(T, D);
     return 0;
