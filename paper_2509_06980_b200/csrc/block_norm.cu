@@ -59,6 +59,7 @@ __device__ __forceinline__ float row_gate(const BlockParams& p, long long t) {
 }
 
 constexpr int kGenThreads = 256;
+constexpr int kSmemLimit = 200 * 1024;           // most dynamic shared memory that a fast form asks for
 
 // ---- any width, stride and alignment: one CTA per row, the row read once per pass (later passes are served by L2) ----------
 template <typename T>
@@ -255,6 +256,441 @@ block_finish_kernel(const Finish f) {
     }
 }
 
+// ---- fast forms ---------------------------------------------------------------------------------
+// A CTA works on R rows at a time, with the next R rows on their way into the other half of a shared-memory buffer (cp.async);
+// a thread owns NV 16-byte vectors of each row.  EDGE: rows on no boundary, all dense tensors' rows alike; a CTA then takes
+// every period-th row, whose places in their vectors are the same, and a row's first and last vector are masked.  The rows of
+// x, whose stride is its own, may sit otherwise (x_shift): they are copied as the aligned chunks that cover them and read by
+// element.
+template <typename T, int NV, int R, bool EDGE>
+struct Stage {
+    static constexpr int P = Vec<T>::P, N = Vec<T>::N;
+    const BlockParams& p;
+    const Rows<T, EDGE> rows;
+    uint4* slots;                   // [2][R][arrays][NV][threads], a slot is its thread's own
+    char* shifted;                  // [2][R] rows of x
+    int arrays, pitch, th, tid;
+    bool shift;
+    unsigned keep[NV];
+    __device__ __forceinline__ Stage(const BlockParams& p_, uint4* smem, const void* dense, int arrays_)
+        : p(p_), rows(dense, p_.D, p_.T, p_.D, p_.period, R), slots(smem), arrays(arrays_), th(blockDim.x), tid(threadIdx.x) {
+        shift = EDGE && p.x_shift;
+        pitch = staged_pitch(p.D, (int)sizeof(T));
+        shifted = reinterpret_cast<char*>(smem + 2 * R * arrays * NV * th);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) keep[i] = EDGE ? rows.bits(tid + i * th, p.D) : (1u << N) - 1u;
+    }
+    __device__ __forceinline__ bool mine(int i) const { return tid + i * th < rows.nvec; }
+    __device__ __forceinline__ uint4* slot(int buf, int k, int a, int i) const { return slots + (((buf * R + k) * arrays + a) * NV + i) * th + tid; }
+    __device__ __forceinline__ void copy(int buf, int k, int a, const void* tensor, long long stride, long long t) const {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (mine(i)) rows.copy(slot(buf, k, a, i), static_cast<const T*>(tensor) + t * stride, tid + i * th, p.D, t == 0);
+    }
+    // x goes into array a, or to its own place
+    __device__ __forceinline__ void copy_x(int buf, int k, int a, long long t) const {
+        if (shift) copy_row<T>(shifted + (buf * R + k) * pitch, static_cast<const T*>(p.x) + t * p.x_stride, p.D, t == 0);
+        else copy(buf, k, a, p.x, p.x_stride, t);
+    }
+    __device__ __forceinline__ void read(int buf, int k, int a, int i, f2 (&v)[P]) const {
+        Vec<T>::unpack(*slot(buf, k, a, i), v);
+        if (EDGE && keep[i] != (1u << N) - 1u) mask_pairs<P>(v, keep[i]);
+    }
+    __device__ __forceinline__ void read_x(int buf, int k, int a, int i, long long t, f2 (&v)[P]) const {
+        if (!shift) {
+            read(buf, k, a, i, v);
+            return;
+        }
+        const T* row = reinterpret_cast<const T*>(shifted + (buf * R + k) * pitch + chunk_head(static_cast<const T*>(p.x) + t * p.x_stride));
+        const int c = (tid + i * th) * N - rows.lead;
+        auto at = [&](int e) { return c + e >= 0 && c + e < p.D ? to_f<T>(row[c + e]) : 0.0f; };
+#pragma unroll
+        for (int e = 0; e < P; ++e) v[e] = f2_make(at(2 * e), at(2 * e + 1));
+    }
+    __device__ __forceinline__ void store(void* tensor, long long t, int i, const f2 (&v)[P]) const {
+        rows.store(static_cast<T*>(tensor) + t * p.D, tid + i * th, Vec<T>::pack(v), keep[i]);
+    }
+    __device__ __forceinline__ void mask(int i, f2 (&v)[P]) const {
+        if (EDGE && keep[i] != (1u << N) - 1u) mask_pairs<P>(v, keep[i]);
+    }
+    // a function of the column, for this thread's columns (0 outside the width)
+    template <typename F> __device__ __forceinline__ void columns(f2 (&f)[NV][P], F of) const {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const int c = (tid + i * th) * N + 2 * e - rows.lead;
+                f[i][e] = f2_make(c >= 0 && c < p.D ? of(c) : 0.0f, c + 1 >= 0 && c + 1 < p.D ? of(c + 1) : 0.0f);
+            }
+    }
+};
+__device__ __forceinline__ f2 f2_dup(float v) { return f2_make(v, v); }
+
+// L: a mean or a bias is in it somewhere (the RMS norms without bias keep no registers for them)
+template <typename T, int NV, int R, bool L, bool EDGE, int MAXT>
+__global__ void __launch_bounds__(MAXT)
+block_fwd_kernel(const BlockParams p) {
+    using V = Vec<T>;
+    constexpr int P = V::P;
+    extern __shared__ __align__(16) uint4 smem[];       // residual, x (where it is like the others)
+    __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * R];
+    int turn = 0;
+    const Stage<T, NV, R, EDGE> st(p, smem, p.res, EDGE && p.x_shift ? 1 : 2);
+    const float inv_d = 1.0f / (float)p.D;
+    const bool post = has_norm(p.post), pre = has_norm(p.pre);
+    float gate_next[R];
+    auto fetch = [&](long long j0, int buf) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            gate_next[k] = 1.0f;
+            if (j0 + k < st.rows.n) {
+                const long long t = st.rows.row(j0 + k);
+                gate_next[k] = row_gate(p, t);
+                st.copy(buf, k, 0, p.res, p.D, t);
+                st.copy_x(buf, k, 1, t);
+            }
+        }
+        cp_async_commit();
+    };
+    long long j0 = st.rows.first;
+    fetch(j0, 0);
+    f2 w1[NV][P], w2[NV][P], b1[L ? NV : 1][P], b2[L ? NV : 1][P];
+    st.columns(w1, [&](int c) { return col_scale(p, c) * post_w(p, c); });
+    st.columns(w2, [&](int c) { return p.w2 ? ld_w(p.w2, p.w_bf16, c) : 0.0f; });
+    if constexpr (L) {
+        st.columns(b1, [&](int c) { return p.b1 ? col_scale(p, c) * ld_w(p.b1, p.w_bf16, c) : 0.0f; });
+        st.columns(b2, [&](int c) { return p.b2 ? ld_w(p.b2, p.w_bf16, c) : 0.0f; });
+    }
+    const f2 alpha = f2_dup(p.alpha);
+    for (int buf = 0; j0 < st.rows.n; j0 += st.rows.step, buf ^= 1) {
+        float gate[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) gate[k] = gate_next[k];
+        if (st.shift) __syncthreads();                  // the other half has been read by everyone
+        fetch(j0 + st.rows.step, buf ^ 1);
+        cp_async_wait1();
+        if (st.shift) __syncthreads();                  // everyone's chunks of this half are here
+        f2 v[R][NV][P];
+        float m1[R], r1[R], m2[R], r2[R], s[R];
+        // mean and 1 / spread of the rows held in v
+        auto stats = [&](bool layer, float (&m)[R], float (&r)[R]) {
+            if (L && layer) {
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    f2 q = 0ull;
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+                        if (st.mine(i))
+#pragma unroll
+                            for (int e = 0; e < P; ++e) q = f2_add(q, v[k][i][e]);
+                    s[k] = f2_sum(q);
+                }
+                cta_sums<R>(s, red, turn);
+            }
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                m[k] = L && layer ? s[k] * inv_d : 0.0f;
+                const f2 c = f2_dup(-m[k]);
+                f2 q = 0ull;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (st.mine(i)) {
+                        f2 d[P];
+#pragma unroll
+                        for (int e = 0; e < P; ++e) d[e] = L ? f2_add(v[k][i][e], c) : v[k][i][e];
+                        if (L) st.mask(i, d);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) q = f2_fma(d[e], d[e], q);
+                    }
+                s[k] = f2_sum(q);
+            }
+            cta_sums<R>(s, red, turn);
+#pragma unroll
+            for (int k = 0; k < R; ++k) r[k] = rsqrtf(s[k] * inv_d + p.eps);
+        };
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            m1[k] = m2[k] = 0.0f;
+            r1[k] = r2[k] = 1.0f;
+            const long long t = st.rows.row(min(j0 + k, st.rows.n - 1));
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (st.mine(i)) st.read_x(buf, k, 1, i, t, v[k][i]);
+        }
+        if (post) stats(p.post == RLF_NORM_LAYER, m1, r1);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const f2 c = f2_dup(-m1[k]), r = f2_dup(r1[k] * gate[k]), g = f2_dup(gate[k]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (st.mine(i)) {
+                    f2 res[P];
+                    st.read(buf, k, 0, i, res);
+#pragma unroll
+                    for (int e = 0; e < P; ++e) {
+                        f2 n = f2_mul(f2_mul(L ? f2_add(v[k][i][e], c) : v[k][i][e], r), w1[i][e]);
+                        if (L) n = f2_fma(g, b1[L ? i : 0][e], n);
+                        v[k][i][e] = f2_fma(alpha, res[e], n);
+                    }
+                }
+        }
+        if (pre) stats(p.pre == RLF_NORM_LAYER, m2, r2);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (j0 + k >= st.rows.n) continue;
+            const long long t = st.rows.row(j0 + k);
+            const f2 c = f2_dup(-m2[k]), r = f2_dup(r2[k]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (st.mine(i)) {
+                    st.store(p.h, t, i, v[k][i]);
+                    if (pre) {
+                        f2 o[P];
+#pragma unroll
+                        for (int e = 0; e < P; ++e) {
+                            o[e] = f2_mul(f2_mul(L ? f2_add(v[k][i][e], c) : v[k][i][e], r), w2[i][e]);
+                            if (L) o[e] = f2_add(o[e], b2[L ? i : 0][e]);
+                        }
+                        st.store(p.y, t, i, o);
+                    }
+                }
+            if (st.tid == 0 && p.stats) {
+                p.stats[t] = m1[k];
+                p.stats[p.T + t] = r1[k];
+                p.stats[2 * p.T + t] = m2[k];
+                p.stats[3 * p.T + t] = r2[k];
+            }
+        }
+    }
+    cp_async_wait0();
+}
+
+// Backward: two sums per row one after the other (the second needs gh, which needs the first), gh held in registers in between; the
+// sums over tokens are added up row after row in registers and leave as one partial row per CTA.
+template <typename T, int NV, int R, bool L, bool EDGE, int MAXT>
+__global__ void __launch_bounds__(MAXT)
+block_bwd_kernel(const BlockParams p) {
+    using V = Vec<T>;
+    constexpr int P = V::P, N = V::N, K = L ? 2 * R : R;
+    extern __shared__ __align__(16) uint4 smem[];       // dy, h (with the pre norm), dh (if given), x (where it is like the others)
+    __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * K];
+    int turn = 0;
+    const bool post = has_norm(p.post), pre = has_norm(p.pre);
+    const int at_dh = pre ? 2 : 0, at_x = at_dh + (p.dh ? 1 : 0);
+    const Stage<T, NV, R, EDGE> st(p, smem, pre ? p.h : p.dh, at_x + (EDGE && p.x_shift ? 0 : 1));
+    const float inv_d = 1.0f / (float)p.D;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    float next[R][5];                                   // the rows' statistics and gate
+    auto fetch = [&](long long j0, int buf) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+#pragma unroll
+            for (int q = 0; q < 5; ++q) next[k][q] = 0.0f;
+            if (j0 + k < st.rows.n) {
+                const long long t = st.rows.row(j0 + k);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (L || (q & 1)) next[k][q] = p.stats[q * p.T + t];
+                next[k][4] = row_gate(p, t);
+                if (pre) {
+                    st.copy(buf, k, 0, p.dy, p.D, t);
+                    st.copy(buf, k, 1, p.h, p.D, t);
+                }
+                if (p.dh) st.copy(buf, k, at_dh, p.dh, p.D, t);
+                st.copy_x(buf, k, at_x, t);
+            }
+        }
+        cp_async_commit();
+    };
+    long long j0 = st.rows.first;
+    fetch(j0, 0);
+    f2 w1[NV][P], w2[NV][P], sum_dyu[NV][P], sum_ghv[NV][P], sum_dy[L ? NV : 1][P], sum_gh[L ? NV : 1][P];
+    st.columns(w1, [&](int c) { return col_scale(p, c) * post_w(p, c); });
+    st.columns(w2, [&](int c) { return p.w2 ? ld_w(p.w2, p.w_bf16, c) : 0.0f; });
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            sum_dyu[i][e] = sum_ghv[i][e] = 0ull;
+            if (L) sum_dy[L ? i : 0][e] = sum_gh[L ? i : 0][e] = 0ull;
+        }
+    for (int buf = 0; j0 < st.rows.n; j0 += st.rows.step, buf ^= 1) {
+        float m1[R], r1[R], m2[R], r2[R], gate[R], s[K];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            m1[k] = next[k][0];
+            r1[k] = next[k][1];
+            m2[k] = next[k][2];
+            r2[k] = next[k][3];
+            gate[k] = next[k][4];
+        }
+        if (st.shift) __syncthreads();
+        fetch(j0 + st.rows.step, buf ^ 1);
+        cp_async_wait1();
+        if (st.shift) __syncthreads();
+        auto unit = [&](int k, const f2& v, const f2& c, const f2& r) { return f2_mul(L ? f2_add(v, c) : v, r); };
+        if (pre) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                f2 a = 0ull, b = 0ull;
+                if (j0 + k < st.rows.n) {
+                    const f2 c = f2_dup(-m2[k]), r = f2_dup(r2[k]);
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+                        if (st.mine(i)) {
+                            f2 dy[P], h[P];
+                            st.read(buf, k, 0, i, dy);
+                            st.read(buf, k, 1, i, h);
+#pragma unroll
+                            for (int e = 0; e < P; ++e) {
+                                const f2 q = f2_mul(dy[e], unit(k, h[e], c, r));
+                                a = f2_fma(q, w2[i][e], a);
+                                sum_dyu[i][e] = f2_add(sum_dyu[i][e], q);
+                                if (L) {
+                                    b = f2_fma(dy[e], w2[i][e], b);
+                                    sum_dy[L ? i : 0][e] = f2_add(sum_dy[L ? i : 0][e], dy[e]);
+                                }
+                            }
+                        }
+                }
+                s[k] = f2_sum(a);
+                if (L) s[L ? R + k : 0] = f2_sum(b);
+            }
+            cta_sums<K>(s, red, turn);
+        }
+        f2 gh[R][NV][P];
+        float a1[R], b1[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            a1[k] = pre ? s[k] * inv_d : 0.0f;
+            b1[k] = L && p.pre == RLF_NORM_LAYER ? s[L ? R + k : 0] * inv_d : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            f2 a = 0ull, b = 0ull;
+            if (j0 + k < st.rows.n) {
+                const long long t = st.rows.row(j0 + k);
+                // gh = dh + r2 dy w2 - r2 b1 - (h - m2) r2^2 a1
+                const f2 c2 = f2_dup(-m2[k]), r = f2_dup(r2[k]), ra = f2_dup(-r2[k] * r2[k] * a1[k]), rb = f2_dup(-r2[k] * b1[k]);
+                const f2 c1 = f2_dup(-m1[k]), rv = f2_dup(r1[k]), g = f2_dup(gate[k]), al = f2_dup(p.alpha);
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (st.mine(i)) {
+                        f2 x[P], o[P];
+                        if (p.dh) {
+                            st.read(buf, k, at_dh, i, gh[k][i]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < P; ++e) gh[k][i][e] = 0ull;
+                        }
+                        if (pre) {
+                            f2 dy[P], h[P];
+                            st.read(buf, k, 0, i, dy);
+                            st.read(buf, k, 1, i, h);
+#pragma unroll
+                            for (int e = 0; e < P; ++e) {
+                                f2 d = f2_mul(f2_mul(dy[e], w2[i][e]), r);
+                                if (L) d = f2_add(d, rb);
+                                d = f2_fma(L ? f2_add(h[e], c2) : h[e], ra, d);
+                                gh[k][i][e] = f2_add(gh[k][i][e], d);
+                            }
+                        }
+                        st.read_x(buf, k, at_x, i, t, x);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) {
+                            const f2 v = unit(k, x[e], c1, rv), q = f2_mul(gh[k][i][e], w1[i][e]), sg = f2_mul(gh[k][i][e], g);
+                            o[e] = f2_mul(gh[k][i][e], al);
+                            a = f2_fma(q, v, a);
+                            sum_ghv[i][e] = f2_fma(sg, v, sum_ghv[i][e]);
+                            if (L) {
+                                b = f2_add(b, q);
+                                sum_gh[L ? i : 0][e] = f2_add(sum_gh[L ? i : 0][e], sg);
+                            }
+                        }
+                        if (p.dres) st.store(p.dres, t, i, o);
+                    }
+            }
+            s[k] = f2_sum(a);
+            if (L) s[L ? R + k : 0] = f2_sum(b);
+        }
+        if (!post && !p.dgate_row) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[k] = 0.0f;
+        } else {
+            cta_sums<K>(s, red, turn);
+        }
+        if (p.dgate_row) {
+            float c[R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) c[k] = 0.0f;
+            if (L && p.b1) {
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    if (j0 + k >= st.rows.n) continue;
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+                        if (st.mine(i))
+#pragma unroll
+                            for (int e = 0; e < P; ++e) {
+                                const int col = (st.tid + i * st.th) * N + 2 * e - st.rows.lead;
+                                float lo, hi;
+                                f2_split(gh[k][i][e], lo, hi);
+                                if (col >= 0 && col < p.D) c[k] = fmaf(lo, p.beta * ld_w(p.b1, p.w_bf16, col), c[k]);
+                                if (col + 1 >= 0 && col + 1 < p.D) c[k] = fmaf(hi, p.beta * ld_w(p.b1, p.w_bf16, col + 1), c[k]);
+                            }
+                }
+                cta_sums<R>(c, red, turn);
+            }
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (st.tid == 0 && j0 + k < st.rows.n) p.dgate_row[st.rows.row(j0 + k)] = s[k] + c[k];
+        }
+        if (p.dx == nullptr) continue;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (j0 + k >= st.rows.n) continue;
+            const long long t = st.rows.row(j0 + k);
+            // gate r1 (gh w1 - b - (x - m1) r1 a)
+            const float gr = gate[k] * r1[k], a = post ? s[k] * inv_d : 0.0f, b = L && p.post == RLF_NORM_LAYER ? s[L ? R + k : 0] * inv_d : 0.0f;
+            const f2 r = f2_dup(gr), ra = f2_dup(-gr * r1[k] * a), rb = f2_dup(-gr * b), c = f2_dup(-m1[k]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (st.mine(i)) {
+                    f2 x[P], o[P];
+                    st.read_x(buf, k, at_x, i, t, x);
+#pragma unroll
+                    for (int e = 0; e < P; ++e) {
+                        o[e] = f2_mul(f2_mul(gh[k][i][e], w1[i][e]), r);
+                        if (L) o[e] = f2_add(o[e], rb);
+                        o[e] = f2_fma(L ? f2_add(x[e], c) : x[e], ra, o[e]);
+                    }
+                    st.store(p.dx, t, i, o);
+                }
+        }
+    }
+    cp_async_wait0();
+    auto leave = [&](int which, const f2 (&g)[P], int i) {
+        if (!((p.want >> which) & 1) || !st.mine(i)) return;
+        float* d = p.part + which * p.part_stride + (long long)blockIdx.x * p.D + (st.tid + i * st.th) * N - st.rows.lead;
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            float lo, hi;
+            f2_split(g[e], lo, hi);
+            if ((st.keep[i] >> (2 * e)) & 1u) d[2 * e] = lo;
+            if ((st.keep[i] >> (2 * e + 1)) & 1u) d[2 * e + 1] = hi;
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        leave(0, sum_dyu[i], i);
+        leave(2, sum_ghv[i], i);
+        if (L) {
+            leave(1, sum_dy[L ? i : 0], i);
+            leave(3, sum_gh[L ? i : 0], i);
+        }
+    }
+}
+
 // ---- host side ----------------------------------------------------------------------------------
 // Most partial rows of a sum over tokens (sizes the workspace): enough for one per resident CTA.
 static long long max_parts(long long T, int D) {
@@ -266,6 +702,93 @@ static long long max_parts(long long T, int D) {
 }
 static long long part_stride(long long parts, int D) { return (parts * D + 63) & ~63ll; }
 static size_t sums_offset(long long T, int D) { return 4 * (size_t)part_stride(max_parts(T, D), D) * sizeof(float); }
+
+// how rows are cut: nv vectors per thread, `threads` threads, `rows` rows at a time, bytes of shared memory
+struct Cut { int nv, threads, rows, smem, max_threads; };
+
+// false: no fast form holds the rows (rows shorter than a vector, or longer than 8192 elements).  `arrays` rows are read per
+// row besides a shifted x.
+static bool pick_cut(bool bf16, bool edge, bool shift, bool fwd, bool full, long long T, int D, int arrays, Cut* c) {
+    const int esz = bf16 ? 2 : 4, v = 16 / esz;
+    if (D < v || D > 8192) return false;
+    const int nvec = edge ? (D + 2 * v - 2) / v : D / v, most_nv = bf16 ? 2 : 4;
+    c->nv = 1;
+    while ((nvec + c->nv - 1) / c->nv > (fwd ? 128 : 128) && c->nv < most_nv) c->nv *= 2;
+    c->threads = ((nvec + c->nv - 1) / c->nv + 31) / 32 * 32;
+    c->max_threads = c->threads <= 256 ? 256 : 512;
+    if (c->threads > 512) return false;
+    c->rows = c->max_threads == 512 ? 1 : 2;
+    (void)full;
+    while (c->rows > 1 && T < 148ll * 4 * c->rows) c->rows /= 2;      // too few rows to put several on a CTA
+    for (;; c->rows /= 2) {
+        c->smem = 2 * c->rows * (arrays * c->nv * c->threads * 16 + (shift ? staged_pitch(D, esz) : 0));
+        if (c->smem <= (c->rows > 1 ? kSmemLimit / 2 : kSmemLimit)) return true;
+        if (c->rows == 1) return false;
+    }
+}
+
+typedef void (*BlockKernel)(const BlockParams);
+#define RLF_BLOCK_FORM(nv_, rows_, max_) \
+    if (c.nv == nv_ && c.rows == rows_ && c.max_threads == max_) return FWD ? block_fwd_kernel<T, nv_, rows_, L, EDGE, max_> : block_bwd_kernel<T, nv_, rows_, L, EDGE, max_>
+template <bool FWD, typename T, bool L, bool EDGE>
+static BlockKernel kernel_form(const Cut& c) {
+    RLF_BLOCK_FORM(1, 1, 256);
+    RLF_BLOCK_FORM(1, 2, 256);
+    if constexpr (sizeof(T) == 2) {
+        RLF_BLOCK_FORM(2, 1, 256);
+        RLF_BLOCK_FORM(2, 2, 256);
+        RLF_BLOCK_FORM(2, 1, 512);
+    } else {
+        RLF_BLOCK_FORM(2, 1, 256);
+        RLF_BLOCK_FORM(2, 2, 256);
+        RLF_BLOCK_FORM(4, 1, 256);
+        RLF_BLOCK_FORM(4, 2, 256);
+        RLF_BLOCK_FORM(4, 1, 512);
+    }
+    return nullptr;
+}
+#undef RLF_BLOCK_FORM
+template <bool FWD>
+static BlockKernel kernel_of(bool bf16, bool full, bool edge, const Cut& c) {
+    if (bf16) {
+        if (full) return edge ? kernel_form<FWD, __nv_bfloat16, true, true>(c) : kernel_form<FWD, __nv_bfloat16, true, false>(c);
+        return edge ? kernel_form<FWD, __nv_bfloat16, false, true>(c) : kernel_form<FWD, __nv_bfloat16, false, false>(c);
+    }
+    if (full) return edge ? kernel_form<FWD, float, true, true>(c) : kernel_form<FWD, float, true, false>(c);
+    return edge ? kernel_form<FWD, float, false, true>(c) : kernel_form<FWD, float, false, false>(c);
+}
+
+// CTAs of this kernel that are resident at once (0: none fits); opts the kernel in to its shared memory on the way
+static int resident_ctas(const void* k, const Cut& c) {
+    static ResidentTable table;
+    return table.get(k, c.threads, c.smem, [&](int dev) {
+        int per_sm = 0, sms = 0;
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, c.threads, c.smem) != cudaSuccess) {
+            cudaGetLastError();
+            per_sm = 0;
+        }
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        return per_sm * (sms > 0 ? sms : 148);
+    });
+}
+
+// Which fast form fits the tensors' rows (the first of `at` is dense): sets period and x_shift.
+static bool fast_form(bool bf16, long long T, int D, const void* const* at, int n, const void* x, long long x_stride, BlockParams* p, bool* edge) {
+    int period = 1;
+    const Form form = row_form(bf16, T, D, at, n, D, D, &period);
+    if (form == kStaged) return false;
+    const int v = bf16 ? 8 : 4;
+    const bool alike = (reinterpret_cast<uintptr_t>(x) - reinterpret_cast<uintptr_t>(at[0])) % 16 == 0 && (T <= 1 || x_stride % v == D % v);
+    p->period = period;
+    p->x_shift = !alike;
+    *edge = form == kEdge || !alike;
+    return true;
+}
+static long long batches(long long T, const Cut& c, int period) {
+    const long long rows = (T + period - 1) / period;
+    return (rows + c.rows - 1) / c.rows * period;
+}
 
 static int row_grid(long long T) { return (int)(T < 148 * 8 ? T : 148 * 8); }
 
@@ -334,6 +857,21 @@ extern "C" rlf_status rlf_block_norm_fwd(const void* x, int64_t x_stride, const 
     p.w1 = post ? post_weight : nullptr; p.b1 = post ? post_bias : nullptr; p.w2 = pre ? pre_weight : nullptr; p.b2 = pre ? pre_bias : nullptr;
     p.gate = gate; p.w_bf16 = w_dt == RLF_BF16; p.post = post_kind; p.pre = pre_kind; p.gate_form = gate_form;
     p.alpha = alpha; p.beta = beta; p.eps = eps; p.h = h_out; p.y = y_out; p.stats = stats_out; p.T = T; p.D = D;
+    const bool bf16 = dt == RLF_BF16, full = post_kind == RLF_NORM_LAYER || pre_kind == RLF_NORM_LAYER || p.b1 || p.b2;
+    const void* const at[] = {residual, h_out, pre ? y_out : nullptr};
+    bool edge;
+    Cut c;
+    if (fast_form(bf16, T, D, at, 3, x, x_stride, &p, &edge) && pick_cut(bf16, edge, p.x_shift, true, full, T, D, p.x_shift ? 1 : 2, &c)) {
+        const BlockKernel k = kernel_of<true>(bf16, full, edge, c);
+        const int resident = k ? resident_ctas((const void*)k, c) : 0;
+        if (resident > 0) {
+            long long grid = batches(T, c, p.period);
+            if (grid > 4ll * resident) grid = 4ll * resident / p.period * p.period;
+            k<<<(unsigned)grid, c.threads, c.smem, s>>>(p);
+            count_launch();
+            return cuda_ok(cudaGetLastError());
+        }
+    }
     if (dt == RLF_BF16) block_fwd_general_kernel<__nv_bfloat16><<<row_grid(T), kGenThreads, 0, s>>>(p);
     else block_fwd_general_kernel<float><<<row_grid(T), kGenThreads, 0, s>>>(p);
     count_launch();
@@ -381,7 +919,29 @@ extern "C" rlf_status rlf_block_norm_bwd(const void* grad_y, const void* grad_h,
     float* part = static_cast<float*>(workspace);
     int parts = 0;
     const bool bf16 = dt == RLF_BF16;
-    if (T > 0 && (grad_x || grad_residual || p.dgate_row || want)) {
+    const bool any = T > 0 && (grad_x || grad_residual || p.dgate_row || want);
+    const bool full = post_kind == RLF_NORM_LAYER || pre_kind == RLF_NORM_LAYER || (want & 10) || (p.b1 && p.dgate_row);
+    const void* const at[] = {pre ? h : grad_h, grad_h, pre ? grad_y : nullptr, grad_x, grad_residual};
+    bool edge, done = false;
+    Cut c;
+    if (any && fast_form(bf16, T, D, at, 5, x, x_stride, &p, &edge) &&
+        pick_cut(bf16, edge, p.x_shift, false, full, T, D, (pre ? 2 : 0) + (grad_h ? 1 : 0) + (p.x_shift ? 0 : 1), &c)) {
+        const BlockKernel k = kernel_of<false>(bf16, full, edge, c);
+        const int resident = k ? resident_ctas((const void*)k, c) : 0;
+        if (resident > 0) {
+            long long grid = batches(T, c, p.period), most = max_parts(T, D);
+            if (most > resident) most = resident;
+            if (grid > most) grid = most / p.period * p.period;
+            parts = (int)grid;
+            p.part = part;
+            p.part_stride = part_stride(parts, D);
+            k<<<(unsigned)grid, c.threads, c.smem, s>>>(p);
+            count_launch();
+            if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
+            done = true;
+        }
+    }
+    if (any && !done) {
         if (want) p.row_sums = reinterpret_cast<float2*>(static_cast<char*>(workspace) + sums_offset(T, D));
         if (bf16) block_bwd_general_kernel<__nv_bfloat16><<<row_grid(T), kGenThreads, 0, s>>>(p);
         else block_bwd_general_kernel<float><<<row_grid(T), kGenThreads, 0, s>>>(p);
