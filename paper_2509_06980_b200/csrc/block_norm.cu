@@ -313,15 +313,55 @@ struct Stage {
     __device__ __forceinline__ void mask(int i, f2 (&v)[P]) const {
         if (EDGE && keep[i] != (1u << N) - 1u) mask_pairs<P>(v, keep[i]);
     }
-    // a function of the column, for this thread's columns (0 outside the width)
-    template <typename F> __device__ __forceinline__ void columns(f2 (&f)[NV][P], F of) const {
+    // this thread's columns of a [D] vector (0 outside the width); `none`: what stands for a vector that is not there
+    __device__ __forceinline__ void columns(f2 (&f)[NV][P], const void* w, float none) const {
+        const bool wide = !EDGE && (reinterpret_cast<uintptr_t>(w) & 15) == 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            const int c = (tid + i * th) * N - rows.lead;
+            if (wide && w != nullptr) {
+                if (!mine(i)) {
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const int c = (tid + i * th) * N + 2 * e - rows.lead;
-                f[i][e] = f2_make(c >= 0 && c < p.D ? of(c) : 0.0f, c + 1 >= 0 && c + 1 < p.D ? of(c + 1) : 0.0f);
+                    for (int e = 0; e < P; ++e) f[i][e] = 0ull;
+                } else if (p.w_bf16) {
+#pragma unroll
+                    for (int e = 0; e < P; e += 2) {
+                        const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(w) + c + 2 * e);
+                        f[i][e] = f2_make(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xffff0000u));
+                        f[i][e + 1] = f2_make(__uint_as_float(q.y << 16), __uint_as_float(q.y & 0xffff0000u));
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < P; e += 2) {
+                        const float4 q = *reinterpret_cast<const float4*>(static_cast<const float*>(w) + c + 2 * e);
+                        f[i][e] = f2_make(q.x, q.y);
+                        f[i][e + 1] = f2_make(q.z, q.w);
+                    }
+                }
+                continue;
             }
+            auto at = [&](int k) { return k < 0 || k >= p.D ? 0.0f : w ? ld_w(w, p.w_bf16, k) : none; };
+#pragma unroll
+            for (int e = 0; e < P; ++e) f[i][e] = f2_make(at(c + 2 * e), at(c + 2 * e + 1));
+        }
+    }
+    // post norm's weight (and bias) times column gate and branch scale
+    __device__ __forceinline__ void post_columns(f2 (&f)[NV][P], const void* w, float none) const {
+        columns(f, w, none);
+        if (p.gate_form == RLF_GATE_COLUMN) {
+            f2 g[NV][P];
+            columns(g, p.gate, 1.0f);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < P; ++e) f[i][e] = f2_mul(f[i][e], g[i][e]);
+        }
+        if (p.beta != 1.0f) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < P; ++e) f[i][e] = f2_mul(f[i][e], f2_make(p.beta, p.beta));
+        }
     }
 };
 __device__ __forceinline__ f2 f2_dup(float v) { return f2_make(v, v); }
@@ -355,11 +395,11 @@ block_fwd_kernel(const BlockParams p) {
     long long j0 = st.rows.first;
     fetch(j0, 0);
     f2 w1[NV][P], w2[NV][P], b1[L ? NV : 1][P], b2[L ? NV : 1][P];
-    st.columns(w1, [&](int c) { return col_scale(p, c) * post_w(p, c); });
-    st.columns(w2, [&](int c) { return p.w2 ? ld_w(p.w2, p.w_bf16, c) : 0.0f; });
+    st.post_columns(w1, p.w1, 1.0f);
+    st.columns(w2, p.w2, 0.0f);
     if constexpr (L) {
-        st.columns(b1, [&](int c) { return p.b1 ? col_scale(p, c) * ld_w(p.b1, p.w_bf16, c) : 0.0f; });
-        st.columns(b2, [&](int c) { return p.b2 ? ld_w(p.b2, p.w_bf16, c) : 0.0f; });
+        st.post_columns(b1, p.b1, 0.0f);
+        st.columns(b2, p.b2, 0.0f);
     }
     const f2 alpha = f2_dup(p.alpha);
     for (int buf = 0; j0 < st.rows.n; j0 += st.rows.step, buf ^= 1) {
@@ -505,8 +545,8 @@ block_bwd_kernel(const BlockParams p) {
     long long j0 = st.rows.first;
     fetch(j0, 0);
     f2 w1[NV][P], w2[NV][P], sum_dyu[NV][P], sum_ghv[NV][P], sum_dy[L ? NV : 1][P], sum_gh[L ? NV : 1][P];
-    st.columns(w1, [&](int c) { return col_scale(p, c) * post_w(p, c); });
-    st.columns(w2, [&](int c) { return p.w2 ? ld_w(p.w2, p.w_bf16, c) : 0.0f; });
+    st.post_columns(w1, p.w1, 1.0f);
+    st.columns(w2, p.w2, 0.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -528,55 +568,17 @@ block_bwd_kernel(const BlockParams p) {
         fetch(j0 + st.rows.step, buf ^ 1);
         cp_async_wait1();
         if (st.shift) __syncthreads();
-        auto unit = [&](int k, const f2& v, const f2& c, const f2& r) { return f2_mul(L ? f2_add(v, c) : v, r); };
-        if (pre) {
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                f2 a = 0ull, b = 0ull;
-                if (j0 + k < st.rows.n) {
-                    const f2 c = f2_dup(-m2[k]), r = f2_dup(r2[k]);
-#pragma unroll
-                    for (int i = 0; i < NV; ++i)
-                        if (st.mine(i)) {
-                            f2 dy[P], h[P];
-                            st.read(buf, k, 0, i, dy);
-                            st.read(buf, k, 1, i, h);
-#pragma unroll
-                            for (int e = 0; e < P; ++e) {
-                                const f2 q = f2_mul(dy[e], unit(k, h[e], c, r));
-                                a = f2_fma(q, w2[i][e], a);
-                                sum_dyu[i][e] = f2_add(sum_dyu[i][e], q);
-                                if (L) {
-                                    b = f2_fma(dy[e], w2[i][e], b);
-                                    sum_dy[L ? i : 0][e] = f2_add(sum_dy[L ? i : 0][e], dy[e]);
-                                }
-                            }
-                        }
-                }
-                s[k] = f2_sum(a);
-                if (L) s[L ? R + k : 0] = f2_sum(b);
-            }
-            cta_sums<K>(s, red, turn);
-        }
-        f2 gh[R][NV][P];
-        float a1[R], b1[R];
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            a1[k] = pre ? s[k] * inv_d : 0.0f;
-            b1[k] = L && p.pre == RLF_NORM_LAYER ? s[L ? R + k : 0] * inv_d : 0.0f;
-        }
+        auto unit = [&](const f2& v, const f2& c, const f2& r) { return f2_mul(L ? f2_add(v, c) : v, r); };
+        // gh: at first dh + r2 dy w2;  uv: u, then v.  Each element is unpacked once.
+        f2 gh[R][NV][P], uv[R][NV][P];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             f2 a = 0ull, b = 0ull;
             if (j0 + k < st.rows.n) {
-                const long long t = st.rows.row(j0 + k);
-                // gh = dh + r2 dy w2 - r2 b1 - (h - m2) r2^2 a1
-                const f2 c2 = f2_dup(-m2[k]), r = f2_dup(r2[k]), ra = f2_dup(-r2[k] * r2[k] * a1[k]), rb = f2_dup(-r2[k] * b1[k]);
-                const f2 c1 = f2_dup(-m1[k]), rv = f2_dup(r1[k]), g = f2_dup(gate[k]), al = f2_dup(p.alpha);
+                const f2 c = f2_dup(-m2[k]), r = f2_dup(r2[k]);
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
                     if (st.mine(i)) {
-                        f2 x[P], o[P];
                         if (p.dh) {
                             st.read(buf, k, at_dh, i, gh[k][i]);
                         } else {
@@ -584,22 +586,51 @@ block_bwd_kernel(const BlockParams p) {
                             for (int e = 0; e < P; ++e) gh[k][i][e] = 0ull;
                         }
                         if (pre) {
-                            f2 dy[P], h[P];
+                            f2 dy[P];
                             st.read(buf, k, 0, i, dy);
-                            st.read(buf, k, 1, i, h);
+                            st.read(buf, k, 1, i, uv[k][i]);
 #pragma unroll
                             for (int e = 0; e < P; ++e) {
-                                f2 d = f2_mul(f2_mul(dy[e], w2[i][e]), r);
-                                if (L) d = f2_add(d, rb);
-                                d = f2_fma(L ? f2_add(h[e], c2) : h[e], ra, d);
-                                gh[k][i][e] = f2_add(gh[k][i][e], d);
+                                const f2 u = unit(uv[k][i][e], c, r), q = f2_mul(dy[e], w2[i][e]);
+                                uv[k][i][e] = u;
+                                a = f2_fma(q, u, a);
+                                gh[k][i][e] = f2_fma(q, r, gh[k][i][e]);
+                                sum_dyu[i][e] = f2_fma(dy[e], u, sum_dyu[i][e]);
+                                if (L) {
+                                    b = f2_add(b, q);
+                                    sum_dy[L ? i : 0][e] = f2_add(sum_dy[L ? i : 0][e], dy[e]);
+                                }
                             }
                         }
+                    }
+            }
+            s[k] = f2_sum(a);
+            if (L) s[L ? R + k : 0] = f2_sum(b);
+        }
+        if (pre) cta_sums<K>(s, red, turn);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            f2 a = 0ull, b = 0ull;
+            if (j0 + k < st.rows.n) {
+                const long long t = st.rows.row(j0 + k);
+                const f2 ra = f2_dup(-r2[k] * (s[k] * inv_d)), rb = f2_dup(L && p.pre == RLF_NORM_LAYER ? -r2[k] * (s[L ? R + k : 0] * inv_d) : 0.0f);
+                const f2 c = f2_dup(-m1[k]), r = f2_dup(r1[k]), g = f2_dup(gate[k]), al = f2_dup(p.alpha);
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (st.mine(i)) {
+                        f2 x[P], o[P];
                         st.read_x(buf, k, at_x, i, t, x);
 #pragma unroll
                         for (int e = 0; e < P; ++e) {
-                            const f2 v = unit(k, x[e], c1, rv), q = f2_mul(gh[k][i][e], w1[i][e]), sg = f2_mul(gh[k][i][e], g);
-                            o[e] = f2_mul(gh[k][i][e], al);
+                            f2 d = gh[k][i][e];
+                            if (pre) {
+                                d = f2_fma(uv[k][i][e], ra, d);
+                                if (L) d = f2_add(d, rb);
+                            }
+                            const f2 v = unit(x[e], c, r), q = f2_mul(d, w1[i][e]), sg = f2_mul(d, g);
+                            gh[k][i][e] = d;
+                            uv[k][i][e] = v;
+                            o[e] = f2_mul(d, al);
                             a = f2_fma(q, v, a);
                             sum_ghv[i][e] = f2_fma(sg, v, sum_ghv[i][e]);
                             if (L) {
@@ -650,19 +681,18 @@ block_bwd_kernel(const BlockParams p) {
         for (int k = 0; k < R; ++k) {
             if (j0 + k >= st.rows.n) continue;
             const long long t = st.rows.row(j0 + k);
-            // gate r1 (gh w1 - b - (x - m1) r1 a)
+            // gate r1 (gh w1 - b - v a)
             const float gr = gate[k] * r1[k], a = post ? s[k] * inv_d : 0.0f, b = L && p.post == RLF_NORM_LAYER ? s[L ? R + k : 0] * inv_d : 0.0f;
-            const f2 r = f2_dup(gr), ra = f2_dup(-gr * r1[k] * a), rb = f2_dup(-gr * b), c = f2_dup(-m1[k]);
+            const f2 r = f2_dup(gr), ra = f2_dup(-gr * a), rb = f2_dup(-gr * b);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (st.mine(i)) {
-                    f2 x[P], o[P];
-                    st.read_x(buf, k, at_x, i, t, x);
+                    f2 o[P];
 #pragma unroll
                     for (int e = 0; e < P; ++e) {
                         o[e] = f2_mul(f2_mul(gh[k][i][e], w1[i][e]), r);
                         if (L) o[e] = f2_add(o[e], rb);
-                        o[e] = f2_fma(L ? f2_add(x[e], c) : x[e], ra, o[e]);
+                        o[e] = f2_fma(uv[k][i][e], ra, o[e]);
                     }
                     st.store(p.dx, t, i, o);
                 }
