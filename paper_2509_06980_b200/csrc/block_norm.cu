@@ -229,7 +229,7 @@ block_finish_kernel(const Finish f) {
     for (int k = 0; k < 2; ++k) {
         if (col < f.D && ((f.want >> (first + k)) & 1)) {
             const float* src = f.part + (first + k) * f.part_stride + col;
-#pragma unroll 4
+#pragma unroll 8
             for (int r = warp; r < f.parts; r += 32) s[k] += src[(long long)r * f.D];
         }
         acc[k][warp][lane] = s[k];
@@ -287,6 +287,14 @@ struct Stage {
         for (int i = 0; i < NV; ++i)
             if (mine(i)) rows.copy(slot(buf, k, a, i), static_cast<const T*>(tensor) + t * stride, tid + i * th, p.D, t == 0);
     }
+    // Slots that no copy writes (of threads without a vector i, or of a tensor that is not there) hold zeros, so that the
+    // arithmetic needs no conditions: under conditions the values carried from pass to pass cost more moves than arithmetic.
+    __device__ __forceinline__ void clear(int a, bool all) const {
+        for (int q = 0; q < 2 * R; ++q)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (all || !mine(i)) *slot(0, q, a, i) = make_uint4(0u, 0u, 0u, 0u);
+    }
     // x goes into array a, or to its own place
     __device__ __forceinline__ void copy_x(int buf, int k, int a, long long t) const {
         if (shift) copy_row<T>(shifted + (buf * R + k) * pitch, static_cast<const T*>(p.x) + t * p.x_stride, p.D, t == 0);
@@ -310,8 +318,15 @@ struct Stage {
     __device__ __forceinline__ void store(void* tensor, long long t, int i, const f2 (&v)[P]) const {
         rows.store(static_cast<T*>(tensor) + t * p.D, tid + i * th, Vec<T>::pack(v), keep[i]);
     }
+    // zeros outside the row
     __device__ __forceinline__ void mask(int i, f2 (&v)[P]) const {
-        if (EDGE && keep[i] != (1u << N) - 1u) mask_pairs<P>(v, keep[i]);
+        if constexpr (EDGE) {
+            if (keep[i] != (1u << N) - 1u) mask_pairs<P>(v, keep[i]);
+        } else {
+            const bool in = mine(i);
+#pragma unroll
+            for (int e = 0; e < P; ++e) v[e] = in ? v[e] : 0ull;
+        }
     }
     // this thread's columns of a [D] vector (0 outside the width); `none`: what stands for a vector that is not there
     __device__ __forceinline__ void columns(f2 (&f)[NV][P], const void* w, float none) const {
@@ -364,6 +379,40 @@ struct Stage {
         }
     }
 };
+// K sums over the CTA of at most W warps, the same in every thread afterwards (one barrier; `red` holds two halves of [K][W]
+// floats used in turn, zeros where a warp is missing).  W is known to the compiler: reading the warps' parts in a loop cost
+// more instructions than the rest of a short row.
+template <int K, int W>
+__device__ __forceinline__ void row_sums(float (&v)[K], float* red, int& turn) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    if (blockDim.x == 32) return;
+    float* r = red + turn * K * W;
+    turn ^= 1;
+    if (lane == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) r[k * W + warp] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        f2 a = 0ull;
+#pragma unroll
+        for (int q = 0; q < W / 4; ++q) {
+            const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(r + k * W + 4 * q);
+            a = f2_add(a, f2_add(x.x, x.y));
+        }
+        v[k] = f2_sum(a);
+    }
+}
+template <int N>
+__device__ __forceinline__ void clear_sums(float (&red)[N]) {
+    for (int i = threadIdx.x; i < N; i += blockDim.x) red[i] = 0.0f;
+    __syncthreads();
+}
+
 __device__ __forceinline__ f2 f2_dup(float v) { return f2_make(v, v); }
 
 // L: a mean or a bias is in it somewhere (the RMS norms without bias keep no registers for them)
@@ -373,11 +422,14 @@ block_fwd_kernel(const BlockParams p) {
     using V = Vec<T>;
     constexpr int P = V::P;
     extern __shared__ __align__(16) uint4 smem[];       // residual, x (where it is like the others)
-    __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * R];
+    __shared__ __align__(16) float red[2 * (MAXT / 32) * R];
     int turn = 0;
+    clear_sums(red);
     const Stage<T, NV, R, EDGE> st(p, smem, p.res, EDGE && p.x_shift ? 1 : 2);
     const float inv_d = 1.0f / (float)p.D;
     const bool post = has_norm(p.post), pre = has_norm(p.pre);
+    st.clear(0, false);
+    if (!st.shift) st.clear(1, false);
     float gate_next[R];
     auto fetch = [&](long long j0, int buf) {
 #pragma unroll
@@ -420,12 +472,11 @@ block_fwd_kernel(const BlockParams p) {
                     f2 q = 0ull;
 #pragma unroll
                     for (int i = 0; i < NV; ++i)
-                        if (st.mine(i))
 #pragma unroll
-                            for (int e = 0; e < P; ++e) q = f2_add(q, v[k][i][e]);
+                        for (int e = 0; e < P; ++e) q = f2_add(q, v[k][i][e]);
                     s[k] = f2_sum(q);
                 }
-                cta_sums<R>(s, red, turn);
+                row_sums<R, MAXT / 32>(s, red, turn);
             }
 #pragma unroll
             for (int k = 0; k < R; ++k) {
@@ -433,18 +484,17 @@ block_fwd_kernel(const BlockParams p) {
                 const f2 c = f2_dup(-m[k]);
                 f2 q = 0ull;
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (st.mine(i)) {
-                        f2 d[P];
+                for (int i = 0; i < NV; ++i) {
+                    f2 d[P];
 #pragma unroll
-                        for (int e = 0; e < P; ++e) d[e] = L ? f2_add(v[k][i][e], c) : v[k][i][e];
-                        if (L) st.mask(i, d);
+                    for (int e = 0; e < P; ++e) d[e] = L ? f2_add(v[k][i][e], c) : v[k][i][e];
+                    if (L) st.mask(i, d);
 #pragma unroll
-                        for (int e = 0; e < P; ++e) q = f2_fma(d[e], d[e], q);
-                    }
+                    for (int e = 0; e < P; ++e) q = f2_fma(d[e], d[e], q);
+                }
                 s[k] = f2_sum(q);
             }
-            cta_sums<R>(s, red, turn);
+            row_sums<R, MAXT / 32>(s, red, turn);
 #pragma unroll
             for (int k = 0; k < R; ++k) r[k] = rsqrtf(s[k] * inv_d + p.eps);
         };
@@ -454,25 +504,23 @@ block_fwd_kernel(const BlockParams p) {
             r1[k] = r2[k] = 1.0f;
             const long long t = st.rows.row(min(j0 + k, st.rows.n - 1));
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (st.mine(i)) st.read_x(buf, k, 1, i, t, v[k][i]);
+            for (int i = 0; i < NV; ++i) st.read_x(buf, k, 1, i, t, v[k][i]);
         }
         if (post) stats(p.post == RLF_NORM_LAYER, m1, r1);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             const f2 c = f2_dup(-m1[k]), r = f2_dup(r1[k] * gate[k]), g = f2_dup(gate[k]);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (st.mine(i)) {
-                    f2 res[P];
-                    st.read(buf, k, 0, i, res);
+            for (int i = 0; i < NV; ++i) {
+                f2 res[P];
+                st.read(buf, k, 0, i, res);
 #pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        f2 n = f2_mul(f2_mul(L ? f2_add(v[k][i][e], c) : v[k][i][e], r), w1[i][e]);
-                        if (L) n = f2_fma(g, b1[L ? i : 0][e], n);
-                        v[k][i][e] = f2_fma(alpha, res[e], n);
-                    }
+                for (int e = 0; e < P; ++e) {
+                    f2 n = f2_mul(f2_mul(L ? f2_add(v[k][i][e], c) : v[k][i][e], r), w1[i][e]);
+                    if (L) n = f2_fma(g, b1[L ? i : 0][e], n);
+                    v[k][i][e] = f2_fma(alpha, res[e], n);
                 }
+            }
         }
         if (pre) stats(p.pre == RLF_NORM_LAYER, m2, r2);
 #pragma unroll
@@ -481,19 +529,18 @@ block_fwd_kernel(const BlockParams p) {
             const long long t = st.rows.row(j0 + k);
             const f2 c = f2_dup(-m2[k]), r = f2_dup(r2[k]);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                f2 o[P];
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    o[e] = f2_mul(f2_mul(L ? f2_add(v[k][i][e], c) : v[k][i][e], r), w2[i][e]);
+                    if (L) o[e] = f2_add(o[e], b2[L ? i : 0][e]);
+                }
                 if (st.mine(i)) {
                     st.store(p.h, t, i, v[k][i]);
-                    if (pre) {
-                        f2 o[P];
-#pragma unroll
-                        for (int e = 0; e < P; ++e) {
-                            o[e] = f2_mul(f2_mul(L ? f2_add(v[k][i][e], c) : v[k][i][e], r), w2[i][e]);
-                            if (L) o[e] = f2_add(o[e], b2[L ? i : 0][e]);
-                        }
-                        st.store(p.y, t, i, o);
-                    }
+                    if (pre) st.store(p.y, t, i, o);
                 }
+            }
             if (st.tid == 0 && p.stats) {
                 p.stats[t] = m1[k];
                 p.stats[p.T + t] = r1[k];
@@ -505,48 +552,76 @@ block_fwd_kernel(const BlockParams p) {
     cp_async_wait0();
 }
 
-// Backward: two sums per row one after the other (the second needs gh, which needs the first), gh held in registers in between; the
-// sums over tokens are added up row after row in registers and leave as one partial row per CTA.
-template <typename T, int NV, int R, bool L, bool EDGE, int MAXT>
-__global__ void __launch_bounds__(MAXT)
+// Backward, one row at a time: two sums per row one after the other (the second needs gh, which needs the first); what the later
+// passes need is held in registers, so that each element is unpacked once.  The sums over tokens are added up row after row in
+// registers and leave as one partial row per CTA.
+template <typename T, int NV, bool L, bool EDGE, int MAXT>
+__global__ void __launch_bounds__(MAXT, L && MAXT <= 256 ? 512 / MAXT : 0)
 block_bwd_kernel(const BlockParams p) {
     using V = Vec<T>;
-    constexpr int P = V::P, N = V::N, K = L ? 2 * R : R;
-    extern __shared__ __align__(16) uint4 smem[];       // dy, h (with the pre norm), dh (if given), x (where it is like the others)
-    __shared__ __align__(16) float red[2 * (kMaxThreads / 32) * K];
+    constexpr int P = V::P, N = V::N, K = L ? 2 : 1, W = MAXT / 32;
+    constexpr bool WS = L;                              // the weights live in shared memory (a thread's own columns), not in registers
+    extern __shared__ __align__(16) uint4 smem[];       // dh, dy, h (zeros for what is not there), x (where it is like the others)
+    __shared__ __align__(16) float red[2 * W * K];
     int turn = 0;
+    clear_sums(red);
     const bool post = has_norm(p.post), pre = has_norm(p.pre);
-    const int at_dh = pre ? 2 : 0, at_x = at_dh + (p.dh ? 1 : 0);
-    const Stage<T, NV, R, EDGE> st(p, smem, pre ? p.h : p.dh, at_x + (EDGE && p.x_shift ? 0 : 1));
+    const Stage<T, NV, 1, EDGE> st(p, smem, pre ? p.h : p.dh, EDGE && p.x_shift ? 3 : 4);
     const float inv_d = 1.0f / (float)p.D;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    float next[R][5];                                   // the rows' statistics and gate
-    auto fetch = [&](long long j0, int buf) {
+    st.clear(0, p.dh == nullptr);
+    st.clear(1, !pre);
+    st.clear(2, !pre);
+    if (!st.shift) st.clear(3, false);
+    float next[5];                                      // the row's statistics and gate
+    auto fetch = [&](long long j, int buf) {
+        if (j < st.rows.n) {
+            const long long t = st.rows.row(j);
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-#pragma unroll
-            for (int q = 0; q < 5; ++q) next[k][q] = 0.0f;
-            if (j0 + k < st.rows.n) {
-                const long long t = st.rows.row(j0 + k);
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (L || (q & 1)) next[k][q] = p.stats[q * p.T + t];
-                next[k][4] = row_gate(p, t);
-                if (pre) {
-                    st.copy(buf, k, 0, p.dy, p.D, t);
-                    st.copy(buf, k, 1, p.h, p.D, t);
-                }
-                if (p.dh) st.copy(buf, k, at_dh, p.dh, p.D, t);
-                st.copy_x(buf, k, at_x, t);
+            for (int q = 0; q < 4; ++q)
+                if (L || (q & 1)) next[q] = p.stats[q * p.T + t];
+            next[4] = row_gate(p, t);
+            if (p.dh) st.copy(buf, 0, 0, p.dh, p.D, t);
+            if (pre) {
+                st.copy(buf, 0, 1, p.dy, p.D, t);
+                st.copy(buf, 0, 2, p.h, p.D, t);
             }
+            st.copy_x(buf, 0, 3, t);
         }
         cp_async_commit();
     };
-    long long j0 = st.rows.first;
-    fetch(j0, 0);
-    f2 w1[NV][P], w2[NV][P], sum_dyu[NV][P], sum_ghv[NV][P], sum_dy[L ? NV : 1][P], sum_gh[L ? NV : 1][P];
-    st.post_columns(w1, p.w1, 1.0f);
-    st.columns(w2, p.w2, 0.0f);
+    long long j = st.rows.first;
+    fetch(j, 0);
+    f2 w1[WS ? 1 : NV][P], w2[WS ? 1 : NV][P], sum_dyu[NV][P], sum_ghv[NV][P], sum_dy[L ? NV : 1][P], sum_gh[L ? NV : 1][P];
+    ulonglong2* const w_s = reinterpret_cast<ulonglong2*>(st.shifted + (st.shift ? 2 * st.pitch : 0)) + st.tid;    // [2][NV][P / 2][threads]
+    if constexpr (WS) {
+        f2 w[NV][P];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (k == 0) st.post_columns(w, p.w1, 1.0f);
+            else st.columns(w, p.w2, 0.0f);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < P / 2; ++e) w_s[((k * NV + i) * (P / 2) + e) * st.th] = make_ulonglong2(w[i][2 * e], w[i][2 * e + 1]);
+        }
+    } else {
+        st.post_columns(w1, p.w1, 1.0f);
+        st.columns(w2, p.w2, 0.0f);
+    }
+    auto weights = [&](int k, int i, f2 (&w)[P]) {
+        if constexpr (WS) {
+#pragma unroll
+            for (int e = 0; e < P / 2; ++e) {
+                const ulonglong2 q = w_s[((k * NV + i) * (P / 2) + e) * st.th];
+                w[2 * e] = q.x;
+                w[2 * e + 1] = q.y;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < P; ++e) w[e] = k == 0 ? w1[WS ? 0 : i][e] : w2[WS ? 0 : i][e];
+        }
+    };
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -554,148 +629,103 @@ block_bwd_kernel(const BlockParams p) {
             sum_dyu[i][e] = sum_ghv[i][e] = 0ull;
             if (L) sum_dy[L ? i : 0][e] = sum_gh[L ? i : 0][e] = 0ull;
         }
-    for (int buf = 0; j0 < st.rows.n; j0 += st.rows.step, buf ^= 1) {
-        float m1[R], r1[R], m2[R], r2[R], gate[R], s[K];
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            m1[k] = next[k][0];
-            r1[k] = next[k][1];
-            m2[k] = next[k][2];
-            r2[k] = next[k][3];
-            gate[k] = next[k][4];
-        }
+    for (int buf = 0; j < st.rows.n; j += st.rows.step, buf ^= 1) {
+        const long long t = st.rows.row(j);
+        const float m1 = next[0], r1 = next[1], m2 = next[2], r2 = next[3], gate = next[4];
         if (st.shift) __syncthreads();
-        fetch(j0 + st.rows.step, buf ^ 1);
+        fetch(j + st.rows.step, buf ^ 1);
         cp_async_wait1();
         if (st.shift) __syncthreads();
         auto unit = [&](const f2& v, const f2& c, const f2& r) { return f2_mul(L ? f2_add(v, c) : v, r); };
-        // gh: at first dh + r2 dy w2;  uv: u, then v.  Each element is unpacked once.
-        f2 gh[R][NV][P], uv[R][NV][P];
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
+        // gh: at first dh + r2 dy w2;  uv: u, then v
+        f2 gh[NV][P], uv[NV][P];
+        float s[K];
+        {
             f2 a = 0ull, b = 0ull;
-            if (j0 + k < st.rows.n) {
-                const f2 c = f2_dup(-m2[k]), r = f2_dup(r2[k]);
+            const f2 c = f2_dup(-m2), r = f2_dup(r2);
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (st.mine(i)) {
-                        if (p.dh) {
-                            st.read(buf, k, at_dh, i, gh[k][i]);
-                        } else {
+            for (int i = 0; i < NV; ++i) {
+                f2 dy[P], w[P];
+                weights(1, i, w);
+                st.read(buf, 0, 0, i, gh[i]);
+                st.read(buf, 0, 1, i, dy);
+                st.read(buf, 0, 2, i, uv[i]);
 #pragma unroll
-                            for (int e = 0; e < P; ++e) gh[k][i][e] = 0ull;
-                        }
-                        if (pre) {
-                            f2 dy[P];
-                            st.read(buf, k, 0, i, dy);
-                            st.read(buf, k, 1, i, uv[k][i]);
-#pragma unroll
-                            for (int e = 0; e < P; ++e) {
-                                const f2 u = unit(uv[k][i][e], c, r), q = f2_mul(dy[e], w2[i][e]);
-                                uv[k][i][e] = u;
-                                a = f2_fma(q, u, a);
-                                gh[k][i][e] = f2_fma(q, r, gh[k][i][e]);
-                                sum_dyu[i][e] = f2_fma(dy[e], u, sum_dyu[i][e]);
-                                if (L) {
-                                    b = f2_add(b, q);
-                                    sum_dy[L ? i : 0][e] = f2_add(sum_dy[L ? i : 0][e], dy[e]);
-                                }
-                            }
-                        }
+                for (int e = 0; e < P; ++e) {
+                    const f2 u = unit(uv[i][e], c, r), q = f2_mul(dy[e], w[e]);
+                    uv[i][e] = u;
+                    a = f2_fma(q, u, a);
+                    gh[i][e] = f2_fma(q, r, gh[i][e]);
+                    sum_dyu[i][e] = f2_fma(dy[e], u, sum_dyu[i][e]);
+                    if (L) {
+                        b = f2_add(b, q);
+                        sum_dy[L ? i : 0][e] = f2_add(sum_dy[L ? i : 0][e], dy[e]);
                     }
-            }
-            s[k] = f2_sum(a);
-            if (L) s[L ? R + k : 0] = f2_sum(b);
-        }
-        if (pre) cta_sums<K>(s, red, turn);
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            f2 a = 0ull, b = 0ull;
-            if (j0 + k < st.rows.n) {
-                const long long t = st.rows.row(j0 + k);
-                const f2 ra = f2_dup(-r2[k] * (s[k] * inv_d)), rb = f2_dup(L && p.pre == RLF_NORM_LAYER ? -r2[k] * (s[L ? R + k : 0] * inv_d) : 0.0f);
-                const f2 c = f2_dup(-m1[k]), r = f2_dup(r1[k]), g = f2_dup(gate[k]), al = f2_dup(p.alpha);
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (st.mine(i)) {
-                        f2 x[P], o[P];
-                        st.read_x(buf, k, at_x, i, t, x);
-#pragma unroll
-                        for (int e = 0; e < P; ++e) {
-                            f2 d = gh[k][i][e];
-                            if (pre) {
-                                d = f2_fma(uv[k][i][e], ra, d);
-                                if (L) d = f2_add(d, rb);
-                            }
-                            const f2 v = unit(x[e], c, r), q = f2_mul(d, w1[i][e]), sg = f2_mul(d, g);
-                            gh[k][i][e] = d;
-                            uv[k][i][e] = v;
-                            o[e] = f2_mul(d, al);
-                            a = f2_fma(q, v, a);
-                            sum_ghv[i][e] = f2_fma(sg, v, sum_ghv[i][e]);
-                            if (L) {
-                                b = f2_add(b, q);
-                                sum_gh[L ? i : 0][e] = f2_add(sum_gh[L ? i : 0][e], sg);
-                            }
-                        }
-                        if (p.dres) st.store(p.dres, t, i, o);
-                    }
-            }
-            s[k] = f2_sum(a);
-            if (L) s[L ? R + k : 0] = f2_sum(b);
-        }
-        if (!post && !p.dgate_row) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) s[k] = 0.0f;
-        } else {
-            cta_sums<K>(s, red, turn);
-        }
-        if (p.dgate_row) {
-            float c[R];
-#pragma unroll
-            for (int k = 0; k < R; ++k) c[k] = 0.0f;
-            if (L && p.b1) {
-#pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    if (j0 + k >= st.rows.n) continue;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i)
-                        if (st.mine(i))
-#pragma unroll
-                            for (int e = 0; e < P; ++e) {
-                                const int col = (st.tid + i * st.th) * N + 2 * e - st.rows.lead;
-                                float lo, hi;
-                                f2_split(gh[k][i][e], lo, hi);
-                                if (col >= 0 && col < p.D) c[k] = fmaf(lo, p.beta * ld_w(p.b1, p.w_bf16, col), c[k]);
-                                if (col + 1 >= 0 && col + 1 < p.D) c[k] = fmaf(hi, p.beta * ld_w(p.b1, p.w_bf16, col + 1), c[k]);
-                            }
                 }
-                cta_sums<R>(c, red, turn);
             }
-#pragma unroll
-            for (int k = 0; k < R; ++k)
-                if (st.tid == 0 && j0 + k < st.rows.n) p.dgate_row[st.rows.row(j0 + k)] = s[k] + c[k];
+            s[0] = f2_sum(a);
+            if (L) s[K - 1] = f2_sum(b);
         }
-        if (p.dx == nullptr) continue;
+        if (pre) row_sums<K, W>(s, red, turn);
+        float bias_sum = 0.0f;
+        {
+            f2 a = 0ull, b = 0ull;
+            const f2 ra = f2_dup(-r2 * (s[0] * inv_d)), rb = f2_dup(L && p.pre == RLF_NORM_LAYER ? -r2 * (s[K - 1] * inv_d) : 0.0f);
+            const f2 c = f2_dup(-m1), r = f2_dup(r1), g = f2_dup(gate), al = f2_dup(p.alpha);
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-            if (j0 + k >= st.rows.n) continue;
-            const long long t = st.rows.row(j0 + k);
-            // gate r1 (gh w1 - b - v a)
-            const float gr = gate[k] * r1[k], a = post ? s[k] * inv_d : 0.0f, b = L && p.post == RLF_NORM_LAYER ? s[L ? R + k : 0] * inv_d : 0.0f;
-            const f2 r = f2_dup(gr), ra = f2_dup(-gr * a), rb = f2_dup(-gr * b);
+            for (int i = 0; i < NV; ++i) {
+                f2 x[P], d[P], o[P], w[P];
+                weights(0, i, w);
+                st.read_x(buf, 0, 3, i, t, x);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (st.mine(i)) {
-                    f2 o[P];
+                for (int e = 0; e < P; ++e) {
+                    d[e] = f2_fma(uv[i][e], ra, gh[i][e]);
+                    if (L) d[e] = f2_add(d[e], rb);
+                    const f2 v = unit(x[e], c, r), q = f2_mul(d[e], w[e]), sg = f2_mul(d[e], g);
+                    gh[i][e] = q;                       // (all that is left to do needs gh w)
+                    uv[i][e] = v;
+                    o[e] = f2_mul(d[e], al);
+                    a = f2_fma(q, v, a);
+                    sum_ghv[i][e] = f2_fma(sg, v, sum_ghv[i][e]);
+                    if (L) {
+                        b = f2_add(b, q);
+                        sum_gh[L ? i : 0][e] = f2_add(sum_gh[L ? i : 0][e], sg);
+                    }
+                }
+                if (p.dres && st.mine(i)) st.store(p.dres, t, i, o);
+                if (L && p.dgate_row && p.b1) {
 #pragma unroll
                     for (int e = 0; e < P; ++e) {
-                        o[e] = f2_mul(f2_mul(gh[k][i][e], w1[i][e]), r);
-                        if (L) o[e] = f2_add(o[e], rb);
-                        o[e] = f2_fma(uv[k][i][e], ra, o[e]);
+                        const int col = (st.tid + i * st.th) * N + 2 * e - st.rows.lead;
+                        float lo, hi;
+                        f2_split(d[e], lo, hi);
+                        if (col >= 0 && col < p.D) bias_sum = fmaf(lo, ld_w(p.b1, p.w_bf16, col), bias_sum);
+                        if (col + 1 >= 0 && col + 1 < p.D) bias_sum = fmaf(hi, ld_w(p.b1, p.w_bf16, col + 1), bias_sum);
                     }
-                    st.store(p.dx, t, i, o);
                 }
+            }
+            s[0] = f2_sum(a);
+            if (L) s[K - 1] = f2_sum(b);
+        }
+        if (post || p.dgate_row) row_sums<K, W>(s, red, turn);
+        if (p.dgate_row) {
+            if (L && p.b1) {
+                float c[K] = {bias_sum};
+                row_sums<K, W>(c, red, turn);
+                bias_sum = c[0];
+            }
+            if (st.tid == 0) p.dgate_row[t] = fmaf(p.beta, bias_sum, s[0]);
+        }
+        if (p.dx == nullptr) continue;
+        // gate r1 (gh w1 - b - v a)
+        const float gr = gate * r1, a = post ? s[0] * inv_d : 0.0f, b = L && p.post == RLF_NORM_LAYER ? s[K - 1] * inv_d : 0.0f;
+        const f2 r = f2_dup(gr), ra = f2_dup(-gr * a), rb = f2_dup(-gr * b);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            f2 o[P];
+#pragma unroll
+            for (int e = 0; e < P; ++e) o[e] = f2_fma(uv[i][e], ra, L ? f2_fma(gh[i][e], r, rb) : f2_mul(gh[i][e], r));
+            if (st.mine(i)) st.store(p.dx, t, i, o);
         }
     }
     cp_async_wait0();
@@ -737,47 +767,56 @@ static size_t sums_offset(long long T, int D) { return 4 * (size_t)part_stride(m
 struct Cut { int nv, threads, rows, smem, max_threads; };
 
 // false: no fast form holds the rows (rows shorter than a vector, or longer than 8192 elements).  `arrays` rows are read per
-// row besides a shifted x.
+// row besides a shifted x.  Up to 128 threads of one vector, then of two (fp32: four) vectors each; the backward of long bf16 rows
+// four vectors on up to 256 threads (10240 x 8192 RMS 178 us with two on 512, 167 with four).  Forward two rows at a time
+// where a CTA has up to 256 threads (8191 x 4096 layer form 61 us with one, 53 with two).
 static bool pick_cut(bool bf16, bool edge, bool shift, bool fwd, bool full, long long T, int D, int arrays, Cut* c) {
     const int esz = bf16 ? 2 : 4, v = 16 / esz;
     if (D < v || D > 8192) return false;
-    const int nvec = edge ? (D + 2 * v - 2) / v : D / v, most_nv = bf16 ? 2 : 4;
+    const int nvec = edge ? (D + 2 * v - 2) / v : D / v;
+    const int most_nv = bf16 && (fwd || nvec <= 512) ? 2 : 4;
     c->nv = 1;
-    while ((nvec + c->nv - 1) / c->nv > (fwd ? 128 : 128) && c->nv < most_nv) c->nv *= 2;
+    while ((nvec + c->nv - 1) / c->nv > 128 && c->nv < most_nv) c->nv *= 2;
     c->threads = ((nvec + c->nv - 1) / c->nv + 31) / 32 * 32;
-    c->max_threads = c->threads <= 256 ? 256 : 512;
-    if (c->threads > 512) return false;
-    c->rows = c->max_threads == 512 ? 1 : 2;
-    (void)full;
+    if (c->threads > 512) return false;                    // (rows of 8192 on no boundary)
+    c->max_threads = c->threads <= 128 ? 128 : c->threads <= 256 ? 256 : 512;
+    if (!fwd && bf16 && c->max_threads == 512) return false;
+    c->rows = !fwd || c->max_threads == 512 ? 1 : 2;
     while (c->rows > 1 && T < 148ll * 4 * c->rows) c->rows /= 2;      // too few rows to put several on a CTA
     for (;; c->rows /= 2) {
         c->smem = 2 * c->rows * (arrays * c->nv * c->threads * 16 + (shift ? staged_pitch(D, esz) : 0));
+        if (!fwd && full) c->smem += 2 * c->nv * c->threads * v * 4;         // the weights
         if (c->smem <= (c->rows > 1 ? kSmemLimit / 2 : kSmemLimit)) return true;
         if (c->rows == 1) return false;
     }
 }
 
 typedef void (*BlockKernel)(const BlockParams);
-#define RLF_BLOCK_FORM(nv_, rows_, max_) \
-    if (c.nv == nv_ && c.rows == rows_ && c.max_threads == max_) return FWD ? block_fwd_kernel<T, nv_, rows_, L, EDGE, max_> : block_bwd_kernel<T, nv_, rows_, L, EDGE, max_>
+template <typename T, int NV, bool L, bool EDGE, int MAXT>
+static BlockKernel fwd_form(const Cut& c) {
+    if constexpr (MAXT < 512) {
+        if (c.rows == 2) return block_fwd_kernel<T, NV, 2, L, EDGE, MAXT>;
+    }
+    return block_fwd_kernel<T, NV, 1, L, EDGE, MAXT>;
+}
+template <bool FWD, typename T, int NV, bool L, bool EDGE, int MAXT>
+static BlockKernel form(const Cut& c) {
+    if constexpr (FWD) return fwd_form<T, NV, L, EDGE, MAXT>(c);
+    else return block_bwd_kernel<T, NV, L, EDGE, MAXT>;
+}
 template <bool FWD, typename T, bool L, bool EDGE>
 static BlockKernel kernel_form(const Cut& c) {
-    RLF_BLOCK_FORM(1, 1, 256);
-    RLF_BLOCK_FORM(1, 2, 256);
+    if (c.nv == 1) return form<FWD, T, 1, L, EDGE, 128>(c);
+    if (c.nv == 2 && c.max_threads == 128) return form<FWD, T, 2, L, EDGE, 128>(c);
     if constexpr (sizeof(T) == 2) {
-        RLF_BLOCK_FORM(2, 1, 256);
-        RLF_BLOCK_FORM(2, 2, 256);
-        RLF_BLOCK_FORM(2, 1, 512);
+        if (c.nv == 2) return FWD && c.max_threads == 512 ? form<true, T, 2, L, EDGE, 512>(c) : form<FWD, T, 2, L, EDGE, 256>(c);
+        if constexpr (!FWD) return form<false, T, 4, L, EDGE, 256>(c);
     } else {
-        RLF_BLOCK_FORM(2, 1, 256);
-        RLF_BLOCK_FORM(2, 2, 256);
-        RLF_BLOCK_FORM(4, 1, 256);
-        RLF_BLOCK_FORM(4, 2, 256);
-        RLF_BLOCK_FORM(4, 1, 512);
+        if (c.max_threads == 128) return form<FWD, T, 4, L, EDGE, 128>(c);
+        return c.max_threads == 256 ? form<FWD, T, 4, L, EDGE, 256>(c) : form<FWD, T, 4, L, EDGE, 512>(c);
     }
     return nullptr;
 }
-#undef RLF_BLOCK_FORM
 template <bool FWD>
 static BlockKernel kernel_of(bool bf16, bool full, bool edge, const Cut& c) {
     if (bf16) {
@@ -896,7 +935,12 @@ extern "C" rlf_status rlf_block_norm_fwd(const void* x, int64_t x_stride, const 
         const int resident = k ? resident_ctas((const void*)k, c) : 0;
         if (resident > 0) {
             long long grid = batches(T, c, p.period);
-            if (grid > 4ll * resident) grid = 4ll * resident / p.period * p.period;
+            // RMS: CTAs that retire early, up to eight generations of them, keep the loads of some under the stores of others (32768 x 2560
+            // bf16: 125 us as one generation, 111 as four, 104 as eight); with means and biases a CTA's start costs more than that
+            // gains (8191 x 4096 layer form 53 us as one, 61 as four)
+            long long gens = full ? 1 : grid / (4ll * resident);
+            gens = gens < 1 ? 1 : gens > 8 ? 8 : gens;
+            if (grid > gens * resident) grid = gens * resident / p.period * p.period;
             k<<<(unsigned)grid, c.threads, c.smem, s>>>(p);
             count_launch();
             return cuda_ok(cudaGetLastError());
@@ -955,7 +999,7 @@ extern "C" rlf_status rlf_block_norm_bwd(const void* grad_y, const void* grad_h,
     bool edge, done = false;
     Cut c;
     if (any && fast_form(bf16, T, D, at, 5, x, x_stride, &p, &edge) &&
-        pick_cut(bf16, edge, p.x_shift, false, full, T, D, (pre ? 2 : 0) + (grad_h ? 1 : 0) + (p.x_shift ? 0 : 1), &c)) {
+        pick_cut(bf16, edge, p.x_shift, false, full, T, D, p.x_shift ? 3 : 4, &c)) {
         const BlockKernel k = kernel_of<false>(bf16, full, edge, c);
         const int resident = k ? resident_ctas((const void*)k, c) : 0;
         if (resident > 0) {
