@@ -262,6 +262,7 @@ block_finish_kernel(const Finish f) {
 // every period-th row, whose places in their vectors are the same, and a row's first and last vector are masked.  The rows of
 // x, whose stride is its own, may sit otherwise (x_shift): they are copied as the aligned chunks that cover them and read by
 // element.
+__host__ __device__ constexpr int shifted_pitch(int D, int esz) { return staged_pitch(D, esz) + 48; }     // (read from 16 before to 32 behind)
 template <typename T, int NV, int R, bool EDGE>
 struct Stage {
     static constexpr int P = Vec<T>::P, N = Vec<T>::N;
@@ -271,14 +272,35 @@ struct Stage {
     char* shifted;                  // [2][R] rows of x
     int arrays, pitch, th, tid;
     bool shift;
-    unsigned keep[NV];
+    unsigned keep[NV];              // which elements of a vector are the row's
     __device__ __forceinline__ Stage(const BlockParams& p_, uint4* smem, const void* dense, int arrays_)
         : p(p_), rows(dense, p_.D, p_.T, p_.D, p_.period, R), slots(smem), arrays(arrays_), th(blockDim.x), tid(threadIdx.x) {
         shift = EDGE && p.x_shift;
-        pitch = staged_pitch(p.D, (int)sizeof(T));
+        pitch = shifted_pitch(p.D, (int)sizeof(T));
         shifted = reinterpret_cast<char*>(smem + 2 * R * arrays * NV * th);
 #pragma unroll
         for (int i = 0; i < NV; ++i) keep[i] = EDGE ? rows.bits(tid + i * th, p.D) : (1u << N) - 1u;
+    }
+    // a first or last vector that other elements than the row's are in
+    __device__ __forceinline__ bool partial(int i) const { return EDGE && keep[i] != (1u << N) - 1u; }
+    __device__ __forceinline__ uint4 masked(uint4 q, int i) const {
+        auto word = [&](int k) {
+            if (N == 4) return (keep[i] >> k) & 1u ? 0xffffffffu : 0u;
+            return ((keep[i] >> (2 * k)) & 1u ? 0xffffu : 0u) | ((keep[i] >> (2 * k + 1)) & 1u ? 0xffff0000u : 0u);
+        };
+        return make_uint4(q.x & word(0), q.y & word(1), q.z & word(2), q.w & word(3));
+    }
+    // what lies outside the rows of a batch that has arrived becomes zero (in the few slots concerned)
+    __device__ __forceinline__ void trim(int buf) const {
+        if constexpr (EDGE) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (partial(i))
+                    for (int q = 0; q < R * arrays; ++q) {
+                        uint4* at = slot(buf, 0, q, i);
+                        *at = masked(*at, i);
+                    }
+        }
     }
     __device__ __forceinline__ bool mine(int i) const { return tid + i * th < rows.nvec; }
     __device__ __forceinline__ uint4* slot(int buf, int k, int a, int i) const { return slots + (((buf * R + k) * arrays + a) * NV + i) * th + tid; }
@@ -297,37 +319,39 @@ struct Stage {
     }
     // x goes into array a, or to its own place
     __device__ __forceinline__ void copy_x(int buf, int k, int a, long long t) const {
-        if (shift) copy_row<T>(shifted + (buf * R + k) * pitch, static_cast<const T*>(p.x) + t * p.x_stride, p.D, t == 0);
+        if (shift) copy_row<T>(shifted + (buf * R + k) * pitch + 16, static_cast<const T*>(p.x) + t * p.x_stride, p.D, t == 0);
         else copy(buf, k, a, p.x, p.x_stride, t);
     }
-    __device__ __forceinline__ void read(int buf, int k, int a, int i, f2 (&v)[P]) const {
-        Vec<T>::unpack(*slot(buf, k, a, i), v);
-        if (EDGE && keep[i] != (1u << N) - 1u) mask_pairs<P>(v, keep[i]);
-    }
+    __device__ __forceinline__ void read(int buf, int k, int a, int i, f2 (&v)[P]) const { Vec<T>::unpack(*slot(buf, k, a, i), v); }
+    // A vector of a row that lies otherwise: two aligned pieces of it, shifted by the same distance in every thread.
     __device__ __forceinline__ void read_x(int buf, int k, int a, int i, long long t, f2 (&v)[P]) const {
-        if (!shift) {
+        if (!EDGE || !shift) {
             read(buf, k, a, i, v);
             return;
         }
-        const T* row = reinterpret_cast<const T*>(shifted + (buf * R + k) * pitch + chunk_head(static_cast<const T*>(p.x) + t * p.x_stride));
-        const int c = (tid + i * th) * N - rows.lead;
-        auto at = [&](int e) { return c + e >= 0 && c + e < p.D ? to_f<T>(row[c + e]) : 0.0f; };
+        const int first = 16 + chunk_head(static_cast<const T*>(p.x) + t * p.x_stride) - rows.lead * (int)sizeof(T);
+        const uint4* from = reinterpret_cast<const uint4*>(shifted + (buf * R + k) * pitch + (first & ~15)) + min(tid + i * th, rows.nvec - 1);
+        const uint4 q0 = from[0], q1 = from[1];
+        uint32_t w[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+        const bool by8 = first & 8, by4 = first & 4;
 #pragma unroll
-        for (int e = 0; e < P; ++e) v[e] = f2_make(at(2 * e), at(2 * e + 1));
+        for (int e = 0; e < 6; ++e) w[e] = by8 ? w[e + 2] : w[e];
+#pragma unroll
+        for (int e = 0; e < 5; ++e) w[e] = by4 ? w[e + 1] : w[e];
+        if constexpr (sizeof(T) == 2) {
+            const unsigned bits = (first & 2) * 8;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = __funnelshift_r(w[e], w[e + 1], bits);
+        }
+        uint4 q = make_uint4(w[0], w[1], w[2], w[3]);
+        if (partial(i)) q = masked(q, i);
+        Vec<T>::unpack(q, v);
     }
     __device__ __forceinline__ void store(void* tensor, long long t, int i, const f2 (&v)[P]) const {
         rows.store(static_cast<T*>(tensor) + t * p.D, tid + i * th, Vec<T>::pack(v), keep[i]);
     }
     // zeros outside the row
-    __device__ __forceinline__ void mask(int i, f2 (&v)[P]) const {
-        if constexpr (EDGE) {
-            if (keep[i] != (1u << N) - 1u) mask_pairs<P>(v, keep[i]);
-        } else {
-            const bool in = mine(i);
-#pragma unroll
-            for (int e = 0; e < P; ++e) v[e] = in ? v[e] : 0ull;
-        }
-    }
+    __device__ __forceinline__ void mask(int i, f2 (&v)[P]) const { mask_pairs<P>(v, keep[i]); }
     // this thread's columns of a [D] vector (0 outside the width); `none`: what stands for a vector that is not there
     __device__ __forceinline__ void columns(f2 (&f)[NV][P], const void* w, float none) const {
         const bool wide = !EDGE && (reinterpret_cast<uintptr_t>(w) & 15) == 0;
@@ -462,6 +486,7 @@ block_fwd_kernel(const BlockParams p) {
         fetch(j0 + st.rows.step, buf ^ 1);
         cp_async_wait1();
         if (st.shift) __syncthreads();                  // everyone's chunks of this half are here
+        st.trim(buf);
         f2 v[R][NV][P];
         float m1[R], r1[R], m2[R], r2[R], s[R];
         // mean and 1 / spread of the rows held in v
@@ -485,12 +510,24 @@ block_fwd_kernel(const BlockParams p) {
                 f2 q = 0ull;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    f2 d[P];
+                    // (a thread without a vector i holds zeros, which stay it)
+                    const f2 here = st.mine(i) ? c : 0ull;
+                    f2 part = 0ull;
 #pragma unroll
-                    for (int e = 0; e < P; ++e) d[e] = L ? f2_add(v[k][i][e], c) : v[k][i][e];
-                    if (L) st.mask(i, d);
+                    for (int e = 0; e < P; ++e) {
+                        const f2 d = L ? f2_add(v[k][i][e], here) : v[k][i][e];
+                        part = f2_fma(d, d, part);
+                    }
+                    if (L && st.partial(i)) {
+                        f2 d[P];
 #pragma unroll
-                    for (int e = 0; e < P; ++e) q = f2_fma(d[e], d[e], q);
+                        for (int e = 0; e < P; ++e) d[e] = f2_add(v[k][i][e], c);
+                        st.mask(i, d);
+                        part = 0ull;
+#pragma unroll
+                        for (int e = 0; e < P; ++e) part = f2_fma(d[e], d[e], part);
+                    }
+                    q = f2_add(q, part);
                 }
                 s[k] = f2_sum(q);
             }
@@ -556,11 +593,11 @@ block_fwd_kernel(const BlockParams p) {
 // passes need is held in registers, so that each element is unpacked once.  The sums over tokens are added up row after row in
 // registers and leave as one partial row per CTA.
 template <typename T, int NV, bool L, bool EDGE, int MAXT>
-__global__ void __launch_bounds__(MAXT, L && MAXT <= 256 ? 512 / MAXT : 0)
+__global__ void __launch_bounds__(MAXT, !L && !EDGE ? 0 : NV * Vec<T>::N <= 16 && MAXT <= 256 ? 512 / MAXT : 1)
 block_bwd_kernel(const BlockParams p) {
     using V = Vec<T>;
     constexpr int P = V::P, N = V::N, K = L ? 2 : 1, W = MAXT / 32;
-    constexpr bool WS = L;                              // the weights live in shared memory (a thread's own columns), not in registers
+    constexpr bool WS = L || EDGE;                              // the weights live in shared memory (a thread's own columns), not in registers
     extern __shared__ __align__(16) uint4 smem[];       // dh, dy, h (zeros for what is not there), x (where it is like the others)
     __shared__ __align__(16) float red[2 * W * K];
     int turn = 0;
@@ -636,6 +673,7 @@ block_bwd_kernel(const BlockParams p) {
         fetch(j + st.rows.step, buf ^ 1);
         cp_async_wait1();
         if (st.shift) __syncthreads();
+        st.trim(buf);
         auto unit = [&](const f2& v, const f2& c, const f2& r) { return f2_mul(L ? f2_add(v, c) : v, r); };
         // gh: at first dh + r2 dy w2;  uv: u, then v
         f2 gh[NV][P], uv[NV][P];
@@ -784,8 +822,8 @@ static bool pick_cut(bool bf16, bool edge, bool shift, bool fwd, bool full, long
     c->rows = !fwd || c->max_threads == 512 ? 1 : 2;
     while (c->rows > 1 && T < 148ll * 4 * c->rows) c->rows /= 2;      // too few rows to put several on a CTA
     for (;; c->rows /= 2) {
-        c->smem = 2 * c->rows * (arrays * c->nv * c->threads * 16 + (shift ? staged_pitch(D, esz) : 0));
-        if (!fwd && full) c->smem += 2 * c->nv * c->threads * v * 4;         // the weights
+        c->smem = 2 * c->rows * (arrays * c->nv * c->threads * 16 + (shift ? shifted_pitch(D, esz) : 0));
+        if (!fwd && (full || edge)) c->smem += 2 * c->nv * c->threads * v * 4;         // the weights
         if (c->smem <= (c->rows > 1 ? kSmemLimit / 2 : kSmemLimit)) return true;
         if (c->rows == 1) return false;
     }
@@ -936,9 +974,9 @@ extern "C" rlf_status rlf_block_norm_fwd(const void* x, int64_t x_stride, const 
         if (resident > 0) {
             long long grid = batches(T, c, p.period);
             // RMS: CTAs that retire early, up to eight generations of them, keep the loads of some under the stores of others (32768 x 2560
-            // bf16: 125 us as one generation, 111 as four, 104 as eight); with means and biases a CTA's start costs more than that
-            // gains (8191 x 4096 layer form 53 us as one, 61 as four)
-            long long gens = full ? 1 : grid / (4ll * resident);
+            // bf16: 125 us as one generation, 111 as four, 104 as eight); with means and biases, or rows on no boundary, a CTA's start
+            // costs more than that gains (8191 x 4096 layer form 53 us as one, 61 as four; 20000 x 2603 RMS 106 and 129)
+            long long gens = full || edge ? 1 : grid / (4ll * resident);
             gens = gens < 1 ? 1 : gens > 8 ? 8 : gens;
             if (grid > gens * resident) grid = gens * resident / p.period * p.period;
             k<<<(unsigned)grid, c.threads, c.smem, s>>>(p);
