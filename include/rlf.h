@@ -719,10 +719,11 @@ rlf_status rlf_tune_lmhead_backward(int row_reference, int two_accumulators);
  * unpaced.  0: no meeting points.  Results do not depend on it. */
 rlf_status rlf_tune_lmhead_pacing(int on);
 
-/* Form of the linear layer's products for later calls in this process.  form: 1 = pairs of CTAs on 256-row tiles, 2 = the
- * streamed form for few rows, 0 = chosen per call (built-in).  tile: accumulator columns of a pair's tile (128, 256), or
- * rows of the streamed form's tile (16 to 256); split: CTAs that share a streamed tile's sum (1, 2, 4, 8); 0 = chosen per
- * call.  Results agree up to fp32 summation order. */
+/* Form of the linear layer's products for later calls in this process.  form: 1 = pairs of CTAs on 256-row tiles, 3 = on
+ * 512-row tiles (two accumulators), 2 = the streamed form for few rows, 0 = chosen per call (built-in).  tile: accumulator
+ * columns of a pair's tile (a multiple of 64, in the backward of 128), or rows of the streamed form's tile (16, 32, 64, 128, 256; 64 at
+ * least for grad_W); split: CTAs that share a streamed tile's sum (1 to 8); 0 = chosen per call, and a tile that does
+ * not fit a product is chosen too.  Results agree up to fp32 summation order. */
 rlf_status rlf_tune_linear(int form, int tile, int split);
 
 /* Number of kernels this library has launched in this process (for accounting). */

@@ -29,7 +29,6 @@ using tc::make_map;
 using tc::map_to_cta;
 using tc::mbar_arrive_cluster;
 using tc::mbar_expect_tx;
-using tc::mbar_wait;
 using tc::pair_rank;
 using tc::smem_addr;
 using tc::smem_desc;
@@ -44,6 +43,20 @@ using tc::tma_load_2d;
 using tc::tma_load_2d_pair;
 
 constexpr int kFewOutputs = 4;
+
+// Bounded wait for a phase of an mbarrier that may take long: every try suspends the thread for up to 10 us.  (Short tries by the
+// waiting warps were four fifths of the instructions of a large product, and at the power cap they cost clock.)
+__device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    for (int i = 0; i < (1 << 20); ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(10000u) : "memory");
+        if (ok) return true;
+        if ((i & 63) == 63 && *abort_flag) return false;
+    }
+    *abort_flag = 1;
+    return false;
+}
 
 // What becomes of an accumulator: out[row][col] = act(acc + bias[col]) (times the up half, when gated) + res[row][col].
 struct Epilogue {
@@ -69,13 +82,33 @@ __device__ __forceinline__ float rcp_approx(float x) {
 }
 // 1 / (1 + e^-x); an e^-x beyond fp32 gives 0
 __device__ __forceinline__ float sigmoid(float x) { return rcp_approx(1.0f + ex2_approx(-kLog2e * x)); }
+// Standard normal distribution and e^(-z^2/2).  With t = 1 / (1 + 0.43 |z| / sqrt 2), erfc(x) e^(x^2) is a smooth function of t; the
+// polynomial is its least relative deviation of degree 8 over x in [0, 10] (1e-7, in fp32 arithmetic 2.6e-7), fitted for this purpose.
+// (The library's normal distribution took four times the instructions: 2048 x 1024 x 4096 with GELU 46 us, so 26.)
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+    const float t = rcp_approx(fmaf(0.43f * 0.70710678f, fabsf(z), 1.0f));
+    e = ex2_approx(-0.5f * kLog2e * z * z);
+    float g = 0.036572903f;
+    g = fmaf(g, t, -0.15404779f);
+    g = fmaf(g, t, 0.1899436f);
+    g = fmaf(g, t, -0.041152104f);
+    g = fmaf(g, t, 0.12254031f);
+    g = fmaf(g, t, 0.102736264f);
+    g = fmaf(g, t, 0.12214691f);
+    g = fmaf(g, t, 0.12125991f);
+    const float tail = g * t * e;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
 constexpr float kGeluRoot = 0.7978845608028654f, kGeluCube = 0.044715f, kInvSqrt2Pi = 0.3989422804014327f;
 
 // (the tanh form: 0.5 (1 + tanh u) = sigmoid(2 u))
 template <int ACT> __device__ __forceinline__ float act_value(float z) {
     if (ACT == RLF_ACT_RELU) return z < 0.0f ? 0.0f : z;
     if (ACT == RLF_ACT_SILU) return z * sigmoid(z);
-    if (ACT == RLF_ACT_GELU) return z * normcdff(z);
+    if (ACT == RLF_ACT_GELU) {
+        float e;
+        return z * normal_cdf(z, e);
+    }
     if (ACT == RLF_ACT_GELU_TANH) return z * sigmoid(2.0f * kGeluRoot * z * fmaf(kGeluCube * z, z, 1.0f));
     return z;
 }
@@ -85,7 +118,11 @@ template <int ACT> __device__ __forceinline__ float act_slope(float z) {
         const float s = sigmoid(z);
         return s * fmaf(z, 1.0f - s, 1.0f);
     }
-    if (ACT == RLF_ACT_GELU) return normcdff(z) + z * kInvSqrt2Pi * ex2_approx(-0.5f * kLog2e * z * z);
+    if (ACT == RLF_ACT_GELU) {
+        float e;
+        const float c = normal_cdf(z, e);
+        return fmaf(z * kInvSqrt2Pi, e, c);
+    }
     if (ACT == RLF_ACT_GELU_TANH) {
         const float s = sigmoid(2.0f * kGeluRoot * z * fmaf(kGeluCube * z, z, 1.0f));
         return s + z * s * (1.0f - s) * 2.0f * kGeluRoot * fmaf(3.0f * kGeluCube * z, z, 1.0f);
@@ -131,13 +168,21 @@ __device__ __forceinline__ void store_any(void* p, int f32, long long i, float v
 // ---- large products: pairs of CTAs, 256-row tiles ---------------------------------------------
 constexpr int kBK = 64;
 constexpr int kTileRows = 128;                        // rows of a tile that a CTA holds
-constexpr int kStages = 6;
-constexpr int kABytes = kTileRows * kBK * 2, kBBytes = 128 * kBK * 2, kStageBytes = kABytes + kBBytes;
+// One accumulator (256 rows) per pair, double-buffered in tensor memory so that a tile drains under the next one's multiplies; or two
+// (512 rows) that share every slab of B they stage: three quarters of the traffic from L2 per flop, but all of tensor memory.  Their
+// drains overlap the next tile's first slabs in part: accumulator 0 restarts while accumulator 1 still drains.
+constexpr int kABytes = kTileRows * kBK * 2, kBBytes = 128 * kBK * 2;
+template <int ACC> struct PairCfg {
+    static constexpr int kStages = ACC == 1 ? 6 : 4;
+    static constexpr int kStageBytes = ACC * kABytes + kBBytes;
+};
+constexpr int kRingBytes = 6 * (kABytes + kBBytes);
+static_assert(PairCfg<1>::kStages * PairCfg<1>::kStageBytes == kRingBytes && PairCfg<2>::kStages * PairCfg<2>::kStageBytes == kRingBytes, "one ring");
 constexpr int kDrainWarps = 8;
 constexpr int kPairThreads = 64 + 32 * kDrainWarps;
 constexpr int kDrainPitch = 33;                       // floats per row of a drain staging tile
 constexpr int kDrainBytes = kDrainWarps * 32 * kDrainPitch * 4;
-constexpr int kPairSmem = kStages * kStageBytes + kDrainBytes + 1024 + 256;
+constexpr int kPairSmem = kRingBytes + kDrainBytes + 1024 + 256;
 static_assert(kPairSmem <= 227 * 1024, "the most shared memory a CTA can have");
 
 struct PairParams {
@@ -152,7 +197,7 @@ struct PairParams {
 };
 
 struct PairCtl {
-    unsigned long long full[kStages], empty[kStages], tmem_full[2], tmem_empty[2];
+    unsigned long long full[6], empty[6], tmem_full[2], tmem_empty[2];
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -217,19 +262,21 @@ __device__ __forceinline__ void store_piece(void* out, long long stride, const v
     __syncwarp();
 }
 
+template <int ACC>
 __global__ void __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const PairParams p) {
+    constexpr int kStages = PairCfg<ACC>::kStages, kStageBytes = PairCfg<ACC>::kStageBytes;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_addr(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;          // operand stages sit on 1024-byte boundaries (swizzle atom)
-    float* drain = reinterpret_cast<float*>(smem_raw + (ring - raw) + kStages * kStageBytes);
-    PairCtl* ctl = reinterpret_cast<PairCtl*>(smem_raw + (ring - raw) + kStages * kStageBytes + kDrainBytes);
+    float* drain = reinterpret_cast<float*>(smem_raw + (ring - raw) + kRingBytes);
+    PairCtl* ctl = reinterpret_cast<PairCtl*>(smem_raw + (ring - raw) + kRingBytes + kDrainBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)pair_rank();
     const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1;
     const long long units = (long long)p.m_units * p.n_tiles;
     const int b_rows = p.bn / 2;                           // rows of B that a CTA stages
-    const uint32_t stage_tx = (uint32_t)(kABytes + b_rows * kBK * 2);
+    const uint32_t stage_tx = (uint32_t)(ACC * kABytes + b_rows * kBK * 2);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -273,17 +320,21 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             for (long long u = worker; u < units && ok; u += workers) {
                 int m, n;
                 unit_at(u, m, n);
-                const int a_row = (2 * m + rank) * kTileRows;
                 const int b_row = p.e.gated ? (rank ? p.up_row : 0) + n * b_rows : n * p.bn + rank * b_rows;
                 for (int kb = 0; kb < p.k_slabs; ++kb) {
-                    if (!mbar_wait(smem_addr(&ctl->empty[stage]), phase ^ 1u, &ctl->abort_flag)) { ok = false; break; }
+                    if (!long_wait(smem_addr(&ctl->empty[stage]), phase ^ 1u, &ctl->abort_flag)) { ok = false; break; }
                     const uint32_t own = smem_addr(&ctl->full[stage]), bar = map_to_cta(own, 0);   // the leader's barrier
-                    const uint32_t sa = ring + stage * kStageBytes, sb = sa + kABytes;
+                    const uint32_t sb = ring + stage * kStageBytes + ACC * kABytes;
                     if (rank == 0) mbar_expect_tx(own, 2 * stage_tx);
-                    if (!p.a_mn) {
-                        tma_load_2d_pair(sa, &map_a, bar, kb * kBK, a_row);
-                    } else {
-                        for (int j = 0; j < kTileRows / 64; ++j) tma_load_2d_pair(sa + j * kSlabBytes, &map_a, bar, a_row + j * 64, kb * kBK);
+#pragma unroll
+                    for (int a = 0; a < ACC; ++a) {
+                        const uint32_t sa = ring + stage * kStageBytes + a * kABytes;
+                        const int a_row = (2 * (ACC * m + a) + rank) * kTileRows;
+                        if (!p.a_mn) {
+                            tma_load_2d_pair(sa, &map_a, bar, kb * kBK, a_row);
+                        } else {
+                            for (int j = 0; j < kTileRows / 64; ++j) tma_load_2d_pair(sa + j * kSlabBytes, &map_a, bar, a_row + j * 64, kb * kBK);
+                        }
                     }
                     if (!p.b_mn) {
                         tma_load_2d_pair(sb, &map_b, bar, kb * kBK, b_row);
@@ -300,27 +351,68 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const uint32_t idesc = instr_desc(p.a_mn, p.b_mn, 2 * kTileRows, p.bn);
             const uint32_t a_step = p.a_mn ? (16 * 128) >> 4 : 32 >> 4, b_step = p.b_mn ? (16 * 128) >> 4 : 32 >> 4;
             int stage = 0, buf = 0;
-            uint32_t phase = 0, tphase[2] = {0, 0};
+            uint32_t phase = 0, tphase = 0;                // bit b: parity of accumulator b
             bool ok = true;
-            for (long long u = worker; u < units && ok; u += workers) {
-                if (!mbar_wait(smem_addr(&ctl->tmem_empty[buf]), tphase[buf] ^ 1u, &ctl->abort_flag)) break;
+            auto ready = [&](int st, uint32_t ph) {
+                ok = long_wait(smem_addr(&ctl->full[st]), ph, &ctl->abort_flag);
                 tc_fence_after();
-                const uint32_t d = tmem_base + (uint32_t)buf * 256u;
-                for (int kb = 0; kb < p.k_slabs; ++kb) {
-                    if (!mbar_wait(smem_addr(&ctl->full[stage]), phase, &ctl->abort_flag)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t sa = ring + stage * kStageBytes;
-                    const uint64_t ad = smem_desc(sa, p.a_mn), bd = smem_desc(sa + kABytes, p.b_mn);
+            };
+            auto drained = [&](int b) {
+                ok = long_wait(smem_addr(&ctl->tmem_empty[b]), ((tphase >> b) & 1u) ^ 1u, &ctl->abort_flag);
+                tphase ^= 1u << b;
+                tc_fence_after();
+            };
+            auto multiply = [&](int st, int a, int b, bool first) {
+                const uint32_t base = ring + st * kStageBytes;
+                const uint64_t ad = smem_desc(base + a * kABytes, p.a_mn), bd = smem_desc(base + ACC * kABytes, p.b_mn);
 #pragma unroll
-                    for (int k = 0; k < kBK / 16; ++k)
-                        tc_mma2(d, ad + (uint64_t)(k * a_step), bd + (uint64_t)(k * b_step), idesc, (kb | k) ? 1u : 0u);
-                    tc_commit2(smem_addr(&ctl->empty[stage]));       // frees the stage in both CTAs when these retire
-                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                for (int k = 0; k < kBK / 16; ++k)
+                    tc_mma2(tmem_base + (uint32_t)b * 256u, ad + (uint64_t)(k * a_step), bd + (uint64_t)(k * b_step), idesc, first && k == 0 ? 0u : 1u);
+            };
+            auto advance = [&](int& st, uint32_t& ph) {
+                if (++st == kStages) { st = 0; ph ^= 1u; }
+            };
+            for (long long u = worker; u < units && ok; u += workers) {
+                if constexpr (ACC == 1) {
+                    drained(buf);
+                    for (int kb = 0; kb < p.k_slabs && ok; ++kb) {
+                        ready(stage, phase);
+                        if (!ok) break;
+                        multiply(stage, 0, buf, kb == 0);
+                        tc_commit2(smem_addr(&ctl->empty[stage]));       // frees the stage in both CTAs when these retire
+                        advance(stage, phase);
+                    }
+                    if (!ok) break;
+                    tc_commit2(smem_addr(&ctl->tmem_full[buf]));
+                    buf ^= 1;
+                } else {
+                    // accumulator 0 takes the ring's slabs while accumulator 1 may still be draining, which then catches up
+                    const int ahead = min(kStages, p.k_slabs);
+                    drained(0);
+                    int st = stage;
+                    uint32_t ph = phase;
+                    for (int kb = 0; kb < ahead && ok; ++kb) {
+                        ready(st, ph);
+                        if (!ok) break;
+                        multiply(st, 0, 0, kb == 0);
+                        if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
+                        advance(st, ph);
+                    }
+                    if (ok) drained(1);
+                    for (int kb = 0; kb < p.k_slabs && ok; ++kb) {
+                        if (kb >= ahead) {
+                            ready(stage, phase);
+                            if (!ok) break;
+                            multiply(stage, 0, 0, false);
+                            if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
+                        }
+                        multiply(stage, 1, 1, kb == 0);
+                        tc_commit2(smem_addr(&ctl->empty[stage]));
+                        advance(stage, phase);
+                    }
+                    if (!ok) break;
+                    tc_commit2(smem_addr(&ctl->tmem_full[1]));
                 }
-                if (!ok) break;
-                tc_commit2(smem_addr(&ctl->tmem_full[buf]));
-                tphase[buf] ^= 1u;
-                buf ^= 1;
             }
         }
     } else {
@@ -330,15 +422,21 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         float* stage = drain + (warp - 2) * 32 * kDrainPitch;
         const int width = e.gated ? p.bn / 2 : p.bn;
         int buf = 0;
-        uint32_t tphase[2] = {0, 0};
+        uint32_t tphase = 0;
         for (long long u = worker; u < units; u += workers) {
             int m, n;
             unit_at(u, m, n);
-            const int row = (2 * m + rank) * kTileRows + quarter * 32 + lane;
+            bool alive = true;
+#pragma unroll 1
+            for (int a = 0; a < ACC && alive; ++a) {
+            const int row = (2 * (ACC * m + a) + rank) * kTileRows + quarter * 32 + lane;
             const bool row_ok = row < p.M;
             int got = 0;
-            if (lane == 0) got = mbar_wait(smem_addr(&ctl->tmem_full[buf]), tphase[buf], &ctl->abort_flag) ? 1 : 0;
-            if (!__shfl_sync(0xffffffffu, got, 0)) break;
+            if (lane == 0) got = long_wait(smem_addr(&ctl->tmem_full[buf]), (tphase >> buf) & 1u, &ctl->abort_flag) ? 1 : 0;
+            if (!__shfl_sync(0xffffffffu, got, 0)) {
+                alive = false;
+                break;
+            }
             tc_fence_after();
             const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)buf * 256u;
 #pragma unroll 1
@@ -382,8 +480,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_addr(&ctl->tmem_empty[buf]), 0));
-            tphase[buf] ^= 1u;
+            tphase ^= 1u << buf;
             buf ^= 1;
+            }
+            if (!alive) break;
         }
     }
 
@@ -493,7 +593,7 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
             uint32_t phase = 0;
             const int i0 = p.e.gated ? it * 64 : it * 128, i1 = p.e.gated ? p.up_row + i0 : i0 + 64;
             for (int kb = k0; kb < k1; ++kb) {
-                if (!mbar_wait(smem_addr(&ctl->empty[stage]), phase ^ 1u, &ctl->abort_flag)) break;
+                if (!long_wait(smem_addr(&ctl->empty[stage]), phase ^ 1u, &ctl->abort_flag)) break;
                 const uint32_t bar = smem_addr(&ctl->full[stage]);
                 const uint32_t ss = ring + stage * stage_bytes, sf = ss + kABytes;
                 mbar_expect_tx(bar, (uint32_t)stage_bytes);
@@ -520,7 +620,7 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
             uint32_t phase = 0;
             bool ok = true;
             for (int kb = k0; kb < k1; ++kb) {
-                if (!mbar_wait(smem_addr(&ctl->full[stage]), phase, &ctl->abort_flag)) { ok = false; break; }
+                if (!long_wait(smem_addr(&ctl->full[stage]), phase, &ctl->abort_flag)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t ss = ring + stage * stage_bytes;
                 const uint64_t sd = smem_desc(ss, p.s_mn), fd = smem_desc(ss + kABytes, p.f_mn);
@@ -535,7 +635,7 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
     } else {
         // the accumulator goes to shared memory as [j][i] (the ring's memory: every copy has been multiplied by then)
         int got = 0;
-        if (lane == 0) got = mbar_wait(smem_addr(&ctl->tmem_full), 0, &ctl->abort_flag) ? 1 : 0;
+        if (lane == 0) got = long_wait(smem_addr(&ctl->tmem_full), 0, &ctl->abort_flag) ? 1 : 0;
         if (__shfl_sync(0xffffffffu, got, 0)) {
             tc_fence_after();
             const int i = (warp & 3) * 32 + lane;
@@ -912,37 +1012,37 @@ struct Operand {
 };
 
 struct Plan {
-    bool narrow;
-    int tile;                       // pair: accumulator columns; narrow: rows of a tile
-    int split;                      // narrow: CTAs that share a tile's K
+    int acc;                        // accumulators of a pair; 0: the streamed form
+    int tile;                       // pair: accumulator columns; streamed: rows of a tile
+    int split;                      // streamed: CTAs that share a tile's K
 };
 static int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-static int narrow_split(long long tiles, int k_slabs, int sms) {
+// CTAs that share a streamed tile's sum: as many as are resident together (four per SM) while each keeps four slabs of K.
+static int narrow_split(long long tiles, int k_slabs, int sms, int tile) {
+    const int per_sm = tile <= 32 ? 4 : tile <= 64 ? 3 : tile <= 128 ? 2 : 1;
     int split = 1;
-    while (split < 8 && tiles * split < 2ll * sms && k_slabs >= 8 * split) split *= 2;
+    while (split < 8 && tiles * (split + 1) <= (long long)per_sm * sms && k_slabs >= 4 * (split + 1)) ++split;
     return split;
 }
-static Plan choose(long long M, int N, int k_slabs, bool gated, bool f_mn, bool s_mn) {
+static Plan choose(long long M, int N, int k_slabs, bool gated, bool f_mn, bool b_mn) {
     const int sms = sm_count();
-    const int cols = gated ? 64 : 128;
-    Plan q = {false, 256, 1};
+    Plan q = {1, 256, 1};
     const int form = g_form.load(), tile = g_tile.load(), split = g_split.load();
-    const bool few = form == 2 || (form == 0 && M <= 256);
-    const int tile_cols = gated ? 128 : 256;
-    const long long units = (long long)div_up(M, 256) * div_up(N, tile_cols);
-    if (few) {
-        q.narrow = true;
+    if (form == 2 || (form == 0 && M <= 256)) {
+        q.acc = 0;
         q.tile = f_mn ? 64 : 16;
         while (q.tile < M && q.tile < 256) q.tile *= 2;
-        if (tile > 0 && (tile == 16 || tile == 32 || tile == 64 || tile == 128 || tile == 256) && (!f_mn || tile >= 64)) q.tile = tile;
-        q.split = split > 0 ? split : narrow_split((long long)div_up(N, cols) * div_up(M, q.tile), k_slabs, sms);
-        if (q.split > k_slabs) q.split = k_slabs >= 4 ? 4 : k_slabs >= 2 ? 2 : 1;      // (every CTA has a part of K)
-    } else {
-        if (units < sms / 2) q.tile = 128;
-        if (tile == 128 || tile == 256) q.tile = tile;
+        if ((tile == 16 || tile == 32 || tile == 64 || tile == 128 || tile == 256) && (!f_mn || tile >= 64)) q.tile = tile;
+        q.split = split > 0 ? split : narrow_split((long long)div_up(N, gated ? 64 : 128) * div_up(M, q.tile), k_slabs, sms, q.tile);
+        if (q.split > k_slabs) q.split = k_slabs;          // (every CTA has a part of K)
+        return q;
     }
-    (void)s_mn;
+    const int tile_cols = gated ? 128 : 256;
+    const long long units = (long long)div_up(M, 256) * div_up(N, tile_cols);
+    if (units < sms / 2) q.tile = 128;
+    if (form == 3) q.acc = 2;
+    if (tile >= 64 && tile % 64 == 0 && (!b_mn || tile % 128 == 0)) q.tile = tile;
     return q;
 }
 
@@ -988,30 +1088,35 @@ static rlf_status product(const Operand& A, const Operand& B, long long M, long 
         return o.mn ? make_map(map, o.at, (uint64_t)K, (uint64_t)rows, (uint64_t)o.stride, 64, 64)
                     : make_map(map, o.at, (uint64_t)rows, (uint64_t)K, (uint64_t)o.stride, 64, (uint32_t)box_rows);
     };
-    if (plan.narrow) {
+    if (plan.acc == 0) {
         NarrowParams p = {};
         p.J = (int)M; p.k_slabs = k_slabs; p.nn = plan.tile; p.s_mn = B.mn; p.f_mn = A.mn; p.up_row = e.N; p.e = e; p.dev_status = dev_status;
-        const int per_cta = plan.tile <= 128 ? 112 * 1024 : 220 * 1024;       // two CTAs per SM while the tile is small
-        p.stages = (per_cta - 1024 - 256) / narrow_stage_bytes(plan.tile);
+        const int i_tiles = div_up(e.N, e.gated ? 64 : 128), j_tiles = div_up(M, plan.tile);
+        // the SM's shared memory is shared by the CTAs that come to it (each CTA keeps 1 KB to the system)
+        int per_sm = div_up((long long)i_tiles * j_tiles * plan.split, sm_count());
+        for (per_sm = per_sm > 4 ? 4 : per_sm;; --per_sm) {
+            p.stages = (228 * 1024 / per_sm - 1024 - 1024 - 256) / narrow_stage_bytes(plan.tile);
+            if (p.stages >= 3 || per_sm == 1) break;
+        }
         if (p.stages > kMaxNarrowStages) p.stages = kMaxNarrowStages;
         const int smem = narrow_ring_bytes(plan.tile, p.stages) + 1024 + 256;
         if (!encode(&mb, B, rows_b, 64) || !encode(&ma, A, M, plan.tile)) return RLF_ERR_CUDA;
         if (!opt_in((const void*)linear_narrow_kernel, 227 * 1024)) return RLF_ERR_CUDA;
-        const int i_tiles = div_up(e.N, e.gated ? 64 : 128), j_tiles = div_up(M, plan.tile);
         return launch_cluster((void*)linear_narrow_kernel, dim3((unsigned)(i_tiles * plan.split), (unsigned)j_tiles), kNarrowThreads, smem,
                               plan.split, mb, ma, &p, s);
     }
     PairParams p = {};
-    p.M = (int)M; p.m_units = div_up(M, 2 * kTileRows); p.k_slabs = k_slabs; p.bn = plan.tile;
+    p.M = (int)M; p.m_units = div_up(M, 2 * kTileRows * plan.acc); p.k_slabs = k_slabs; p.bn = plan.tile;
     p.n_tiles = div_up(e.N, e.gated ? plan.tile / 2 : plan.tile);
     p.a_mn = A.mn; p.b_mn = B.mn; p.up_row = e.N; p.e = e; p.dev_status = dev_status;
-    p.group = 8;
+    p.group = 8 / plan.acc;
     if (!encode(&ma, A, M, kTileRows) || !encode(&mb, B, rows_b, plan.tile / 2)) return RLF_ERR_CUDA;
-    if (!opt_in((const void*)linear_pair_kernel, kPairSmem)) return RLF_ERR_CUDA;
+    void* const kernel = plan.acc == 2 ? (void*)linear_pair_kernel<2> : (void*)linear_pair_kernel<1>;
+    if (!opt_in(kernel, kPairSmem)) return RLF_ERR_CUDA;
     const long long units = (long long)p.m_units * p.n_tiles;
     const int pairs = sm_count() / 2;
     const int workers = units < pairs ? (int)units : pairs;
-    return launch_cluster((void*)linear_pair_kernel, dim3((unsigned)(2 * workers)), kPairThreads, kPairSmem, 2, ma, mb, &p, s);
+    return launch_cluster(kernel, dim3((unsigned)(2 * workers)), kPairThreads, kPairSmem, 2, ma, mb, &p, s);
 }
 
 static bool rows_aligned(const void* at, long long stride, int esz) { return aligned(at, 16) && stride * esz % 16 == 0; }
@@ -1210,8 +1315,7 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
 }
 
 extern "C" rlf_status rlf_tune_linear(int form, int tile, int split) {
-    if (form < 0 || form > 2 || (tile != 0 && tile != 16 && tile != 32 && tile != 64 && tile != 128 && tile != 256)) return RLF_ERR_SHAPE;
-    if (split != 0 && split != 1 && split != 2 && split != 4 && split != 8) return RLF_ERR_SHAPE;
+    if (form < 0 || form > 3 || tile < 0 || tile > 256 || (tile != 16 && tile != 32 && tile % 64 != 0) || split < 0 || split > 8) return RLF_ERR_SHAPE;
     rlf::ln::g_form = form;
     rlf::ln::g_tile = tile;
     rlf::ln::g_split = split;

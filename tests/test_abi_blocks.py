@@ -54,7 +54,7 @@ def test_linear_backward_refuses(lib):
 def test_linear_tuning_refuses(lib):
     f = lib.rlf_tune_linear
     f.argtypes = [ci, ci, ci]
-    assert f(3, 0, 0) == SHAPE and f(-1, 0, 0) == SHAPE and f(1, 100, 0) == SHAPE and f(2, 0, 3) == SHAPE and f(2, 64, 4) == 0 and f(0, 0, 0) == 0
+    assert f(4, 0, 0) == SHAPE and f(-1, 0, 0) == SHAPE and f(1, 100, 0) == SHAPE and f(2, 0, 9) == SHAPE and f(2, 0, -1) == SHAPE and f(2, 64, 4) == 0 and f(0, 0, 0) == 0
 
 
 def test_workspace_sizes(lib):

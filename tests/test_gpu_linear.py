@@ -149,7 +149,7 @@ def test_few_outputs(T, D, N):
     both_ways(T, D, N, ACTS[N], bias=BF, residual=BF, pad=16, seed=2, dy_pad=1)
 
 
-@pytest.mark.parametrize("form,tile,split", [(1, 128, 0), (1, 256, 0), (2, 16, 1), (2, 32, 2), (2, 64, 4), (2, 128, 8), (2, 256, 2), (2, 256, 8)])
+@pytest.mark.parametrize("form,tile,split", [(1, 128, 0), (1, 256, 0), (2, 16, 1), (2, 32, 2), (2, 64, 4), (2, 128, 8), (2, 256, 2), (2, 256, 8), (2, 32, 3), (2, 64, 7), (1, 192, 0), (1, 64, 0), (3, 256, 0), (3, 128, 0)])
 @pytest.mark.parametrize("T,D,N,gated", [(40, 512, 200, False), (40, 512, 200, True), (513, 328, 264, False), (300, 1024, 137, True)])
 def test_every_form(form, tile, split, T, D, N, gated):
     b = gc.binding()
