@@ -71,7 +71,7 @@ struct Epilogue {
     int out_f32;
     __nv_bfloat16* pre;             // acc + bias as bf16, [rows][N], gated [rows][2 N]; nullable
     long long pre_stride;
-    int vec, vec_pre;               // rows of out and res (of pre) lie on 16-byte boundaries
+    int vec_out, vec_res, vec_pre;  // rows of out, res and pre lie on 16-byte boundaries
 };
 
 // ---- activations ------------------------------------------------------------------------------
@@ -180,8 +180,8 @@ constexpr int kRingBytes = 6 * (kABytes + kBBytes);
 static_assert(PairCfg<1>::kStages * PairCfg<1>::kStageBytes == kRingBytes && PairCfg<2>::kStages * PairCfg<2>::kStageBytes == kRingBytes, "one ring");
 constexpr int kDrainWarps = 8;
 constexpr int kPairThreads = 64 + 32 * kDrainWarps;
-constexpr int kDrainPitch = 33;                       // floats per row of a drain staging tile
-constexpr int kDrainBytes = kDrainWarps * 32 * kDrainPitch * 4;
+constexpr int kDrainTile = 4096;                      // bytes of a drain warp's output tile: 32 rows of 32 columns, fp32 or two of bf16
+constexpr int kDrainBytes = kDrainWarps * (kDrainTile + 128);
 constexpr int kPairSmem = kRingBytes + kDrainBytes + 1024 + 256;
 static_assert(kPairSmem <= 227 * 1024, "the most shared memory a CTA can have");
 
@@ -203,73 +203,102 @@ struct PairCtl {
 };
 static_assert(sizeof(PairCtl) <= 256, "the barriers have 256 bytes behind the stage ring");
 
-// 32 columns of one row per thread -> memory.  Rows on 16-byte boundaries are stored by their threads; others (and a ragged
-// last piece) go through a staging tile, so that a warp stores 32 columns of a row at a time.  With ADD, res is added.
+// A drain warp's output tiles.  Results leave as 32 x 32 tiles by TMA stores (rows of 64 or 128 bytes, swizzled so that the threads'
+// 16-byte pieces meet no bank twice): whole sectors, and clipped at the last row and column.  (One row per thread stored straight
+// to memory is 16 bytes of a sector at a time; those writes took as much of L2 as the operands: 8192 x 2560 x 10240 with two
+// accumulators 413 us.)  Rows on no 16-byte boundary are stored by element, a row's 32 columns at a time.
+struct Drain {
+    unsigned char* tile;            // kDrainTile bytes
+    float* bias;                    // 32 floats
+    int lane, next;
+};
 template <bool F32>
-__device__ __forceinline__ void store_piece(void* out, long long stride, const void* res, long long res_stride, int row, bool row_ok,
-                                            int M, int col, int nvalid, bool vec, float (&v)[32], float* stage, int lane) {
-    if (vec && nvalid == 32) {
-        if (!row_ok) return;
-        if (F32) {
-            float4* d = reinterpret_cast<float4*>(static_cast<float*>(out) + row * stride + col);
-            if (res) {
-                const float4* r = reinterpret_cast<const float4*>(static_cast<const float*>(res) + row * res_stride + col);
+__device__ __forceinline__ void store_piece(Drain& d, const CUtensorMap* map, bool tma, int third, bool mixed, void* out, long long stride,
+                                            int row0, int M, int col, int nvalid, const float (&v)[32]) {
+    const int lane = d.lane;
+    if (tma) {
+        // the store that read this tile last has read it (the other bf16 tile's may still be on its way)
+        if (lane == 0) {
+            if (F32 || mixed) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        }
+        __syncwarp();
+        const uint32_t at = smem_addr(d.tile) + (F32 ? 0u : (uint32_t)d.next * 2048u);
+        d.next ^= 1;
+        if constexpr (F32) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float4 q = r[i];
-                    d[i] = make_float4(v[4 * i] + q.x, v[4 * i + 1] + q.y, v[4 * i + 2] + q.z, v[4 * i + 3] + q.w);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            }
+            for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};"
+                             :: "r"(at + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) << 4))), "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]),
+                                "f"(v[4 * i + 3]) : "memory");
         } else {
-            uint4* d = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + row * stride + col);
-            if (res) {
-                const uint4* r = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(res) + row * res_stride + col);
-                uint4 q[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) q[i] = r[i];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        v[8 * i + 2 * k] += bf_lo(w[k]);
-                        v[8 * i + 2 * k + 1] += bf_hi(w[k]);
-                    }
-                }
-            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                d[i] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
-                                  pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                             :: "r"(at + (uint32_t)(lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4))), "r"(pack_bf16x2(v[8 * i], v[8 * i + 1])),
+                                "r"(pack_bf16x2(v[8 * i + 2], v[8 * i + 3])), "r"(pack_bf16x2(v[8 * i + 4], v[8 * i + 5])),
+                                "r"(pack_bf16x2(v[8 * i + 6], v[8 * i + 7])) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            if (row0 < M)
+                asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                             :: "l"(map), "r"(at), "r"(col), "r"(third), "r"(row0) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
         return;
     }
-#pragma unroll
-    for (int i = 0; i < 32; ++i) stage[lane * kDrainPitch + i] = v[i];
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
-    const int row0 = row - lane, rows = min(32, M - row0);
+    float* t = reinterpret_cast<float*>(d.tile);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t[lane * 32 + (i ^ lane)] = v[i];
+    __syncwarp();
+    const int rows = min(32, M - row0);
     if (lane < nvalid) {
 #pragma unroll 4
-        for (int r = 0; r < rows; ++r) {
-            float o = stage[r * kDrainPitch + lane];
-            if (res) o += load_any(res, F32, (long long)(row0 + r) * res_stride + col + lane);
-            store_any(out, F32, (long long)(row0 + r) * stride + col + lane, o);
-        }
+        for (int r = 0; r < rows; ++r) store_any(out, F32, (long long)(row0 + r) * stride + col + lane, t[r * 32 + (lane ^ r)]);
     }
     __syncwarp();
+}
+// 32 columns of this thread's row of the residual
+__device__ __forceinline__ void load_residual(const Epilogue& e, int row, bool row_ok, int col, int nvalid, float (&r)[32]) {
+    if (!row_ok) return;
+    const long long at = row * e.res_stride + col;
+    if (e.vec_res && nvalid == 32) {
+        if (e.out_f32) {
+            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(e.res) + at);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 q = p[i];
+                r[4 * i] = q.x; r[4 * i + 1] = q.y; r[4 * i + 2] = q.z; r[4 * i + 3] = q.w;
+            }
+        } else {
+            const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(e.res) + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 q = p[i];
+                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { r[8 * i + 2 * k] = bf_lo(w[k]); r[8 * i + 2 * k + 1] = bf_hi(w[k]); }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) r[i] = i < nvalid ? load_any(e.res, e.out_f32, at + i) : 0.0f;
+    }
 }
 
 template <int ACC>
 __global__ void __launch_bounds__(kPairThreads, 1)
-linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const PairParams p) {
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+                   const __grid_constant__ CUtensorMap map_pre, const PairParams p) {
     constexpr int kStages = PairCfg<ACC>::kStages, kStageBytes = PairCfg<ACC>::kStageBytes;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_addr(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;          // operand stages sit on 1024-byte boundaries (swizzle atom)
-    float* drain = reinterpret_cast<float*>(smem_raw + (ring - raw) + kRingBytes);
+    unsigned char* drain = smem_raw + (ring - raw) + kRingBytes;
     PairCtl* ctl = reinterpret_cast<PairCtl*>(smem_raw + (ring - raw) + kRingBytes + kDrainBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)pair_rank();
@@ -419,7 +448,11 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         // ---------------- epilogue: one row per thread, two warps share a row's 32-column pieces ----------------
         const Epilogue& e = p.e;
         const int quarter = warp & 3, half = (warp - 2) >> 2;
-        float* stage = drain + (warp - 2) * 32 * kDrainPitch;
+        Drain d;
+        d.tile = drain + (warp - 2) * kDrainTile;
+        d.bias = reinterpret_cast<float*>(drain + kDrainWarps * kDrainTile) + (warp - 2) * 32;
+        d.lane = lane;
+        d.next = 0;
         const int width = e.gated ? p.bn / 2 : p.bn;
         int buf = 0;
         uint32_t tphase = 0;
@@ -445,24 +478,21 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 if (col >= e.N) break;                     // (warp-uniform)
                 const int nvalid = min(32, e.N - col);
                 uint32_t raw_v[32];
-                float v[32];
-                auto take = [&](uint32_t at, int shift) {  // accumulator columns + bias
+                float v[32], r[32];
+                if (e.res) load_residual(e, row, row_ok, col, nvalid, r);
+                auto take = [&](uint32_t at, int half_of_w) {    // accumulator columns + bias
                     tc_ld32(t_row + at, raw_v);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw_v[i]);
+                    const int shift = half_of_w ? e.N : 0;
                     if (e.bias) {
-                        stage[lane] = lane < nvalid ? load_any(e.bias, !e.bias_bf16, shift + col + lane) : 0.0f;
+                        d.bias[lane] = lane < nvalid ? load_any(e.bias, !e.bias_bf16, shift + col + lane) : 0.0f;
                         __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] += stage[i];
+                        for (int i = 0; i < 32; ++i) v[i] += d.bias[i];
                         __syncwarp();
                     }
-                    if (e.pre) {
-                        float w[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) w[i] = v[i];
-                        store_piece<false>(e.pre + shift, e.pre_stride, nullptr, 0, row, row_ok, p.M, col, nvalid, e.vec_pre, w, stage, lane);
-                    }
+                    if (e.pre) store_piece<false>(d, &map_pre, e.vec_pre, half_of_w, e.out_f32, e.pre + shift, e.pre_stride, row - lane, p.M, col, nvalid, v);
                 };
                 take((uint32_t)(c * 32), 0);
                 activate<32>(e.act, v);
@@ -470,12 +500,16 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     float g[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) g[i] = v[i];
-                    take((uint32_t)(width + c * 32), e.N);
+                    take((uint32_t)(width + c * 32), 1);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] *= g[i];
                 }
-                if (e.out_f32) store_piece<true>(e.out, e.out_stride, e.res, e.res_stride, row, row_ok, p.M, col, nvalid, e.vec, v, stage, lane);
-                else store_piece<false>(e.out, e.out_stride, e.res, e.res_stride, row, row_ok, p.M, col, nvalid, e.vec, v, stage, lane);
+                if (e.res) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] += r[i];
+                }
+                if (e.out_f32) store_piece<true>(d, &map_out, e.vec_out, 0, true, e.out, e.out_stride, row - lane, p.M, col, nvalid, v);
+                else store_piece<false>(d, &map_out, e.vec_out, 0, false, e.out, e.out_stride, row - lane, p.M, col, nvalid, v);
             }
             tc_fence_before();
             __syncwarp();
@@ -485,6 +519,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             }
             if (!alive) break;
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // the last tiles are written before their memory goes
     }
 
     tc_fence_before();
@@ -686,7 +721,7 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
             for (int k = 0; k < 4; ++k) z[k] *= up[k];
         }
         const long long o = row * e.out_stride + col, ro = row * e.res_stride + col;
-        if (e.vec && nvalid == 4) {
+        if (e.vec_out && e.vec_res && nvalid == 4) {
             if (e.out_f32) {
                 if (e.res) {
                     const float4 r = *reinterpret_cast<const float4*>(static_cast<const float*>(e.res) + ro);
@@ -1055,8 +1090,7 @@ static bool opt_in(const void* kernel, int bytes) {
     }) == 1;
 }
 
-static rlf_status launch_cluster(void* kernel, dim3 grid, int threads, int smem, int cluster, const CUtensorMap& a, const CUtensorMap& b,
-                                 const void* params, cudaStream_t s) {
+static rlf_status launch_cluster(void* kernel, dim3 grid, int threads, int smem, int cluster, void** args, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
@@ -1069,13 +1103,26 @@ static rlf_status launch_cluster(void* kernel, dim3 grid, int threads, int smem,
     at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    void* args[] = {const_cast<CUtensorMap*>(&a), const_cast<CUtensorMap*>(&b), const_cast<void*>(params)};
     if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) {
         cudaGetLastError();
         return RLF_ERR_CUDA;
     }
     count_launch();
     return RLF_OK;
+}
+
+// rows of `halves` x N elements, stored in tiles of 32 x 32
+static bool make_tile_map(CUtensorMap* map, const void* base, long long rows, int N, int halves, long long stride, bool f32) {
+    const tc::EncodeTiledFn fn = tc::encode_fn();
+    if (!fn) return false;
+    const int esz = f32 ? 4 : 2;
+    const cuuint64_t dims[3] = {(cuuint64_t)N, (cuuint64_t)halves, (cuuint64_t)rows};
+    // (a single half: its stride is never taken)
+    const cuuint64_t strides[2] = {(cuuint64_t)(halves > 1 ? N : stride) * esz, (cuuint64_t)stride * esz};
+    const cuuint32_t box[3] = {32, 1, 32}, step[3] = {1, 1, 1};
+    return fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // out[m][n] = epilogue(sum_k A[m][k] B[n][k]), M rows, e.N columns (gated: B has 2 e.N rows), K terms
@@ -1102,8 +1149,8 @@ static rlf_status product(const Operand& A, const Operand& B, long long M, long 
         const int smem = narrow_ring_bytes(plan.tile, p.stages) + 1024 + 256;
         if (!encode(&mb, B, rows_b, 64) || !encode(&ma, A, M, plan.tile)) return RLF_ERR_CUDA;
         if (!opt_in((const void*)linear_narrow_kernel, 227 * 1024)) return RLF_ERR_CUDA;
-        return launch_cluster((void*)linear_narrow_kernel, dim3((unsigned)(i_tiles * plan.split), (unsigned)j_tiles), kNarrowThreads, smem,
-                              plan.split, mb, ma, &p, s);
+        void* args[] = {&mb, &ma, &p};
+        return launch_cluster((void*)linear_narrow_kernel, dim3((unsigned)(i_tiles * plan.split), (unsigned)j_tiles), kNarrowThreads, smem, plan.split, args, s);
     }
     PairParams p = {};
     p.M = (int)M; p.m_units = div_up(M, 2 * kTileRows * plan.acc); p.k_slabs = k_slabs; p.bn = plan.tile;
@@ -1116,7 +1163,12 @@ static rlf_status product(const Operand& A, const Operand& B, long long M, long 
     const long long units = (long long)p.m_units * p.n_tiles;
     const int pairs = sm_count() / 2;
     const int workers = units < pairs ? (int)units : pairs;
-    return launch_cluster(kernel, dim3((unsigned)(2 * workers)), kPairThreads, kPairSmem, 2, ma, mb, &p, s);
+    // output tiles: 32 columns x one half x 32 rows
+    CUtensorMap mo = ma, mp = ma;
+    if (e.vec_out && !make_tile_map(&mo, e.out, M, e.N, 1, e.out_stride, e.out_f32 != 0)) return RLF_ERR_CUDA;
+    if (e.pre && e.vec_pre && !make_tile_map(&mp, e.pre, M, e.N, e.gated ? 2 : 1, e.pre_stride, false)) return RLF_ERR_CUDA;
+    void* args[] = {&ma, &mb, &mo, &mp, &p};
+    return launch_cluster(kernel, dim3((unsigned)(2 * workers)), kPairThreads, kPairSmem, 2, args, s);
 }
 
 static bool rows_aligned(const void* at, long long stride, int esz) { return aligned(at, 16) && stride * esz % 16 == 0; }
@@ -1207,7 +1259,8 @@ extern "C" rlf_status rlf_linear_fwd(const void* x, int64_t T, int32_t D, int64_
     e.act = act; e.gated = gated; e.N = N; e.bias = bias; e.bias_bf16 = bias_dt == RLF_BF16;
     e.res = residual; e.res_stride = residual_stride; e.out = y_out; e.out_stride = N; e.out_f32 = y_dt == RLF_F32;
     e.pre = static_cast<__nv_bfloat16*>(pre_out); e.pre_stride = gated ? 2ll * N : N;
-    e.vec = rows_aligned(y_out, N, (int)osz) && (!residual || rows_aligned(residual, residual_stride, (int)osz));
+    e.vec_out = rows_aligned(y_out, N, (int)osz);
+    e.vec_res = !residual || rows_aligned(residual, residual_stride, (int)osz);
     e.vec_pre = rows_aligned(pre_out, N, 2);
     if (!gated && N <= kFewOutputs) {
         const __nv_bfloat16* xb = static_cast<const __nv_bfloat16*>(x);
@@ -1300,14 +1353,14 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
     }
     if (grad_x) {
         Epilogue e = {};
-        e.N = D; e.out = grad_x; e.out_stride = D; e.vec = 1;
+        e.N = D; e.out = grad_x; e.out_stride = D; e.vec_out = e.vec_res = 1;
         st = product(gz, {W, D, 1}, T, rows, e, dev_status, s);
         if (st != RLF_OK) return st;
     }
     if (grad_W) {
         Epilogue e = {};
         e.N = D; e.out = grad_W; e.out_stride = D; e.out_f32 = grad_W_dt == RLF_F32;
-        e.vec = rows_aligned(grad_W, D, (int)wsz);
+        e.vec_out = e.vec_res = rows_aligned(grad_W, D, (int)wsz);
         if (accumulate) { e.res = grad_W; e.res_stride = D; }
         st = product({gz.at, gz.stride, 1}, {x, x_stride, 1}, rows, T, e, dev_status, s);
     }
