@@ -47,6 +47,7 @@ constexpr int kFewOutputs = 4;
 // Bounded wait for a phase of an mbarrier that may take long: every try suspends the thread for up to 10 us.  (Short tries by the
 // waiting warps were four fifths of the instructions of a large product, and at the power cap they cost clock.)
 __device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    if (mbar_try_wait(bar, parity)) return true;
     for (int i = 0; i < (1 << 20); ++i) {
         uint32_t ok;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -57,6 +58,16 @@ __device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatil
     *abort_flag = 1;
     return false;
 }
+
+// One lane of a warp.  The issuing warps run their loops as a whole and elect a lane for the copies and multiplies only: with warp-uniform
+// loops the operands of those instructions are formed in uniform registers.  As a single thread's loop a 64-deep slab took 580
+// clocks to issue, whatever its width, where a 256 x 256 one is multiplied in 512.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 // What becomes of an accumulator: out[row][col] = act(acc + bias[col]) (times the up half, when gated) + res[row][col].
 struct Epilogue {
@@ -300,8 +311,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const uint32_t ring = (raw + 1023u) & ~1023u;          // operand stages sit on 1024-byte boundaries (swizzle atom)
     unsigned char* drain = smem_raw + (ring - raw) + kRingBytes;
     PairCtl* ctl = reinterpret_cast<PairCtl*>(smem_raw + (ring - raw) + kRingBytes + kDrainBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = (int)pair_rank();
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int rank = uniform((int)pair_rank());
     const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1;
     const long long units = (long long)p.m_units * p.n_tiles;
     const int b_rows = p.bn / 2;                           // rows of B that a CTA stages
@@ -328,7 +339,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     __syncthreads();
     cluster_sync_all();                                    // both CTAs' barriers exist before either signals the other
     tc_fence_after();
-    const uint32_t tmem_base = ctl->tmem_base;
+    const uint32_t tmem_base = (uint32_t)uniform((int)ctl->tmem_base);
 
     // Raster: groups of row units; inside a group row units fastest, so that the workers running at one time cover a block of
     // about as many rows as columns and share both operands through L2.
@@ -342,19 +353,20 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
     if (warp == 0) {
         // ---------------- loads (each CTA its own rows of A and half of B) ----------------
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (long long u = worker; u < units && ok; u += workers) {
-                int m, n;
-                unit_at(u, m, n);
-                const int b_row = p.e.gated ? (rank ? p.up_row : 0) + n * b_rows : n * p.bn + rank * b_rows;
-                for (int kb = 0; kb < p.k_slabs; ++kb) {
-                    if (!long_wait(smem_addr(&ctl->empty[stage]), phase ^ 1u, &ctl->abort_flag)) { ok = false; break; }
-                    const uint32_t own = smem_addr(&ctl->full[stage]), bar = map_to_cta(own, 0);   // the leader's barrier
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        const uint32_t full0 = smem_addr(&ctl->full[0]), empty0 = smem_addr(&ctl->empty[0]), lead0 = (uint32_t)uniform((int)map_to_cta(full0, 0));
+        for (long long u = worker; u < units && ok; u += workers) {
+            int m, n;
+            unit_at(u, m, n);
+            const int b_row = p.e.gated ? (rank ? p.up_row : 0) + n * b_rows : n * p.bn + rank * b_rows;
+            for (int kb = 0; kb < p.k_slabs; ++kb) {
+                if (!__all_sync(0xffffffffu, long_wait(empty0 + 8 * stage, phase ^ 1u, &ctl->abort_flag))) { ok = false; break; }
+                if (elect_one()) {
+                    const uint32_t bar = lead0 + 8 * stage;             // the leader's barrier
                     const uint32_t sb = ring + stage * kStageBytes + ACC * kABytes;
-                    if (rank == 0) mbar_expect_tx(own, 2 * stage_tx);
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * stage, 2 * stage_tx);
 #pragma unroll
                     for (int a = 0; a < ACC; ++a) {
                         const uint32_t sa = ring + stage * kStageBytes + a * kABytes;
@@ -362,38 +374,42 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         if (!p.a_mn) {
                             tma_load_2d_pair(sa, &map_a, bar, kb * kBK, a_row);
                         } else {
+#pragma unroll
                             for (int j = 0; j < kTileRows / 64; ++j) tma_load_2d_pair(sa + j * kSlabBytes, &map_a, bar, a_row + j * 64, kb * kBK);
                         }
                     }
                     if (!p.b_mn) {
                         tma_load_2d_pair(sb, &map_b, bar, kb * kBK, b_row);
                     } else {
-                        for (int j = 0; j < b_rows / 64; ++j) tma_load_2d_pair(sb + j * kSlabBytes, &map_b, bar, b_row + j * 64, kb * kBK);
+                        tma_load_2d_pair(sb, &map_b, bar, b_row, kb * kBK);
+                        if (b_rows > 64) tma_load_2d_pair(sb + kSlabBytes, &map_b, bar, b_row + 64, kb * kBK);
                     }
-                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
                 }
+                __syncwarp();
+                if (++stage == kStages) { stage = 0; phase ^= 1u; }
             }
         }
     } else if (warp == 1) {
-        // ---------------- multiplies (one thread of the leader CTA) ----------------
-        if (lane == 0 && rank == 0) {
+        // ---------------- multiplies (the leader CTA) ----------------
+        if (rank == 0) {
             const uint32_t idesc = instr_desc(p.a_mn, p.b_mn, 2 * kTileRows, p.bn);
             const uint32_t a_step = p.a_mn ? (16 * 128) >> 4 : 32 >> 4, b_step = p.b_mn ? (16 * 128) >> 4 : 32 >> 4;
             int stage = 0, buf = 0;
             uint32_t phase = 0, tphase = 0;                // bit b: parity of accumulator b
             bool ok = true;
+            const uint32_t full0 = smem_addr(&ctl->full[0]), empty0 = smem_addr(&ctl->empty[0]);
             auto ready = [&](int st, uint32_t ph) {
-                ok = long_wait(smem_addr(&ctl->full[st]), ph, &ctl->abort_flag);
+                ok = __all_sync(0xffffffffu, long_wait(full0 + 8 * st, ph, &ctl->abort_flag));
                 tc_fence_after();
             };
             auto drained = [&](int b) {
-                ok = long_wait(smem_addr(&ctl->tmem_empty[b]), ((tphase >> b) & 1u) ^ 1u, &ctl->abort_flag);
+                ok = __all_sync(0xffffffffu, long_wait(smem_addr(&ctl->tmem_empty[b]), ((tphase >> b) & 1u) ^ 1u, &ctl->abort_flag));
                 tphase ^= 1u << b;
                 tc_fence_after();
             };
+            const uint64_t ad0 = smem_desc(ring, p.a_mn), bd0 = smem_desc(ring + ACC * kABytes, p.b_mn);
             auto multiply = [&](int st, int a, int b, bool first) {
-                const uint32_t base = ring + st * kStageBytes;
-                const uint64_t ad = smem_desc(base + a * kABytes, p.a_mn), bd = smem_desc(base + ACC * kABytes, p.b_mn);
+                const uint64_t ad = ad0 + (uint64_t)((st * kStageBytes + a * kABytes) >> 4), bd = bd0 + (uint64_t)((st * kStageBytes) >> 4);
 #pragma unroll
                 for (int k = 0; k < kBK / 16; ++k)
                     tc_mma2(tmem_base + (uint32_t)b * 256u, ad + (uint64_t)(k * a_step), bd + (uint64_t)(k * b_step), idesc, first && k == 0 ? 0u : 1u);
@@ -407,12 +423,15 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     for (int kb = 0; kb < p.k_slabs && ok; ++kb) {
                         ready(stage, phase);
                         if (!ok) break;
-                        multiply(stage, 0, buf, kb == 0);
-                        tc_commit2(smem_addr(&ctl->empty[stage]));       // frees the stage in both CTAs when these retire
+                        if (elect_one()) {
+                            multiply(stage, 0, buf, kb == 0);
+                            tc_commit2(empty0 + 8 * stage);              // frees the stage in both CTAs when these retire
+                            if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[buf]));
+                        }
+                        __syncwarp();
                         advance(stage, phase);
                     }
                     if (!ok) break;
-                    tc_commit2(smem_addr(&ctl->tmem_full[buf]));
                     buf ^= 1;
                 } else {
                     // accumulator 0 takes the ring's slabs while accumulator 1 may still be draining, which then catches up
@@ -423,8 +442,11 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     for (int kb = 0; kb < ahead && ok; ++kb) {
                         ready(st, ph);
                         if (!ok) break;
-                        multiply(st, 0, 0, kb == 0);
-                        if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
+                        if (elect_one()) {
+                            multiply(st, 0, 0, kb == 0);
+                            if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
+                        }
+                        __syncwarp();
                         advance(st, ph);
                     }
                     if (ok) drained(1);
@@ -432,15 +454,20 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         if (kb >= ahead) {
                             ready(stage, phase);
                             if (!ok) break;
-                            multiply(stage, 0, 0, false);
-                            if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
                         }
-                        multiply(stage, 1, 1, kb == 0);
-                        tc_commit2(smem_addr(&ctl->empty[stage]));
+                        if (elect_one()) {
+                            if (kb >= ahead) {
+                                multiply(stage, 0, 0, false);
+                                if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
+                            }
+                            multiply(stage, 1, 1, kb == 0);
+                            tc_commit2(empty0 + 8 * stage);
+                            if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[1]));
+                        }
+                        __syncwarp();
                         advance(stage, phase);
                     }
                     if (!ok) break;
-                    tc_commit2(smem_addr(&ctl->tmem_full[1]));
                 }
             }
         }
@@ -597,8 +624,8 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
     float* staged = reinterpret_cast<float*>(smem_raw + (ring - raw));
     const int stage_bytes = narrow_stage_bytes(p.nn);
     NarrowCtl* ctl = reinterpret_cast<NarrowCtl*>(smem_raw + (ring - raw) + narrow_ring_bytes(p.nn, p.stages));
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int split = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int split = uniform((int)cluster_nctarank()), rank = uniform((int)cluster_ctarank());
     const int it = blockIdx.x / split, jt = blockIdx.y;
     const int k0 = (int)((long long)p.k_slabs * rank / split), k1 = (int)((long long)p.k_slabs * (rank + 1) / split);
     const uint32_t columns = p.nn < 32 ? 32u : (uint32_t)p.nn;
@@ -620,16 +647,17 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem_base = ctl->tmem_base;
+    const uint32_t tmem_base = (uint32_t)uniform((int)ctl->tmem_base);
 
+    const uint32_t full0 = smem_addr(&ctl->full[0]), empty0 = smem_addr(&ctl->empty[0]);
     if (warp == 0) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            const int i0 = p.e.gated ? it * 64 : it * 128, i1 = p.e.gated ? p.up_row + i0 : i0 + 64;
-            for (int kb = k0; kb < k1; ++kb) {
-                if (!long_wait(smem_addr(&ctl->empty[stage]), phase ^ 1u, &ctl->abort_flag)) break;
-                const uint32_t bar = smem_addr(&ctl->full[stage]);
+        int stage = 0;
+        uint32_t phase = 0;
+        const int i0 = p.e.gated ? it * 64 : it * 128, i1 = p.e.gated ? p.up_row + i0 : i0 + 64;
+        for (int kb = k0; kb < k1; ++kb) {
+            if (!__all_sync(0xffffffffu, long_wait(empty0 + 8 * stage, phase ^ 1u, &ctl->abort_flag))) break;
+            if (elect_one()) {
+                const uint32_t bar = full0 + 8 * stage;
                 const uint32_t ss = ring + stage * stage_bytes, sf = ss + kABytes;
                 mbar_expect_tx(bar, (uint32_t)stage_bytes);
                 if (p.s_mn) {
@@ -644,28 +672,29 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
                 } else {
                     tma_load_2d(sf, &map_f, bar, kb * kBK, jt * p.nn);
                 }
-                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
             }
+            __syncwarp();
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = instr_desc(p.s_mn, p.f_mn, 128, p.nn);
-            const uint32_t s_step = p.s_mn ? (16 * 128) >> 4 : 32 >> 4, f_step = p.f_mn ? (16 * 128) >> 4 : 32 >> 4;
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (int kb = k0; kb < k1; ++kb) {
-                if (!long_wait(smem_addr(&ctl->full[stage]), phase, &ctl->abort_flag)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t ss = ring + stage * stage_bytes;
-                const uint64_t sd = smem_desc(ss, p.s_mn), fd = smem_desc(ss + kABytes, p.f_mn);
+        const uint32_t idesc = instr_desc(p.s_mn, p.f_mn, 128, p.nn);
+        const uint32_t s_step = p.s_mn ? (16 * 128) >> 4 : 32 >> 4, f_step = p.f_mn ? (16 * 128) >> 4 : 32 >> 4;
+        const uint64_t sd0 = smem_desc(ring, p.s_mn), fd0 = smem_desc(ring + kABytes, p.f_mn);
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int kb = k0; kb < k1; ++kb) {
+            if (!__all_sync(0xffffffffu, long_wait(full0 + 8 * stage, phase, &ctl->abort_flag))) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t at = (uint64_t)((stage * stage_bytes) >> 4);
 #pragma unroll
                 for (int k = 0; k < kBK / 16; ++k)
-                    tc_mma(tmem_base, sd + (uint64_t)(k * s_step), fd + (uint64_t)(k * f_step), idesc, (kb > k0 || k) ? 1u : 0u);
-                tc_commit(smem_addr(&ctl->empty[stage]));
-                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+                    tc_mma(tmem_base, sd0 + at + (uint64_t)(k * s_step), fd0 + at + (uint64_t)(k * f_step), idesc, (kb > k0 || k) ? 1u : 0u);
+                tc_commit(empty0 + 8 * stage);
+                if (kb + 1 == k1) tc_commit(smem_addr(&ctl->tmem_full));
             }
-            if (ok) tc_commit(smem_addr(&ctl->tmem_full));
+            __syncwarp();
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
     } else {
         // the accumulator goes to shared memory as [j][i] (the ring's memory: every copy has been multiplied by then)
