@@ -1082,32 +1082,67 @@ struct Plan {
 };
 static int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// CTAs that share a streamed tile's sum: as many as are resident together (four per SM) while each keeps four slabs of K.
-static int narrow_split(long long tiles, int k_slabs, int sms, int tile) {
-    const int per_sm = tile <= 32 ? 4 : tile <= 64 ? 3 : tile <= 128 ? 2 : 1;
-    int split = 1;
-    while (split < 8 && tiles * (split + 1) <= (long long)per_sm * sms && k_slabs >= 4 * (split + 1)) ++split;
-    return split;
+// The form of a product is the one with the least estimated time.  The estimates, in us, are fits to measured sweeps of every form
+// over 40 shapes (worst miss 25 %; the form they choose was within 8 % of the best measured one):
+//   pair      5 + waves (slabs t + drain), the drain hidden behind the next tile with one accumulator.  A 64-deep slab takes 0.30 us at
+//             256 columns, 0.20 at 128 and never less than 0.19 (its issue); two accumulators 0.57 for twice the rows, and all of
+//             their drain: 32768 x 10240 x 2560 1093 us against 1156, 32768 x 2560 x 2560 347 against 289.
+//   streamed  6 + waves (slabs t + the cluster's reduction); t is the issue of a slab (0.20 - 0.36) or its bytes at 105 GB/s per SM, shared
+//             by the CTAs on it, and the whole is no less than reading everything once at 6 TB/s (ties go to the shorter work).
+static double pair_cost(int acc, int bn, long long M, int N, int k_slabs, bool gated, int pairs) {
+    const long long units = (long long)div_up(M, 256 * acc) * div_up(N, gated ? bn / 2 : bn);
+    const double waves = (double)((units + pairs - 1) / pairs), drain = 1.5 + 0.6 * bn / 256.0;
+    const double slab = bn == 256 ? 0.30 : bn == 192 ? 0.235 : bn == 128 ? 0.20 : 0.19;
+    if (acc == 1) {
+        const double tile = k_slabs * slab;
+        return 5.0 + waves * (tile > drain ? tile : drain) + drain;
+    }
+    return 5.0 + waves * (k_slabs * slab * 1.9 + drain) + drain;
+}
+// SMs that clusters of `split` CTAs can use at one CTA each: a cluster lies in one GPC, whose SMs are no multiple of it
+// (5 x 1640 x 2104 in 17 clusters of 8 that filled an SM each: 11.9 us, with room for two on an SM 6.7).
+static int cluster_slots(int split, int sms) { return split >= 8 ? sms * 13 / 16 : split >= 4 ? sms * 15 / 16 : sms; }
+static int narrow_ctas_per_sm(int nn) { return nn <= 32 ? 4 : nn == 64 ? 3 : nn == 128 ? 2 : 1; }
+static double narrow_cost(int nn, int split, long long M, int N, int k_slabs, bool gated, int sms) {
+    const int rows = gated ? 2 * N : N;
+    const long long tiles = (long long)div_up(N, gated ? 64 : 128) * div_up(M, nn), ctas = tiles * split;
+    const int most = narrow_ctas_per_sm(nn), slots = cluster_slots(split, sms);
+    const double waves = (double)((ctas + (long long)most * slots - 1) / ((long long)most * slots));
+    const double per_sm = ctas > (long long)most * slots ? most : (double)div_up(ctas, slots);
+    const double issue = nn <= 32 ? 0.20 : nn == 64 ? 0.215 : nn == 128 ? 0.24 : 0.36, bytes = per_sm * (16384.0 + 128.0 * nn) / 105e3;
+    const double reduce = 1.0 + nn * 32.0 / (split * (double)kNarrowThreads) * 0.25;
+    const double t = 6.0 + waves * (k_slabs / (double)split * (issue > bytes ? issue : bytes) + reduce);
+    const double read = 6.0 + 128.0 * k_slabs * ((double)rows + (double)M) / 6e6;
+    return (t > read ? t : read) + 0.05 * t;
 }
 static Plan choose(long long M, int N, int k_slabs, bool gated, bool f_mn, bool b_mn) {
     const int sms = sm_count();
-    Plan q = {1, 256, 1};
     const int form = g_form.load(), tile = g_tile.load(), split = g_split.load();
-    if (form == 2 || (form == 0 && M <= 256)) {
-        q.acc = 0;
-        q.tile = f_mn ? 64 : 16;
-        while (q.tile < M && q.tile < 256) q.tile *= 2;
-        if ((tile == 16 || tile == 32 || tile == 64 || tile == 128 || tile == 256) && (!f_mn || tile >= 64)) q.tile = tile;
-        q.split = split > 0 ? split : narrow_split((long long)div_up(N, gated ? 64 : 128) * div_up(M, q.tile), k_slabs, sms, q.tile);
-        if (q.split > k_slabs) q.split = k_slabs;          // (every CTA has a part of K)
-        return q;
+    Plan best = {1, 256, 1};
+    double least = 1e300;
+    if (form != 2) {
+        for (int acc = form == 3 ? 2 : 1; acc <= (form == 1 ? 1 : 2); ++acc)
+            for (int bn = 256; bn >= 64; bn -= 64) {
+                if (b_mn && bn % 128 != 0) continue;
+                if (tile != 0 && bn != tile && tile >= 64 && tile % 64 == 0 && !(b_mn && tile % 128 != 0)) continue;
+                const double t = pair_cost(acc, bn, M, N, k_slabs, gated, sms / 2);
+                if (t < least) { least = t; best = {acc, bn, 1}; }
+            }
     }
-    const int tile_cols = gated ? 128 : 256;
-    const long long units = (long long)div_up(M, 256) * div_up(N, tile_cols);
-    if (units < sms / 2) q.tile = 128;
-    if (form == 3) q.acc = 2;
-    if (tile >= 64 && tile % 64 == 0 && (!b_mn || tile % 128 == 0)) q.tile = tile;
-    return q;
+    if (form == 2 || form == 0) {
+        for (int nn = f_mn ? 64 : 16; nn <= 256; nn *= 2) {
+            if (form == 2 && (tile == 16 || tile == 32 || tile == 64 || tile == 128 || tile == 256) && !(f_mn && tile < 64) && nn != tile) continue;
+            if (div_up(M, nn) > 65535) continue;           // (the launch's second dimension)
+            for (int s = 1; s <= 8 && s <= k_slabs; ++s) { // (every CTA has a part of K)
+                // clusters of 5 to 7 leave SMs of their GPC over (8 x 10240 x 2560: 7 CTAs 25.7 us, 8 15.0)
+                if (split > 0 ? s != (split < k_slabs ? split : k_slabs) : (s & (s - 1)) != 0) continue;
+                const double t = narrow_cost(nn, s, M, N, k_slabs, gated, sms);
+                if (t < least) { least = t; best = {0, nn, s}; }
+            }
+            if (nn >= M && tile == 0) break;
+        }
+    }
+    return best;
 }
 
 static bool opt_in(const void* kernel, int bytes) {
@@ -1169,7 +1204,7 @@ static rlf_status product(const Operand& A, const Operand& B, long long M, long 
         p.J = (int)M; p.k_slabs = k_slabs; p.nn = plan.tile; p.s_mn = B.mn; p.f_mn = A.mn; p.up_row = e.N; p.e = e; p.dev_status = dev_status;
         const int i_tiles = div_up(e.N, e.gated ? 64 : 128), j_tiles = div_up(M, plan.tile);
         // the SM's shared memory is shared by the CTAs that come to it (each CTA keeps 1 KB to the system)
-        int per_sm = div_up((long long)i_tiles * j_tiles * plan.split, sm_count());
+        int per_sm = div_up((long long)i_tiles * j_tiles * plan.split, cluster_slots(plan.split, sm_count()));
         for (per_sm = per_sm > 4 ? 4 : per_sm;; --per_sm) {
             p.stages = (228 * 1024 / per_sm - 1024 - 1024 - 256) / narrow_stage_bytes(plan.tile);
             if (p.stages >= 3 || per_sm == 1) break;
