@@ -771,28 +771,28 @@ def rlf_linear_bwd(grad_y, x, W, pre=None, act=ACT_NONE, gated=False, want_grad_
 GATE_NONE, GATE_COLUMN, GATE_ROW = 0, 1, 2
 
 
-def _norm_vectors(x, here, post_kind, pre_kind, gate_form, gate, **vectors):
+def _norm_vectors(T, D, here, post_kind, pre_kind, gate_form, gate, post_weight, post_bias, pre_weight, pre_bias):
     """Checks of the block norm's [D] vectors (one type among them) and its gate.
-    -> (their type's code, their addresses by name, the gate's address)"""
-    T, D = x.shape
-    if x.dtype not in _DTYPES:
-        raise TypeError("x must be bfloat16 or float32")
+    -> (their type's code, the addresses of post_weight, post_bias, pre_weight, pre_bias and the gate)"""
     if (gate is None) != (gate_form == GATE_NONE):
         raise ValueError("gate and gate_form go together")
-    there = [t for t in vectors.values() if t is not None]
-    if gate_form == GATE_COLUMN:
-        there.append(gate)
-    w_dt = there[0].dtype if there else _f32
+    if (post_kind == NORM_NONE) != (post_weight is None) or (post_weight is None and post_bias is not None):
+        raise ValueError("post_weight (and post_bias) belong to the post norm, which needs post_weight")
+    if (pre_kind == NORM_NONE) != (pre_weight is None) or (pre_weight is None and pre_bias is not None):
+        raise ValueError("pre_weight (and pre_bias) belong to the pre norm, which needs pre_weight")
+    first = post_weight if post_weight is not None else pre_weight
+    w_dt = _f32 if first is None else first.dtype
     if w_dt not in _DTYPES:
         raise TypeError("weights, biases and a column gate must be bfloat16 or float32")
-    for name, kind in (("post", post_kind), ("pre", pre_kind)):
-        if kind != NORM_NONE and vectors[name + "_weight"] is None:
-            raise ValueError("the %s norm needs %s_weight" % (name, name))
-        if kind == NORM_NONE and (vectors[name + "_weight"] is not None or vectors.get(name + "_bias") is not None):
-            raise ValueError("%s_weight and %s_bias belong to the %s norm" % (name, name, name))
-    at = {k: _at(t, here, k, w_dt, (D,)) for k, t in vectors.items()}
-    gp = _at(gate, here, "gate", w_dt if gate_form == GATE_COLUMN else _f32, (D,) if gate_form == GATE_COLUMN else (T,))
-    return _DTYPES[w_dt], at, gp
+    row = (D,)
+    if gate is None:
+        gp = None
+    elif gate_form == GATE_ROW:
+        gp = _at(gate, here, "gate", _f32, (T,))
+    else:
+        gp = _at(gate, here, "gate", w_dt, row)
+    return (_DTYPES[w_dt], _at(post_weight, here, "post_weight", w_dt, row), _at(post_bias, here, "post_bias", w_dt, row),
+            _at(pre_weight, here, "pre_weight", w_dt, row), _at(pre_bias, here, "pre_bias", w_dt, row), gp)
 
 
 def rlf_block_norm_fwd(x, residual, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, post_kind=NORM_RMS,
@@ -805,22 +805,31 @@ def rlf_block_norm_fwd(x, residual, post_weight=None, post_bias=None, pre_weight
     here = _device_of(x)
     xp, xs = _rows(x, here, "x")
     shape = T, D = x.shape
-    w_dt, at, gp = _norm_vectors(x, here, post_kind, pre_kind, gate_form, gate, post_weight=post_weight, post_bias=post_bias,
-                                 pre_weight=pre_weight, pre_bias=pre_bias)
     dt = x.dtype
-    rp = _at(residual, here, "residual", dt, shape)
+    if dt not in _DTYPES:
+        raise TypeError("x must be bfloat16 or float32")
     if residual is None:
         raise ValueError("residual is needed")
+    w_dt, w1, b1, w2, b2, gp = _norm_vectors(T, D, here, post_kind, pre_kind, gate_form, gate, post_weight, post_bias, pre_weight, pre_bias)
     if h_out is None:
         h_out = _dense_like(x)
-    if y_out is None and pre_kind != NORM_NONE:
+        hp = h_out.data_ptr()
+    else:
+        hp = _at(h_out, here, "h_out", dt, shape)
+    yp = None
+    if y_out is not None:
+        yp = _at(y_out, here, "y_out", dt, shape)
+    elif pre_kind != NORM_NONE:
         y_out = _dense_like(x)
+        yp = y_out.data_ptr()
     if stats_out is None:
         stats_out = x.new_empty((4, T), dtype=_f32)
+        sp = stats_out.data_ptr()
+    else:
+        sp = _at(stats_out, here, "stats_out", _f32, (4, T))
     _check(_lib.rlf_block_norm_fwd(
-        xp, xs, rp, _DTYPES[dt], T, D, at["post_weight"], at["post_bias"], post_kind, at["pre_weight"], at["pre_bias"], pre_kind, w_dt,
-        gp, gate_form, alpha, beta, eps, _at(h_out, here, "h_out", dt, shape), _at(y_out, here, "y_out", dt, shape),
-        _at(stats_out, here, "stats_out", _f32, (4, T)), _raw_stream(here)), "rlf_block_norm_fwd")
+        xp, xs, _at(residual, here, "residual", dt, shape), _DTYPES[dt], T, D, w1, b1, post_kind, w2, b2, pre_kind, w_dt, gp, gate_form,
+        alpha, beta, eps, hp, yp, sp, _raw_stream(here)), "rlf_block_norm_fwd")
     return h_out, y_out, stats_out
 
 
@@ -836,41 +845,52 @@ def rlf_block_norm_bwd(grad_y, grad_h, x, h, stats, post_weight=None, post_bias=
     here = _device_of(x)
     xp, xs = _rows(x, here, "x")
     shape = T, D = x.shape
-    w_dt, at, gp = _norm_vectors(x, here, post_kind, pre_kind, gate_form, gate, post_weight=post_weight, post_bias=post_bias,
-                                 pre_weight=pre_weight)
     dt = x.dtype
+    if dt not in _DTYPES:
+        raise TypeError("x must be bfloat16 or float32")
+    w_dt, w1, b1, w2, _, gp = _norm_vectors(T, D, here, post_kind, pre_kind, gate_form, gate, post_weight, post_bias, pre_weight, None)
     pre, post = pre_kind != NORM_NONE, post_kind != NORM_NONE
     if pre and (grad_y is None or h is None):
         raise ValueError("the pre norm needs grad_y and h")
     if not pre and grad_h is None:
         raise ValueError("without the pre norm grad_h is needed")
-    wanted = dict(grad_post_weight=post and want_grad_weight, grad_post_bias=post and want_grad_bias, grad_pre_weight=pre and want_grad_weight,
-                  grad_pre_bias=pre and want_grad_bias, grad_gate=gate_form != GATE_NONE and want_grad_gate)
-    out = dict(grad_x=grad_x, grad_residual=grad_residual, grad_gate=grad_gate, grad_post_weight=grad_post_weight,
-               grad_post_bias=grad_post_bias, grad_pre_weight=grad_pre_weight, grad_pre_bias=grad_pre_bias)
-    over_tokens = False
-    for k, want in wanted.items():
-        per_row = k == "grad_gate" and gate_form == GATE_ROW
-        if out[k] is None and want:
-            if accumulate and not per_row:
-                raise ValueError("accumulate needs the buffers that are added to")
-            out[k] = x.new_empty(T if per_row else D, dtype=_f32)
-        over_tokens = over_tokens or (out[k] is not None and not per_row)
-    if out["grad_x"] is None and want_grad_x:
-        out["grad_x"] = _dense_like(x)
-    if out["grad_residual"] is None and want_grad_residual:
-        out["grad_residual"] = _dense_like(x)
+
+    def rows(t, want, what):                     # a [T, D] output: (the tensor, its address)
+        if t is not None:
+            return t, _at(t, here, what, dt, shape)
+        if not want:
+            return None, None
+        t = _dense_like(x)
+        return t, t.data_ptr()
+
+    def vector(t, want, what, n, summed=True):   # a gradient over tokens (or, not summed, one per token)
+        if t is not None:
+            return t, _at(t, here, what, _f32, (n,))
+        if not want:
+            return None, None
+        if accumulate and summed:
+            raise ValueError("accumulate needs the buffers that are added to")
+        t = x.new_empty(n, dtype=_f32)
+        return t, t.data_ptr()
+
+    per_row = gate_form == GATE_ROW
+    grad_x, gxp = rows(grad_x, want_grad_x, "grad_x")
+    grad_residual, grp = rows(grad_residual, want_grad_residual, "grad_residual")
+    grad_gate, ggp = vector(grad_gate, want_grad_gate and gate is not None, "grad_gate", T if per_row else D, not per_row)
+    grad_post_weight, gw1 = vector(grad_post_weight, want_grad_weight and post, "grad_post_weight", D)
+    grad_post_bias, gb1 = vector(grad_post_bias, want_grad_bias and post, "grad_post_bias", D)
+    grad_pre_weight, gw2 = vector(grad_pre_weight, want_grad_weight and pre, "grad_pre_weight", D)
+    grad_pre_bias, gb2 = vector(grad_pre_bias, want_grad_bias and pre, "grad_pre_bias", D)
     wp, wn = None, 0
-    if workspace is not None or over_tokens:
+    if workspace is not None or gw1 or gb1 or gw2 or gb2 or (ggp and not per_row):
         workspace, wp, wn = _workspace(workspace, here, x, FN_BLOCK_NORM_BWD, T, 0, D, RLF_F32)
-    vec = lambda k: _at(out[k], here, k, _f32, (T,) if k == "grad_gate" and gate_form == GATE_ROW else (D,))
     _check(_lib.rlf_block_norm_bwd(
         _at(grad_y, here, "grad_y", dt, shape) if pre else None, _at(grad_h, here, "grad_h", dt, shape), xp, xs,
-        _at(h, here, "h", dt, shape) if pre else None, _DTYPES[dt], T, D, at["post_weight"], at["post_bias"], post_kind, at["pre_weight"],
-        pre_kind, w_dt, gp, gate_form, alpha, beta, _at(stats, here, "stats", _f32, (4, T)), _at(out["grad_x"], here, "grad_x", dt, shape),
-        _at(out["grad_residual"], here, "grad_residual", dt, shape), vec("grad_gate"), vec("grad_post_weight"), vec("grad_post_bias"),
-        vec("grad_pre_weight"), vec("grad_pre_bias"), 1 if accumulate else 0, wp, wn, _raw_stream(here)), "rlf_block_norm_bwd")
-    return out
+        _at(h, here, "h", dt, shape) if pre else None, _DTYPES[dt], T, D, w1, b1, post_kind, w2, pre_kind, w_dt, gp, gate_form, alpha, beta,
+        _at(stats, here, "stats", _f32, (4, T)), gxp, grp, ggp, gw1, gb1, gw2, gb2, 1 if accumulate else 0, wp, wn, _raw_stream(here)),
+        "rlf_block_norm_bwd")
+    return dict(grad_x=grad_x, grad_residual=grad_residual, grad_gate=grad_gate, grad_post_weight=grad_post_weight,
+                grad_post_bias=grad_post_bias, grad_pre_weight=grad_pre_weight, grad_pre_bias=grad_pre_bias)
 
 
 def step_arena_bytes(T, V, B, dt=RLF_BF16):

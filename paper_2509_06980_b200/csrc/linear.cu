@@ -69,6 +69,12 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
+// Launches of this file follow one another without a gap (programmatic dependent launch): a kernel may be set up while the one before
+// it still runs.  Each lets its successor start at once, and touches memory only after pdl_wait, that is when everything
+// before it in the stream has finished.
+__device__ __forceinline__ void pdl_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // What becomes of an accumulator: out[row][col] = act(acc + bias[col]) (times the up half, when gated) + res[row][col].
 struct Epilogue {
     int act, gated;
@@ -305,6 +311,7 @@ template <int ACC>
 __global__ void __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
                    const __grid_constant__ CUtensorMap map_pre, const PairParams p) {
+    pdl_start();
     constexpr int kStages = PairCfg<ACC>::kStages, kStageBytes = PairCfg<ACC>::kStageBytes;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_addr(smem_raw);
@@ -339,6 +346,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     __syncthreads();
     cluster_sync_all();                                    // both CTAs' barriers exist before either signals the other
     tc_fence_after();
+    pdl_wait();
     const uint32_t tmem_base = (uint32_t)uniform((int)ctl->tmem_base);
 
     // Raster: groups of row units; inside a group row units fastest, so that the workers running at one time cover a block of
@@ -593,6 +601,9 @@ __host__ __device__ constexpr int narrow_ring_bytes(int nn, int stages) {
     return r > staged ? r : (staged + 255) / 256 * 256;
 }
 
+__device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* map, int x, int y) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" :: "l"(map), "r"(x), "r"(y) : "memory");
+}
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t local_addr, uint32_t rank) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
@@ -618,6 +629,7 @@ __device__ __forceinline__ void narrow_bias_pre(const Epilogue& e, int row, int 
 
 __global__ void __launch_bounds__(kNarrowThreads)
 linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_f, const NarrowParams p) {
+    pdl_start();
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_addr(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;
@@ -650,10 +662,18 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
     const uint32_t tmem_base = (uint32_t)uniform((int)ctl->tmem_base);
 
     const uint32_t full0 = smem_addr(&ctl->full[0]), empty0 = smem_addr(&ctl->empty[0]);
+    const int i0 = p.e.gated ? it * 64 : it * 128, i1 = p.e.gated ? p.up_row + i0 : i0 + 64;
+    // the streamed operand's first slabs are on their way to L2 while the kernel before this one ends (L2 takes its writes too)
+    if (warp == 0 && elect_one())
+        for (int kb = k0; kb < k1 && kb < k0 + p.stages; ++kb) {
+            tma_prefetch_2d(&map_s, p.s_mn ? i0 : kb * kBK, p.s_mn ? kb * kBK : i0);
+            tma_prefetch_2d(&map_s, p.s_mn ? i1 : kb * kBK, p.s_mn ? kb * kBK : i1);
+        }
+    __syncwarp();
+    pdl_wait();
     if (warp == 0) {
         int stage = 0;
         uint32_t phase = 0;
-        const int i0 = p.e.gated ? it * 64 : it * 128, i1 = p.e.gated ? p.up_row + i0 : i0 + 64;
         for (int kb = k0; kb < k1; ++kb) {
             if (!__all_sync(0xffffffffu, long_wait(empty0 + 8 * stage, phase ^ 1u, &ctl->abort_flag))) break;
             if (elect_one()) {
@@ -785,6 +805,8 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
 template <int N, int R>
 __global__ void __launch_bounds__(256)
 linear_few_fwd_kernel(const __nv_bfloat16* __restrict__ x, long long x_stride, const __nv_bfloat16* __restrict__ W, long long T, int D, const Epilogue e) {
+    pdl_start();
+    pdl_wait();
     const int lane = threadIdx.x & 31;
     const long long t0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * R;
     if (t0 >= T) return;
@@ -797,7 +819,7 @@ linear_few_fwd_kernel(const __nv_bfloat16* __restrict__ x, long long x_stride, c
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int n = 0; n < N; ++n) acc[r][n] = 0ull;
-#pragma unroll(R == 1 ? 4 : 2)
+#pragma unroll(N <= 2 ? 4 : 2)
     for (int c = lane; c < nvec; c += 32) {
         uint4 xv[R];
 #pragma unroll
@@ -851,6 +873,8 @@ __global__ void __launch_bounds__(256)
 linear_few_bwd_kernel(const FewBwd p) {
     __shared__ float gz[kFewChunk][N];
     __shared__ float sum[256][9];
+    pdl_start();
+    pdl_wait();
     const int tx = threadIdx.x, ty = threadIdx.y, nx = blockDim.x, ny = blockDim.y, tid = ty * nx + tx;
     const int col = (blockIdx.x * nx + tx) * 8;
     const bool live = col < p.D;
@@ -884,31 +908,37 @@ linear_few_bwd_kernel(const FewBwd p) {
 #pragma unroll
                 for (int n = 0; n < N; ++n) bias[n] += gz[r][n];
         if (!live) continue;
-#pragma unroll 4
-        for (int r = ty; r < tokens; r += ny) {
-            const long long t = tc0 + r;
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (p.part_w) v = *reinterpret_cast<const uint4*>(p.x + t * p.x_stride + col);
-            const uint32_t q[4] = {v.x, v.y, v.z, v.w};
-            f2 d[4] = {0ull, 0ull, 0ull, 0ull};
+        // eight tokens' x at a time: their loads are all under way before the first is used
+        for (int r0 = ty; r0 < tokens; r0 += 8 * ny) {
+            uint4 v[8];
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const f2 g = f2_make(gz[r][n], gz[r][n]);
+            for (int k = 0; k < 8; ++k)
+                if (p.part_w && r0 + k * ny < tokens) v[k] = ld_stream(reinterpret_cast<const uint4*>(p.x + (tc0 + r0 + k * ny) * p.x_stride + col));
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    acc[n][k] = f2_fma(g, f2_make(bf_lo(q[k]), bf_hi(q[k])), acc[n][k]);
-                    d[k] = f2_fma(g, w[n][k], d[k]);
+            for (int b = 0; b < 8; ++b) {
+                const int r = r0 + b * ny;
+                if (r >= tokens) break;
+                f2 d[4] = {0ull, 0ull, 0ull, 0ull};
+                const uint32_t q[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    const f2 g = f2_make(gz[r][n], gz[r][n]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (p.part_w) acc[n][k] = f2_fma(g, f2_make(bf_lo(q[k]), bf_hi(q[k])), acc[n][k]);
+                        d[k] = f2_fma(g, w[n][k], d[k]);
+                    }
                 }
-            }
-            if (p.dx) {
-                uint32_t o[4];
+                if (p.dx) {
+                    uint32_t o[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float a, b;
-                    f2_split(d[k], a, b);
-                    o[k] = pack_bf16x2(a, b);
+                    for (int k = 0; k < 4; ++k) {
+                        float lo, hi;
+                        f2_split(d[k], lo, hi);
+                        o[k] = pack_bf16x2(lo, hi);
+                    }
+                    *reinterpret_cast<uint4*>(p.dx + (tc0 + r) * p.D + col) = make_uint4(o[0], o[1], o[2], o[3]);
                 }
-                *reinterpret_cast<uint4*>(p.dx + t * p.D + col) = make_uint4(o[0], o[1], o[2], o[3]);
             }
         }
     }
@@ -936,23 +966,35 @@ linear_few_bwd_kernel(const FewBwd p) {
     }
 }
 
-// partial rows -> sum, in a fixed order.  A CTA covers 32 columns; warp w adds the rows w, w + 32, ..., and the 32 sums in order.
+// partial rows -> sums, in a fixed order: the first `blocks` CTAs cover 32 columns each of one sum, the others of a second (the bias
+// gradient).  Warp w adds the rows w, w + 32, ..., and the 32 sums are added in order.
+struct Join {
+    const float* part[2];
+    long long width[2];
+    void* out[2];
+    int out_f32[2];
+    int parts, accumulate, blocks;
+};
 __global__ void __launch_bounds__(1024)
-linear_join_kernel(const float* __restrict__ part, int parts, long long width, int accumulate, void* out, int out_f32) {
+linear_join_kernel(const Join j) {
     __shared__ float acc[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long col = (long long)blockIdx.x * 32 + lane;
+    const int which = (int)blockIdx.x >= j.blocks ? 1 : 0;
+    const long long col = (long long)(blockIdx.x - (which ? j.blocks : 0)) * 32 + lane, width = j.width[which];
+    pdl_start();
+    pdl_wait();
     float s = 0.0f;
     if (col < width) {
-#pragma unroll 4
-        for (int k = warp; k < parts; k += 32) s += part[(long long)k * width + col];
+        const float* part = j.part[which] + col;
+#pragma unroll 8
+        for (int k = warp; k < j.parts; k += 32) s += part[(long long)k * width];
     }
     acc[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && col < width) {
         for (int w = 1; w < 32; ++w) s += acc[w][lane];
-        if (accumulate) s += load_any(out, out_f32, col);
-        store_any(out, out_f32, col, s);
+        if (j.accumulate) s += load_any(j.out[which], j.out_f32[which], col);
+        store_any(j.out[which], j.out_f32[which], col, s);
     }
 }
 
@@ -974,6 +1016,8 @@ template <int V, int ACT, bool GATED>
 __global__ void __launch_bounds__(256)
 linear_pregrad_kernel(const PreGrad p) {
     __shared__ float sum[8][32 * V + 1];
+    pdl_start();
+    pdl_wait();
     const int tx = threadIdx.x, ty = threadIdx.y;          // 32 x 8
     const int col = (blockIdx.x * 32 + tx) * V;
     const long long t0 = (long long)blockIdx.y * p.rows, t1 = min(p.T, t0 + p.rows);
@@ -1154,19 +1198,21 @@ static bool opt_in(const void* kernel, int bytes) {
     }) == 1;
 }
 
-static rlf_status launch_cluster(void* kernel, dim3 grid, int threads, int smem, int cluster, void** args, cudaStream_t s) {
+static rlf_status launch(const void* kernel, dim3 grid, dim3 threads, int smem, int cluster, void** args, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
+    cfg.blockDim = threads;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster;
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) {
         cudaGetLastError();
         return RLF_ERR_CUDA;
@@ -1214,7 +1260,7 @@ static rlf_status product(const Operand& A, const Operand& B, long long M, long 
         if (!encode(&mb, B, rows_b, 64) || !encode(&ma, A, M, plan.tile)) return RLF_ERR_CUDA;
         if (!opt_in((const void*)linear_narrow_kernel, 227 * 1024)) return RLF_ERR_CUDA;
         void* args[] = {&mb, &ma, &p};
-        return launch_cluster((void*)linear_narrow_kernel, dim3((unsigned)(i_tiles * plan.split), (unsigned)j_tiles), kNarrowThreads, smem, plan.split, args, s);
+        return launch((const void*)linear_narrow_kernel, dim3((unsigned)(i_tiles * plan.split), (unsigned)j_tiles), kNarrowThreads, smem, plan.split, args, s);
     }
     PairParams p = {};
     p.M = (int)M; p.m_units = div_up(M, 2 * kTileRows * plan.acc); p.k_slabs = k_slabs; p.bn = plan.tile;
@@ -1232,7 +1278,7 @@ static rlf_status product(const Operand& A, const Operand& B, long long M, long 
     if (e.vec_out && !make_tile_map(&mo, e.out, M, e.N, 1, e.out_stride, e.out_f32 != 0)) return RLF_ERR_CUDA;
     if (e.pre && e.vec_pre && !make_tile_map(&mp, e.pre, M, e.N, e.gated ? 2 : 1, e.pre_stride, false)) return RLF_ERR_CUDA;
     void* args[] = {&ma, &mb, &mo, &mp, &p};
-    return launch_cluster(kernel, dim3((unsigned)(2 * workers)), kPairThreads, kPairSmem, 2, args, s);
+    return launch(kernel, dim3((unsigned)(2 * workers)), kPairThreads, kPairSmem, 2, args, s);
 }
 
 static bool rows_aligned(const void* at, long long stride, int esz) { return aligned(at, 16) && stride * esz % 16 == 0; }
@@ -1265,31 +1311,45 @@ static rlf_status check_linear(int64_t T, int32_t D, int32_t N, int act, int gat
 }
 
 template <int R>
-static void launch_few_fwd(int N, unsigned grid, const __nv_bfloat16* x, long long xs, const __nv_bfloat16* W, int64_t T, int D, const Epilogue& e, cudaStream_t s) {
+static const void* few_fwd_kernel(int N) {
     switch (N) {
-        case 1: linear_few_fwd_kernel<1, R><<<grid, 256, 0, s>>>(x, xs, W, T, D, e); break;
-        case 2: linear_few_fwd_kernel<2, R><<<grid, 256, 0, s>>>(x, xs, W, T, D, e); break;
-        case 3: linear_few_fwd_kernel<3, R><<<grid, 256, 0, s>>>(x, xs, W, T, D, e); break;
-        default: linear_few_fwd_kernel<4, R><<<grid, 256, 0, s>>>(x, xs, W, T, D, e); break;
+        case 1: return (const void*)linear_few_fwd_kernel<1, R>;
+        case 2: return (const void*)linear_few_fwd_kernel<2, R>;
+        case 3: return (const void*)linear_few_fwd_kernel<3, R>;
+        default: return (const void*)linear_few_fwd_kernel<4, R>;
     }
 }
-
+static const void* few_bwd_kernel(int N) {
+    switch (N) {
+        case 1: return (const void*)linear_few_bwd_kernel<1>;
+        case 2: return (const void*)linear_few_bwd_kernel<2>;
+        case 3: return (const void*)linear_few_bwd_kernel<3>;
+        default: return (const void*)linear_few_bwd_kernel<4>;
+    }
+}
 template <int V, bool GATED>
-static void launch_pregrad(const PreGrad& p, dim3 grid, cudaStream_t s) {
-    const dim3 block(32, 8);
-    switch (p.act) {
-        case RLF_ACT_RELU: linear_pregrad_kernel<V, RLF_ACT_RELU, GATED><<<grid, block, 0, s>>>(p); break;
-        case RLF_ACT_SILU: linear_pregrad_kernel<V, RLF_ACT_SILU, GATED><<<grid, block, 0, s>>>(p); break;
-        case RLF_ACT_GELU: linear_pregrad_kernel<V, RLF_ACT_GELU, GATED><<<grid, block, 0, s>>>(p); break;
-        case RLF_ACT_GELU_TANH: linear_pregrad_kernel<V, RLF_ACT_GELU_TANH, GATED><<<grid, block, 0, s>>>(p); break;
-        default: linear_pregrad_kernel<V, RLF_ACT_NONE, GATED><<<grid, block, 0, s>>>(p); break;
+static const void* pregrad_kernel(int act) {
+    switch (act) {
+        case RLF_ACT_RELU: return (const void*)linear_pregrad_kernel<V, RLF_ACT_RELU, GATED>;
+        case RLF_ACT_SILU: return (const void*)linear_pregrad_kernel<V, RLF_ACT_SILU, GATED>;
+        case RLF_ACT_GELU: return (const void*)linear_pregrad_kernel<V, RLF_ACT_GELU, GATED>;
+        case RLF_ACT_GELU_TANH: return (const void*)linear_pregrad_kernel<V, RLF_ACT_GELU_TANH, GATED>;
+        default: return (const void*)linear_pregrad_kernel<V, RLF_ACT_NONE, GATED>;
     }
 }
-
-static rlf_status launch_join(const float* part, int parts, long long width, int accumulate, void* out, int out_f32, cudaStream_t s) {
-    linear_join_kernel<<<(unsigned)((width + 31) / 32), 1024, 0, s>>>(part, parts, width, accumulate, out, out_f32);
-    count_launch();
-    return cuda_ok(cudaGetLastError());
+// sums of the slices' partial rows of grad_W (nullable) and grad_bias (nullable)
+static rlf_status launch_join(int parts, int accumulate, const float* part_w, long long width_w, void* grad_W, int w_f32, const float* part_b,
+                              long long width_b, float* grad_bias, cudaStream_t s) {
+    Join j = {};
+    j.parts = parts;
+    j.accumulate = accumulate;
+    j.part[0] = part_w; j.width[0] = grad_W ? width_w : 0; j.out[0] = grad_W; j.out_f32[0] = w_f32;
+    j.part[1] = part_b; j.width[1] = grad_bias ? width_b : 0; j.out[1] = grad_bias; j.out_f32[1] = 1;
+    j.blocks = div_up(j.width[0], 32);
+    const unsigned grid = (unsigned)(j.blocks + div_up(j.width[1], 32));
+    if (grid == 0) return RLF_OK;
+    void* args[] = {&j};
+    return launch((const void*)linear_join_kernel, dim3(grid), dim3(1024), 0, 1, args, s);
 }
 
 }  // namespace ln
@@ -1329,10 +1389,10 @@ extern "C" rlf_status rlf_linear_fwd(const void* x, int64_t T, int32_t D, int64_
     if (!gated && N <= kFewOutputs) {
         const __nv_bfloat16* xb = static_cast<const __nv_bfloat16*>(x);
         const __nv_bfloat16* wb = static_cast<const __nv_bfloat16*>(W);
-        if (T >= 8ll * 4 * sm_count()) launch_few_fwd<4>(N, (unsigned)((T + 31) / 32), xb, x_stride, wb, T, D, e, s);
-        else launch_few_fwd<1>(N, (unsigned)((T + 7) / 8), xb, x_stride, wb, T, D, e, s);
-        count_launch();
-        return cuda_ok(cudaGetLastError());
+        long long xs = x_stride, tokens = T;
+        void* args[] = {&xb, &xs, &wb, &tokens, &D, &e};
+        const bool two = T >= 8ll * 2 * sm_count();
+        return launch(two ? few_fwd_kernel<2>(N) : few_fwd_kernel<1>(N), dim3((unsigned)div_up(T, two ? 16 : 8)), dim3(256), 0, 1, args, s);
     }
     return product({x, x_stride, 0}, {W, D, 0}, T, D, e, dev_status, s);
 }
@@ -1382,18 +1442,17 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
         p.T = T; p.rows = per_slice; p.D = D;
         int nx = 1;
         while (nx < 256 && nx * 8 < D) nx *= 2;
-        const dim3 block(nx, 256 / nx), grid((unsigned)((D + nx * 8 - 1) / (nx * 8)), (unsigned)used);
-        switch (N) {
-            case 1: linear_few_bwd_kernel<1><<<grid, block, 0, s>>>(p); break;
-            case 2: linear_few_bwd_kernel<2><<<grid, block, 0, s>>>(p); break;
-            case 3: linear_few_bwd_kernel<3><<<grid, block, 0, s>>>(p); break;
-            default: linear_few_bwd_kernel<4><<<grid, block, 0, s>>>(p); break;
-        }
-        count_launch();
-        if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
-        if (grad_W) st = launch_join(p.part_w, used, (long long)N * D, accumulate, grad_W, grad_W_dt == RLF_F32, s);
-        if (st == RLF_OK && grad_bias) st = launch_join(part_b, used, N, accumulate, grad_bias, 1, s);
-        return st;
+        // as many slices as make whole generations of three CTAs per SM, within what the workspace holds
+        const int columns = div_up(D, nx * 8);
+        int parts = 3 * sm_count() / columns;
+        if (parts > slices) parts = slices;
+        if (parts < 1) parts = 1;
+        p.rows = (T + parts - 1) / parts;
+        parts = div_up(T, p.rows);
+        void* args[] = {&p};
+        st = launch(few_bwd_kernel(N), dim3((unsigned)columns, (unsigned)parts), dim3(nx, 256 / nx), 0, 1, args, s);
+        if (st != RLF_OK) return st;
+        return launch_join(parts, accumulate, p.part_w, (long long)N * D, grad_W, grad_W_dt == RLF_F32, part_b, N, grad_bias, s);
     }
 
     // gz: grad_y itself where nothing is to be done to it and TMA can read it
@@ -1408,11 +1467,11 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
         p.gz_stride = up8(rows); p.part_b = part_b; p.T = T; p.rows = per_slice; p.N = N;
         const bool wide = N % 8 == 0 && rows_aligned(grad_y, grad_y_stride, (int)ysz) && (!p.pre || aligned(p.pre, 16));
         const dim3 grid((unsigned)((N + (wide ? 255 : 31)) / (wide ? 256 : 32)), (unsigned)used);
-        if (wide) gated ? launch_pregrad<8, true>(p, grid, s) : launch_pregrad<8, false>(p, grid, s);
-        else gated ? launch_pregrad<1, true>(p, grid, s) : launch_pregrad<1, false>(p, grid, s);
-        count_launch();
-        if (cudaGetLastError() != cudaSuccess) return RLF_ERR_CUDA;
-        if (grad_bias) st = launch_join(part_b, used, rows, accumulate, grad_bias, 1, s);
+        const void* kernel = wide ? (gated ? pregrad_kernel<8, true>(act) : pregrad_kernel<8, false>(act))
+                                  : (gated ? pregrad_kernel<1, true>(act) : pregrad_kernel<1, false>(act));
+        void* args[] = {&p};
+        st = launch(kernel, grid, dim3(32, 8), 0, 1, args, s);
+        if (st == RLF_OK && grad_bias) st = launch_join(used, accumulate, nullptr, 0, nullptr, 1, part_b, rows, grad_bias, s);
         if (st != RLF_OK) return st;
     }
     if (grad_x) {
