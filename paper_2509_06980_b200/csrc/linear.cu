@@ -146,9 +146,52 @@ template <int ACT> __device__ __forceinline__ float act_slope(float z) {
     }
     return 1.0f;
 }
+// The same on two values at a time: packed arithmetic leaves the epilogue to the exponentials and reciprocals (two a value), which
+// are then what bounds it.
+__device__ __forceinline__ f2 f2_each(f2 v, float (*f)(float)) {
+    float a, b;
+    f2_split(v, a, b);
+    return f2_make(f(a), f(b));
+}
+__device__ __forceinline__ f2 f2_of(float v) { return f2_make(v, v); }
+__device__ __forceinline__ f2 sigmoid2(f2 minus_log2e_x) {      // of x, given -x log2 e
+    const f2 e = f2_each(minus_log2e_x, ex2_approx);
+    return f2_each(f2_add(e, f2_of(1.0f)), rcp_approx);
+}
+template <int ACT> __device__ __forceinline__ f2 act_value2(f2 z) {
+    if (ACT == RLF_ACT_SILU) return f2_mul(z, sigmoid2(f2_mul(z, f2_of(-kLog2e))));
+    if (ACT == RLF_ACT_GELU_TANH) {
+        const f2 u = f2_mul(z, f2_of(-2.0f * kGeluRoot * kLog2e));
+        return f2_mul(z, sigmoid2(f2_mul(u, f2_fma(f2_mul(z, f2_of(kGeluCube)), z, f2_of(1.0f)))));
+    }
+    if (ACT == RLF_ACT_GELU) {
+        float a, b, p, q;
+        f2_split(z, a, b);
+        const f2 t = f2_each(f2_fma(f2_make(fabsf(a), fabsf(b)), f2_of(0.43f * 0.70710678f), f2_of(1.0f)), rcp_approx);
+        const f2 e = f2_each(f2_mul(f2_mul(z, f2_of(-0.5f * kLog2e)), z), ex2_approx);
+        f2 g = f2_of(0.036572903f);
+        g = f2_fma(g, t, f2_of(-0.15404779f));
+        g = f2_fma(g, t, f2_of(0.1899436f));
+        g = f2_fma(g, t, f2_of(-0.041152104f));
+        g = f2_fma(g, t, f2_of(0.12254031f));
+        g = f2_fma(g, t, f2_of(0.102736264f));
+        g = f2_fma(g, t, f2_of(0.12214691f));
+        g = f2_fma(g, t, f2_of(0.12125991f));
+        f2_split(f2_mul(f2_mul(g, t), e), p, q);
+        return f2_mul(z, f2_make(a < 0.0f ? p : 1.0f - p, b < 0.0f ? q : 1.0f - q));
+    }
+    float a, b;
+    f2_split(z, a, b);
+    return f2_make(act_value<ACT>(a), act_value<ACT>(b));
+}
 template <int ACT, int N> __device__ __forceinline__ void act_all(float (&v)[N]) {
+    if constexpr (N % 2 == 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = act_value<ACT>(v[i]);
+        for (int i = 0; i < N; i += 2) f2_split(act_value2<ACT>(f2_make(v[i], v[i + 1])), v[i], v[i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = act_value<ACT>(v[i]);
+    }
 }
 template <int N> __device__ __forceinline__ void activate(int act, float (&v)[N]) {
     switch (act) {
@@ -1266,7 +1309,10 @@ static rlf_status product(const Operand& A, const Operand& B, long long M, long 
     p.M = (int)M; p.m_units = div_up(M, 2 * kTileRows * plan.acc); p.k_slabs = k_slabs; p.bn = plan.tile;
     p.n_tiles = div_up(e.N, e.gated ? plan.tile / 2 : plan.tile);
     p.a_mn = A.mn; p.b_mn = B.mn; p.up_row = e.N; p.e = e; p.dev_status = dev_status;
-    p.group = 8 / plan.acc;
+    // about 28 MB of A's rows are live at a time (8192 x 4096 x 16384: groups of 4, 8, 16 units 826, 788, 779 us sustained; 32768 x 10240 x
+    // 2560: 1340, 1353, 1370)
+    const double panel = 512.0 * plan.acc * (double)K;
+    p.group = panel > 7e6 ? 4 : panel < 1.75e6 ? 16 : (int)(28e6 / panel);
     if (!encode(&ma, A, M, kTileRows) || !encode(&mb, B, rows_b, plan.tile / 2)) return RLF_ERR_CUDA;
     void* const kernel = plan.acc == 2 ? (void*)linear_pair_kernel<2> : (void*)linear_pair_kernel<1>;
     if (!opt_in(kernel, kPairSmem)) return RLF_ERR_CUDA;
@@ -1283,9 +1329,13 @@ static rlf_status product(const Operand& A, const Operand& B, long long M, long 
 
 static bool rows_aligned(const void* at, long long stride, int esz) { return aligned(at, 16) && stride * esz % 16 == 0; }
 
-// slices of tokens of the elementwise passes (each leaves one partial row of a weight or bias gradient)
+// slices of tokens of the elementwise passes (each leaves one partial row of a weight or bias gradient; a single one is the gradient)
 static int token_slices(int64_t T) {
     const int64_t n = (T + 31) / 32;
+    return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
+}
+static int few_slices(int64_t T) {
+    const int64_t n = (T + 7) / 8;
     return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
 }
 static long long up8(long long n) { return (n + 7) & ~7ll; }
@@ -1294,7 +1344,7 @@ struct BwdWs { size_t gz, part_b, part_w, total; };
 static BwdWs bwd_workspace(int64_t T, int32_t rows, int32_t D) {
     BwdWs w;
     size_t o = 0;
-    const size_t slices = (size_t)token_slices(T);
+    const size_t slices = (size_t)(rows <= kFewOutputs ? few_slices(T) : token_slices(T));
     w.gz = o;     o += rows <= kFewOutputs ? 0 : up256((size_t)T * (size_t)up8(rows) * 2);
     w.part_b = o; o += up256(slices * (size_t)rows * 4);
     w.part_w = o; o += rows <= kFewOutputs ? up256(slices * (size_t)rows * (size_t)D * 4) : 0;
@@ -1445,7 +1495,7 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
         // as many slices as make whole generations of three CTAs per SM, within what the workspace holds
         const int columns = div_up(D, nx * 8);
         int parts = 3 * sm_count() / columns;
-        if (parts > slices) parts = slices;
+        if (parts > few_slices(T)) parts = few_slices(T);
         if (parts < 1) parts = 1;
         p.rows = (T + parts - 1) / parts;
         parts = div_up(T, p.rows);
@@ -1464,14 +1514,15 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
         p.dy = grad_y; p.dy_stride = grad_y_stride; p.dy_f32 = grad_y_dt == RLF_F32; p.act = act; p.gated = gated;
         p.pre = need_pre ? static_cast<const __nv_bfloat16*>(pre) : nullptr;
         p.gz = !in_place && (grad_x || grad_W) ? reinterpret_cast<__nv_bfloat16*>(base + ws.gz) : nullptr;
-        p.gz_stride = up8(rows); p.part_b = part_b; p.T = T; p.rows = per_slice; p.N = N;
+        const bool direct = used == 1 && !accumulate;
+        p.gz_stride = up8(rows); p.part_b = direct ? grad_bias : part_b; p.T = T; p.rows = per_slice; p.N = N;
         const bool wide = N % 8 == 0 && rows_aligned(grad_y, grad_y_stride, (int)ysz) && (!p.pre || aligned(p.pre, 16));
         const dim3 grid((unsigned)((N + (wide ? 255 : 31)) / (wide ? 256 : 32)), (unsigned)used);
         const void* kernel = wide ? (gated ? pregrad_kernel<8, true>(act) : pregrad_kernel<8, false>(act))
                                   : (gated ? pregrad_kernel<1, true>(act) : pregrad_kernel<1, false>(act));
         void* args[] = {&p};
         st = launch(kernel, grid, dim3(32, 8), 0, 1, args, s);
-        if (st == RLF_OK && grad_bias) st = launch_join(used, accumulate, nullptr, 0, nullptr, 1, part_b, rows, grad_bias, s);
+        if (st == RLF_OK && grad_bias && !direct) st = launch_join(used, accumulate, nullptr, 0, nullptr, 1, part_b, rows, grad_bias, s);
         if (st != RLF_OK) return st;
     }
     if (grad_x) {
