@@ -714,20 +714,24 @@ def rlf_linear_fwd(x, W, bias=None, act=ACT_NONE, gated=False, residual=None, ou
     shape = (T, N)
     if y_out is None:
         y_out = x.new_empty(shape, dtype=out_dtype or (_bf16 if residual is None else residual.dtype))
-    elif out_dtype is not None and y_out.dtype != out_dtype:
-        raise TypeError("y_out must be %s" % out_dtype)
+        yp = y_out.data_ptr()
+    else:
+        yp = _at(y_out, here, "y_out", out_dtype, shape)
     dt = _dt(y_out, "the output")
     rp, rs = None, 0
     if residual is not None:
         if residual.shape != shape or residual.dtype != y_out.dtype:
             raise ValueError("residual must have the shape and type of the output")
         rp, rs = _rows(residual, here, "residual")
-    if pre_out is None and want_pre:
+    zp = None
+    if pre_out is not None:
+        zp = _at(pre_out, here, "pre_out", _bf16, (T, rows))
+    elif want_pre:
         pre_out = x.new_empty((T, rows))
+        zp = pre_out.data_ptr()
     _check(_lib.rlf_linear_fwd(
         xp, T, D, xs, _at(W, here, "W", _bf16), N, _at(bias, here, "bias", None, (rows,)), 0 if bias is None else _dt(bias, "bias"),
-        act, 1 if gated else 0, rp, rs, _at(y_out, here, "y_out", None, shape), dt, _at(pre_out, here, "pre_out", _bf16, (T, rows)),
-        _at(dev_status, here, "dev_status", _i32t), _raw_stream(here)), "rlf_linear_fwd")
+        act, 1 if gated else 0, rp, rs, yp, dt, zp, _at(dev_status, here, "dev_status", _i32t), _raw_stream(here)), "rlf_linear_fwd")
     return y_out, pre_out
 
 
@@ -753,18 +757,28 @@ def rlf_linear_bwd(grad_y, x, W, pre=None, act=ACT_NONE, gated=False, want_grad_
         raise ValueError("an activation or a gate needs pre, the z of the forward call")
     if accumulate and ((grad_W is None and want_grad_W) or (grad_bias is None and want_grad_bias)):
         raise ValueError("accumulate needs the buffers that are added to")
-    if grad_x is None and want_grad_x:
+    xo = wo = bo = None
+    w_dt = RLF_F32
+    if grad_x is not None:
+        xo = _at(grad_x, here, "grad_x", _bf16, (T, D))
+    elif want_grad_x:
         grad_x = x.new_empty((T, D))
-    if grad_W is None and want_grad_W:
+        xo = grad_x.data_ptr()
+    if grad_W is not None:
+        wo, w_dt = _at(grad_W, here, "grad_W", None, (rows, D)), _dt(grad_W, "grad_W")
+    elif want_grad_W:
         grad_W = x.new_empty((rows, D), dtype=grad_W_dtype)
-    if grad_bias is None and want_grad_bias:
+        wo, w_dt = grad_W.data_ptr(), _dt(grad_W, "grad_W")
+    if grad_bias is not None:
+        bo = _at(grad_bias, here, "grad_bias", _f32, (rows,))
+    elif want_grad_bias:
         grad_bias = x.new_empty(rows, dtype=_f32)
+        bo = grad_bias.data_ptr()
     workspace, wp, wn = _workspace(workspace, here, x, FN_LINEAR_BWD, T, rows, D, RLF_BF16)
     _check(_lib.rlf_linear_bwd(
         gp, _dt(grad_y, "grad_y"), gs, _at(pre, here, "pre", _bf16, (T, rows)), xp, T, D, xs, _at(W, here, "W", _bf16), N, act,
-        1 if gated else 0, _at(grad_x, here, "grad_x", _bf16, (T, D)), _at(grad_W, here, "grad_W", None, (rows, D)),
-        RLF_F32 if grad_W is None else _dt(grad_W, "grad_W"), _at(grad_bias, here, "grad_bias", _f32, (rows,)),
-        1 if accumulate else 0, wp, wn, _at(dev_status, here, "dev_status", _i32t), _raw_stream(here)), "rlf_linear_bwd")
+        1 if gated else 0, xo, wo, w_dt, bo, 1 if accumulate else 0, wp, wn, _at(dev_status, here, "dev_status", _i32t),
+        _raw_stream(here)), "rlf_linear_bwd")
     return grad_x, grad_W, grad_bias
 
 
