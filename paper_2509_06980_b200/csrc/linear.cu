@@ -245,7 +245,8 @@ constexpr int kDrainBytes = kDrainWarps * (kDrainTile + 128);
 constexpr int kPairSmem = kRingBytes + kDrainBytes + 1024 + 256;
 static_assert(kPairSmem <= 227 * 1024, "the most shared memory a CTA can have");
 
-struct PairParams {
+// One launch multiplies one product or two (a backward pass' dx and dW: no launch and no ragged last wave between them).
+struct PairProblem {
     int M;                          // output rows
     int m_units, n_tiles, k_slabs;  // 256-row units, column tiles, 64-deep slabs
     int bn;                         // accumulator columns of a tile (gated: half of them gate, half up)
@@ -253,7 +254,15 @@ struct PairParams {
     int group;                      // row units that are taken together (see the raster)
     int up_row;                     // gated: B's row with which the up half begins
     Epilogue e;
+};
+struct PairParams {
+    PairProblem q[2];
+    long long units0, units;        // tiles of the first product, of both
+    int mixed;                      // an output is fp32: a drain tile is then one store's at a time
     int32_t* dev_status;
+};
+struct alignas(64) PairMaps {
+    CUtensorMap a[2], b[2], out[2], pre;
 };
 
 struct PairCtl {
@@ -352,8 +361,7 @@ __device__ __forceinline__ void load_residual(const Epilogue& e, int row, bool r
 
 template <int ACC>
 __global__ void __launch_bounds__(kPairThreads, 1)
-linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
-                   const __grid_constant__ CUtensorMap map_pre, const PairParams p) {
+linear_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ PairParams p) {
     pdl_start();
     constexpr int kStages = PairCfg<ACC>::kStages, kStageBytes = PairCfg<ACC>::kStageBytes;
     extern __shared__ unsigned char smem_raw[];
@@ -364,9 +372,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = uniform((int)pair_rank());
     const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1;
-    const long long units = (long long)p.m_units * p.n_tiles;
-    const int b_rows = p.bn / 2;                           // rows of B that a CTA stages
-    const uint32_t stage_tx = (uint32_t)(ACC * kABytes + b_rows * kBK * 2);
+    const long long units = p.units;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -394,12 +400,16 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
     // Raster: groups of row units; inside a group row units fastest, so that the workers running at one time cover a block of
     // about as many rows as columns and share both operands through L2.
-    auto unit_at = [&](long long u, int& m, int& n) {
-        const long long per_group = (long long)p.group * p.n_tiles;
+    auto unit_at = [&](long long u, int& m, int& n) -> int {
+        const int which = u >= p.units0 ? 1 : 0;
+        const PairProblem& q = p.q[which];
+        if (which) u -= p.units0;
+        const long long per_group = (long long)q.group * q.n_tiles;
         const int g = (int)(u / per_group);
-        const int within = (int)(u - g * per_group), rows_here = min(p.group, p.m_units - g * p.group);
+        const int within = (int)(u - g * per_group), rows_here = min(q.group, q.m_units - g * q.group);
         n = within / rows_here;
-        m = g * p.group + (within - n * rows_here);
+        m = g * q.group + (within - n * rows_here);
+        return which;
     };
 
     if (warp == 0) {
@@ -410,9 +420,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         const uint32_t full0 = smem_addr(&ctl->full[0]), empty0 = smem_addr(&ctl->empty[0]), lead0 = (uint32_t)uniform((int)map_to_cta(full0, 0));
         for (long long u = worker; u < units && ok; u += workers) {
             int m, n;
-            unit_at(u, m, n);
-            const int b_row = p.e.gated ? (rank ? p.up_row : 0) + n * b_rows : n * p.bn + rank * b_rows;
-            for (int kb = 0; kb < p.k_slabs; ++kb) {
+            const int which = unit_at(u, m, n);
+            const PairProblem& q = p.q[which];
+            const CUtensorMap *map_a = &maps.a[which], *map_b = &maps.b[which];
+            const int b_rows = q.bn / 2, k_slabs = q.k_slabs, a_mn = q.a_mn, b_mn = q.b_mn;            // (b_rows: rows of B that a CTA stages)
+            const int b_row = q.e.gated ? (rank ? q.up_row : 0) + n * b_rows : n * q.bn + rank * b_rows;
+            const uint32_t stage_tx = (uint32_t)(ACC * kABytes + b_rows * kBK * 2);
+            for (int kb = 0; kb < k_slabs; ++kb) {
                 if (!__all_sync(0xffffffffu, long_wait(empty0 + 8 * stage, phase ^ 1u, &ctl->abort_flag))) { ok = false; break; }
                 if (elect_one()) {
                     const uint32_t bar = lead0 + 8 * stage;             // the leader's barrier
@@ -422,18 +436,18 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     for (int a = 0; a < ACC; ++a) {
                         const uint32_t sa = ring + stage * kStageBytes + a * kABytes;
                         const int a_row = (2 * (ACC * m + a) + rank) * kTileRows;
-                        if (!p.a_mn) {
-                            tma_load_2d_pair(sa, &map_a, bar, kb * kBK, a_row);
+                        if (!a_mn) {
+                            tma_load_2d_pair(sa, map_a, bar, kb * kBK, a_row);
                         } else {
 #pragma unroll
-                            for (int j = 0; j < kTileRows / 64; ++j) tma_load_2d_pair(sa + j * kSlabBytes, &map_a, bar, a_row + j * 64, kb * kBK);
+                            for (int j = 0; j < kTileRows / 64; ++j) tma_load_2d_pair(sa + j * kSlabBytes, map_a, bar, a_row + j * 64, kb * kBK);
                         }
                     }
-                    if (!p.b_mn) {
-                        tma_load_2d_pair(sb, &map_b, bar, kb * kBK, b_row);
+                    if (!b_mn) {
+                        tma_load_2d_pair(sb, map_b, bar, kb * kBK, b_row);
                     } else {
-                        tma_load_2d_pair(sb, &map_b, bar, b_row, kb * kBK);
-                        if (b_rows > 64) tma_load_2d_pair(sb + kSlabBytes, &map_b, bar, b_row + 64, kb * kBK);
+                        tma_load_2d_pair(sb, map_b, bar, b_row, kb * kBK);
+                        if (b_rows > 64) tma_load_2d_pair(sb + kSlabBytes, map_b, bar, b_row + 64, kb * kBK);
                     }
                 }
                 __syncwarp();
@@ -443,8 +457,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     } else if (warp == 1) {
         // ---------------- multiplies (the leader CTA) ----------------
         if (rank == 0) {
-            const uint32_t idesc = instr_desc(p.a_mn, p.b_mn, 2 * kTileRows, p.bn);
-            const uint32_t a_step = p.a_mn ? (16 * 128) >> 4 : 32 >> 4, b_step = p.b_mn ? (16 * 128) >> 4 : 32 >> 4;
+            uint32_t idesc = 0, a_step = 0, b_step = 0;
+            uint64_t ad0 = 0, bd0 = 0;
+            int k_slabs = 0;
             int stage = 0, buf = 0;
             uint32_t phase = 0, tphase = 0;                // bit b: parity of accumulator b
             bool ok = true;
@@ -458,7 +473,6 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 tphase ^= 1u << b;
                 tc_fence_after();
             };
-            const uint64_t ad0 = smem_desc(ring, p.a_mn), bd0 = smem_desc(ring + ACC * kABytes, p.b_mn);
             auto multiply = [&](int st, int a, int b, bool first) {
                 const uint64_t ad = ad0 + (uint64_t)((st * kStageBytes + a * kABytes) >> 4), bd = bd0 + (uint64_t)((st * kStageBytes) >> 4);
 #pragma unroll
@@ -469,15 +483,22 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 if (++st == kStages) { st = 0; ph ^= 1u; }
             };
             for (long long u = worker; u < units && ok; u += workers) {
+                const PairProblem& q = p.q[u >= p.units0 ? 1 : 0];
+                idesc = instr_desc(q.a_mn, q.b_mn, 2 * kTileRows, q.bn);
+                a_step = q.a_mn ? (16 * 128) >> 4 : 32 >> 4;
+                b_step = q.b_mn ? (16 * 128) >> 4 : 32 >> 4;
+                ad0 = smem_desc(ring, q.a_mn);
+                bd0 = smem_desc(ring + ACC * kABytes, q.b_mn);
+                k_slabs = q.k_slabs;
                 if constexpr (ACC == 1) {
                     drained(buf);
-                    for (int kb = 0; kb < p.k_slabs && ok; ++kb) {
+                    for (int kb = 0; kb < k_slabs && ok; ++kb) {
                         ready(stage, phase);
                         if (!ok) break;
                         if (elect_one()) {
                             multiply(stage, 0, buf, kb == 0);
                             tc_commit2(empty0 + 8 * stage);              // frees the stage in both CTAs when these retire
-                            if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[buf]));
+                            if (kb + 1 == k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[buf]));
                         }
                         __syncwarp();
                         advance(stage, phase);
@@ -486,7 +507,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     buf ^= 1;
                 } else {
                     // accumulator 0 takes the ring's slabs while accumulator 1 may still be draining, which then catches up
-                    const int ahead = min(kStages, p.k_slabs);
+                    const int ahead = min(kStages, k_slabs);
                     drained(0);
                     int st = stage;
                     uint32_t ph = phase;
@@ -495,13 +516,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         if (!ok) break;
                         if (elect_one()) {
                             multiply(st, 0, 0, kb == 0);
-                            if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
+                            if (kb + 1 == k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
                         }
                         __syncwarp();
                         advance(st, ph);
                     }
                     if (ok) drained(1);
-                    for (int kb = 0; kb < p.k_slabs && ok; ++kb) {
+                    for (int kb = 0; kb < k_slabs && ok; ++kb) {
                         if (kb >= ahead) {
                             ready(stage, phase);
                             if (!ok) break;
@@ -509,11 +530,11 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         if (elect_one()) {
                             if (kb >= ahead) {
                                 multiply(stage, 0, 0, false);
-                                if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
+                                if (kb + 1 == k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[0]));
                             }
                             multiply(stage, 1, 1, kb == 0);
                             tc_commit2(empty0 + 8 * stage);
-                            if (kb + 1 == p.k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[1]));
+                            if (kb + 1 == k_slabs) tc_commit2(smem_addr(&ctl->tmem_full[1]));
                         }
                         __syncwarp();
                         advance(stage, phase);
@@ -524,24 +545,25 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         }
     } else {
         // ---------------- epilogue: one row per thread, two warps share a row's 32-column pieces ----------------
-        const Epilogue& e = p.e;
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         Drain d;
         d.tile = drain + (warp - 2) * kDrainTile;
         d.bias = reinterpret_cast<float*>(drain + kDrainWarps * kDrainTile) + (warp - 2) * 32;
         d.lane = lane;
         d.next = 0;
-        const int width = e.gated ? p.bn / 2 : p.bn;
         int buf = 0;
         uint32_t tphase = 0;
         for (long long u = worker; u < units; u += workers) {
             int m, n;
-            unit_at(u, m, n);
+            const int which = unit_at(u, m, n);
+            const Epilogue& e = p.q[which].e;
+            const CUtensorMap* map_out = &maps.out[which];
+            const int width = e.gated ? p.q[which].bn / 2 : p.q[which].bn, M = p.q[which].M;
             bool alive = true;
 #pragma unroll 1
             for (int a = 0; a < ACC && alive; ++a) {
             const int row = (2 * (ACC * m + a) + rank) * kTileRows + quarter * 32 + lane;
-            const bool row_ok = row < p.M;
+            const bool row_ok = row < M;
             int got = 0;
             if (lane == 0) got = long_wait(smem_addr(&ctl->tmem_full[buf]), (tphase >> buf) & 1u, &ctl->abort_flag) ? 1 : 0;
             if (!__shfl_sync(0xffffffffu, got, 0)) {
@@ -570,7 +592,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         for (int i = 0; i < 32; ++i) v[i] += d.bias[i];
                         __syncwarp();
                     }
-                    if (e.pre) store_piece<false>(d, &map_pre, e.vec_pre, half_of_w, e.out_f32, e.pre + shift, e.pre_stride, row - lane, p.M, col, nvalid, v);
+                    if (e.pre) store_piece<false>(d, &maps.pre, e.vec_pre, half_of_w, p.mixed, e.pre + shift, e.pre_stride, row - lane, M, col, nvalid, v);
                 };
                 take((uint32_t)(c * 32), 0);
                 activate<32>(e.act, v);
@@ -586,8 +608,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] += r[i];
                 }
-                if (e.out_f32) store_piece<true>(d, &map_out, e.vec_out, 0, true, e.out, e.out_stride, row - lane, p.M, col, nvalid, v);
-                else store_piece<false>(d, &map_out, e.vec_out, 0, false, e.out, e.out_stride, row - lane, p.M, col, nvalid, v);
+                if (e.out_f32) store_piece<true>(d, map_out, e.vec_out, 0, true, e.out, e.out_stride, row - lane, M, col, nvalid, v);
+                else store_piece<false>(d, map_out, e.vec_out, 0, p.mixed, e.out, e.out_stride, row - lane, M, col, nvalid, v);
             }
             tc_fence_before();
             __syncwarp();
@@ -1202,7 +1224,11 @@ static double narrow_cost(int nn, int split, long long M, int N, int k_slabs, bo
     const double read = 6.0 + 128.0 * k_slabs * ((double)rows + (double)M) / 6e6;
     return (t > read ? t : read) + 0.05 * t;
 }
-static Plan choose(long long M, int N, int k_slabs, bool gated, bool f_mn, bool b_mn) {
+static bool wanted_bn(int bn, bool b_mn, int tile) {
+    if (b_mn && bn % 128 != 0) return false;
+    return !(tile != 0 && bn != tile && tile >= 64 && tile % 64 == 0 && !(b_mn && tile % 128 != 0));
+}
+static Plan choose(long long M, int N, int k_slabs, bool gated, bool f_mn, bool b_mn, double* cost) {
     const int sms = sm_count();
     const int form = g_form.load(), tile = g_tile.load(), split = g_split.load();
     Plan best = {1, 256, 1};
@@ -1210,8 +1236,7 @@ static Plan choose(long long M, int N, int k_slabs, bool gated, bool f_mn, bool 
     if (form != 2) {
         for (int acc = form == 3 ? 2 : 1; acc <= (form == 1 ? 1 : 2); ++acc)
             for (int bn = 256; bn >= 64; bn -= 64) {
-                if (b_mn && bn % 128 != 0) continue;
-                if (tile != 0 && bn != tile && tile >= 64 && tile % 64 == 0 && !(b_mn && tile % 128 != 0)) continue;
+                if (!wanted_bn(bn, b_mn, tile)) continue;
                 const double t = pair_cost(acc, bn, M, N, k_slabs, gated, sms / 2);
                 if (t < least) { least = t; best = {acc, bn, 1}; }
             }
@@ -1229,6 +1254,7 @@ static Plan choose(long long M, int N, int k_slabs, bool gated, bool f_mn, bool 
             if (nn >= M && tile == 0) break;
         }
     }
+    *cost = least;
     return best;
 }
 
@@ -1279,52 +1305,113 @@ static bool make_tile_map(CUtensorMap* map, const void* base, long long rows, in
 }
 
 // out[m][n] = epilogue(sum_k A[m][k] B[n][k]), M rows, e.N columns (gated: B has 2 e.N rows), K terms
-static rlf_status product(const Operand& A, const Operand& B, long long M, long long K, const Epilogue& e, int32_t* dev_status, cudaStream_t s) {
-    const int rows_b = e.gated ? 2 * e.N : e.N;
-    const int k_slabs = div_up(K, kBK);
-    const Plan plan = choose(M, e.N, k_slabs, e.gated, A.mn, B.mn);
+struct Product {
+    Operand A, B;
+    long long M, K;
+    Epilogue e;
+    int k_slabs() const { return div_up(K, kBK); }
+    int rows_b() const { return e.gated ? 2 * e.N : e.N; }
+};
+static bool encode(CUtensorMap* map, const Operand& o, long long K, long long rows, int box_rows) {
+    return o.mn ? make_map(map, o.at, (uint64_t)K, (uint64_t)rows, (uint64_t)o.stride, 64, 64)
+                : make_map(map, o.at, (uint64_t)rows, (uint64_t)K, (uint64_t)o.stride, 64, (uint32_t)box_rows);
+}
+static rlf_status launch_narrow(const Product& g, const Plan& plan, int32_t* dev_status, cudaStream_t s) {
+    NarrowParams p = {};
     CUtensorMap ma, mb;
-    auto encode = [&](CUtensorMap* map, const Operand& o, long long rows, int box_rows) {
-        return o.mn ? make_map(map, o.at, (uint64_t)K, (uint64_t)rows, (uint64_t)o.stride, 64, 64)
-                    : make_map(map, o.at, (uint64_t)rows, (uint64_t)K, (uint64_t)o.stride, 64, (uint32_t)box_rows);
-    };
-    if (plan.acc == 0) {
-        NarrowParams p = {};
-        p.J = (int)M; p.k_slabs = k_slabs; p.nn = plan.tile; p.s_mn = B.mn; p.f_mn = A.mn; p.up_row = e.N; p.e = e; p.dev_status = dev_status;
-        const int i_tiles = div_up(e.N, e.gated ? 64 : 128), j_tiles = div_up(M, plan.tile);
-        // the SM's shared memory is shared by the CTAs that come to it (each CTA keeps 1 KB to the system)
-        int per_sm = div_up((long long)i_tiles * j_tiles * plan.split, cluster_slots(plan.split, sm_count()));
-        for (per_sm = per_sm > 4 ? 4 : per_sm;; --per_sm) {
-            p.stages = (228 * 1024 / per_sm - 1024 - 1024 - 256) / narrow_stage_bytes(plan.tile);
-            if (p.stages >= 3 || per_sm == 1) break;
-        }
-        if (p.stages > kMaxNarrowStages) p.stages = kMaxNarrowStages;
-        const int smem = narrow_ring_bytes(plan.tile, p.stages) + 1024 + 256;
-        if (!encode(&mb, B, rows_b, 64) || !encode(&ma, A, M, plan.tile)) return RLF_ERR_CUDA;
-        if (!opt_in((const void*)linear_narrow_kernel, 227 * 1024)) return RLF_ERR_CUDA;
-        void* args[] = {&mb, &ma, &p};
-        return launch((const void*)linear_narrow_kernel, dim3((unsigned)(i_tiles * plan.split), (unsigned)j_tiles), kNarrowThreads, smem, plan.split, args, s);
+    p.J = (int)g.M; p.k_slabs = g.k_slabs(); p.nn = plan.tile; p.s_mn = g.B.mn; p.f_mn = g.A.mn; p.up_row = g.e.N; p.e = g.e; p.dev_status = dev_status;
+    const int i_tiles = div_up(g.e.N, g.e.gated ? 64 : 128), j_tiles = div_up(g.M, plan.tile);
+    // the SM's shared memory is shared by the CTAs that come to it (each CTA keeps 1 KB to the system)
+    int per_sm = div_up((long long)i_tiles * j_tiles * plan.split, cluster_slots(plan.split, sm_count()));
+    for (per_sm = per_sm > 4 ? 4 : per_sm;; --per_sm) {
+        p.stages = (228 * 1024 / per_sm - 1024 - 1024 - 256) / narrow_stage_bytes(plan.tile);
+        if (p.stages >= 3 || per_sm == 1) break;
     }
+    if (p.stages > kMaxNarrowStages) p.stages = kMaxNarrowStages;
+    const int smem = narrow_ring_bytes(plan.tile, p.stages) + 1024 + 256;
+    if (!encode(&mb, g.B, g.K, g.rows_b(), 64) || !encode(&ma, g.A, g.K, g.M, plan.tile)) return RLF_ERR_CUDA;
+    if (!opt_in((const void*)linear_narrow_kernel, 227 * 1024)) return RLF_ERR_CUDA;
+    void* args[] = {&mb, &ma, &p};
+    return launch((const void*)linear_narrow_kernel, dim3((unsigned)(i_tiles * plan.split), (unsigned)j_tiles), kNarrowThreads, smem, plan.split, args, s);
+}
+// one product, or two with tiles of their own widths
+static rlf_status launch_pair(const Product* g, int count, int acc, const int* bn, int32_t* dev_status, cudaStream_t s) {
     PairParams p = {};
-    p.M = (int)M; p.m_units = div_up(M, 2 * kTileRows * plan.acc); p.k_slabs = k_slabs; p.bn = plan.tile;
-    p.n_tiles = div_up(e.N, e.gated ? plan.tile / 2 : plan.tile);
-    p.a_mn = A.mn; p.b_mn = B.mn; p.up_row = e.N; p.e = e; p.dev_status = dev_status;
-    // about 28 MB of A's rows are live at a time (8192 x 4096 x 16384: groups of 4, 8, 16 units 826, 788, 779 us sustained; 32768 x 10240 x
-    // 2560: 1340, 1353, 1370)
-    const double panel = 512.0 * plan.acc * (double)K;
-    p.group = panel > 7e6 ? 4 : panel < 1.75e6 ? 16 : (int)(28e6 / panel);
-    if (!encode(&ma, A, M, kTileRows) || !encode(&mb, B, rows_b, plan.tile / 2)) return RLF_ERR_CUDA;
-    void* const kernel = plan.acc == 2 ? (void*)linear_pair_kernel<2> : (void*)linear_pair_kernel<1>;
+    PairMaps maps;
+    for (int i = 0; i < count; ++i) {
+        PairProblem& q = p.q[i];
+        const Epilogue& e = g[i].e;
+        q.M = (int)g[i].M; q.m_units = div_up(g[i].M, 2 * kTileRows * acc); q.k_slabs = g[i].k_slabs(); q.bn = bn[i];
+        q.n_tiles = div_up(e.N, e.gated ? bn[i] / 2 : bn[i]);
+        q.a_mn = g[i].A.mn; q.b_mn = g[i].B.mn; q.up_row = e.N; q.e = e;
+        // about 28 MB of A's rows are live at a time (8192 x 4096 x 16384: groups of 4, 8, 16 units 826, 788, 779 us sustained; 32768 x 10240 x
+        // 2560: 1340, 1353, 1370)
+        const double panel = 512.0 * acc * (double)g[i].K;
+        q.group = panel > 7e6 ? 4 : panel < 1.75e6 ? 16 : (int)(28e6 / panel);
+        p.units += (long long)q.m_units * q.n_tiles;
+        if (i == 0) p.units0 = p.units;
+        p.mixed |= e.out_f32;
+        if (!encode(&maps.a[i], g[i].A, g[i].K, g[i].M, kTileRows) || !encode(&maps.b[i], g[i].B, g[i].K, g[i].rows_b(), bn[i] / 2)) return RLF_ERR_CUDA;
+        // output tiles: 32 columns x one half x 32 rows
+        maps.out[i] = maps.a[i];
+        if (e.vec_out && !make_tile_map(&maps.out[i], e.out, g[i].M, e.N, 1, e.out_stride, e.out_f32 != 0)) return RLF_ERR_CUDA;
+    }
+    maps.pre = maps.a[0];
+    const Epilogue& e = g[0].e;
+    if (e.pre && e.vec_pre && !make_tile_map(&maps.pre, e.pre, g[0].M, e.N, e.gated ? 2 : 1, e.pre_stride, false)) return RLF_ERR_CUDA;
+    if (count == 1) maps.a[1] = maps.b[1] = maps.out[1] = maps.a[0];
+    p.dev_status = dev_status;
+    const void* const kernel = acc == 2 ? (const void*)linear_pair_kernel<2> : (const void*)linear_pair_kernel<1>;
     if (!opt_in(kernel, kPairSmem)) return RLF_ERR_CUDA;
-    const long long units = (long long)p.m_units * p.n_tiles;
     const int pairs = sm_count() / 2;
-    const int workers = units < pairs ? (int)units : pairs;
-    // output tiles: 32 columns x one half x 32 rows
-    CUtensorMap mo = ma, mp = ma;
-    if (e.vec_out && !make_tile_map(&mo, e.out, M, e.N, 1, e.out_stride, e.out_f32 != 0)) return RLF_ERR_CUDA;
-    if (e.pre && e.vec_pre && !make_tile_map(&mp, e.pre, M, e.N, e.gated ? 2 : 1, e.pre_stride, false)) return RLF_ERR_CUDA;
-    void* args[] = {&ma, &mb, &mo, &mp, &p};
+    const int workers = p.units < pairs ? (int)p.units : pairs;
+    void* args[] = {&maps, &p};
     return launch(kernel, dim3((unsigned)(2 * workers)), kPairThreads, kPairSmem, 2, args, s);
+}
+static rlf_status run(const Product& g, const Plan& plan, int32_t* dev_status, cudaStream_t s) {
+    if (plan.acc == 0) return launch_narrow(g, plan, dev_status, s);
+    return launch_pair(&g, 1, plan.acc, &plan.tile, dev_status, s);
+}
+static Plan choose(const Product& g, double* cost) { return choose(g.M, g.e.N, g.k_slabs(), g.e.gated, g.A.mn, g.B.mn, cost); }
+static rlf_status product(const Product& g, int32_t* dev_status, cudaStream_t s) {
+    double cost;
+    return run(g, choose(g, &cost), dev_status, s);
+}
+// Two products that depend on the same things: in one launch where that is estimated to be an eighth shorter than one after the other
+// (backward of 2048 x 1024 x 1024 20 -> 12 us, 1000 x 2560 x 2560 34 -> 24, 4096 x 2560 x 2560 89 -> 76; below that margin it
+// loses: 32768 x 1024 x 1024 at 0.99 of the estimate 116 -> 145).  The product with the longer tiles comes first; its tiles and the
+// other's are dealt to the pairs as one list.
+static rlf_status both_products(const Product& first, const Product& second, int32_t* dev_status, cudaStream_t s) {
+    double c0, c1, least = 1e300;
+    const Plan p0 = choose(first, &c0), p1 = choose(second, &c1);
+    const int tile = g_tile.load(), pairs = sm_count() / 2;
+    int bn[2] = {256, 256};
+    const bool swap = first.k_slabs() < second.k_slabs();
+    const Product &g0 = swap ? second : first, &g1 = swap ? first : second;
+    if (g_form.load() <= 1)
+        for (int b0 = 256; b0 >= 64; b0 -= 64)
+            for (int b1 = 256; b1 >= 64; b1 -= 64) {
+                if (!wanted_bn(b0, g0.B.mn, tile) || !wanted_bn(b1, g1.B.mn, tile)) continue;
+                double all = 0.0, longest = 0.0, drain = 0.0;
+                const Product* const g[2] = {&g0, &g1};
+                for (int i = 0; i < 2; ++i) {
+                    const int b = i ? b1 : b0;
+                    const double d = 1.5 + 0.6 * b / 256.0, slabs = g[i]->k_slabs() * (b == 256 ? 0.30 : b == 192 ? 0.235 : b == 128 ? 0.20 : 0.19);
+                    const double t = slabs > d ? slabs : d;
+                    all += t * div_up(g[i]->M, 256) * (double)div_up(g[i]->e.N, b);
+                    longest = t > longest ? t : longest;
+                    drain = d;                             // (the last tiles are the second product's)
+                }
+                const double even = all / pairs + 0.5 * (div_up(g1.M, 256) * (double)div_up(g1.e.N, b1) >= pairs ? longest * 0.5 : longest);
+                const double t = 5.0 + (even > longest ? even : longest) + drain;
+                if (t < least) { least = t; bn[0] = b0; bn[1] = b1; }
+            }
+    if (least < 0.87 * (c0 + c1 - 3.0)) {                  // (3 us: the second launch is set up under the first)
+        const Product g[2] = {g0, g1};
+        return launch_pair(g, 2, 1, bn, dev_status, s);
+    }
+    const rlf_status st = run(first, p0, dev_status, s);
+    return st == RLF_OK ? run(second, p1, dev_status, s) : st;
 }
 
 static bool rows_aligned(const void* at, long long stride, int esz) { return aligned(at, 16) && stride * esz % 16 == 0; }
@@ -1444,7 +1531,7 @@ extern "C" rlf_status rlf_linear_fwd(const void* x, int64_t T, int32_t D, int64_
         const bool two = T >= 8ll * 2 * sm_count();
         return launch(two ? few_fwd_kernel<2>(N) : few_fwd_kernel<1>(N), dim3((unsigned)div_up(T, two ? 16 : 8)), dim3(256), 0, 1, args, s);
     }
-    return product({x, x_stride, 0}, {W, D, 0}, T, D, e, dev_status, s);
+    return product({{x, x_stride, 0}, {W, D, 0}, T, D, e}, dev_status, s);
 }
 
 extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, int64_t grad_y_stride, const void* pre, const void* x, int64_t T,
@@ -1525,20 +1612,14 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
         if (st == RLF_OK && grad_bias && !direct) st = launch_join(used, accumulate, nullptr, 0, nullptr, 1, part_b, rows, grad_bias, s);
         if (st != RLF_OK) return st;
     }
-    if (grad_x) {
-        Epilogue e = {};
-        e.N = D; e.out = grad_x; e.out_stride = D; e.vec_out = e.vec_res = 1;
-        st = product(gz, {W, D, 1}, T, rows, e, dev_status, s);
-        if (st != RLF_OK) return st;
-    }
-    if (grad_W) {
-        Epilogue e = {};
-        e.N = D; e.out = grad_W; e.out_stride = D; e.out_f32 = grad_W_dt == RLF_F32;
-        e.vec_out = e.vec_res = rows_aligned(grad_W, D, (int)wsz);
-        if (accumulate) { e.res = grad_W; e.res_stride = D; }
-        st = product({gz.at, gz.stride, 1}, {x, x_stride, 1}, rows, T, e, dev_status, s);
-    }
-    return st;
+    Product gx = {gz, {W, D, 1}, T, rows, {}}, gw = {{gz.at, gz.stride, 1}, {x, x_stride, 1}, rows, T, {}};
+    gx.e.N = D; gx.e.out = grad_x; gx.e.out_stride = D; gx.e.vec_out = gx.e.vec_res = 1;
+    gw.e.N = D; gw.e.out = grad_W; gw.e.out_stride = D; gw.e.out_f32 = grad_W_dt == RLF_F32;
+    gw.e.vec_out = gw.e.vec_res = rows_aligned(grad_W, D, (int)wsz);
+    if (accumulate) { gw.e.res = grad_W; gw.e.res_stride = D; }
+    if (grad_x && grad_W) return both_products(gx, gw, dev_status, s);
+    if (grad_x) return product(gx, dev_status, s);
+    return grad_W ? product(gw, dev_status, s) : RLF_OK;
 }
 
 extern "C" rlf_status rlf_tune_linear(int form, int tile, int split) {
