@@ -70,8 +70,9 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 // Launches of this file follow one another without a gap (programmatic dependent launch): a kernel may be set up while the one before
-// it still runs.  Each lets its successor start at once, and touches memory only after pdl_wait, that is when everything
-// before it in the stream has finished.
+// it still runs.  Each lets its successor start at once (once it has its tensor memory: a successor on the same SM that took
+// it first would wait for this kernel's end while this one waited for the memory), and reads and writes memory only after
+// pdl_wait, that is when everything before it in the stream has finished.
 __device__ __forceinline__ void pdl_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -362,7 +363,6 @@ __device__ __forceinline__ void load_residual(const Epilogue& e, int row, bool r
 template <int ACC>
 __global__ void __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ PairParams p) {
-    pdl_start();
     constexpr int kStages = PairCfg<ACC>::kStages, kStageBytes = PairCfg<ACC>::kStageBytes;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_addr(smem_raw);
@@ -395,6 +395,7 @@ linear_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant_
     __syncthreads();
     cluster_sync_all();                                    // both CTAs' barriers exist before either signals the other
     tc_fence_after();
+    pdl_start();
     pdl_wait();
     const uint32_t tmem_base = (uint32_t)uniform((int)ctl->tmem_base);
 
@@ -694,7 +695,6 @@ __device__ __forceinline__ void narrow_bias_pre(const Epilogue& e, int row, int 
 
 __global__ void __launch_bounds__(kNarrowThreads)
 linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_f, const NarrowParams p) {
-    pdl_start();
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_addr(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;
@@ -724,6 +724,7 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_start();
     const uint32_t tmem_base = (uint32_t)uniform((int)ctl->tmem_base);
 
     const uint32_t full0 = smem_addr(&ctl->full[0]), empty0 = smem_addr(&ctl->empty[0]);
