@@ -143,7 +143,8 @@ template <int ACT> __device__ __forceinline__ float act_slope(float z) {
     }
     if (ACT == RLF_ACT_GELU_TANH) {
         const float s = sigmoid(2.0f * kGeluRoot * z * fmaf(kGeluCube * z, z, 1.0f));
-        return s + z * s * (1.0f - s) * 2.0f * kGeluRoot * fmaf(3.0f * kGeluCube * z, z, 1.0f);
+        // (s (1 - s) is zero long before |z| = 100; z^2 that overflows would make its product NaN)
+        return s + z * s * (1.0f - s) * 2.0f * kGeluRoot * fmaf(3.0f * kGeluCube, fminf(z * z, 1e4f), 1.0f);
     }
     return 1.0f;
 }

@@ -299,3 +299,33 @@ def test_wrapper_refuses():
         b.rlf_linear_bwd(dy, x, W, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
     with pytest.raises(b.RlfError):
         b.rlf_linear_bwd(dy, x, W, grad_W=torch.zeros(24, 64, dtype=BF, device=DEV), accumulate=True, want_grad_x=False)
+
+
+@pytest.mark.parametrize("kind", ACTS)
+@pytest.mark.parametrize("N,gated", [(2, False), (72, False), (71, False), (72, True), (71, True)])
+def test_large_values_before_the_activation(N, gated, kind):
+    """Finite values up to the type's largest, whose squares overflow fp32: z of column 0 is x's first element, every other
+    column (and its part of W) is zero, the up half is one.  One term per sum, so an output is off by the activation's own error
+    and its rounding, a gradient by those of the slope and of gz and itself to bf16."""
+    b = gc.binding()
+    big = [0.5, 3.0, 100.0, 3e4, 1e10, 6e19, 1e30, 3e38]
+    x = torch.zeros(2 * len(big), 8, dtype=BF, device=DEV)
+    x[:, 0] = torch.tensor(big + [-v for v in big])
+    rows = 2 * N if gated else N
+    W = torch.zeros(rows, 8, dtype=BF, device=DEV)
+    W[0, 0] = 1.0
+    bias = torch.zeros(rows, device=DEV)
+    if gated:
+        bias[N:] = 1.0
+    y, pre = b.rlf_linear_fwd(x, W, bias=bias, act=kind, gated=gated, want_pre=True)
+    z = _f64(x)[:, :1]
+    small = np.minimum(np.abs(z), 100.0)        # (beyond that the slope is 0 or 1 to every digit)
+    want = b64.act(z, kind)
+    err = np.abs(_f64(y)[:, :1] - want)
+    assert (err <= 1.01 * (2.0 ** -8 + _act_error(small, kind)) * np.abs(want) + 1e-30).all()
+    dy = torch.ones(len(x), N, dtype=BF, device=DEV)
+    gx, _, _ = b.rlf_linear_bwd(dy, x, W, pre=pre, act=kind, gated=gated, want_grad_W=False)
+    slope = b64.act_grad(z, kind)
+    bound = (_act_error(small, kind) + 8 * U) * (1 + small) + 2 * 2.0 ** -8 * np.abs(slope)
+    err = np.abs(_f64(gx)[:, :1] - slope)
+    assert (err <= 1.01 * bound).all()
