@@ -333,31 +333,54 @@ __device__ __forceinline__ void store_piece(Drain& d, const CUtensorMap* map, bo
     }
     __syncwarp();
 }
-// 32 columns of this thread's row of the residual
-__device__ __forceinline__ void load_residual(const Epilogue& e, int row, bool row_ok, int col, int nvalid, float (&r)[32]) {
-    if (!row_ok) return;
-    const long long at = row * e.res_stride + col;
-    if (e.vec_res && nvalid == 32) {
-        if (e.out_f32) {
-            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(e.res) + at);
+// A 32 x 32 piece of the residual on its way: 32 columns of this thread's row where rows lie on 16-byte boundaries, else this
+// lane's column of the 32 rows (by row, element after element, a warp touches 32 rows at once: 2047 x 1024 x 4099 91 us, so
+// 32).  It is fetched before the piece's accumulator is waited for.
+struct Residual {
+    uint32_t q[32];
+    bool by_row;
+};
+__device__ __forceinline__ void fetch_residual(const Epilogue& e, int row, int M, int lane, int col, int nvalid, Residual& r) {
+    r.by_row = e.vec_res && nvalid == 32;
+    if (r.by_row) {
+        if (row >= M) return;
+        const char* from = static_cast<const char*>(e.res) + (row * e.res_stride + col) * (e.out_f32 ? 4 : 2);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 q = p[i];
-                r[4 * i] = q.x; r[4 * i + 1] = q.y; r[4 * i + 2] = q.z; r[4 * i + 3] = q.w;
-            }
-        } else {
-            const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(e.res) + at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 q = p[i];
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) { r[8 * i + 2 * k] = bf_lo(w[k]); r[8 * i + 2 * k + 1] = bf_hi(w[k]); }
-            }
+        for (int i = 0; i < 8; ++i) {
+            if (i >= 4 && !e.out_f32) break;
+            const uint4 q = reinterpret_cast<const uint4*>(from)[i];
+            r.q[4 * i] = q.x; r.q[4 * i + 1] = q.y; r.q[4 * i + 2] = q.z; r.q[4 * i + 3] = q.w;
         }
     } else {
+        // (no condition between the loads; what lies beyond the last row or column is read from there and not used)
+        const int row0 = row - lane;
+        const long long at = col + min(lane, nvalid - 1);
+        if (e.out_f32) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) r[i] = i < nvalid ? load_any(e.res, e.out_f32, at + i) : 0.0f;
+            for (int i = 0; i < 32; ++i) r.q[i] = static_cast<const unsigned*>(e.res)[min(row0 + i, M - 1) * e.res_stride + at];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r.q[i] = static_cast<const unsigned short*>(e.res)[min(row0 + i, M - 1) * e.res_stride + at];
+        }
+    }
+}
+__device__ __forceinline__ void add_residual(const Epilogue& e, Drain& d, const Residual& r, float (&v)[32]) {
+    if (!r.by_row) {
+        if (d.lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+        float* t = reinterpret_cast<float*>(d.tile);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t[i * 32 + (d.lane ^ i)] = __uint_as_float(e.out_f32 ? r.q[i] : r.q[i] << 16);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] += t[d.lane * 32 + (i ^ d.lane)];
+        __syncwarp();
+    } else if (e.out_f32) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(r.q[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { v[2 * i] += bf_lo(r.q[i]); v[2 * i + 1] += bf_hi(r.q[i]); }
     }
 }
 
@@ -562,10 +585,25 @@ linear_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant_
             const CUtensorMap* map_out = &maps.out[which];
             const int width = e.gated ? p.q[which].bn / 2 : p.q[which].bn, M = p.q[which].M;
             bool alive = true;
+            // the tile's bias and first piece of the residual are fetched before its accumulator is waited for
+            float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};      // this lane's column in each of this warp's pieces (gated: gate, up, gate, up)
+            if (e.bias) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int col = n * width + (half + 2 * (e.gated ? k >> 1 : k)) * 32 + lane;
+                    if (half + 2 * (e.gated ? k >> 1 : k) < width / 32 && col < e.N)
+                        bias[k] = load_any(e.bias, !e.bias_bf16, (e.gated && (k & 1) ? e.N : 0) + col);
+                }
+            }
 #pragma unroll 1
             for (int a = 0; a < ACC && alive; ++a) {
             const int row = (2 * (ACC * m + a) + rank) * kTileRows + quarter * 32 + lane;
-            const bool row_ok = row < M;
+            Residual r;
+            auto fetch = [&](int c) {
+                const int col = n * width + c * 32;
+                if (c < width / 32 && col < e.N) fetch_residual(e, row, M, lane, col, min(32, e.N - col), r);
+            };
+            if (e.res) fetch(half);
             int got = 0;
             if (lane == 0) got = long_wait(smem_addr(&ctl->tmem_full[buf]), (tphase >> buf) & 1u, &ctl->abort_flag) ? 1 : 0;
             if (!__shfl_sync(0xffffffffu, got, 0)) {
@@ -580,18 +618,21 @@ linear_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant_
                 if (col >= e.N) break;                     // (warp-uniform)
                 const int nvalid = min(32, e.N - col);
                 uint32_t raw_v[32];
-                float v[32], r[32];
-                if (e.res) load_residual(e, row, row_ok, col, nvalid, r);
+                float v[32];
                 auto take = [&](uint32_t at, int half_of_w) {    // accumulator columns + bias
                     tc_ld32(t_row + at, raw_v);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw_v[i]);
                     const int shift = half_of_w ? e.N : 0;
                     if (e.bias) {
-                        d.bias[lane] = lane < nvalid ? load_any(e.bias, !e.bias_bf16, shift + col + lane) : 0.0f;
+                        const int k = e.gated ? (c & ~1) + half_of_w : c >> 1;
+                        d.bias[lane] = k == 0 ? bias[0] : k == 1 ? bias[1] : k == 2 ? bias[2] : bias[3];
                         __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] += d.bias[i];
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 q = reinterpret_cast<const float4*>(d.bias)[i];
+                            v[4 * i] += q.x; v[4 * i + 1] += q.y; v[4 * i + 2] += q.z; v[4 * i + 3] += q.w;
+                        }
                         __syncwarp();
                     }
                     if (e.pre) store_piece<false>(d, &maps.pre, e.vec_pre, half_of_w, p.mixed, e.pre + shift, e.pre_stride, row - lane, M, col, nvalid, v);
@@ -607,8 +648,8 @@ linear_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant_
                     for (int i = 0; i < 32; ++i) v[i] *= g[i];
                 }
                 if (e.res) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] += r[i];
+                    add_residual(e, d, r, v);
+                    fetch(c + 2);
                 }
                 if (e.out_f32) store_piece<true>(d, map_out, e.vec_out, 0, true, e.out, e.out_stride, row - lane, M, col, nvalid, v);
                 else store_piece<false>(d, map_out, e.vec_out, 0, p.mixed, e.out, e.out_stride, row - lane, M, col, nvalid, v);
