@@ -12,6 +12,7 @@
 // A column gate is a factor of the post norm's sums over tokens, S1 = sum_t [row gate] gh v and S2 = sum_t [row gate] gh, so that
 // the gradients of gate, weight and bias all come from these two (finish kernel).
 #include "norm_rows.cuh"
+#include "row.cuh"
 
 namespace rlf {
 namespace bn {
@@ -201,10 +202,18 @@ block_sums_general_kernel(const BlockParams p, long long rows_per_slice) {
     }
 }
 
+// the same shared-memory float of CTA `rank` of this cluster
+__device__ __forceinline__ float ld_cluster_f32(const float* p, uint32_t rank) {
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
 struct Finish {
     const float* part;
     long long part_stride;
-    int parts, D, want, accumulate;
+    int parts, D, want, accumulate, split;
     const void* w1;
     const void* b1;
     const void* gate;
@@ -216,30 +225,51 @@ struct Finish {
     float* db1;
     float* dgate;                   // [D], nullable
 };
-// partial rows -> gradients, added in a fixed order: a CTA covers 32 columns of the pre (blockIdx.y = 0) or post norm's two
-// sums; warp w adds the partial rows w, w + 32, ... and the 32 sums are added in order.
+// partial rows -> gradients, added in a fixed order: a cluster of `split` CTAs covers 32 columns of the pre (blockIdx.y = 0) or
+// post norm's two sums.  Warp w of all of them adds the partial rows w, w + 32 split, ..., and the 32 sums are added in order,
+// then the CTAs' (with one CTA the many partial rows of narrow rows were this kernel's whole time: backward of 5768 x 128 fp32,
+// 2960 partial rows, 32 us, so 11).
 __global__ void __launch_bounds__(1024)
 block_finish_kernel(const Finish f) {
     __shared__ float acc[2][32][33];
+    __shared__ float total[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int col = blockIdx.x * 32 + lane, first = 2 * blockIdx.y;
+    uint32_t block;
+    asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(block));
+    const int rank = (int)cluster_ctarank(), col0 = (int)block * 32, first = 2 * blockIdx.y, step = 32 * f.split;
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int col = col0 + lane;
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         if (col < f.D && ((f.want >> (first + k)) & 1)) {
             const float* src = f.part + (first + k) * f.part_stride + col;
 #pragma unroll 8
-            for (int r = warp; r < f.parts; r += 32) s[k] += src[(long long)r * f.D];
+            for (int r = rank * 32 + warp; r < f.parts; r += step) s[k] += src[(long long)r * f.D];
         }
         acc[k][warp][lane] = s[k];
     }
     __syncthreads();
-    if (warp != 0 || col >= f.D) return;
-    for (int w = 1; w < 32; ++w) {
-        s[0] += acc[0][w][lane];
-        s[1] += acc[1][w][lane];
+    if (warp == 0) {
+        for (int w = 1; w < 32; ++w) {
+            s[0] += acc[0][w][lane];
+            s[1] += acc[1][w][lane];
+        }
     }
+    if (f.split > 1) {
+        if (warp == 0) {
+            total[0][lane] = s[0];
+            total[1][lane] = s[1];
+        }
+        cluster_sync_all();
+        if (warp == 0 && rank == 0)
+            for (int q = 1; q < f.split; ++q) {
+                s[0] += ld_cluster_f32(&total[0][lane], (uint32_t)q);
+                s[1] += ld_cluster_f32(&total[1][lane], (uint32_t)q);
+            }
+        cluster_sync_all();                                // the others' sums have been read
+    }
+    if (warp != 0 || rank != 0 || col >= f.D) return;
     auto leave = [&](float* d, float v) {
         if (d) d[col] = f.accumulate ? d[col] + v : v;
     };
@@ -263,13 +293,13 @@ block_finish_kernel(const Finish f) {
 // x, whose stride is its own, may sit otherwise (x_shift): they are copied as the aligned chunks that cover them and read by
 // element.
 __host__ __device__ constexpr int shifted_pitch(int D, int esz) { return staged_pitch(D, esz) + 48; }     // (read from 16 before to 32 behind)
-template <typename T, int NV, int R, bool EDGE>
+template <typename T, int NV, int R, bool EDGE, int BUFS = 2>
 struct Stage {
     static constexpr int P = Vec<T>::P, N = Vec<T>::N;
     const BlockParams& p;
     const Rows<T, EDGE> rows;
-    uint4* slots;                   // [2][R][arrays][NV][threads], a slot is its thread's own
-    char* shifted;                  // [2][R] rows of x
+    uint4* slots;                   // [BUFS][R][arrays][NV][threads], a slot is its thread's own
+    char* shifted;                  // [BUFS][R] rows of x
     int arrays, pitch, th, tid;
     bool shift;
     unsigned keep[NV];              // which elements of a vector are the row's
@@ -277,7 +307,7 @@ struct Stage {
         : p(p_), rows(dense, p_.D, p_.T, p_.D, p_.period, R), slots(smem), arrays(arrays_), th(blockDim.x), tid(threadIdx.x) {
         shift = EDGE && p.x_shift;
         pitch = shifted_pitch(p.D, (int)sizeof(T));
-        shifted = reinterpret_cast<char*>(smem + 2 * R * arrays * NV * th);
+        shifted = reinterpret_cast<char*>(smem + BUFS * R * arrays * NV * th);
 #pragma unroll
         for (int i = 0; i < NV; ++i) keep[i] = EDGE ? rows.bits(tid + i * th, p.D) : (1u << N) - 1u;
     }
@@ -312,7 +342,7 @@ struct Stage {
     // Slots that no copy writes (of threads without a vector i, or of a tensor that is not there) hold zeros, so that the
     // arithmetic needs no conditions: under conditions the values carried from pass to pass cost more moves than arithmetic.
     __device__ __forceinline__ void clear(int a, bool all) const {
-        for (int q = 0; q < 2 * R; ++q)
+        for (int q = 0; q < BUFS * R; ++q)
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (all || !mine(i)) *slot(0, q, a, i) = make_uint4(0u, 0u, 0u, 0u);
@@ -466,7 +496,7 @@ block_fwd_kernel(const BlockParams p) {
                 st.copy_x(buf, k, 1, t);
             }
         }
-        cp_async_commit();
+        nm::cp_async_commit();
     };
     long long j0 = st.rows.first;
     fetch(j0, 0);
@@ -592,7 +622,9 @@ block_fwd_kernel(const BlockParams p) {
 // Backward, one row at a time: two sums per row one after the other (the second needs gh, which needs the first); what the later
 // passes need is held in registers, so that each element is unpacked once.  The sums over tokens are added up row after row in
 // registers and leave as one partial row per CTA.
-template <typename T, int NV, bool L, bool EDGE, int MAXT>
+// Rows too long for two buffers (ONE: fp32, wider than 5000 to 6200 columns) take one, and a slot is filled again as soon as it has been read
+// (8949 x 7104 fp32 layer form 277 us; by the general form 1200).
+template <typename T, int NV, bool L, bool EDGE, int MAXT, bool ONE>
 __global__ void __launch_bounds__(MAXT, !L && !EDGE ? 0 : NV * Vec<T>::N <= 16 && MAXT <= 256 ? 512 / MAXT : 1)
 block_bwd_kernel(const BlockParams p) {
     using V = Vec<T>;
@@ -603,7 +635,7 @@ block_bwd_kernel(const BlockParams p) {
     int turn = 0;
     clear_sums(red);
     const bool post = has_norm(p.post), pre = has_norm(p.pre);
-    const Stage<T, NV, 1, EDGE> st(p, smem, pre ? p.h : p.dh, EDGE && p.x_shift ? 3 : 4);
+    const Stage<T, NV, 1, EDGE, ONE ? 1 : 2> st(p, smem, pre ? p.h : p.dh, EDGE && p.x_shift ? 3 : 4);
     const float inv_d = 1.0f / (float)p.D;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     st.clear(0, p.dh == nullptr);
@@ -623,14 +655,19 @@ block_bwd_kernel(const BlockParams p) {
                 st.copy(buf, 0, 1, p.dy, p.D, t);
                 st.copy(buf, 0, 2, p.h, p.D, t);
             }
-            st.copy_x(buf, 0, 3, t);
+            if (!ONE) st.copy_x(buf, 0, 3, t);
         }
-        cp_async_commit();
+        nm::cp_async_commit();
+    };
+    auto fetch_x = [&](long long j) {                   // (ONE)
+        if (j < st.rows.n) st.copy_x(0, 0, 3, st.rows.row(j));
+        nm::cp_async_commit();
     };
     long long j = st.rows.first;
     fetch(j, 0);
+    if constexpr (ONE) fetch_x(j);
     f2 w1[WS ? 1 : NV][P], w2[WS ? 1 : NV][P], sum_dyu[NV][P], sum_ghv[NV][P], sum_dy[L ? NV : 1][P], sum_gh[L ? NV : 1][P];
-    ulonglong2* const w_s = reinterpret_cast<ulonglong2*>(st.shifted + (st.shift ? 2 * st.pitch : 0)) + st.tid;    // [2][NV][P / 2][threads]
+    ulonglong2* const w_s = reinterpret_cast<ulonglong2*>(st.shifted + (st.shift ? (ONE ? 1 : 2) * st.pitch : 0)) + st.tid;    // [2][NV][P / 2][threads]
     if constexpr (WS) {
         f2 w[NV][P];
 #pragma unroll
@@ -666,12 +703,16 @@ block_bwd_kernel(const BlockParams p) {
             sum_dyu[i][e] = sum_ghv[i][e] = 0ull;
             if (L) sum_dy[L ? i : 0][e] = sum_gh[L ? i : 0][e] = 0ull;
         }
-    for (int buf = 0; j < st.rows.n; j += st.rows.step, buf ^= 1) {
+    for (int buf = 0; j < st.rows.n; j += st.rows.step, buf ^= ONE ? 0 : 1) {
         const long long t = st.rows.row(j);
         const float m1 = next[0], r1 = next[1], m2 = next[2], r2 = next[3], gate = next[4];
-        if (st.shift) __syncthreads();
-        fetch(j + st.rows.step, buf ^ 1);
-        cp_async_wait1();
+        if constexpr (ONE) {
+            cp_async_wait0();
+        } else {
+            if (st.shift) __syncthreads();
+            fetch(j + st.rows.step, buf ^ 1);
+            cp_async_wait1();
+        }
         if (st.shift) __syncthreads();
         st.trim(buf);
         auto unit = [&](const f2& v, const f2& c, const f2& r) { return f2_mul(L ? f2_add(v, c) : v, r); };
@@ -704,6 +745,7 @@ block_bwd_kernel(const BlockParams p) {
             s[0] = f2_sum(a);
             if (L) s[K - 1] = f2_sum(b);
         }
+        if constexpr (ONE) fetch(j + st.rows.step, 0);
         if (pre) row_sums<K, W>(s, red, turn);
         float bias_sum = 0.0f;
         {
@@ -745,6 +787,10 @@ block_bwd_kernel(const BlockParams p) {
             s[0] = f2_sum(a);
             if (L) s[K - 1] = f2_sum(b);
         }
+        if constexpr (ONE) {
+            if (st.shift) __syncthreads();              // the row of x has been read by everyone
+            fetch_x(j + st.rows.step);
+        }
         if (post || p.dgate_row) row_sums<K, W>(s, red, turn);
         if (p.dgate_row) {
             if (L && p.b1) {
@@ -770,12 +816,17 @@ block_bwd_kernel(const BlockParams p) {
     auto leave = [&](int which, const f2 (&g)[P], int i) {
         if (!((p.want >> which) & 1) || !st.mine(i)) return;
         float* d = p.part + which * p.part_stride + (long long)blockIdx.x * p.D + (st.tid + i * st.th) * N - st.rows.lead;
+        float v[N];
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-            float lo, hi;
-            f2_split(g[e], lo, hi);
-            if ((st.keep[i] >> (2 * e)) & 1u) d[2 * e] = lo;
-            if ((st.keep[i] >> (2 * e + 1)) & 1u) d[2 * e + 1] = hi;
+        for (int e = 0; e < P; ++e) f2_split(g[e], v[2 * e], v[2 * e + 1]);
+        // whole vectors where rows fill them (as single floats these stores are partial sectors: 8191 x 4096 bf16, layer form: 102 us, so 87)
+        if constexpr (!EDGE) {
+#pragma unroll
+            for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(d + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if ((st.keep[i] >> e) & 1u) d[e] = v[e];
         }
     };
 #pragma unroll
@@ -801,8 +852,8 @@ static long long max_parts(long long T, int D) {
 static long long part_stride(long long parts, int D) { return (parts * D + 63) & ~63ll; }
 static size_t sums_offset(long long T, int D) { return 4 * (size_t)part_stride(max_parts(T, D), D) * sizeof(float); }
 
-// how rows are cut: nv vectors per thread, `threads` threads, `rows` rows at a time, bytes of shared memory
-struct Cut { int nv, threads, rows, smem, max_threads; };
+// how rows are cut: nv vectors per thread, `threads` threads, `rows` rows at a time in each of `buffers`, bytes of shared memory
+struct Cut { int nv, threads, rows, smem, max_threads, buffers; };
 
 // false: no fast form holds the rows (rows shorter than a vector, or longer than 8192 elements).  `arrays` rows are read per
 // row besides a shifted x.  Up to 128 threads of one vector, then of two (fp32: four) vectors each; the backward of long bf16 rows
@@ -821,11 +872,14 @@ static bool pick_cut(bool bf16, bool edge, bool shift, bool fwd, bool full, long
     if (!fwd && bf16 && c->max_threads == 512) return false;
     c->rows = !fwd || c->max_threads == 512 ? 1 : 2;
     while (c->rows > 1 && T < 148ll * 4 * c->rows) c->rows /= 2;      // too few rows to put several on a CTA
-    for (;; c->rows /= 2) {
-        c->smem = 2 * c->rows * (arrays * c->nv * c->threads * 16 + (shift ? shifted_pitch(D, esz) : 0));
+    c->buffers = 2;
+    for (;;) {
+        c->smem = c->buffers * c->rows * (arrays * c->nv * c->threads * 16 + (shift ? shifted_pitch(D, esz) : 0));
         if (!fwd && (full || edge)) c->smem += 2 * c->nv * c->threads * v * 4;         // the weights
         if (c->smem <= (c->rows > 1 ? kSmemLimit / 2 : kSmemLimit)) return true;
-        if (c->rows == 1) return false;
+        if (c->rows > 1) c->rows /= 2;
+        else if (!fwd && c->max_threads == 512 && c->buffers == 2) c->buffers = 1;
+        else return false;
     }
 }
 
@@ -840,7 +894,10 @@ static BlockKernel fwd_form(const Cut& c) {
 template <bool FWD, typename T, int NV, bool L, bool EDGE, int MAXT>
 static BlockKernel form(const Cut& c) {
     if constexpr (FWD) return fwd_form<T, NV, L, EDGE, MAXT>(c);
-    else return block_bwd_kernel<T, NV, L, EDGE, MAXT>;
+    if constexpr (!FWD && MAXT == 512) {
+        if (c.buffers == 1) return block_bwd_kernel<T, NV, L, EDGE, MAXT, true>;
+    }
+    if constexpr (!FWD) return block_bwd_kernel<T, NV, L, EDGE, MAXT, false>;
 }
 template <bool FWD, typename T, bool L, bool EDGE>
 static BlockKernel kernel_form(const Cut& c) {
@@ -912,14 +969,18 @@ static rlf_status check_block(int64_t T, int32_t D, rlf_dtype dt, rlf_dtype w_dt
 
 static rlf_status launch_finish(const Finish& f, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
-    cfg.gridDim = dim3((unsigned)((f.D + 31) / 32), 2);
+    cudaLaunchAttribute at[2];
+    cfg.gridDim = dim3((unsigned)((f.D + 31) / 32 * f.split), 2);
     cfg.blockDim = dim3(1024);
     cfg.stream = s;
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = f.split;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = f.split > 1 ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, block_finish_kernel, f) != cudaSuccess) {
         cudaGetLastError();
         return RLF_ERR_CUDA;
@@ -1076,5 +1137,8 @@ extern "C" rlf_status rlf_block_norm_bwd(const void* grad_y, const void* grad_h,
     f.part = part; f.part_stride = part_stride(parts, D); f.parts = parts; f.D = D; f.want = want; f.accumulate = accumulate;
     f.w1 = p.w1; f.b1 = p.b1; f.gate = gate; f.w_bf16 = p.w_bf16; f.gate_form = gate_form; f.beta = beta;
     f.dw2 = grad_pre_weight; f.db2 = grad_pre_bias; f.dw1 = grad_post_weight; f.db1 = grad_post_bias; f.dgate = col_gate ? grad_gate : nullptr;
+    // CTAs for a column block: while a warp has more than one batch of loads and the GPU has room for them
+    f.split = 1;
+    while (f.split < 8 && parts > 32 * 8 * f.split && (D + 31) / 32 * 2 * f.split * 2 <= 296) f.split *= 2;
     return launch_finish(f, s);
 }

@@ -356,3 +356,11 @@ def test_wrapper_refuses():
         b.rlf_block_norm_fwd(c.x, c.residual, post_kind=b.NORM_NONE, pre_kind=b.NORM_NONE)
     with pytest.raises(b.RlfError):
         b.rlf_block_norm_bwd(c.dy, c.dh, c.x, h, stats, workspace=torch.empty(256, dtype=torch.uint8, device=DEV), **good)
+
+
+@pytest.mark.parametrize("T,D,dt", [(400, 7104, F32), (400, 6001, F32), (350, 8188, F32), (330, 5600, F32), (6000, 72, BF), (6000, 40, F32)])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_long_rows_and_many_partial_rows(T, D, dt, kind):
+    """fp32 rows too long for two buffers, several to a CTA; narrow rows, whose partial sums a cluster of CTAs adds up."""
+    both_ways(T, D, dt, F32, kind, kind, bias=kind == "layer", form="column", alpha=0.75, beta=0.5)
+    both_ways(T, D, dt, dt, kind, kind, form="row", pad=3, seed=1, with_dh=False)
