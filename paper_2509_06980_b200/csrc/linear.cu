@@ -1075,7 +1075,8 @@ linear_few_bwd_kernel(const FewBwd p) {
 }
 
 // partial rows -> sums, in a fixed order: the first `blocks` CTAs cover 32 columns each of one sum, the others of a second (the bias
-// gradient).  Warp w adds the rows w, w + 32, ..., and the 32 sums are added in order.
+// gradient).  Warp w adds the rows w, w + 32, ..., at most 8 of them.
+constexpr int kMostParts = 256;
 struct Join {
     const float* part[2];
     long long width[2];
@@ -1094,15 +1095,19 @@ linear_join_kernel(const Join j) {
     float s = 0.0f;
     if (col < width) {
         const float* part = j.part[which] + col;
-#pragma unroll 8
-        for (int k = warp; k < j.parts; k += 32) s += part[(long long)k * width];
+        float v[8];                                        // (at most 256 parts: all of a warp's loads at once)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = warp + 32 * i < j.parts ? part[(warp + 32 * i) * width] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += v[i];
     }
     acc[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && col < width) {
-        for (int w = 1; w < 32; ++w) s += acc[w][lane];
-        if (j.accumulate) s += load_any(j.out[which], j.out_f32[which], col);
-        store_any(j.out[which], j.out_f32[which], col, s);
+    s = warp_sum(acc[lane][warp]);                         // column `warp` of the block
+    const long long c = col - lane + warp;
+    if (lane == 0 && c < width) {
+        if (j.accumulate) s += load_any(j.out[which], j.out_f32[which], c);
+        store_any(j.out[which], j.out_f32[which], c, s);
     }
 }
 
@@ -1462,11 +1467,11 @@ static bool rows_aligned(const void* at, long long stride, int esz) { return ali
 // slices of tokens of the elementwise passes (each leaves one partial row of a weight or bias gradient; a single one is the gradient)
 static int token_slices(int64_t T) {
     const int64_t n = (T + 31) / 32;
-    return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
+    return (int)(n < 1 ? 1 : n > kMostParts ? kMostParts : n);
 }
 static int few_slices(int64_t T) {
     const int64_t n = (T + 7) / 8;
-    return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
+    return (int)(n < 1 ? 1 : n > kMostParts ? kMostParts : n);
 }
 static long long up8(long long n) { return (n + 7) & ~7ll; }
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
