@@ -37,6 +37,8 @@ using tc::tc_commit2;
 using tc::tc_fence_after;
 using tc::tc_fence_before;
 using tc::tc_ld32;
+using tc::tc_ld32_issue;
+using tc::tc_ld_wait;
 using tc::tc_mma;
 using tc::tc_mma2;
 using tc::tma_load_2d;
@@ -255,12 +257,13 @@ struct PairProblem {
     int a_mn, b_mn;                 // operand stored with the summed axis along its rows
     int group;                      // row units that are taken together (see the raster)
     int up_row;                     // gated: B's row with which the up half begins
+    int wide;                       // results leave 64 columns at a time
     Epilogue e;
 };
 struct PairParams {
     PairProblem q[2];
     long long units0, units;        // tiles of the first product, of both
-    int mixed;                      // an output is fp32: a drain tile is then one store's at a time
+    int mixed;                      // an output is fp32, or leaves 64 columns at a time: a drain tile is then one store's at a time
     int32_t* dev_status;
 };
 struct alignas(64) PairMaps {
@@ -332,6 +335,26 @@ __device__ __forceinline__ void store_piece(Drain& d, const CUtensorMap* map, bo
         for (int r = 0; r < rows; ++r) store_any(out, F32, (long long)(row0 + r) * stride + col + lane, t[r * 32 + (lane ^ r)]);
     }
     __syncwarp();
+}
+// 32 rows of 64 bf16 columns, a whole line each: half the loads, fences and stores that two tiles of 32 columns take.  Where K is
+// short the drain is what a tile takes, and its time is theirs, one after the other (13312 x 128 x 5120 54 -> 47 us).
+__device__ __forceinline__ void store_wide(Drain& d, const CUtensorMap* map, int row0, int M, int col, const uint32_t (&q)[32]) {
+    if (d.lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+    const uint32_t at = smem_addr(d.tile);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                     :: "r"(at + (uint32_t)(d.lane * 128 + ((i ^ (d.lane & 7)) << 4))), "r"(q[4 * i]), "r"(q[4 * i + 1]), "r"(q[4 * i + 2]),
+                        "r"(q[4 * i + 3]) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (d.lane == 0) {
+        if (row0 < M)
+            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                         :: "l"(map), "r"(at), "r"(col), "r"(0), "r"(row0) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
 }
 // A 32 x 32 piece of the residual on its way: 32 columns of this thread's row where rows lie on 16-byte boundaries, else this
 // lane's column of the 32 rows (by row, element after element, a warp touches 32 rows at once: 2047 x 1024 x 4099 91 us, so
@@ -584,15 +607,15 @@ linear_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant_
             const Epilogue& e = p.q[which].e;
             const CUtensorMap* map_out = &maps.out[which];
             const int width = e.gated ? p.q[which].bn / 2 : p.q[which].bn, M = p.q[which].M;
+            const bool wide = p.q[which].wide;
             bool alive = true;
             // the tile's bias and first piece of the residual are fetched before its accumulator is waited for
             float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};      // this lane's column in each of this warp's pieces (gated: gate, up, gate, up)
             if (e.bias) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int col = n * width + (half + 2 * (e.gated ? k >> 1 : k)) * 32 + lane;
-                    if (half + 2 * (e.gated ? k >> 1 : k) < width / 32 && col < e.N)
-                        bias[k] = load_any(e.bias, !e.bias_bf16, (e.gated && (k & 1) ? e.N : 0) + col);
+                    const int c = e.gated ? half + (k & 2) : wide ? 2 * half + (k & 1) + 2 * (k & 2) : half + 2 * k, col = n * width + c * 32 + lane;
+                    if (c < width / 32 && col < e.N) bias[k] = load_any(e.bias, !e.bias_bf16, (e.gated && (k & 1) ? e.N : 0) + col);
                 }
             }
 #pragma unroll 1
@@ -612,6 +635,40 @@ linear_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant_
             }
             tc_fence_after();
             const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)buf * 256u;
+            if (wide) {
+#pragma unroll 1
+                for (int g = half; 2 * g < width / 32; g += 2) {
+                    const int col = n * width + g * 64;
+                    if (col >= e.N) break;
+                    uint32_t lo[32], hi[32];
+                    tc_ld32_issue(t_row + (uint32_t)(g * 64), lo);
+                    tc_ld32_issue(t_row + (uint32_t)(g * 64 + 32), hi);
+                    tc_ld_wait(lo);
+                    tc_ld_wait(hi);
+                    uint32_t packed[32];
+                    auto finish = [&](const uint32_t (&raw)[32], int h) {      // bias and activation; to bf16
+                        float v[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
+                        if (e.bias) {
+                            d.bias[lane] = g == half ? bias[h] : bias[2 + h];
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float4 q = reinterpret_cast<const float4*>(d.bias)[i];
+                                v[4 * i] += q.x; v[4 * i + 1] += q.y; v[4 * i + 2] += q.z; v[4 * i + 3] += q.w;
+                            }
+                            __syncwarp();
+                        }
+                        activate<32>(e.act, v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) packed[16 * h + i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+                    };
+                    finish(lo, 0);
+                    finish(hi, 1);
+                    store_wide(d, map_out, row - lane, M, col, packed);
+                }
+            } else
 #pragma unroll 1
             for (int c = half; c < width / 32; c += 2) {
                 const int col = n * width + c * 32;
@@ -1338,17 +1395,17 @@ static rlf_status launch(const void* kernel, dim3 grid, dim3 threads, int smem, 
     return RLF_OK;
 }
 
-// rows of `halves` x N elements, stored in tiles of 32 x 32
-static bool make_tile_map(CUtensorMap* map, const void* base, long long rows, int N, int halves, long long stride, bool f32) {
+// rows of `halves` x N elements, stored in tiles of 32 rows x 32 columns (bf16 also 64)
+static bool make_tile_map(CUtensorMap* map, const void* base, long long rows, int N, int halves, long long stride, bool f32, int columns) {
     const tc::EncodeTiledFn fn = tc::encode_fn();
     if (!fn) return false;
     const int esz = f32 ? 4 : 2;
     const cuuint64_t dims[3] = {(cuuint64_t)N, (cuuint64_t)halves, (cuuint64_t)rows};
     // (a single half: its stride is never taken)
     const cuuint64_t strides[2] = {(cuuint64_t)(halves > 1 ? N : stride) * esz, (cuuint64_t)stride * esz};
-    const cuuint32_t box[3] = {32, 1, 32}, step[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)columns, 1, 32}, step[3] = {1, 1, 1};
     return fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, columns * esz == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -1398,15 +1455,17 @@ static rlf_status launch_pair(const Product* g, int count, int acc, const int* b
         q.group = panel > 7e6 ? 4 : panel < 1.75e6 ? 16 : (int)(28e6 / panel);
         p.units += (long long)q.m_units * q.n_tiles;
         if (i == 0) p.units0 = p.units;
-        p.mixed |= e.out_f32;
         if (!encode(&maps.a[i], g[i].A, g[i].K, g[i].M, kTileRows) || !encode(&maps.b[i], g[i].B, g[i].K, g[i].rows_b(), bn[i] / 2)) return RLF_ERR_CUDA;
-        // output tiles: 32 columns x one half x 32 rows
+        // results by 64 columns where the drain is longer than the multiplies; a longer K gains nothing, and with a residual or `pre`,
+        // whose pieces are of 32 columns, it loses (8192 x 1024 x 1024 with residual 23 -> 25 us)
+        q.wide = !e.out_f32 && !e.gated && !e.pre && !e.res && e.vec_out && bn[i] >= 128 && q.k_slabs <= 8;
+        p.mixed |= e.out_f32 || q.wide;
         maps.out[i] = maps.a[i];
-        if (e.vec_out && !make_tile_map(&maps.out[i], e.out, g[i].M, e.N, 1, e.out_stride, e.out_f32 != 0)) return RLF_ERR_CUDA;
+        if (e.vec_out && !make_tile_map(&maps.out[i], e.out, g[i].M, e.N, 1, e.out_stride, e.out_f32 != 0, q.wide ? 64 : 32)) return RLF_ERR_CUDA;
     }
     maps.pre = maps.a[0];
     const Epilogue& e = g[0].e;
-    if (e.pre && e.vec_pre && !make_tile_map(&maps.pre, e.pre, g[0].M, e.N, e.gated ? 2 : 1, e.pre_stride, false)) return RLF_ERR_CUDA;
+    if (e.pre && e.vec_pre && !make_tile_map(&maps.pre, e.pre, g[0].M, e.N, e.gated ? 2 : 1, e.pre_stride, false, 32)) return RLF_ERR_CUDA;
     if (count == 1) maps.a[1] = maps.b[1] = maps.out[1] = maps.a[0];
     p.dev_status = dev_status;
     const void* const kernel = acc == 2 ? (const void*)linear_pair_kernel<2> : (const void*)linear_pair_kernel<1>;

@@ -329,3 +329,25 @@ def test_large_values_before_the_activation(N, gated, kind):
     bound = (_act_error(small, kind) + 8 * U) * (1 + small) + 2 * 2.0 ** -8 * np.abs(slope)
     err = np.abs(_f64(gx)[:, :1] - slope)
     assert (err <= 1.01 * bound).all()
+
+
+@pytest.mark.parametrize("form,tile", [(0, 0), (1, 256), (1, 192), (1, 128), (1, 64), (3, 256), (3, 128)])
+@pytest.mark.parametrize("T,D,N", [(700, 72, 328), (1100, 512, 1000), (257, 200, 72)])
+def test_short_sums(form, tile, T, D, N):
+    """Sums short enough that results leave 64 columns at a time (bf16, no `pre`, no residual), ragged in rows and columns; the
+    gradients of a few tokens likewise, bf16 and fp32 ones in one launch too."""
+    b = gc.binding()
+    b.tune_linear(form, tile, 0)
+    try:
+        x, W, bias, _ = _draw(T, D, N, bias=BF)
+        for kind in (b64.NONE, b64.SILU):
+            buf = torch.full((T + 40, N), 7.0, dtype=BF, device=DEV)
+            y, _ = b.rlf_linear_fwd(x, W, bias=bias, act=kind, y_out=buf[:T])
+            check_fwd(y, None, x, W, bias, kind, False, None)
+            assert (buf[T:] == 7).all()
+        both_ways(T, D, N, grad_w=BF)
+        both_ways(T, D, N)
+        both_ways(200, D, N, grad_w=BF)
+        both_ways(200, N // 8 * 8, D)
+    finally:
+        b.tune_linear(0, 0, 0)
