@@ -351,3 +351,17 @@ def test_short_sums(form, tile, T, D, N):
         both_ways(200, N // 8 * 8, D)
     finally:
         b.tune_linear(0, 0, 0)
+
+
+@pytest.mark.parametrize("form", [0, 1, 2, 3])
+@pytest.mark.parametrize("T,N,out,res_pad", [(300, 264, BF, 0), (300, 264, BF, 3), (300, 264, F32, 1), (130, 132, F32, 0), (130, 131, BF, 5), (130, 131, F32, 0)])
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gated"])
+def test_residual_and_output_on_any_boundary(form, T, N, out, res_pad, gated):
+    """The residual's rows on 16-byte boundaries or not, its last columns fewer than a piece; output and `pre` aligned apart from
+    each other."""
+    b = gc.binding()
+    b.tune_linear(form, 0, 0)
+    try:
+        both_ways(T, 200, N, b64.SILU, gated, bias=F32, residual=out, out=out, res_pad=res_pad)
+    finally:
+        b.tune_linear(0, 0, 0)
