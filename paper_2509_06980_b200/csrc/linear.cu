@@ -14,8 +14,8 @@
 //           one launch takes one product or both of a backward pass;
 //   narrow  few rows (decoding, short batches) or few tiles: the operand with the output's columns is streamed in 128-row tiles
 //           as the M side of the multiplies, the few rows are their N side, and K is cut over a cluster whose CTAs add up their
-//           accumulators through distributed shared memory.  Bound by reading the streamed operand (8 x 2560 x 10240 gated, 105 MB:
-//           17 us, 6.1 TB/s).
+//           accumulators through distributed shared memory.  Bound by reading the streamed operand (8 x 2560 x 10240, 52 MB: 13 us;
+//           gated, 105 MB: 21 us; 8 x 4096 x 12288 gated, 201 MB: 34 us, 5.9 TB/s).
 // An output of at most four columns (the values of a critic, a few reward scores) takes no tensor cores: it is bound by
 // reading x, and its sums are plain fp32 ones (8191 x 4096 x 1, 67 MB: 14.7 us, 4.6 TB/s; backward, 134 MB: 28.6).
 #include <atomic>
@@ -1300,16 +1300,24 @@ struct Plan {
 static int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // The form of a product is the one with the least estimated time.  The estimates, in us, are fits to measured sweeps of every form
-// over 40 shapes (worst miss 25 %; the form they choose was within 8 % of the best measured one):
+// over 100 shapes (worst miss 25 %; the form they choose was within 10 % of the best measured one):
 //   pair      5 + waves (slabs t + drain), the drain hidden behind the next tile with one accumulator.  A 64-deep slab takes 0.30 us at
 //             256 columns, 0.20 at 128 and never less than 0.19 (its issue); two accumulators 0.57 for twice the rows, and all of
 //             their drain: 32768 x 10240 x 2560 1093 us against 1156, 32768 x 2560 x 2560 347 against 289.
-//   streamed  6 + waves (slabs t + the cluster's reduction); t is the issue of a slab (0.20 - 0.36) or its bytes at 105 GB/s per SM, shared
-//             by the CTAs on it, and the whole is no less than reading everything once at 6 TB/s (ties go to the shorter work).
+//   streamed  3.5 + waves (2.5 + slabs t + the cluster's reduction); t is the issue of a slab (0.20 - 0.36) or its bytes at 105 GB/s per SM, shared
+//             by the CTAs on it, and the whole is no less than 5 + reading everything once at 6.7 TB/s (ties go to the shorter work).
+static double pair_slab(int bn, long long M, int unit) {
+    const double slab = bn == 256 ? 0.30 : bn == 192 ? 0.235 : bn == 128 ? 0.20 : 0.19;
+    if (M > unit) return slab;
+    // a single row unit: all of B comes from HBM, each slab for one pair (100 x 2560 x 10240 gated 0.28 at 192 columns, 0.33 at 256), and a
+    // handful of rows are a few lines that every pair asks for (8 x 4096 x 12288 gated 0.49)
+    const double alone = (0.13 + bn * 0.00088) * (M <= 16 ? 2.0 : 1.0);
+    return slab > alone ? slab : alone;
+}
 static double pair_cost(int acc, int bn, long long M, int N, int k_slabs, bool gated, int pairs) {
     const long long units = (long long)div_up(M, 256 * acc) * div_up(N, gated ? bn / 2 : bn);
     const double waves = (double)((units + pairs - 1) / pairs), drain = 1.5 + 0.6 * bn / 256.0;
-    const double slab = bn == 256 ? 0.30 : bn == 192 ? 0.235 : bn == 128 ? 0.20 : 0.19;
+    const double slab = pair_slab(bn, M, 256 * acc);
     if (acc == 1) {
         const double tile = k_slabs * slab;
         return 5.0 + waves * (tile > drain ? tile : drain) + drain;
@@ -1319,7 +1327,7 @@ static double pair_cost(int acc, int bn, long long M, int N, int k_slabs, bool g
 // SMs that clusters of `split` CTAs can use at one CTA each: a cluster lies in one GPC, whose SMs are no multiple of it
 // (5 x 1640 x 2104 in 17 clusters of 8 that filled an SM each: 11.9 us, with room for two on an SM 6.7).
 static int cluster_slots(int split, int sms) { return split >= 8 ? sms * 13 / 16 : split >= 4 ? sms * 15 / 16 : sms; }
-static int narrow_ctas_per_sm(int nn) { return nn <= 32 ? 4 : nn == 64 ? 3 : nn == 128 ? 2 : 1; }
+static int narrow_ctas_per_sm(int nn) { return nn <= 16 ? 4 : nn <= 64 ? 3 : nn == 128 ? 2 : 1; }      // (with three stages at least)
 static double narrow_cost(int nn, int split, long long M, int N, int k_slabs, bool gated, int sms) {
     const int rows = gated ? 2 * N : N;
     const long long tiles = (long long)div_up(N, gated ? 64 : 128) * div_up(M, nn), ctas = tiles * split;
@@ -1328,8 +1336,8 @@ static double narrow_cost(int nn, int split, long long M, int N, int k_slabs, bo
     const double per_sm = ctas > (long long)most * slots ? most : (double)div_up(ctas, slots);
     const double issue = nn <= 32 ? 0.20 : nn == 64 ? 0.215 : nn == 128 ? 0.24 : 0.36, bytes = per_sm * (16384.0 + 128.0 * nn) / 105e3;
     const double reduce = 1.0 + nn * 32.0 / (split * (double)kNarrowThreads) * 0.25;
-    const double t = 6.0 + waves * (k_slabs / (double)split * (issue > bytes ? issue : bytes) + reduce);
-    const double read = 6.0 + 128.0 * k_slabs * ((double)rows + (double)M) / 6e6;
+    const double t = 3.5 + waves * (2.5 + k_slabs / (double)split * (issue > bytes ? issue : bytes) + reduce);
+    const double read = 5.0 + 128.0 * k_slabs * ((double)rows + (double)M) / 6.7e6;
     return (t > read ? t : read) + 0.05 * t;
 }
 static bool wanted_bn(int bn, bool b_mn, int tile) {
@@ -1504,9 +1512,9 @@ static rlf_status both_products(const Product& first, const Product& second, int
                 if (!wanted_bn(b0, g0.B.mn, tile) || !wanted_bn(b1, g1.B.mn, tile)) continue;
                 double all = 0.0, longest = 0.0, drain = 0.0;
                 const Product* const g[2] = {&g0, &g1};
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < 2; ++i) {              // (a single row unit's stream is hidden by the other product)
                     const int b = i ? b1 : b0;
-                    const double d = 1.5 + 0.6 * b / 256.0, slabs = g[i]->k_slabs() * (b == 256 ? 0.30 : b == 192 ? 0.235 : b == 128 ? 0.20 : 0.19);
+                    const double d = 1.5 + 0.6 * b / 256.0, slabs = g[i]->k_slabs() * pair_slab(b, 1 << 30, 256);
                     const double t = slabs > d ? slabs : d;
                     all += t * div_up(g[i]->M, 256) * (double)div_up(g[i]->e.N, b);
                     longest = t > longest ? t : longest;
