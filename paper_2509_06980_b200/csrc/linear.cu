@@ -1545,14 +1545,23 @@ static int few_slices(int64_t T) {
 }
 static long long up8(long long n) { return (n + 7) & ~7ll; }
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
-struct BwdWs { size_t gz, part_b, part_w, total; };
+// gz, partial rows of grad_bias, partial rows of grad_W, one behind the other
+struct BwdWs {
+    size_t gz, part_b, part_w, total;
+    bool holds(size_t gz_bytes, size_t b_bytes, size_t w_bytes) const {
+        return gz_bytes <= part_b - gz && b_bytes <= part_w - part_b && w_bytes <= total - part_w;
+    }
+};
+// The size is asked for by the rows of W.  Up to four of them may be those of a plain layer with as many outputs, which needs partial rows of
+// grad_W and no gz, or, an even number, of a gated layer with half as many, which needs gz like any other: there is room for either.
 static BwdWs bwd_workspace(int64_t T, int32_t rows, int32_t D) {
     BwdWs w;
     size_t o = 0;
-    const size_t slices = (size_t)(rows <= kFewOutputs ? few_slices(T) : token_slices(T));
-    w.gz = o;     o += rows <= kFewOutputs ? 0 : up256((size_t)T * (size_t)up8(rows) * 2);
+    const bool few = rows <= kFewOutputs;
+    const size_t slices = (size_t)(few ? few_slices(T) : token_slices(T));         // (few: the more of the two)
+    w.gz = o;     o += few && rows % 2 != 0 ? 0 : up256((size_t)T * (size_t)up8(rows) * 2);
     w.part_b = o; o += up256(slices * (size_t)rows * 4);
-    w.part_w = o; o += rows <= kFewOutputs ? up256(slices * (size_t)rows * (size_t)D * 4) : 0;
+    w.part_w = o; o += few ? up256(slices * (size_t)rows * (size_t)D * 4) : 0;
     w.total = o;
     return w;
 }
@@ -1704,6 +1713,7 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
         if (parts < 1) parts = 1;
         p.rows = (T + parts - 1) / parts;
         parts = div_up(T, p.rows);
+        if (!ws.holds(0, p.part_b ? (size_t)parts * N * 4 : 0, p.part_w ? (size_t)parts * N * (size_t)D * 4 : 0)) return RLF_ERR_WORKSPACE;
         void* args[] = {&p};
         st = launch(few_bwd_kernel(N), dim3((unsigned)columns, (unsigned)parts), dim3(nx, 256 / nx), 0, 1, args, s);
         if (st != RLF_OK) return st;
@@ -1714,6 +1724,7 @@ extern "C" rlf_status rlf_linear_bwd(const void* grad_y, rlf_dtype grad_y_dt, in
     const bool in_place = !need_pre && grad_y_dt == RLF_BF16 && rows_aligned(grad_y, grad_y_stride, 2);
     Operand gz = {grad_y, grad_y_stride, 0};
     if (!in_place) gz = {base + ws.gz, up8(rows), 0};
+    if (!ws.holds(in_place ? 0 : (size_t)T * (size_t)up8(rows) * 2, (size_t)used * rows * 4, 0)) return RLF_ERR_WORKSPACE;
     if ((!in_place && (grad_x || grad_W)) || grad_bias) {
         PreGrad p = {};
         p.dy = grad_y; p.dy_stride = grad_y_stride; p.dy_f32 = grad_y_dt == RLF_F32; p.act = act; p.gated = gated;
