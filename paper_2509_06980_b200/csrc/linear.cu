@@ -969,10 +969,12 @@ linear_narrow_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_con
 }
 
 // ---- at most four outputs ------------------------------------------------------------------------
-// Forward: a warp takes R tokens; its lanes run along the row, 16 bytes of x and of each weight row at a time.
+// Forward: a warp takes R tokens; its lanes run along the row, 16 bytes of x and of each weight row at a time.  (No __restrict__ on what is
+// read: it lets loads take the path for data that nothing writes while the kernel runs, and the launch before, under which this one
+// is set up, may be writing x.)
 template <int N, int R>
 __global__ void __launch_bounds__(256)
-linear_few_fwd_kernel(const __nv_bfloat16* __restrict__ x, long long x_stride, const __nv_bfloat16* __restrict__ W, long long T, int D, const Epilogue e) {
+linear_few_fwd_kernel(const __nv_bfloat16* x, long long x_stride, const __nv_bfloat16* W, long long T, int D, const Epilogue e) {
     pdl_start();
     pdl_wait();
     const int lane = threadIdx.x & 31;
