@@ -7,8 +7,8 @@
 //   with s = beta gate:   dx = r1 (g - [layer] mean(g) - v mean(g v)),  g = s gh w_post   (no norm: dx = s gh)
 //   dw_pre = sum_t dy u,  db_pre = sum_t dy,  dw_post = sum_t s gh v,  db_post = sum_t s gh,  dgate = beta sum gh n  (over t, or the row)
 //
-// Bound by HBM: forward reads two rows and writes two, backward reads four and writes two (32768 x 2560 bf16 RMS: 107 us, 6.2 TB/s, and
-// 160 us, 6.3; the layer forms with biases by latency, 8191 x 4096: 55 us, 4.9 TB/s, and 87, 4.6).  Statistics and sums are fp32 and no
+// Bound by HBM: forward reads two rows and writes two, backward reads four and writes two (32768 x 2560 bf16 RMS: 108 us, 6.2 TB/s, and
+// 162 us, 6.2; as calls 109 - 113 and 168 - 175; the layer forms with biases by latency, 8191 x 4096: 55 us, 4.9 TB/s, and 88, 4.6).  Statistics and sums are fp32 and no
 // intermediate is rounded: y comes from the unrounded h, dx from the unrounded gh.
 // A column gate is a factor of the post norm's sums over tokens, S1 = sum_t [row gate] gh v and S2 = sum_t [row gate] gh, so that
 // the gradients of gate, weight and bias all come from these two (finish kernel).
@@ -63,7 +63,9 @@ __device__ __forceinline__ float row_gate(const BlockParams& p, long long t) {
 constexpr int kGenThreads = 256;
 constexpr int kSmemLimit = 200 * 1024;           // most dynamic shared memory that a fast form asks for
 
-// ---- any width, stride and alignment: one CTA per row, the row read once per pass (later passes are served by L2) ----------
+// ---- any width, stride and alignment: one CTA per row, the row read once per pass (later passes are served by L2): rows shorter than a
+// vector, longer than 8192 elements, or of tensors that sit apart in their vectors (4096 x 16384 bf16 470 us forward, 1021 backward, where
+// the bytes are 82 and 123) --------
 template <typename T>
 __global__ void __launch_bounds__(kGenThreads)
 block_fwd_general_kernel(const BlockParams p) {

@@ -10,14 +10,16 @@
 // and one epilogue serves them: out = act(acc + bias) + residual (accumulation into dW is a residual that is the output itself).
 // Two kernels share it:
 //   pair    large products: a persistent pair of CTAs multiplies 256 x 256 tiles (tcgen05 cta_group::2), bound by the tensor cores (32768 x
-//           10240 x 2560 1.1 - 1.3 ms, 0.95 of the rate that the power cap sustains) or, where k is short, by draining the results;
+//           10240 x 2560 1.1 ms for a single call, 1.2 - 1.4 one after the other: 0.90 - 0.95 of the rate that the power cap sustains) or,
+//           where k is short, by draining the results;
 //           one launch takes one product or both of a backward pass;
 //   narrow  few rows (decoding, short batches) or few tiles: the operand with the output's columns is streamed in 128-row tiles
 //           as the M side of the multiplies, the few rows are their N side, and K is cut over a cluster whose CTAs add up their
-//           accumulators through distributed shared memory.  Bound by reading the streamed operand (8 x 2560 x 10240, 52 MB: 13 us;
-//           gated, 105 MB: 21 us; 8 x 4096 x 12288 gated, 201 MB: 34 us, 5.9 TB/s).
+//           accumulators through distributed shared memory.  Bound by reading the streamed operand (8 x 2560 x 10240, 52 MB: 12 - 13 us;
+//           gated, 105 MB: 21 us; 8 x 4096 x 12288 gated, 201 MB: 34 - 36 us, 5.6 - 5.9 TB/s).
 // An output of at most four columns (the values of a critic, a few reward scores) takes no tensor cores: it is bound by
-// reading x, and its sums are plain fp32 ones (8191 x 4096 x 1, 67 MB: 14.7 us, 4.6 TB/s; backward, 134 MB: 28.6).
+// reading x, and its sums are plain fp32 ones (8191 x 4096 x 1, 67 MB: 14.6 - 15.1 us, 4.6 TB/s; backward, 134 MB: 26 on the GPU, 29 - 30 a
+// call).  A gated layer of one or two outputs is no such head: it takes the products above.
 #include <atomic>
 
 #include "row.cuh"
@@ -1301,8 +1303,10 @@ struct Plan {
 };
 static int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// The form of a product is the one with the least estimated time.  The estimates, in us, are fits to measured sweeps of every form
-// over 100 shapes (worst miss 25 %; the form they choose was within 10 % of the best measured one):
+// The form of a product is the one with the least estimated time.  The estimates, in us, are fits to sweeps of every form over 100 shapes
+// on one B200 (worst miss 25 %).  On 75 others (1 to 32768 tokens, widths of 128 to 14336, gated and not) the form they choose is within
+// 5 % of the fastest one 53 times, within 10 % 63 times and within 20 % 72 times; what is further off are launches of 4 to 13 us (2 x 256 x
+// 3328 4.7 us, 3.6 without a cluster; 43 x 576 x 576 5.7, 4.4; 862 x 3008 x 192 gated 13.3, 10.8):
 //   pair      5 + waves (slabs t + drain), the drain hidden behind the next tile with one accumulator.  A 64-deep slab takes 0.30 us at
 //             256 columns, 0.20 at 128 and never less than 0.19 (its issue); two accumulators 0.57 for twice the rows, and all of
 //             their drain: 32768 x 10240 x 2560 1093 us against 1156, 32768 x 2560 x 2560 347 against 289.
